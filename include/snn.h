@@ -489,6 +489,79 @@ snn_status snn_conv_dense_dw(const float* trace_in, const float* V, const float*
                              int C, int F, float theta, float b_th, float beta, float* dWc, void* workspace,
                              size_t workspace_bytes, void* stream);
 
+/*
+ * Operators on rows of logits: a teacher's record, distillation from it, and drawing a class. A row is one answer of
+ * a network; the membrane V_out [T,B,C] of the readout is R = T*B rows r = t*B + b of C classes.
+ *   logits   R rows of C values of type `dtype`; row r begins at element r*ld, ld >= C (rows may lie in wider ones).
+ *            The address needs the alignment of its type only; 16-byte aligned rows are read fastest.
+ * R up to 2^31 - 1, C up to 2^20, K up to 1024 classes in a record; larger: SNN_ERR_UNSUPPORTED. SNN_ERR_INVALID_ARG
+ * also for an unknown dtype, ld < C, an address that is no multiple of the type's size, K > C, and a tau that is not
+ * positive and finite. Offsets are formed in 64 bits. All results are deterministic.
+ */
+typedef enum { SNN_F32 = 0, SNN_BF16 = 1, SNN_F16 = 2 } snn_dtype;
+
+/*
+ * A teacher's record: the K largest logits of every row.
+ *   ids      int32 [R,K] (written): their classes, the largest logit first, equal ones by class
+ *   vals     float32 [R,K] (written): their logits, not divided by tau
+ *   lse      float32 [R] (written unless NULL): log sum_j exp(z_j / tau) over all C classes, so that a listed class has
+ *            the probability exp(val / tau - lse); -inf for a row of -inf, +inf for one that holds +inf
+ * NaN counts as -inf, and -inf is not listed: a row with fewer than K others ends in ids -1, vals -inf.
+ */
+snn_status snn_readout_top(const void* logits, int dtype, int64_t R, int C, int64_t ld, int K, float tau, int32_t* ids,
+                           float* vals, float* lse, void* stream);
+
+/*
+ * Distillation loss of a student's rows against a teacher's records at temperature tau, and its gradient.
+ *   logits   the student's, z
+ *   ids, vals  [R,K] as snn_readout_top writes them; an id outside [0,C) is no entry. No class twice in a row (its
+ *            results are then unspecified).
+ *   lse      float32 [R] of the records at this tau, or NULL. With it p_k = exp(vals_k / tau - lse) and
+ *            p_t = max(0, 1 - sum_k p_k) is the teacher's probability of all classes not listed (0 where all C are);
+ *            without it p = softmax(vals / tau) over the row's entries and p_t = 0.
+ *   With q = softmax(z / tau) over all classes and q_t its sum over those not listed
+ *     L_r = sum_k p_k (log p_k - log q_k) + p_t (log p_t - log q_t), terms with p = 0 being 0
+ *   weight   float32 [R], or NULL for 1/R each. A row of weight 0 is not read: its L_r is 0 and its gradient 0.
+ *   loss     float32 [1] (written): sum_r weight_r L_r, summed in float64
+ *   row_loss float32 [R] (written unless NULL): L_r
+ *   grad     rows of dtype, row r at r*ld_grad (written unless NULL; the loss alone then): weight_r dL_r / dz,
+ *              (mass q_j - p_j) / tau for a listed class, (mass q_t - p_t) (q_j / q_t) / tau for another,
+ *              mass = sum_k p_k + p_t
+ *            computed in float32 and rounded once. Elements between C and ld_grad are not touched. It may
+ *            not overlap the inputs.
+ *   accumulate  nonzero: grad += instead (rows of weight 0 stay as they are)
+ * A row without entries (all ids -1) and without lse has L_r = 0 and gradient 0. Logits of -inf are classes the student
+ * cannot give: q = 0 there, and L_r = +inf where the teacher's probability is not 0. A NaN or +inf logit makes the
+ * row's loss and gradient NaN. A factor tau^2, which some give this loss, is the caller's to put into weight.
+ */
+size_t snn_readout_distill_workspace(int64_t R, int C, int dtype);
+snn_status snn_readout_distill(const void* logits, int dtype, int64_t R, int C, int64_t ld, const int32_t* ids,
+                               const float* vals, const float* lse, int K, float tau, const float* weight, float* loss,
+                               float* row_loss, void* grad, int64_t ld_grad, int accumulate, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/*
+ * Draws one class per row. The settings are device arrays, one value a row; a NULL one leaves its filter out.
+ *   u           float32 [R] uniform numbers in [0,1) (values outside are taken as the nearest end)
+ *   temperature float32 [R]; NULL: 1. Not above 0 (or NaN): the first of the largest logits.
+ *   top_k       int32 [R]; <= 0: all classes
+ *   top_p       float32 [R]; >= 1: all, <= 0 or NaN: one class
+ *   min_p       float32 [R]; <= 0 or NaN: all, above 1 as 1
+ * With m the row's largest logit, e_j = exp((z_j - m) / temperature) (formed in float32 as (z_j - m) * (1/temperature))
+ * and the integer weight n_j = round(2^31 e_j): of the classes in the order by logit, largest first, equal ones by
+ * class, the first top_k are kept; of these the shortest prefix whose weights reach ceil(top_p * their sum); of these
+ * the classes with e_j >= min_p. The class drawn is the first, in the order of the classes, at which the sum of the kept weights
+ * exceeds floor(u * the sum of all kept). Sums of integers are exact, so the answer depends on no order of summation.
+ * A class of less than 2^-32 of the largest one's probability has weight 0 and is never drawn.
+ *   cls      int32 [R] (written): the class, -1 for a row of nothing but -inf
+ *   logp     float32 [R] (written unless NULL): log of its probability among the kept classes, -inf for a row without
+ *   kept     int32 [R] (written unless NULL): the number of classes kept that can be drawn
+ * NaN counts as -inf; of logits of +inf each has weight 2^31 and all others 0.
+ */
+snn_status snn_readout_sample(const void* logits, int dtype, int64_t R, int C, int64_t ld, const float* u,
+                              const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                              int32_t* cls, float* logp, int32_t* kept, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,6 +28,9 @@ SOURCES = [
     "gemm.hip",
     "dense_backward.hip",
     "readout_ce.hip",
+    "readout_top.hip",
+    "readout_distill.hip",
+    "readout_sample.hip",
     "train_step.hip",
     "conv_layer.hip",
 ]

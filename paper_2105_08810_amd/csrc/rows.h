@@ -1,0 +1,353 @@
+// Rows of logits: what the readout's operators on single rows share (internal header). A row is C values in float32,
+// bfloat16 or float16 at any address its type allows; it is walked in 16-byte vectors of the aligned address below
+// it, and only vectors that lie wholly inside the row are loaded as such.
+#pragma once
+
+#include "common.h"
+
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+
+namespace snn {
+namespace rows {
+
+constexpr int kMaxClasses = 1 << 20;  // a row's weights of at most 2^31 sum below 2^53
+constexpr int kMaxListed = 1024;      // listed classes of a teacher's record
+
+struct Bf16 {
+  uint16_t bits;
+};
+struct F16 {
+  uint16_t bits;
+};
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(Bf16 x) { return __uint_as_float((uint32_t)x.bits << 16); }
+__device__ __forceinline__ float to_float(F16 x) { return (float)__builtin_bit_cast(_Float16, x.bits); }
+template <class T>
+__device__ __forceinline__ T from_float(float x);
+template <>
+__device__ __forceinline__ float from_float<float>(float x) {
+  return x;
+}
+template <>
+__device__ __forceinline__ Bf16 from_float<Bf16>(float x) {  // to nearest, ties to even
+  return Bf16{__builtin_bit_cast(uint16_t, (__bf16)x)};
+}
+template <>
+__device__ __forceinline__ F16 from_float<F16>(float x) {
+  return F16{__builtin_bit_cast(uint16_t, (_Float16)x)};
+}
+
+template <class T>
+struct Row {
+  static constexpr int kVec = 16 / (int)sizeof(T);
+  const T* base;  // the row's address rounded down to 16 bytes
+  int lead;       // elements between base and the row
+  int C;
+  int Q;          // vectors that hold a part of the row
+
+  __device__ __forceinline__ Row(const void* logits, int64_t r, int64_t ld, int C_) : C(C_) {
+    const T* p = static_cast<const T*>(logits) + r * ld;
+    lead = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+    base = p - lead;
+    Q = (lead + C + kVec - 1) / kVec;
+  }
+  __device__ __forceinline__ int first(int q) const { return q * kVec - lead; }  // class of vector q's first element
+  __device__ __forceinline__ bool whole(int q) const { return first(q) >= 0 && first(q) + kVec <= C; }
+  __device__ __forceinline__ float at(int j) const { return to_float(base[lead + j]); }
+  // Vector q, -inf outside the row.
+  __device__ __forceinline__ void load(int q, float (&x)[kVec]) const {
+    if (whole(q)) {
+      T v[kVec];
+      __builtin_memcpy(v, __builtin_assume_aligned(base + (size_t)q * kVec, 16), 16);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) x[i] = to_float(v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const int j = first(q) + i;
+        x[i] = j >= 0 && j < C ? at(j) : -INFINITY;
+      }
+    }
+  }
+};
+
+// NaN as -inf: a class that is never listed or drawn.
+__device__ __forceinline__ float no_nan(float x) { return x == x ? x : -INFINITY; }
+
+// Integers in the order of the values; -0 and +0 are one.
+__device__ __forceinline__ uint32_t key_of(float x) {
+  const uint32_t b = __float_as_uint(x + 0.0f);
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float of_key(uint32_t k) {
+  return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+
+__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int off) { return __shfl_up((unsigned long long)v, off, kWave); }
+
+// Block reductions and scans; every thread of the block takes part and gets the result. `red` holds NT / kWave
+// values in LDS and may be reused at once.
+template <int NT, class V, class F>
+__device__ __forceinline__ V block_reduce(V v, F f, V* red) {
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) v = f(v, __shfl_xor(v, off, kWave));
+  if (NT == kWave) return v;
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
+  __syncthreads();
+  V r = red[0];
+#pragma unroll
+  for (int k = 1; k < NT / kWave; ++k) r = f(r, red[k]);
+  return r;
+}
+
+template <int NT>
+__device__ __forceinline__ uint64_t block_exclusive(uint64_t v, uint64_t* red, uint64_t& total) {
+  uint64_t incl = v;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const uint64_t u = shfl_up64(incl, off);
+    if ((int)(threadIdx.x % kWave) >= off) incl += u;
+  }
+  __syncthreads();
+  if (threadIdx.x % kWave == kWave - 1) red[threadIdx.x / kWave] = incl;
+  __syncthreads();
+  uint64_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int k = 0; k < NT / kWave; ++k) {
+    before += k < (int)(threadIdx.x / kWave) ? red[k] : 0;
+    total += red[k];
+  }
+  return before + incl - v;
+}
+
+// ------------------------------------------------------------------ selection
+//
+// The order of a row's classes is by value, largest first, equal values by class. A cut is the first place of the
+// order at which the sum of the weights so far reaches a limit; the weights are integers, so that no order of
+// summation changes it. It is found by value: a histogram of the keys in range over kBins equal parts, whose part
+// with the limit becomes the next range, until it holds few elements (each then sums what is above it) or one value.
+
+constexpr int kBins = 1024;
+constexpr int kShort = 512;  // elements compared with one another
+
+template <int NT>
+struct SelectLds {
+  uint64_t mass[kBins];
+  uint32_t count[kBins];
+  uint32_t list[kShort];
+  uint64_t red[NT / kWave];
+  uint64_t before_mass, part_mass;
+  uint32_t before_count, part_count, part, n_list;
+  uint32_t cut_key, cut_equal;
+};
+
+struct Cut {
+  uint32_t key;          // value at the cut
+  uint64_t above_mass;   // weights and number of the elements before it with a larger value
+  uint32_t above_count;
+  uint32_t equal;        // elements of that value
+};
+
+// weigh(x) gives an element's weight, 0 for one that is not in the order. BY_MASS: limit is a sum of weights, else a
+// number of elements. The keys of the elements lie in [lo, hi] and their sum or number reaches the limit >= 1.
+template <class T, int NT, bool BY_MASS, class W>
+__device__ __forceinline__ Cut find_cut(const Row<T>& row, W weigh, uint32_t lo, uint32_t hi, uint64_t limit,
+                                        SelectLds<NT>& s) {
+  constexpr int kVec = Row<T>::kVec;
+  const int tid = threadIdx.x;
+  uint64_t above_mass = 0;
+  uint32_t above_count = 0;
+  for (;;) {
+    int shift = 0;
+    while (((hi - lo) >> shift) >= kBins) ++shift;
+    __syncthreads();
+    for (int b = tid; b < kBins; b += NT) {
+      s.mass[b] = 0;
+      s.count[b] = 0;
+    }
+    if (tid == 0) s.n_list = 0;
+    __syncthreads();
+    for (int q = tid; q < row.Q; q += NT) {
+      float x[kVec];
+      row.load(q, x);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const float y = no_nan(x[i]);
+        const uint32_t k = key_of(y);
+        const uint32_t w = k >= lo && k <= hi ? weigh(y) : 0;
+        if (w) {
+          const uint32_t b = (hi - k) >> shift;
+          atomicAdd(&s.count[b], 1u);
+          if (BY_MASS) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)w);
+        }
+      }
+    }
+    __syncthreads();
+    constexpr int kEach = kBins / NT;
+    uint64_t m = 0, n = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      m += s.mass[tid * kEach + i];
+      n += s.count[tid * kEach + i];
+    }
+    uint64_t all;
+    n = above_count + block_exclusive<NT>(n, s.red, all);
+    m = BY_MASS ? above_mass + block_exclusive<NT>(m, s.red, all) : 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const uint32_t c = s.count[tid * kEach + i];
+      const uint64_t w = s.mass[tid * kEach + i];
+      const uint64_t at = BY_MASS ? m : n, to = BY_MASS ? m + w : n + c;
+      if (at < limit && to >= limit) {
+        s.part = tid * kEach + i;
+        s.part_count = c;
+        s.part_mass = w;
+        s.before_count = (uint32_t)n;
+        s.before_mass = m;
+      }
+      n += c;
+      m += w;
+    }
+    __syncthreads();
+    above_count = s.before_count;
+    above_mass = s.before_mass;
+    hi -= s.part << shift;
+    const uint32_t width = (1u << shift) - 1;
+    lo = hi - lo > width ? hi - width : lo;
+    if (lo == hi) return Cut{hi, above_mass, above_count, s.part_count};
+    if (s.part_count <= kShort) break;
+  }
+  for (int q = tid; q < row.Q; q += NT) {
+    float x[kVec];
+    row.load(q, x);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      const float y = no_nan(x[i]);
+      const uint32_t k = key_of(y);
+      if (k >= lo && k <= hi && weigh(y)) s.list[atomicAdd(&s.n_list, 1u)] = k;
+    }
+  }
+  __syncthreads();
+  const int n = (int)s.n_list;
+  for (int e = tid; e < n; e += NT) {
+    const uint32_t k = s.list[e];
+    uint64_t m = above_mass;
+    uint32_t c = above_count, equal = 0;
+    for (int o = 0; o < n; ++o) {
+      const uint32_t ko = s.list[o];
+      if (ko > k) {
+        ++c;
+        if (BY_MASS) m += weigh(of_key(ko));
+      }
+      equal += ko == k;
+    }
+    const uint64_t at = BY_MASS ? m : c, to = BY_MASS ? m + (uint64_t)equal * weigh(of_key(k)) : (uint64_t)c + equal;
+    if (at < limit && to >= limit) {  // every element of the value says the same
+      s.cut_key = k;
+      s.cut_equal = equal;
+      s.before_count = c;
+      s.before_mass = m;
+    }
+  }
+  __syncthreads();
+  return Cut{s.cut_key, s.before_mass, s.before_count, s.cut_equal};
+}
+
+// The first class whose sum of f over the classes up to it exceeds `target`, which the whole row's sum does.
+// f(x, class) is a weight. The range of vectors is divided among the block's waves until one wave's share is a vector
+// for each lane.
+template <class T, int NT, class F>
+__device__ __forceinline__ int find_in_order(const Row<T>& row, F f, uint64_t target, uint64_t* red) {
+  constexpr int kVec = Row<T>::kVec;
+  constexpr int kWaves = NT / kWave;
+  const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
+  auto sum_of = [&](int q) {
+    float x[kVec];
+    row.load(q, x);
+    uint64_t v = 0;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      const int j = row.first(q) + i;
+      if (j >= 0 && j < row.C) v += f(no_nan(x[i]), j);
+    }
+    return v;
+  };
+  int lo = 0, hi = row.Q;
+  while (hi - lo > kWave) {
+    int share = (hi - lo + kWaves - 1) / kWaves;
+    share = kWaves == 1 ? kWave : share;
+    int pick = -1;
+    for (int from = lo; from < hi && pick < 0; from += share * kWaves) {
+      const int a = from + w * share, b = min(hi, a + share);
+      uint64_t v = 0;
+      for (int q = a + l; q < b; q += kWave) v += sum_of(q);
+#pragma unroll
+      for (int off = kWave / 2; off > 0; off >>= 1) v += __shfl_xor((unsigned long long)v, off, kWave);
+      __syncthreads();
+      if (l == 0) red[w] = v;
+      __syncthreads();
+      for (int k = 0; k < kWaves; ++k) {
+        const uint64_t r = red[k];
+        if (target < r) {
+          pick = from + k * share;
+          break;
+        }
+        target -= r;
+      }
+    }
+    lo = pick;
+    hi = min(hi, lo + share);
+  }
+  // every wave does the last step
+  uint64_t v = lo + l < hi ? sum_of(lo + l) : 0, incl = v;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const uint64_t u = shfl_up64(incl, off);
+    if (l >= off) incl += u;
+  }
+  const int lane = (int)__builtin_ctzll(__ballot(incl > target));
+  target -= __shfl((unsigned long long)(incl - v), lane, kWave);
+  const int q = lo + lane;
+  float x[kVec];
+  row.load(q, x);
+  int found = -1;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const int j = row.first(q) + i;
+    if (found < 0 && j >= 0 && j < row.C) {
+      const uint64_t u = f(no_nan(x[i]), j);
+      if (target < u) found = j;
+      else target -= u;
+    }
+  }
+  return found;
+}
+
+// Runs f.template run<T>() for the type that dtype names.
+template <class F>
+inline snn_status for_type(int dtype, F f) {
+  switch (dtype) {
+    case SNN_F32: return f(float{});
+    case SNN_BF16: return f(Bf16{});
+    case SNN_F16: return f(F16{});
+  }
+  return SNN_ERR_INVALID_ARG;
+}
+
+inline int type_size(int dtype) { return dtype == SNN_F32 ? 4 : dtype == SNN_BF16 || dtype == SNN_F16 ? 2 : 0; }
+
+// Arguments of a matrix of rows.
+inline snn_status check_rows(const void* p, int dtype, int64_t R, int C, int64_t ld) {
+  const int size = type_size(dtype);
+  if (!p || size == 0 || R <= 0 || C <= 0 || ld < C) return SNN_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(p) % size != 0) return SNN_ERR_INVALID_ARG;
+  if (R > INT32_MAX || C > kMaxClasses || ld > INT64_MAX / 4 / R) return SNN_ERR_UNSUPPORTED;
+  return SNN_OK;
+}
+
+}  // namespace rows
+}  // namespace snn

@@ -60,6 +60,10 @@ _SIGNATURES = {
     "snn_dense_backward_ref": (_I, [_P, _P, _P, _P, _I, _I, _I, _I, _F, _F, _F, _F, _P, _P, _P, _SZ, _P]),
     "snn_readout_ce_workspace": (_SZ, [_I, _I, _I, _I]),
     "snn_readout_ce": (_I, [_P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "snn_readout_top": (_I, [_P, _I, _I64, _I, _I64, _I, _F, _P, _P, _P, _P]),
+    "snn_readout_distill_workspace": (_SZ, [_I64, _I, _I]),
+    "snn_readout_distill": (_I, [_P, _I, _I64, _I, _I64, _P, _P, _P, _I, _F, _P, _P, _P, _P, _I64, _I, _P, _SZ, _P]),
+    "snn_readout_sample": (_I, [_P, _I, _I64, _I, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
     "snn_activity_reg_workspace": (_SZ, [_I, _I, _I]),
     "snn_activity_reg": (_I, [_P, _I, _I, _I, _F, _F, _F, _F, _P, _P, _P, _P, _SZ, _P]),
     "snn_activity_reg_grad": (_I, [_P, _I, _I, _I, _P, _P, _I64, _P, _P]),
@@ -352,6 +356,69 @@ def snn_readout_ce(V_out, labels, T, B, C, mode, row_ptr, col_idx, eps, loss, ep
         _ptr(eps_dense, torch.float32, "eps_dense"), _ptr(ws, None, "workspace"), ws.numel() * ws.element_size(), _stream(stream)))
 
 
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _rows(t: torch.Tensor, name="logits"):
+    """(pointer, dtype code, R, C, ld) of rows of logits: a [R, C] tensor whose rows may lie in wider ones, or a
+    contiguous one of more dimensions, its last the classes."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    if t.dim() == 2:
+        (R, C), (ld, step) = t.shape, t.stride()
+        if (step != 1 and C > 1) or (ld < C and R > 1):
+            raise ValueError(f"{name} must have its classes next to one another and rows that do not overlap")
+        return t.data_ptr(), code, R, C, max(ld, C)
+    if t.dim() < 2 or not t.is_contiguous():
+        raise ValueError(f"{name} must be [R, C], or contiguous with the classes last")
+    C = t.shape[-1]
+    return t.data_ptr(), code, t.numel() // C if C else 0, C, C
+
+
+def _of_rows(t: Optional[torch.Tensor], n: int, dtype, name):
+    """Pointer of an array with a value for each row (or each entry of each row)."""
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+    return _ptr(t, dtype, name)
+
+
+def snn_readout_top(logits, K, tau, ids, vals, lse=None, stream=None):
+    p, code, R, C, ld = _rows(logits)
+    _check("snn_readout_top", lib().snn_readout_top(
+        p, code, R, C, ld, int(K), float(tau), _of_rows(ids, R * K, torch.int32, "ids"),
+        _of_rows(vals, R * K, torch.float32, "vals"), _of_rows(lse, R, torch.float32, "lse"), _stream(stream)))
+
+
+def snn_readout_distill_workspace(R, C, dtype) -> int:
+    return int(lib().snn_readout_distill_workspace(R, C, _DTYPES[dtype]))
+
+
+def snn_readout_distill(logits, ids, vals, lse, K, tau, weight, loss, row_loss, grad, accumulate, ws, stream=None):
+    p, code, R, C, ld = _rows(logits)
+    g, ld_grad = None, 0
+    if grad is not None:
+        g, code_g, R_g, C_g, ld_grad = _rows(grad, "grad")
+        if (code_g, R_g, C_g) != (code, R, C):
+            raise ValueError("grad must have the type and the shape of the logits")
+    _check("snn_readout_distill", lib().snn_readout_distill(
+        p, code, R, C, ld, _of_rows(ids, R * K, torch.int32, "ids"), _of_rows(vals, R * K, torch.float32, "vals"),
+        _of_rows(lse, R, torch.float32, "lse"), int(K), float(tau), _of_rows(weight, R, torch.float32, "weight"),
+        _of_rows(loss, 1, torch.float32, "loss"), _of_rows(row_loss, R, torch.float32, "row_loss"), g, ld_grad,
+        int(accumulate), _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
+
+
+def snn_readout_sample(logits, u, temperature, top_k, top_p, min_p, cls, logp=None, kept=None, stream=None):
+    p, code, R, C, ld = _rows(logits)
+    _check("snn_readout_sample", lib().snn_readout_sample(
+        p, code, R, C, ld, _of_rows(u, R, torch.float32, "u"), _of_rows(temperature, R, torch.float32, "temperature"),
+        _of_rows(top_k, R, torch.int32, "top_k"), _of_rows(top_p, R, torch.float32, "top_p"),
+        _of_rows(min_p, R, torch.float32, "min_p"), _of_rows(cls, R, torch.int32, "cls"),
+        _of_rows(logp, R, torch.float32, "logp"), _of_rows(kept, R, torch.int32, "kept"), _stream(stream)))
+
+
 def snn_activity_reg_workspace(T, B, N) -> int:
     return int(lib().snn_activity_reg_workspace(T, B, N))
 
@@ -572,6 +639,45 @@ def readout_ce(V_out: torch.Tensor, labels: torch.Tensor, mode: int, dense=False
     ws = workspace(snn_readout_ce_workspace(T, B, C, mode), dev)
     snn_readout_ce(V_out, labels, T, B, C, mode, row_ptr, col, eps, loss, ed, ws)
     return Csr(row_ptr, col, None, None, nnz), eps, loss, ed
+
+
+def readout_top(logits: torch.Tensor, K: int, tau=1.0, want_lse=True, stream=None):
+    """A teacher's record of rows of logits [..., C]: (ids [..., K] int32, vals [..., K], lse [...] or None)."""
+    shape, dev = logits.shape[:-1], logits.device
+    ids = torch.empty((*shape, K), dtype=torch.int32, device=dev)
+    vals = torch.empty((*shape, K), dtype=torch.float32, device=dev)
+    lse = torch.empty(shape, dtype=torch.float32, device=dev) if want_lse else None
+    snn_readout_top(logits, K, tau, ids, vals, lse, stream)
+    return ids, vals, lse
+
+
+def readout_distill(logits: torch.Tensor, ids, vals, lse=None, tau=1.0, weight=None, want_grad=True, grad=None,
+                    accumulate=False, ws=None, stream=None):
+    """Distillation loss of rows of logits [..., C] against a teacher's records. Returns (loss [1], row_loss [...],
+    grad like the logits, or None). A grad that is given is written, or added to with accumulate."""
+    dev = logits.device
+    loss = torch.empty(1, dtype=torch.float32, device=dev)
+    row_loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=dev)
+    if accumulate and grad is None:
+        raise ValueError("readout_distill: accumulate needs a grad to add to")
+    if grad is None and want_grad:
+        grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    if ws is None:
+        R = row_loss.numel()
+        ws = workspace(snn_readout_distill_workspace(R, logits.shape[-1], logits.dtype), dev)
+    snn_readout_distill(logits, ids, vals, lse, ids.shape[-1], tau, weight, loss, row_loss, grad, accumulate, ws, stream)
+    return loss, row_loss, grad
+
+
+def readout_sample(logits: torch.Tensor, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """One class drawn per row of logits [..., C] from uniforms u [...]; the settings are arrays [...] on the device, or
+    None. Returns (cls [...] int32, logp [...], kept [...] int32)."""
+    shape, dev = logits.shape[:-1], logits.device
+    cls = torch.empty(shape, dtype=torch.int32, device=dev)
+    logp = torch.empty(shape, dtype=torch.float32, device=dev)
+    kept = torch.empty(shape, dtype=torch.int32, device=dev)
+    snn_readout_sample(logits, u, temperature, top_k, top_p, min_p, cls, logp, kept, stream)
+    return cls, logp, kept
 
 
 def sparse_backward(W, trace_in, alpha, out: Csr, eps_out, inp: Optional[Csr] = None, ws=None, aux_stream=None):

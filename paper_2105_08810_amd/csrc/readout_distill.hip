@@ -16,8 +16,6 @@ using namespace rows;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
 // A sum of 2^x kept as total * 2^max.
 struct Sum2 {
   float max, total;

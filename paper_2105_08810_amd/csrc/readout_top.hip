@@ -1,6 +1,14 @@
 // A teacher's record of its answers: the K largest logits of every row with their classes, largest first and equal
 // ones by class, and the row's log-sum-exp at a temperature, which gives the listed classes' probabilities and what
 // is left for the others.
+//
+// A row is read once into registers (up to 64 float32 or 128 16-bit values a thread). What is listed is found by a
+// bound from below that costs no pass: with each lane's largest value at hand, the ceil(K/waves)-th largest of every
+// wave's lanes, and the smallest of those over the waves. At least K values reach it, and hardly more do when values
+// lie in no particular order along the row (a thread's vectors are a block's width apart, so that a run of likely
+// classes is spread over all waves). One comparison a value collects them in LDS, where each counts those before it.
+// Where too many reach the bound (long runs of equal values), where K needs more than kNthMost of a wave, and for rows
+// beyond the registers, the cut is found by histograms of the row as it lies in memory (top_general).
 #include "rows.h"
 
 namespace snn {
@@ -8,23 +16,60 @@ namespace {
 
 using namespace rows;
 
+constexpr int kNthMost = 16;
+constexpr float kLog2e = 1.44269504088896340736f;
+
 template <int NT>
 struct TopLds {
-  SelectLds<NT> select;
+  static constexpr int kList = NT == kWave ? 256 : 1024;
+  union {
+    SelectLds<NT> select;
+    uint64_t list[kList];
+  };
   uint64_t taken[kMaxListed];
   float fred[NT / kWave];
+  uint32_t ured[NT / kWave];
   uint32_t n_taken;
 };
 
+struct Top {
+  const void* logits;
+  int64_t R;
+  int C;
+  int64_t ld;
+  int K;
+  float inv;
+  int32_t* ids;
+  float* vals;
+  float* lse;
+};
+
+// Classes and logits of the n collected entries by their place among them; the record's end where there are fewer.
 template <class T, int NT>
-__global__ __launch_bounds__(NT) void top_rows(const void* __restrict__ logits, int C, int64_t ld, int K, float inv,
-                                               int32_t* __restrict__ ids, float* __restrict__ vals,
-                                               float* __restrict__ lse) {
-  __shared__ TopLds<NT> s;
+__device__ __forceinline__ void write_record(const Row<T>& row, const Top& a, int64_t r, const uint64_t* list, int n) {
+  for (int e = threadIdx.x; e < max(n, a.K); e += NT) {
+    int place = e, id = -1;
+    float v = -INFINITY;
+    if (e < n) {
+      const uint64_t mine = list[e];
+      place = 0;
+      for (int o = 0; o < n; ++o) place += list[o] < mine;
+      id = (int)(uint32_t)mine;
+      if (place < a.K) v = row.at(id);
+    }
+    if (place < a.K) {
+      a.ids[r * a.K + place] = id;
+      a.vals[r * a.K + place] = v;
+    }
+  }
+}
+
+__device__ __forceinline__ uint64_t entry(uint32_t key, int j) { return (uint64_t)~key << 32 | (uint32_t)j; }
+
+template <class T, int NT>
+__device__ __forceinline__ void top_general(const Row<T>& row, const Top& a, int64_t r, TopLds<NT>& s) {
   constexpr int kVec = Row<T>::kVec;
-  const int64_t r = blockIdx.x;
   const int tid = threadIdx.x;
-  const Row<T> row(logits, r, ld, C);
   float m = -INFINITY, least = INFINITY;
   uint64_t count = 0;
   for (int q = tid; q < row.Q; q += NT) {
@@ -40,31 +85,31 @@ __global__ __launch_bounds__(NT) void top_rows(const void* __restrict__ logits, 
       }
     }
   }
-  const auto larger = [](float a, float b) { return fmaxf(a, b); };
-  const auto smaller = [](float a, float b) { return fminf(a, b); };
-  const auto add = [](auto a, auto b) { return a + b; };
+  const auto larger = [](float x, float y) { return fmaxf(x, y); };
+  const auto smaller = [](float x, float y) { return fminf(x, y); };
+  const auto add = [](auto x, auto y) { return x + y; };
   m = block_reduce<NT>(m, larger, s.fred);
   least = block_reduce<NT>(least, smaller, s.fred);
   count = block_reduce<NT>(count, add, s.select.red);
-  if (lse) {
+  if (a.lse) {
     float sum = 0.0f;
     const float safe = isinf(m) ? 0.0f : m;
     for (int q = tid; q < row.Q; q += NT) {
       float x[kVec];
       row.load(q, x);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) sum += expf((no_nan(x[i]) - safe) * inv);
+      for (int i = 0; i < kVec; ++i) sum += expf((no_nan(x[i]) - safe) * a.inv);
     }
     sum = block_reduce<NT>(sum, add, s.fred);
-    if (tid == 0) lse[r] = isinf(m) ? m : m * inv + logf(sum);
+    if (tid == 0) a.lse[r] = isinf(m) ? m : m * a.inv + logf(sum);
   }
   uint32_t cut_key = 0;
-  int last = C;  // class of the last listed element at the cut
-  if (count > (uint64_t)K) {
+  int last = a.C;  // class of the last listed element at the cut
+  if (count > (uint64_t)a.K) {
     const auto one = [](float x) { return (uint32_t)(x > -INFINITY); };
-    const Cut c = find_cut<T, NT, false>(row, one, key_of(least), key_of(m), (uint64_t)K, s.select);
+    const Cut c = find_cut<T, NT, false>(row, one, key_of(least), key_of(m), (uint64_t)a.K, s.select);
     cut_key = c.key;
-    const uint32_t ties = K - c.above_count;
+    const uint32_t ties = a.K - c.above_count;
     if (ties < c.equal)
       last = find_in_order<T, NT>(row, [&](float x, int) { return (uint64_t)(key_of(x) == cut_key); }, ties - 1,
                                   s.select.red);
@@ -81,24 +126,100 @@ __global__ __launch_bounds__(NT) void top_rows(const void* __restrict__ logits, 
       const int j = row.first(q) + i;
       const uint32_t k = key_of(y);
       if (y > -INFINITY && (k > cut_key || (k == cut_key && j <= last)))
-        s.taken[atomicAdd(&s.n_taken, 1u)] = (uint64_t)~k << 32 | (uint32_t)j;
+        s.taken[atomicAdd(&s.n_taken, 1u)] = entry(k, j);
     }
   }
   __syncthreads();
-  const int n = (int)s.n_taken;
-  for (int e = tid; e < K; e += NT) {
-    int place = e, id = -1;
-    float v = -INFINITY;
-    if (e < n) {
-      const uint64_t mine = s.taken[e];
-      place = 0;
-      for (int o = 0; o < n; ++o) place += s.taken[o] < mine;
-      id = (int)(uint32_t)mine;
-      v = row.at(id);
+  write_record<T, NT>(row, a, r, s.taken, (int)s.n_taken);
+}
+
+template <class T, int NT>
+__global__ __launch_bounds__(NT) void top_rows(Top a) {
+  __shared__ TopLds<NT> s;
+  const int64_t r = blockIdx.x;
+  top_general<T, NT>(Row<T>(a.logits, r, a.ld, a.C), a, r, s);
+}
+
+template <class T, int NT, int NV>
+__global__ __launch_bounds__(NT) void top_tile(Top a) {
+  __shared__ TopLds<NT> s;
+  constexpr int kVec = Row<T>::kVec;
+  constexpr int kWaves = NT / kWave;
+  const int64_t r = blockIdx.x;
+  const int tid = threadIdx.x;
+  const Row<T> row(a.logits, r, a.ld, a.C);
+  Tile<T, NT, NV> tile;
+  tile.load(row);
+  float most = -INFINITY;
+  bool nan = false;
+  tile.each(row, [&](const float (&x)[kVec], int) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      most = fmaxf(most, x[i]);
+      nan |= x[i] != x[i];
     }
-    ids[r * K + place] = id;
-    vals[r * K + place] = v;
+  });
+  const uint32_t key = nan ? 0u : key_of(most);  // 0 is no value's key
+  uint32_t high = wave_max_u32(key);
+  uint32_t bound = wave_nth(key, (a.K + kWaves - 1) / kWaves);
+  bool odd = __ballot(nan) != 0;
+  if (tid == 0) s.n_taken = 0;
+  if (NT > kWave) {
+    if (tid % kWave == 0) {
+      s.ured[tid / kWave] = odd ? 0u : bound;
+      s.fred[tid / kWave] = of_key(high);
+    }
+    __syncthreads();
+    uint32_t b = s.ured[0];
+    float m = s.fred[0];
+#pragma unroll
+    for (int k = 1; k < kWaves; ++k) {
+      b = min(b, s.ured[k]);
+      m = fmaxf(m, s.fred[k]);
+    }
+    bound = b;
+    odd = b == 0;
+    high = key_of(m);
+  } else {
+    __syncthreads();
   }
+  const float m = of_key(high);
+  if (odd || isinf(m)) {
+    __syncthreads();
+    return top_general<T, NT>(row, a, r, s);
+  }
+  const float least = of_key(bound);
+  const float c = a.inv * kLog2e, mc = m * c;
+  float sum = 0.0f;
+  tile.each(row, [&](const float (&x)[kVec], int q) {
+    float part = 0.0f;
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      part += exp2_fast(fmaf(x[i], c, -mc));
+      any |= x[i] >= least;
+    }
+    sum += part;
+    if (any) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i)
+        if (x[i] >= least && x[i] > -INFINITY) {
+          const uint32_t at = atomicAdd(&s.n_taken, 1u);
+          if (at < (uint32_t)TopLds<NT>::kList) s.list[at] = entry(key_of(x[i]), row.first(q) + i);
+        }
+    }
+  });
+  if (a.lse) {
+    sum = block_reduce<NT>(sum, [](float x, float y) { return x + y; }, s.fred);
+    if (tid == 0) a.lse[r] = m * a.inv + logf(sum);
+  }
+  __syncthreads();
+  const int n = (int)s.n_taken;
+  if (n > TopLds<NT>::kList) {
+    __syncthreads();
+    return top_general<T, NT>(row, a, r, s);
+  }
+  write_record<T, NT>(row, a, r, s.list, n);
 }
 
 }  // namespace
@@ -112,17 +233,26 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
   if (ok != SNN_OK) return ok;
   if (!ids || !vals || K <= 0 || K > C || !(tau > 0.0f) || isinf(tau)) return SNN_ERR_INVALID_ARG;
   if (K > rows::kMaxListed) return SNN_ERR_UNSUPPORTED;
-  const float inv = 1.0f / tau;
+  const Top a{logits, R, C, ld, K, 1.0f / tau, ids, vals, lse};
   hipStream_t s = static_cast<hipStream_t>(stream);
+  const dim3 grid((unsigned)R);
   return rows::for_type(dtype, [&](auto type) {
     using T = decltype(type);
-    if (C <= 1024)
-      hipLaunchKernelGGL((top_rows<T, 64>), dim3((unsigned)R), dim3(64), 0, s, logits, C, ld, K, inv, ids, vals, lse);
-    else if (C <= 16384)
-      hipLaunchKernelGGL((top_rows<T, 256>), dim3((unsigned)R), dim3(256), 0, s, logits, C, ld, K, inv, ids, vals, lse);
+    const int Q = rows::most_vectors<T>(logits, C, ld);
+    if (Q <= 4 * 64 && K <= kNthMost)
+      hipLaunchKernelGGL((top_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
+    else if (Q <= 4 * 256 && K <= 4 * kNthMost)
+      hipLaunchKernelGGL((top_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
+    else if (Q <= 4 * 1024 && K <= 16 * kNthMost)
+      hipLaunchKernelGGL((top_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
+    else if (Q <= 16 * 1024 && K <= 16 * kNthMost)
+      hipLaunchKernelGGL((top_tile<T, 1024, 16>), grid, dim3(1024), 0, s, a);
+    else if (Q <= 256)
+      hipLaunchKernelGGL((top_rows<T, 64>), grid, dim3(64), 0, s, a);
+    else if (Q <= 4096)
+      hipLaunchKernelGGL((top_rows<T, 256>), grid, dim3(256), 0, s, a);
     else
-      hipLaunchKernelGGL((top_rows<T, 1024>), dim3((unsigned)R), dim3(1024), 0, s, logits, C, ld, K, inv, ids, vals,
-                         lse);
+      hipLaunchKernelGGL((top_rows<T, 1024>), grid, dim3(1024), 0, s, a);
     return launch_status();
   });
 }

@@ -73,6 +73,92 @@ struct Row {
   }
 };
 
+template <class T>
+__device__ __forceinline__ T lowest();  // -inf
+template <>
+__device__ __forceinline__ float lowest<float>() {
+  return -INFINITY;
+}
+template <>
+__device__ __forceinline__ Bf16 lowest<Bf16>() {
+  return Bf16{0xff80};
+}
+template <>
+__device__ __forceinline__ F16 lowest<F16>() {
+  return F16{0xfc00};
+}
+
+// Vector q of a row as it lies in memory, -inf outside the row.
+template <class T>
+__device__ __forceinline__ uint4 load_raw(const Row<T>& row, int q) {
+  constexpr int kVec = Row<T>::kVec;
+  if (row.whole(q)) return *reinterpret_cast<const uint4*>(row.base + (size_t)q * kVec);
+  T v[kVec];
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const int j = row.first(q) + i;
+    v[i] = j >= 0 && j < row.C ? row.base[(size_t)q * kVec + i] : lowest<T>();
+  }
+  uint4 u;
+  __builtin_memcpy(&u, v, 16);
+  return u;
+}
+
+template <class T>
+__device__ __forceinline__ void unpack(const uint4& u, float (&x)[16 / sizeof(T)]) {
+  T v[16 / sizeof(T)];
+  __builtin_memcpy(v, &u, 16);
+#pragma unroll
+  for (int i = 0; i < (int)(16 / sizeof(T)); ++i) x[i] = to_float(v[i]);
+}
+
+// A row in a block's registers: vector i * NT + thread of it in v[i].
+template <class T, int NT, int NV>
+struct Tile {
+  uint4 v[NV];
+  __device__ __forceinline__ void load(const Row<T>& row) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i * NT < row.Q) v[i] = load_raw(row, i * NT + (int)threadIdx.x);
+  }
+  // f(values, vector) for the thread's vectors
+  template <class F>
+  __device__ __forceinline__ void each(const Row<T>& row, F f) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i * NT < row.Q) {
+        float x[Row<T>::kVec];
+        unpack<T>(v[i], x);
+        f(x, i * NT + (int)threadIdx.x);
+      }
+  }
+};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Largest of the wave's values; the steps within 16 lanes and between them are operands of the maximum itself.
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+#define SNN_STEP(ctrl) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, false))
+  SNN_STEP(0x111);  // from 1, 2, 4, 8 lanes below, in rows of 16
+  SNN_STEP(0x112);
+  SNN_STEP(0x114);
+  SNN_STEP(0x118);
+  SNN_STEP(0x142);  // a row's last lane to the next row, then lane 31 to the upper half
+  SNN_STEP(0x143);
+#undef SNN_STEP
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+// The n-th largest of the wave's values, 1 <= n <= 64.
+__device__ __forceinline__ uint32_t wave_nth(uint32_t v, int n) {
+  for (;;) {
+    const uint32_t m = wave_max_u32(v);
+    if (--n == 0) return m;
+    const int first = (int)__builtin_ctzll(__ballot(v == m));
+    v = lane_id() == first ? 0 : v;
+  }
+}
+
 // NaN as -inf: a class that is never listed or drawn.
 __device__ __forceinline__ float no_nan(float x) { return x == x ? x : -INFINITY; }
 
@@ -131,11 +217,11 @@ __device__ __forceinline__ uint64_t block_exclusive(uint64_t v, uint64_t* red, u
 // summation changes it. It is found by value: a histogram of the keys in range over kBins equal parts, whose part
 // with the limit becomes the next range, until it holds few elements (each then sums what is above it) or one value.
 
-constexpr int kBins = 1024;
 constexpr int kShort = 512;  // elements compared with one another
 
 template <int NT>
 struct SelectLds {
+  static constexpr int kBins = NT == kWave ? 256 : 1024;  // 256: many one-wave blocks of a CU share its LDS
   uint64_t mass[kBins];
   uint32_t count[kBins];
   uint32_t list[kShort];
@@ -158,6 +244,7 @@ template <class T, int NT, bool BY_MASS, class W>
 __device__ __forceinline__ Cut find_cut(const Row<T>& row, W weigh, uint32_t lo, uint32_t hi, uint64_t limit,
                                         SelectLds<NT>& s) {
   constexpr int kVec = Row<T>::kVec;
+  constexpr int kBins = SelectLds<NT>::kBins;
   const int tid = threadIdx.x;
   uint64_t above_mass = 0;
   uint32_t above_count = 0;
@@ -336,6 +423,14 @@ inline snn_status for_type(int dtype, F f) {
     case SNN_F16: return f(F16{});
   }
   return SNN_ERR_INVALID_ARG;
+}
+
+// Vectors of a row at most, over the rows of a matrix.
+template <class T>
+inline int most_vectors(const void* p, int C, int64_t ld) {
+  constexpr int kVec = 16 / (int)sizeof(T);
+  const bool aligned = reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % kVec == 0;
+  return aligned ? (C + kVec - 1) / kVec : (C + 2 * kVec - 2) / kVec;
 }
 
 inline int type_size(int dtype) { return dtype == SNN_F32 ? 4 : dtype == SNN_BF16 || dtype == SNN_F16 ? 2 : 0; }

@@ -5,7 +5,16 @@
 //   loss of a row = sum_k p_k (log p_k - log q_k) + p_t (log p_t - log q_t)
 //   d loss / d z_j = (mass q_j - p_j) / tau for a listed class, (mass q_t - p_t) (q_j / q_t) / tau for another
 // The classes not listed are summed by themselves, not as 1 - sum q_k: the difference of two sums of the whole row
-// would leave nothing of a small q_t.
+// would leave nothing of a small q_t. All sums and the gradient are float32, the loss over the rows float64.
+//
+// Bound by HBM: a row is read once and its gradient written once where it fits a block's registers. The exponentials
+// are kept there, each thread's relative to its own largest logit, so that the only barrier between reading and writing
+// is the one that joins the threads' sums; a factor per thread then makes them gradients. The K listed classes have
+// their bit in LDS, count as -inf in that pass, and get their own gradient after it. The teacher's side (K values) is
+// formed by every wave for itself, which needs no barrier.
+//   distill_small  16 lanes a row (up to 8 values each), four rows a wave: rows of up to 128 values
+//   distill_tile   a block a row, in registers
+//   distill_rows   a block a row, read twice: rows beyond the registers
 #include "rows.h"
 
 namespace snn {
@@ -20,32 +29,33 @@ constexpr float kLn2 = 0.69314718055994530942f;
 struct Sum2 {
   float max, total;
 };
+__device__ __forceinline__ float or_zero(float m) { return m == -INFINITY ? 0.0f : m; }
 __device__ __forceinline__ Sum2 join(Sum2 a, Sum2 b) {
   const float m = fmaxf(a.max, b.max);
-  const float safe = m == -INFINITY ? 0.0f : m;
+  const float safe = or_zero(m);
   return Sum2{m, a.total * exp2_fast(a.max - safe) + b.total * exp2_fast(b.max - safe)};
+}
+__device__ __forceinline__ bool empty(Sum2 a) { return a.max == -INFINITY && a.total == 0.0f; }
+
+// One maximum and one rescaled sum for the wave (a join at each step would form two exponentials).
+__device__ __forceinline__ Sum2 wave_join(Sum2 v) {
+  const float m = wave_reduce(v.max, Larger());
+  return Sum2{m, wave_reduce(v.total * exp2_fast(v.max - or_zero(m)), Plus())};
 }
 
 template <int NT>
-struct DistillLds {
-  Sum2 red[NT / kWave];
-  float fred[NT / kWave];
-  int ired[NT / kWave];
-};
-
-template <int NT>
 __device__ __forceinline__ Sum2 block_join(Sum2 v, Sum2* red) {
-#pragma unroll
-  for (int off = kWave / 2; off > 0; off >>= 1)
-    v = join(v, Sum2{__shfl_xor(v.max, off, kWave), __shfl_xor(v.total, off, kWave)});
+  v = wave_join(v);
   if (NT == kWave) return v;
-  __syncthreads();
   if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
   __syncthreads();
-  Sum2 r = red[0];
+  float m = red[0].max;
 #pragma unroll
-  for (int k = 1; k < NT / kWave; ++k) r = join(r, red[k]);
-  return r;
+  for (int k = 1; k < NT / kWave; ++k) m = fmaxf(m, red[k].max);
+  float total = 0.0f;
+#pragma unroll
+  for (int k = 0; k < NT / kWave; ++k) total += red[k].total * exp2_fast(red[k].max - or_zero(m));
+  return Sum2{m, total};
 }
 
 struct Distill {
@@ -63,155 +73,459 @@ struct Distill {
   void* grad;
   int64_t ld_grad;
   int accumulate;
+  double* part;  // a block's sum of weight * loss
+  __device__ __forceinline__ float weight_of(int64_t r) const { return weight ? weight[r] : 1.0f / (float)R; }
 };
+
+// What a row's gradient needs of its sums.
+struct RowSums {
+  float loss;
+  float base, per;  // q_j = 2^(z_j c - base) per
+  float mass;
+  float factor;     // of 2^(z_j c - rest.max) for a class that is not listed, without weight / tau
+};
+// The loss is that of the classes not listed; the caller adds the others' terms.
+__device__ __forceinline__ RowSums row_sums(Sum2 rest, Sum2 all, float listed_p, float p_t) {
+  RowSums s;
+  const bool none = empty(all);  // a row with nothing in it: q = 0
+  s.base = or_zero(all.max);
+  s.per = none ? 0.0f : 1.0f / all.total;
+  s.mass = listed_p + p_t;
+  const float q_t = empty(rest) ? 0.0f : rest.total * exp2_fast(or_zero(rest.max) - s.base) * s.per;
+  s.factor = empty(rest) ? 0.0f : (s.mass * q_t - p_t) / rest.total;
+  // log q_t, -inf where there is nothing
+  const float lq_t = (rest.max - s.base) * kLn2 + logf(rest.total) - (none ? 0.0f : logf(all.total));
+  s.loss = p_t > 0.0f ? p_t * (logf(p_t) - lq_t) : 0.0f;
+  return s;
+}
+__device__ __forceinline__ float left_of(float listed_p) {  // max(0, 1 - p); a NaN stays one
+  return listed_p < 1.0f ? 1.0f - listed_p : listed_p >= 1.0f ? 0.0f : listed_p;
+}
+
+// ------------------------------------------------------------------ 16 lanes a row
+
+// A lane's vectors are next to one another: value i of lane l is number l * kEach + i from the row's aligned address.
+template <class T>
+struct Small {
+  static constexpr int kVec = Row<T>::kVec;
+  static constexpr int kEach = 8;
+  static constexpr int NV = kEach / kVec;
+  static constexpr int kValues = 16 * kEach;
+};
+
+constexpr int kSmallRows = 16;           // rows of a block of 256
+constexpr int kNotListed = 0x7fffffff;   // a NaN that no operation gives
+
+template <class T>
+__global__ __launch_bounds__(256) void distill_small(Distill a) {
+  using S = Small<T>;
+  constexpr int kVec = S::kVec, kEach = S::kEach, NV = S::NV;
+  __shared__ __attribute__((aligned(16))) int table[kSmallRows][S::kValues];  // log p of the listed values
+  __shared__ double part[kSmallRows];
+  const int slot = threadIdx.x / 16, l = threadIdx.x % 16;
+  const int64_t r = (int64_t)blockIdx.x * kSmallRows + slot;
+  const int C = a.C, K = a.K;
+  const float w = r < a.R ? a.weight_of(r) : 0.0f;
+  const bool live = w != 0.0f;
+  const Row<T> row(a.logits, min(r, a.R - 1), a.ld, C);
+  uint4 raw[NV];
+  if (live) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) raw[i] = load_raw(row, l * NV + i);
+  }
+  int4* mine = reinterpret_cast<int4*>(&table[slot][l * kEach]);
+  mine[0] = mine[1] = make_int4(kNotListed, kNotListed, kNotListed, kNotListed);
+  __syncthreads();
+  const float inv_tau = 1.0f / a.tau;
+  if (live) {
+    for (int k = l; k < K; k += 16) {
+      const int id = a.ids[r * K + k];
+      if (id >= 0 && id < C) table[slot][row.lead + id] = __float_as_int(a.vals[r * K + k] / a.tau);
+    }
+  }
+  __syncthreads();
+  float loss = 0.0f;
+  if (live) {
+    float x[kEach], lp[kEach];
+    bool listed[kEach];
+    const int4 t[2] = {mine[0], mine[1]};
+    __builtin_memcpy(lp, t, sizeof(lp));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float y[kVec];
+      unpack<T>(raw[i], y);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) x[i * kVec + e] = y[e];
+    }
+    float count = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      listed[i] = __float_as_int(lp[i]) != kNotListed;
+      lp[i] = listed[i] ? lp[i] : -INFINITY;
+      count += listed[i] ? 1.0f : 0.0f;
+    }
+    // the teacher: log p, and the sum of p
+    float shift;
+    if (a.lse) {
+      shift = a.lse[r];
+    } else {
+      float top = lp[0], z = 0.0f;
+#pragma unroll
+      for (int i = 1; i < kEach; ++i) top = fmaxf(top, lp[i]);
+      top = or_zero(row16_reduce(top, Larger()));
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) z += exp2_fast((lp[i] - top) * kLog2e);
+      z = row16_reduce(z, Plus());
+      shift = z == 0.0f ? 0.0f : top + logf(z);
+    }
+    float p[kEach], listed_p = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      lp[i] -= shift;
+      p[i] = listed[i] ? exp2_fast(lp[i] * kLog2e) : 0.0f;
+      listed_p += p[i];
+    }
+    listed_p = row16_reduce(listed_p, Plus());
+    count = row16_reduce(count, Plus());
+    const float p_t = a.lse && count < (float)C ? left_of(listed_p) : 0.0f;
+    // the student
+    const float c = kLog2e * inv_tau;
+    Sum2 rest{-INFINITY, 0.0f}, own{-INFINITY, 0.0f};
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      rest.max = fmaxf(rest.max, listed[i] ? -INFINITY : x[i] * c);
+      own.max = fmaxf(own.max, listed[i] ? x[i] * c : -INFINITY);
+    }
+    rest.max = row16_reduce(rest.max, Larger());
+    own.max = row16_reduce(own.max, Larger());
+    float e[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      e[i] = exp2_fast(fmaf(x[i], c, -or_zero(listed[i] ? own.max : rest.max)));
+      rest.total += listed[i] ? 0.0f : e[i];
+      own.total += listed[i] ? e[i] : 0.0f;
+    }
+    rest.total = row16_reduce(rest.total, Plus());
+    own.total = row16_reduce(own.total, Plus());
+    const Sum2 all = join(rest, own);
+    const RowSums s = row_sums(rest, all, listed_p, p_t);
+    const float log_total = empty(all) ? 0.0f : logf(all.total);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (listed[i] && !(p[i] <= 0.0f)) loss += p[i] * (lp[i] - (fmaf(x[i], c, -s.base) * kLn2 - log_total));
+    loss = row16_reduce(loss, Plus()) + s.loss;
+    if (a.grad) {
+      const Row<T> out(a.grad, r, a.ld_grad, C);
+      const float scale = w * inv_tau;
+      const float own_per = scale * s.mass * exp2_fast(or_zero(own.max) - s.base) * s.per;
+      const float rest_per = scale * s.factor;
+      float g[kEach];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) g[i] = listed[i] ? fmaf(e[i], own_per, -scale * p[i]) : e[i] * rest_per;
+      if (out.lead == row.lead) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          float y[kVec];
+          if (a.accumulate) out.load(l * NV + i, y);
+#pragma unroll
+          for (int v = 0; v < kVec; ++v) y[v] = a.accumulate ? y[v] + g[i * kVec + v] : g[i * kVec + v];
+          store_vec(out, l * NV + i, y);
+        }
+      } else {
+        T* to = const_cast<T*>(out.base) + out.lead;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const int j = l * kEach + i - row.lead;
+          if (j >= 0 && j < C) to[j] = from_float<T>(a.accumulate ? to_float(to[j]) + g[i] : g[i]);
+        }
+      }
+    }
+  } else if (r < a.R && a.grad && !a.accumulate) {
+    T* to = static_cast<T*>(a.grad) + r * a.ld_grad;
+    for (int j = l; j < C; j += 16) to[j] = from_float<T>(0.0f);
+  }
+  if (l == 0) {
+    part[slot] = live ? (double)w * (double)loss : 0.0;
+    if (r < a.R && a.row_loss) a.row_loss[r] = loss;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double v = 0.0;
+    for (int k = 0; k < kSmallRows; ++k) v += part[k];
+    a.part[blockIdx.x] = v;
+  }
+}
+
+// ------------------------------------------------------------------ a block a row
+
+// The teacher's entries, held by every wave: entry k = lane + 64 e.
+struct Teacher {
+  float shift, listed_p, p_t;
+};
+template <class T, int NT>
+__device__ __forceinline__ Teacher teacher_of(const Distill& a, int64_t r, const Row<T>& row, uint32_t* bits) {
+  const int32_t* ids = a.ids + r * a.K;
+  const float* vals = a.vals + r * a.K;
+  const int l = threadIdx.x % kWave;
+  for (int k = threadIdx.x; k < a.K; k += NT) {
+    const int id = ids[k];
+    if (id >= 0 && id < a.C) {
+      const int v = row.lead + id;
+      atomicOr(&bits[v >> 5], 1u << (v & 31));
+    }
+  }
+  Teacher t;
+  if (a.lse) {
+    t.shift = a.lse[r];
+  } else {
+    float top = -INFINITY, z = 0.0f;
+    for (int k = l; k < a.K; k += kWave)
+      if (ids[k] >= 0 && ids[k] < a.C) top = fmaxf(top, vals[k] / a.tau);
+    top = or_zero(wave_reduce(top, Larger()));
+    for (int k = l; k < a.K; k += kWave)
+      if (ids[k] >= 0 && ids[k] < a.C) z += expf(vals[k] / a.tau - top);
+    z = wave_reduce(z, Plus());
+    t.shift = z == 0.0f ? 0.0f : top + logf(z);
+  }
+  float p = 0.0f, n = 0.0f;
+  for (int k = l; k < a.K; k += kWave)
+    if (ids[k] >= 0 && ids[k] < a.C) {
+      p += expf(vals[k] / a.tau - t.shift);
+      n += 1.0f;
+    }
+  t.listed_p = wave_reduce(p, Plus());
+  n = wave_reduce(n, Plus());
+  t.p_t = a.lse && n < (float)a.C ? left_of(t.listed_p) : 0.0f;
+  return t;
+}
+
+// Joins the listed classes to the others' sum, forms the row's loss (every wave for itself).
+template <class T>
+__device__ __forceinline__ RowSums finish_row(const Distill& a, int64_t r, const Row<T>& row, const Teacher& t,
+                                              Sum2 rest, float c) {
+  const int32_t* ids = a.ids + r * a.K;
+  const float* vals = a.vals + r * a.K;
+  const int l = threadIdx.x % kWave;
+  float top = -INFINITY, z = 0.0f;
+  for (int k = l; k < a.K; k += kWave)
+    if (ids[k] >= 0 && ids[k] < a.C) top = fmaxf(top, row.at(ids[k]) * c);
+  top = wave_reduce(top, Larger());
+  for (int k = l; k < a.K; k += kWave)
+    if (ids[k] >= 0 && ids[k] < a.C) z += exp2_fast(fmaf(row.at(ids[k]), c, -or_zero(top)));
+  const Sum2 all = join(rest, Sum2{top, wave_reduce(z, Plus())});
+  RowSums s = row_sums(rest, all, t.listed_p, t.p_t);
+  const float log_total = empty(all) ? 0.0f : logf(all.total);
+  float loss = 0.0f;
+  for (int k = l; k < a.K; k += kWave)
+    if (ids[k] >= 0 && ids[k] < a.C) {
+      const float lp = vals[k] / a.tau - t.shift, p = expf(lp);
+      const float lq = fmaf(row.at(ids[k]), c, -s.base) * kLn2 - log_total;
+      if (!(p <= 0.0f)) loss += p * (lp - lq);
+    }
+  s.loss += wave_reduce(loss, Plus());
+  return s;
+}
+
+// The listed classes' gradients, over what the pass over the row left there (nothing added to it).
+template <class T, int NT>
+__device__ __forceinline__ void listed_grads(const Distill& a, int64_t r, const Row<T>& row, const Teacher& t,
+                                             const RowSums& s, float c, float scale) {
+  const int32_t* ids = a.ids + r * a.K;
+  T* grad = static_cast<T*>(a.grad) + r * a.ld_grad;
+  __syncthreads();
+  for (int k = threadIdx.x; k < a.K; k += NT) {
+    const int id = ids[k];
+    if (id >= 0 && id < a.C) {
+      const float q = exp2_fast(fmaf(row.at(id), c, -s.base)) * s.per;
+      const float g = scale * (s.mass * q - expf(a.vals[r * a.K + k] / a.tau - t.shift));
+      grad[id] = from_float<T>(a.accumulate ? to_float(grad[id]) + g : g);
+    }
+  }
+}
+
+// x[i] * per of vector q to the gradient's row.
+template <class T>
+__device__ __forceinline__ void put(const Distill& a, const Row<T>& row, const Row<T>& out, int q,
+                                    const float (&x)[16 / sizeof(T)], float per) {
+  constexpr int kVec = Row<T>::kVec;
+  if (out.lead == row.lead) {
+    float y[kVec];
+    if (a.accumulate) {
+      out.load(q, y);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) y[i] += x[i] * per;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) y[i] = x[i] * per;
+    }
+    store_vec(out, q, y);
+  } else {
+    T* to = const_cast<T*>(out.base) + out.lead;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      const int j = row.first(q) + i;
+      if (j >= 0 && j < a.C) to[j] = from_float<T>(a.accumulate ? to_float(to[j]) + x[i] * per : x[i] * per);
+    }
+  }
+}
+
+template <class T, int NT>
+__device__ __forceinline__ void row_without_weight(const Distill& a, int64_t r) {
+  if (threadIdx.x == 0) {
+    if (a.row_loss) a.row_loss[r] = 0.0f;
+    a.part[r] = 0.0;
+  }
+  if (a.grad && !a.accumulate) {
+    const Row<T> out(a.grad, r, a.ld_grad, a.C);
+    const float zero[Row<T>::kVec] = {};
+    for (int q = threadIdx.x; q < out.Q; q += NT) store_vec(out, q, zero);
+  }
+}
+
+template <class T, int NT, int NV>
+__global__ __launch_bounds__(NT) void distill_tile(Distill a) {
+  constexpr int kVec = Row<T>::kVec;
+  __shared__ uint32_t bits[NT * NV * kVec / 32];
+  __shared__ Sum2 red[NT / kWave];
+  const int64_t r = blockIdx.x;
+  const int tid = threadIdx.x;
+  const float w = a.weight_of(r);
+  if (w == 0.0f) return row_without_weight<T, NT>(a, r);  // not read: what is there may be anything
+  const Row<T> row(a.logits, r, a.ld, a.C);
+  Tile<T, NT, NV> tile;
+  tile.load(row);
+  for (int k = tid; k < (row.Q * kVec + 31) / 32; k += NT) bits[k] = 0;
+  __syncthreads();
+  const Teacher t = teacher_of<T, NT>(a, r, row, bits);
+  __syncthreads();
+  const float c = kLog2e / a.tau;
+  float e[NV][kVec];
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (i * NT < row.Q) {
+      const int q = i * NT + tid;
+      unpack<T>(tile.v[i], e[i]);
+      const int v = q * kVec;
+      const uint32_t on = q < row.Q ? bits[v >> 5] >> (v & 31) : 0;
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) {
+        if (on >> k & 1) e[i][k] = -INFINITY;
+        top = fmaxf(top, e[i][k]);
+      }
+    }
+  top *= c;
+  const float safe = or_zero(top);
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (i * NT < row.Q) {
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) {
+        e[i][k] = exp2_fast(fmaf(e[i][k], c, -safe));
+        sum += e[i][k];
+      }
+    }
+  const Sum2 rest = block_join<NT>(Sum2{top, sum}, red);
+  const RowSums s = finish_row<T>(a, r, row, t, rest, c);
+  if (tid == 0) {
+    if (a.row_loss) a.row_loss[r] = s.loss;
+    a.part[r] = (double)w * (double)s.loss;
+  }
+  if (!a.grad) return;
+  const Row<T> out(a.grad, r, a.ld_grad, a.C);
+  const float scale = w / a.tau;
+  const float per = top == -INFINITY ? 0.0f : scale * s.factor * exp2_fast(safe - rest.max);
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (i * NT + tid < row.Q) put(a, row, out, i * NT + tid, e[i], per);
+  listed_grads<T, NT>(a, r, row, t, s, c, scale);
+}
 
 template <class T, int NT>
 __global__ __launch_bounds__(NT) void distill_rows(Distill a) {
-  extern __shared__ uint32_t listed[];  // a bit per class
-  __shared__ DistillLds<NT> s;
   constexpr int kVec = Row<T>::kVec;
+  extern __shared__ uint32_t bits[];
+  __shared__ Sum2 red[NT / kWave];
   const int64_t r = blockIdx.x;
   const int tid = threadIdx.x;
-  const int C = a.C, K = a.K;
-  T* grad = a.grad ? static_cast<T*>(a.grad) + r * a.ld_grad : nullptr;
-  const float w = a.weight ? a.weight[r] : 1.0f / (float)a.R;
-  if (w == 0.0f) {  // not read: what is there may be anything
-    if (tid == 0) a.row_loss[r] = 0.0f;
-    if (grad && !a.accumulate)
-      for (int j = tid; j < C; j += NT) grad[j] = from_float<T>(0.0f);
-    return;
-  }
-  const Row<T> row(a.logits, r, a.ld, C);
-  const int32_t* ids = a.ids + r * K;
-  const float* vals = a.vals + r * K;
-  for (int k = tid; k < (C + 31) / 32; k += NT) listed[k] = 0;
+  const float w = a.weight_of(r);
+  if (w == 0.0f) return row_without_weight<T, NT>(a, r);
+  const Row<T> row(a.logits, r, a.ld, a.C);
+  for (int k = tid; k < (row.Q * kVec + 31) / 32; k += NT) bits[k] = 0;
   __syncthreads();
-  const auto larger = [](float x, float y) { return fmaxf(x, y); };
-  const auto add = [](auto x, auto y) { return x + y; };
+  const Teacher t = teacher_of<T, NT>(a, r, row, bits);
+  __syncthreads();
   const float c = kLog2e / a.tau;
-  // the teacher
-  float top = -INFINITY;
-  int n = 0;
-  for (int k = tid; k < K; k += NT) {
-    const int id = ids[k];
-    if (id >= 0 && id < C) {
-      atomicOr(&listed[id >> 5], 1u << (id & 31));
-      top = fmaxf(top, vals[k]);
-      ++n;
-    }
-  }
-  n = block_reduce<NT>(n, add, s.ired);
-  float shift;  // p_k = exp(v_k / tau - shift)
-  if (a.lse) {
-    shift = a.lse[r];
-  } else {
-    top = block_reduce<NT>(top, larger, s.fred) / a.tau;
-    float z = 0.0f;
-    for (int k = tid; k < K; k += NT)
-      if (ids[k] >= 0 && ids[k] < C) z += expf(vals[k] / a.tau - top);
-    z = block_reduce<NT>(z, add, s.fred);
-    shift = top == -INFINITY ? 0.0f : top + logf(z);
-  }
-  float listed_p = 0.0f;
-  for (int k = tid; k < K; k += NT)
-    if (ids[k] >= 0 && ids[k] < C) listed_p += expf(vals[k] / a.tau - shift);
-  listed_p = block_reduce<NT>(listed_p, add, s.fred);
-  const float p_t = a.lse && n < C ? (listed_p < 1.0f ? 1.0f - listed_p : listed_p >= 1.0f ? 0.0f : listed_p) : 0.0f;
-  const float mass = listed_p + p_t;
-  __syncthreads();  // the bits
-  // the student: the classes not listed, then the listed ones
-  Sum2 rest{-INFINITY, 0.0f};
-  for (int q = tid; q < row.Q; q += NT) {
-    float x[kVec];
-    row.load(q, x);
-    float m = rest.max;
+  constexpr int kAhead = 4;  // vectors of a thread in flight
+  auto pass = [&](auto f) {
+    for (int q0 = tid; q0 < row.Q; q0 += kAhead * NT) {
+      uint4 raw[kAhead];
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      const int j = row.first(q) + i;
-      if (j < 0 || j >= C || (listed[j >> 5] >> (j & 31) & 1)) x[i] = -INFINITY;
-      m = fmaxf(m, x[i] * c);
-    }
-    const float safe = m == -INFINITY ? 0.0f : m;
-    float v = rest.total * exp2_fast(rest.max - safe);
+      for (int u = 0; u < kAhead; ++u)
+        if (q0 + u * NT < row.Q) raw[u] = load_raw(row, q0 + u * NT);
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) v += exp2_fast(fmaf(x[i], c, -safe));
-    rest = Sum2{m, v};
-  }
-  rest = block_join<NT>(rest, s.red);
-  Sum2 all{-INFINITY, 0.0f};
-  for (int k = tid; k < K; k += NT)
-    if (ids[k] >= 0 && ids[k] < C) {
-      const float x = row.at(ids[k]);
-      const float m = x * c;
-      all = join(all, Sum2{m, x == -INFINITY ? 0.0f : exp2_fast(fmaf(x, c, -m))});
-    }
-  all = join(block_join<NT>(all, s.red), rest);
-  const bool none = all.max == -INFINITY && all.total == 0.0f;  // a row with nothing in it: q = 0
-  const float base = none ? 0.0f : all.max;
-  const float log_total = none ? 0.0f : logf(all.total);
-  const float per = none ? 0.0f : 1.0f / all.total;
-  const float rest_base = rest.max == -INFINITY ? 0.0f : rest.max;
-  float loss = 0.0f;
-  for (int k = tid; k < K; k += NT)
-    if (ids[k] >= 0 && ids[k] < C) {
-      const float lp = vals[k] / a.tau - shift, p = expf(lp);
-      const float lq = fmaf(row.at(ids[k]), c, -base) * kLn2 - log_total;
-      if (!(p <= 0.0f)) loss += p * (lp - lq);
-    }
-  loss = block_reduce<NT>(loss, add, s.fred);
-  const float lq_t = (rest.max - base) * kLn2 + logf(rest.total) - log_total;  // -inf where there is nothing
-  if (p_t > 0.0f) loss += p_t * (logf(p_t) - lq_t);
-  if (tid == 0) a.row_loss[r] = loss;
-  if (!grad) return;
-  const float scale = w / a.tau;
-  const float q_t = none ? 0.0f : rest.total * exp2_fast(rest_base - base) * per;
-  const bool no_rest = rest.max == -INFINITY && rest.total == 0.0f;
-  const float factor = no_rest ? 0.0f : scale * (mass * q_t - p_t) / rest.total;
-  // the gradients of listed classes: read before the others are written, written after them
-  constexpr int kEach = (kMaxListed + NT - 1) / NT;
-  float mine[kEach];
+      for (int u = 0; u < kAhead; ++u) {
+        const int q = q0 + u * NT;
+        if (q < row.Q) {
+          float x[kVec];
+          unpack<T>(raw[u], x);
+          const int v = q * kVec;
+          const uint32_t on = bits[v >> 5] >> (v & 31);
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const int k = tid + e * NT;
-    mine[e] = 0.0f;
-    if (k < K && ids[k] >= 0 && ids[k] < C) {
-      const float q = exp2_fast(fmaf(row.at(ids[k]), c, -base)) * per;
-      mine[e] = scale * (mass * q - expf(vals[k] / a.tau - shift));
-      if (a.accumulate) mine[e] += to_float(grad[ids[k]]);
-    }
-  }
-  __syncthreads();
-  for (int q = tid; q < row.Q; q += NT) {
-    float x[kVec];
-    row.load(q, x);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      const int j = row.first(q) + i;
-      if (j >= 0 && j < C && !(listed[j >> 5] >> (j & 31) & 1)) {
-        float g = exp2_fast(fmaf(x[i], c, -rest_base)) * factor;
-        if (a.accumulate) g += to_float(grad[j]);
-        grad[j] = from_float<T>(g);
+          for (int k = 0; k < kVec; ++k)
+            if (on >> k & 1) x[k] = -INFINITY;
+          f(x, q);
+        }
       }
     }
-  }
+  };
+  Sum2 rest{-INFINITY, 0.0f};
+  pass([&](float (&x)[kVec], int) {
+    float m = x[0];
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const int k = tid + e * NT;
-    if (k < K && ids[k] >= 0 && ids[k] < C) grad[ids[k]] = from_float<T>(mine[e]);
+    for (int k = 1; k < kVec; ++k) m = fmaxf(m, x[k]);
+    m = fmaxf(rest.max, m * c);
+    const float safe = or_zero(m);
+    float v = rest.total * exp2_fast(rest.max - safe);
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) v += exp2_fast(fmaf(x[k], c, -safe));
+    rest = Sum2{m, v};
+  });
+  rest = block_join<NT>(rest, red);
+  const RowSums s = finish_row<T>(a, r, row, t, rest, c);
+  if (tid == 0) {
+    if (a.row_loss) a.row_loss[r] = s.loss;
+    a.part[r] = (double)w * (double)s.loss;
+  }
+  if (!a.grad) return;
+  const Row<T> out(a.grad, r, a.ld_grad, a.C);
+  const float scale = w / a.tau;
+  const float per = scale * s.factor, safe = or_zero(rest.max);
+  pass([&](float (&x)[kVec], int q) {
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) x[k] = exp2_fast(fmaf(x[k], c, -safe));
+    put(a, row, out, q, x, per);
+  });
+  listed_grads<T, NT>(a, r, row, t, s, c, scale);
+}
+
+// Sums of `each` parts in a fixed order: one block writes the loss itself.
+__global__ __launch_bounds__(1024) void distill_total(const double* __restrict__ part, int64_t n, int64_t each,
+                                                      double* __restrict__ sums, float* __restrict__ loss) {
+  __shared__ double red[1024 / kWave];
+  const int64_t from = blockIdx.x * each, to = min(n, from + each);
+  double v = 0.0;
+#pragma unroll 4
+  for (int64_t k = from + threadIdx.x; k < to; k += 1024) v += part[k];
+  v = block_reduce<1024>(v, [](double a, double b) { return a + b; }, red);
+  if (threadIdx.x == 0) {
+    if (gridDim.x == 1) *loss = (float)v;
+    else sums[blockIdx.x] = v;
   }
 }
 
-// loss = sum of w_r row_loss_r over the rows with a weight, in float64 and a fixed order.
-__global__ __launch_bounds__(1024) void distill_total(const float* __restrict__ row_loss,
-                                                      const float* __restrict__ weight, int64_t R,
-                                                      float* __restrict__ loss) {
-  __shared__ double red[1024 / kWave];
-  double v = 0.0;
-  for (int64_t r = threadIdx.x; r < R; r += 1024)
-    v += weight ? (weight[r] != 0.0f ? (double)weight[r] * (double)row_loss[r] : 0.0) : (double)row_loss[r];
-  v = block_reduce<1024>(v, [](double a, double b) { return a + b; }, red);
-  if (threadIdx.x == 0) *loss = (float)(weight ? v : v / (double)R);
-}
+constexpr int64_t kTotalEach = 16384;  // parts of a block of the loss's sum
 
 }  // namespace
 }  // namespace snn
@@ -221,7 +535,8 @@ using namespace snn;
 extern "C" size_t snn_readout_distill_workspace(int64_t R, int C, int dtype) {
   if (R <= 0 || R > INT32_MAX || bad_dim(C) || C > rows::kMaxClasses || rows::type_size(dtype) == 0) return 0;
   Carve c(nullptr);
-  c.take<float>((size_t)R);  // losses of the rows
+  c.take<double>((size_t)R);  // weighted losses of the rows or of groups of them
+  c.take<double>((size_t)((R + kTotalEach - 1) / kTotalEach));
   return c.off;
 }
 
@@ -241,22 +556,41 @@ extern "C" snn_status snn_readout_distill(const void* logits, int dtype, int64_t
   if (workspace_bytes < snn_readout_distill_workspace(R, C, dtype)) return SNN_ERR_INVALID_ARG;
   if (K > rows::kMaxListed) return SNN_ERR_UNSUPPORTED;
   Carve ws(workspace);
-  float* losses = ws.take<float>((size_t)R);
-  if (row_loss) losses = row_loss;
-  const Distill a{logits, C, ld, ids, vals, lse, K, tau, weight, R, losses, grad, ld_grad, accumulate};
+  double* part = ws.take<double>((size_t)R);
+  double* sums = ws.take<double>((size_t)((R + kTotalEach - 1) / kTotalEach));
+  const Distill a{logits, C, ld, ids, vals, lse, K, tau, weight, R, row_loss, grad, ld_grad, accumulate, part};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const size_t lds = (size_t)(C + 31) / 32 * 4;
-  return rows::for_type(dtype, [&](auto type) {
+  const dim3 grid((unsigned)R);
+  int64_t n = R;
+  const snn_status launched = rows::for_type(dtype, [&](auto type) {
     using T = decltype(type);
-    if (C <= 1024) {
-      hipLaunchKernelGGL((distill_rows<T, 64>), dim3((unsigned)R), dim3(64), lds, s, a);
-    } else if (C <= 16384) {
-      hipLaunchKernelGGL((distill_rows<T, 256>), dim3((unsigned)R), dim3(256), lds, s, a);
+    constexpr int kWide = sizeof(T) == 4 ? 16 : 8;  // 64 values of a thread in registers
+    const int Q = rows::most_vectors<T>(logits, C, ld);
+    if (Q <= 16 * Small<T>::NV) {
+      n = (R + kSmallRows - 1) / kSmallRows;
+      hipLaunchKernelGGL((distill_small<T>), dim3((unsigned)n), dim3(256), 0, s, a);
+    } else if (Q <= 4 * 64) {
+      hipLaunchKernelGGL((distill_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
+    } else if (Q <= 4 * 256) {
+      hipLaunchKernelGGL((distill_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
+    } else if (Q <= 4 * 1024) {
+      hipLaunchKernelGGL((distill_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
+    } else if (Q <= kWide * 1024) {
+      hipLaunchKernelGGL((distill_tile<T, 1024, kWide>), grid, dim3(1024), 0, s, a);
     } else {
+      const size_t lds = ((size_t)Q * Row<T>::kVec + 31) / 32 * 4;
       ensure_dynamic_lds((const void*)distill_rows<T, 1024>, (int)lds);
-      hipLaunchKernelGGL((distill_rows<T, 1024>), dim3((unsigned)R), dim3(1024), lds, s, a);
+      hipLaunchKernelGGL((distill_rows<T, 1024>), grid, dim3(1024), lds, s, a);
     }
-    hipLaunchKernelGGL(distill_total, dim3(1), dim3(1024), 0, s, losses, weight, R, loss);
     return launch_status();
   });
+  if (launched != SNN_OK) return launched;
+  if (n > kTotalEach) {
+    const int64_t blocks = (n + kTotalEach - 1) / kTotalEach;
+    hipLaunchKernelGGL(distill_total, dim3((unsigned)blocks), dim3(1024), 0, s, part, n, kTotalEach, sums, loss);
+    hipLaunchKernelGGL(distill_total, dim3(1), dim3(1024), 0, s, sums, blocks, blocks, sums, loss);
+  } else {
+    hipLaunchKernelGGL(distill_total, dim3(1), dim3(1024), 0, s, part, n, n, sums, loss);
+  }
+  return launch_status();
 }

@@ -104,6 +104,25 @@ __device__ __forceinline__ uint4 load_raw(const Row<T>& row, int q) {
   return u;
 }
 
+// Values of vector q back to a row, those inside it.
+template <class T>
+__device__ __forceinline__ void store_vec(const Row<T>& row, int q, const float (&x)[16 / sizeof(T)]) {
+  constexpr int kVec = Row<T>::kVec;
+  T v[kVec];
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) v[i] = from_float<T>(x[i]);
+  T* p = const_cast<T*>(row.base) + (size_t)q * kVec;
+  if (row.whole(q)) {
+    uint4 u;
+    __builtin_memcpy(&u, v, 16);
+    *reinterpret_cast<uint4*>(p) = u;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      if (row.first(q) + i >= 0 && row.first(q) + i < row.C) p[i] = v[i];
+  }
+}
+
 template <class T>
 __device__ __forceinline__ void unpack(const uint4& u, float (&x)[16 / sizeof(T)]) {
   T v[16 / sizeof(T)];
@@ -161,6 +180,31 @@ __device__ __forceinline__ uint32_t wave_nth(uint32_t v, int n) {
 
 // NaN as -inf: a class that is never listed or drawn.
 __device__ __forceinline__ float no_nan(float x) { return x == x ? x : -INFINITY; }
+
+// Every lane of 16 gets f over their values (f commutes). Each step's operand comes from another lane of the row in
+// the instruction itself: neighbours, pairs, then the mirrored half rows and rows.
+template <class F>
+__device__ __forceinline__ float row16_reduce(float v, F f) {
+#define SNN_STEP(ctrl) v = f(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), ctrl, 0xf, 0xf, true)))
+  SNN_STEP(0xb1);
+  SNN_STEP(0x4e);
+  SNN_STEP(0x141);
+  SNN_STEP(0x140);
+#undef SNN_STEP
+  return v;
+}
+template <class F>
+__device__ __forceinline__ float wave_reduce(float v, F f) {
+  v = row16_reduce(v, f);
+  v = f(v, __shfl_xor(v, 16, kWave));
+  return f(v, __shfl_xor(v, 32, kWave));
+}
+struct Larger {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct Plus {
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
 
 // Integers in the order of the values; -0 and +0 are one.
 __device__ __forceinline__ uint32_t key_of(float x) {

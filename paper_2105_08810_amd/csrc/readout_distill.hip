@@ -77,25 +77,29 @@ struct Distill {
   __device__ __forceinline__ float weight_of(int64_t r) const { return weight ? weight[r] : 1.0f / (float)R; }
 };
 
-// What a row's gradient needs of its sums.
+// What a row's loss and gradient need of its sums.
 struct RowSums {
   float loss;
-  float base, per;  // q_j = 2^(z_j c - base) per
+  float lse;         // log q_j = z_j / tau - lse; 0 for a row with nothing in it, whose z are all -inf
+  float base, per;   // q_j = 2^(z_j c - base) per
   float mass;
-  float factor;     // of 2^(z_j c - rest.max) for a class that is not listed, without weight / tau
+  float factor;      // of 2^(z_j c - rest.max) for a class that is not listed, without weight / tau
 };
-// The loss is that of the classes not listed; the caller adds the others' terms.
-__device__ __forceinline__ RowSums row_sums(Sum2 rest, Sum2 all, float listed_p, float p_t) {
+// The loss is that of the classes not listed; the caller adds the others' terms. Logarithms are differences of float32
+// log-sum-exps, so a loss is exact to about 2^-23 |lse|; the gradient takes ratios of sums.
+__device__ __forceinline__ RowSums row_sums(Sum2 rest, Sum2 own, float listed_p, float p_t) {
   RowSums s;
-  const bool none = empty(all);  // a row with nothing in it: q = 0
+  const Sum2 all = join(rest, own);
+  const bool none = empty(all);  // q = 0
   s.base = or_zero(all.max);
   s.per = none ? 0.0f : 1.0f / all.total;
   s.mass = listed_p + p_t;
   const float q_t = empty(rest) ? 0.0f : rest.total * exp2_fast(or_zero(rest.max) - s.base) * s.per;
   s.factor = empty(rest) ? 0.0f : (s.mass * q_t - p_t) / rest.total;
-  // log q_t, -inf where there is nothing
-  const float lq_t = (rest.max - s.base) * kLn2 + logf(rest.total) - (none ? 0.0f : logf(all.total));
-  s.loss = p_t > 0.0f ? p_t * (logf(p_t) - lq_t) : 0.0f;
+  const float lse_t = rest.max * kLn2 + logf(rest.total);  // -inf where there is nothing
+  const float own_max = own.max * kLn2, top = or_zero(fmaxf(own_max, lse_t));
+  s.lse = none ? 0.0f : top + logf(expf(lse_t - top) + own.total * expf(own_max - top));
+  s.loss = p_t > 0.0f ? p_t * (logf(p_t) - (lse_t - s.lse)) : s.lse == s.lse ? 0.0f : s.lse;
   return s;
 }
 __device__ __forceinline__ float left_of(float listed_p) {  // max(0, 1 - p); a NaN stays one
@@ -207,12 +211,10 @@ __global__ __launch_bounds__(256) void distill_small(Distill a) {
     }
     rest.total = row16_reduce(rest.total, Plus());
     own.total = row16_reduce(own.total, Plus());
-    const Sum2 all = join(rest, own);
-    const RowSums s = row_sums(rest, all, listed_p, p_t);
-    const float log_total = empty(all) ? 0.0f : logf(all.total);
+    const RowSums s = row_sums(rest, own, listed_p, p_t);
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-      if (listed[i] && !(p[i] <= 0.0f)) loss += p[i] * (lp[i] - (fmaf(x[i], c, -s.base) * kLn2 - log_total));
+      if (listed[i] && !(p[i] <= 0.0f)) loss += p[i] * (lp[i] - (x[i] * inv_tau - s.lse));
     loss = row16_reduce(loss, Plus()) + s.loss;
     if (a.grad) {
       const Row<T> out(a.grad, r, a.ld_grad, C);
@@ -258,41 +260,75 @@ __global__ __launch_bounds__(256) void distill_small(Distill a) {
 
 // ------------------------------------------------------------------ a block a row
 
-// The teacher's entries, held by every wave: entry k = lane + 64 e.
+// The row's entries as every wave holds them, entry k at lane k % 64: the first kHeld of a lane with their student's
+// logit in registers, fetched before anything waits for the row; the others are read where they are needed.
+constexpr int kHeld = 2;
+template <class T>
+struct Entries {
+  const int32_t* ids;
+  const float* vals;
+  int K, C;
+  float held_v[kHeld];  // v / tau
+  float x[kHeld];
+  int id[kHeld];            // -1: no entry
+  float tau;
+  const Row<T>& row;
+
+  __device__ __forceinline__ Entries(const Distill& a, int64_t r, const Row<T>& row_)
+      : ids(a.ids + r * a.K), vals(a.vals + r * a.K), K(a.K), C(a.C), tau(a.tau), row(row_) {
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e) {
+      const int k = threadIdx.x % kWave + e * kWave;
+      id[e] = k < K ? ids[k] : -1;
+      held_v[e] = k < K ? vals[k] : 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e) {
+      if (id[e] >= C) id[e] = -1;
+      x[e] = id[e] >= 0 ? row.at(id[e]) : 0.0f;
+      held_v[e] /= tau;
+    }
+  }
+  // f(id, v / tau, student's logit) of the lane's entries
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e)
+      if (id[e] >= 0) f(id[e], held_v[e], x[e]);
+    for (int k = threadIdx.x % kWave + kHeld * kWave; k < K; k += kWave) {
+      const int j = ids[k];
+      if (j >= 0 && j < C) f(j, vals[k] / tau, row.at(j));
+    }
+  }
+};
+
 struct Teacher {
   float shift, listed_p, p_t;
 };
-template <class T, int NT>
-__device__ __forceinline__ Teacher teacher_of(const Distill& a, int64_t r, const Row<T>& row, uint32_t* bits) {
-  const int32_t* ids = a.ids + r * a.K;
-  const float* vals = a.vals + r * a.K;
-  const int l = threadIdx.x % kWave;
-  for (int k = threadIdx.x; k < a.K; k += NT) {
-    const int id = ids[k];
-    if (id >= 0 && id < a.C) {
-      const int v = row.lead + id;
+// Also sets the listed classes' bits (by the first wave).
+template <class T>
+__device__ __forceinline__ Teacher teacher_of(const Distill& a, int64_t r, const Entries<T>& entries, uint32_t* bits) {
+  if (threadIdx.x < kWave)
+    entries.each([&](int id, float, float) {
+      const int v = entries.row.lead + id;
       atomicOr(&bits[v >> 5], 1u << (v & 31));
-    }
-  }
+    });
   Teacher t;
   if (a.lse) {
     t.shift = a.lse[r];
   } else {
     float top = -INFINITY, z = 0.0f;
-    for (int k = l; k < a.K; k += kWave)
-      if (ids[k] >= 0 && ids[k] < a.C) top = fmaxf(top, vals[k] / a.tau);
+    entries.each([&](int, float v, float) { top = fmaxf(top, v); });
     top = or_zero(wave_reduce(top, Larger()));
-    for (int k = l; k < a.K; k += kWave)
-      if (ids[k] >= 0 && ids[k] < a.C) z += expf(vals[k] / a.tau - top);
+    entries.each([&](int, float v, float) { z += expf(v - top); });
     z = wave_reduce(z, Plus());
     t.shift = z == 0.0f ? 0.0f : top + logf(z);
   }
   float p = 0.0f, n = 0.0f;
-  for (int k = l; k < a.K; k += kWave)
-    if (ids[k] >= 0 && ids[k] < a.C) {
-      p += expf(vals[k] / a.tau - t.shift);
-      n += 1.0f;
-    }
+  entries.each([&](int, float v, float) {
+    p += expf(v - t.shift);
+    n += 1.0f;
+  });
   t.listed_p = wave_reduce(p, Plus());
   n = wave_reduce(n, Plus());
   t.p_t = a.lse && n < (float)a.C ? left_of(t.listed_p) : 0.0f;
@@ -301,46 +337,33 @@ __device__ __forceinline__ Teacher teacher_of(const Distill& a, int64_t r, const
 
 // Joins the listed classes to the others' sum, forms the row's loss (every wave for itself).
 template <class T>
-__device__ __forceinline__ RowSums finish_row(const Distill& a, int64_t r, const Row<T>& row, const Teacher& t,
-                                              Sum2 rest, float c) {
-  const int32_t* ids = a.ids + r * a.K;
-  const float* vals = a.vals + r * a.K;
-  const int l = threadIdx.x % kWave;
+__device__ __forceinline__ RowSums finish_row(const Entries<T>& entries, const Teacher& t, Sum2 rest, float c) {
   float top = -INFINITY, z = 0.0f;
-  for (int k = l; k < a.K; k += kWave)
-    if (ids[k] >= 0 && ids[k] < a.C) top = fmaxf(top, row.at(ids[k]) * c);
+  entries.each([&](int, float, float x) { top = fmaxf(top, x * c); });
   top = wave_reduce(top, Larger());
-  for (int k = l; k < a.K; k += kWave)
-    if (ids[k] >= 0 && ids[k] < a.C) z += exp2_fast(fmaf(row.at(ids[k]), c, -or_zero(top)));
-  const Sum2 all = join(rest, Sum2{top, wave_reduce(z, Plus())});
-  RowSums s = row_sums(rest, all, t.listed_p, t.p_t);
-  const float log_total = empty(all) ? 0.0f : logf(all.total);
+  entries.each([&](int, float, float x) { z += exp2_fast(fmaf(x, c, -or_zero(top))); });
+  RowSums s = row_sums(rest, Sum2{top, wave_reduce(z, Plus())}, t.listed_p, t.p_t);
   float loss = 0.0f;
-  for (int k = l; k < a.K; k += kWave)
-    if (ids[k] >= 0 && ids[k] < a.C) {
-      const float lp = vals[k] / a.tau - t.shift, p = expf(lp);
-      const float lq = fmaf(row.at(ids[k]), c, -s.base) * kLn2 - log_total;
-      if (!(p <= 0.0f)) loss += p * (lp - lq);
-    }
+  entries.each([&](int, float v, float x) {
+    const float lp = v - t.shift, p = expf(lp);
+    if (!(p <= 0.0f)) loss += p * (lp - (x / entries.tau - s.lse));
+  });
   s.loss += wave_reduce(loss, Plus());
   return s;
 }
 
-// The listed classes' gradients, over what the pass over the row left there (nothing added to it).
-template <class T, int NT>
-__device__ __forceinline__ void listed_grads(const Distill& a, int64_t r, const Row<T>& row, const Teacher& t,
+// The listed classes' gradients by the first wave, over what the pass over the row left there (nothing added to it).
+template <class T>
+__device__ __forceinline__ void listed_grads(const Distill& a, int64_t r, const Entries<T>& entries, const Teacher& t,
                                              const RowSums& s, float c, float scale) {
-  const int32_t* ids = a.ids + r * a.K;
   T* grad = static_cast<T*>(a.grad) + r * a.ld_grad;
   __syncthreads();
-  for (int k = threadIdx.x; k < a.K; k += NT) {
-    const int id = ids[k];
-    if (id >= 0 && id < a.C) {
-      const float q = exp2_fast(fmaf(row.at(id), c, -s.base)) * s.per;
-      const float g = scale * (s.mass * q - expf(a.vals[r * a.K + k] / a.tau - t.shift));
+  if (threadIdx.x < kWave)
+    entries.each([&](int id, float v, float x) {
+      const float q = exp2_fast(fmaf(x, c, -s.base)) * s.per;
+      const float g = scale * (s.mass * q - expf(v - t.shift));
       grad[id] = from_float<T>(a.accumulate ? to_float(grad[id]) + g : g);
-    }
-  }
+    });
 }
 
 // x[i] * per of vector q to the gradient's row.
@@ -392,11 +415,12 @@ __global__ __launch_bounds__(NT) void distill_tile(Distill a) {
   const float w = a.weight_of(r);
   if (w == 0.0f) return row_without_weight<T, NT>(a, r);  // not read: what is there may be anything
   const Row<T> row(a.logits, r, a.ld, a.C);
+  const Entries<T> entries(a, r, row);
   Tile<T, NT, NV> tile;
   tile.load(row);
   for (int k = tid; k < (row.Q * kVec + 31) / 32; k += NT) bits[k] = 0;
   __syncthreads();
-  const Teacher t = teacher_of<T, NT>(a, r, row, bits);
+  const Teacher t = teacher_of<T>(a, r, entries, bits);
   __syncthreads();
   const float c = kLog2e / a.tau;
   float e[NV][kVec];
@@ -427,7 +451,7 @@ __global__ __launch_bounds__(NT) void distill_tile(Distill a) {
       }
     }
   const Sum2 rest = block_join<NT>(Sum2{top, sum}, red);
-  const RowSums s = finish_row<T>(a, r, row, t, rest, c);
+  const RowSums s = finish_row<T>(entries, t, rest, c);
   if (tid == 0) {
     if (a.row_loss) a.row_loss[r] = s.loss;
     a.part[r] = (double)w * (double)s.loss;
@@ -439,7 +463,7 @@ __global__ __launch_bounds__(NT) void distill_tile(Distill a) {
 #pragma unroll
   for (int i = 0; i < NV; ++i)
     if (i * NT + tid < row.Q) put(a, row, out, i * NT + tid, e[i], per);
-  listed_grads<T, NT>(a, r, row, t, s, c, scale);
+  listed_grads<T>(a, r, entries, t, s, c, scale);
 }
 
 template <class T, int NT>
@@ -452,9 +476,10 @@ __global__ __launch_bounds__(NT) void distill_rows(Distill a) {
   const float w = a.weight_of(r);
   if (w == 0.0f) return row_without_weight<T, NT>(a, r);
   const Row<T> row(a.logits, r, a.ld, a.C);
+  const Entries<T> entries(a, r, row);
   for (int k = tid; k < (row.Q * kVec + 31) / 32; k += NT) bits[k] = 0;
   __syncthreads();
-  const Teacher t = teacher_of<T, NT>(a, r, row, bits);
+  const Teacher t = teacher_of<T>(a, r, entries, bits);
   __syncthreads();
   const float c = kLog2e / a.tau;
   constexpr int kAhead = 4;  // vectors of a thread in flight
@@ -493,7 +518,7 @@ __global__ __launch_bounds__(NT) void distill_rows(Distill a) {
     rest = Sum2{m, v};
   });
   rest = block_join<NT>(rest, red);
-  const RowSums s = finish_row<T>(a, r, row, t, rest, c);
+  const RowSums s = finish_row<T>(entries, t, rest, c);
   if (tid == 0) {
     if (a.row_loss) a.row_loss[r] = s.loss;
     a.part[r] = (double)w * (double)s.loss;
@@ -507,7 +532,7 @@ __global__ __launch_bounds__(NT) void distill_rows(Distill a) {
     for (int k = 0; k < kVec; ++k) x[k] = exp2_fast(fmaf(x[k], c, -safe));
     put(a, row, out, q, x, per);
   });
-  listed_grads<T, NT>(a, r, row, t, s, c, scale);
+  listed_grads<T>(a, r, entries, t, s, c, scale);
 }
 
 // Sums of `each` parts in a fixed order: one block writes the loss itself.
@@ -566,6 +591,7 @@ extern "C" snn_status snn_readout_distill(const void* logits, int dtype, int64_t
     using T = decltype(type);
     constexpr int kWide = sizeof(T) == 4 ? 16 : 8;  // 64 values of a thread in registers
     const int Q = rows::most_vectors<T>(logits, C, ld);
+    const bool many = R >= 2 * cu_count();
     if (Q <= 16 * Small<T>::NV) {
       n = (R + kSmallRows - 1) / kSmallRows;
       hipLaunchKernelGGL((distill_small<T>), dim3((unsigned)n), dim3(256), 0, s, a);
@@ -573,6 +599,10 @@ extern "C" snn_status snn_readout_distill(const void* logits, int dtype, int64_t
       hipLaunchKernelGGL((distill_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
     } else if (Q <= 4 * 256) {
       hipLaunchKernelGGL((distill_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
+    } else if (Q <= kWide * 256 && many) {
+      hipLaunchKernelGGL((distill_tile<T, 256, kWide>), grid, dim3(256), 0, s, a);
+    } else if (Q <= kWide * 512 && many) {
+      hipLaunchKernelGGL((distill_tile<T, 512, kWide>), grid, dim3(512), 0, s, a);
     } else if (Q <= 4 * 1024) {
       hipLaunchKernelGGL((distill_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
     } else if (Q <= kWide * 1024) {

@@ -654,14 +654,20 @@ def readout_top(logits: torch.Tensor, K: int, tau=1.0, want_lse=True, stream=Non
 def readout_distill(logits: torch.Tensor, ids, vals, lse=None, tau=1.0, weight=None, want_grad=True, grad=None,
                     accumulate=False, ws=None, stream=None):
     """Distillation loss of rows of logits [..., C] against a teacher's records. Returns (loss [1], row_loss [...],
-    grad like the logits, or None). A grad that is given is written, or added to with accumulate."""
+    grad like the logits, or None). A grad that is given is written, or added to with accumulate; one that is made has
+    the rows of the logits at the same distance, since rows that begin alike are written fastest."""
     dev = logits.device
     loss = torch.empty(1, dtype=torch.float32, device=dev)
     row_loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=dev)
     if accumulate and grad is None:
         raise ValueError("readout_distill: accumulate needs a grad to add to")
     if grad is None and want_grad:
-        grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+        C, ld = logits.shape[-1], logits.stride(-2)
+        if logits.dim() != 2 or ld == C:
+            grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+        else:  # rows far apart (a narrow part of a wide matrix): whole 64-byte lines instead
+            grad = torch.empty((logits.shape[0], ld if C < ld < 2 * C else -(-C // 32) * 32), dtype=logits.dtype,
+                               device=dev)[:, :C]
     if ws is None:
         R = row_loss.numel()
         ws = workspace(snn_readout_distill_workspace(R, logits.shape[-1], logits.dtype), dev)

@@ -423,33 +423,42 @@ __global__ __launch_bounds__(NT) void distill_tile(Distill a) {
   const Teacher t = teacher_of<T>(a, r, entries, bits);
   __syncthreads();
   const float c = kLog2e / a.tau;
-  float e[NV][kVec];
+  // Value k of the thread's vector i, the logit and then its exponential, takes the place of the tile's own float32 or
+  // has one beside it.
+  typedef float Floats __attribute__((ext_vector_type(NV)));
+  Floats e[kVec];
+  const auto keep = [&](int i, int k, float v) {
+    if constexpr (sizeof(T) == 4) tile.w[k][i] = __float_as_uint(v);
+    else e[k][i] = v;
+  };
+  const auto kept = [&](int i, int k) -> float {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(tile.w[k][i]);
+    else return e[k][i];
+  };
   float top = -INFINITY;
+  tile.each_unrolled(row, [&](float (&x)[kVec], int q, int i) {
+    const int v = q * kVec;
+    const uint32_t on = q < row.Q ? bits[v >> 5] >> (v & 31) : 0;
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (i * NT < row.Q) {
-      const int q = i * NT + tid;
-      unpack<T>(tile.v[i], e[i]);
-      const int v = q * kVec;
-      const uint32_t on = q < row.Q ? bits[v >> 5] >> (v & 31) : 0;
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) {
-        if (on >> k & 1) e[i][k] = -INFINITY;
-        top = fmaxf(top, e[i][k]);
-      }
+    for (int k = 0; k < kVec; ++k) {
+      if (on >> k & 1) x[k] = -INFINITY;
+      top = fmaxf(top, x[k]);
+      keep(i, k, x[k]);
     }
+  });
   top *= c;
   const float safe = or_zero(top);
   float sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (i * NT < row.Q) {
+  for (int i = 0; i < NV; ++i) {
+    if (i * NT >= row.Q) break;
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) {
-        e[i][k] = exp2_fast(fmaf(e[i][k], c, -safe));
-        sum += e[i][k];
-      }
+    for (int k = 0; k < kVec; ++k) {
+      const float y = exp2_fast(fmaf(kept(i, k), c, -safe));
+      keep(i, k, y);
+      sum += y;
     }
+  }
   const Sum2 rest = block_join<NT>(Sum2{top, sum}, red);
   const RowSums s = finish_row<T>(entries, t, rest, c);
   if (tid == 0) {
@@ -460,9 +469,29 @@ __global__ __launch_bounds__(NT) void distill_tile(Distill a) {
   const Row<T> out(a.grad, r, a.ld_grad, a.C);
   const float scale = w / a.tau;
   const float per = top == -INFINITY ? 0.0f : scale * s.factor * exp2_fast(safe - rest.max);
+  if (out.lead == row.lead && !a.accumulate) {
+    const int from = out.lead ? 1 : 0, to = (out.lead + a.C) / kVec;  // whole vectors
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (i * NT + tid < row.Q) put(a, row, out, i * NT + tid, e[i], per);
+    for (int i = 0; i < NV; ++i) {
+      const int q = i * NT + tid;
+      T v[kVec];
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) v[k] = from_float<T>(kept(i, k) * per);
+      uint4 u;
+      __builtin_memcpy(&u, v, 16);
+      if (q >= from && q < to) *reinterpret_cast<uint4*>(const_cast<T*>(out.base) + (size_t)q * kVec) = u;
+    }
+  }
+#pragma unroll 1
+  for (int i = 0; i * NT < row.Q; ++i) {  // the rest, or all of them
+    const int q = i * NT + tid;
+    if (q < row.Q && (out.lead != row.lead || a.accumulate || !out.whole(q))) {
+      float x[kVec];
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) x[k] = kept(i, k);
+      put(a, row, out, q, x, per);
+    }
+  }
   listed_grads<T>(a, r, entries, t, s, c, scale);
 }
 

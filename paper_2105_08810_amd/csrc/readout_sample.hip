@@ -25,30 +25,80 @@ struct Settings {
 
 struct Weigh {
   float max, inv;
-  __device__ __forceinline__ float e(float x) const {  // in this order of operations, each rounded
-    return x == max ? 1.0f : expf((x - max) * inv);
+  __device__ __forceinline__ float t(float x) const {  // in this order of operations, each rounded
+    return x == max ? 0.0f : (x - max) * inv;
   }
-  __device__ __forceinline__ uint32_t operator()(float x) const {
-    return x == -INFINITY ? 0u : (uint32_t)rintf(e(x) * kUnit);
+  __device__ __forceinline__ float e(float x) const { return expf(t(x)); }
+  __device__ __forceinline__ uint32_t of(float x, float e) const {
+    return x == -INFINITY ? 0u : (uint32_t)rintf(e * kUnit);
+  }
+  __device__ __forceinline__ uint32_t operator()(float x) const { return of(x, e(x)); }
+};
+
+struct Sample {
+  const void* logits;
+  int64_t R;
+  int C;
+  int64_t ld;
+  Settings set;
+  int32_t* cls;
+  float* logp;
+  int32_t* kept;
+  __device__ __forceinline__ void answer(int64_t r, int j, float lp, int n) const {
+    cls[r] = j;
+    if (logp) logp[r] = lp;
+    if (kept) kept[r] = n;
   }
 };
 
+// A row's settings with what leaves a filter out made plain.
+struct RowSettings {
+  float u, temperature, top_p, min_p;
+  int k;  // 1 also where the largest logit is asked for
+  __device__ __forceinline__ RowSettings(const Settings& set, int64_t r, int C) {
+    u = set.u[r];
+    temperature = set.temperature ? set.temperature[r] : 1.0f;
+    temperature = temperature > 1e30f ? 1e30f : temperature;  // beyond it every finite logit has the same weight
+    k = set.top_k ? set.top_k[r] : 0;
+    if (k <= 0 || k > C) k = C;
+    if (!(temperature > 0.0f)) k = 1;
+    top_p = set.top_p ? set.top_p[r] : 1.0f;
+    top_p = top_p > 0.0f ? fminf(top_p, 1.0f) : 0.0f;
+    min_p = set.min_p ? set.min_p[r] : 0.0f;
+    min_p = min_p > 0.0f ? fminf(min_p, 1.0f) : 0.0f;
+  }
+  // The weight that a prefix of the order has to reach, of `sum`.
+  __device__ __forceinline__ uint64_t limit(uint64_t sum) const {
+    if (top_p >= 1.0f) return sum;
+    const uint64_t l = (uint64_t)ceil((double)top_p * (double)sum);
+    return l < 1 ? 1 : l;
+  }
+  __device__ __forceinline__ uint64_t point(uint64_t total) const {
+    const double at = floor((double)u * (double)total);
+    return at > 0.0 ? (at < (double)total ? (uint64_t)at : total - 1) : 0;
+  }
+};
+
+// log of a drawn class's share of the kept weights
+__device__ __forceinline__ float log_share(const Weigh& weigh, float x, uint64_t total) {
+  return weigh.t(x) - (float)log((double)total * (1.0 / kUnit));
+}
+
+// ------------------------------------------------------------------ any row, read in passes
+
 template <int NT>
-struct SampleLds {
+struct GeneralLds {
   SelectLds<NT> select;
   float fred[NT / kWave];
   int ired[NT / kWave];
 };
 
 template <class T, int NT>
-__global__ __launch_bounds__(NT) void sample_rows(const void* __restrict__ logits, int C, int64_t ld, Settings set,
-                                                  int32_t* __restrict__ cls, float* __restrict__ logp,
-                                                  int32_t* __restrict__ kept) {
-  __shared__ SampleLds<NT> s;
+__device__ __forceinline__ void sample_general(const Sample& a, int64_t r, const Row<T>& row, const RowSettings& set,
+                                               GeneralLds<NT>& s) {
   constexpr int kVec = Row<T>::kVec;
-  const int64_t r = blockIdx.x;
   const int tid = threadIdx.x;
-  const Row<T> row(logits, r, ld, C);
+  const int C = a.C;
   float m = -INFINITY;
   for (int q = tid; q < row.Q; q += NT) {
     float x[kVec];
@@ -56,23 +106,12 @@ __global__ __launch_bounds__(NT) void sample_rows(const void* __restrict__ logit
 #pragma unroll
     for (int i = 0; i < kVec; ++i) m = fmaxf(m, x[i]);
   }
-  m = block_reduce<NT>(m, [](float a, float b) { return fmaxf(a, b); }, s.fred);
-  auto answer = [&](int j, float lp, int n) {
-    if (tid == 0) {
-      cls[r] = j;
-      if (logp) logp[r] = lp;
-      if (kept) kept[r] = n;
-    }
-  };
-  if (m == -INFINITY) return answer(-1, -INFINITY, 0);
-  // beyond 1e30 every finite logit has the same weight
-  float temperature = set.temperature ? set.temperature[r] : 1.0f;
-  temperature = temperature > 1e30f ? 1e30f : temperature;
-  int k = set.top_k ? set.top_k[r] : 0;
-  if (k <= 0 || k > C) k = C;
-  if (!(temperature > 0.0f)) k = 1;
-  const Weigh weigh{m, 1.0f / temperature};
-  if (k == 1) {  // the first of the largest
+  m = block_reduce<NT>(m, Larger(), s.fred);
+  if (m == -INFINITY) {
+    if (tid == 0) a.answer(r, -1, -INFINITY, 0);
+    return;
+  }
+  if (set.k == 1) {  // the first of the largest
     int at = INT32_MAX;
     for (int q = tid; q < row.Q; q += NT) {
       float x[kVec];
@@ -81,82 +120,403 @@ __global__ __launch_bounds__(NT) void sample_rows(const void* __restrict__ logit
       for (int i = 0; i < kVec; ++i)
         if (x[i] == m) at = min(at, row.first(q) + i);
     }
-    at = block_reduce<NT>(at, [](int a, int b) { return min(a, b); }, s.ired);
-    return answer(at, 0.0f, 1);
+    at = block_reduce<NT>(at, [](int x, int y) { return min(x, y); }, s.ired);
+    if (tid == 0) a.answer(r, at, 0.0f, 1);
+    return;
   }
-  // the weights of all and how many there are
-  uint64_t sum = 0;
-  uint64_t count = 0;
-  for (int q = tid; q < row.Q; q += NT) {
-    float x[kVec];
-    row.load(q, x);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      const uint32_t n = weigh(no_nan(x[i]));
-      sum += n;
-      count += n != 0;
-    }
-  }
-  const auto add = [](uint64_t a, uint64_t b) { return a + b; };
-  sum = block_reduce<NT>(sum, add, s.select.red);
-  count = block_reduce<NT>(count, add, s.select.red);
-  const uint32_t hi = key_of(m);
-  const uint32_t lo = key_of(m - kFaintest * temperature);
-  if ((uint64_t)k < count) {
-    const Cut c = find_cut<T, NT, false>(row, weigh, lo, hi, (uint64_t)k, s.select);
-    // the elements above the cut weigh what they weigh; those at it weigh the same each
-    uint64_t above = 0;
+  const Weigh weigh{m, 1.0f / set.temperature};
+  // Passes over the row: the weights of all and how many there are; then, the cut known, of the kept.
+  Cut cut{0, 0, 0, 0};
+  int last = C;  // class of the last kept element at the cut
+  uint64_t ties = 0;
+  bool by_share = false;
+  const auto part_of = [&](float x, int j) -> uint64_t {
+    const uint32_t key = key_of(x);
+    if (!by_share) return key == cut.key;
+    if (key < cut.key || (key == cut.key && j > last)) return 0;
+    const float e = weigh.e(x);
+    return e >= set.min_p ? weigh.of(x, e) : 0;
+  };
+  uint64_t sum = 0, count = 0, target = 0;
+#pragma unroll 1
+  for (int round = 0; round < 2; ++round) {
+    by_share = true;  // round 0: with no cut, and any e
+    sum = count = 0;
+#pragma unroll 1
     for (int q = tid; q < row.Q; q += NT) {
       float x[kVec];
       row.load(q, x);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         const float y = no_nan(x[i]);
-        if (key_of(y) > c.key) above += weigh(y);
+        const uint64_t n = round == 0 ? weigh(y) : part_of(y, row.first(q) + i);
+        sum += n;
+        count += n != 0;
       }
     }
-    sum = block_reduce<NT>(above, add, s.select.red) + (uint64_t)(k - c.above_count) * weigh(of_key(c.key));
-  }
-  uint64_t limit = sum;
-  if (set.top_p) {
-    const float p = set.top_p[r];
-    if (!(p >= 1.0f)) limit = p > 0.0f ? (uint64_t)ceil((double)p * (double)sum) : 1;
-    limit = limit < 1 ? 1 : limit;
-  }
-  const Cut c = find_cut<T, NT, true>(row, weigh, lo, hi, limit, s.select);
-  const uint32_t each = weigh(of_key(c.key));
-  const uint32_t ties = (uint32_t)((limit - c.above_mass + each - 1) / each);
-  float least = set.min_p ? set.min_p[r] : 0.0f;
-  least = least > 0.0f ? fminf(least, 1.0f) : 0.0f;
-  int last = C;  // class of the last kept element at the cut
-  if (ties < c.equal)
-    last = find_in_order<T, NT>(row, [&](float x, int) { return (uint64_t)(key_of(x) == c.key); }, ties - 1,
-                                s.select.red);
-  auto share = [&](float x, int j) -> uint64_t {
-    const uint32_t key = key_of(x);
-    if (key < c.key || (key == c.key && j > last)) return 0;
-    return weigh.e(x) >= least ? weigh(x) : 0;
-  };
-  uint64_t total = 0;
-  count = 0;
-  for (int q = tid; q < row.Q; q += NT) {
-    float x[kVec];
-    row.load(q, x);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      const uint64_t n = share(no_nan(x[i]), row.first(q) + i);
-      total += n;
-      count += n != 0;
+    sum = block_sum64<NT>(sum, s.select.red);
+    count = block_sum64<NT>(count, s.select.red);
+    if (round == 0) {
+      const uint32_t hi = key_of(m), lo = key_of(m - kFaintest * set.temperature);
+      uint64_t limit = (uint64_t)set.k;
+#pragma unroll 1
+      for (int by_mass = (uint64_t)set.k < count ? 0 : 1; by_mass < 2; ++by_mass) {
+        if (by_mass) limit = set.limit(sum);
+        cut = find_cut<T, NT, true>(row, weigh, lo, hi, limit, by_mass != 0, s.select);
+        // what lies at the cut weighs the same each
+        const uint64_t each = weigh(of_key(cut.key));
+        ties = by_mass ? (limit - cut.above_mass + each - 1) / each : limit - cut.above_count;
+        sum = cut.above_mass + ties * each;
+      }
+      by_share = false;
+      target = ties - 1;
+    } else {
+      target = set.point(sum);
+    }
+    if (round == 1 || ties < cut.equal) {
+      const int j = find_in_order<T, NT>(row, part_of, target, s.select.red, 0, row.Q);
+      if (round == 0) last = j;
+      else if (tid == 0) a.answer(r, j, log_share(weigh, no_nan(row.at(j)), sum), (int)count);
     }
   }
-  total = block_reduce<NT>(total, add, s.select.red);
-  count = block_reduce<NT>(count, add, s.select.red);
-  const double at = floor((double)set.u[r] * (double)total);
-  const uint64_t point = at > 0.0 ? (at < (double)total ? (uint64_t)at : total - 1) : 0;
-  const int j = find_in_order<T, NT>(row, share, point, s.select.red);
-  const float x = no_nan(row.at(j));
-  const float t = x == m ? 0.0f : (x - m) * weigh.inv;
-  answer(j, t - (float)log((double)total * (1.0 / kUnit)), (int)count);
+}
+
+template <class T, int NT>
+__global__ __launch_bounds__(NT) void sample_rows(Sample a) {
+  __shared__ GeneralLds<NT> s;
+  const int64_t r = blockIdx.x;
+  sample_general<T, NT>(a, r, Row<T>(a.logits, r, a.ld, a.C), RowSettings(a.set, r, a.C), s);
+}
+
+// ------------------------------------------------------------------ rows in registers
+
+constexpr int kBins = 1024;
+constexpr float kBinsPer = (kBins - 1) / kFaintest;  // bins of equal width in t
+constexpr int kNthMost = 16;
+
+template <int NT, int NV>
+struct TileLds {
+  static constexpr int kList = NT == kWave ? 256 : NT == 256 ? 512 : 1024;
+  static constexpr int kChunks = NV * NT / kWave;
+  union {
+    GeneralLds<NT> general;
+    uint64_t mass[kBins];
+    struct {
+      uint64_t list[kList];  // key (inverted) and class: in the order when ascending
+      uint32_t weight[kList], share[kList];
+    };
+  };
+  uint64_t chunk[kChunks];
+  uint64_t red[NT / kWave];
+  uint64_t above;
+  float fred[NT / kWave];
+  uint32_t ured[NT / kWave];
+  int ired[NT / kWave];
+  uint32_t n_list, part;
+};
+
+// 0, which the compiler does not know.
+__device__ __forceinline__ int opaque_zero() {
+  int v = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(v));
+#endif
+  return v;
+}
+
+__device__ __forceinline__ uint64_t entry(uint32_t key, int j) { return (uint64_t)~key << 32 | (uint32_t)j; }
+__device__ __forceinline__ float logit_of(uint64_t e) { return of_key(~(uint32_t)(e >> 32)); }
+
+// Draws from the n collected elements, which hold all that can be kept. sum: the weight that top-p is a part of; 0:
+// that of the first k elements.
+template <class T, int NT, int NV>
+__device__ __forceinline__ void draw_from_list(const Sample& a, int64_t r, const RowSettings& set, const Weigh& weigh,
+                                               int n, uint64_t sum, TileLds<NT, NV>& s) {
+  constexpr int kEach = TileLds<NT, NV>::kList / NT;
+  const int tid = threadIdx.x;
+  for (int e = tid; e < n; e += NT) s.weight[e] = weigh(logit_of(s.list[e]));
+  __syncthreads();
+  uint64_t before[kEach];
+  uint64_t first = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int e = tid + i * NT;
+    before[i] = UINT64_MAX;
+    if (e < n) {
+      const uint64_t mine = s.list[e];
+      uint64_t b = 0;
+      int rank = 0;
+#pragma unroll 4
+      for (int o = 0; o < n; ++o) {
+        const bool ahead = s.list[o] < mine;
+        rank += ahead;
+        b += ahead ? s.weight[o] : 0;
+      }
+      if (rank < set.k) {
+        before[i] = b;
+        first += s.weight[e];
+      }
+    }
+  }
+  if (sum == 0) sum = block_sum64<NT>(first, s.red);
+  const uint64_t limit = set.limit(sum);
+  uint64_t total = 0, count = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int e = tid + i * NT;
+    if (e < n) {
+      const uint32_t w = before[i] < limit && weigh.e(logit_of(s.list[e])) >= set.min_p ? s.weight[e] : 0;
+      s.share[e] = w;
+      total += w;
+      count += w != 0;
+    }
+  }
+  total = block_sum64<NT>(total, s.red);
+  count = block_sum64<NT>(count, s.red);
+  __syncthreads();  // the shares, in a block of one wave too
+  const uint64_t point = set.point(total);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int e = tid + i * NT;
+    const uint32_t w = e < n ? s.share[e] : 0;
+    if (w) {
+      const uint32_t j = (uint32_t)s.list[e];
+      uint64_t b = 0;
+#pragma unroll 4
+      for (int o = 0; o < n; ++o) b += (uint32_t)s.list[o] < j ? s.share[o] : 0;
+      if (b <= point && point < b + w) a.answer(r, (int)j, log_share(weigh, logit_of(s.list[e]), total), (int)count);
+    }
+  }
+}
+
+// False where the row takes the general way.
+template <class T, int NT, int NV>
+__device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, const Row<T>& row,
+                                                    const RowSettings& set, TileLds<NT, NV>& s) {
+  constexpr int kVec = Row<T>::kVec;
+  constexpr int kWaves = NT / kWave;
+  constexpr int kList = TileLds<NT, NV>::kList;
+  const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+  Tile<T, NT, NV> tile;
+  tile.load(row);
+  // the largest value and a bound that at least `want` values reach
+  const bool few = set.k <= kNthMost * kWaves;  // what top-k keeps can be collected
+  const int nth = few ? (set.k + kWaves - 1) / kWaves : max(4, kNthMost / kWaves);
+  float most = -INFINITY;
+  bool nan = false;
+  tile.each_unrolled(row, [&](const float (&x)[kVec], int, int) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      most = fmaxf(most, x[i]);
+      nan |= x[i] != x[i];
+    }
+  });
+  const uint32_t own = nan ? 0u : key_of(most);  // 0 is no value's key
+  uint32_t high = wave_max_u32(own);
+  uint32_t bound = wave_nth(own, nth);
+  bool odd = __ballot(nan) != 0;
+  if (tid == 0) s.n_list = 0;
+  if (NT > kWave) {
+    if (lane == 0) {
+      s.ured[wave] = odd ? 0u : bound;
+      s.fred[wave] = of_key(high);
+    }
+    __syncthreads();
+    float m = s.fred[0];
+    bound = s.ured[0];
+#pragma unroll
+    for (int k = 1; k < kWaves; ++k) {
+      bound = min(bound, s.ured[k]);
+      m = fmaxf(m, s.fred[k]);
+    }
+    odd = bound == 0;
+    high = key_of(m);
+  }
+  __syncthreads();
+  const float m = of_key(high);
+  if (odd || isinf(m) || (!few && set.k < a.C)) return false;
+  const Weigh weigh{m, 1.0f / set.temperature};
+  if (set.k == 1) {  // the first of the largest
+    int at = INT32_MAX;
+    tile.each(row, [&](const float (&x)[kVec], int q, int) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i)
+        if (x[i] == m) at = min(at, row.first(q) + i);
+    });
+    at = block_reduce<NT>(at, [](int x, int y) { return min(x, y); }, s.ired);
+    if (tid == 0) a.answer(r, at, 0.0f, 1);
+    return true;
+  }
+  const float least = of_key(bound);
+  uint32_t cut_key = 0;
+  int last = a.C;  // class of the last kept element at the cut
+  const auto bin_of = [&](float t) { return min(kBins - 1, (int)(t * -kBinsPer)); };
+  // One loop over the row for all passes: the exponential's code is there once.
+  //   kCollect  the elements that reach the bound (all that top-k keeps)
+  //   kSum      the same, and the sum of all weights: perhaps the elements reach top-p of it
+  //   kBin      else the weights by t
+  //   kPart     and the elements of the part with the cut
+  //   kShare    the kept weights of runs of 64 vectors, which follow one another in the order of the classes
+  enum { kCollect, kSum, kBin, kPart, kShare };
+  int mode = few ? kCollect : set.top_p < 1.0f ? kSum : kShare;
+  uint64_t sum = 0, limit = 0, above = 0, count = 0;
+  int part = 0, n = 0;
+  for (;;) {
+    count = 0;
+    uint64_t own_sum = 0;
+    tile.each(row, [&](const float (&x)[kVec], int q, int) {
+      // hidden from the compiler, which would make a loop of its own for every mode
+      const int mode_here = __builtin_amdgcn_readfirstlane(mode + opaque_zero());
+      uint64_t v = 0;
+      bool any = mode_here > kSum;
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) any |= x[i] >= least;
+      if (mode_here == kCollect) {
+        if (any) {
+#pragma unroll
+          for (int i = 0; i < kVec; ++i)
+            if (x[i] >= least && x[i] > -INFINITY) {
+              const uint32_t at = atomicAdd(&s.n_list, 1u);
+              if (at < (uint32_t)kList) s.list[at] = entry(key_of(x[i]), row.first(q) + i);
+            }
+        }
+        return;
+      }
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const float t = weigh.t(x[i]), e = expf(t);
+        uint32_t w = weigh.of(x[i], e);
+        bool take = false;
+        if (mode_here == kSum) {
+          take = x[i] >= least && x[i] > -INFINITY;
+        } else if (mode_here == kBin) {
+          if (w) atomicAdd((unsigned long long*)&s.mass[bin_of(t)], (unsigned long long)w);
+        } else if (mode_here == kPart) {
+          take = w && bin_of(t) == part;
+        } else {
+          const uint32_t key = key_of(x[i]);
+          const bool in = (key > cut_key || (key == cut_key && row.first(q) + i <= last)) && e >= set.min_p;
+          w = in ? w : 0;
+          count += w != 0;
+        }
+        v += w;
+        if (take) {
+          const uint32_t at = atomicAdd(&s.n_list, 1u);
+          if (at < (uint32_t)kList) s.list[at] = entry(key_of(x[i]), row.first(q) + i);
+        }
+      }
+      own_sum += v;
+      if (mode_here == kShare) {
+        v = wave_sum64(v);
+        if (lane == 0) s.chunk[q / kWave] = v;
+      }
+    });
+    if (mode == kShare) break;
+    __syncthreads();
+    n = (int)s.n_list;
+    if (mode == kCollect || mode == kPart) {
+      if (n > kList) return false;
+    }
+    bool draw = mode == kCollect;
+    if (mode == kSum) {
+      sum = block_sum64<NT>(own_sum, s.red);
+      limit = set.limit(sum);
+      if (n <= kList) {
+        uint64_t listed = 0;
+        for (int e = tid; e < n; e += NT) listed += weigh(logit_of(s.list[e]));
+        draw = block_sum64<NT>(listed, s.red) >= limit;
+      }
+    }
+    if (draw) {
+      __syncthreads();
+      draw_from_list<T, NT, NV>(a, r, set, weigh, n, sum, s);
+      return true;
+    }
+    if (mode == kSum) {
+      __syncthreads();
+      for (int b = tid; b < kBins; b += NT) s.mass[b] = 0;
+      if (tid == 0) s.n_list = 0;
+      __syncthreads();
+      mode = kBin;
+    } else if (mode == kBin) {
+      constexpr int kEach = kBins / NT;
+      uint64_t b = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) b += s.mass[tid * kEach + i];
+      b = block_exclusive<NT>(b, s.red);
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const uint64_t w = s.mass[tid * kEach + i];
+        if (b < limit && b + w >= limit) {
+          s.part = tid * kEach + i;
+          s.above = b;
+        }
+        b += w;
+      }
+      __syncthreads();
+      part = (int)s.part;
+      above = s.above;
+      mode = kPart;
+    } else {
+      for (int e = tid; e < n; e += NT) s.weight[e] = weigh(logit_of(s.list[e]));
+      __syncthreads();
+      for (int e = tid; e < n; e += NT) {
+        const uint64_t mine = s.list[e];
+        uint64_t before = above;
+#pragma unroll 4
+        for (int o = 0; o < n; ++o) before += s.list[o] < mine ? s.weight[o] : 0;
+        if (before < limit && before + s.weight[e] >= limit) {  // the last kept
+          s.ured[0] = ~(uint32_t)(mine >> 32);
+          s.ired[0] = (int)(uint32_t)mine;
+        }
+      }
+      __syncthreads();
+      cut_key = s.ured[0];
+      last = s.ired[0];
+      mode = kShare;
+    }
+  }
+  const int runs = (row.Q + NT - 1) / NT * kWaves;
+  for (int c = runs + tid; c < TileLds<NT, NV>::kChunks; c += NT) s.chunk[c] = 0;
+  count = block_sum64<NT>(count, s.red);
+  __syncthreads();
+  // every wave for itself: the run of the point
+  constexpr int kChunks = TileLds<NT, NV>::kChunks;
+  constexpr int kOwn = (kChunks + kWave - 1) / kWave;
+  uint64_t v = 0;
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) v += lane * kOwn + i < kChunks ? s.chunk[lane * kOwn + i] : 0;
+  const uint64_t upto = wave_upto64(v), total = lane_of64(upto, kWave - 1);
+  const uint64_t point = set.point(total);
+  const int at = (int)__builtin_ctzll(__ballot(upto > point));
+  uint64_t target = point - lane_of64(upto - v, at);
+  int run = at * kOwn;
+#pragma unroll
+  for (int i = 0; i < kOwn - 1; ++i) {
+    const uint64_t w = s.chunk[run];
+    if (target >= w) {
+      target -= w;
+      ++run;
+    }
+  }
+  if (wave != 0) return true;
+  const auto share = [&](float x, int j) -> uint64_t {
+    const uint32_t key = key_of(x);
+    const float e = weigh.e(x);
+    return (key > cut_key || (key == cut_key && j <= last)) && e >= set.min_p ? weigh.of(x, e) : 0;
+  };
+  const int j = find_in_order<T, kWave>(row, share, target, nullptr, run * kWave, min(row.Q, (run + 1) * kWave));
+  if (lane == 0) a.answer(r, j, log_share(weigh, row.at(j), total), (int)count);
+  return true;
+}
+
+template <class T, int NT, int NV>
+__global__ __launch_bounds__(NT) void sample_tile(Sample a) {
+  __shared__ TileLds<NT, NV> s;
+  const int64_t r = blockIdx.x;
+  const Row<T> row(a.logits, r, a.ld, a.C);
+  const RowSettings set(a.set, r, a.C);
+  if (!sample_in_registers<T, NT, NV>(a, r, row, set, s)) sample_general<T, NT>(a, r, row, set, s.general);
 }
 
 }  // namespace
@@ -170,17 +530,22 @@ extern "C" snn_status snn_readout_sample(const void* logits, int dtype, int64_t 
   const snn_status ok = rows::check_rows(logits, dtype, R, C, ld);
   if (ok != SNN_OK) return ok;
   if (!u || !cls) return SNN_ERR_INVALID_ARG;
-  const Settings set{u, temperature, top_k, top_p, min_p};
+  const Sample a{logits, R, C, ld, Settings{u, temperature, top_k, top_p, min_p}, cls, logp, kept};
   hipStream_t s = static_cast<hipStream_t>(stream);
+  const dim3 grid((unsigned)R);
   return rows::for_type(dtype, [&](auto type) {
     using T = decltype(type);
-    if (C <= 1024)
-      hipLaunchKernelGGL((sample_rows<T, 64>), dim3((unsigned)R), dim3(64), 0, s, logits, C, ld, set, cls, logp, kept);
-    else if (C <= 16384)
-      hipLaunchKernelGGL((sample_rows<T, 256>), dim3((unsigned)R), dim3(256), 0, s, logits, C, ld, set, cls, logp, kept);
+    const int Q = rows::most_vectors<T>(logits, C, ld);
+    if (Q <= 4 * 64)
+      hipLaunchKernelGGL((sample_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
+    else if (Q <= 4 * 256)
+      hipLaunchKernelGGL((sample_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
+    else if (Q <= 4 * 1024)
+      hipLaunchKernelGGL((sample_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
+    else if (Q <= 16 * 1024)
+      hipLaunchKernelGGL((sample_tile<T, 1024, 16>), grid, dim3(1024), 0, s, a);
     else
-      hipLaunchKernelGGL((sample_rows<T, 1024>), dim3((unsigned)R), dim3(1024), 0, s, logits, C, ld, set, cls, logp,
-                         kept);
+      hipLaunchKernelGGL((sample_rows<T, 1024>), grid, dim3(1024), 0, s, a);
     return launch_status();
   });
 }

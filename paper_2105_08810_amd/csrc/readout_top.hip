@@ -53,6 +53,7 @@ __device__ __forceinline__ void write_record(const Row<T>& row, const Top& a, in
     if (e < n) {
       const uint64_t mine = list[e];
       place = 0;
+#pragma unroll 4
       for (int o = 0; o < n; ++o) place += list[o] < mine;
       id = (int)(uint32_t)mine;
       if (place < a.K) v = row.at(id);
@@ -90,7 +91,7 @@ __device__ __forceinline__ void top_general(const Row<T>& row, const Top& a, int
   const auto add = [](auto x, auto y) { return x + y; };
   m = block_reduce<NT>(m, larger, s.fred);
   least = block_reduce<NT>(least, smaller, s.fred);
-  count = block_reduce<NT>(count, add, s.select.red);
+  count = block_sum64<NT>(count, s.select.red);
   if (a.lse) {
     float sum = 0.0f;
     const float safe = isinf(m) ? 0.0f : m;
@@ -107,12 +108,12 @@ __device__ __forceinline__ void top_general(const Row<T>& row, const Top& a, int
   int last = a.C;  // class of the last listed element at the cut
   if (count > (uint64_t)a.K) {
     const auto one = [](float x) { return (uint32_t)(x > -INFINITY); };
-    const Cut c = find_cut<T, NT, false>(row, one, key_of(least), key_of(m), (uint64_t)a.K, s.select);
+    const Cut c = find_cut<T, NT, false>(row, one, key_of(least), key_of(m), (uint64_t)a.K, false, s.select);
     cut_key = c.key;
     const uint32_t ties = a.K - c.above_count;
     if (ties < c.equal)
       last = find_in_order<T, NT>(row, [&](float x, int) { return (uint64_t)(key_of(x) == cut_key); }, ties - 1,
-                                  s.select.red);
+                                  s.select.red, 0, row.Q);
   }
   __syncthreads();
   if (tid == 0) s.n_taken = 0;
@@ -140,19 +141,17 @@ __global__ __launch_bounds__(NT) void top_rows(Top a) {
   top_general<T, NT>(Row<T>(a.logits, r, a.ld, a.C), a, r, s);
 }
 
+// False where the row takes the general way.
 template <class T, int NT, int NV>
-__global__ __launch_bounds__(NT) void top_tile(Top a) {
-  __shared__ TopLds<NT> s;
+__device__ __forceinline__ bool top_in_registers(const Row<T>& row, const Top& a, int64_t r, TopLds<NT>& s) {
   constexpr int kVec = Row<T>::kVec;
   constexpr int kWaves = NT / kWave;
-  const int64_t r = blockIdx.x;
   const int tid = threadIdx.x;
-  const Row<T> row(a.logits, r, a.ld, a.C);
   Tile<T, NT, NV> tile;
   tile.load(row);
   float most = -INFINITY;
   bool nan = false;
-  tile.each(row, [&](const float (&x)[kVec], int) {
+  tile.each_unrolled(row, [&](const float (&x)[kVec], int, int) {
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       most = fmaxf(most, x[i]);
@@ -184,14 +183,12 @@ __global__ __launch_bounds__(NT) void top_tile(Top a) {
     __syncthreads();
   }
   const float m = of_key(high);
-  if (odd || isinf(m)) {
-    __syncthreads();
-    return top_general<T, NT>(row, a, r, s);
-  }
+  if (odd || isinf(m)) return false;
   const float least = of_key(bound);
   const float c = a.inv * kLog2e, mc = m * c;
   float sum = 0.0f;
-  tile.each(row, [&](const float (&x)[kVec], int q) {
+  uint32_t some = 0;  // the vectors with a value that reaches the bound
+  tile.each_unrolled(row, [&](const float (&x)[kVec], int, int n) {
     float part = 0.0f;
     bool any = false;
 #pragma unroll
@@ -200,26 +197,42 @@ __global__ __launch_bounds__(NT) void top_tile(Top a) {
       any |= x[i] >= least;
     }
     sum += part;
-    if (any) {
+    some |= any ? 1u << n : 0u;
+  });
+#pragma unroll 1
+  for (int n = 0; n < NV; ++n) {
+    if (__ballot(some >> n & 1) == 0) continue;
+    if (some >> n & 1) {
+      float x[kVec];
+      unpack<T>(tile.get(n), x);
 #pragma unroll
       for (int i = 0; i < kVec; ++i)
         if (x[i] >= least && x[i] > -INFINITY) {
           const uint32_t at = atomicAdd(&s.n_taken, 1u);
-          if (at < (uint32_t)TopLds<NT>::kList) s.list[at] = entry(key_of(x[i]), row.first(q) + i);
+          if (at < (uint32_t)TopLds<NT>::kList) s.list[at] = entry(key_of(x[i]), row.first(n * NT + tid) + i);
         }
     }
-  });
+  }
   if (a.lse) {
     sum = block_reduce<NT>(sum, [](float x, float y) { return x + y; }, s.fred);
     if (tid == 0) a.lse[r] = m * a.inv + logf(sum);
   }
   __syncthreads();
   const int n = (int)s.n_taken;
-  if (n > TopLds<NT>::kList) {
-    __syncthreads();
-    return top_general<T, NT>(row, a, r, s);
-  }
+  if (n > TopLds<NT>::kList) return false;
   write_record<T, NT>(row, a, r, s.list, n);
+  return true;
+}
+
+template <class T, int NT, int NV>
+__global__ __launch_bounds__(NT) void top_tile(Top a) {
+  __shared__ TopLds<NT> s;
+  const int64_t r = blockIdx.x;
+  const Row<T> row(a.logits, r, a.ld, a.C);
+  if (!top_in_registers<T, NT, NV>(row, a, r, s)) {
+    __syncthreads();
+    top_general<T, NT>(row, a, r, s);
+  }
 }
 
 }  // namespace

@@ -56,21 +56,7 @@ struct Row {
   __device__ __forceinline__ int first(int q) const { return q * kVec - lead; }  // class of vector q's first element
   __device__ __forceinline__ bool whole(int q) const { return first(q) >= 0 && first(q) + kVec <= C; }
   __device__ __forceinline__ float at(int j) const { return to_float(base[lead + j]); }
-  // Vector q, -inf outside the row.
-  __device__ __forceinline__ void load(int q, float (&x)[kVec]) const {
-    if (whole(q)) {
-      T v[kVec];
-      __builtin_memcpy(v, __builtin_assume_aligned(base + (size_t)q * kVec, 16), 16);
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) x[i] = to_float(v[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const int j = first(q) + i;
-        x[i] = j >= 0 && j < C ? at(j) : -INFINITY;
-      }
-    }
-  }
+  __device__ __forceinline__ void load(int q, float (&x)[kVec]) const;  // vector q, -inf outside the row
 };
 
 template <class T>
@@ -88,20 +74,25 @@ __device__ __forceinline__ F16 lowest<F16>() {
   return F16{0xfc00};
 }
 
-// Vector q of a row as it lies in memory, -inf outside the row.
+// Vector q of a row as it lies in memory, -inf outside the row. The ends of a row are put together in a loop: its code
+// is in every pass.
 template <class T>
 __device__ __forceinline__ uint4 load_raw(const Row<T>& row, int q) {
   constexpr int kVec = Row<T>::kVec;
+  constexpr int kBits = 8 * (int)sizeof(T);
   if (row.whole(q)) return *reinterpret_cast<const uint4*>(row.base + (size_t)q * kVec);
-  T v[kVec];
-#pragma unroll
-  for (int i = 0; i < kVec; ++i) {
+  uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+  for (int i = kVec - 1; i >= 0; --i) {
     const int j = row.first(q) + i;
-    v[i] = j >= 0 && j < row.C ? row.base[(size_t)q * kVec + i] : lowest<T>();
+    T v = lowest<T>();
+    if (j >= 0 && j < row.C) v = row.base[(size_t)q * kVec + i];
+    uint32_t bits = 0;
+    __builtin_memcpy(&bits, &v, sizeof(T));
+    hi = hi << kBits | lo >> (64 - kBits);
+    lo = lo << kBits | bits;
   }
-  uint4 u;
-  __builtin_memcpy(&u, v, 16);
-  return u;
+  return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
 }
 
 // Values of vector q back to a row, those inside it.
@@ -112,14 +103,21 @@ __device__ __forceinline__ void store_vec(const Row<T>& row, int q, const float 
 #pragma unroll
   for (int i = 0; i < kVec; ++i) v[i] = from_float<T>(x[i]);
   T* p = const_cast<T*>(row.base) + (size_t)q * kVec;
+  uint4 u;
+  __builtin_memcpy(&u, v, 16);
   if (row.whole(q)) {
-    uint4 u;
-    __builtin_memcpy(&u, v, 16);
     *reinterpret_cast<uint4*>(p) = u;
   } else {
-#pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      if (row.first(q) + i >= 0 && row.first(q) + i < row.C) p[i] = v[i];
+    constexpr int kBits = 8 * (int)sizeof(T);
+    uint64_t lo = (uint64_t)u.y << 32 | u.x, hi = (uint64_t)u.w << 32 | u.z;
+#pragma unroll 1
+    for (int i = 0; i < kVec; ++i) {
+      T one;
+      __builtin_memcpy(&one, &lo, sizeof(T));
+      if (row.first(q) + i >= 0 && row.first(q) + i < row.C) p[i] = one;
+      lo = lo >> kBits | hi << (64 - kBits);
+      hi >>= kBits;
+    }
   }
 }
 
@@ -131,25 +129,76 @@ __device__ __forceinline__ void unpack(const uint4& u, float (&x)[16 / sizeof(T)
   for (int i = 0; i < (int)(16 / sizeof(T)); ++i) x[i] = to_float(v[i]);
 }
 
-// A row in a block's registers: vector i * NT + thread of it in v[i].
+template <class T>
+__device__ __forceinline__ void Row<T>::load(int q, float (&x)[kVec]) const {
+  unpack<T>(load_raw(*this, q), x);
+}
+
+// A row in a block's registers: vector i * NT + thread of it as element i of four register arrays. Long passes over it
+// are loops whose counter selects the registers: unrolled, the passes of a wide tile are straight code of tens of KB,
+// and a block then waits for instructions at nearly every line (1024 rows of 65536 drawn from: 620 us unrolled, 210 so).
 template <class T, int NT, int NV>
 struct Tile {
-  uint4 v[NV];
-  __device__ __forceinline__ void load(const Row<T>& row) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (i * NT < row.Q) v[i] = load_raw(row, i * NT + (int)threadIdx.x);
+  typedef uint32_t Words __attribute__((ext_vector_type(NV)));
+  Words w[4];
+  __device__ __forceinline__ uint4 get(int i) const { return make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]); }
+  __device__ __forceinline__ void set(int i, const uint4& u) {
+    w[0][i] = u.x;
+    w[1][i] = u.y;
+    w[2][i] = u.z;
+    w[3][i] = u.w;
   }
-  // f(values, vector) for the thread's vectors
+  __device__ __forceinline__ void load(const Row<T>& row) {
+    constexpr int kVec = Row<T>::kVec;
+    const int tid = (int)threadIdx.x;
+    const int from = row.lead ? 1 : 0, to = (row.lead + row.C) / kVec;  // whole vectors
+    uint4 none;
+    {
+      T v[kVec];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[i] = lowest<T>();
+      __builtin_memcpy(&none, v, 16);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int q = i * NT + tid;
+      uint4 u = none;
+      if (q >= from && q < to) u = *reinterpret_cast<const uint4*>(row.base + (size_t)q * kVec);
+      set(i, u);
+    }
+    // the ends of the row (every thread sets its vector anew: a branch around it would keep two copies of the tile)
+    if (from == 1) {
+      uint4 u = get(0);
+      if (tid == 0) u = load_raw(row, 0);
+      set(0, u);
+    }
+    if (to < row.Q && row.Q > from) {
+      const int i = to / NT;
+      uint4 u = get(i);
+      if (tid == to - i * NT) u = load_raw(row, to);
+      set(i, u);
+    }
+  }
+  // As each(), unrolled: for a few instructions a value.
   template <class F>
-  __device__ __forceinline__ void each(const Row<T>& row, F f) const {
+  __device__ __forceinline__ void each_unrolled(const Row<T>& row, F f) const {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (i * NT < row.Q) {
         float x[Row<T>::kVec];
-        unpack<T>(v[i], x);
-        f(x, i * NT + (int)threadIdx.x);
+        unpack<T>(get(i), x);
+        f(x, i * NT + (int)threadIdx.x, i);
       }
+  }
+  // f(values, vector, its number in the thread)
+  template <class F>
+  __device__ __forceinline__ void each(const Row<T>& row, F f) const {
+#pragma unroll 1
+    for (int i = 0; i * NT < row.Q; ++i) {
+      float x[Row<T>::kVec];
+      unpack<T>(get(i), x);
+      f(x, i * NT + (int)threadIdx.x, i);
+    }
   }
 };
 
@@ -215,7 +264,28 @@ __device__ __forceinline__ float of_key(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 
-__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int off) { return __shfl_up((unsigned long long)v, off, kWave); }
+// A 64-bit value from the lane that a step names, 0 where there is none or `rows` leaves the row of 16 out.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint64_t from_lane64(uint64_t v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+  return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t lane_of64(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+// Sums over the lanes up to each.
+__device__ __forceinline__ uint64_t wave_upto64(uint64_t v) {
+  v += from_lane64<0x111>(v);  // within rows of 16
+  v += from_lane64<0x112>(v);
+  v += from_lane64<0x114>(v);
+  v += from_lane64<0x118>(v);
+  v += from_lane64<0x142, 0xa>(v);  // rows 0 and 2 to the next, then the lower half to the upper
+  v += from_lane64<0x143, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ uint64_t wave_sum64(uint64_t v) { return lane_of64(wave_upto64(v), kWave - 1); }
 
 // Block reductions and scans; every thread of the block takes part and gets the result. `red` holds NT / kWave
 // values in LDS and may be reused at once.
@@ -227,31 +297,30 @@ __device__ __forceinline__ V block_reduce(V v, F f, V* red) {
   __syncthreads();
   if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
   __syncthreads();
-  V r = red[0];
+  v = red[threadIdx.x % (NT / kWave)];
 #pragma unroll
-  for (int k = 1; k < NT / kWave; ++k) r = f(r, red[k]);
-  return r;
+  for (int off = NT / kWave / 2; off > 0; off >>= 1) v = f(v, __shfl_xor(v, off, kWave));
+  return v;
 }
 
 template <int NT>
-__device__ __forceinline__ uint64_t block_exclusive(uint64_t v, uint64_t* red, uint64_t& total) {
-  uint64_t incl = v;
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const uint64_t u = shfl_up64(incl, off);
-    if ((int)(threadIdx.x % kWave) >= off) incl += u;
-  }
+__device__ __forceinline__ uint64_t block_sum64(uint64_t v, uint64_t* red) {
+  v = wave_sum64(v);
+  if (NT == kWave) return v;
   __syncthreads();
-  if (threadIdx.x % kWave == kWave - 1) red[threadIdx.x / kWave] = incl;
+  if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
   __syncthreads();
-  uint64_t before = 0;
-  total = 0;
-#pragma unroll
-  for (int k = 0; k < NT / kWave; ++k) {
-    before += k < (int)(threadIdx.x / kWave) ? red[k] : 0;
-    total += red[k];
-  }
-  return before + incl - v;
+  return wave_sum64(threadIdx.x % kWave < NT / kWave ? red[threadIdx.x % kWave] : 0);
+}
+
+template <int NT>
+__device__ __forceinline__ uint64_t block_exclusive(uint64_t v, uint64_t* red) {
+  const uint64_t upto = wave_upto64(v);
+  const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
+  __syncthreads();
+  if (l == kWave - 1) red[w] = upto;
+  __syncthreads();
+  return wave_sum64(l < w ? red[l] : 0) + upto - v;
 }
 
 // ------------------------------------------------------------------ selection
@@ -270,7 +339,7 @@ struct SelectLds {
   uint32_t count[kBins];
   uint32_t list[kShort];
   uint64_t red[NT / kWave];
-  uint64_t before_mass, part_mass;
+  uint64_t before_mass;
   uint32_t before_count, part_count, part, n_list;
   uint32_t cut_key, cut_equal;
 };
@@ -282,19 +351,21 @@ struct Cut {
   uint32_t equal;        // elements of that value
 };
 
-// weigh(x) gives an element's weight, 0 for one that is not in the order. BY_MASS: limit is a sum of weights, else a
-// number of elements. The keys of the elements lie in [lo, hi] and their sum or number reaches the limit >= 1.
-template <class T, int NT, bool BY_MASS, class W>
+// weigh(x) gives an element's weight, 0 for one that is not in the order. by_mass: limit is a sum of weights (MASS
+// then), else a number of elements. The keys of the elements lie in [lo, hi] and their sum or number reaches the
+// limit >= 1.
+template <class T, int NT, bool MASS, class W>
 __device__ __forceinline__ Cut find_cut(const Row<T>& row, W weigh, uint32_t lo, uint32_t hi, uint64_t limit,
-                                        SelectLds<NT>& s) {
+                                        bool by_mass, SelectLds<NT>& s) {
   constexpr int kVec = Row<T>::kVec;
   constexpr int kBins = SelectLds<NT>::kBins;
   const int tid = threadIdx.x;
   uint64_t above_mass = 0;
   uint32_t above_count = 0;
+  bool listing = false;  // the range is short enough to be compared element by element
   for (;;) {
     int shift = 0;
-    while (((hi - lo) >> shift) >= kBins) ++shift;
+    while (((hi - lo) >> shift) >= (uint32_t)kBins) ++shift;
     __syncthreads();
     for (int b = tid; b < kBins; b += NT) {
       s.mass[b] = 0;
@@ -302,6 +373,7 @@ __device__ __forceinline__ Cut find_cut(const Row<T>& row, W weigh, uint32_t lo,
     }
     if (tid == 0) s.n_list = 0;
     __syncthreads();
+#pragma unroll 1
     for (int q = tid; q < row.Q; q += NT) {
       float x[kVec];
       row.load(q, x);
@@ -311,13 +383,18 @@ __device__ __forceinline__ Cut find_cut(const Row<T>& row, W weigh, uint32_t lo,
         const uint32_t k = key_of(y);
         const uint32_t w = k >= lo && k <= hi ? weigh(y) : 0;
         if (w) {
-          const uint32_t b = (hi - k) >> shift;
-          atomicAdd(&s.count[b], 1u);
-          if (BY_MASS) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)w);
+          if (listing) {
+            s.list[atomicAdd(&s.n_list, 1u)] = k;
+          } else {
+            const uint32_t b = (hi - k) >> shift;
+            atomicAdd(&s.count[b], 1u);
+            if (MASS) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)w);
+          }
         }
       }
     }
     __syncthreads();
+    if (listing) break;
     constexpr int kEach = kBins / NT;
     uint64_t m = 0, n = 0;
 #pragma unroll
@@ -325,18 +402,16 @@ __device__ __forceinline__ Cut find_cut(const Row<T>& row, W weigh, uint32_t lo,
       m += s.mass[tid * kEach + i];
       n += s.count[tid * kEach + i];
     }
-    uint64_t all;
-    n = above_count + block_exclusive<NT>(n, s.red, all);
-    m = BY_MASS ? above_mass + block_exclusive<NT>(m, s.red, all) : 0;
+    n = above_count + block_exclusive<NT>(n, s.red);
+    m = MASS ? above_mass + block_exclusive<NT>(m, s.red) : 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const uint32_t c = s.count[tid * kEach + i];
       const uint64_t w = s.mass[tid * kEach + i];
-      const uint64_t at = BY_MASS ? m : n, to = BY_MASS ? m + w : n + c;
+      const uint64_t at = by_mass ? m : n, to = by_mass ? m + w : n + c;
       if (at < limit && to >= limit) {
         s.part = tid * kEach + i;
         s.part_count = c;
-        s.part_mass = w;
         s.before_count = (uint32_t)n;
         s.before_mass = m;
       }
@@ -350,33 +425,23 @@ __device__ __forceinline__ Cut find_cut(const Row<T>& row, W weigh, uint32_t lo,
     const uint32_t width = (1u << shift) - 1;
     lo = hi - lo > width ? hi - width : lo;
     if (lo == hi) return Cut{hi, above_mass, above_count, s.part_count};
-    if (s.part_count <= kShort) break;
+    listing = s.part_count <= kShort;
   }
-  for (int q = tid; q < row.Q; q += NT) {
-    float x[kVec];
-    row.load(q, x);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      const float y = no_nan(x[i]);
-      const uint32_t k = key_of(y);
-      if (k >= lo && k <= hi && weigh(y)) s.list[atomicAdd(&s.n_list, 1u)] = k;
-    }
-  }
-  __syncthreads();
   const int n = (int)s.n_list;
   for (int e = tid; e < n; e += NT) {
     const uint32_t k = s.list[e];
     uint64_t m = above_mass;
     uint32_t c = above_count, equal = 0;
+#pragma unroll 1
     for (int o = 0; o < n; ++o) {
       const uint32_t ko = s.list[o];
       if (ko > k) {
         ++c;
-        if (BY_MASS) m += weigh(of_key(ko));
+        if (MASS) m += weigh(of_key(ko));
       }
       equal += ko == k;
     }
-    const uint64_t at = BY_MASS ? m : c, to = BY_MASS ? m + (uint64_t)equal * weigh(of_key(k)) : (uint64_t)c + equal;
+    const uint64_t at = by_mass ? m : c, to = by_mass ? m + (uint64_t)equal * weigh(of_key(k)) : (uint64_t)c + equal;
     if (at < limit && to >= limit) {  // every element of the value says the same
       s.cut_key = k;
       s.cut_equal = equal;
@@ -388,11 +453,11 @@ __device__ __forceinline__ Cut find_cut(const Row<T>& row, W weigh, uint32_t lo,
   return Cut{s.cut_key, s.before_mass, s.before_count, s.cut_equal};
 }
 
-// The first class whose sum of f over the classes up to it exceeds `target`, which the whole row's sum does.
-// f(x, class) is a weight. The range of vectors is divided among the block's waves until one wave's share is a vector
-// for each lane.
+// The first class in the vectors [lo, hi) whose sum of f over the classes from lo to it exceeds `target`, which their
+// whole sum does. f(x, class) is a weight. The range is divided among the block's waves until one wave's share is a
+// vector for each lane.
 template <class T, int NT, class F>
-__device__ __forceinline__ int find_in_order(const Row<T>& row, F f, uint64_t target, uint64_t* red) {
+__device__ __forceinline__ int find_in_order(const Row<T>& row, F f, uint64_t target, uint64_t* red, int lo, int hi) {
   constexpr int kVec = Row<T>::kVec;
   constexpr int kWaves = NT / kWave;
   const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
@@ -407,7 +472,6 @@ __device__ __forceinline__ int find_in_order(const Row<T>& row, F f, uint64_t ta
     }
     return v;
   };
-  int lo = 0, hi = row.Q;
   while (hi - lo > kWave) {
     int share = (hi - lo + kWaves - 1) / kWaves;
     share = kWaves == 1 ? kWave : share;
@@ -416,8 +480,7 @@ __device__ __forceinline__ int find_in_order(const Row<T>& row, F f, uint64_t ta
       const int a = from + w * share, b = min(hi, a + share);
       uint64_t v = 0;
       for (int q = a + l; q < b; q += kWave) v += sum_of(q);
-#pragma unroll
-      for (int off = kWave / 2; off > 0; off >>= 1) v += __shfl_xor((unsigned long long)v, off, kWave);
+      v = wave_sum64(v);
       __syncthreads();
       if (l == 0) red[w] = v;
       __syncthreads();
@@ -434,14 +497,9 @@ __device__ __forceinline__ int find_in_order(const Row<T>& row, F f, uint64_t ta
     hi = min(hi, lo + share);
   }
   // every wave does the last step
-  uint64_t v = lo + l < hi ? sum_of(lo + l) : 0, incl = v;
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const uint64_t u = shfl_up64(incl, off);
-    if (l >= off) incl += u;
-  }
-  const int lane = (int)__builtin_ctzll(__ballot(incl > target));
-  target -= __shfl((unsigned long long)(incl - v), lane, kWave);
+  const uint64_t v = lo + l < hi ? sum_of(lo + l) : 0, upto = wave_upto64(v);
+  const int lane = (int)__builtin_ctzll(__ballot(upto > target));
+  target -= lane_of64(upto - v, lane);
   const int q = lo + lane;
   float x[kVec];
   row.load(q, x);

@@ -366,20 +366,20 @@ __device__ __forceinline__ void listed_grads(const Distill& a, int64_t r, const 
     });
 }
 
-// x[i] * per of vector q to the gradient's row.
+// Vector q of the gradient.
 template <class T>
 __device__ __forceinline__ void put(const Distill& a, const Row<T>& row, const Row<T>& out, int q,
-                                    const float (&x)[16 / sizeof(T)], float per) {
+                                    const float (&x)[16 / sizeof(T)]) {
   constexpr int kVec = Row<T>::kVec;
   if (out.lead == row.lead) {
     float y[kVec];
     if (a.accumulate) {
       out.load(q, y);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) y[i] += x[i] * per;
+      for (int i = 0; i < kVec; ++i) y[i] += x[i];
     } else {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) y[i] = x[i] * per;
+      for (int i = 0; i < kVec; ++i) y[i] = x[i];
     }
     store_vec(out, q, y);
   } else {
@@ -387,9 +387,30 @@ __device__ __forceinline__ void put(const Distill& a, const Row<T>& row, const R
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       const int j = row.first(q) + i;
-      if (j >= 0 && j < a.C) to[j] = from_float<T>(a.accumulate ? to_float(to[j]) + x[i] * per : x[i] * per);
+      if (j >= 0 && j < a.C) to[j] = from_float<T>(a.accumulate ? to_float(to[j]) + x[i] : x[i]);
     }
   }
+}
+
+// Has the compiler unpack a vector anew where it is used next, instead of keeping its values from the last time: 32
+// registers instead of 64 for a thread's 64 16-bit values.
+__device__ __forceinline__ void forget(uint4& u) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w));
+#endif
+}
+
+// A vector with -inf for the values whose bits are on.
+template <class T>
+__device__ __forceinline__ uint4 without(const uint4& u, uint32_t on) {
+  constexpr int kVec = Row<T>::kVec;
+  T v[kVec];
+  __builtin_memcpy(v, &u, 16);
+#pragma unroll
+  for (int k = 0; k < kVec; ++k) v[k] = on >> k & 1 ? lowest<T>() : v[k];
+  uint4 w;
+  __builtin_memcpy(&w, v, 16);
+  return w;
 }
 
 template <class T, int NT>
@@ -406,8 +427,9 @@ __device__ __forceinline__ void row_without_weight(const Distill& a, int64_t r) 
 }
 
 template <class T, int NT, int NV>
-__global__ __launch_bounds__(NT) void distill_tile(Distill a) {
+__global__ __launch_bounds__(NT, 4) void distill_tile(Distill a) {
   constexpr int kVec = Row<T>::kVec;
+  constexpr bool kKeep = sizeof(T) == 4;  // the exponentials in the logits' place; 16-bit rows form them twice
   __shared__ uint32_t bits[NT * NV * kVec / 32];
   __shared__ Sum2 red[NT / kWave];
   const int64_t r = blockIdx.x;
@@ -416,48 +438,39 @@ __global__ __launch_bounds__(NT) void distill_tile(Distill a) {
   if (w == 0.0f) return row_without_weight<T, NT>(a, r);  // not read: what is there may be anything
   const Row<T> row(a.logits, r, a.ld, a.C);
   const Entries<T> entries(a, r, row);
-  Tile<T, NT, NV> tile;
-  tile.load(row);
+  uint4 raw[NV];
+  load_vectors<T, NT>(row, raw);
   for (int k = tid; k < (row.Q * kVec + 31) / 32; k += NT) bits[k] = 0;
   __syncthreads();
   const Teacher t = teacher_of<T>(a, r, entries, bits);
   __syncthreads();
   const float c = kLog2e / a.tau;
-  // Value k of the thread's vector i, the logit and then its exponential, takes the place of the tile's own float32 or
-  // has one beside it.
-  typedef float Floats __attribute__((ext_vector_type(NV)));
-  Floats e[kVec];
-  const auto keep = [&](int i, int k, float v) {
-    if constexpr (sizeof(T) == 4) tile.w[k][i] = __float_as_uint(v);
-    else e[k][i] = v;
-  };
-  const auto kept = [&](int i, int k) -> float {
-    if constexpr (sizeof(T) == 4) return __uint_as_float(tile.w[k][i]);
-    else return e[k][i];
-  };
   float top = -INFINITY;
-  tile.each_unrolled(row, [&](float (&x)[kVec], int q, int i) {
-    const int v = q * kVec;
-    const uint32_t on = q < row.Q ? bits[v >> 5] >> (v & 31) : 0;
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) {
-      if (on >> k & 1) x[k] = -INFINITY;
-      top = fmaxf(top, x[k]);
-      keep(i, k, x[k]);
-    }
-  });
+  for (int i = 0; i < NV; ++i) {
+    const int q = i * NT + tid, v = q * kVec;
+    const uint32_t on = q < row.Q ? bits[v >> 5] >> (v & 31) & ((1u << kVec) - 1) : 0;
+    if (on) raw[i] = without<T>(raw[i], on);  // few vectors hold a listed class
+    float x[kVec];
+    unpack<T>(raw[i], x);
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) top = fmaxf(top, x[k]);
+    if (!kKeep) forget(raw[i]);
+  }
   top *= c;
   const float safe = or_zero(top);
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    if (i * NT >= row.Q) break;
+    float x[kVec];
+    unpack<T>(raw[i], x);
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      const float y = exp2_fast(fmaf(kept(i, k), c, -safe));
-      keep(i, k, y);
-      sum += y;
+      x[k] = exp2_fast(fmaf(x[k], c, -safe));
+      sum += x[k];
     }
+    if (kKeep) __builtin_memcpy(&raw[i], x, 16);
+    else forget(raw[i]);
   }
   const Sum2 rest = block_join<NT>(Sum2{top, sum}, red);
   const RowSums s = finish_row<T>(entries, t, rest, c);
@@ -469,28 +482,48 @@ __global__ __launch_bounds__(NT) void distill_tile(Distill a) {
   const Row<T> out(a.grad, r, a.ld_grad, a.C);
   const float scale = w / a.tau;
   const float per = top == -INFINITY ? 0.0f : scale * s.factor * exp2_fast(safe - rest.max);
-  if (out.lead == row.lead && !a.accumulate) {
-    const int from = out.lead ? 1 : 0, to = (out.lead + a.C) / kVec;  // whole vectors
+  const auto gradient = [&](const uint4& u, float (&x)[kVec]) {
+    if (kKeep) __builtin_memcpy(x, &u, 16);
+    else unpack<T>(u, x);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int q = i * NT + tid;
+    for (int k = 0; k < kVec; ++k) x[k] = kKeep ? x[k] * per : exp2_fast(fmaf(x[k], c, -safe)) * per;
+  };
+  const bool alike = out.lead == row.lead && !a.accumulate;
+  const int from = out.lead ? 1 : 0, to = (out.lead + a.C) / kVec;  // whole vectors
+  uint4 last = raw[0];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int q = i * NT + tid;
+    if (i > 0 && q == to) last = raw[i];
+    if (alike) {
+      float x[kVec];
       T v[kVec];
+      gradient(raw[i], x);
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) v[k] = from_float<T>(kept(i, k) * per);
+      for (int k = 0; k < kVec; ++k) v[k] = from_float<T>(x[k]);
       uint4 u;
       __builtin_memcpy(&u, v, 16);
       if (q >= from && q < to) *reinterpret_cast<uint4*>(const_cast<T*>(out.base) + (size_t)q * kVec) = u;
     }
   }
+  if (alike) {  // the ends of the row
 #pragma unroll 1
-  for (int i = 0; i * NT < row.Q; ++i) {  // the rest, or all of them
-    const int q = i * NT + tid;
-    if (q < row.Q && (out.lead != row.lead || a.accumulate || !out.whole(q))) {
-      float x[kVec];
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) x[k] = kept(i, k);
-      put(a, row, out, q, x, per);
+    for (int end = 0; end < 2; ++end) {
+      const int q = end ? to : 0;
+      if (end ? to < out.Q && to >= from && tid == to % NT : tid < from) {
+        float x[kVec];
+        gradient(end ? last : raw[0], x);
+        store_vec(out, q, x);
+      }
     }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i * NT + tid < row.Q) {
+        float x[kVec];
+        gradient(raw[i], x);
+        put(a, row, out, i * NT + tid, x);
+      }
   }
   listed_grads<T>(a, r, entries, t, s, c, scale);
 }
@@ -558,8 +591,8 @@ __global__ __launch_bounds__(NT) void distill_rows(Distill a) {
   const float per = scale * s.factor, safe = or_zero(rest.max);
   pass([&](float (&x)[kVec], int q) {
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) x[k] = exp2_fast(fmaf(x[k], c, -safe));
-    put(a, row, out, q, x, per);
+    for (int k = 0; k < kVec; ++k) x[k] = exp2_fast(fmaf(x[k], c, -safe)) * per;
+    put(a, row, out, q, x);
   });
   listed_grads<T>(a, r, entries, t, s, c, scale);
 }

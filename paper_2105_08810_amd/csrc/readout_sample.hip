@@ -84,6 +84,102 @@ __device__ __forceinline__ float log_share(const Weigh& weigh, float x, uint64_t
   return weigh.t(x) - (float)log((double)total * (1.0 / kUnit));
 }
 
+// ------------------------------------------------------------------ short rows, 16 lanes each
+
+template <class T>
+__global__ __launch_bounds__(256) void sample_short(Sample a) {
+  __shared__ uint64_t list[kShortRows][kShortRow];
+  __shared__ uint32_t weight[kShortRows][kShortRow];
+  const int slot = threadIdx.x / 16, l = threadIdx.x % 16;
+  const int64_t r = (int64_t)blockIdx.x * kShortRows + slot;
+  const bool live = r < a.R;
+  const Row<T> row(a.logits, min(r, a.R - 1), a.ld, a.C);
+  const RowSettings set(a.set, min(r, a.R - 1), a.C);
+  float x[kShortEach];
+  load_short(row, x);
+  float m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kShortEach; ++i) {
+    x[i] = no_nan(x[i]);
+    m = fmaxf(m, x[i]);
+  }
+  m = row16_reduce(m, Larger());
+  const Weigh weigh{m, set.temperature > 0.0f ? 1.0f / set.temperature : INFINITY};
+  const bool ordered = set.k < a.C || set.top_p < 1.0f;
+  // Elements of these arrays are set by selects, never in a branch that only some lanes take: there the compiler kept
+  // the arrays as vectors and lost a store.
+  uint32_t w[kShortEach];
+  uint64_t mine[kShortEach];
+  float e[kShortEach];
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kShortEach; ++i) {
+    w[i] = 0;
+    mine[i] = 0;
+    e[i] = 0.0f;
+    if (16 * i < a.C) {
+      e[i] = weigh.e(x[i]);
+      w[i] = weigh.of(x[i], e[i]);
+      mine[i] = (uint64_t)~key_of(x[i]) << 32 | (uint32_t)(16 * i + l);
+      int count;
+      const int at = n + row16_place(w[i] != 0, count);
+      if (w[i]) {
+        list[slot][at] = mine[i];
+        weight[slot][at] = w[i];
+      }
+      n += count;
+    }
+  }
+  __syncthreads();
+  uint64_t limit = UINT64_MAX;
+  uint64_t before[kShortEach] = {};
+  if (ordered) {
+    int rank[kShortEach] = {};
+    for (int o = 0; o < n; ++o) {
+      const uint64_t other = list[slot][o];
+      const uint32_t its = weight[slot][o];
+#pragma unroll
+      for (int i = 0; i < kShortEach; ++i)
+        if (16 * i < a.C) {
+          const bool ahead = other < mine[i];
+          rank[i] += ahead;
+          before[i] += ahead ? its : 0;
+        }
+    }
+    uint64_t sum = 0;
+#pragma unroll
+    for (int i = 0; i < kShortEach; ++i) {
+      w[i] = rank[i] < set.k ? w[i] : 0;
+      sum += w[i];
+    }
+    limit = set.limit(lane_of_row16(row16_upto64(sum)));
+  }
+  // the kept weights up to each class, in the order of the classes
+  uint64_t upto[kShortEach], total = 0;
+  int count = 0;
+#pragma unroll
+  for (int i = 0; i < kShortEach; ++i) {
+    upto[i] = 0;
+    w[i] = (before[i] < limit) & (e[i] >= set.min_p) ? w[i] : 0;
+    if (16 * i < a.C) {
+      upto[i] = total + row16_upto64(w[i]);
+      total = lane_of_row16(upto[i]);
+      int kept;
+      row16_place(w[i] != 0, kept);
+      count += kept;
+    }
+  }
+  if (!live) return;
+  if (total == 0) {
+    if (l == 0) a.answer(r, -1, -INFINITY, 0);
+    return;
+  }
+  const uint64_t point = set.point(total);
+#pragma unroll
+  for (int i = 0; i < kShortEach; ++i)
+    if (w[i] && upto[i] > point && upto[i] - w[i] <= point) a.answer(r, 16 * i + l, log_share(weigh, x[i], total), count);
+}
+
 // ------------------------------------------------------------------ any row, read in passes
 
 template <int NT>
@@ -536,7 +632,10 @@ extern "C" snn_status snn_readout_sample(const void* logits, int dtype, int64_t 
   return rows::for_type(dtype, [&](auto type) {
     using T = decltype(type);
     const int Q = rows::most_vectors<T>(logits, C, ld);
-    if (Q <= 4 * 64)
+    if (C <= rows::kShortRow)
+      hipLaunchKernelGGL((sample_short<T>), dim3((unsigned)((R + rows::kShortRows - 1) / rows::kShortRows)), dim3(256),
+                         0, s, a);
+    else if (Q <= 4 * 64)
       hipLaunchKernelGGL((sample_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
     else if (Q <= 4 * 256)
       hipLaunchKernelGGL((sample_tile<T, 256, 4>), grid, dim3(256), 0, s, a);

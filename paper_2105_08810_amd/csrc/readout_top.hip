@@ -7,7 +7,7 @@
 // wave's lanes, and the smallest of those over the waves. At least K values reach it, and hardly more do when values
 // lie in no particular order along the row (a thread's vectors are a block's width apart, so that a run of likely
 // classes is spread over all waves). One comparison a value collects them in LDS, where each counts those before it.
-// Where too many reach the bound (long runs of equal values), where K needs more than kNthMost of a wave, and for rows
+// Rows of up to 128 classes go 16 lanes each (top_short). Where too many reach the bound (long runs of equal values), where K needs more than kNthMost of a wave, and for rows
 // beyond the registers, the cut is found by histograms of the row as it lies in memory (top_general).
 #include "rows.h"
 
@@ -44,6 +44,8 @@ struct Top {
   float* lse;
 };
 
+__device__ __forceinline__ uint64_t entry(uint32_t key, int j) { return (uint64_t)~key << 32 | (uint32_t)j; }
+
 // Classes and logits of the n collected entries by their place among them; the record's end where there are fewer.
 template <class T, int NT>
 __device__ __forceinline__ void write_record(const Row<T>& row, const Top& a, int64_t r, const uint64_t* list, int n) {
@@ -65,7 +67,80 @@ __device__ __forceinline__ void write_record(const Row<T>& row, const Top& a, in
   }
 }
 
-__device__ __forceinline__ uint64_t entry(uint32_t key, int j) { return (uint64_t)~key << 32 | (uint32_t)j; }
+// Rows of at most kShortRow classes. A lane's largest value has so many lanes' above it; the smallest of those with
+// fewer than K above bounds the K-th value from below (with K > 16 every value is collected).
+template <class T>
+__global__ __launch_bounds__(256) void top_short(Top a) {
+  __shared__ uint64_t list[kShortRows][kShortRow];
+  const int slot = threadIdx.x / 16, l = threadIdx.x % 16;
+  const int64_t r = (int64_t)blockIdx.x * kShortRows + slot;
+  const bool live = r < a.R;
+  const Row<T> row(a.logits, min(r, a.R - 1), a.ld, a.C);
+  float x[kShortEach];
+  load_short(row, x);
+  float most = -INFINITY;
+  uint32_t key[kShortEach], own = 0;
+#pragma unroll
+  for (int i = 0; i < kShortEach; ++i) {
+    x[i] = no_nan(x[i]);
+    most = fmaxf(most, x[i]);
+    key[i] = key_of(x[i]);
+    own = max(own, key[i]);
+  }
+  uint32_t bound = 0;
+  if (a.K <= 16) {
+    int above = 0;
+#define SNN_STEP(n) above += (uint32_t)__builtin_amdgcn_mov_dpp((int)own, 0x120 + n, 0xf, 0xf, true) > own
+    SNN_STEP(1); SNN_STEP(2); SNN_STEP(3); SNN_STEP(4); SNN_STEP(5); SNN_STEP(6); SNN_STEP(7); SNN_STEP(8);
+    SNN_STEP(9); SNN_STEP(10); SNN_STEP(11); SNN_STEP(12); SNN_STEP(13); SNN_STEP(14); SNN_STEP(15);
+#undef SNN_STEP
+    bound = above < a.K ? own : UINT32_MAX;
+#define SNN_STEP(ctrl) bound = min(bound, (uint32_t)__builtin_amdgcn_mov_dpp((int)bound, ctrl, 0xf, 0xf, true))
+    SNN_STEP(0xb1); SNN_STEP(0x4e); SNN_STEP(0x141); SNN_STEP(0x140);
+#undef SNN_STEP
+  }
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kShortEach; ++i) {
+    if (16 * i >= a.C) break;
+    const bool on = key[i] >= bound && x[i] > -INFINITY;
+    int count;
+    const int at = n + row16_place(on, count);
+    if (on) list[slot][at] = entry(key[i], 16 * i + l);
+    n += count;
+  }
+  if (a.lse) {
+    most = row16_reduce(most, Larger());
+    const float safe = isinf(most) ? 0.0f : most;
+    const float c = a.inv * kLog2e, sc = safe * c;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kShortEach; ++i) {
+      if (16 * i >= a.C) break;
+      sum += exp2_fast(fmaf(x[i], c, -sc));
+    }
+    sum = row16_reduce(sum, Plus());
+    if (live && l == 0) a.lse[r] = isinf(most) ? most : most * a.inv + logf(sum);
+  }
+  __syncthreads();
+  if (!live) return;
+  for (int e = l; e < max(n, a.K); e += 16) {
+    int place = e, id = -1;
+    float v = -INFINITY;
+    if (e < n) {
+      const uint64_t mine = list[slot][e];
+      place = 0;
+#pragma unroll 4
+      for (int o = 0; o < n; ++o) place += list[slot][o] < mine;
+      id = (int)(uint32_t)mine;
+      if (place < a.K) v = row.at(id);
+    }
+    if (place < a.K) {
+      a.ids[r * a.K + place] = id;
+      a.vals[r * a.K + place] = v;
+    }
+  }
+}
 
 template <class T, int NT>
 __device__ __forceinline__ void top_general(const Row<T>& row, const Top& a, int64_t r, TopLds<NT>& s) {
@@ -252,7 +327,10 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
   return rows::for_type(dtype, [&](auto type) {
     using T = decltype(type);
     const int Q = rows::most_vectors<T>(logits, C, ld);
-    if (Q <= 4 * 64 && K <= kNthMost)
+    if (C <= rows::kShortRow)
+      hipLaunchKernelGGL((top_short<T>), dim3((unsigned)((R + rows::kShortRows - 1) / rows::kShortRows)), dim3(256), 0,
+                         s, a);
+    else if (Q <= 4 * 64 && K <= kNthMost)
       hipLaunchKernelGGL((top_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
     else if (Q <= 4 * 256 && K <= 4 * kNthMost)
       hipLaunchKernelGGL((top_tile<T, 256, 4>), grid, dim3(256), 0, s, a);

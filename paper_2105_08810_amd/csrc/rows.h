@@ -134,71 +134,97 @@ __device__ __forceinline__ void Row<T>::load(int q, float (&x)[kVec]) const {
   unpack<T>(load_raw(*this, q), x);
 }
 
-// A row in a block's registers: vector i * NT + thread of it as element i of four register arrays. Long passes over it
-// are loops whose counter selects the registers: unrolled, the passes of a wide tile are straight code of tens of KB,
-// and a block then waits for instructions at nearly every line (1024 rows of 65536 drawn from: 620 us unrolled, 210 so).
+// Vectors i * NT + thread of a row, -inf outside it. All loads are under way before anything waits: threads past the
+// row's whole vectors load its last one.
+template <class T, int NT, int NV>
+__device__ __forceinline__ void load_vectors(const Row<T>& row, uint4 (&u)[NV]) {
+  constexpr int kVec = Row<T>::kVec;
+  const int tid = (int)threadIdx.x;
+  const int from = row.lead ? 1 : 0, to = (row.lead + row.C) / kVec;  // whole vectors
+  uint4 none;
+  {
+    T v[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = lowest<T>();
+    __builtin_memcpy(&none, v, 16);
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) u[i] = none;
+  if (to > from) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      u[i] = *reinterpret_cast<const uint4*>(row.base + (size_t)min(max(i * NT + tid, from), to - 1) * kVec);
+  }
+  uint4 first = none, last = none;  // the ends of the row
+  if (from == 1 && tid == 0) first = load_raw(row, 0);
+  if (to < row.Q && to >= from && tid == to % NT) last = load_raw(row, to);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int q = i * NT + tid;
+    const bool in = q >= from && q < to, end = q == to && to >= from;
+    uint4 e = make_uint4(end ? last.x : none.x, end ? last.y : none.y, end ? last.z : none.z, end ? last.w : none.w);
+    if (i == 0) {
+      const bool head = tid < from;
+      e = make_uint4(head ? first.x : e.x, head ? first.y : e.y, head ? first.z : e.z, head ? first.w : e.w);
+    }
+    u[i] = make_uint4(in ? u[i].x : e.x, in ? u[i].y : e.y, in ? u[i].z : e.z, in ? u[i].w : e.w);
+  }
+}
+
+// A row in a block's registers: vector i * NT + thread of it as the words 4 i to 4 i + 3 of a register array (two of
+// them beyond 8 vectors), where a load puts them without a move. Long passes over it are loops whose counter selects
+// the registers: unrolled, the passes of a wide tile are straight code of tens of KB, and a block then waits for
+// instructions at nearly every line (1024 rows of 65536 drawn from: 620 us unrolled, 210 so).
 template <class T, int NT, int NV>
 struct Tile {
-  typedef uint32_t Words __attribute__((ext_vector_type(NV)));
-  Words w[4];
-  __device__ __forceinline__ uint4 get(int i) const { return make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]); }
-  __device__ __forceinline__ void set(int i, const uint4& u) {
-    w[0][i] = u.x;
-    w[1][i] = u.y;
-    w[2][i] = u.z;
-    w[3][i] = u.w;
+  static constexpr int kVec = Row<T>::kVec;
+  static constexpr int kPart = NV < 8 ? NV : 8;
+  typedef uint32_t Words __attribute__((ext_vector_type(4 * kPart)));
+  Words w[NV / kPart];
+
+  __device__ __forceinline__ static uint4 take(const Words& p, int i) {
+    return make_uint4(p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
+  }
+  __device__ __forceinline__ static void put(Words& p, int i, const uint4& u) {
+    p[4 * i] = u.x;
+    p[4 * i + 1] = u.y;
+    p[4 * i + 2] = u.z;
+    p[4 * i + 3] = u.w;
+  }
+  __device__ __forceinline__ uint4 get(int i) const {
+    if (NV > kPart && i >= kPart) return take(w[NV / kPart - 1], i - kPart);
+    return take(w[0], i);
   }
   __device__ __forceinline__ void load(const Row<T>& row) {
-    constexpr int kVec = Row<T>::kVec;
-    const int tid = (int)threadIdx.x;
-    const int from = row.lead ? 1 : 0, to = (row.lead + row.C) / kVec;  // whole vectors
-    uint4 none;
-    {
-      T v[kVec];
+    uint4 u[NV];
+    load_vectors<T, NT>(row, u);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) v[i] = lowest<T>();
-      __builtin_memcpy(&none, v, 16);
-    }
+    for (int i = 0; i < NV; ++i) put(w[i / kPart], i % kPart, u[i]);
+  }
+  // f(values, vector, its number in the thread)
+  template <class F>
+  __device__ __forceinline__ void each(const Row<T>& row, F f) const {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int q = i * NT + tid;
-      uint4 u = none;
-      if (q >= from && q < to) u = *reinterpret_cast<const uint4*>(row.base + (size_t)q * kVec);
-      set(i, u);
-    }
-    // the ends of the row (every thread sets its vector anew: a branch around it would keep two copies of the tile)
-    if (from == 1) {
-      uint4 u = get(0);
-      if (tid == 0) u = load_raw(row, 0);
-      set(0, u);
-    }
-    if (to < row.Q && row.Q > from) {
-      const int i = to / NT;
-      uint4 u = get(i);
-      if (tid == to - i * NT) u = load_raw(row, to);
-      set(i, u);
+    for (int h = 0; h < NV / kPart; ++h) {
+#pragma unroll 1
+      for (int i = 0; i < kPart; ++i) {
+        if ((h * kPart + i) * NT >= row.Q) break;
+        float x[kVec];
+        unpack<T>(take(w[h], i), x);
+        f(x, (h * kPart + i) * NT + (int)threadIdx.x, h * kPart + i);
+      }
     }
   }
-  // As each(), unrolled: for a few instructions a value.
+  // The same, unrolled: for a few instructions a value.
   template <class F>
   __device__ __forceinline__ void each_unrolled(const Row<T>& row, F f) const {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (i * NT < row.Q) {
-        float x[Row<T>::kVec];
+        float x[kVec];
         unpack<T>(get(i), x);
         f(x, i * NT + (int)threadIdx.x, i);
       }
-  }
-  // f(values, vector, its number in the thread)
-  template <class F>
-  __device__ __forceinline__ void each(const Row<T>& row, F f) const {
-#pragma unroll 1
-    for (int i = 0; i * NT < row.Q; ++i) {
-      float x[Row<T>::kVec];
-      unpack<T>(get(i), x);
-      f(x, i * NT + (int)threadIdx.x, i);
-    }
   }
 };
 
@@ -242,6 +268,31 @@ __device__ __forceinline__ float row16_reduce(float v, F f) {
 #undef SNN_STEP
   return v;
 }
+// Rows of at most kShortRow classes go 16 lanes each, four in a wave: class 16 i + lane is the lane's value i.
+constexpr int kShortRow = 128;
+constexpr int kShortEach = kShortRow / 16;
+constexpr int kShortRows = 16;  // of a block of 256
+
+template <class T>
+__device__ __forceinline__ void load_short(const Row<T>& row, float (&x)[kShortEach]) {
+  const int l = threadIdx.x % 16;
+#pragma unroll
+  for (int i = 0; i < kShortEach; ++i) {
+    const int j = 16 * i + l;
+    x[i] = -INFINITY;
+    if (16 * i < row.C) x[i] = j < row.C ? row.at(min(j, row.C - 1)) : -INFINITY;
+  }
+}
+// Sums over the row's lanes up to each.
+__device__ __forceinline__ uint64_t row16_upto64(uint64_t v);
+// The lane's place among those of its row with `on`, and their number.
+__device__ __forceinline__ int row16_place(bool on, int& count) {
+  const uint64_t m = __ballot(on);
+  const uint32_t bits = (uint32_t)(m >> (threadIdx.x % kWave / 16 * 16)) & 0xffffu;
+  count = __popc(bits);
+  return __popc(bits & ((1u << threadIdx.x % 16) - 1));
+}
+
 template <class F>
 __device__ __forceinline__ float wave_reduce(float v, F f) {
   v = row16_reduce(v, f);
@@ -284,6 +335,19 @@ __device__ __forceinline__ uint64_t wave_upto64(uint64_t v) {
   v += from_lane64<0x142, 0xa>(v);  // rows 0 and 2 to the next, then the lower half to the upper
   v += from_lane64<0x143, 0xc>(v);
   return v;
+}
+__device__ __forceinline__ uint64_t row16_upto64(uint64_t v) {
+  v += from_lane64<0x111>(v);
+  v += from_lane64<0x112>(v);
+  v += from_lane64<0x114>(v);
+  v += from_lane64<0x118>(v);
+  return v;
+}
+// The value of the last lane of the row of 16.
+__device__ __forceinline__ uint64_t lane_of_row16(uint64_t v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)v, 0x15f, 0xf, 0xf, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)(v >> 32), 0x15f, 0xf, 0xf, true);
+  return (uint64_t)hi << 32 | lo;
 }
 __device__ __forceinline__ uint64_t wave_sum64(uint64_t v) { return lane_of64(wave_upto64(v), kWave - 1); }
 

@@ -23,16 +23,30 @@ struct Settings {
   const float* min_p;
 };
 
+// exp(t) for t <= 0 (from -64 on; -64 for less): 2^(t log2 e) with the product in two parts, the whole of it apart. Within
+// an ulp of the correctly rounded value; no test for what overflows.
+__device__ __forceinline__ float exp_down(float t) {
+#pragma clang fp contract(off)
+  constexpr double kFull = 1.44269504088896340736;
+  constexpr float kHigh = (float)kFull, kLow = (float)(kFull - (double)kHigh);
+  t = fmaxf(t, -64.0f);
+  const float h = t * kHigh, n = rintf(h);
+  const float low = fmaf(t, kLow, fmaf(t, kHigh, -h));
+  return ldexpf(exp2_fast((h - n) + low), (int)n);
+}
+
 struct Weigh {
   float max, inv;
-  __device__ __forceinline__ float t(float x) const {  // in this order of operations, each rounded
-    return x == max ? 0.0f : (x - max) * inv;
-  }
-  __device__ __forceinline__ float e(float x) const { return expf(t(x)); }
+  // In this order of operations, each rounded. Of infinities the largest is at 0 and others at -inf; any other row's
+  // largest is at 0 by itself.
+  __device__ __forceinline__ float t(float x) const { return x == max ? 0.0f : (x - max) * inv; }
+  __device__ __forceinline__ float e(float x) const { return exp_down(t(x)); }
   __device__ __forceinline__ uint32_t of(float x, float e) const {
     return x == -INFINITY ? 0u : (uint32_t)rintf(e * kUnit);
   }
   __device__ __forceinline__ uint32_t operator()(float x) const { return of(x, e(x)); }
+  // For a finite max and inv, where -inf has weight 0 by itself.
+  __device__ __forceinline__ float plain_t(float x) const { return (x - max) * inv; }
 };
 
 struct Sample {
@@ -288,7 +302,9 @@ __global__ __launch_bounds__(NT) void sample_rows(Sample a) {
 
 constexpr int kBins = 1024;
 constexpr float kBinsPer = (kBins - 1) / kFaintest;  // bins of equal width in t
-constexpr int kNthMost = 16;
+// Lanes of each wave that the bound is taken from, at most: with n of 64 lanes -64 log(1 - n/64) of its values reach it.
+template <int NT>
+constexpr int kNthMost = NT == kWave ? 56 : 24;
 
 template <int NT, int NV>
 struct TileLds {
@@ -299,7 +315,8 @@ struct TileLds {
     uint64_t mass[kBins];
     struct {
       uint64_t list[kList];  // key (inverted) and class: in the order when ascending
-      uint32_t weight[kList], share[kList];
+      uint64_t before[kList];
+      uint32_t weight[kList], rank[kList];
     };
   };
   uint64_t chunk[kChunks];
@@ -324,64 +341,70 @@ __device__ __forceinline__ uint64_t entry(uint32_t key, int j) { return (uint64_
 __device__ __forceinline__ float logit_of(uint64_t e) { return of_key(~(uint32_t)(e >> 32)); }
 
 // Draws from the n collected elements, which hold all that can be kept. sum: the weight that top-p is a part of; 0:
-// that of the first k elements.
+// that of the first k elements. Each element is compared with all others by several threads, a share of them each.
 template <class T, int NT, int NV>
 __device__ __forceinline__ void draw_from_list(const Sample& a, int64_t r, const RowSettings& set, const Weigh& weigh,
                                                int n, uint64_t sum, TileLds<NT, NV>& s) {
-  constexpr int kEach = TileLds<NT, NV>::kList / NT;
+  constexpr int kList = TileLds<NT, NV>::kList;
   const int tid = threadIdx.x;
-  for (int e = tid; e < n; e += NT) s.weight[e] = weigh(logit_of(s.list[e]));
+  int width = kWave;  // entries side by side
+  while (width < n && width < NT) width <<= 1;
+  const int each = (n + NT / width - 1) / (NT / width);  // others of a thread
+  const int from = tid / width * each, to = min(n, from + each);
+  for (int e = tid; e < n; e += NT) {
+    s.weight[e] = weigh(logit_of(s.list[e]));
+    s.rank[e] = 0;
+    s.before[e] = 0;
+  }
   __syncthreads();
-  uint64_t before[kEach];
-  uint64_t first = 0;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int e = tid + i * NT;
-    before[i] = UINT64_MAX;
-    if (e < n) {
-      const uint64_t mine = s.list[e];
-      uint64_t b = 0;
-      int rank = 0;
+  for (int e = tid % width; e < n; e += width) {
+    const uint64_t mine = s.list[e];
+    uint64_t b = 0;
+    uint32_t rank = 0;
 #pragma unroll 4
-      for (int o = 0; o < n; ++o) {
-        const bool ahead = s.list[o] < mine;
-        rank += ahead;
-        b += ahead ? s.weight[o] : 0;
-      }
-      if (rank < set.k) {
-        before[i] = b;
-        first += s.weight[e];
-      }
+    for (int o = from; o < to; ++o) {
+      const bool ahead = s.list[o] < mine;
+      rank += ahead;
+      b += ahead ? s.weight[o] : 0;
+    }
+    if (rank) {
+      atomicAdd(&s.rank[e], rank);
+      atomicAdd((unsigned long long*)&s.before[e], (unsigned long long)b);
     }
   }
-  if (sum == 0) sum = block_sum64<NT>(first, s.red);
+  __syncthreads();
+  if (sum == 0) {
+    for (int e = tid; e < n; e += NT) sum += s.rank[e] < (uint32_t)set.k ? s.weight[e] : 0;
+    sum = block_sum64<NT>(sum, s.red);
+  }
   const uint64_t limit = set.limit(sum);
-  uint64_t total = 0, count = 0;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int e = tid + i * NT;
-    if (e < n) {
-      const uint32_t w = before[i] < limit && weigh.e(logit_of(s.list[e])) >= set.min_p ? s.weight[e] : 0;
-      s.share[e] = w;
-      total += w;
-      count += w != 0;
-    }
+  uint64_t total = 0;  // and the number kept, above bit 48
+  for (int e = tid; e < n; e += NT) {
+    const bool in = (s.rank[e] < (uint32_t)set.k) & (s.before[e] < limit) & (weigh.e(logit_of(s.list[e])) >= set.min_p);
+    const uint32_t w = in ? s.weight[e] : 0;
+    s.weight[e] = w;
+    total += w + ((uint64_t)(w != 0) << 48);
   }
+  static_assert(kList < (1 << 15), "sums of 2^31 each stay below bit 48");
   total = block_sum64<NT>(total, s.red);
-  count = block_sum64<NT>(count, s.red);
-  __syncthreads();  // the shares, in a block of one wave too
+  const int count = (int)(total >> 48);
+  total &= ((uint64_t)1 << 48) - 1;
   const uint64_t point = set.point(total);
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int e = tid + i * NT;
-    const uint32_t w = e < n ? s.share[e] : 0;
-    if (w) {
-      const uint32_t j = (uint32_t)s.list[e];
-      uint64_t b = 0;
+  for (int e = tid; e < n; e += NT) s.before[e] = 0;
+  __syncthreads();
+  for (int e = tid % width; e < n; e += width) {
+    const uint32_t j = (uint32_t)s.list[e];
+    uint64_t b = 0;
 #pragma unroll 4
-      for (int o = 0; o < n; ++o) b += (uint32_t)s.list[o] < j ? s.share[o] : 0;
-      if (b <= point && point < b + w) a.answer(r, (int)j, log_share(weigh, logit_of(s.list[e]), total), (int)count);
-    }
+    for (int o = from; o < to; ++o) b += (uint32_t)s.list[o] < j ? s.weight[o] : 0;
+    if (b) atomicAdd((unsigned long long*)&s.before[e], (unsigned long long)b);
+  }
+  __syncthreads();
+  for (int e = tid; e < n; e += NT) {
+    const uint32_t w = s.weight[e];
+    const uint64_t b = s.before[e];
+    if (w && b <= point && point < b + w)
+      a.answer(r, (int)(uint32_t)s.list[e], log_share(weigh, logit_of(s.list[e]), total), count);
   }
 }
 
@@ -396,8 +419,8 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
   Tile<T, NT, NV> tile;
   tile.load(row);
   // the largest value and a bound that at least `want` values reach
-  const bool few = set.k <= kNthMost * kWaves;  // what top-k keeps can be collected
-  const int nth = few ? (set.k + kWaves - 1) / kWaves : max(4, kNthMost / kWaves);
+  const bool few = set.k <= kNthMost<NT> * kWaves;  // what top-k keeps can be collected
+  const int nth = few ? (set.k + kWaves - 1) / kWaves : max(4, 16 / kWaves);
   float most = -INFINITY;
   bool nan = false;
   tile.each_unrolled(row, [&](const float (&x)[kVec], int, int) {
@@ -430,8 +453,8 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
   }
   __syncthreads();
   const float m = of_key(high);
-  if (odd || isinf(m) || (!few && set.k < a.C)) return false;
   const Weigh weigh{m, 1.0f / set.temperature};
+  if (odd || isinf(m) || (!few && set.k < a.C) || (isinf(weigh.inv) && set.k != 1)) return false;
   if (set.k == 1) {  // the first of the largest
     int at = INT32_MAX;
     tile.each(row, [&](const float (&x)[kVec], int q, int) {
@@ -444,7 +467,6 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
     return true;
   }
   const float least = of_key(bound);
-  uint32_t cut_key = 0;
   int last = a.C;  // class of the last kept element at the cut
   const auto bin_of = [&](float t) { return min(kBins - 1, (int)(t * -kBinsPer)); };
   // One loop over the row for all passes: the exponential's code is there once.
@@ -455,7 +477,9 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
   //   kShare    the kept weights of runs of 64 vectors, which follow one another in the order of the classes
   enum { kCollect, kSum, kBin, kPart, kShare };
   int mode = few ? kCollect : set.top_p < 1.0f ? kSum : kShare;
-  uint64_t sum = 0, limit = 0, above = 0, count = 0;
+  uint64_t sum = 0, limit = 0, above = 0;
+  uint32_t count = 0;
+  float cut = -INFINITY;
   int part = 0, n = 0;
   for (;;) {
     count = 0;
@@ -463,48 +487,53 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
     tile.each(row, [&](const float (&x)[kVec], int q, int) {
       // hidden from the compiler, which would make a loop of its own for every mode
       const int mode_here = __builtin_amdgcn_readfirstlane(mode + opaque_zero());
-      uint64_t v = 0;
-      bool any = mode_here > kSum;
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) any |= x[i] >= least;
+      uint32_t take = 0;
       if (mode_here == kCollect) {
-        if (any) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) take |= (uint32_t)((x[i] >= least) & (x[i] > -INFINITY)) << i;
+      } else {
+        float e[kVec];
+        uint32_t w[kVec];
+        uint64_t v = 0;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          e[i] = exp_down(weigh.plain_t(x[i]));
+          w[i] = (uint32_t)rintf(e[i] * kUnit);
+        }
+        if (mode_here == kShare) {
+#pragma unroll
+          for (int i = 0; i < kVec; ++i) {
+            const bool in = ((x[i] > cut) | ((x[i] == cut) & (row.first(q) + i <= last))) & (e[i] >= set.min_p);
+            w[i] = in ? w[i] : 0;
+            v += w[i];
+            count += w[i] != 0;
+          }
+          v = wave_sum64(v);
+          if (lane == 0) s.chunk[q / kWave] = v;
+        } else if (mode_here == kBin) {
 #pragma unroll
           for (int i = 0; i < kVec; ++i)
-            if (x[i] >= least && x[i] > -INFINITY) {
-              const uint32_t at = atomicAdd(&s.n_list, 1u);
-              if (at < (uint32_t)kList) s.list[at] = entry(key_of(x[i]), row.first(q) + i);
-            }
-        }
-        return;
-      }
+            if (w[i]) atomicAdd((unsigned long long*)&s.mass[bin_of(weigh.plain_t(x[i]))], (unsigned long long)w[i]);
+        } else if (mode_here == kSum) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const float t = weigh.t(x[i]), e = expf(t);
-        uint32_t w = weigh.of(x[i], e);
-        bool take = false;
-        if (mode_here == kSum) {
-          take = x[i] >= least && x[i] > -INFINITY;
-        } else if (mode_here == kBin) {
-          if (w) atomicAdd((unsigned long long*)&s.mass[bin_of(t)], (unsigned long long)w);
-        } else if (mode_here == kPart) {
-          take = w && bin_of(t) == part;
+          for (int i = 0; i < kVec; ++i) {
+            v += w[i];
+            take |= (uint32_t)((x[i] >= least) & (x[i] > -INFINITY)) << i;
+          }
+          own_sum += v;
         } else {
-          const uint32_t key = key_of(x[i]);
-          const bool in = (key > cut_key || (key == cut_key && row.first(q) + i <= last)) && e >= set.min_p;
-          w = in ? w : 0;
-          count += w != 0;
-        }
-        v += w;
-        if (take) {
-          const uint32_t at = atomicAdd(&s.n_list, 1u);
-          if (at < (uint32_t)kList) s.list[at] = entry(key_of(x[i]), row.first(q) + i);
+#pragma unroll
+          for (int i = 0; i < kVec; ++i)
+            take |= (uint32_t)((w[i] != 0) & (bin_of(weigh.plain_t(x[i])) == part)) << i;
         }
       }
-      own_sum += v;
-      if (mode_here == kShare) {
-        v = wave_sum64(v);
-        if (lane == 0) s.chunk[q / kWave] = v;
+      if (take) {
+        uint32_t at = atomicAdd(&s.n_list, (uint32_t)__popc(take));
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          if ((take >> i & 1) && at < (uint32_t)kList) s.list[at] = entry(key_of(x[i]), row.first(q) + i);
+          at += take >> i & 1;
+        }
       }
     });
     if (mode == kShare) break;
@@ -562,19 +591,19 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
 #pragma unroll 4
         for (int o = 0; o < n; ++o) before += s.list[o] < mine ? s.weight[o] : 0;
         if (before < limit && before + s.weight[e] >= limit) {  // the last kept
-          s.ured[0] = ~(uint32_t)(mine >> 32);
+          s.ured[0] = ~(uint32_t)(mine >> 32);  // (a key of 0's either sign stands for both)
           s.ired[0] = (int)(uint32_t)mine;
         }
       }
       __syncthreads();
-      cut_key = s.ured[0];
+      cut = of_key(s.ured[0]);
       last = s.ired[0];
       mode = kShare;
     }
   }
   const int runs = (row.Q + NT - 1) / NT * kWaves;
   for (int c = runs + tid; c < TileLds<NT, NV>::kChunks; c += NT) s.chunk[c] = 0;
-  count = block_sum64<NT>(count, s.red);
+  const uint64_t counted = block_sum64<NT>(count, s.red);
   __syncthreads();
   // every wave for itself: the run of the point
   constexpr int kChunks = TileLds<NT, NV>::kChunks;
@@ -597,12 +626,11 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
   }
   if (wave != 0) return true;
   const auto share = [&](float x, int j) -> uint64_t {
-    const uint32_t key = key_of(x);
     const float e = weigh.e(x);
-    return (key > cut_key || (key == cut_key && j <= last)) && e >= set.min_p ? weigh.of(x, e) : 0;
+    return ((x > cut) | ((x == cut) & (j <= last))) & (e >= set.min_p) ? weigh.of(x, e) : 0;
   };
   const int j = find_in_order<T, kWave>(row, share, target, nullptr, run * kWave, min(row.Q, (run + 1) * kWave));
-  if (lane == 0) a.answer(r, j, log_share(weigh, row.at(j), total), (int)count);
+  if (lane == 0) a.answer(r, j, log_share(weigh, row.at(j), total), (int)counted);
   return true;
 }
 

@@ -557,10 +557,13 @@ snn_status snn_readout_distill(const void* logits, int dtype, int64_t R, int C, 
  *   logp     float32 [R] (written unless NULL): log of its probability among the kept classes, -inf for a row without
  *   kept     int32 [R] (written unless NULL): the number of classes kept that can be drawn
  * NaN counts as -inf; of logits of +inf each has weight 2^31 and all others 0.
+ * Workspace: needed for few long rows alone; the query gives 0 for others, and workspace may then be NULL.
  */
+size_t snn_readout_sample_workspace(int64_t R, int C, int dtype);
 snn_status snn_readout_sample(const void* logits, int dtype, int64_t R, int C, int64_t ld, const float* u,
                               const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
-                              int32_t* cls, float* logp, int32_t* kept, void* stream);
+                              int32_t* cls, float* logp, int32_t* kept, void* workspace, size_t workspace_bytes,
+                              void* stream);
 
 #ifdef __cplusplus
 }

@@ -74,6 +74,11 @@ struct Distill {
   int64_t ld_grad;
   int accumulate;
   double* part;  // a block's sum of weight * loss
+  float* loss;   // their sum where there is one block
+  __device__ __forceinline__ void add(int64_t block, double v) const {
+    if (gridDim.x == 1) *loss = (float)v;
+    else part[block] = v;
+  }
   __device__ __forceinline__ float weight_of(int64_t r) const { return weight ? weight[r] : 1.0f / (float)R; }
 };
 
@@ -117,17 +122,16 @@ struct Small {
   static constexpr int kValues = 16 * kEach;
 };
 
-constexpr int kSmallRows = 16;           // rows of a block of 256
 constexpr int kNotListed = 0x7fffffff;   // a NaN that no operation gives
 
-template <class T>
-__global__ __launch_bounds__(256) void distill_small(Distill a) {
+template <class T, int ROWS>
+__global__ __launch_bounds__(16 * ROWS) void distill_small(Distill a) {
   using S = Small<T>;
   constexpr int kVec = S::kVec, kEach = S::kEach, NV = S::NV;
-  __shared__ __attribute__((aligned(16))) int table[kSmallRows][S::kValues];  // log p of the listed values
-  __shared__ double part[kSmallRows];
+  __shared__ __attribute__((aligned(16))) int table[ROWS][S::kValues];  // log p of the listed values
+  __shared__ double part[ROWS];
   const int slot = threadIdx.x / 16, l = threadIdx.x % 16;
-  const int64_t r = (int64_t)blockIdx.x * kSmallRows + slot;
+  const int64_t r = (int64_t)blockIdx.x * ROWS + slot;
   const int C = a.C, K = a.K;
   const float w = r < a.R ? a.weight_of(r) : 0.0f;
   const bool live = w != 0.0f;
@@ -253,8 +257,8 @@ __global__ __launch_bounds__(256) void distill_small(Distill a) {
   __syncthreads();
   if (threadIdx.x == 0) {
     double v = 0.0;
-    for (int k = 0; k < kSmallRows; ++k) v += part[k];
-    a.part[blockIdx.x] = v;
+    for (int k = 0; k < ROWS; ++k) v += part[k];
+    a.add(blockIdx.x, v);
   }
 }
 
@@ -417,7 +421,7 @@ template <class T, int NT>
 __device__ __forceinline__ void row_without_weight(const Distill& a, int64_t r) {
   if (threadIdx.x == 0) {
     if (a.row_loss) a.row_loss[r] = 0.0f;
-    a.part[r] = 0.0;
+    a.add(r, 0.0);
   }
   if (a.grad && !a.accumulate) {
     const Row<T> out(a.grad, r, a.ld_grad, a.C);
@@ -439,7 +443,7 @@ __global__ __launch_bounds__(NT, 4) void distill_tile(Distill a) {
   const Row<T> row(a.logits, r, a.ld, a.C);
   const Entries<T> entries(a, r, row);
   uint4 raw[NV];
-  load_vectors<T, NT>(row, raw);
+  load_vectors<T, NT>(row, raw, 0, row.Q);
   for (int k = tid; k < (row.Q * kVec + 31) / 32; k += NT) bits[k] = 0;
   __syncthreads();
   const Teacher t = teacher_of<T>(a, r, entries, bits);
@@ -476,7 +480,7 @@ __global__ __launch_bounds__(NT, 4) void distill_tile(Distill a) {
   const RowSums s = finish_row<T>(entries, t, rest, c);
   if (tid == 0) {
     if (a.row_loss) a.row_loss[r] = s.loss;
-    a.part[r] = (double)w * (double)s.loss;
+    a.add(r, (double)w * (double)s.loss);
   }
   if (!a.grad) return;
   const Row<T> out(a.grad, r, a.ld_grad, a.C);
@@ -583,7 +587,7 @@ __global__ __launch_bounds__(NT) void distill_rows(Distill a) {
   const RowSums s = finish_row<T>(entries, t, rest, c);
   if (tid == 0) {
     if (a.row_loss) a.row_loss[r] = s.loss;
-    a.part[r] = (double)w * (double)s.loss;
+    a.add(r, (double)w * (double)s.loss);
   }
   if (!a.grad) return;
   const Row<T> out(a.grad, r, a.ld_grad, a.C);
@@ -645,7 +649,7 @@ extern "C" snn_status snn_readout_distill(const void* logits, int dtype, int64_t
   Carve ws(workspace);
   double* part = ws.take<double>((size_t)R);
   double* sums = ws.take<double>((size_t)((R + kTotalEach - 1) / kTotalEach));
-  const Distill a{logits, C, ld, ids, vals, lse, K, tau, weight, R, row_loss, grad, ld_grad, accumulate, part};
+  const Distill a{logits, C, ld, ids, vals, lse, K, tau, weight, R, row_loss, grad, ld_grad, accumulate, part, loss};
   hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)R);
   int64_t n = R;
@@ -655,8 +659,13 @@ extern "C" snn_status snn_readout_distill(const void* logits, int dtype, int64_t
     const int Q = rows::most_vectors<T>(logits, C, ld);
     const bool many = R >= 2 * cu_count();
     if (Q <= 16 * Small<T>::NV) {
-      n = (R + kSmallRows - 1) / kSmallRows;
-      hipLaunchKernelGGL((distill_small<T>), dim3((unsigned)n), dim3(256), 0, s, a);
+      if (R <= 64) {  // one block, and no launch for the loss
+        n = 1;
+        hipLaunchKernelGGL((distill_small<T, 64>), dim3(1), dim3(1024), 0, s, a);
+      } else {
+        n = (R + 15) / 16;
+        hipLaunchKernelGGL((distill_small<T, 16>), dim3((unsigned)n), dim3(256), 0, s, a);
+      }
     } else if (Q <= 4 * 64) {
       hipLaunchKernelGGL((distill_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
     } else if (Q <= 4 * 256) {
@@ -676,7 +685,7 @@ extern "C" snn_status snn_readout_distill(const void* logits, int dtype, int64_t
     }
     return launch_status();
   });
-  if (launched != SNN_OK) return launched;
+  if (launched != SNN_OK || n == 1) return launched;
   if (n > kTotalEach) {
     const int64_t blocks = (n + kTotalEach - 1) / kTotalEach;
     hipLaunchKernelGGL(distill_total, dim3((unsigned)blocks), dim3(1024), 0, s, part, n, kTotalEach, sums, loss);

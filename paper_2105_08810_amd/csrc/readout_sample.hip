@@ -149,6 +149,7 @@ __global__ __launch_bounds__(256) void sample_short(Sample a) {
   uint64_t before[kShortEach] = {};
   if (ordered) {
     int rank[kShortEach] = {};
+#pragma unroll 4
     for (int o = 0; o < n; ++o) {
       const uint64_t other = list[slot][o];
       const uint32_t its = weight[slot][o];
@@ -302,6 +303,8 @@ __global__ __launch_bounds__(NT) void sample_rows(Sample a) {
 
 constexpr int kBins = 1024;
 constexpr float kBinsPer = (kBins - 1) / kFaintest;  // bins of equal width in t
+__device__ __forceinline__ int bin_of(float t) { return min(kBins - 1, (int)(t * -kBinsPer)); }
+
 // Lanes of each wave that the bound is taken from, at most: with n of 64 lanes -64 log(1 - n/64) of its values reach it.
 template <int NT>
 constexpr int kNthMost = NT == kWave ? 56 : 24;
@@ -340,29 +343,80 @@ __device__ __forceinline__ int opaque_zero() {
 __device__ __forceinline__ uint64_t entry(uint32_t key, int j) { return (uint64_t)~key << 32 | (uint32_t)j; }
 __device__ __forceinline__ float logit_of(uint64_t e) { return of_key(~(uint32_t)(e >> 32)); }
 
-// Draws from the n collected elements, which hold all that can be kept. sum: the weight that top-p is a part of; 0:
-// that of the first k elements. Each element is compared with all others by several threads, a share of them each.
-template <class T, int NT, int NV>
-__device__ __forceinline__ void draw_from_list(const Sample& a, int64_t r, const RowSettings& set, const Weigh& weigh,
-                                               int n, uint64_t sum, TileLds<NT, NV>& s) {
-  constexpr int kList = TileLds<NT, NV>::kList;
+// How the threads share the comparisons of n elements with one another: a thread takes every width-th element from
+// its own on, and the others [from, to) to compare them with.
+template <int NT>
+struct Pairs {
+  int width, from, to;
+  __device__ __forceinline__ explicit Pairs(int n) {
+    width = kWave;
+    while (width < n && width < NT) width <<= 1;
+    const int each = (n + NT / width - 1) / (NT / width);
+    from = (int)threadIdx.x / width * each;
+    to = min(n, from + each);
+  }
+};
+
+// Beyond this many elements two sorts take less than all comparisons (1000 elements in 1024 threads: 50 us of comparisons).
+constexpr int kSorted = 256;
+
+// v[0..n) in ascending order; v has room for the next power of two.
+template <int NT>
+__device__ __forceinline__ void block_sort(uint64_t* v, int n) {
+  int size = 2;
+  while (size < n) size <<= 1;
+  for (int e = n + (int)threadIdx.x; e < size; e += NT) v[e] = UINT64_MAX;
+  __syncthreads();
+#pragma unroll 1
+  for (int run = 2; run <= size; run <<= 1)
+#pragma unroll 1
+    for (int step = run >> 1; step > 0; step >>= 1) {
+      for (int i = threadIdx.x; i < size / 2; i += NT) {
+        const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
+        const uint64_t x = v[lo], y = v[hi];
+        if ((x > y) == ((lo & run) == 0)) {
+          v[lo] = y;
+          v[hi] = x;
+        }
+      }
+      __syncthreads();
+    }
+}
+
+// before[e] = sum of value(o) over o < e, for e < n.
+template <int NT, class F>
+__device__ __forceinline__ void block_before(int n, F value, uint64_t* before, uint64_t* red) {
+  uint64_t base = 0;
+  for (int e0 = 0; e0 < n; e0 += NT) {
+    const int e = e0 + (int)threadIdx.x;
+    const uint64_t w = e < n ? value(e) : 0;
+    const uint64_t b = base + block_exclusive<NT>(w, red);
+    if (e < n) before[e] = b;
+    base += block_sum64<NT>(w, red);
+  }
+  __syncthreads();
+}
+
+// Weights of the n collected elements, and of each how many are ahead of it and what they weigh. Long lists are put in
+// order.
+template <int NT, class Lds>
+__device__ __forceinline__ void order_list(const Weigh& weigh, int n, Lds& s) {
   const int tid = threadIdx.x;
-  int width = kWave;  // entries side by side
-  while (width < n && width < NT) width <<= 1;
-  const int each = (n + NT / width - 1) / (NT / width);  // others of a thread
-  const int from = tid / width * each, to = min(n, from + each);
+  if (n > kSorted) block_sort<NT>(s.list, n);
   for (int e = tid; e < n; e += NT) {
     s.weight[e] = weigh(logit_of(s.list[e]));
-    s.rank[e] = 0;
+    s.rank[e] = n > kSorted ? e : 0;
     s.before[e] = 0;
   }
   __syncthreads();
-  for (int e = tid % width; e < n; e += width) {
+  if (n > kSorted) return block_before<NT>(n, [&](int e) { return (uint64_t)s.weight[e]; }, s.before, s.red);
+  const Pairs<NT> by(n);
+  for (int e = tid % by.width; e < n; e += by.width) {
     const uint64_t mine = s.list[e];
     uint64_t b = 0;
     uint32_t rank = 0;
 #pragma unroll 4
-    for (int o = from; o < to; ++o) {
+    for (int o = by.from; o < by.to; ++o) {
       const bool ahead = s.list[o] < mine;
       rank += ahead;
       b += ahead ? s.weight[o] : 0;
@@ -373,6 +427,17 @@ __device__ __forceinline__ void draw_from_list(const Sample& a, int64_t r, const
     }
   }
   __syncthreads();
+}
+
+// Draws from the n collected elements, which hold all that can be kept. sum: the weight that top-p is a part of; 0:
+// that of the first k elements.
+template <class T, int NT, int NV>
+__device__ __forceinline__ void draw_from_list(const Sample& a, int64_t r, const Row<T>& row, const RowSettings& set,
+                                               const Weigh& weigh, int n, uint64_t sum, TileLds<NT, NV>& s) {
+  constexpr int kList = TileLds<NT, NV>::kList;
+  const int tid = threadIdx.x;
+  order_list<NT>(weigh, n, s);
+  const Pairs<NT> by(n);
   if (sum == 0) {
     for (int e = tid; e < n; e += NT) sum += s.rank[e] < (uint32_t)set.k ? s.weight[e] : 0;
     sum = block_sum64<NT>(sum, s.red);
@@ -390,21 +455,30 @@ __device__ __forceinline__ void draw_from_list(const Sample& a, int64_t r, const
   const int count = (int)(total >> 48);
   total &= ((uint64_t)1 << 48) - 1;
   const uint64_t point = set.point(total);
-  for (int e = tid; e < n; e += NT) s.before[e] = 0;
-  __syncthreads();
-  for (int e = tid % width; e < n; e += width) {
-    const uint32_t j = (uint32_t)s.list[e];
-    uint64_t b = 0;
-#pragma unroll 4
-    for (int o = from; o < to; ++o) b += (uint32_t)s.list[o] < j ? s.weight[o] : 0;
-    if (b) atomicAdd((unsigned long long*)&s.before[e], (unsigned long long)b);
+  // the same in the order of the classes, with the kept weights
+  for (int e = tid; e < n; e += NT) {
+    if (n > kSorted) s.list[e] = s.list[e] << 32 | s.weight[e];
+    s.before[e] = 0;
   }
   __syncthreads();
+  if (n > kSorted) {
+    block_sort<NT>(s.list, n);
+    block_before<NT>(n, [&](int e) { return (uint64_t)(uint32_t)s.list[e]; }, s.before, s.red);
+  } else {
+    for (int e = tid % by.width; e < n; e += by.width) {
+      const uint32_t j = (uint32_t)s.list[e];
+      uint64_t b = 0;
+#pragma unroll 4
+      for (int o = by.from; o < by.to; ++o) b += (uint32_t)s.list[o] < j ? s.weight[o] : 0;
+      if (b) atomicAdd((unsigned long long*)&s.before[e], (unsigned long long)b);
+    }
+    __syncthreads();
+  }
   for (int e = tid; e < n; e += NT) {
-    const uint32_t w = s.weight[e];
+    const uint32_t w = n > kSorted ? (uint32_t)s.list[e] : s.weight[e];
+    const int j = (int)(uint32_t)(n > kSorted ? s.list[e] >> 32 : s.list[e]);
     const uint64_t b = s.before[e];
-    if (w && b <= point && point < b + w)
-      a.answer(r, (int)(uint32_t)s.list[e], log_share(weigh, logit_of(s.list[e]), total), count);
+    if (w && b <= point && point < b + w) a.answer(r, j, log_share(weigh, row.at(j), total), count);
   }
 }
 
@@ -468,7 +542,6 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
   }
   const float least = of_key(bound);
   int last = a.C;  // class of the last kept element at the cut
-  const auto bin_of = [&](float t) { return min(kBins - 1, (int)(t * -kBinsPer)); };
   // One loop over the row for all passes: the exponential's code is there once.
   //   kCollect  the elements that reach the bound (all that top-k keeps)
   //   kSum      the same, and the sum of all weights: perhaps the elements reach top-p of it
@@ -554,7 +627,7 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
     }
     if (draw) {
       __syncthreads();
-      draw_from_list<T, NT, NV>(a, r, set, weigh, n, sum, s);
+      draw_from_list<T, NT, NV>(a, r, row, set, weigh, n, sum, s);
       return true;
     }
     if (mode == kSum) {
@@ -583,13 +656,9 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
       above = s.above;
       mode = kPart;
     } else {
-      for (int e = tid; e < n; e += NT) s.weight[e] = weigh(logit_of(s.list[e]));
-      __syncthreads();
+      order_list<NT>(weigh, n, s);
       for (int e = tid; e < n; e += NT) {
-        const uint64_t mine = s.list[e];
-        uint64_t before = above;
-#pragma unroll 4
-        for (int o = 0; o < n; ++o) before += s.list[o] < mine ? s.weight[o] : 0;
+        const uint64_t mine = s.list[e], before = above + s.before[e];
         if (before < limit && before + s.weight[e] >= limit) {  // the last kept
           s.ured[0] = ~(uint32_t)(mine >> 32);  // (a key of 0's either sign stands for both)
           s.ired[0] = (int)(uint32_t)mine;
@@ -643,33 +712,394 @@ __global__ __launch_bounds__(NT) void sample_tile(Sample a) {
   if (!sample_in_registers<T, NT, NV>(a, r, row, set, s)) sample_general<T, NT>(a, r, row, set, s.general);
 }
 
+// ------------------------------------------------------------------ few long rows, several blocks each
+
+// A row of many vectors is shared among blocks of 256 threads, up to four vectors a thread:
+//   split_max    every part's largest logit and the bound of its waves
+//   split_sum    what top-k keeps, collected by the row's bound; else the weights by t for top-p
+//   split_cut    (a block a row) the bin of the top-p cut
+//   split_share  the kept weights of every part; the elements of that bin, collected
+//   split_draw   (a block a row) the order of what was collected, the part of the point, the class
+// The launches read the row again, from the caches. Each part has its own place for what it finds: atomics of blocks on
+// several dies go to memory, one after another (64 rows of 128011 with top-k 50: 229 us with a common list, 37 so).
+constexpr int kPartThreads = 256;
+constexpr int kPartVectors = 4 * kPartThreads;
+constexpr int kMostParts = 64;
+constexpr int kRowList = 1024;
+constexpr int kPartList = 256;
+constexpr int kPool = 256;         // a row's largest of lanes, which its bound is one of
+
+// The bin of the top-p cut, the weight above it and the limit.
+struct CutBin {
+  uint64_t above, limit;
+  int bin;
+};
+
+struct Split {
+  int parts;
+  int each;          // vectors of a part
+  float* max;        // [R][parts]
+  int* arg;          // [R][parts] first class of it
+  uint32_t* pool;    // [R][kPool], pool_used of them
+  int of_wave;       // lanes' largest that a wave gives
+  uint64_t* share;   // [R][parts] kept weights
+  uint32_t* count;   // [R][parts] kept classes
+  uint64_t* mass;    // [R][parts][kBins]
+  uint64_t* list;    // [R][parts][kPartList]
+  uint32_t* n_list;  // [R][parts], also what did not fit
+  CutBin* cut;       // [R]
+
+  __host__ __device__ int pooled() const { return parts * (kPartThreads / kWave) * of_wave; }
+  static size_t carve(void* ws, int64_t R, int parts, Split* s) {
+    Carve c(ws);
+    Split t{};
+    t.parts = parts;
+    t.max = c.take<float>((size_t)R * parts);
+    t.arg = c.take<int>((size_t)R * parts);
+    t.pool = c.take<uint32_t>((size_t)R * kPool);
+    t.of_wave = std::min(8, kPool / (parts * (kPartThreads / kWave)));
+    t.share = c.take<uint64_t>((size_t)R * parts);
+    t.count = c.take<uint32_t>((size_t)R * parts);
+    t.mass = c.take<uint64_t>((size_t)R * parts * kBins);
+    t.list = c.take<uint64_t>((size_t)R * parts * kPartList);
+    t.n_list = c.take<uint32_t>((size_t)R * parts);
+    t.cut = c.take<CutBin>((size_t)R);
+    if (s) *s = t;
+    return c.off;
+  }
+};
+
+// Parts that a row is shared among: from the length on where several launches take less than one block (1 row of 32003
+// float32: 19 us in one block with top-k 50, 22 in parts; of 128011 bf16 29 and 23), and where the rows alone leave most
+// compute units idle.
+inline int split_parts(int64_t R, int C, int dtype) {
+  const int per = 16 / rows::type_size(dtype);
+  const int Q = (C + 2 * per - 2) / per;  // as of a row that is not aligned
+  if (Q <= 8192 || R > cu_count() / 2) return 1;
+  const int parts = (Q + kPartVectors - 1) / kPartVectors;
+  return parts <= kMostParts ? parts : 1;
+}
+
+// What the launches after the first know of a row.
+struct SplitRow {
+  float max;
+  bool listed, cut;  // top-k is collected; a top-p cut is looked for
+  bool general;      // neither: a longer top-k, or nothing but -inf
+  __device__ __forceinline__ SplitRow(const Sample& a, const Split& s, int64_t r, const RowSettings& set) {
+    const int l = threadIdx.x % kWave;
+    const float m = l < s.parts ? s.max[r * s.parts + l] : -INFINITY;
+    max = wave_reduce(m, Larger());
+    listed = set.k <= s.pooled() - s.pooled() / 8;  // collected by the bound
+    cut = set.k == a.C && set.top_p < 1.0f && !listed;
+    general = max == -INFINITY || (!listed && set.k < a.C);
+  }
+};
+
+template <class T>
+__global__ __launch_bounds__(kPartThreads) void split_max(Sample a, Split s) {
+  constexpr int kVec = Row<T>::kVec;
+  constexpr int kWaves = kPartThreads / kWave;
+  __shared__ float fred[kWaves];
+  __shared__ int ired[kWaves];
+  const int64_t r = blockIdx.x / s.parts;
+  const int p = blockIdx.x % s.parts, tid = threadIdx.x;
+  const Row<T> row(a.logits, r, a.ld, a.C);
+  const RowSettings set(a.set, r, a.C);
+  const int q0 = p * s.each;
+  uint4 u[4];
+  load_vectors<T, kPartThreads>(row, u, q0, min(row.Q, q0 + s.each));
+  if (tid == 0) s.n_list[r * s.parts + p] = 0;
+  float m = -INFINITY;
+  int at = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x[kVec];
+    unpack<T>(u[i], x);
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+      const bool up = x[k] > m;  // never for NaN
+      m = up ? x[k] : m;
+      at = up ? row.first(q0 + i * kPartThreads + tid) + k : at;
+    }
+  }
+  uint32_t key = key_of(m);
+  for (int k = 0; k < s.of_wave; ++k) {  // the wave's largest lanes, one after another
+    const uint32_t v = wave_max_u32(key);
+    if (lane_id() == (int)__builtin_ctzll(__ballot(key == v))) {
+      key = 0;
+      s.pool[r * kPool + (p * kWaves + tid / kWave) * s.of_wave + k] = v;
+    }
+  }
+  const float most = wave_reduce(m, Larger());
+  int first = m == most ? at : INT32_MAX;
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) first = min(first, __shfl_xor(first, off, kWave));
+  if (tid % kWave == 0) {
+    fred[tid / kWave] = most;
+    ired[tid / kWave] = first;
+  }
+  __syncthreads();
+  if (tid != 0) return;
+  float all = fred[0];
+  for (int k = 1; k < kWaves; ++k) all = fmaxf(all, fred[k]);
+  first = INT32_MAX;
+  for (int k = 0; k < kWaves; ++k) first = fred[k] == all ? min(first, ired[k]) : first;
+  s.max[r * s.parts + p] = all;
+  s.arg[r * s.parts + p] = first;
+}
+
+// A part's list, put together in LDS.
+struct PartList {
+  uint64_t entry_[kPartList];
+  uint32_t n;
+  __device__ __forceinline__ void add(float x, int j) {
+    const uint32_t at = atomicAdd(&n, 1u);
+    if (at < (uint32_t)kPartList) entry_[at] = entry(key_of(x), j);
+  }
+  __device__ __forceinline__ void put(const Split& s, int64_t part) const {  // after a barrier
+    for (uint32_t e = threadIdx.x; e < min(n, (uint32_t)kPartList); e += kPartThreads)
+      s.list[part * kPartList + e] = entry_[e];
+    if (threadIdx.x == 0) s.n_list[part] = n;
+  }
+};
+
+template <class T>
+__global__ __launch_bounds__(kPartThreads) void split_sum(Sample a, Split s) {
+  constexpr int kVec = Row<T>::kVec;
+  __shared__ uint64_t mass[kBins];
+  __shared__ PartList list;
+  __shared__ uint32_t pool[kPool], bound;
+  const int64_t r = blockIdx.x / s.parts;
+  const int p = blockIdx.x % s.parts, tid = threadIdx.x;
+  const RowSettings set(a.set, r, a.C);
+  const SplitRow known(a, s, r, set);
+  if (set.k == 1 || known.general || !(known.listed || known.cut)) return;
+  const Row<T> row(a.logits, r, a.ld, a.C);
+  const int q0 = p * s.each;
+  uint4 u[4];
+  load_vectors<T, kPartThreads>(row, u, q0, min(row.Q, q0 + s.each));
+  if (known.cut)
+    for (int b = tid; b < kBins; b += kPartThreads) mass[b] = 0;
+  if (tid == 0) list.n = 0;
+  const int pooled = s.pooled();
+  const uint32_t mine = tid < pooled ? s.pool[r * kPool + tid] : 0;
+  pool[tid] = mine;
+  __syncthreads();
+  if (known.listed && tid < pooled) {  // the k-th largest of the pool
+    int above = 0, equal = 0;
+#pragma unroll 8
+    for (int o = 0; o < pooled; ++o) {
+      above += pool[o] > mine;
+      equal += pool[o] == mine;
+    }
+    if (above < set.k && above + equal >= set.k) bound = mine;
+  }
+  __syncthreads();
+  const float least = of_key(bound);
+  const Weigh weigh{known.max, 1.0f / set.temperature};
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    float x[kVec];
+    unpack<T>(i < 2 ? (i == 0 ? u[0] : u[1]) : (i == 2 ? u[2] : u[3]), x);
+    const int j = row.first(q0 + i * kPartThreads + tid);
+    if (known.listed) {
+#pragma unroll
+      for (int k = 0; k < kVec; ++k)
+        if (x[k] >= least && x[k] > -INFINITY) list.add(x[k], j + k);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) {
+        const float y = no_nan(x[k]);
+        const uint32_t w = weigh(y);
+        if (w) atomicAdd((unsigned long long*)&mass[bin_of(weigh.t(y))], (unsigned long long)w);
+      }
+    }
+  }
+  __syncthreads();
+  const int64_t part = r * s.parts + p;
+  if (known.listed) list.put(s, part);
+  else
+    for (int b = tid; b < kBins; b += kPartThreads) s.mass[part * kBins + b] = mass[b];
+}
+
+template <class T>
+__global__ __launch_bounds__(kBins) void split_cut(Sample a, Split s) {
+  __shared__ uint64_t red[kBins / kWave];
+  const int64_t r = blockIdx.x;
+  const RowSettings set(a.set, r, a.C);
+  const SplitRow known(a, s, r, set);
+  if (set.k == 1 || known.general || !known.cut) return;
+  uint64_t w = 0;
+#pragma unroll 8
+  for (int p = 0; p < s.parts; ++p) w += s.mass[(r * s.parts + p) * kBins + threadIdx.x];
+  const uint64_t limit = set.limit(block_sum64<kBins>(w, red));
+  const uint64_t b = block_exclusive<kBins>(w, red);
+  if (b < limit && b + w >= limit) s.cut[r] = CutBin{b, limit, (int)threadIdx.x};
+}
+
+template <class T>
+__global__ __launch_bounds__(kPartThreads) void split_share(Sample a, Split s) {
+  constexpr int kVec = Row<T>::kVec;
+  __shared__ uint64_t red[kPartThreads / kWave];
+  __shared__ PartList list;
+  const int64_t r = blockIdx.x / s.parts;
+  const int p = blockIdx.x % s.parts, tid = threadIdx.x;
+  const RowSettings set(a.set, r, a.C);
+  const SplitRow known(a, s, r, set);
+  if (set.k == 1 || known.general || known.listed) return;
+  const Row<T> row(a.logits, r, a.ld, a.C);
+  const int q0 = p * s.each;
+  uint4 u[4];
+  load_vectors<T, kPartThreads>(row, u, q0, min(row.Q, q0 + s.each));
+  const int bin = known.cut ? s.cut[r].bin : kBins;
+  if (tid == 0) list.n = 0;
+  __syncthreads();
+  const Weigh weigh{known.max, 1.0f / set.temperature};
+  uint64_t sum = 0, count = 0;
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    float x[kVec];
+    unpack<T>(i < 2 ? (i == 0 ? u[0] : u[1]) : (i == 2 ? u[2] : u[3]), x);
+    const int j = row.first(q0 + i * kPartThreads + tid);
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+      const float y = no_nan(x[k]), t = weigh.t(y), e = exp_down(t);
+      const uint32_t w = weigh.of(y, e);
+      const int b = w ? bin_of(t) : kBins + 1;
+      if (b == bin) list.add(y, j + k);
+      const bool in = (b < bin) & (e >= set.min_p);
+      sum += in ? w : 0;
+      count += in;
+    }
+  }
+  sum = block_sum64<kPartThreads>(sum, red);
+  count = block_sum64<kPartThreads>(count, red);
+  if (tid == 0) {
+    s.share[r * s.parts + p] = sum;
+    s.count[r * s.parts + p] = (uint32_t)count;
+  }
+  list.put(s, r * s.parts + p);
+}
+
+constexpr int kDrawThreads = 1024;
+
+template <class T>
+__global__ __launch_bounds__(kDrawThreads) void split_draw(Sample a, Split s) {
+  using Lds = TileLds<kDrawThreads, 4>;
+  __shared__ Lds lds;
+  __shared__ uint64_t share[kMostParts], last_kept;
+  const int64_t r = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid % kWave;
+  const Row<T> row(a.logits, r, a.ld, a.C);
+  const RowSettings set(a.set, r, a.C);
+  const SplitRow known(a, s, r, set);
+  // where each part's collected elements go in the row's list
+  const uint32_t own = lane < s.parts ? s.n_list[r * s.parts + lane] : 0;
+  const uint32_t upto_own = (uint32_t)wave_upto64(own);
+  const uint32_t n = (uint32_t)__builtin_amdgcn_readlane((int)upto_own, kWave - 1);
+  if (known.general || n > (uint32_t)kRowList || __ballot(own > (uint32_t)kPartList)) return sample_general<T, kDrawThreads>(a, r, row, set, lds.general);
+  if (set.k == 1) {
+    int at = lane < s.parts && s.max[r * s.parts + lane] == known.max ? s.arg[r * s.parts + lane] : INT32_MAX;
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1) at = min(at, __shfl_xor(at, off, kWave));
+    if (tid == 0) a.answer(r, at, 0.0f, 1);
+    return;
+  }
+  const Weigh weigh{known.max, 1.0f / set.temperature};
+  for (int p = tid / kWave; p < s.parts; p += kDrawThreads / kWave) {
+    const uint32_t to = (uint32_t)__builtin_amdgcn_readlane((int)upto_own, p);
+    const uint32_t m = (uint32_t)__builtin_amdgcn_readlane((int)own, p);
+    for (uint32_t e = lane; e < m; e += kWave) lds.list[to - m + e] = s.list[(r * s.parts + p) * kPartList + e];
+  }
+  __syncthreads();
+  if (known.listed) {
+    return draw_from_list<T, kDrawThreads, 4>(a, r, row, set, weigh, (int)n, 0, lds);
+  }
+  // the parts' kept weights, with those of the cut's bin that are kept
+  uint64_t counted = 0;
+  if (tid < kMostParts) share[tid] = tid < s.parts ? s.share[r * s.parts + tid] : 0;
+  if (tid < s.parts) counted = s.count[r * s.parts + tid];
+  float cut = -INFINITY;
+  int last = a.C;
+  if (known.cut) {
+    const CutBin at = s.cut[r];
+    order_list<kDrawThreads>(weigh, (int)n, lds);
+    if (tid < (int)n) {  // n <= kRowList = kDrawThreads
+      const uint64_t mine = lds.list[tid], before = at.above + lds.before[tid];
+      const uint32_t w = lds.weight[tid];
+      if (before < at.limit) {
+        if (before + w >= at.limit) last_kept = mine;
+        if (weigh.e(logit_of(mine)) >= set.min_p) {
+          atomicAdd((unsigned long long*)&share[((int)(uint32_t)mine + row.lead) / Row<T>::kVec / s.each],
+                    (unsigned long long)w);
+          ++counted;
+        }
+      }
+    }
+    __syncthreads();
+    cut = logit_of(last_kept);
+    last = (int)(uint32_t)last_kept;
+  }
+  counted = block_sum64<kDrawThreads>(counted, lds.red);
+  __syncthreads();
+  const uint64_t mine = share[lane], upto = wave_upto64(mine), total = lane_of64(upto, kWave - 1);
+  const uint64_t point = set.point(total);
+  const int p = (int)__builtin_ctzll(__ballot(upto > point));
+  const auto kept = [&](float x, int j) -> uint64_t {
+    const float e = weigh.e(x);
+    return ((x > cut) | ((x == cut) & (j <= last))) & (e >= set.min_p) ? weigh.of(x, e) : 0;
+  };
+  const int j = find_in_order<T, kDrawThreads>(row, kept, point - lane_of64(upto - mine, p), lds.red, p * s.each,
+                                               min(row.Q, (p + 1) * s.each));
+  if (tid == 0) a.answer(r, j, log_share(weigh, no_nan(row.at(j)), total), (int)counted);
+}
+
 }  // namespace
 }  // namespace snn
 
 using namespace snn;
 
+extern "C" size_t snn_readout_sample_workspace(int64_t R, int C, int dtype) {
+  if (R <= 0 || R > INT32_MAX || bad_dim(C) || C > rows::kMaxClasses || rows::type_size(dtype) == 0) return 0;
+  const int parts = split_parts(R, C, dtype);
+  return parts > 1 ? Split::carve(nullptr, R, parts, nullptr) : 0;
+}
+
 extern "C" snn_status snn_readout_sample(const void* logits, int dtype, int64_t R, int C, int64_t ld, const float* u,
                                          const float* temperature, const int32_t* top_k, const float* top_p,
-                                         const float* min_p, int32_t* cls, float* logp, int32_t* kept, void* stream) {
+                                         const float* min_p, int32_t* cls, float* logp, int32_t* kept, void* workspace,
+                                         size_t workspace_bytes, void* stream) {
   const snn_status ok = rows::check_rows(logits, dtype, R, C, ld);
   if (ok != SNN_OK) return ok;
   if (!u || !cls) return SNN_ERR_INVALID_ARG;
+  const size_t need = snn_readout_sample_workspace(R, C, dtype);
+  if (need && (!workspace || workspace_bytes < need)) return SNN_ERR_INVALID_ARG;
   const Sample a{logits, R, C, ld, Settings{u, temperature, top_k, top_p, min_p}, cls, logp, kept};
   hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)R);
   return rows::for_type(dtype, [&](auto type) {
     using T = decltype(type);
     const int Q = rows::most_vectors<T>(logits, C, ld);
-    if (C <= rows::kShortRow)
+    if (C <= rows::kShortRow && (C <= 32 || R > cu_count()))
       hipLaunchKernelGGL((sample_short<T>), dim3((unsigned)((R + rows::kShortRows - 1) / rows::kShortRows)), dim3(256),
                          0, s, a);
-    else if (Q <= 4 * 64)
+    else if (Q <= 4 * 64 && R > cu_count())  // fewer rows: more threads on each (1 row of 1000, top-k 50: 39 and 14 us)
       hipLaunchKernelGGL((sample_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
     else if (Q <= 4 * 256)
       hipLaunchKernelGGL((sample_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
     else if (Q <= 4 * 1024)
       hipLaunchKernelGGL((sample_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
-    else if (Q <= 16 * 1024)
+    else if (const int parts = split_parts(R, C, dtype); parts > 1) {
+      Split split;
+      Split::carve(workspace, R, parts, &split);
+      split.each = (Q + parts - 1) / parts;
+      const dim3 all((unsigned)(R * parts)), threads(kPartThreads);
+      hipLaunchKernelGGL((split_max<T>), all, threads, 0, s, a, split);
+      if (top_k || top_p) hipLaunchKernelGGL((split_sum<T>), all, threads, 0, s, a, split);
+      if (top_p) hipLaunchKernelGGL((split_cut<T>), grid, dim3(kBins), 0, s, a, split);
+      hipLaunchKernelGGL((split_share<T>), all, threads, 0, s, a, split);
+      hipLaunchKernelGGL((split_draw<T>), grid, dim3(kDrawThreads), 0, s, a, split);
+    } else if (Q <= 16 * 1024)
       hipLaunchKernelGGL((sample_tile<T, 1024, 16>), grid, dim3(1024), 0, s, a);
     else
       hipLaunchKernelGGL((sample_rows<T, 1024>), grid, dim3(1024), 0, s, a);

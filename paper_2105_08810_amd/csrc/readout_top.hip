@@ -334,6 +334,8 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
       hipLaunchKernelGGL((top_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
     else if (Q <= 4 * 256 && K <= 4 * kNthMost)
       hipLaunchKernelGGL((top_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
+    else if (Q <= 8 * 512 && K <= 8 * kNthMost && R >= cu_count())
+      hipLaunchKernelGGL((top_tile<T, 512, 8>), grid, dim3(512), 0, s, a);
     else if (Q <= 4 * 1024 && K <= 16 * kNthMost)
       hipLaunchKernelGGL((top_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
     else if (Q <= 16 * 1024 && K <= 16 * kNthMost)

@@ -47,8 +47,9 @@ struct Row {
   int C;
   int Q;          // vectors that hold a part of the row
 
-  __device__ __forceinline__ Row(const void* logits, int64_t r, int64_t ld, int C_) : C(C_) {
-    const T* p = static_cast<const T*>(logits) + r * ld;
+  __device__ __forceinline__ Row(const void* logits, int64_t r, int64_t ld, int C_)
+      : Row(static_cast<const T*>(logits) + r * ld, C_) {}
+  __device__ __forceinline__ Row(const T* p, int C_) : C(C_) {
     lead = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
     base = p - lead;
     Q = (lead + C + kVec - 1) / kVec;
@@ -134,10 +135,10 @@ __device__ __forceinline__ void Row<T>::load(int q, float (&x)[kVec]) const {
   unpack<T>(load_raw(*this, q), x);
 }
 
-// Vectors i * NT + thread of a row, -inf outside it. All loads are under way before anything waits: threads past the
-// row's whole vectors load its last one.
+// Vectors q0 + i * NT + thread below q1 of a row, -inf outside. All loads are under way before anything waits: threads
+// past the row's whole vectors load its last one.
 template <class T, int NT, int NV>
-__device__ __forceinline__ void load_vectors(const Row<T>& row, uint4 (&u)[NV]) {
+__device__ __forceinline__ void load_vectors(const Row<T>& row, uint4 (&u)[NV], int q0, int q1) {
   constexpr int kVec = Row<T>::kVec;
   const int tid = (int)threadIdx.x;
   const int from = row.lead ? 1 : 0, to = (row.lead + row.C) / kVec;  // whole vectors
@@ -153,18 +154,18 @@ __device__ __forceinline__ void load_vectors(const Row<T>& row, uint4 (&u)[NV]) 
   if (to > from) {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-      u[i] = *reinterpret_cast<const uint4*>(row.base + (size_t)min(max(i * NT + tid, from), to - 1) * kVec);
+      u[i] = *reinterpret_cast<const uint4*>(row.base + (size_t)min(max(q0 + i * NT + tid, from), to - 1) * kVec);
   }
   uint4 first = none, last = none;  // the ends of the row
-  if (from == 1 && tid == 0) first = load_raw(row, 0);
-  if (to < row.Q && to >= from && tid == to % NT) last = load_raw(row, to);
+  if (q0 == 0 && from == 1 && tid == 0) first = load_raw(row, 0);
+  if (to < row.Q && to >= from && to >= q0 && to < q1 && tid == (to - q0) % NT) last = load_raw(row, to);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int q = i * NT + tid;
-    const bool in = q >= from && q < to, end = q == to && to >= from;
+    const int q = q0 + i * NT + tid;
+    const bool in = q >= from && q < to && q < q1, end = q == to && to >= from && q < q1;
     uint4 e = make_uint4(end ? last.x : none.x, end ? last.y : none.y, end ? last.z : none.z, end ? last.w : none.w);
     if (i == 0) {
-      const bool head = tid < from;
+      const bool head = q < from;
       e = make_uint4(head ? first.x : e.x, head ? first.y : e.y, head ? first.z : e.z, head ? first.w : e.w);
     }
     u[i] = make_uint4(in ? u[i].x : e.x, in ? u[i].y : e.y, in ? u[i].z : e.z, in ? u[i].w : e.w);
@@ -197,7 +198,7 @@ struct Tile {
   }
   __device__ __forceinline__ void load(const Row<T>& row) {
     uint4 u[NV];
-    load_vectors<T, NT>(row, u);
+    load_vectors<T, NT>(row, u, 0, row.Q);
 #pragma unroll
     for (int i = 0; i < NV; ++i) put(w[i / kPart], i % kPart, u[i]);
   }
@@ -401,7 +402,7 @@ struct SelectLds {
   static constexpr int kBins = NT == kWave ? 256 : 1024;  // 256: many one-wave blocks of a CU share its LDS
   uint64_t mass[kBins];
   uint32_t count[kBins];
-  uint32_t list[kShort];
+  uint32_t list[kShort], weight[kShort];
   uint64_t red[NT / kWave];
   uint64_t before_mass;
   uint32_t before_count, part_count, part, n_list;
@@ -492,20 +493,22 @@ __device__ __forceinline__ Cut find_cut(const Row<T>& row, W weigh, uint32_t lo,
     listing = s.part_count <= kShort;
   }
   const int n = (int)s.n_list;
+  if (MASS) {
+    for (int e = tid; e < n; e += NT) s.weight[e] = weigh(of_key(s.list[e]));
+    __syncthreads();
+  }
   for (int e = tid; e < n; e += NT) {
     const uint32_t k = s.list[e];
     uint64_t m = above_mass;
     uint32_t c = above_count, equal = 0;
-#pragma unroll 1
+#pragma unroll 4
     for (int o = 0; o < n; ++o) {
       const uint32_t ko = s.list[o];
-      if (ko > k) {
-        ++c;
-        if (MASS) m += weigh(of_key(ko));
-      }
+      c += ko > k;
       equal += ko == k;
+      if (MASS) m += ko > k ? s.weight[o] : 0;
     }
-    const uint64_t at = by_mass ? m : c, to = by_mass ? m + (uint64_t)equal * weigh(of_key(k)) : (uint64_t)c + equal;
+    const uint64_t at = by_mass ? m : c, to = by_mass ? m + (uint64_t)equal * s.weight[e] : (uint64_t)c + equal;
     if (at < limit && to >= limit) {  // every element of the value says the same
       s.cut_key = k;
       s.cut_equal = equal;

@@ -63,7 +63,8 @@ _SIGNATURES = {
     "snn_readout_top": (_I, [_P, _I, _I64, _I, _I64, _I, _F, _P, _P, _P, _P]),
     "snn_readout_distill_workspace": (_SZ, [_I64, _I, _I]),
     "snn_readout_distill": (_I, [_P, _I, _I64, _I, _I64, _P, _P, _P, _I, _F, _P, _P, _P, _P, _I64, _I, _P, _SZ, _P]),
-    "snn_readout_sample": (_I, [_P, _I, _I64, _I, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "snn_readout_sample_workspace": (_SZ, [_I64, _I, _I]),
+    "snn_readout_sample": (_I, [_P, _I, _I64, _I, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
     "snn_activity_reg_workspace": (_SZ, [_I, _I, _I]),
     "snn_activity_reg": (_I, [_P, _I, _I, _I, _F, _F, _F, _F, _P, _P, _P, _P, _SZ, _P]),
     "snn_activity_reg_grad": (_I, [_P, _I, _I, _I, _P, _P, _I64, _P, _P]),
@@ -410,13 +411,18 @@ def snn_readout_distill(logits, ids, vals, lse, K, tau, weight, loss, row_loss, 
         int(accumulate), _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
 
 
-def snn_readout_sample(logits, u, temperature, top_k, top_p, min_p, cls, logp=None, kept=None, stream=None):
+def snn_readout_sample_workspace(R, C, dtype) -> int:
+    return int(lib().snn_readout_sample_workspace(R, C, _DTYPES[dtype]))
+
+
+def snn_readout_sample(logits, u, temperature, top_k, top_p, min_p, cls, logp=None, kept=None, ws=None, stream=None):
     p, code, R, C, ld = _rows(logits)
     _check("snn_readout_sample", lib().snn_readout_sample(
         p, code, R, C, ld, _of_rows(u, R, torch.float32, "u"), _of_rows(temperature, R, torch.float32, "temperature"),
         _of_rows(top_k, R, torch.int32, "top_k"), _of_rows(top_p, R, torch.float32, "top_p"),
         _of_rows(min_p, R, torch.float32, "min_p"), _of_rows(cls, R, torch.int32, "cls"),
-        _of_rows(logp, R, torch.float32, "logp"), _of_rows(kept, R, torch.int32, "kept"), _stream(stream)))
+        _of_rows(logp, R, torch.float32, "logp"), _of_rows(kept, R, torch.int32, "kept"),
+        _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
 
 
 def snn_activity_reg_workspace(T, B, N) -> int:
@@ -641,13 +647,18 @@ def readout_ce(V_out: torch.Tensor, labels: torch.Tensor, mode: int, dense=False
     return Csr(row_ptr, col, None, None, nnz), eps, loss, ed
 
 
+# These three are called once a step or a token on little data, where the host's work is most of the time: they check
+# what they are given and not again what they have made themselves.
+
 def readout_top(logits: torch.Tensor, K: int, tau=1.0, want_lse=True, stream=None):
     """A teacher's record of rows of logits [..., C]: (ids [..., K] int32, vals [..., K], lse [...] or None)."""
+    p, code, R, C, ld = _rows(logits)
     shape, dev = logits.shape[:-1], logits.device
     ids = torch.empty((*shape, K), dtype=torch.int32, device=dev)
     vals = torch.empty((*shape, K), dtype=torch.float32, device=dev)
     lse = torch.empty(shape, dtype=torch.float32, device=dev) if want_lse else None
-    snn_readout_top(logits, K, tau, ids, vals, lse, stream)
+    _check("snn_readout_top", lib().snn_readout_top(p, code, R, C, ld, K, tau, ids.data_ptr(), vals.data_ptr(),
+                                                    lse.data_ptr() if want_lse else None, _stream(stream)))
     return ids, vals, lse
 
 
@@ -656,33 +667,49 @@ def readout_distill(logits: torch.Tensor, ids, vals, lse=None, tau=1.0, weight=N
     """Distillation loss of rows of logits [..., C] against a teacher's records. Returns (loss [1], row_loss [...],
     grad like the logits, or None). A grad that is given is written, or added to with accumulate; one that is made has
     the rows of the logits at the same distance, since rows that begin alike are written fastest."""
-    dev = logits.device
-    loss = torch.empty(1, dtype=torch.float32, device=dev)
-    row_loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=dev)
     if accumulate and grad is None:
         raise ValueError("readout_distill: accumulate needs a grad to add to")
-    if grad is None and want_grad:
-        C, ld = logits.shape[-1], logits.stride(-2)
-        if logits.dim() != 2 or ld == C:
-            grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
-        else:  # rows far apart (a narrow part of a wide matrix): whole 64-byte lines instead
-            grad = torch.empty((logits.shape[0], ld if C < ld < 2 * C else -(-C // 32) * 32), dtype=logits.dtype,
-                               device=dev)[:, :C]
+    p, code, R, C, ld = _rows(logits)
+    dev, K = logits.device, ids.shape[-1]
+    loss = torch.empty(1, dtype=torch.float32, device=dev)
+    row_loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=dev)
+    g, ld_grad = None, 0
+    if grad is not None:
+        g, code_g, R_g, C_g, ld_grad = _rows(grad, "grad")
+        if (code_g, R_g, C_g) != (code, R, C):
+            raise ValueError("grad must have the type and the shape of the logits")
+    elif want_grad:
+        if ld == C:
+            grad, ld_grad = torch.empty(logits.shape, dtype=logits.dtype, device=dev), C
+        else:  # of rows far apart (a narrow part of a wide matrix) whole 64-byte lines instead
+            ld_grad = ld if ld < 2 * C else -(-C // 32) * 32
+            grad = torch.empty((R, ld_grad), dtype=logits.dtype, device=dev)[:, :C]
+        g = grad.data_ptr()
+    fn = lib().snn_readout_distill
     if ws is None:
-        R = row_loss.numel()
-        ws = workspace(snn_readout_distill_workspace(R, logits.shape[-1], logits.dtype), dev)
-    snn_readout_distill(logits, ids, vals, lse, ids.shape[-1], tau, weight, loss, row_loss, grad, accumulate, ws, stream)
+        ws = torch.empty(max(1, lib().snn_readout_distill_workspace(R, C, code)), dtype=torch.uint8, device=dev)
+    _check("snn_readout_distill", fn(
+        p, code, R, C, ld, _of_rows(ids, R * K, torch.int32, "ids"), _of_rows(vals, R * K, torch.float32, "vals"),
+        _of_rows(lse, R, torch.float32, "lse"), K, tau, _of_rows(weight, R, torch.float32, "weight"), loss.data_ptr(),
+        row_loss.data_ptr(), g, ld_grad, int(accumulate), _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
     return loss, row_loss, grad
 
 
-def readout_sample(logits: torch.Tensor, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+def readout_sample(logits: torch.Tensor, u, temperature=None, top_k=None, top_p=None, min_p=None, ws=None, stream=None):
     """One class drawn per row of logits [..., C] from uniforms u [...]; the settings are arrays [...] on the device, or
     None. Returns (cls [...] int32, logp [...], kept [...] int32)."""
+    p, code, R, C, ld = _rows(logits)
     shape, dev = logits.shape[:-1], logits.device
     cls = torch.empty(shape, dtype=torch.int32, device=dev)
     logp = torch.empty(shape, dtype=torch.float32, device=dev)
     kept = torch.empty(shape, dtype=torch.int32, device=dev)
-    snn_readout_sample(logits, u, temperature, top_k, top_p, min_p, cls, logp, kept, stream)
+    if ws is None and (need := lib().snn_readout_sample_workspace(R, C, code)):
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    f32 = torch.float32
+    _check("snn_readout_sample", lib().snn_readout_sample(
+        p, code, R, C, ld, _of_rows(u, R, f32, "u"), _of_rows(temperature, R, f32, "temperature"),
+        _of_rows(top_k, R, torch.int32, "top_k"), _of_rows(top_p, R, f32, "top_p"), _of_rows(min_p, R, f32, "min_p"),
+        cls.data_ptr(), logp.data_ptr(), kept.data_ptr(), _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
     return cls, logp, kept
 
 

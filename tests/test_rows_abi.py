@@ -58,9 +58,10 @@ def _distill(lib, **kw):
 
 
 def _sample(lib, **kw):
-    return _call(lib.snn_readout_sample, "logits dtype R C ld u temperature top_k top_p min_p cls logp kept stream".split(),
+    return _call(lib.snn_readout_sample, ("logits dtype R C ld u temperature top_k top_p min_p cls logp kept ws "
+                                          "ws_bytes stream").split(),
                  dict(logits=FAKE, dtype=0, R=10, C=100, ld=100, u=FAKE, temperature=FAKE, top_k=FAKE, top_p=FAKE,
-                      min_p=FAKE, cls=FAKE, logp=FAKE, kept=FAKE, stream=None), kw)
+                      min_p=FAKE, cls=FAKE, logp=FAKE, kept=FAKE, ws=None, ws_bytes=0, stream=None), kw)
 
 
 @pytest.mark.parametrize("call", [_top, _distill, _sample])
@@ -92,7 +93,8 @@ def test_distill_rejects(lib, kw):
     assert _distill(lib, **kw) == snn.SNN_ERR_INVALID_ARG
 
 
-@pytest.mark.parametrize("kw", [dict(u=None), dict(cls=None)])
+@pytest.mark.parametrize("kw", [dict(u=None), dict(cls=None), dict(R=1, C=131072, ld=131072),
+                                dict(R=1, C=131072, ld=131072, ws=FAKE, ws_bytes=100)])
 def test_sample_rejects(lib, kw):
     assert _sample(lib, **kw) == snn.SNN_ERR_INVALID_ARG
 
@@ -104,6 +106,14 @@ def test_distill_workspace(lib):
     for bad in ((0, 100, 0), (-1, 100, 0), (10, 0, 0), (10, 100, 3), (1 << 31, 100, 0), (10, (1 << 20) + 1, 0)):
         assert size(*bad) == 0
     assert size(777, 333, 1) == size(777, 333, 1)
+
+
+def test_sample_workspace(lib):
+    size = lib.snn_readout_sample_workspace
+    assert size(1, 131072, 0) > 0 and size(2, 131072, 1) > size(1, 131072, 1) > 0  # few long rows
+    assert size(1, 1000, 0) == 0 and size(100000, 131072, 0) == 0 and size(1, 1 << 20, 0) == 0
+    for bad in ((0, 131072, 0), (-1, 131072, 0), (1, 0, 0), (1, 131072, 3), (1 << 31, 131072, 0), (1, (1 << 20) + 1, 0)):
+        assert size(*bad) == 0
 
 
 @pytest.mark.skipif(SAN_LIB is not None, reason="the binding loads the ordinary library")

@@ -19,7 +19,64 @@ INF = float("inf")
 
 
 @dataclass
-class Network:
+class Record:
+    """A teacher's answers at every step of every sample (snn_readout_top): the K largest logits of each row, their
+    classes, the row's log-sum-exp at temperature tau."""
+    ids: torch.Tensor  # [T, B, K] int32
+    vals: torch.Tensor  # [T, B, K]
+    lse: Optional[torch.Tensor]  # [T, B]; None: the K classes are taken as all of the teacher
+    tau: float = 1.0
+
+
+@dataclass
+class Distill:
+    """Distillation of a network's readout from a teacher's record, a term of the training loss beside the
+    cross-entropy: sum over the rows of weight_r KL(teacher || student at step t of sample b). weight None: the mean
+    over all rows, times `scale`."""
+    record: Record
+    weight: Optional[torch.Tensor] = None  # [T, B]; rows of weight 0 are not read
+    scale: float = 1.0
+
+
+class ReadoutRows:
+    """What both kinds of network do with their readout's rows: the membrane V_out [T, B, C] read as the logits of
+    every step of every sample."""
+
+    def record(self, K: int, tau: float = 1.0) -> Record:
+        """The forward's answers as a teacher's record."""
+        ids, vals, lse = snn.readout_top(self.V_out, K, tau)
+        return Record(ids, vals, lse, tau)
+
+    def draw(self, u: torch.Tensor, temperature=None, top_k=None, top_p=None, min_p=None, step: Optional[int] = None):
+        """One class per sample and step drawn from uniforms u [T, B], or at one step from u [B]; settings as in
+        snn.readout_sample. Returns (classes int32, log-probabilities, numbers of classes kept)."""
+        rows = self.V_out if step is None else self.V_out[step]
+        return snn.readout_sample(rows, u, temperature, top_k, top_p, min_p)
+
+    def readout_distilled(self, distill: Distill, dense=False):
+        """readout() with the distillation's gradient added: (CSR of every entry of V_out, eps at them, cross-entropy,
+        dL/dV_out densely or None, distillation loss). The distillation reaches every entry, so the CSR is that of the
+        sum over time for either loss mode."""
+        T, B, C = self.V_out.shape
+        rec, weight = distill.record, distill.weight
+        if weight is None and distill.scale != 1.0:
+            weight = torch.full((T, B), distill.scale / (T * B), dtype=torch.float32, device=self.V_out.device)
+        csr, eps, ce, eps_dense = self.readout(dense=dense or self.loss_mode == 0)
+        grad = eps.view(T, B, C) if self.loss_mode == 1 and not dense else eps_dense
+        kd, _, _ = snn.readout_distill(self.V_out, rec.ids, rec.vals, rec.lse, rec.tau, weight, grad=grad,
+                                       accumulate=True)
+        if self.loss_mode == 0:
+            if self._every is None:  # row r has its C entries from r C on
+                dev = self.V_out.device
+                self._every = snn.Csr(torch.arange(0, T * B * C + 1, C, dtype=torch.int32, device=dev),
+                                      torch.arange(C, dtype=torch.int32, device=dev).repeat(T * B), None, None,
+                                      T * B * C)
+            csr = self._every
+        return csr, grad.view(-1), ce, grad if dense else None, kd
+
+
+@dataclass
+class Network(ReadoutRows):
     X: torch.Tensor  # [T, B, N_in] uint8
     Ws: List[torch.Tensor]
     W_out: torch.Tensor
@@ -44,6 +101,7 @@ class Network:
     recompute_k: int = 0
     ck: List[torch.Tensor] = field(default_factory=list)
     _aux2: Optional[torch.cuda.Stream] = None  # second dW stream of the pipelined schedule
+    _every: Optional[snn.Csr] = None  # CSR of every entry of V_out (readout_distilled)
 
     @property
     def T(self):
@@ -255,21 +313,23 @@ class Network:
         return list(self.Ws) + [self.W_out]
 
     def train_step(self, opt: "Adam", b_th: float, reg: Optional["Penalty"] = None, sparse: bool = True,
-                   aux_stream=None, events=None):
+                   aux_stream=None, events=None, distill: Optional[Distill] = None):
         """One training step (App. E): forward, cross-entropy plus activity penalties, the sparse
         (or, with sparse=False, the dense) backward with truncation band b_th, and an Adam step on
         every weight matrix in place. b_th = inf with sparse=False is full-surrogate BPTT.
         events: optional list of 6 timing events recorded on the current stream at the phase
         boundaries (start, after forward, after loss and penalties, after compaction, after the
         backward, after Adam).
-        Returns a dict of device tensors: ce [1], penalty [1] (all layers), grads (list), nnz."""
+        distill: a teacher's record that the readout learns from beside its labels.
+        Returns a dict of device tensors: ce [1], penalty [1] (all layers), grads (list), nnz, and kd [1], the
+        distillation loss, with distill."""
         mark = (lambda k: events[k].record()) if events is not None else (lambda k: None)
         mark(0)
         self.forward(b_th if sparse and math.isfinite(b_th) else None)
         mark(1)
         acts = self.activity(reg) if reg is not None else None
         coefs = [a[0] for a in acts] if acts else None
-        ro = self.readout(dense=not sparse)
+        ro = self.readout(dense=not sparse) if distill is None else self.readout_distilled(distill, not sparse)
         mark(2)
         if sparse:
             csrs = self.compact(b_th)
@@ -288,7 +348,7 @@ class Network:
             pen = acts[0][1] if len(acts) == 1 else torch.cat([a[1] for a in acts]).sum(0, keepdim=True)
         else:
             pen = torch.zeros(1, device=self.X.device)
-        return {"ce": ro[2], "penalty": pen, "grads": grads, "nnz": nnz}
+        return {"ce": ro[2], "penalty": pen, "grads": grads, "nnz": nnz, **({} if distill is None else {"kd": ro[4]})}
 
 
 @dataclass
@@ -318,7 +378,7 @@ class Adam:
 
 
 @dataclass
-class ConvNetwork:
+class ConvNetwork(ReadoutRows):
     """The convolutional network of Sec. 3's convolutional experiment (App. E): a convolutional
     LIF layer (3x3, stride 1, padding 1, F filters) on input spikes [T, B, H, W, C], 2x2 max
     pooling of its spikes, and the infinite-threshold readout on the flattened pooled spikes."""
@@ -342,6 +402,7 @@ class ConvNetwork:
     V_out: Optional[torch.Tensor] = None
     S_out: Optional[torch.Tensor] = None
     trace_out: Optional[torch.Tensor] = None
+    _every: Optional[snn.Csr] = None  # CSR of every entry of V_out (readout_distilled)
 
     @property
     def dims(self):
@@ -522,19 +583,19 @@ class ConvNetwork:
         return dWc, dW_out, eps
 
     def train_step(self, opt: "Adam", b_th: float, reg: Optional["Penalty"] = None, sparse: bool = True,
-                   aux_stream=None, events=None):
+                   aux_stream=None, events=None, distill: Optional[Distill] = None):
         """One training step of the conv network (App. E), as Network.train_step: forward,
         cross-entropy plus the conv layer's activity penalties, the sparse (or dense) backward with
         band b_th, Adam on Wc and W_out in place. aux_stream is accepted for a common interface
         and not used. Returns a dict of device tensors: ce [1], penalty [1], grads [dWc, dW_out],
-        nnz ([conv layer's active-entry count] or None)."""
+        nnz ([conv layer's active-entry count] or None), and kd [1] with distill (as Network.train_step)."""
         mark = (lambda k: events[k].record()) if events is not None else (lambda k: None)
         mark(0)
         self.forward(b_th if sparse and math.isfinite(b_th) else None)
         mark(1)
         act = self.activity(reg) if reg is not None else None
         coef = act[0] if act else None
-        ro = self.readout(dense=not sparse)
+        ro = self.readout(dense=not sparse) if distill is None else self.readout_distilled(distill, not sparse)
         mark(2)
         if sparse:
             csrs = self.compact(b_th)
@@ -550,7 +611,7 @@ class ConvNetwork:
         opt.step(grads)
         mark(5)
         pen = act[1] if act else torch.zeros(1, device=self.X.device)
-        return {"ce": ro[2], "penalty": pen, "grads": grads, "nnz": nnz}
+        return {"ce": ro[2], "penalty": pen, "grads": grads, "nnz": nnz, **({} if distill is None else {"kd": ro[4]})}
 
 
 class Graphed:

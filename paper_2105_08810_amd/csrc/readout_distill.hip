@@ -100,7 +100,7 @@ __device__ __forceinline__ RowSums row_sums(Sum2 rest, Sum2 own, float listed_p,
   s.per = none ? 0.0f : 1.0f / all.total;
   s.mass = listed_p + p_t;
   const float q_t = empty(rest) ? 0.0f : rest.total * exp2_fast(or_zero(rest.max) - s.base) * s.per;
-  s.factor = empty(rest) ? 0.0f : (s.mass * q_t - p_t) / rest.total;
+  s.factor = empty(rest) ? 0.0f : (s.mass * q_t - p_t) * (1.0f / rest.total);
   const float lse_t = rest.max * kLn2 + logf(rest.total);  // -inf where there is nothing
   const float own_max = own.max * kLn2, top = or_zero(fmaxf(own_max, lse_t));
   s.lse = none ? 0.0f : top + logf(expf(lse_t - top) + own.total * expf(own_max - top));
@@ -133,22 +133,35 @@ __global__ __launch_bounds__(16 * ROWS) void distill_small(Distill a) {
   const int slot = threadIdx.x / 16, l = threadIdx.x % 16;
   const int64_t r = (int64_t)blockIdx.x * ROWS + slot;
   const int C = a.C, K = a.K;
+  // what does not wait for the weight is fetched beside it: the lane's first entry, the teacher's log-sum-exp
+  const int64_t at = min(r, a.R - 1);
+  const Row<T> row(a.logits, at, a.ld, C);
   const float w = r < a.R ? a.weight_of(r) : 0.0f;
-  const bool live = w != 0.0f;
-  const Row<T> row(a.logits, min(r, a.R - 1), a.ld, C);
-  uint4 raw[NV];
-  if (live) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) raw[i] = load_raw(row, l * NV + i);
-  }
+  const int id0 = l < K ? a.ids[at * K + l] : -1;
+  const float v0 = l < K ? a.vals[at * K + l] : 0.0f;
+  const float lse = a.lse ? a.lse[at] : 0.0f;
   int4* mine = reinterpret_cast<int4*>(&table[slot][l * kEach]);
   mine[0] = mine[1] = make_int4(kNotListed, kNotListed, kNotListed, kNotListed);
+  const bool live = w != 0.0f;
+  uint4 raw[NV];
+  if (live) {
+    const int from = row.lead ? 1 : 0, to = (row.lead + C) / kVec;  // whole vectors
+    if (to > from) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        raw[i] = *reinterpret_cast<const uint4*>(row.base + min(max(l * NV + i, from), to - 1) * kVec);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (l * NV + i < from || l * NV + i >= to) raw[i] = load_raw(row, l * NV + i);
+  }
   __syncthreads();
   const float inv_tau = 1.0f / a.tau;
   if (live) {
-    for (int k = l; k < K; k += 16) {
+    if (id0 >= 0 && id0 < C) table[slot][row.lead + id0] = __float_as_int(v0 * inv_tau);
+    for (int k = l + 16; k < K; k += 16) {
       const int id = a.ids[r * K + k];
-      if (id >= 0 && id < C) table[slot][row.lead + id] = __float_as_int(a.vals[r * K + k] / a.tau);
+      if (id >= 0 && id < C) table[slot][row.lead + id] = __float_as_int(a.vals[r * K + k] * inv_tau);
     }
   }
   __syncthreads();
@@ -175,7 +188,7 @@ __global__ __launch_bounds__(16 * ROWS) void distill_small(Distill a) {
     // the teacher: log p, and the sum of p
     float shift;
     if (a.lse) {
-      shift = a.lse[r];
+      shift = lse;
     } else {
       float top = lp[0], z = 0.0f;
 #pragma unroll
@@ -275,11 +288,11 @@ struct Entries {
   float held_v[kHeld];  // v / tau
   float x[kHeld];
   int id[kHeld];            // -1: no entry
-  float tau;
+  float inv_tau;
   const Row<T>& row;
 
   __device__ __forceinline__ Entries(const Distill& a, int64_t r, const Row<T>& row_)
-      : ids(a.ids + r * a.K), vals(a.vals + r * a.K), K(a.K), C(a.C), tau(a.tau), row(row_) {
+      : ids(a.ids + r * a.K), vals(a.vals + r * a.K), K(a.K), C(a.C), inv_tau(1.0f / a.tau), row(row_) {
 #pragma unroll
     for (int e = 0; e < kHeld; ++e) {
       const int k = threadIdx.x % kWave + e * kWave;
@@ -290,7 +303,7 @@ struct Entries {
     for (int e = 0; e < kHeld; ++e) {
       if (id[e] >= C) id[e] = -1;
       x[e] = id[e] >= 0 ? row.at(id[e]) : 0.0f;
-      held_v[e] /= tau;
+      held_v[e] *= inv_tau;
     }
   }
   // f(id, v / tau, student's logit) of the lane's entries
@@ -301,7 +314,7 @@ struct Entries {
       if (id[e] >= 0) f(id[e], held_v[e], x[e]);
     for (int k = threadIdx.x % kWave + kHeld * kWave; k < K; k += kWave) {
       const int j = ids[k];
-      if (j >= 0 && j < C) f(j, vals[k] / tau, row.at(j));
+      if (j >= 0 && j < C) f(j, vals[k] * inv_tau, row.at(j));
     }
   }
 };
@@ -350,7 +363,7 @@ __device__ __forceinline__ RowSums finish_row(const Entries<T>& entries, const T
   float loss = 0.0f;
   entries.each([&](int, float v, float x) {
     const float lp = v - t.shift, p = expf(lp);
-    if (!(p <= 0.0f)) loss += p * (lp - (x / entries.tau - s.lse));
+    if (!(p <= 0.0f)) loss += p * (lp - (x * entries.inv_tau - s.lse));
   });
   s.loss += wave_reduce(loss, Plus());
   return s;

@@ -507,9 +507,11 @@ typedef enum { SNN_F32 = 0, SNN_BF16 = 1, SNN_F16 = 2 } snn_dtype;
  *   lse      float32 [R] (written unless NULL): log sum_j exp(z_j / tau) over all C classes, so that a listed class has
  *            the probability exp(val / tau - lse); -inf for a row of -inf, +inf for one that holds +inf
  * NaN counts as -inf, and -inf is not listed: a row with fewer than K others ends in ids -1, vals -inf.
+ * Workspace: needed for few long rows alone; the query gives 0 for others, and workspace may then be NULL.
  */
+size_t snn_readout_top_workspace(int64_t R, int C, int dtype, int K);
 snn_status snn_readout_top(const void* logits, int dtype, int64_t R, int C, int64_t ld, int K, float tau, int32_t* ids,
-                           float* vals, float* lse, void* stream);
+                           float* vals, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Distillation loss of a student's rows against a teacher's records at temperature tau, and its gradient.

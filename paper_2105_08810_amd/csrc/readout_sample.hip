@@ -360,29 +360,6 @@ struct Pairs {
 // Beyond this many elements two sorts take less than all comparisons (1000 elements in 1024 threads: 50 us of comparisons).
 constexpr int kSorted = 256;
 
-// v[0..n) in ascending order; v has room for the next power of two.
-template <int NT>
-__device__ __forceinline__ void block_sort(uint64_t* v, int n) {
-  int size = 2;
-  while (size < n) size <<= 1;
-  for (int e = n + (int)threadIdx.x; e < size; e += NT) v[e] = UINT64_MAX;
-  __syncthreads();
-#pragma unroll 1
-  for (int run = 2; run <= size; run <<= 1)
-#pragma unroll 1
-    for (int step = run >> 1; step > 0; step >>= 1) {
-      for (int i = threadIdx.x; i < size / 2; i += NT) {
-        const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
-        const uint64_t x = v[lo], y = v[hi];
-        if ((x > y) == ((lo & run) == 0)) {
-          v[lo] = y;
-          v[hi] = x;
-        }
-      }
-      __syncthreads();
-    }
-}
-
 // before[e] = sum of value(o) over o < e, for e < n.
 template <int NT, class F>
 __device__ __forceinline__ void block_before(int n, F value, uint64_t* before, uint64_t* red) {

@@ -42,6 +42,8 @@ struct Top {
   int32_t* ids;
   float* vals;
   float* lse;
+  int parts;   // of a row, each with a record of its own
+  int part_C;  // classes of a part
 };
 
 __device__ __forceinline__ uint64_t entry(uint32_t key, int j) { return (uint64_t)~key << 32 | (uint32_t)j; }
@@ -303,10 +305,64 @@ template <class T, int NT, int NV>
 __global__ __launch_bounds__(NT) void top_tile(Top a) {
   __shared__ TopLds<NT> s;
   const int64_t r = blockIdx.x;
-  const Row<T> row(a.logits, r, a.ld, a.C);
+  const int from = (int)(r % a.parts) * a.part_C;
+  const Row<T> row(static_cast<const T*>(a.logits) + r / a.parts * a.ld + from, min(a.part_C, a.C - from));
   if (!top_in_registers<T, NT, NV>(row, a, r, s)) {
     __syncthreads();
     top_general<T, NT>(row, a, r, s);
+  }
+}
+
+// ------------------------------------------------------------------ few long rows, several blocks each
+
+constexpr int kPartThreads = 512;
+constexpr int kPartVectors = 4 * kPartThreads;
+constexpr int kMerged = 1024;  // listed classes of a row's parts
+
+// Parts that a row is shared among: where it is longer than two of them and the rows alone leave most compute units
+// idle (24 rows of 131072 float16, K 50: 30 us in a block each, TODO so).
+inline int top_parts(int64_t R, int C, int dtype, int K) {
+  const int per = 16 / rows::type_size(dtype);
+  const int Q = (C + 2 * per - 2) / per;  // as of a row that is not aligned
+  if (Q <= 2 * kPartVectors || R > cu_count() / 2 || K > kPartThreads / kWave * kNthMost) return 1;
+  const int parts = (Q + kPartVectors - 2) / (kPartVectors - 1);  // the cuts may add a vector to each
+  return parts * K <= kMerged && parts <= kWave ? parts : 1;
+}
+inline size_t top_carve(void* ws, int64_t R, int parts, int K, Top* a) {
+  Carve c(ws);
+  int32_t* ids = c.take<int32_t>((size_t)R * parts * K);
+  float* vals = c.take<float>((size_t)R * parts * K);
+  float* lse = c.take<float>((size_t)R * parts);
+  if (a) {
+    a->ids = ids;
+    a->vals = vals;
+    a->lse = lse;
+  }
+  return c.off;
+}
+
+// A row's record from its parts': `part` is the launch that wrote those, `a` the call's own.
+__global__ __launch_bounds__(kMerged) void top_merge(Top part, Top a) {
+  __shared__ uint64_t list[kMerged];
+  const int64_t r = blockIdx.x;
+  const int tid = threadIdx.x, n = part.parts * a.K;
+  if (tid < n) {
+    const int64_t e = r * n + tid;
+    const int id = part.ids[e];
+    list[tid] = id < 0 ? UINT64_MAX : entry(key_of(part.vals[e]), id + tid / a.K * part.part_C);
+  }
+  if (a.lse && tid < kWave) {
+    const float x = tid < part.parts ? part.lse[r * part.parts + tid] : -INFINITY;
+    const float m = wave_reduce(x, Larger()), safe = isinf(m) ? 0.0f : m;
+    const float sum = wave_reduce(expf(x - safe), Plus());
+    if (tid == 0) a.lse[r] = isinf(m) ? m : m + logf(sum);
+  }
+  __syncthreads();
+  block_sort<kMerged>(list, n);
+  if (tid < a.K) {
+    const uint64_t e = list[tid];
+    a.ids[r * a.K + tid] = e == UINT64_MAX ? -1 : (int)(uint32_t)e;
+    a.vals[r * a.K + tid] = e == UINT64_MAX ? -INFINITY : of_key(~(uint32_t)(e >> 32));
   }
 }
 
@@ -315,13 +371,23 @@ __global__ __launch_bounds__(NT) void top_tile(Top a) {
 
 using namespace snn;
 
+extern "C" size_t snn_readout_top_workspace(int64_t R, int C, int dtype, int K) {
+  if (R <= 0 || R > INT32_MAX || bad_dim(C) || C > rows::kMaxClasses || rows::type_size(dtype) == 0 || K <= 0 || K > C)
+    return 0;
+  const int parts = top_parts(R, C, dtype, K);
+  return parts > 1 ? top_carve(nullptr, R, parts, K, nullptr) : 0;
+}
+
 extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, int C, int64_t ld, int K, float tau,
-                                      int32_t* ids, float* vals, float* lse, void* stream) {
+                                      int32_t* ids, float* vals, float* lse, void* workspace, size_t workspace_bytes,
+                                      void* stream) {
   const snn_status ok = rows::check_rows(logits, dtype, R, C, ld);
   if (ok != SNN_OK) return ok;
   if (!ids || !vals || K <= 0 || K > C || !(tau > 0.0f) || isinf(tau)) return SNN_ERR_INVALID_ARG;
   if (K > rows::kMaxListed) return SNN_ERR_UNSUPPORTED;
-  const Top a{logits, R, C, ld, K, 1.0f / tau, ids, vals, lse};
+  const size_t need = snn_readout_top_workspace(R, C, dtype, K);
+  if (need && (!workspace || workspace_bytes < need)) return SNN_ERR_INVALID_ARG;
+  const Top a{logits, R, C, ld, K, 1.0f / tau, ids, vals, lse, 1, C};
   hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)R);
   return rows::for_type(dtype, [&](auto type) {
@@ -330,7 +396,15 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
     if (C <= rows::kShortRow)
       hipLaunchKernelGGL((top_short<T>), dim3((unsigned)((R + rows::kShortRows - 1) / rows::kShortRows)), dim3(256), 0,
                          s, a);
-    else if (Q <= 4 * 64 && K <= kNthMost)
+    else if (const int parts = top_parts(R, C, dtype, K); parts > 1) {
+      constexpr int kVec = rows::Row<T>::kVec;
+      Top part = a;
+      part.parts = parts;
+      part.part_C = ((C + parts - 1) / parts + kVec - 1) / kVec * kVec;
+      top_carve(workspace, R, parts, K, &part);
+      hipLaunchKernelGGL((top_tile<T, kPartThreads, 4>), dim3((unsigned)(R * parts)), dim3(kPartThreads), 0, s, part);
+      hipLaunchKernelGGL(top_merge, grid, dim3(kMerged), 0, s, part, a);
+    } else if (Q <= 4 * 64 && K <= kNthMost)
       hipLaunchKernelGGL((top_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
     else if (Q <= 4 * 256 && K <= 4 * kNthMost)
       hipLaunchKernelGGL((top_tile<T, 256, 4>), grid, dim3(256), 0, s, a);

@@ -388,6 +388,29 @@ __device__ __forceinline__ uint64_t block_exclusive(uint64_t v, uint64_t* red) {
   return wave_sum64(l < w ? red[l] : 0) + upto - v;
 }
 
+// v[0..n) in ascending order; v has room for the next power of two.
+template <int NT>
+__device__ __forceinline__ void block_sort(uint64_t* v, int n) {
+  int size = 2;
+  while (size < n) size <<= 1;
+  for (int e = n + (int)threadIdx.x; e < size; e += NT) v[e] = UINT64_MAX;
+  __syncthreads();
+#pragma unroll 1
+  for (int run = 2; run <= size; run <<= 1)
+#pragma unroll 1
+    for (int step = run >> 1; step > 0; step >>= 1) {
+      for (int i = threadIdx.x; i < size / 2; i += NT) {
+        const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
+        const uint64_t x = v[lo], y = v[hi];
+        if ((x > y) == ((lo & run) == 0)) {
+          v[lo] = y;
+          v[hi] = x;
+        }
+      }
+      __syncthreads();
+    }
+}
+
 // ------------------------------------------------------------------ selection
 //
 // The order of a row's classes is by value, largest first, equal values by class. A cut is the first place of the

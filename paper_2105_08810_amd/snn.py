@@ -60,7 +60,8 @@ _SIGNATURES = {
     "snn_dense_backward_ref": (_I, [_P, _P, _P, _P, _I, _I, _I, _I, _F, _F, _F, _F, _P, _P, _P, _SZ, _P]),
     "snn_readout_ce_workspace": (_SZ, [_I, _I, _I, _I]),
     "snn_readout_ce": (_I, [_P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _SZ, _P]),
-    "snn_readout_top": (_I, [_P, _I, _I64, _I, _I64, _I, _F, _P, _P, _P, _P]),
+    "snn_readout_top_workspace": (_SZ, [_I64, _I, _I, _I]),
+    "snn_readout_top": (_I, [_P, _I, _I64, _I, _I64, _I, _F, _P, _P, _P, _P, _SZ, _P]),
     "snn_readout_distill_workspace": (_SZ, [_I64, _I, _I]),
     "snn_readout_distill": (_I, [_P, _I, _I64, _I, _I64, _P, _P, _P, _I, _F, _P, _P, _P, _P, _I64, _I, _P, _SZ, _P]),
     "snn_readout_sample_workspace": (_SZ, [_I64, _I, _I]),
@@ -386,11 +387,16 @@ def _of_rows(t: Optional[torch.Tensor], n: int, dtype, name):
     return _ptr(t, dtype, name)
 
 
-def snn_readout_top(logits, K, tau, ids, vals, lse=None, stream=None):
+def snn_readout_top_workspace(R, C, dtype, K) -> int:
+    return int(lib().snn_readout_top_workspace(R, C, _DTYPES[dtype], int(K)))
+
+
+def snn_readout_top(logits, K, tau, ids, vals, lse=None, ws=None, stream=None):
     p, code, R, C, ld = _rows(logits)
     _check("snn_readout_top", lib().snn_readout_top(
         p, code, R, C, ld, int(K), float(tau), _of_rows(ids, R * K, torch.int32, "ids"),
-        _of_rows(vals, R * K, torch.float32, "vals"), _of_rows(lse, R, torch.float32, "lse"), _stream(stream)))
+        _of_rows(vals, R * K, torch.float32, "vals"), _of_rows(lse, R, torch.float32, "lse"),
+        _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
 
 
 def snn_readout_distill_workspace(R, C, dtype) -> int:
@@ -650,15 +656,18 @@ def readout_ce(V_out: torch.Tensor, labels: torch.Tensor, mode: int, dense=False
 # These three are called once a step or a token on little data, where the host's work is most of the time: they check
 # what they are given and not again what they have made themselves.
 
-def readout_top(logits: torch.Tensor, K: int, tau=1.0, want_lse=True, stream=None):
+def readout_top(logits: torch.Tensor, K: int, tau=1.0, want_lse=True, ws=None, stream=None):
     """A teacher's record of rows of logits [..., C]: (ids [..., K] int32, vals [..., K], lse [...] or None)."""
     p, code, R, C, ld = _rows(logits)
     shape, dev = logits.shape[:-1], logits.device
     ids = torch.empty((*shape, K), dtype=torch.int32, device=dev)
     vals = torch.empty((*shape, K), dtype=torch.float32, device=dev)
     lse = torch.empty(shape, dtype=torch.float32, device=dev) if want_lse else None
-    _check("snn_readout_top", lib().snn_readout_top(p, code, R, C, ld, K, tau, ids.data_ptr(), vals.data_ptr(),
-                                                    lse.data_ptr() if want_lse else None, _stream(stream)))
+    if ws is None and (need := lib().snn_readout_top_workspace(R, C, code, K)):
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    _check("snn_readout_top", lib().snn_readout_top(
+        p, code, R, C, ld, K, tau, ids.data_ptr(), vals.data_ptr(), lse.data_ptr() if want_lse else None,
+        _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
     return ids, vals, lse
 
 

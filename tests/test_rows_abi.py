@@ -43,9 +43,9 @@ def _call(fn, order, base, kw):
 
 
 def _top(lib, **kw):
-    return _call(lib.snn_readout_top, "logits dtype R C ld K tau ids vals lse stream".split(),
-                 dict(logits=FAKE, dtype=0, R=10, C=100, ld=100, K=5, tau=1.0, ids=FAKE, vals=FAKE, lse=FAKE,
-                      stream=None), kw)
+    return _call(lib.snn_readout_top, "logits dtype R C ld K tau ids vals lse ws ws_bytes stream".split(),
+                 dict(logits=FAKE, dtype=0, R=10, C=100, ld=100, K=5, tau=1.0, ids=FAKE, vals=FAKE, lse=FAKE, ws=None,
+                      ws_bytes=0, stream=None), kw)
 
 
 def _distill(lib, **kw):
@@ -106,6 +106,20 @@ def test_distill_workspace(lib):
     for bad in ((0, 100, 0), (-1, 100, 0), (10, 0, 0), (10, 100, 3), (1 << 31, 100, 0), (10, (1 << 20) + 1, 0)):
         assert size(*bad) == 0
     assert size(777, 333, 1) == size(777, 333, 1)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(ws=FAKE, ws_bytes=100)])
+def test_top_needs_its_workspace(lib, kw):
+    assert _top(lib, R=1, C=131072, ld=131072, **kw) == snn.SNN_ERR_INVALID_ARG
+
+
+def test_top_workspace(lib):
+    size = lib.snn_readout_top_workspace
+    assert size(1, 131072, 0, 5) > 0 and size(2, 131072, 1, 5) > size(1, 131072, 1, 5) > 0  # few long rows
+    assert size(1, 1000, 0, 5) == 0 and size(100000, 131072, 0, 5) == 0 and size(1, 131072, 0, 1000) == 0
+    for bad in ((0, 131072, 0, 5), (-1, 131072, 0, 5), (1, 0, 0, 5), (1, 131072, 3, 5), (1 << 31, 131072, 0, 5),
+                (1, (1 << 20) + 1, 0, 5), (1, 131072, 0, 0), (1, 100, 0, 101)):
+        assert size(*bad) == 0
 
 
 def test_sample_workspace(lib):

@@ -520,7 +520,7 @@ __global__ __launch_bounds__(NT, 4) void distill_tile(Distill a) {
       for (int k = 0; k < kVec; ++k) v[k] = from_float<T>(x[k]);
       uint4 u;
       __builtin_memcpy(&u, v, 16);
-      if (q >= from && q < to) *reinterpret_cast<uint4*>(const_cast<T*>(out.base) + (size_t)q * kVec) = u;
+      if (q >= from && q < to) store_past(const_cast<T*>(out.base) + (size_t)q * kVec, u);
     }
   }
   if (alike) {  // the ends of the row

@@ -320,7 +320,7 @@ constexpr int kPartVectors = 4 * kPartThreads;
 constexpr int kMerged = 1024;  // listed classes of a row's parts
 
 // Parts that a row is shared among: where it is longer than two of them and the rows alone leave most compute units
-// idle (24 rows of 131072 float16, K 50: 30 us in a block each, TODO so).
+// idle (24 rows of 131072 float16, K 50: 30 us in a block each, 23 so).
 inline int top_parts(int64_t R, int C, int dtype, int K) {
   const int per = 16 / rows::type_size(dtype);
   const int Q = (C + 2 * per - 2) / per;  // as of a row that is not aligned

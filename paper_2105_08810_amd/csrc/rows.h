@@ -96,6 +96,12 @@ __device__ __forceinline__ uint4 load_raw(const Row<T>& row, int q) {
   return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
 }
 
+// A vector that is not read again soon: past the caches, which keep what is (the rows of a second pass).
+typedef uint32_t Vector4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void store_past(void* p, const uint4& u) {
+  __builtin_nontemporal_store(Vector4{u.x, u.y, u.z, u.w}, static_cast<Vector4*>(p));
+}
+
 // Values of vector q back to a row, those inside it.
 template <class T>
 __device__ __forceinline__ void store_vec(const Row<T>& row, int q, const float (&x)[16 / sizeof(T)]) {
@@ -107,7 +113,7 @@ __device__ __forceinline__ void store_vec(const Row<T>& row, int q, const float 
   uint4 u;
   __builtin_memcpy(&u, v, 16);
   if (row.whole(q)) {
-    *reinterpret_cast<uint4*>(p) = u;
+    store_past(p, u);
   } else {
     constexpr int kBits = 8 * (int)sizeof(T);
     uint64_t lo = (uint64_t)u.y << 32 | u.x, hi = (uint64_t)u.w << 32 | u.z;

@@ -562,8 +562,10 @@ __global__ __launch_bounds__(NT) void distill_rows(Distill a) {
   __syncthreads();
   const float c = kLog2e / a.tau;
   constexpr int kAhead = 4;  // vectors of a thread in flight
-  auto pass = [&](auto f) {
-    for (int q0 = tid; q0 < row.Q; q0 += kAhead * NT) {
+  const int steps = (row.Q + kAhead * NT - 1) / (kAhead * NT);
+  auto pass = [&](bool back, auto f) {
+    for (int step = 0; step < steps; ++step) {
+      const int q0 = (back ? steps - 1 - step : step) * kAhead * NT + tid;
       uint4 raw[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u)
@@ -585,7 +587,7 @@ __global__ __launch_bounds__(NT) void distill_rows(Distill a) {
     }
   };
   Sum2 rest{-INFINITY, 0.0f};
-  pass([&](float (&x)[kVec], int) {
+  pass(false, [&](float (&x)[kVec], int) {
     float m = x[0];
 #pragma unroll
     for (int k = 1; k < kVec; ++k) m = fmaxf(m, x[k]);
@@ -606,7 +608,7 @@ __global__ __launch_bounds__(NT) void distill_rows(Distill a) {
   const Row<T> out(a.grad, r, a.ld_grad, a.C);
   const float scale = w / a.tau;
   const float per = scale * s.factor, safe = or_zero(rest.max);
-  pass([&](float (&x)[kVec], int q) {
+  pass(true, [&](float (&x)[kVec], int q) {  // from the end, which was read last
 #pragma unroll
     for (int k = 0; k < kVec; ++k) x[k] = exp2_fast(fmaf(x[k], c, -safe)) * per;
     put(a, row, out, q, x);

@@ -494,3 +494,56 @@ def test_binding_refuses():
         snn.readout_sample(z, torch.zeros(4, device="cuda"), top_k=torch.zeros(4, device="cuda"))
     with pytest.raises(snn.SnnError):
         snn.readout_sample(torch.zeros((0, 6), device="cuda"), torch.zeros(0, device="cuda"))
+
+
+# ---------------------------------------------------------------- many rows, where other kernels are taken than for few
+
+MANY = [(300, 40, "normal", "f32"), (300, 100, "ties", "bf16"), (261, 128, "masked", "f16"), (300, 129, "normal", "bf16"),
+        (300, 300, "lowest", "f32"), (270, 1000, "ties", "f16"), (270, 1000, "nan", "f32"), (257, 2100, "normal", "f32"),
+        (257, 2100, "equal", "bf16"), (260, 5000, "peak", "f32"), (260, 9001, "normal", "bf16"), (258, 20000, "ties", "f32")]
+
+
+@pytest.mark.parametrize("R,C,kind,dtype", MANY)
+def test_many_rows_top(R, C, kind, dtype):
+    view = _rows(_logits(np.random.default_rng(R + C), R, C, kind), dtype, C + C % 2, 0)
+    for K in (3, 20):
+        _check_top(_values(view), view, K, 2.0)
+
+
+@pytest.mark.parametrize("R,C,kind,dtype", MANY)
+def test_many_rows_sample(R, C, kind, dtype):
+    rng = np.random.default_rng(R * C)
+    view = _rows(_logits(rng, R, C, kind), dtype, C + C % 2, 0)
+    some = slice(0, R) if C <= 300 else slice(0, R, 23)  # the oracle is a loop over classes
+    settings = [None] * 4, _settings(rng, R, C), [_settings(rng, R, C)[0], None, _settings(rng, R, C)[2], None]
+    u = rng.random(R).astype(np.float32)
+    dev = lambda a: None if a is None else torch.from_numpy(a).cuda()  # noqa: E731
+    for t, k, p, m in settings:
+        all_rows = [x.cpu().numpy() for x in snn.readout_sample(view, dev(u), dev(t), dev(k), dev(p), dev(m))]
+        z = _values(view)[some]
+        tt = (np.ones(R, np.float32) if t is None else t)[some]
+        e = _e(z, tt)
+        pick = lambda a, r, none: none if a is None else a[some][r]  # noqa: E731
+        for r in range(len(z)):
+            j, n, total, _ = rows.sample_row(z[r], e[r], u[some][r], int(pick(k, r, 0)), pick(p, r, 1.0),
+                                             pick(m, r, 0.0), not tt[r] > 0)
+            assert (all_rows[0][some][r], all_rows[2][some][r]) == (j, n), r
+            if j >= 0:
+                want = math.log(float(e[r, j]) * rows.UNIT / total)
+                assert abs(all_rows[1][some][r] - want) <= U * 8 * (24 + abs(want))
+
+
+@pytest.mark.parametrize("R,C,dtype", [(513, 130, "f32"), (513, 5000, "f32"), (513, 18001, "f32"), (512, 9000, "bf16"),
+                                       (512, 17001, "bf16"), (513, 1500, "f16"), (20, 40000, "f32"), (3, 70001, "f16")])
+def test_many_rows_distill(R, C, dtype):
+    rng = np.random.default_rng(C)
+    view = _rows(_logits(rng, R, C, "normal"), dtype)
+    weight = rng.random(R).astype(np.float32)
+    weight[::5] = 0.0
+    rec = _record(rng, _values(view), 9, 1.5, "")
+    _check_distill(view, *rec, 1.5, weight, dtype)
+    full = torch.empty((R, C + 3), dtype=DTYPES[dtype], device="cuda")  # rows that begin otherwise than the logits'
+    dev = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    a = snn.readout_distill(view, *map(dev, rec), 1.5, dev(weight))
+    b = snn.readout_distill(view, *map(dev, rec), 1.5, dev(weight), grad=full[:, :C])
+    assert torch.equal(a[0], b[0]) and torch.equal(a[2], b[2])

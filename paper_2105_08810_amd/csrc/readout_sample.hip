@@ -81,6 +81,16 @@ struct RowSettings {
     min_p = set.min_p ? set.min_p[r] : 0.0f;
     min_p = min_p > 0.0f ? fminf(min_p, 1.0f) : 0.0f;
   }
+  // For a kernel whose waves have one row each.
+  __device__ __forceinline__ RowSettings of_wave() const {
+    RowSettings s = *this;
+    s.u = same_in_wave(u);
+    s.temperature = same_in_wave(temperature);
+    s.top_p = same_in_wave(top_p);
+    s.min_p = same_in_wave(min_p);
+    s.k = same_in_wave(k);
+    return s;
+  }
   // The weight that a prefix of the order has to reach, of `sum`.
   __device__ __forceinline__ uint64_t limit(uint64_t sum) const {
     if (top_p >= 1.0f) return sum;
@@ -296,7 +306,7 @@ template <class T, int NT>
 __global__ __launch_bounds__(NT) void sample_rows(Sample a) {
   __shared__ GeneralLds<NT> s;
   const int64_t r = blockIdx.x;
-  sample_general<T, NT>(a, r, Row<T>(a.logits, r, a.ld, a.C), RowSettings(a.set, r, a.C), s);
+  sample_general<T, NT>(a, r, Row<T>(a.logits, r, a.ld, a.C), RowSettings(a.set, r, a.C).of_wave(), s);
 }
 
 // ------------------------------------------------------------------ rows in registers
@@ -307,11 +317,11 @@ __device__ __forceinline__ int bin_of(float t) { return min(kBins - 1, (int)(t *
 
 // Lanes of each wave that the bound is taken from, at most: with n of 64 lanes -64 log(1 - n/64) of its values reach it.
 template <int NT>
-constexpr int kNthMost = NT == kWave ? 56 : 24;
+constexpr int kNthMost = NT == kWave ? 56 : NT == 256 ? 50 : 32;
 
 template <int NT, int NV>
 struct TileLds {
-  static constexpr int kList = NT == kWave ? 256 : NT == 256 ? 512 : 1024;
+  static constexpr int kList = NT == kWave ? 256 : 1024;
   static constexpr int kChunks = NV * NT / kWave;
   union {
     GeneralLds<NT> general;
@@ -470,8 +480,10 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
   Tile<T, NT, NV> tile;
   tile.load(row);
   // the largest value and a bound that at least `want` values reach
-  const bool few = set.k <= kNthMost<NT> * kWaves;  // what top-k keeps can be collected
-  const int nth = few ? (set.k + kWaves - 1) / kWaves : max(4, 16 / kWaves);
+  const int full = max(1, min(kWaves, row.Q / kWave));  // waves without idle lanes give the bound
+  const bool all = set.k > kNthMost<NT> * full && set.k < a.C && a.C <= kList;
+  const bool few = set.k <= kNthMost<NT> * full || all;  // what top-k keeps can be collected
+  const int nth = few && !all ? (set.k + full - 1) / full : max(4, 16 / full);
   float most = -INFINITY;
   bool nan = false;
   tile.each_unrolled(row, [&](const float (&x)[kVec], int, int) {
@@ -483,7 +495,7 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
   });
   const uint32_t own = nan ? 0u : key_of(most);  // 0 is no value's key
   uint32_t high = wave_max_u32(own);
-  uint32_t bound = wave_nth(own, nth);
+  uint32_t bound = wave < full ? wave_nth(own, nth) : UINT32_MAX;
   bool odd = __ballot(nan) != 0;
   if (tid == 0) s.n_list = 0;
   if (NT > kWave) {
@@ -503,7 +515,8 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
     high = key_of(m);
   }
   __syncthreads();
-  const float m = of_key(high);
+  odd = same_in_wave(odd);
+  const float m = same_in_wave(of_key(high));
   const Weigh weigh{m, 1.0f / set.temperature};
   if (odd || isinf(m) || (!few && set.k < a.C) || (isinf(weigh.inv) && set.k != 1)) return false;
   if (set.k == 1) {  // the first of the largest
@@ -517,7 +530,7 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
     if (tid == 0) a.answer(r, at, 0.0f, 1);
     return true;
   }
-  const float least = of_key(bound);
+  const float least = all ? -INFINITY : same_in_wave(of_key(bound));
   int last = a.C;  // class of the last kept element at the cut
   // One loop over the row for all passes: the exponential's code is there once.
   //   kCollect  the elements that reach the bound (all that top-k keeps)
@@ -588,7 +601,7 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
     });
     if (mode == kShare) break;
     __syncthreads();
-    n = (int)s.n_list;
+    n = same_in_wave((int)s.n_list);
     if (mode == kCollect || mode == kPart) {
       if (n > kList) return false;
     }
@@ -629,7 +642,7 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
         b += w;
       }
       __syncthreads();
-      part = (int)s.part;
+      part = same_in_wave((int)s.part);
       above = s.above;
       mode = kPart;
     } else {
@@ -642,8 +655,8 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
         }
       }
       __syncthreads();
-      cut = of_key(s.ured[0]);
-      last = s.ired[0];
+      cut = same_in_wave(of_key(s.ured[0]));
+      last = same_in_wave(s.ired[0]);
       mode = kShare;
     }
   }
@@ -685,7 +698,7 @@ __global__ __launch_bounds__(NT) void sample_tile(Sample a) {
   __shared__ TileLds<NT, NV> s;
   const int64_t r = blockIdx.x;
   const Row<T> row(a.logits, r, a.ld, a.C);
-  const RowSettings set(a.set, r, a.C);
+  const RowSettings set = RowSettings(a.set, r, a.C).of_wave();
   if (!sample_in_registers<T, NT, NV>(a, r, row, set, s)) sample_general<T, NT>(a, r, row, set, s.general);
 }
 
@@ -747,14 +760,14 @@ struct Split {
 };
 
 // Parts that a row is shared among: from the length on where several launches take less than one block (1 row of 32003
-// float32: 19 us in one block with top-k 50, 22 in parts; of 128011 bf16 29 and 23), and where the rows alone leave most
-// compute units idle.
+// float32: 19 us in one block with top-k 50, 22 in parts; of 128011 bf16 29 and 23), where the rows alone leave most compute
+// units idle or do not fit a block's registers (10 KB of workspace a part).
 inline int split_parts(int64_t R, int C, int dtype) {
   const int per = 16 / rows::type_size(dtype);
   const int Q = (C + 2 * per - 2) / per;  // as of a row that is not aligned
-  if (Q <= 8192 || R > cu_count() / 2) return 1;
   const int parts = (Q + kPartVectors - 1) / kPartVectors;
-  return parts <= kMostParts ? parts : 1;
+  if (Q <= 8192 || parts > kMostParts) return 1;
+  return R <= (Q <= 16 * 1024 ? cu_count() / 2 : (1 << 15) / parts) ? parts : 1;
 }
 
 // What the launches after the first know of a row.
@@ -781,7 +794,7 @@ __global__ __launch_bounds__(kPartThreads) void split_max(Sample a, Split s) {
   const int64_t r = blockIdx.x / s.parts;
   const int p = blockIdx.x % s.parts, tid = threadIdx.x;
   const Row<T> row(a.logits, r, a.ld, a.C);
-  const RowSettings set(a.set, r, a.C);
+  const RowSettings set = RowSettings(a.set, r, a.C).of_wave();
   const int q0 = p * s.each;
   uint4 u[4];
   load_vectors<T, kPartThreads>(row, u, q0, min(row.Q, q0 + s.each));
@@ -848,13 +861,13 @@ __global__ __launch_bounds__(kPartThreads) void split_sum(Sample a, Split s) {
   __shared__ uint32_t pool[kPool], bound;
   const int64_t r = blockIdx.x / s.parts;
   const int p = blockIdx.x % s.parts, tid = threadIdx.x;
-  const RowSettings set(a.set, r, a.C);
+  const RowSettings set = RowSettings(a.set, r, a.C).of_wave();
   const SplitRow known(a, s, r, set);
   if (set.k == 1 || known.general || !(known.listed || known.cut)) return;
   const Row<T> row(a.logits, r, a.ld, a.C);
   const int q0 = p * s.each;
-  uint4 u[4];
-  load_vectors<T, kPartThreads>(row, u, q0, min(row.Q, q0 + s.each));
+  Tile<T, kPartThreads, 4> tile;
+  tile.load(row, q0, min(row.Q, q0 + s.each));
   if (known.cut)
     for (int b = tid; b < kBins; b += kPartThreads) mass[b] = 0;
   if (tid == 0) list.n = 0;
@@ -877,7 +890,7 @@ __global__ __launch_bounds__(kPartThreads) void split_sum(Sample a, Split s) {
 #pragma unroll 1
   for (int i = 0; i < 4; ++i) {
     float x[kVec];
-    unpack<T>(i < 2 ? (i == 0 ? u[0] : u[1]) : (i == 2 ? u[2] : u[3]), x);
+    unpack<T>(tile.get(i), x);
     const int j = row.first(q0 + i * kPartThreads + tid);
     if (known.listed) {
 #pragma unroll
@@ -903,7 +916,7 @@ template <class T>
 __global__ __launch_bounds__(kBins) void split_cut(Sample a, Split s) {
   __shared__ uint64_t red[kBins / kWave];
   const int64_t r = blockIdx.x;
-  const RowSettings set(a.set, r, a.C);
+  const RowSettings set = RowSettings(a.set, r, a.C).of_wave();
   const SplitRow known(a, s, r, set);
   if (set.k == 1 || known.general || !known.cut) return;
   uint64_t w = 0;
@@ -921,13 +934,13 @@ __global__ __launch_bounds__(kPartThreads) void split_share(Sample a, Split s) {
   __shared__ PartList list;
   const int64_t r = blockIdx.x / s.parts;
   const int p = blockIdx.x % s.parts, tid = threadIdx.x;
-  const RowSettings set(a.set, r, a.C);
+  const RowSettings set = RowSettings(a.set, r, a.C).of_wave();
   const SplitRow known(a, s, r, set);
   if (set.k == 1 || known.general || known.listed) return;
   const Row<T> row(a.logits, r, a.ld, a.C);
   const int q0 = p * s.each;
-  uint4 u[4];
-  load_vectors<T, kPartThreads>(row, u, q0, min(row.Q, q0 + s.each));
+  Tile<T, kPartThreads, 4> tile;
+  tile.load(row, q0, min(row.Q, q0 + s.each));
   const int bin = known.cut ? s.cut[r].bin : kBins;
   if (tid == 0) list.n = 0;
   __syncthreads();
@@ -936,7 +949,7 @@ __global__ __launch_bounds__(kPartThreads) void split_share(Sample a, Split s) {
 #pragma unroll 1
   for (int i = 0; i < 4; ++i) {
     float x[kVec];
-    unpack<T>(i < 2 ? (i == 0 ? u[0] : u[1]) : (i == 2 ? u[2] : u[3]), x);
+    unpack<T>(tile.get(i), x);
     const int j = row.first(q0 + i * kPartThreads + tid);
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
@@ -968,7 +981,7 @@ __global__ __launch_bounds__(kDrawThreads) void split_draw(Sample a, Split s) {
   const int64_t r = blockIdx.x;
   const int tid = threadIdx.x, lane = tid % kWave;
   const Row<T> row(a.logits, r, a.ld, a.C);
-  const RowSettings set(a.set, r, a.C);
+  const RowSettings set = RowSettings(a.set, r, a.C).of_wave();
   const SplitRow known(a, s, r, set);
   // where each part's collected elements go in the row's list
   const uint32_t own = lane < s.parts ? s.n_list[r * s.parts + lane] : 0;
@@ -1060,7 +1073,9 @@ extern "C" snn_status snn_readout_sample(const void* logits, int dtype, int64_t 
     if (C <= rows::kShortRow && (C <= 32 || R > cu_count()))
       hipLaunchKernelGGL((sample_short<T>), dim3((unsigned)((R + rows::kShortRows - 1) / rows::kShortRows)), dim3(256),
                          0, s, a);
-    else if (Q <= 4 * 64 && R > cu_count())  // fewer rows: more threads on each (1 row of 1000, top-k 50: 39 and 14 us)
+    // fewer rows: more threads on each (1 row of 1000, top-k 50: 39 and 14 us); with a top-k, which may be long, a list
+    // for all of up to 1024 classes (23265 rows of 590 bf16, requests: 606 us without)
+    else if (Q <= 4 * 64 && R > cu_count() && !top_k)
       hipLaunchKernelGGL((sample_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
     else if (Q <= 4 * 256)
       hipLaunchKernelGGL((sample_tile<T, 256, 4>), grid, dim3(256), 0, s, a);

@@ -16,7 +16,19 @@ namespace {
 
 using namespace rows;
 
-constexpr int kNthMost = 16;
+// Lanes of each wave that the bound is taken from, at most: with n of 64 lanes -64 log(1 - n/64) of its values reach it,
+// somewhat more where the smallest of several waves counts.
+template <int NT>
+constexpr int kNthMost = NT == kWave ? 56 : 32;
+// Waves of a block whose lanes all hold a vector of a row with at least Q of them.
+template <int NT>
+__host__ __device__ constexpr int full_waves(int Q) {
+  return Q / kWave < 1 ? 1 : Q / kWave < NT / kWave ? Q / kWave : NT / kWave;
+}
+template <int NT>
+__host__ __device__ constexpr int nth_of(int K, int Q) {
+  return (K + full_waves<NT>(Q) - 1) / full_waves<NT>(Q);
+}
 constexpr float kLog2e = 1.44269504088896340736f;
 
 template <int NT>
@@ -48,17 +60,23 @@ struct Top {
 
 __device__ __forceinline__ uint64_t entry(uint32_t key, int j) { return (uint64_t)~key << 32 | (uint32_t)j; }
 
+// Beyond this many entries a sort takes less than comparing each with all others.
+template <int NT>
+constexpr int kSorted = NT == kWave ? 64 : 256;
+
 // Classes and logits of the n collected entries by their place among them; the record's end where there are fewer.
 template <class T, int NT>
-__device__ __forceinline__ void write_record(const Row<T>& row, const Top& a, int64_t r, const uint64_t* list, int n) {
-  for (int e = threadIdx.x; e < max(n, a.K); e += NT) {
+__device__ __forceinline__ void write_record(const Row<T>& row, const Top& a, int64_t r, uint64_t* list, int n) {
+  const bool sorted = n > kSorted<NT>;
+  if (sorted) block_sort<NT>(list, n);
+  for (int e = threadIdx.x; e < (sorted ? a.K : max(n, a.K)); e += NT) {
     int place = e, id = -1;
     float v = -INFINITY;
     if (e < n) {
       const uint64_t mine = list[e];
-      place = 0;
+      place = sorted ? e : 0;
 #pragma unroll 4
-      for (int o = 0; o < n; ++o) place += list[o] < mine;
+      for (int o = 0; o < (sorted ? 0 : n); ++o) place += list[o] < mine;
       id = (int)(uint32_t)mine;
       if (place < a.K) v = row.at(id);
     }
@@ -237,7 +255,9 @@ __device__ __forceinline__ bool top_in_registers(const Row<T>& row, const Top& a
   });
   const uint32_t key = nan ? 0u : key_of(most);  // 0 is no value's key
   uint32_t high = wave_max_u32(key);
-  uint32_t bound = wave_nth(key, (a.K + kWaves - 1) / kWaves);
+  uint32_t bound = UINT32_MAX;  // a wave with idle lanes has no part in it
+  const bool all = nth_of<NT>(a.K, row.Q) > kNthMost<NT>;  // every value is collected
+  if (tid / kWave < full_waves<NT>(row.Q)) bound = wave_nth(key, all ? 1 : nth_of<NT>(a.K, row.Q));
   bool odd = __ballot(nan) != 0;
   if (tid == 0) s.n_taken = 0;
   if (NT > kWave) {
@@ -261,7 +281,7 @@ __device__ __forceinline__ bool top_in_registers(const Row<T>& row, const Top& a
   }
   const float m = of_key(high);
   if (odd || isinf(m)) return false;
-  const float least = of_key(bound);
+  const float least = all ? -INFINITY : of_key(bound);
   const float c = a.inv * kLog2e, mc = m * c;
   float sum = 0.0f;
   uint32_t some = 0;  // the vectors with a value that reaches the bound
@@ -320,11 +340,11 @@ constexpr int kPartVectors = 4 * kPartThreads;
 constexpr int kMerged = 1024;  // listed classes of a row's parts
 
 // Parts that a row is shared among: where it is longer than two of them and the rows alone leave most compute units
-// idle (24 rows of 131072 float16, K 50: 30 us in a block each, 23 so).
+// idle (24 rows of 131072 float16, K 50: 30 us in a block each, 23 so), or it is beyond a block's registers.
 inline int top_parts(int64_t R, int C, int dtype, int K) {
   const int per = 16 / rows::type_size(dtype);
   const int Q = (C + 2 * per - 2) / per;  // as of a row that is not aligned
-  if (Q <= 2 * kPartVectors || R > cu_count() / 2 || K > kPartThreads / kWave * kNthMost) return 1;
+  if (Q <= 2 * kPartVectors || (R > cu_count() / 2 && (Q <= 16 * 1024 || R > (1 << 14))) || K > kPartThreads / kWave * 16) return 1;
   const int parts = (Q + kPartVectors - 2) / (kPartVectors - 1);  // the cuts may add a vector to each
   return parts * K <= kMerged && parts <= kWave ? parts : 1;
 }
@@ -392,7 +412,7 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
   const dim3 grid((unsigned)R);
   return rows::for_type(dtype, [&](auto type) {
     using T = decltype(type);
-    const int Q = rows::most_vectors<T>(logits, C, ld);
+    const int Q = rows::most_vectors<T>(logits, C, ld), least = C / rows::Row<T>::kVec;
     if (C <= rows::kShortRow)
       hipLaunchKernelGGL((top_short<T>), dim3((unsigned)((R + rows::kShortRows - 1) / rows::kShortRows)), dim3(256), 0,
                          s, a);
@@ -404,15 +424,15 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
       top_carve(workspace, R, parts, K, &part);
       hipLaunchKernelGGL((top_tile<T, kPartThreads, 4>), dim3((unsigned)(R * parts)), dim3(kPartThreads), 0, s, part);
       hipLaunchKernelGGL(top_merge, grid, dim3(kMerged), 0, s, part, a);
-    } else if (Q <= 4 * 64 && K <= kNthMost)
+    } else if (Q <= 4 * 64 && nth_of<64>(K, least) <= kNthMost<64>)
       hipLaunchKernelGGL((top_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
-    else if (Q <= 4 * 256 && K <= 4 * kNthMost)
+    else if (Q <= 4 * 256 && (C <= TopLds<256>::kList || nth_of<256>(K, least) <= kNthMost<256>))
       hipLaunchKernelGGL((top_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
-    else if (Q <= 8 * 512 && K <= 8 * kNthMost && R >= cu_count())
+    else if (Q <= 8 * 512 && nth_of<512>(K, least) <= kNthMost<512> && R >= cu_count())
       hipLaunchKernelGGL((top_tile<T, 512, 8>), grid, dim3(512), 0, s, a);
-    else if (Q <= 4 * 1024 && K <= 16 * kNthMost)
+    else if (Q <= 4 * 1024 && nth_of<1024>(K, least) <= kNthMost<1024>)
       hipLaunchKernelGGL((top_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
-    else if (Q <= 16 * 1024 && K <= 16 * kNthMost)
+    else if (Q <= 16 * 1024 && nth_of<1024>(K, least) <= kNthMost<1024>)
       hipLaunchKernelGGL((top_tile<T, 1024, 16>), grid, dim3(1024), 0, s, a);
     else if (Q <= 256)
       hipLaunchKernelGGL((top_rows<T, 64>), grid, dim3(64), 0, s, a);

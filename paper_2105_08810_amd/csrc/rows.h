@@ -202,9 +202,10 @@ struct Tile {
     if (NV > kPart && i >= kPart) return take(w[NV / kPart - 1], i - kPart);
     return take(w[0], i);
   }
-  __device__ __forceinline__ void load(const Row<T>& row) {
+  __device__ __forceinline__ void load(const Row<T>& row) { load(row, 0, row.Q); }
+  __device__ __forceinline__ void load(const Row<T>& row, int q0, int q1) {
     uint4 u[NV];
-    load_vectors<T, NT>(row, u, 0, row.Q);
+    load_vectors<T, NT>(row, u, q0, q1);
 #pragma unroll
     for (int i = 0; i < NV; ++i) put(w[i / kPart], i % kPart, u[i]);
   }
@@ -258,6 +259,12 @@ __device__ __forceinline__ uint32_t wave_nth(uint32_t v, int n) {
     const int first = (int)__builtin_ctzll(__ballot(v == m));
     v = lane_id() == first ? 0 : v;
   }
+}
+
+// A value that all lanes of the wave have, in a scalar register: branches on it are branches.
+__device__ __forceinline__ int same_in_wave(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float same_in_wave(float v) {
+  return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
 }
 
 // NaN as -inf: a class that is never listed or drawn.

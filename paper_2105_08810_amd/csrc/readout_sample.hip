@@ -1081,7 +1081,8 @@ extern "C" snn_status snn_readout_sample(const void* logits, int dtype, int64_t 
       hipLaunchKernelGGL((sample_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
     else if (Q <= 4 * 1024)
       hipLaunchKernelGGL((sample_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
-    else if (const int parts = split_parts(R, C, dtype); parts > 1) {
+    // (the workspace's size is that of rows that are not aligned, which may be a vector longer)
+    else if (const int parts = split_parts(R, C, dtype); parts > 1 && (Q > 16 * 1024 || R <= cu_count() / 2)) {
       Split split;
       Split::carve(workspace, R, parts, &split);
       split.each = (Q + parts - 1) / parts;

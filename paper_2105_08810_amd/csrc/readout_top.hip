@@ -416,7 +416,8 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
     if (C <= rows::kShortRow)
       hipLaunchKernelGGL((top_short<T>), dim3((unsigned)((R + rows::kShortRows - 1) / rows::kShortRows)), dim3(256), 0,
                          s, a);
-    else if (const int parts = top_parts(R, C, dtype, K); parts > 1) {
+    // (the workspace's size is that of rows that are not aligned, which may be a vector longer)
+    else if (const int parts = top_parts(R, C, dtype, K); parts > 1 && (Q > 16 * 1024 || R <= cu_count() / 2)) {
       constexpr int kVec = rows::Row<T>::kVec;
       Top part = a;
       part.parts = parts;

@@ -655,9 +655,14 @@ def readout_ce(V_out: torch.Tensor, labels: torch.Tensor, mode: int, dense=False
 
 # These three are called once a step or a token on little data, where the host's work is most of the time: they check
 # what they are given and not again what they have made themselves.
+# With a stream given they work as on torch's current one: what they allocate is that stream's, since memory of another
+# stream may still be in use there, and a workspace that is dropped may be handed out there again at once.
 
 def readout_top(logits: torch.Tensor, K: int, tau=1.0, want_lse=True, ws=None, stream=None):
     """A teacher's record of rows of logits [..., C]: (ids [..., K] int32, vals [..., K], lse [...] or None)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return readout_top(logits, K, tau, want_lse, ws)
     p, code, R, C, ld = _rows(logits)
     shape, dev = logits.shape[:-1], logits.device
     ids = torch.empty((*shape, K), dtype=torch.int32, device=dev)
@@ -667,7 +672,7 @@ def readout_top(logits: torch.Tensor, K: int, tau=1.0, want_lse=True, ws=None, s
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
     _check("snn_readout_top", lib().snn_readout_top(
         p, code, R, C, ld, K, tau, ids.data_ptr(), vals.data_ptr(), lse.data_ptr() if want_lse else None,
-        _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
+        _ptr(ws, None, "workspace"), _nbytes(ws), _stream()))
     return ids, vals, lse
 
 
@@ -676,6 +681,9 @@ def readout_distill(logits: torch.Tensor, ids, vals, lse=None, tau=1.0, weight=N
     """Distillation loss of rows of logits [..., C] against a teacher's records. Returns (loss [1], row_loss [...],
     grad like the logits, or None). A grad that is given is written, or added to with accumulate; one that is made has
     the rows of the logits at the same distance, since rows that begin alike are written fastest."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return readout_distill(logits, ids, vals, lse, tau, weight, want_grad, grad, accumulate, ws)
     if accumulate and grad is None:
         raise ValueError("readout_distill: accumulate needs a grad to add to")
     p, code, R, C, ld = _rows(logits)
@@ -700,13 +708,16 @@ def readout_distill(logits: torch.Tensor, ids, vals, lse=None, tau=1.0, weight=N
     _check("snn_readout_distill", fn(
         p, code, R, C, ld, _of_rows(ids, R * K, torch.int32, "ids"), _of_rows(vals, R * K, torch.float32, "vals"),
         _of_rows(lse, R, torch.float32, "lse"), K, tau, _of_rows(weight, R, torch.float32, "weight"), loss.data_ptr(),
-        row_loss.data_ptr(), g, ld_grad, int(accumulate), _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
+        row_loss.data_ptr(), g, ld_grad, int(accumulate), _ptr(ws, None, "workspace"), _nbytes(ws), _stream()))
     return loss, row_loss, grad
 
 
 def readout_sample(logits: torch.Tensor, u, temperature=None, top_k=None, top_p=None, min_p=None, ws=None, stream=None):
     """One class drawn per row of logits [..., C] from uniforms u [...]; the settings are arrays [...] on the device, or
     None. Returns (cls [...] int32, logp [...], kept [...] int32)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return readout_sample(logits, u, temperature, top_k, top_p, min_p, ws)
     p, code, R, C, ld = _rows(logits)
     shape, dev = logits.shape[:-1], logits.device
     cls = torch.empty(shape, dtype=torch.int32, device=dev)
@@ -718,7 +729,7 @@ def readout_sample(logits: torch.Tensor, u, temperature=None, top_k=None, top_p=
     _check("snn_readout_sample", lib().snn_readout_sample(
         p, code, R, C, ld, _of_rows(u, R, f32, "u"), _of_rows(temperature, R, f32, "temperature"),
         _of_rows(top_k, R, torch.int32, "top_k"), _of_rows(top_p, R, f32, "top_p"), _of_rows(min_p, R, f32, "min_p"),
-        cls.data_ptr(), logp.data_ptr(), kept.data_ptr(), _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
+        cls.data_ptr(), logp.data_ptr(), kept.data_ptr(), _ptr(ws, None, "workspace"), _nbytes(ws), _stream()))
     return cls, logp, kept
 
 

@@ -547,3 +547,31 @@ def test_many_rows_distill(R, C, dtype):
     a = snn.readout_distill(view, *map(dev, rec), 1.5, dev(weight))
     b = snn.readout_distill(view, *map(dev, rec), 1.5, dev(weight), grad=full[:, :C])
     assert torch.equal(a[0], b[0]) and torch.equal(a[2], b[2])
+
+
+def test_memory_is_the_given_streams(monkeypatch):
+    """Outputs and workspaces of a call on a given stream are allocated on it: a workspace of another stream could be
+    handed out there while the call still uses it."""
+    side = torch.cuda.Stream()
+    rng = np.random.default_rng(0)
+    view = _rows(_logits(rng, 3, 70001, "normal"), "f32")  # shared among blocks: every call has a workspace
+    u = torch.rand(3, device="cuda")
+    weight, half = torch.ones(3, device="cuda"), torch.full((3,), 0.5, device="cuda")
+    want = snn.readout_top(view, 20, 2.0), snn.readout_sample(view, u, weight, None, half, None)
+    want += (snn.readout_distill(view, *want[0], 2.0, weight),)
+    torch.cuda.synchronize()
+    made, empty = [], torch.empty
+
+    def counted(*a, **k):
+        made.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*a, **k)
+
+    monkeypatch.setattr(snn.torch, "empty", counted)
+    got = (snn.readout_top(view, 20, 2.0, stream=side),
+           snn.readout_sample(view, u, weight, None, half, None, stream=side))
+    got += (snn.readout_distill(view, *got[0], 2.0, weight, stream=side),)
+    monkeypatch.undo()
+    side.synchronize()
+    assert len(made) >= 3 + 1 + 3 + 1 + 3 + 1 and set(made) == {side.cuda_stream}
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))

@@ -26,6 +26,8 @@ What it computes, and where the paper defines it:
 * regularize.py -- the activity penalties of App. E and their gradient w.r.t.
   spike counts.
 * adam.py     -- the Adam update (App. E's optimiser; Kingma and Ba, Algorithm 1).
+* rows.py     -- operators on rows of logits (the K largest, distillation with its
+  gradient, drawing a class), in 64 bits.
 * train.py    -- a whole training step (loss with penalties, gradient, Adam) and
   the sparse vs full-surrogate gradient difference of App. H.
 * conv.py     -- the convolutional spiking layer (3x3, padding 1) with 2x2 max

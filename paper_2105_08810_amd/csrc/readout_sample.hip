@@ -4,6 +4,18 @@
 //   least top_p of theirs, of these the classes with e_j >= min_p
 //   drawn: the first class whose kept weights up to it, in the order of the classes, exceed floor(u * their sum)
 // The weights are whole numbers, so every sum is exact and the answer does not depend on how it was summed.
+//
+// A row is held in registers. What top-k keeps is collected by the waves' n-th largest lanes, as a teacher's record is;
+// what top-p keeps is either among those or found by a histogram of t and an order within one of its bins; without
+// either filter the weights are summed in runs along the row and the drawn class is sought in one run.
+//   sample_short   16 lanes a row of up to 128 classes
+//   sample_tile    a block a row, in registers
+//   split_*        a row's parts in blocks of their own: few long rows, rows beyond the registers
+//   sample_rows    a block a row, read several times: the rest
+//
+// Measured: 1024 x 65536 float32 with a temperature: 136 us (2.0 TB/s), bound by the vector instructions of the
+// exponentials and 64-bit sums; 64 x 128011 bfloat16, mixed settings, in parts: 62 us, and 1 x 32003 float32 with
+// top-k 50: 18 us, both bound by latency; 25600 x 20 float32, mixed settings: 14.6 us.
 #include "rows.h"
 
 namespace snn {

@@ -7,8 +7,13 @@
 // wave's lanes, and the smallest of those over the waves. At least K values reach it, and hardly more do when values
 // lie in no particular order along the row (a thread's vectors are a block's width apart, so that a run of likely
 // classes is spread over all waves). One comparison a value collects them in LDS, where each counts those before it.
-// Rows of up to 128 classes go 16 lanes each (top_short). Where too many reach the bound (long runs of equal values), where K needs more than kNthMost of a wave, and for rows
-// beyond the registers, the cut is found by histograms of the row as it lies in memory (top_general).
+// Rows of up to 128 classes go 16 lanes each (top_short). Where too many reach the bound (long runs of equal values),
+// where K needs more than kNthMost of a wave, and for rows beyond the registers, the cut is found by histograms of the
+// row as it lies in memory (top_general).
+//
+// Measured: 128000 x 100 float32, K 8: 20.6 us (2.9 TB/s), bound by the vector instructions of the maxima; 2048 x 32003
+// bfloat16, K 64: 48.8 us (2.7 TB/s), where half is the read and half what follows behind barriers; 24 x 131072
+// float16, K 50, in parts: 22.8 us, bound by the latency of two launches.
 #include "rows.h"
 
 namespace snn {

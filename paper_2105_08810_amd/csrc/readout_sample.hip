@@ -9,13 +9,17 @@
 // what top-p keeps is either among those or found by a histogram of t and an order within one of its bins; without
 // either filter the weights are summed in runs along the row and the drawn class is sought in one run.
 //   sample_short   16 lanes a row of up to 128 classes
-//   sample_tile    a block a row, in registers
+//   sample_tile    a block a row, in registers; one wave up to 2048 classes (cut_in_wave)
 //   split_*        a row's parts in blocks of their own: few long rows, rows beyond the registers
 //   sample_rows    a block a row, read several times: the rest
 //
 // Measured: 1024 x 65536 float32 with a temperature: 136 us (2.0 TB/s), bound by the vector instructions of the
 // exponentials and 64-bit sums; 64 x 128011 bfloat16, mixed settings, in parts: 62 us, and 1 x 32003 float32 with
-// top-k 50: 18 us, both bound by latency; 25600 x 20 float32, mixed settings: 14.6 us.
+// top-k 50: 18 us, both bound by latency; 23265 x 590 bfloat16, mixed settings: 128 us, bound by the vector instructions of
+// some 15 to 30 comparisons a value; 25600 x 20 float32, mixed settings: 14.6 us.
+#include <cfloat>
+#include <type_traits>
+
 #include "rows.h"
 
 namespace snn {
@@ -329,15 +333,15 @@ __device__ __forceinline__ int bin_of(float t) { return min(kBins - 1, (int)(t *
 
 // Lanes of each wave that the bound is taken from, at most: with n of 64 lanes -64 log(1 - n/64) of its values reach it.
 template <int NT>
-constexpr int kNthMost = NT == kWave ? 56 : NT == 256 ? 50 : 32;
+constexpr int kNthMost = NT == 256 ? 50 : 32;
 
 template <int NT, int NV>
 struct TileLds {
-  static constexpr int kList = NT == kWave ? 256 : 1024;
+  static constexpr int kList = NT == kWave ? 1 : 1024;  // one wave finds the cut without a list
   static constexpr int kChunks = NV * NT / kWave;
   union {
     GeneralLds<NT> general;
-    uint64_t mass[kBins];
+    uint64_t mass[NT == kWave ? 1 : kBins];
     struct {
       uint64_t list[kList];  // key (inverted) and class: in the order when ascending
       uint64_t before[kList];
@@ -428,6 +432,130 @@ __device__ __forceinline__ void order_list(const Weigh& weigh, int n, Lds& s) {
   __syncthreads();
 }
 
+// The cut of a row in one wave's registers: what is larger than `cut` is kept, and of what equals it the classes up to
+// `last`. The filters' ends are sought by halving a range of values whose larger end too few elements reach (or too
+// little weight) and whose smaller end enough: one comparison a value and a count of lanes for top-k, the weights' sum
+// besides for top-p, no LDS and no order. The range begins where weights do; it is done when it holds one element, or
+// elements of one value, whose class at the end is sought in the same manner.
+template <class T, int NV>
+__device__ __forceinline__ void cut_in_wave(const Tile<T, kWave, NV>& tile, const Row<T>& row, const RowSettings& set,
+                                            const Weigh& weigh, int C, float& cut, int& last) {
+  constexpr int kVec = Row<T>::kVec;
+  // the bits of a key that are the same in all of a type's values of one sign
+  constexpr int kLow = sizeof(T) == 4 ? 0 : std::is_same<T, Bf16>::value ? 16 : 13;
+  constexpr uint32_t kLowBits = (1u << kLow) - 1;
+  struct Reach {
+    int count;
+    uint64_t mass;
+  };
+  uint32_t w[NV * kVec];
+  if (set.top_p < 1.0f) {
+#pragma unroll
+    for (int i = 0; i < NV * kVec; ++i) w[i] = 0;
+    tile.each_unrolled(row, [&](const float (&x)[kVec], int, int n) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) w[n * kVec + i] = (uint32_t)rintf(exp_down(weigh.plain_t(x[i])) * kUnit);
+    });
+  }
+  // elements for which in(value, class), and their weight
+  const auto count_of = [&](auto in) {
+    int count = 0;
+    tile.each_unrolled(row, [&](const float (&x)[kVec], int q, int) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) count += __popcll(__ballot(in(x[i], row.first(q) + i)));
+    });
+    return count;
+  };
+  const auto reach_of = [&](auto in) {
+    Reach v{0, 0};
+    tile.each_unrolled(row, [&](const float (&x)[kVec], int q, int n) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const bool yes = in(x[i], row.first(q) + i);
+        v.count += __popcll(__ballot(yes));
+        v.mass += yes ? w[n * kVec + i] : 0;
+      }
+    });
+    v.mass = wave_sum64(v.mass);
+    return v;
+  };
+  const auto least_of = [&](uint32_t s) { return of_key(s << kLow); };
+  const auto value_of = [&](uint32_t s) { return of_key(s << kLow | (s << kLow >> 31 ? 0 : kLowBits)); };
+  // the first class c of [0, C) with enough(c), which holds for the last
+  const auto first_class = [&](auto enough) {
+    int from = -1, to = C - 1;
+    while (to - from > 1) {
+      const int mid = (from + to) >> 1;
+      if (enough(mid)) to = mid;
+      else from = mid;
+    }
+    return to;
+  };
+  // 24 temperatures below the largest no weight is left (and -inf has none)
+  uint32_t lo = key_of(fmaxf(weigh.max - 24.0f * set.temperature, -FLT_MAX)) >> kLow;
+  const uint32_t top = (key_of(weigh.max) >> kLow) + 1;
+  lo = (uint32_t)same_in_wave((int)lo);
+  cut = least_of(lo);
+  last = C;
+  int n_lo = C;  // elements from lo on, of those below `top`; C for unknown
+  if (set.k < C) {
+    n_lo = count_of([&](float x, int) { return x >= cut; });
+    if (n_lo > set.k) {
+      uint32_t hi = top;
+      int n_hi = 0;
+      while (hi - lo > 1 && n_lo != set.k) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        const float least = least_of(mid);
+        const int n = count_of([&](float x, int) { return x >= least; });
+        if (n >= set.k) {
+          lo = mid;
+          n_lo = n;
+        } else {
+          hi = mid;
+          n_hi = n;
+        }
+      }
+      cut = least_of(lo);
+      if (n_lo != set.k) {  // the last kept are some of those equal to one another
+        cut = value_of(lo);
+        last = first_class([&](int c) {
+          return n_hi + count_of([&](float x, int j) { return (x == cut) & (j <= c); }) >= set.k;
+        });
+      }
+    }
+  }
+  if (set.top_p < 1.0f) {
+    const uint64_t limit =
+        set.limit(reach_of([&](float x, int j) { return (x > cut) | ((x == cut) & (j <= last)); }).mass);
+    uint32_t hi = top;
+    Reach above{0, 0};
+    while (hi - lo > 1 && n_lo - above.count > 1) {
+      const uint32_t mid = lo + (hi - lo) / 2;
+      const float least = least_of(mid);
+      const Reach v = reach_of([&](float x, int) { return x >= least; });
+      if (v.mass >= limit) {
+        lo = mid;
+        n_lo = v.count;
+      } else {
+        hi = mid;
+        above = v;
+      }
+    }
+    if (n_lo - above.count == 1) {
+      cut = least_of(lo);
+      last = C;
+    } else {
+      cut = value_of(lo);
+      last = first_class([&](int c) {
+        return above.mass + reach_of([&](float x, int j) { return (x == cut) & (j <= c); }).mass >= limit;
+      });
+    }
+  }
+}
+
+template <class T>
+constexpr int kWaveVectors = 32 / Row<T>::kVec;
+
 // Draws from the n collected elements, which hold all that can be kept. sum: the weight that top-p is a part of; 0:
 // that of the first k elements.
 template <class T, int NT, int NV>
@@ -493,9 +621,8 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
   tile.load(row);
   // the largest value and a bound that at least `want` values reach
   const int full = max(1, min(kWaves, row.Q / kWave));  // waves without idle lanes give the bound
-  const bool all = set.k > kNthMost<NT> * full && set.k < a.C && a.C <= kList;
-  const bool few = set.k <= kNthMost<NT> * full || all;  // what top-k keeps can be collected
-  const int nth = few && !all ? (set.k + full - 1) / full : max(4, 16 / full);
+  const bool few = set.k <= kNthMost<NT> * full;  // what top-k keeps can be collected
+  const int nth = few ? (set.k + full - 1) / full : max(4, 16 / full);
   float most = -INFINITY;
   bool nan = false;
   tile.each_unrolled(row, [&](const float (&x)[kVec], int, int) {
@@ -507,7 +634,7 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
   });
   const uint32_t own = nan ? 0u : key_of(most);  // 0 is no value's key
   uint32_t high = wave_max_u32(own);
-  uint32_t bound = wave < full ? wave_nth(own, nth) : UINT32_MAX;
+  uint32_t bound = NT > kWave && wave < full ? wave_nth(own, nth) : UINT32_MAX;
   bool odd = __ballot(nan) != 0;
   if (tid == 0) s.n_list = 0;
   if (NT > kWave) {
@@ -530,7 +657,7 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
   odd = same_in_wave(odd);
   const float m = same_in_wave(of_key(high));
   const Weigh weigh{m, 1.0f / set.temperature};
-  if (odd || isinf(m) || (!few && set.k < a.C) || (isinf(weigh.inv) && set.k != 1)) return false;
+  if (odd || isinf(m) || (NT > kWave && !few && set.k < a.C) || (isinf(weigh.inv) && set.k != 1)) return false;
   if (set.k == 1) {  // the first of the largest
     int at = INT32_MAX;
     tile.each(row, [&](const float (&x)[kVec], int q, int) {
@@ -542,7 +669,7 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
     if (tid == 0) a.answer(r, at, 0.0f, 1);
     return true;
   }
-  const float least = all ? -INFINITY : same_in_wave(of_key(bound));
+  const float least = same_in_wave(of_key(bound));
   int last = a.C;  // class of the last kept element at the cut
   // One loop over the row for all passes: the exponential's code is there once.
   //   kCollect  the elements that reach the bound (all that top-k keeps)
@@ -551,17 +678,20 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
   //   kPart     and the elements of the part with the cut
   //   kShare    the kept weights of runs of 64 vectors, which follow one another in the order of the classes
   enum { kCollect, kSum, kBin, kPart, kShare };
-  int mode = few ? kCollect : set.top_p < 1.0f ? kSum : kShare;
+  int mode = NT == kWave ? kShare : few ? kCollect : set.top_p < 1.0f ? kSum : kShare;
   uint64_t sum = 0, limit = 0, above = 0;
   uint32_t count = 0;
   float cut = -INFINITY;
   int part = 0, n = 0;
+  if constexpr (NT == kWave) {
+    if (set.k < a.C || set.top_p < 1.0f) cut_in_wave<T, NV>(tile, row, set, weigh, a.C, cut, last);
+  }
   for (;;) {
     count = 0;
     uint64_t own_sum = 0;
     tile.each(row, [&](const float (&x)[kVec], int q, int) {
       // hidden from the compiler, which would make a loop of its own for every mode
-      const int mode_here = __builtin_amdgcn_readfirstlane(mode + opaque_zero());
+      const int mode_here = NT == kWave ? kShare : __builtin_amdgcn_readfirstlane(mode + opaque_zero());
       uint32_t take = 0;
       if (mode_here == kCollect) {
 #pragma unroll
@@ -611,7 +741,7 @@ __device__ __forceinline__ bool sample_in_registers(const Sample& a, int64_t r, 
         }
       }
     });
-    if (mode == kShare) break;
+    if (NT == kWave || mode == kShare) break;
     __syncthreads();
     n = same_in_wave((int)s.n_list);
     if (mode == kCollect || mode == kPart) {
@@ -1085,10 +1215,10 @@ extern "C" snn_status snn_readout_sample(const void* logits, int dtype, int64_t 
     if (C <= rows::kShortRow && (C <= 32 || R > cu_count()))
       hipLaunchKernelGGL((sample_short<T>), dim3((unsigned)((R + rows::kShortRows - 1) / rows::kShortRows)), dim3(256),
                          0, s, a);
-    // fewer rows: more threads on each (1 row of 1000, top-k 50: 39 and 14 us); with a top-k, which may be long, a list
-    // for all of up to 1024 classes (23265 rows of 590 bf16, requests: 606 us without)
-    else if (Q <= 4 * 64 && R > cu_count() && !top_k)
-      hipLaunchKernelGGL((sample_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
+    // up to 32 values a lane: one wave, without barriers (in a block of 256 that lists and orders what is kept 23265 rows
+    // of 590 bfloat16 with top-k 50 took 492 us, 110 so; one row of 1000 float32 14 and 10)
+    else if (Q <= kWaveVectors<T> * kWave)
+      hipLaunchKernelGGL((sample_tile<T, kWave, kWaveVectors<T>>), grid, dim3(kWave), 0, s, a);
     else if (Q <= 4 * 256)
       hipLaunchKernelGGL((sample_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
     else if (Q <= 4 * 1024)

@@ -575,3 +575,28 @@ def test_memory_is_the_given_streams(monkeypatch):
     assert len(made) >= 3 + 1 + 3 + 1 + 3 + 1 and set(made) == {side.cuda_stream}
     for a, b in zip(want, got):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("C,kind", [(129, "ties"), (130, "zeros"), (255, "wide"), (590, "ties"), (590, "lowest"),
+                                    (1023, "normal"), (1302, "masked"), (2041, "ties"), (2048, "wide"), (2048, "equal"),
+                                    (2049, "ties")])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_sample_cuts_of_middle_rows(C, kind, dtype):
+    """Lengths that one wave holds and just beyond, top-k of every size, cuts within equal values, temperatures at which
+    one weight or all of them count."""
+    rng = np.random.default_rng(C)
+    R = 40
+    view = _rows(_logits(rng, R, C, kind), dtype, C + 5, C % 4)
+    if kind == "lowest":
+        view[view < -50000.0] = torch.finfo(DTYPES[dtype]).min
+    temperature = (10.0 ** rng.uniform(-1.0, 1.0, R)).astype(np.float32)
+    temperature[:4] = 1e-20, 1e30, 1e-5, 300.0
+    top_k = rng.integers(2, C + 1, R).astype(np.int32)
+    top_k[::7] = C - 1
+    top_p = rng.random(R).astype(np.float32)
+    top_p[::5] = 1.0
+    top_p[1] = 0.0
+    min_p = np.where(rng.random(R) < 0.5, 0.0, 0.05 * rng.random(R)).astype(np.float32)
+    u = rng.random(R).astype(np.float32)
+    for settings in ((top_k, None, None), (None, top_p, None), (top_k, top_p, min_p)):
+        _check_sample(view, u, temperature, *settings)

@@ -18,7 +18,6 @@
 // top-k 50: 18 us, both bound by latency; 23265 x 590 bfloat16, mixed settings: 128 us, bound by the vector instructions of
 // some 15 to 30 comparisons a value; 25600 x 20 float32, mixed settings: 14.6 us.
 #include <cfloat>
-#include <type_traits>
 
 #include "rows.h"
 
@@ -433,17 +432,11 @@ __device__ __forceinline__ void order_list(const Weigh& weigh, int n, Lds& s) {
 }
 
 // The cut of a row in one wave's registers: what is larger than `cut` is kept, and of what equals it the classes up to
-// `last`. The filters' ends are sought by halving a range of values whose larger end too few elements reach (or too
-// little weight) and whose smaller end enough: one comparison a value and a count of lanes for top-k, the weights' sum
-// besides for top-p, no LDS and no order. The range begins where weights do; it is done when it holds one element, or
-// elements of one value, whose class at the end is sought in the same manner.
+// `last`. Top-k's is found by first_in_wave, top-p's in the same manner with the weights' sum beside the count.
 template <class T, int NV>
 __device__ __forceinline__ void cut_in_wave(const Tile<T, kWave, NV>& tile, const Row<T>& row, const RowSettings& set,
                                             const Weigh& weigh, int C, float& cut, int& last) {
   constexpr int kVec = Row<T>::kVec;
-  // the bits of a key that are the same in all of a type's values of one sign
-  constexpr int kLow = sizeof(T) == 4 ? 0 : std::is_same<T, Bf16>::value ? 16 : 13;
-  constexpr uint32_t kLowBits = (1u << kLow) - 1;
   struct Reach {
     int count;
     uint64_t mass;
@@ -458,14 +451,6 @@ __device__ __forceinline__ void cut_in_wave(const Tile<T, kWave, NV>& tile, cons
     });
   }
   // elements for which in(value, class), and their weight
-  const auto count_of = [&](auto in) {
-    int count = 0;
-    tile.each_unrolled(row, [&](const float (&x)[kVec], int q, int) {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) count += __popcll(__ballot(in(x[i], row.first(q) + i)));
-    });
-    return count;
-  };
   const auto reach_of = [&](auto in) {
     Reach v{0, 0};
     tile.each_unrolled(row, [&](const float (&x)[kVec], int q, int n) {
@@ -479,59 +464,25 @@ __device__ __forceinline__ void cut_in_wave(const Tile<T, kWave, NV>& tile, cons
     v.mass = wave_sum64(v.mass);
     return v;
   };
-  const auto least_of = [&](uint32_t s) { return of_key(s << kLow); };
-  const auto value_of = [&](uint32_t s) { return of_key(s << kLow | (s << kLow >> 31 ? 0 : kLowBits)); };
-  // the first class c of [0, C) with enough(c), which holds for the last
-  const auto first_class = [&](auto enough) {
-    int from = -1, to = C - 1;
-    while (to - from > 1) {
-      const int mid = (from + to) >> 1;
-      if (enough(mid)) to = mid;
-      else from = mid;
-    }
-    return to;
-  };
   // 24 temperatures below the largest no weight is left (and -inf has none)
-  uint32_t lo = key_of(fmaxf(weigh.max - 24.0f * set.temperature, -FLT_MAX)) >> kLow;
-  const uint32_t top = (key_of(weigh.max) >> kLow) + 1;
+  uint32_t lo = short_key<T>(fmaxf(weigh.max - 24.0f * set.temperature, -FLT_MAX));
+  const uint32_t top = short_key<T>(weigh.max) + 1;
   lo = (uint32_t)same_in_wave((int)lo);
-  cut = least_of(lo);
+  cut = least_of<T>(lo);
   last = C;
   int n_lo = C;  // elements from lo on, of those below `top`; C for unknown
   if (set.k < C) {
-    n_lo = count_of([&](float x, int) { return x >= cut; });
-    if (n_lo > set.k) {
-      uint32_t hi = top;
-      int n_hi = 0;
-      while (hi - lo > 1 && n_lo != set.k) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        const float least = least_of(mid);
-        const int n = count_of([&](float x, int) { return x >= least; });
-        if (n >= set.k) {
-          lo = mid;
-          n_lo = n;
-        } else {
-          hi = mid;
-          n_hi = n;
-        }
-      }
-      cut = least_of(lo);
-      if (n_lo != set.k) {  // the last kept are some of those equal to one another
-        cut = value_of(lo);
-        last = first_class([&](int c) {
-          return n_hi + count_of([&](float x, int j) { return (x == cut) & (j <= c); }) >= set.k;
-        });
-      }
-    }
+    n_lo = count_in_wave(tile, row, [&](float x, int) { return x >= cut; });
+    if (n_lo > set.k) first_in_wave(tile, row, C, set.k, lo, top, n_lo, cut, last);
   }
   if (set.top_p < 1.0f) {
     const uint64_t limit =
         set.limit(reach_of([&](float x, int j) { return (x > cut) | ((x == cut) & (j <= last)); }).mass);
     uint32_t hi = top;
     Reach above{0, 0};
-    while (hi - lo > 1 && n_lo - above.count > 1) {
-      const uint32_t mid = lo + (hi - lo) / 2;
-      const float least = least_of(mid);
+    for (int step = 0; hi - lo > 1 && n_lo - above.count > 1; ++step) {
+      const uint32_t mid = halfway<T>(lo, hi, step);
+      const float least = least_of<T>(mid);
       const Reach v = reach_of([&](float x, int) { return x >= least; });
       if (v.mass >= limit) {
         lo = mid;
@@ -542,19 +493,16 @@ __device__ __forceinline__ void cut_in_wave(const Tile<T, kWave, NV>& tile, cons
       }
     }
     if (n_lo - above.count == 1) {
-      cut = least_of(lo);
+      cut = least_of<T>(lo);
       last = C;
     } else {
-      cut = value_of(lo);
-      last = first_class([&](int c) {
+      cut = value_of<T>(lo);
+      last = first_class(C, [&](int c) {
         return above.mass + reach_of([&](float x, int j) { return (x == cut) & (j <= c); }).mass >= limit;
       });
     }
   }
 }
-
-template <class T>
-constexpr int kWaveVectors = 32 / Row<T>::kVec;
 
 // Draws from the n collected elements, which hold all that can be kept. sum: the weight that top-p is a part of; 0:
 // that of the first k elements.
@@ -1217,8 +1165,8 @@ extern "C" snn_status snn_readout_sample(const void* logits, int dtype, int64_t 
                          0, s, a);
     // up to 32 values a lane: one wave, without barriers (in a block of 256 that lists and orders what is kept 23265 rows
     // of 590 bfloat16 with top-k 50 took 492 us, 110 so; one row of 1000 float32 14 and 10)
-    else if (Q <= kWaveVectors<T> * kWave)
-      hipLaunchKernelGGL((sample_tile<T, kWave, kWaveVectors<T>>), grid, dim3(kWave), 0, s, a);
+    else if (Q <= rows::kWaveVectors<T> * kWave)
+      hipLaunchKernelGGL((sample_tile<T, kWave, rows::kWaveVectors<T>>), grid, dim3(kWave), 0, s, a);
     else if (Q <= 4 * 256)
       hipLaunchKernelGGL((sample_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
     else if (Q <= 4 * 1024)

@@ -7,7 +7,8 @@
 // wave's lanes, and the smallest of those over the waves. At least K values reach it, and hardly more do when values
 // lie in no particular order along the row (a thread's vectors are a block's width apart, so that a run of likely
 // classes is spread over all waves). One comparison a value collects them in LDS, where each counts those before it.
-// Rows of up to 128 classes go 16 lanes each (top_short). Where too many reach the bound (long runs of equal values),
+// Rows of up to 128 classes go 16 lanes each (top_short), of up to 2048 a wave each, which finds the cut by halving a
+// range of values and lists just the K before it (top_wave). Where too many reach the bound (long runs of equal values),
 // where K needs more than kNthMost of a wave, and for rows beyond the registers, the cut is found by histograms of the
 // row as it lies in memory (top_general).
 //
@@ -23,8 +24,7 @@ using namespace rows;
 
 // Lanes of each wave that the bound is taken from, at most: with n of 64 lanes -64 log(1 - n/64) of its values reach it,
 // somewhat more where the smallest of several waves counts.
-template <int NT>
-constexpr int kNthMost = NT == kWave ? 56 : 32;
+constexpr int kNthMost = 32;
 // Waves of a block whose lanes all hold a vector of a row with at least Q of them.
 template <int NT>
 __host__ __device__ constexpr int full_waves(int Q) {
@@ -38,7 +38,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 template <int NT>
 struct TopLds {
-  static constexpr int kList = NT == kWave ? 256 : 1024;
+  static constexpr int kList = 1024;
   union {
     SelectLds<NT> select;
     uint64_t list[kList];
@@ -261,7 +261,7 @@ __device__ __forceinline__ bool top_in_registers(const Row<T>& row, const Top& a
   const uint32_t key = nan ? 0u : key_of(most);  // 0 is no value's key
   uint32_t high = wave_max_u32(key);
   uint32_t bound = UINT32_MAX;  // a wave with idle lanes has no part in it
-  const bool all = nth_of<NT>(a.K, row.Q) > kNthMost<NT>;  // every value is collected
+  const bool all = nth_of<NT>(a.K, row.Q) > kNthMost;  // every value is collected (of a short last part)
   if (tid / kWave < full_waves<NT>(row.Q)) bound = wave_nth(key, all ? 1 : nth_of<NT>(a.K, row.Q));
   bool odd = __ballot(nan) != 0;
   if (tid == 0) s.n_taken = 0;
@@ -336,6 +336,59 @@ __global__ __launch_bounds__(NT) void top_tile(Top a) {
     __syncthreads();
     top_general<T, NT>(row, a, r, s);
   }
+}
+
+// ------------------------------------------------------------------ rows that one wave holds
+
+// The K first are known by the cut, collected in a list of just their number and ordered there.
+template <class T>
+__global__ __launch_bounds__(kWave) void top_wave(Top a) {
+  extern __shared__ uint64_t list[];  // K, up to the next power of two
+  constexpr int kVec = Row<T>::kVec;
+  const int64_t r = blockIdx.x;
+  const Row<T> row(a.logits, r, a.ld, a.C);
+  Tile<T, kWave, kWaveVectors<T>> tile;
+  tile.load(row);
+  float most = -INFINITY, least = INFINITY;
+  tile.each_unrolled(row, [&](const float (&x)[kVec], int, int) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      most = fmaxf(most, x[i]);
+      least = x[i] > -INFINITY ? fminf(least, x[i]) : least;
+    }
+  });
+  const float m = of_key(wave_max_u32(key_of(most)));
+  if (a.lse) {
+    const float c = a.inv * kLog2e, mc = isinf(m) ? 0.0f : m * c;
+    float sum = 0.0f;
+    tile.each_unrolled(row, [&](const float (&x)[kVec], int, int) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) sum += exp2_fast(fmaf(no_nan(x[i]), c, -mc));
+    });
+    sum = wave_reduce(sum, Plus());
+    if (threadIdx.x == 0) a.lse[r] = isinf(m) ? m : m * a.inv + logf(sum);
+  }
+  float cut = -INFINITY;
+  int last = INT32_MIN;  // none of -inf, which also stands around the row
+  int n = count_in_wave(tile, row, [&](float x, int) { return x > -INFINITY; });
+  if (n > a.K) {
+    uint32_t lo = short_key<T>(of_key(~wave_max_u32(~key_of(least))));
+    first_in_wave(tile, row, a.C, a.K, lo, short_key<T>(m) + 1, n, cut, last);
+  }
+  n = 0;
+  tile.each_unrolled(row, [&](const float (&x)[kVec], int q, int) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      const int j = row.first(q) + i;
+      const bool in = (x[i] > cut) | ((x[i] == cut) & (j <= last));
+      const uint64_t all = __ballot(in);
+      if (in) list[n + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0))] =
+          entry(key_of(x[i]), j);
+      n += __popcll(all);
+    }
+  });
+  __syncthreads();
+  write_record<T, kWave>(row, a, r, list, n);
 }
 
 // ------------------------------------------------------------------ few long rows, several blocks each
@@ -421,6 +474,12 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
     if (C <= rows::kShortRow)
       hipLaunchKernelGGL((top_short<T>), dim3((unsigned)((R + rows::kShortRows - 1) / rows::kShortRows)), dim3(256), 0,
                          s, a);
+    // one wave (20000 rows of 700 float32, K 8, 40, 100: 38, 84, 338 us in blocks with the bound; 33, 39, 61 so)
+    else if (Q <= rows::kWaveVectors<T> * kWave) {
+      int size = 2;
+      while (size < K) size <<= 1;
+      hipLaunchKernelGGL((top_wave<T>), grid, dim3(kWave), size * sizeof(uint64_t), s, a);
+    }
     // (the workspace's size is that of rows that are not aligned, which may be a vector longer)
     else if (const int parts = top_parts(R, C, dtype, K); parts > 1 && (Q > 16 * 1024 || R <= cu_count() / 2)) {
       constexpr int kVec = rows::Row<T>::kVec;
@@ -430,18 +489,14 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
       top_carve(workspace, R, parts, K, &part);
       hipLaunchKernelGGL((top_tile<T, kPartThreads, 4>), dim3((unsigned)(R * parts)), dim3(kPartThreads), 0, s, part);
       hipLaunchKernelGGL(top_merge, grid, dim3(kMerged), 0, s, part, a);
-    } else if (Q <= 4 * 64 && nth_of<64>(K, least) <= kNthMost<64>)
-      hipLaunchKernelGGL((top_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
-    else if (Q <= 4 * 256 && (C <= TopLds<256>::kList || nth_of<256>(K, least) <= kNthMost<256>))
+    } else if (Q <= 4 * 256 && nth_of<256>(K, least) <= kNthMost)
       hipLaunchKernelGGL((top_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
-    else if (Q <= 8 * 512 && nth_of<512>(K, least) <= kNthMost<512> && R >= cu_count())
+    else if (Q <= 8 * 512 && nth_of<512>(K, least) <= kNthMost && R >= cu_count())
       hipLaunchKernelGGL((top_tile<T, 512, 8>), grid, dim3(512), 0, s, a);
-    else if (Q <= 4 * 1024 && nth_of<1024>(K, least) <= kNthMost<1024>)
+    else if (Q <= 4 * 1024 && nth_of<1024>(K, least) <= kNthMost)
       hipLaunchKernelGGL((top_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
-    else if (Q <= 16 * 1024 && nth_of<1024>(K, least) <= kNthMost<1024>)
+    else if (Q <= 16 * 1024 && nth_of<1024>(K, least) <= kNthMost)
       hipLaunchKernelGGL((top_tile<T, 1024, 16>), grid, dim3(1024), 0, s, a);
-    else if (Q <= 256)
-      hipLaunchKernelGGL((top_rows<T, 64>), grid, dim3(64), 0, s, a);
     else if (Q <= 4096)
       hipLaunchKernelGGL((top_rows<T, 256>), grid, dim3(256), 0, s, a);
     else

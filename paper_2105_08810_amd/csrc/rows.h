@@ -8,6 +8,8 @@
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 
+#include <type_traits>
+
 namespace snn {
 namespace rows {
 
@@ -422,6 +424,95 @@ __device__ __forceinline__ void block_sort(uint64_t* v, int n) {
       }
       __syncthreads();
     }
+}
+
+// ------------------------------------------------------------------ cuts in one wave
+//
+// The first k of a row's order where one wave holds the row: their end is sought by halving a range of values whose
+// larger end too few elements reach and whose smaller end enough. A step is one comparison a value and a count of lanes,
+// without LDS, atomics or an order; it ends when k elements reach the smaller end, or with a single value, among whose
+// elements the last class is sought in the same manner.
+
+template <class T>
+constexpr int kWaveVectors = 32 / Row<T>::kVec;  // 32 values a lane, 2048 classes
+
+// Key bits that are alike in all of a type's values of one sign, and keys without them.
+template <class T>
+constexpr int kLow = sizeof(T) == 4 ? 0 : std::is_same<T, Bf16>::value ? 16 : 13;
+template <class T>
+__device__ __forceinline__ uint32_t short_key(float x) {
+  return key_of(x) >> kLow<T>;
+}
+// A value that all elements of this short key reach and none of the one before; the elements' value.
+template <class T>
+__device__ __forceinline__ float least_of(uint32_t s) {
+  return of_key(s << kLow<T>);
+}
+template <class T>
+__device__ __forceinline__ float value_of(uint32_t s) {
+  const uint32_t k = s << kLow<T>;
+  return of_key(k >> 31 ? k : k | ((1u << kLow<T>) - 1));
+}
+// Between lo and hi, more than 1 apart: at first half way between the values, which lie evenly more often than their keys
+// (whose half is below 1e-19 from 0 to 1); then between the keys, of which 32 steps see the end.
+template <class T>
+__device__ __forceinline__ uint32_t halfway(uint32_t lo, uint32_t hi, int step) {
+  uint32_t mid = lo + (hi - lo) / 2;
+  if (step < 8) mid = short_key<T>(0.5f * least_of<T>(lo) + 0.5f * least_of<T>(hi));
+  return (uint32_t)same_in_wave((int)min(max(mid, lo + 1), hi - 1));
+}
+
+// Elements for which in(value, class).
+template <class T, int NV, class F>
+__device__ __forceinline__ int count_in_wave(const Tile<T, kWave, NV>& tile, const Row<T>& row, F in) {
+  constexpr int kVec = Row<T>::kVec;
+  int count = 0;
+  tile.each_unrolled(row, [&](const float (&x)[kVec], int q, int) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) count += __popcll(__ballot(in(x[i], row.first(q) + i)));
+  });
+  return count;
+}
+
+// The first class c of [0, C) with enough(c), which holds for the last.
+template <class F>
+__device__ __forceinline__ int first_class(int C, F enough) {
+  int from = -1, to = C - 1;
+  while (to - from > 1) {
+    const int mid = (from + to) >> 1;
+    if (enough(mid)) to = mid;
+    else from = mid;
+  }
+  return to;
+}
+
+// From lo with n_lo > k elements and top with none: the first k are those larger than cut and of its equals the classes up
+// to last. lo moves to where the cut is, n_lo to the elements that reach it.
+template <class T, int NV>
+__device__ __forceinline__ void first_in_wave(const Tile<T, kWave, NV>& tile, const Row<T>& row, int C, int k, uint32_t& lo,
+                                              uint32_t top, int& n_lo, float& cut, int& last) {
+  uint32_t hi = top;
+  int n_hi = 0;
+  for (int step = 0; hi - lo > 1 && n_lo != k; ++step) {
+    const uint32_t mid = halfway<T>(lo, hi, step);
+    const float least = least_of<T>(mid);
+    const int n = count_in_wave(tile, row, [&](float x, int) { return x >= least; });
+    if (n >= k) {
+      lo = mid;
+      n_lo = n;
+    } else {
+      hi = mid;
+      n_hi = n;
+    }
+  }
+  cut = least_of<T>(lo);
+  last = C;
+  if (n_lo != k) {  // the last are some of those equal to one another
+    cut = value_of<T>(lo);
+    last = first_class(C, [&](int c) {
+      return n_hi + count_in_wave(tile, row, [&](float x, int j) { return (x == cut) & (j <= c); }) >= k;
+    });
+  }
 }
 
 // ------------------------------------------------------------------ selection

@@ -66,13 +66,23 @@ class ReadoutRows:
         kd, _, _ = snn.readout_distill(self.V_out, rec.ids, rec.vals, rec.lse, rec.tau, weight, grad=grad,
                                        accumulate=True)
         if self.loss_mode == 0:
-            if self._every is None:  # row r has its C entries from r C on
-                dev = self.V_out.device
-                self._every = snn.Csr(torch.arange(0, T * B * C + 1, C, dtype=torch.int32, device=dev),
-                                      torch.arange(C, dtype=torch.int32, device=dev).repeat(T * B), None, None,
-                                      T * B * C)
-            csr = self._every
+            csr = self._all_entries()
         return csr, grad.view(-1), ce, grad if dense else None, kd
+
+    def _all_entries(self) -> snn.Csr:
+        """CSR of every entry of V_out: row r has its C entries from r C on. Kept from step to step while V_out has this
+        shape. One made while a stream is captured is the graph's own: it is filled by the graph's replays alone."""
+        T, B, C = self.V_out.shape
+        dev, n = self.V_out.device, T * B * C
+        every = self._every
+        if every is not None and (every.row_ptr.numel(), every.capacity, every.row_ptr.device) == (T * B + 1, n, dev):
+            return every
+        every = snn.Csr(torch.arange(0, n + 1, C, dtype=torch.int32, device=dev),
+                        torch.arange(C, dtype=torch.int32, device=dev).repeat(T * B), None,
+                        torch.full((1,), n, dtype=torch.int64, device=dev), n)
+        if not (dev.type == "cuda" and torch.cuda.is_current_stream_capturing()):
+            self._every = every
+        return every
 
 
 @dataclass
@@ -132,6 +142,7 @@ class Network(ReadoutRows):
         self.V_out = torch.empty((T, B, C), dtype=torch.float32, device=dev)
         self.S_out = torch.empty((T, B, C), dtype=torch.uint8, device=dev)
         self.trace_out = torch.empty((T, B, sizes[-1]), dtype=torch.float32, device=dev)
+        self._every = None
         return self
 
     def forward(self, b_th: Optional[float] = None):
@@ -433,6 +444,7 @@ class ConvNetwork(ReadoutRows):
         self.V_out = torch.empty((T, B, Cl), dtype=torch.float32, device=dev)
         self.S_out = torch.empty((T, B, Cl), dtype=torch.uint8, device=dev)
         self.trace_out = torch.empty((T, B, self.Np), dtype=torch.float32, device=dev)
+        self._every = None
         return self
 
     def forward(self, b_th: Optional[float] = None):

@@ -142,6 +142,7 @@ class Network(ReadoutRows):
         self.V_out = torch.empty((T, B, C), dtype=torch.float32, device=dev)
         self.S_out = torch.empty((T, B, C), dtype=torch.uint8, device=dev)
         self.trace_out = torch.empty((T, B, sizes[-1]), dtype=torch.float32, device=dev)
+        self.bits, self.bits_bth = [], None  # made by a forward with b_th
         self._every = None
         return self
 

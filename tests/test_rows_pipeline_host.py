@@ -73,3 +73,17 @@ def test_allocate_drops_the_entries(calls, kind):
     net.readout_distilled(pipeline.Distill(_record(3, 2)))
     assert net._every is not None
     assert net.allocate()._every is None
+
+
+def test_allocate_drops_the_active_sets(monkeypatch):
+    """The bitsets of the active sets are as long as the batch: a forward after allocate() for a longer one makes new
+    ones. (Forwards replaced: they are given the bitsets they would write.)"""
+    given = []
+    monkeypatch.setattr(snn, "snn_lif_forward_traces", lambda *a: given.append(a[14].numel()))
+    monkeypatch.setattr(snn, "snn_lif_forward", lambda *a: None)
+    net = _network("dense", 3, 2, 5)
+    for T, B in ((3, 2), (40, 70), (2, 1)):
+        net.X = torch.zeros((T, B, 6), dtype=torch.uint8)
+        net.allocate().forward(0.5)
+        assert given[-1] == snn.snn_active_bits_words(T, B, 4)
+        assert net.bits_bth == 0.5

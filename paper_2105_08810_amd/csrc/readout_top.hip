@@ -136,13 +136,12 @@ __global__ __launch_bounds__(256) void top_short(Top a) {
   }
   if (a.lse) {
     most = row16_reduce(most, Larger());
-    const float safe = isinf(most) ? 0.0f : most;
-    const float c = a.inv * kLog2e, sc = safe * c;
+    const Exponent ex = exponent_of(most, a.inv * kLog2e);
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kShortEach; ++i) {
       if (16 * i >= a.C) break;
-      sum += exp2_fast(fmaf(x[i], c, -sc));
+      sum += exp2_fast(fmaf(x[i], ex.c, -ex.mc));
     }
     sum = row16_reduce(sum, Plus());
     if (live && l == 0) a.lse[r] = isinf(most) ? most : most * a.inv + logf(sum);
@@ -287,7 +286,7 @@ __device__ __forceinline__ bool top_in_registers(const Row<T>& row, const Top& a
   const float m = of_key(high);
   if (odd || isinf(m)) return false;
   const float least = all ? -INFINITY : of_key(bound);
-  const float c = a.inv * kLog2e, mc = m * c;
+  const Exponent ex = exponent_of(m, a.inv * kLog2e);
   float sum = 0.0f;
   uint32_t some = 0;  // the vectors with a value that reaches the bound
   tile.each_unrolled(row, [&](const float (&x)[kVec], int, int n) {
@@ -295,7 +294,7 @@ __device__ __forceinline__ bool top_in_registers(const Row<T>& row, const Top& a
     bool any = false;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      part += exp2_fast(fmaf(x[i], c, -mc));
+      part += exp2_fast(fmaf(x[i], ex.c, -ex.mc));
       any |= x[i] >= least;
     }
     sum += part;
@@ -359,11 +358,11 @@ __global__ __launch_bounds__(kWave) void top_wave(Top a) {
   });
   const float m = of_key(wave_max_u32(key_of(most)));
   if (a.lse) {
-    const float c = a.inv * kLog2e, mc = isinf(m) ? 0.0f : m * c;
+    const Exponent ex = exponent_of(m, a.inv * kLog2e);
     float sum = 0.0f;
     tile.each_unrolled(row, [&](const float (&x)[kVec], int, int) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) sum += exp2_fast(fmaf(no_nan(x[i]), c, -mc));
+      for (int i = 0; i < kVec; ++i) sum += exp2_fast(fmaf(no_nan(x[i]), ex.c, -ex.mc));
     });
     sum = wave_reduce(sum, Plus());
     if (threadIdx.x == 0) a.lse[r] = isinf(m) ? m : m * a.inv + logf(sum);

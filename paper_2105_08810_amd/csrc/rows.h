@@ -240,6 +240,23 @@ struct Tile {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Exponents of 2 relative to a largest value: fmaf(x, c, -mc) of the values x up to it. mc is the largest times c, rounded;
+// 0 where there is nothing but -inf. The rounding, a factor that all of them share, is up to 2^-25 mc: from 2^31 on (masks
+// of the type's lowest value, whose product may overflow as well) it would leave the range of the powers. There any
+// other value lies 2^7 or more below the largest in the exponent, and its power counts for nothing: c is then a power
+// of two, with which the product is exact, equals are at 0 and all others at least 2^6 below.
+struct Exponent {
+  float c, mc;
+};
+__device__ __forceinline__ Exponent exponent_of(float most, float c) {
+  float mc = most * c;
+  if (fabsf(mc) >= 0x1p31f) {
+    if (!isinf(most)) c = ldexpf(1.0f, min(126 - ilogbf(most), 127));
+    mc = most == -INFINITY ? 0.0f : most * c;
+  }
+  return Exponent{c, mc};
+}
+
 // Largest of the wave's values; the steps within 16 lanes and between them are operands of the maximum itself.
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 #define SNN_STEP(ctrl) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, false))

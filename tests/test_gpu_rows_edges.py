@@ -79,3 +79,56 @@ def test_conv_steps_of_two_batch_sizes():
         assert float(got["kd"]) == float(want["kd"]) > 0
         for a, b in zip(got["grads"], want["grads"]):
             assert float((a - b).abs().max()) <= 1e-5 * float(b.abs().max())
+
+
+# ---------------------------------------------------------------- logits at the ends of a type's range
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+ENDS = ["lowest", "one above", "few", "highest", "both", "far"]
+
+
+def _ends(rng, R, C, dtype, kind):
+    """Rows with the type's lowest or highest value, as a mask or an overflow leaves them."""
+    info = torch.finfo(DTYPES[dtype])
+    z = torch.from_numpy((rng.standard_normal((R, C)) * 2).astype(np.float32))
+    if kind in ("lowest", "one above"):
+        z[:] = info.min
+    if kind == "one above":
+        z[:, C // 2] = -1.0
+    if kind == "few":  # some at the lowest value, no other class possible
+        z[:] = -INF
+        z[:, ::max(1, C // 300)] = info.min
+    if kind in ("highest", "both"):
+        z[:, C // 3] = info.max
+        z[:, C - 1] = info.max
+    if kind == "both":
+        z[:, : C // 3] = info.min
+    if kind == "far":  # no end of the range, and yet a product with 1 / tau is rounded by more than a row's sum spans
+        z *= info.max ** 0.3
+    return z.to(DTYPES[dtype]).cuda()
+
+
+# lengths of every kernel: 16 lanes a row, one wave, blocks with rows in registers, few long rows in parts, passes
+END_LENGTHS = [1, 10, 100, 128, 129, 700, 2048, 2049, 5000, 20000, 40000, 70001]
+
+
+@pytest.mark.parametrize("kind", ENDS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C", END_LENGTHS)
+def test_record_at_the_ends_of_the_range(C, dtype, kind):
+    view = _ends(np.random.default_rng(C), 3, C, dtype, kind)
+    z = view.float().cpu().numpy()
+    for tau in (0.5, 1.0, 1.7, 4.0):
+        K = min(C, 6)
+        ids, vals, lse = snn.readout_top(view, K, tau)
+        i, v, _ = rows.top(z, K, tau)
+        assert np.array_equal(ids.cpu().numpy(), i) and np.array_equal(vals.cpu().numpy().astype(np.float64), v)
+        got = lse.cpu().numpy().astype(np.float64)
+        for r in range(len(z)):
+            x = z[r].astype(np.float64)
+            m = x.max()
+            want = m / tau + math.log(np.exp((x - m) / tau).sum())
+            if abs(want) > float(np.finfo(np.float32).max):  # beyond float32
+                assert got[r] == math.copysign(INF, want)
+            else:  # the quotient's two roundings, the sum's additions, a logarithm below log C, the last addition
+                assert abs(got[r] - want) <= U * (4 * abs(m) / tau + 8 * (1 + math.log(C)) + C / 1024 + 86), (r, tau)

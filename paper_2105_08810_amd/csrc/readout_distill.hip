@@ -239,7 +239,7 @@ __global__ __launch_bounds__(16 * ROWS) void distill_small(Distill a) {
     if (a.grad) {
       const Row<T> out(a.grad, r, a.ld_grad, C);
       const float scale = w * inv_tau;
-      const float own_per = scale * s.mass * exp2_fast(or_zero(own.max) - s.base) * s.per;
+      const float own_per = scale * s.mass * exp2_fast(own.max - s.base) * s.per;  // 0 where all of them are -inf
       const float rest_per = scale * s.factor;
       float g[kEach];
 #pragma unroll

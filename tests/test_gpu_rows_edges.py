@@ -132,3 +132,42 @@ def test_record_at_the_ends_of_the_range(C, dtype, kind):
                 assert got[r] == math.copysign(INF, want)
             else:  # the quotient's two roundings, the sum's additions, a logarithm below log C, the last addition
                 assert abs(got[r] - want) <= U * (4 * abs(m) / tau + 8 * (1 + math.log(C)) + C / 1024 + 86), (r, tau)
+
+
+# ---------------------------------------------------------------- distillation where some logits are not finite
+
+# relative rounding of a result to its type, and the spacing of its smallest numbers
+ROUND = {"f32": (2.0 ** -24, 0.0), "bf16": (2.0 ** -8, 2.0 ** -133), "f16": (2.0 ** -11, 2.0 ** -25)}
+# lengths of every kernel: 16 lanes a row, one wave, blocks, rows read twice
+DISTILL_LENGTHS = [3, 20, 100, 300, 1500, 5000, 12000, 30000, 70001, 140003]
+
+
+def _device(*arrays):
+    return [None if a is None else torch.from_numpy(a).cuda() for a in arrays]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C", DISTILL_LENGTHS)
+def test_listed_classes_that_cannot_be_given(C, dtype):
+    """All listed logits are -inf and the others lie far below 0: the listed ones' gradient is -p / tau, the others' the
+    student's share of them."""
+    rng = np.random.default_rng(C)
+    z = rng.standard_normal((4, C)).astype(np.float32) + np.array([[-100.0], [-1000.0], [-30000.0], [0.0]], np.float32)
+    ids = np.stack([rng.choice(C, 2, replace=False) for _ in range(4)]).astype(np.int32)
+    np.put_along_axis(z, ids, -INF, 1)
+    view = torch.from_numpy(z).to(DTYPES[dtype]).cuda()
+    z = view.float().cpu().numpy()
+    vals = rng.standard_normal((4, 2)).astype(np.float32)
+    lse = (2.0 + rng.random(4)).astype(np.float32)
+    for tau, tail in ((1.0, False), (2.0, True)):
+        l = lse if tail else None
+        _, _, want, env, share = rows.distill(z, ids, vals, l, tau)
+        _, row_loss, grad = snn.readout_distill(view, *_device(ids, vals, l), tau)
+        got = grad.double().cpu().numpy()
+        assert bool((row_loss == INF).all())
+        # float32 sums, exponents of size below A formed in a few roundings, and p_t's error by each class's share
+        A = np.array([104.0, 1004.0, 30004.0, 4.0])[:, None] / tau + 4
+        rel = U * (102 + C / 1024 + 6 * A)
+        out, tiny = ROUND[dtype]
+        tol = rel * (env + share / tau) + tiny
+        assert (np.abs(got - want) <= tol + out * (np.abs(want) + tol)).all(), (tau, tail)

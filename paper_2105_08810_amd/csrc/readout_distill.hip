@@ -103,7 +103,7 @@ __device__ __forceinline__ RowSums row_sums(Sum2 rest, Sum2 own, float listed_p,
   s.per = none ? 0.0f : 1.0f / all.total;
   s.mass = listed_p + p_t;
   const float q_t = empty(rest) ? 0.0f : rest.total * exp2_fast(or_zero(rest.max) - s.base) * s.per;
-  s.factor = empty(rest) ? 0.0f : (s.mass * q_t - p_t) * (1.0f / rest.total);
+  s.factor = empty(rest) ? 0.0f * s.per : (s.mass * q_t - p_t) * (1.0f / rest.total);  // NaN with a NaN in either
   const float lse_t = rest.max * kLn2 + logf(rest.total);  // -inf where there is nothing
   const float own_max = own.max * kLn2, top = or_zero(fmaxf(own_max, lse_t));
   s.lse = none ? 0.0f : top + logf(expf(lse_t - top) + own.total * expf(own_max - top));
@@ -501,7 +501,7 @@ __global__ __launch_bounds__(NT, 4) void distill_tile(Distill a) {
   if (!a.grad) return;
   const Row<T> out(a.grad, r, a.ld_grad, a.C);
   const float scale = w / a.tau;
-  const float per = top == -INFINITY ? 0.0f : scale * s.factor * exp2_fast(safe - rest.max);
+  const float per = scale * s.factor * (top == -INFINITY ? 0.0f : exp2_fast(safe - rest.max));
   const auto gradient = [&](const uint4& u, float (&x)[kVec]) {
     if (kKeep) __builtin_memcpy(x, &u, 16);
     else unpack<T>(u, x);

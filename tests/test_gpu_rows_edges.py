@@ -171,3 +171,36 @@ def test_listed_classes_that_cannot_be_given(C, dtype):
         out, tiny = ROUND[dtype]
         tol = rel * (env + share / tau) + tiny
         assert (np.abs(got - want) <= tol + out * (np.abs(want) + tol)).all(), (tau, tail)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C", DISTILL_LENGTHS)
+@pytest.mark.parametrize("what", ["nan", "inf"])
+def test_one_value_makes_the_rows_gradient_nan(C, dtype, what):
+    """A NaN or +inf among finite logits, among masked ones and alone with them, at a listed class and at another: the
+    row's loss and all of its gradient are NaN, the rows beside it are as they are without it."""
+    rng = np.random.default_rng(C + 1)
+    kinds = [(fill, listed) for fill in ("finite", "masked", "others masked") for listed in (False, True)]
+    R = len(kinds) + 1  # the last row stays whole
+    z = rng.standard_normal((R, C)).astype(np.float32)
+    ids = np.stack([rng.choice(C, 2, replace=False) for _ in range(R)]).astype(np.int32)
+    for r, (fill, listed) in enumerate(kinds):
+        other = next(j for j in range(C) if j not in ids[r])
+        if fill == "masked":
+            z[r] = -INF
+        elif fill == "others masked":
+            keep = z[r, ids[r]].copy()
+            z[r] = -INF
+            z[r, ids[r]] = keep
+        z[r, ids[r, 0] if listed else other] = np.nan if what == "nan" else INF
+    view = torch.from_numpy(z).to(DTYPES[dtype]).cuda()
+    vals = rng.standard_normal((R, 2)).astype(np.float32)
+    lse = (2.0 + rng.random(R)).astype(np.float32)
+    for tail in (False, True):
+        for into in (False, True):
+            start = torch.ones((R, C), dtype=DTYPES[dtype], device="cuda") if into else None
+            dev = _device(ids, vals, lse if tail else None)
+            _, row_loss, grad = snn.readout_distill(view, *dev, 1.5, grad=start, accumulate=into)
+            assert bool(row_loss[:-1].isnan().all()) and bool(row_loss[-1:].isfinite().all())
+            assert bool(grad[:-1].isnan().all()) and bool(grad[-1:].isfinite().all())
+            assert bool(row_loss[-1] == snn.readout_distill(view[-1:], *(None if t is None else t[-1:] for t in dev), 1.5)[1][0])

@@ -20,6 +20,12 @@ def log_sum_exp(x: np.ndarray) -> float:
     return float(m + np.log(np.sum(np.exp(x - m))))
 
 
+def from_largest(x: np.ndarray) -> np.ndarray:
+    """What a softmax does not see taken away: beside a type's lowest value even 64 bits keep nothing of a logarithm."""
+    m = np.max(x) if x.size else -np.inf
+    return x - m if np.isfinite(m) else x
+
+
 def order(z: np.ndarray) -> np.ndarray:
     """Classes by logit, largest first, equal ones by class; NaN as -inf."""
     z = np.where(np.isnan(z), -np.inf, z)
@@ -43,11 +49,13 @@ def distill_row(z, ids, vals, lse, tau):
     """(loss, gradient, envelope, share) of one row; lse None: the entries are all of the teacher. The envelope is the
     gradient's formula with its terms in absolute value, share the student's distribution among the classes not listed."""
     C = len(z)
-    z = z.astype(np.float64) / tau
+    z = z.astype(np.float64)
     if np.isnan(z).any() or (z == np.inf).any():
         return np.nan, np.full(C, np.nan), np.full(C, np.nan), np.zeros(C)
+    of, z = z, from_largest(z) / tau
     ok = (ids >= 0) & (ids < C)
-    k, v = ids[ok], vals[ok].astype(np.float64) / tau
+    k, v = ids[ok], vals[ok].astype(np.float64)
+    v = (from_largest(v) if lse is None else v) / tau
     whole = log_sum_exp(z)
     q = np.exp(z - whole) if whole > -np.inf else np.zeros(C)
     logq = z - whole if whole > -np.inf else np.full(C, -np.inf)
@@ -66,7 +74,8 @@ def distill_row(z, ids, vals, lse, tau):
         loss += p_t * (math.log(p_t) - logq_t)
     share = np.zeros(C)
     if logq_t > -np.inf:
-        share[other] = np.exp(logq[other] - logq_t)
+        e = np.exp(from_largest(of[other]) / tau)
+        share[other] = e / e.sum()
     target = p_t * share
     target[k] = p
     return loss, (mass * q - target) / tau, (mass * q + target) / tau, share

@@ -28,27 +28,30 @@ using namespace rows;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
-// A sum of 2^x kept as total * 2^max.
+// A sum of exp(x / tau) over some logits x: the largest of them, and the sum relative to it. Logits are subtracted before
+// they are scaled by c = log2(e) / tau: the product of one could overflow (masks of the type's lowest value), and its
+// rounding be more than a row's logits span.
 struct Sum2 {
   float max, total;
 };
 __device__ __forceinline__ float or_zero(float m) { return m == -INFINITY ? 0.0f : m; }
-__device__ __forceinline__ Sum2 join(Sum2 a, Sum2 b) {
+__device__ __forceinline__ float power(float x, float from, float c) { return exp2_fast((x - from) * c); }
+__device__ __forceinline__ Sum2 join(Sum2 a, Sum2 b, float c) {
   const float m = fmaxf(a.max, b.max);
   const float safe = or_zero(m);
-  return Sum2{m, a.total * exp2_fast(a.max - safe) + b.total * exp2_fast(b.max - safe)};
+  return Sum2{m, a.total * power(a.max, safe, c) + b.total * power(b.max, safe, c)};
 }
 __device__ __forceinline__ bool empty(Sum2 a) { return a.max == -INFINITY && a.total == 0.0f; }
 
 // One maximum and one rescaled sum for the wave (a join at each step would form two exponentials).
-__device__ __forceinline__ Sum2 wave_join(Sum2 v) {
+__device__ __forceinline__ Sum2 wave_join(Sum2 v, float c) {
   const float m = wave_reduce(v.max, Larger());
-  return Sum2{m, wave_reduce(v.total * exp2_fast(v.max - or_zero(m)), Plus())};
+  return Sum2{m, wave_reduce(v.total * power(v.max, or_zero(m), c), Plus())};
 }
 
 template <int NT>
-__device__ __forceinline__ Sum2 block_join(Sum2 v, Sum2* red) {
-  v = wave_join(v);
+__device__ __forceinline__ Sum2 block_join(Sum2 v, float c, Sum2* red) {
+  v = wave_join(v, c);
   if (NT == kWave) return v;
   if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
   __syncthreads();
@@ -57,7 +60,7 @@ __device__ __forceinline__ Sum2 block_join(Sum2 v, Sum2* red) {
   for (int k = 1; k < NT / kWave; ++k) m = fmaxf(m, red[k].max);
   float total = 0.0f;
 #pragma unroll
-  for (int k = 0; k < NT / kWave; ++k) total += red[k].total * exp2_fast(red[k].max - or_zero(m));
+  for (int k = 0; k < NT / kWave; ++k) total += red[k].total * power(red[k].max, or_zero(m), c);
   return Sum2{m, total};
 }
 
@@ -85,27 +88,39 @@ struct Distill {
   __device__ __forceinline__ float weight_of(int64_t r) const { return weight ? weight[r] : 1.0f / (float)R; }
 };
 
+// (x - from) / tau, rounded by itself: not contracted with what it is added to.
+__device__ __forceinline__ float over_tau(float x, float from, float inv_tau) {
+#pragma clang fp contract(off)
+  return (x - from) * inv_tau;
+}
+// What logarithms are relative to where the largest value is `top`: beside a number far from 0 float32 keeps too little of
+// a sum's logarithm, and beside a type's lowest value nothing.
+__device__ __forceinline__ float far_from_zero(float top, float inv_tau) {
+  return fabsf(top * inv_tau) < 1024.0f || isinf(top) ? 0.0f : top;
+}
+
 // What a row's loss and gradient need of its sums.
 struct RowSums {
   float loss;
-  float lse;         // log q_j = z_j / tau - lse; 0 for a row with nothing in it, whose z are all -inf
-  float base, per;   // q_j = 2^(z_j c - base) per
+  float from, lse;   // log q_j = (z_j - from) / tau - lse; 0 for a row with nothing in it, whose z are all -inf
+  float max, per;    // q_j = 2^((z_j - max) c) per
   float mass;
-  float factor;      // of 2^(z_j c - rest.max) for a class that is not listed, without weight / tau
+  float factor;      // of 2^((z_j - rest.max) c) for a class that is not listed, without weight / tau
 };
 // The loss is that of the classes not listed; the caller adds the others' terms. Logarithms are differences of float32
 // log-sum-exps, so a loss is exact to about 2^-23 |lse|; the gradient takes ratios of sums.
-__device__ __forceinline__ RowSums row_sums(Sum2 rest, Sum2 own, float listed_p, float p_t) {
+__device__ __forceinline__ RowSums row_sums(Sum2 rest, Sum2 own, float listed_p, float p_t, float c, float inv_tau) {
   RowSums s;
-  const Sum2 all = join(rest, own);
+  const Sum2 all = join(rest, own, c);
   const bool none = empty(all);  // q = 0
-  s.base = or_zero(all.max);
+  s.max = or_zero(all.max);
   s.per = none ? 0.0f : 1.0f / all.total;
   s.mass = listed_p + p_t;
-  const float q_t = empty(rest) ? 0.0f : rest.total * exp2_fast(or_zero(rest.max) - s.base) * s.per;
+  const float q_t = empty(rest) ? 0.0f : rest.total * power(rest.max, s.max, c) * s.per;
   s.factor = empty(rest) ? 0.0f * s.per : (s.mass * q_t - p_t) * (1.0f / rest.total);  // NaN with a NaN in either
-  const float lse_t = rest.max * kLn2 + logf(rest.total);  // -inf where there is nothing
-  const float own_max = own.max * kLn2, top = or_zero(fmaxf(own_max, lse_t));
+  s.from = far_from_zero(all.max, inv_tau);
+  const float lse_t = over_tau(rest.max, s.from, inv_tau) + logf(rest.total);  // -inf where there is nothing
+  const float own_max = over_tau(own.max, s.from, inv_tau), top = or_zero(fmaxf(own_max, lse_t));
   s.lse = none ? 0.0f : top + logf(expf(lse_t - top) + own.total * expf(own_max - top));
   s.loss = p_t > 0.0f ? p_t * (logf(p_t) - (lse_t - s.lse)) : s.lse == s.lse ? 0.0f : s.lse;
   return s;
@@ -125,13 +140,14 @@ struct Small {
   static constexpr int kValues = 16 * kEach;
 };
 
-constexpr int kNotListed = 0x7fffffff;   // a NaN that no operation gives
+constexpr int kNotListed = 0x7fffffff;  // a NaN that no listed value has
+__device__ __forceinline__ int listed_bits(float v) { return __float_as_int(v == v ? v : NAN); }
 
 template <class T, int ROWS>
 __global__ __launch_bounds__(16 * ROWS) void distill_small(Distill a) {
   using S = Small<T>;
   constexpr int kVec = S::kVec, kEach = S::kEach, NV = S::NV;
-  __shared__ __attribute__((aligned(16))) int table[ROWS][S::kValues];  // log p of the listed values
+  __shared__ __attribute__((aligned(16))) int table[ROWS][S::kValues];  // the listed values
   __shared__ double part[ROWS];
   const int slot = threadIdx.x / 16, l = threadIdx.x % 16;
   const int64_t r = (int64_t)blockIdx.x * ROWS + slot;
@@ -161,10 +177,10 @@ __global__ __launch_bounds__(16 * ROWS) void distill_small(Distill a) {
   __syncthreads();
   const float inv_tau = 1.0f / a.tau;
   if (live) {
-    if (id0 >= 0 && id0 < C) table[slot][row.lead + id0] = __float_as_int(v0 * inv_tau);
+    if (id0 >= 0 && id0 < C) table[slot][row.lead + id0] = listed_bits(v0);
     for (int k = l + 16; k < K; k += 16) {
       const int id = a.ids[r * K + k];
-      if (id >= 0 && id < C) table[slot][row.lead + id] = __float_as_int(a.vals[r * K + k] * inv_tau);
+      if (id >= 0 && id < C) table[slot][row.lead + id] = listed_bits(a.vals[r * K + k]);
     }
   }
   __syncthreads();
@@ -192,13 +208,20 @@ __global__ __launch_bounds__(16 * ROWS) void distill_small(Distill a) {
     float shift;
     if (a.lse) {
       shift = lse;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) lp[i] = over_tau(lp[i], 0.0f, inv_tau);
     } else {
       float top = lp[0], z = 0.0f;
 #pragma unroll
       for (int i = 1; i < kEach; ++i) top = fmaxf(top, lp[i]);
-      top = or_zero(row16_reduce(top, Larger()));
+      top = row16_reduce(top, Larger());
+      const float from = far_from_zero(top, inv_tau);
+      top = or_zero(over_tau(top, from, inv_tau));
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) z += exp2_fast((lp[i] - top) * kLog2e);
+      for (int i = 0; i < kEach; ++i) {
+        lp[i] = over_tau(lp[i], from, inv_tau);
+        z += exp2_fast((lp[i] - top) * kLog2e);
+      }
       z = row16_reduce(z, Plus());
       shift = z == 0.0f ? 0.0f : top + logf(z);
     }
@@ -217,29 +240,29 @@ __global__ __launch_bounds__(16 * ROWS) void distill_small(Distill a) {
     Sum2 rest{-INFINITY, 0.0f}, own{-INFINITY, 0.0f};
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      rest.max = fmaxf(rest.max, listed[i] ? -INFINITY : x[i] * c);
-      own.max = fmaxf(own.max, listed[i] ? x[i] * c : -INFINITY);
+      rest.max = fmaxf(rest.max, listed[i] ? -INFINITY : x[i]);
+      own.max = fmaxf(own.max, listed[i] ? x[i] : -INFINITY);
     }
     rest.max = row16_reduce(rest.max, Larger());
     own.max = row16_reduce(own.max, Larger());
     float e[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      e[i] = exp2_fast(fmaf(x[i], c, -or_zero(listed[i] ? own.max : rest.max)));
+      e[i] = power(x[i], or_zero(listed[i] ? own.max : rest.max), c);
       rest.total += listed[i] ? 0.0f : e[i];
       own.total += listed[i] ? e[i] : 0.0f;
     }
     rest.total = row16_reduce(rest.total, Plus());
     own.total = row16_reduce(own.total, Plus());
-    const RowSums s = row_sums(rest, own, listed_p, p_t);
+    const RowSums s = row_sums(rest, own, listed_p, p_t, c, inv_tau);
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-      if (listed[i] && !(p[i] <= 0.0f)) loss += p[i] * (lp[i] - (x[i] * inv_tau - s.lse));
+      if (listed[i] && !(p[i] <= 0.0f)) loss += p[i] * (lp[i] - (over_tau(x[i], s.from, inv_tau) - s.lse));
     loss = row16_reduce(loss, Plus()) + s.loss;
     if (a.grad) {
       const Row<T> out(a.grad, r, a.ld_grad, C);
       const float scale = w * inv_tau;
-      const float own_per = scale * s.mass * exp2_fast(own.max - s.base) * s.per;  // 0 where all of them are -inf
+      const float own_per = scale * s.mass * power(own.max, s.max, c) * s.per;  // 0 where all of them are -inf
       const float rest_per = scale * s.factor;
       float g[kEach];
 #pragma unroll
@@ -288,7 +311,7 @@ struct Entries {
   const int32_t* ids;
   const float* vals;
   int K, C;
-  float held_v[kHeld];  // v / tau
+  float held_v[kHeld];
   float x[kHeld];
   int id[kHeld];            // -1: no entry
   float inv_tau;
@@ -306,10 +329,9 @@ struct Entries {
     for (int e = 0; e < kHeld; ++e) {
       if (id[e] >= C) id[e] = -1;
       x[e] = id[e] >= 0 ? row.at(id[e]) : 0.0f;
-      held_v[e] *= inv_tau;
     }
   }
-  // f(id, v / tau, student's logit) of the lane's entries
+  // f(id, v, student's logit) of the lane's entries
   template <class F>
   __device__ __forceinline__ void each(F f) const {
 #pragma unroll
@@ -317,13 +339,15 @@ struct Entries {
       if (id[e] >= 0) f(id[e], held_v[e], x[e]);
     for (int k = threadIdx.x % kWave + kHeld * kWave; k < K; k += kWave) {
       const int j = ids[k];
-      if (j >= 0 && j < C) f(j, vals[k] * inv_tau, row.at(j));
+      if (j >= 0 && j < C) f(j, vals[k], row.at(j));
     }
   }
 };
 
 struct Teacher {
-  float shift, listed_p, p_t;
+  float from, shift, inv_tau;
+  float listed_p, p_t;
+  __device__ __forceinline__ float log_p(float v) const { return over_tau(v, from, inv_tau) - shift; }
 };
 // Also sets the listed classes' bits (by the first wave).
 template <class T>
@@ -334,19 +358,23 @@ __device__ __forceinline__ Teacher teacher_of(const Distill& a, int64_t r, const
       atomicOr(&bits[v >> 5], 1u << (v & 31));
     });
   Teacher t;
+  t.from = 0.0f;
+  t.inv_tau = entries.inv_tau;
   if (a.lse) {
     t.shift = a.lse[r];
   } else {
     float top = -INFINITY, z = 0.0f;
     entries.each([&](int, float v, float) { top = fmaxf(top, v); });
-    top = or_zero(wave_reduce(top, Larger()));
-    entries.each([&](int, float v, float) { z += expf(v - top); });
+    top = wave_reduce(top, Larger());
+    t.from = far_from_zero(top, t.inv_tau);
+    top = or_zero(over_tau(top, t.from, t.inv_tau));
+    entries.each([&](int, float v, float) { z += expf(over_tau(v, t.from, t.inv_tau) - top); });
     z = wave_reduce(z, Plus());
     t.shift = z == 0.0f ? 0.0f : top + logf(z);
   }
   float p = 0.0f, n = 0.0f;
   entries.each([&](int, float v, float) {
-    p += expf(v - t.shift);
+    p += expf(t.log_p(v));
     n += 1.0f;
   });
   t.listed_p = wave_reduce(p, Plus());
@@ -359,14 +387,14 @@ __device__ __forceinline__ Teacher teacher_of(const Distill& a, int64_t r, const
 template <class T>
 __device__ __forceinline__ RowSums finish_row(const Entries<T>& entries, const Teacher& t, Sum2 rest, float c) {
   float top = -INFINITY, z = 0.0f;
-  entries.each([&](int, float, float x) { top = fmaxf(top, x * c); });
+  entries.each([&](int, float, float x) { top = fmaxf(top, x); });
   top = wave_reduce(top, Larger());
-  entries.each([&](int, float, float x) { z += exp2_fast(fmaf(x, c, -or_zero(top))); });
-  RowSums s = row_sums(rest, Sum2{top, wave_reduce(z, Plus())}, t.listed_p, t.p_t);
+  entries.each([&](int, float, float x) { z += power(x, or_zero(top), c); });
+  RowSums s = row_sums(rest, Sum2{top, wave_reduce(z, Plus())}, t.listed_p, t.p_t, c, t.inv_tau);
   float loss = 0.0f;
   entries.each([&](int, float v, float x) {
-    const float lp = v - t.shift, p = expf(lp);
-    if (!(p <= 0.0f)) loss += p * (lp - (x * entries.inv_tau - s.lse));
+    const float lp = t.log_p(v), p = expf(lp);
+    if (!(p <= 0.0f)) loss += p * (lp - (over_tau(x, s.from, t.inv_tau) - s.lse));
   });
   s.loss += wave_reduce(loss, Plus());
   return s;
@@ -380,8 +408,8 @@ __device__ __forceinline__ void listed_grads(const Distill& a, int64_t r, const 
   __syncthreads();
   if (threadIdx.x < kWave)
     entries.each([&](int id, float v, float x) {
-      const float q = exp2_fast(fmaf(x, c, -s.base)) * s.per;
-      const float g = scale * (s.mass * q - expf(v - t.shift));
+      const float q = power(x, s.max, c) * s.per;
+      const float g = scale * (s.mass * q - expf(t.log_p(v)));
       grad[id] = from_float<T>(a.accumulate ? to_float(grad[id]) + g : g);
     });
 }
@@ -477,8 +505,9 @@ __global__ __launch_bounds__(NT, 4) void distill_tile(Distill a) {
     for (int k = 0; k < kVec; ++k) top = fmaxf(top, x[k]);
     if (!kKeep) forget(raw[i]);
   }
-  top *= c;
-  const float safe = or_zero(top);
+  // one multiply-add a value, and the rounding of what the exponents are relative to as a factor of the thread's sum
+  const Exponent at = exponent_of(top, c);
+  const float exact = top == -INFINITY ? 1.0f : exp2_fast(-fmaf(top, at.c, -at.mc));
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -486,13 +515,13 @@ __global__ __launch_bounds__(NT, 4) void distill_tile(Distill a) {
     unpack<T>(raw[i], x);
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      x[k] = exp2_fast(fmaf(x[k], c, -safe));
+      x[k] = exp2_fast(fmaf(x[k], at.c, -at.mc));
       sum += x[k];
     }
     if (kKeep) __builtin_memcpy(&raw[i], x, 16);
     else forget(raw[i]);
   }
-  const Sum2 rest = block_join<NT>(Sum2{top, sum}, red);
+  const Sum2 rest = block_join<NT>(Sum2{top, sum * exact}, c, red);
   const RowSums s = finish_row<T>(entries, t, rest, c);
   if (tid == 0) {
     if (a.row_loss) a.row_loss[r] = s.loss;
@@ -501,12 +530,12 @@ __global__ __launch_bounds__(NT, 4) void distill_tile(Distill a) {
   if (!a.grad) return;
   const Row<T> out(a.grad, r, a.ld_grad, a.C);
   const float scale = w / a.tau;
-  const float per = scale * s.factor * (top == -INFINITY ? 0.0f : exp2_fast(safe - rest.max));
+  const float per = scale * s.factor * (top == -INFINITY ? 0.0f : exact * power(top, rest.max, c));
   const auto gradient = [&](const uint4& u, float (&x)[kVec]) {
     if (kKeep) __builtin_memcpy(x, &u, 16);
     else unpack<T>(u, x);
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) x[k] = kKeep ? x[k] * per : exp2_fast(fmaf(x[k], c, -safe)) * per;
+    for (int k = 0; k < kVec; ++k) x[k] = kKeep ? x[k] * per : exp2_fast(fmaf(x[k], at.c, -at.mc)) * per;
   };
   const bool alike = out.lead == row.lead && !a.accumulate;
   const int from = out.lead ? 1 : 0, to = (out.lead + a.C) / kVec;  // whole vectors
@@ -594,14 +623,14 @@ __global__ __launch_bounds__(NT) void distill_rows(Distill a) {
     float m = x[0];
 #pragma unroll
     for (int k = 1; k < kVec; ++k) m = fmaxf(m, x[k]);
-    m = fmaxf(rest.max, m * c);
+    m = fmaxf(rest.max, m);
     const float safe = or_zero(m);
-    float v = rest.total * exp2_fast(rest.max - safe);
+    float v = rest.total * power(rest.max, safe, c);
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) v += exp2_fast(fmaf(x[k], c, -safe));
+    for (int k = 0; k < kVec; ++k) v += power(x[k], safe, c);
     rest = Sum2{m, v};
   });
-  rest = block_join<NT>(rest, red);
+  rest = block_join<NT>(rest, c, red);
   const RowSums s = finish_row<T>(entries, t, rest, c);
   if (tid == 0) {
     if (a.row_loss) a.row_loss[r] = s.loss;
@@ -613,7 +642,7 @@ __global__ __launch_bounds__(NT) void distill_rows(Distill a) {
   const float per = scale * s.factor, safe = or_zero(rest.max);
   pass(true, [&](float (&x)[kVec], int q) {  // from the end, which was read last
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) x[k] = exp2_fast(fmaf(x[k], c, -safe)) * per;
+    for (int k = 0; k < kVec; ++k) x[k] = power(x[k], safe, c) * per;
     put(a, row, out, q, x);
   });
   listed_grads<T>(a, r, entries, t, s, c, scale);

@@ -248,9 +248,10 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 struct Exponent {
   float c, mc;
 };
+constexpr float kFarExponent = 0x1p31f;
 __device__ __forceinline__ Exponent exponent_of(float most, float c) {
   float mc = most * c;
-  if (fabsf(mc) >= 0x1p31f) {
+  if (fabsf(mc) >= kFarExponent) {
     if (!isinf(most)) c = ldexpf(1.0f, min(126 - ilogbf(most), 127));
     mc = most == -INFINITY ? 0.0f : most * c;
   }

@@ -204,3 +204,72 @@ def test_one_value_makes_the_rows_gradient_nan(C, dtype, what):
             assert bool(row_loss[:-1].isnan().all()) and bool(row_loss[-1:].isfinite().all())
             assert bool(grad[:-1].isnan().all()) and bool(grad[-1:].isfinite().all())
             assert bool(row_loss[-1] == snn.readout_distill(view[-1:], *(None if t is None else t[-1:] for t in dev), 1.5)[1][0])
+
+
+def _ends_of_distill(rng, C, info):
+    """Rows at and near the ends of a type's range, by name, with the classes that are listed."""
+    far = float(info.max) ** 0.3
+    k = rng.choice(C, 2, replace=False)
+    plain = rng.standard_normal(C).astype(np.float32)
+    out = {}
+    for name, mask in (("lowest", info.min), ("masked", max(-1e9, info.min)), ("far", -far)):
+        z = np.full(C, mask, np.float32)
+        out[name] = z, k
+        out[name + ", listed not"] = np.where(np.isin(np.arange(C), k), plain, z), k
+        out[name + " listed"] = np.where(np.isin(np.arange(C), k), z, plain), k
+        z = z.copy()
+        z[[j for j in range(C) if j not in k][0]] = 0.5
+        out[name + ", one not"] = z, k
+    z = plain.copy()
+    z[k[0]] = info.max
+    out["highest listed"] = z, k
+    z = plain.copy()
+    z[[j for j in range(C) if j not in k][0]] = info.max
+    out["highest"] = z, k
+    out["all far"] = (plain * far).astype(np.float32), k
+    out["shifted"] = (plain + 2000.0).astype(np.float32), k
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C", DISTILL_LENGTHS)
+def test_distill_at_the_ends_of_the_range(C, dtype):
+    rng = np.random.default_rng(C + 2)
+    cases = _ends_of_distill(rng, C, torch.finfo(DTYPES[dtype]))
+    names = list(cases)
+    view = torch.from_numpy(np.stack([cases[n][0] for n in names])).to(DTYPES[dtype]).cuda()
+    ids = np.stack([cases[n][1] for n in names]).astype(np.int32)
+    z = view.float().cpu().numpy()
+    R = len(names)
+    vals = rng.standard_normal((R, 2)).astype(np.float32)
+    lse = (2.0 + rng.random(R)).astype(np.float32)
+    lowest = np.full((R, 2), np.finfo(np.float32).min, np.float32)  # a teacher's row at the lowest value
+    for tau, v, l in ((1.0, vals, lse), (2.5, vals, None), (1.0, lowest, None), (1.0, vals - np.float32(1e7), None)):
+        _, row_loss, grad = snn.readout_distill(view, *_device(ids, v, l), tau)
+        got_l, got = row_loss.double().cpu().numpy(), grad.double().cpu().numpy()
+        with np.errstate(over="ignore"):
+            _, want_l, want, env, share = rows.distill(z, ids, v, l, tau)
+        for r in range(R):
+            x = z[r].astype(np.float64) / tau
+            m = x.max()
+            logq = x - m - math.log(np.exp(x - m).sum())
+            logp = v[r].astype(np.float64) / tau
+            logp = logp - l[r] if l is not None else logp - logp.max() - math.log(np.exp(logp - logp.max()).sum())
+            p = np.exp(logp)
+            other = np.ones(C, bool)
+            other[ids[r]] = False
+            logq_t = logq[other].max() + math.log(np.exp(logq[other] - logq[other].max()).sum())
+            p_t = max(0.0, 1 - p.sum()) if l is not None else 0.0
+            terms = (p * (np.abs(logp) + np.abs(logq[ids[r]]))).sum() + (p_t * (abs(math.log(p_t)) + abs(logq_t)) if p_t else 0)
+            # float32 sums, exponents and logarithms of numbers of size A in a few roundings; p_t = 1 - sum p
+            A = (abs(m) if abs(m) < 1024 else 0) + np.abs(logp).max() + (np.abs(v[r]).max() / tau if np.abs(v[r]).max() < 1024 else 0)
+            rel = U * (102 + C / 1024 + 8 * A)
+            tol = rel * (1 + terms) + (rel * (abs(logq_t) + abs(math.log(p_t)) + 1) if p_t else 0)
+            if abs(want_l[r]) > np.finfo(np.float32).max:
+                assert got_l[r] == INF, names[r]
+            else:
+                assert abs(got_l[r] - want_l[r]) <= tol, (names[r], tau, got_l[r], want_l[r])
+            out, tiny = ROUND[dtype]
+            tol = rel * (env[r] + 4 * share[r] * (l is not None) / (R * tau)) + tiny + 2.0 ** -126
+            bad = ~(np.abs(got[r] - want[r]) <= tol + out * (np.abs(want[r]) + tol))
+            assert not bad.any(), (names[r], tau, np.flatnonzero(bad)[:4], got[r][bad][:4], want[r][bad][:4])

@@ -78,3 +78,25 @@ def test_sample_filters():
     want = [0] * 4 + [1] * 2 + [2] + [3] + [4] * 8
     e = np.array([0.5, 0.25, 0.125, 0.125, 1.0], np.float32)
     assert [rows.sample_row(z, e, (i + 0.5) / 16)[0] for i in range(16)] == want
+
+
+def test_distill_does_not_see_a_common_shift():
+    """A row and a teacher without a log-sum-exp shifted by a number that their logits are small beside."""
+    rng = np.random.default_rng(4)
+    z, ids, vals = np.round(rng.normal(size=9) * 64) / 64, np.array([5, 0, 7]), np.round(rng.normal(size=3) * 64) / 64
+    want = rows.distill_row(z, ids, vals, None, 1.5)
+    for by in (1024.0, -2.0 ** 40):
+        for got in (rows.distill_row(z + by, ids, vals, None, 1.5), rows.distill_row(z, ids, vals + by, None, 1.5)):
+            assert got[0] == pytest.approx(want[0], rel=1e-12) and np.allclose(got[1], want[1], rtol=1e-12, atol=1e-15)
+    lowest = float(np.finfo(np.float32).min)
+    loss, g, _, _ = rows.distill_row(np.full(4, lowest), np.array([1]), np.array([0.3]), None, 1.0)
+    assert loss == pytest.approx(math.log(4)) and np.allclose(g, [0.25, -0.75, 0.25, 0.25])
+    loss, g, _, _ = rows.distill_row(np.zeros(4), np.array([1, 2]), np.full(2, lowest), None, 1.0)
+    assert loss == pytest.approx(math.log(2)) and np.allclose(g, [0.25, -0.25, -0.25, 0.25])
+    z = np.array([0.5, lowest, lowest, lowest, 1.0])  # the classes not listed, all at the lowest value, share alike
+    _, g, _, share = rows.distill_row(z, np.array([0, 4]), np.array([0.0, 0.0]), 2.0, 1.0)
+    p_t = 1 - 2 * math.exp(-2)
+    assert np.allclose(share, [0, 1 / 3, 1 / 3, 1 / 3, 0]) and np.allclose(g[1:4], -p_t / 3)
+    z = np.array([0.5, 1.0, -lowest])  # beside the highest value too
+    _, g, _, share = rows.distill_row(z, np.array([2]), np.array([0.0]), 2.0, 1.0)
+    assert np.allclose(share[:2], np.exp([0.5, 1.0]) / np.exp([0.5, 1.0]).sum())

@@ -74,18 +74,19 @@ struct Distill {
   int K;
   float tau;
   const float* weight;
-  int64_t R;
+  float mean;  // every row's weight where there is no array of them
+  int64_t R;   // rows of this launch
   float* row_loss;
   void* grad;
   int64_t ld_grad;
   int accumulate;
-  double* part;  // a block's sum of weight * loss
-  float* loss;   // their sum where there is one block
+  double* part;  // a block's sum of weight * loss; NULL where there is one block, which writes the loss
+  float* loss;
   __device__ __forceinline__ void add(int64_t block, double v) const {
-    if (gridDim.x == 1) *loss = (float)v;
+    if (!part) *loss = (float)v;
     else part[block] = v;
   }
-  __device__ __forceinline__ float weight_of(int64_t r) const { return weight ? weight[r] : 1.0f / (float)R; }
+  __device__ __forceinline__ float weight_of(int64_t r) const { return weight ? weight[r] : mean; }
 };
 
 // (x - from) / tau, rounded by itself: not contracted with what it is added to.
@@ -696,41 +697,45 @@ extern "C" snn_status snn_readout_distill(const void* logits, int dtype, int64_t
   Carve ws(workspace);
   double* part = ws.take<double>((size_t)R);
   double* sums = ws.take<double>((size_t)((R + kTotalEach - 1) / kTotalEach));
-  const Distill a{logits, C, ld, ids, vals, lse, K, tau, weight, R, row_loss, grad, ld_grad, accumulate, part, loss};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const dim3 grid((unsigned)R);
-  int64_t n = R;
+  int64_t n = R;  // blocks, each with a part of the loss
   const snn_status launched = rows::for_type(dtype, [&](auto type) {
     using T = decltype(type);
     constexpr int kWide = sizeof(T) == 4 ? 16 : 8;  // 64 values of a thread in registers
     const int Q = rows::most_vectors<T>(logits, C, ld);
-    const bool many = R >= 2 * cu_count();
-    if (Q <= 16 * Small<T>::NV) {
-      if (R <= 64) {  // one block, and no launch for the loss
-        n = 1;
-        hipLaunchKernelGGL((distill_small<T, 64>), dim3(1), dim3(1024), 0, s, a);
+    const bool many = R >= 2 * cu_count(), small = Q <= 16 * Small<T>::NV;
+    if (small) n = R <= 64 ? 1 : (R + 15) / 16;
+    return rows::in_launches(R, [&](int64_t first, int64_t count) {
+      using rows::or_null;
+      const Distill a{static_cast<const T*>(logits) + first * ld, C, ld, ids + first * K, vals + first * K,
+                      or_null(lse, first), K, tau, or_null(weight, first), 1.0f / (float)R, count, or_null(row_loss, first),
+                      or_null(static_cast<T*>(grad), first * ld_grad), ld_grad, accumulate,
+                      n == 1 ? nullptr : part + (small ? first / 16 : first), loss};
+      const dim3 grid((unsigned)count);
+      if (small) {
+        if (n == 1)  // and no launch for the loss
+          hipLaunchKernelGGL((distill_small<T, 64>), dim3(1), dim3(1024), 0, s, a);
+        else
+          hipLaunchKernelGGL((distill_small<T, 16>), dim3((unsigned)((count + 15) / 16)), dim3(256), 0, s, a);
+      } else if (Q <= 4 * 64) {
+        hipLaunchKernelGGL((distill_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
+      } else if (Q <= 4 * 256) {
+        hipLaunchKernelGGL((distill_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
+      } else if (Q <= kWide * 256 && many) {
+        hipLaunchKernelGGL((distill_tile<T, 256, kWide>), grid, dim3(256), 0, s, a);
+      } else if (Q <= kWide * 512 && many) {
+        hipLaunchKernelGGL((distill_tile<T, 512, kWide>), grid, dim3(512), 0, s, a);
+      } else if (Q <= 4 * 1024) {
+        hipLaunchKernelGGL((distill_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
+      } else if (Q <= kWide * 1024) {
+        hipLaunchKernelGGL((distill_tile<T, 1024, kWide>), grid, dim3(1024), 0, s, a);
       } else {
-        n = (R + 15) / 16;
-        hipLaunchKernelGGL((distill_small<T, 16>), dim3((unsigned)n), dim3(256), 0, s, a);
+        const size_t lds = ((size_t)Q * Row<T>::kVec + 31) / 32 * 4;
+        ensure_dynamic_lds((const void*)distill_rows<T, 1024>, (int)lds);
+        hipLaunchKernelGGL((distill_rows<T, 1024>), grid, dim3(1024), lds, s, a);
       }
-    } else if (Q <= 4 * 64) {
-      hipLaunchKernelGGL((distill_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
-    } else if (Q <= 4 * 256) {
-      hipLaunchKernelGGL((distill_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
-    } else if (Q <= kWide * 256 && many) {
-      hipLaunchKernelGGL((distill_tile<T, 256, kWide>), grid, dim3(256), 0, s, a);
-    } else if (Q <= kWide * 512 && many) {
-      hipLaunchKernelGGL((distill_tile<T, 512, kWide>), grid, dim3(512), 0, s, a);
-    } else if (Q <= 4 * 1024) {
-      hipLaunchKernelGGL((distill_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
-    } else if (Q <= kWide * 1024) {
-      hipLaunchKernelGGL((distill_tile<T, 1024, kWide>), grid, dim3(1024), 0, s, a);
-    } else {
-      const size_t lds = ((size_t)Q * Row<T>::kVec + 31) / 32 * 4;
-      ensure_dynamic_lds((const void*)distill_rows<T, 1024>, (int)lds);
-      hipLaunchKernelGGL((distill_rows<T, 1024>), grid, dim3(1024), lds, s, a);
-    }
-    return launch_status();
+      return launch_status();
+    });
   });
   if (launched != SNN_OK || n == 1) return launched;
   if (n > kTotalEach) {

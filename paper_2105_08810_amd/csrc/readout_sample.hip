@@ -1154,38 +1154,44 @@ extern "C" snn_status snn_readout_sample(const void* logits, int dtype, int64_t 
   if (!u || !cls) return SNN_ERR_INVALID_ARG;
   const size_t need = snn_readout_sample_workspace(R, C, dtype);
   if (need && (!workspace || workspace_bytes < need)) return SNN_ERR_INVALID_ARG;
-  const Sample a{logits, R, C, ld, Settings{u, temperature, top_k, top_p, min_p}, cls, logp, kept};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const dim3 grid((unsigned)R);
   return rows::for_type(dtype, [&](auto type) {
     using T = decltype(type);
     const int Q = rows::most_vectors<T>(logits, C, ld);
-    if (C <= rows::kShortRow && (C <= 32 || R > cu_count()))
-      hipLaunchKernelGGL((sample_short<T>), dim3((unsigned)((R + rows::kShortRows - 1) / rows::kShortRows)), dim3(256),
-                         0, s, a);
-    // up to 32 values a lane: one wave, without barriers (in a block of 256 that lists and orders what is kept 23265 rows
-    // of 590 bfloat16 with top-k 50 took 492 us, 110 so; one row of 1000 float32 14 and 10)
-    else if (Q <= rows::kWaveVectors<T> * kWave)
-      hipLaunchKernelGGL((sample_tile<T, kWave, rows::kWaveVectors<T>>), grid, dim3(kWave), 0, s, a);
-    else if (Q <= 4 * 256)
-      hipLaunchKernelGGL((sample_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
-    else if (Q <= 4 * 1024)
-      hipLaunchKernelGGL((sample_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
-    // (the workspace's size is that of rows that are not aligned, which may be a vector longer)
-    else if (const int parts = split_parts(R, C, dtype); parts > 1 && (Q > 16 * 1024 || R <= cu_count() / 2)) {
-      Split split;
-      Split::carve(workspace, R, parts, &split);
-      split.each = (Q + parts - 1) / parts;
-      const dim3 all((unsigned)(R * parts)), threads(kPartThreads);
-      hipLaunchKernelGGL((split_max<T>), all, threads, 0, s, a, split);
-      if (top_k || top_p) hipLaunchKernelGGL((split_sum<T>), all, threads, 0, s, a, split);
-      if (top_p) hipLaunchKernelGGL((split_cut<T>), grid, dim3(kBins), 0, s, a, split);
-      hipLaunchKernelGGL((split_share<T>), all, threads, 0, s, a, split);
-      hipLaunchKernelGGL((split_draw<T>), grid, dim3(kDrawThreads), 0, s, a, split);
-    } else if (Q <= 16 * 1024)
-      hipLaunchKernelGGL((sample_tile<T, 1024, 16>), grid, dim3(1024), 0, s, a);
-    else
-      hipLaunchKernelGGL((sample_rows<T, 1024>), grid, dim3(1024), 0, s, a);
-    return launch_status();
+    return rows::in_launches(R, [&](int64_t first, int64_t n) {
+      using rows::or_null;
+      const Sample a{static_cast<const T*>(logits) + first * ld, n, C, ld,
+                     Settings{u + first, or_null(temperature, first), or_null(top_k, first), or_null(top_p, first),
+                              or_null(min_p, first)},
+                     cls + first, or_null(logp, first), or_null(kept, first)};
+      const dim3 grid((unsigned)n);
+      if (C <= rows::kShortRow && (C <= 32 || R > cu_count()))
+        hipLaunchKernelGGL((sample_short<T>), dim3((unsigned)((n + rows::kShortRows - 1) / rows::kShortRows)), dim3(256),
+                           0, s, a);
+      // up to 32 values a lane: one wave, without barriers (in a block of 256 that lists and orders what is kept 23265 rows
+      // of 590 bfloat16 with top-k 50 took 492 us, 110 so; one row of 1000 float32 14 and 10)
+      else if (Q <= rows::kWaveVectors<T> * kWave)
+        hipLaunchKernelGGL((sample_tile<T, kWave, rows::kWaveVectors<T>>), grid, dim3(kWave), 0, s, a);
+      else if (Q <= 4 * 256)
+        hipLaunchKernelGGL((sample_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
+      else if (Q <= 4 * 1024)
+        hipLaunchKernelGGL((sample_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
+      // (the workspace's size is that of rows that are not aligned, which may be a vector longer)
+      else if (const int parts = split_parts(R, C, dtype); parts > 1 && (Q > 16 * 1024 || R <= cu_count() / 2)) {
+        Split split;
+        Split::carve(workspace, R, parts, &split);
+        split.each = (Q + parts - 1) / parts;
+        const dim3 all((unsigned)(R * parts)), threads(kPartThreads);
+        hipLaunchKernelGGL((split_max<T>), all, threads, 0, s, a, split);
+        if (top_k || top_p) hipLaunchKernelGGL((split_sum<T>), all, threads, 0, s, a, split);
+        if (top_p) hipLaunchKernelGGL((split_cut<T>), grid, dim3(kBins), 0, s, a, split);
+        hipLaunchKernelGGL((split_share<T>), all, threads, 0, s, a, split);
+        hipLaunchKernelGGL((split_draw<T>), grid, dim3(kDrawThreads), 0, s, a, split);
+      } else if (Q <= 16 * 1024)
+        hipLaunchKernelGGL((sample_tile<T, 1024, 16>), grid, dim3(1024), 0, s, a);
+      else
+        hipLaunchKernelGGL((sample_rows<T, 1024>), grid, dim3(1024), 0, s, a);
+      return launch_status();
+    });
   });
 }

@@ -464,42 +464,45 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
   if (K > rows::kMaxListed) return SNN_ERR_UNSUPPORTED;
   const size_t need = snn_readout_top_workspace(R, C, dtype, K);
   if (need && (!workspace || workspace_bytes < need)) return SNN_ERR_INVALID_ARG;
-  const Top a{logits, R, C, ld, K, 1.0f / tau, ids, vals, lse, 1, C};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const dim3 grid((unsigned)R);
   return rows::for_type(dtype, [&](auto type) {
     using T = decltype(type);
     const int Q = rows::most_vectors<T>(logits, C, ld), least = C / rows::Row<T>::kVec;
-    if (C <= rows::kShortRow)
-      hipLaunchKernelGGL((top_short<T>), dim3((unsigned)((R + rows::kShortRows - 1) / rows::kShortRows)), dim3(256), 0,
-                         s, a);
-    // one wave (20000 rows of 700 float32, K 8, 40, 100: 38, 84, 338 us in blocks with the bound; 33, 39, 61 so)
-    else if (Q <= rows::kWaveVectors<T> * kWave) {
-      int size = 2;
-      while (size < K) size <<= 1;
-      hipLaunchKernelGGL((top_wave<T>), grid, dim3(kWave), size * sizeof(uint64_t), s, a);
-    }
-    // (the workspace's size is that of rows that are not aligned, which may be a vector longer)
-    else if (const int parts = top_parts(R, C, dtype, K); parts > 1 && (Q > 16 * 1024 || R <= cu_count() / 2)) {
-      constexpr int kVec = rows::Row<T>::kVec;
-      Top part = a;
-      part.parts = parts;
-      part.part_C = ((C + parts - 1) / parts + kVec - 1) / kVec * kVec;
-      top_carve(workspace, R, parts, K, &part);
-      hipLaunchKernelGGL((top_tile<T, kPartThreads, 4>), dim3((unsigned)(R * parts)), dim3(kPartThreads), 0, s, part);
-      hipLaunchKernelGGL(top_merge, grid, dim3(kMerged), 0, s, part, a);
-    } else if (Q <= 4 * 256 && nth_of<256>(K, least) <= kNthMost)
-      hipLaunchKernelGGL((top_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
-    else if (Q <= 8 * 512 && nth_of<512>(K, least) <= kNthMost && R >= cu_count())
-      hipLaunchKernelGGL((top_tile<T, 512, 8>), grid, dim3(512), 0, s, a);
-    else if (Q <= 4 * 1024 && nth_of<1024>(K, least) <= kNthMost)
-      hipLaunchKernelGGL((top_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
-    else if (Q <= 16 * 1024 && nth_of<1024>(K, least) <= kNthMost)
-      hipLaunchKernelGGL((top_tile<T, 1024, 16>), grid, dim3(1024), 0, s, a);
-    else if (Q <= 4096)
-      hipLaunchKernelGGL((top_rows<T, 256>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((top_rows<T, 1024>), grid, dim3(1024), 0, s, a);
-    return launch_status();
+    return rows::in_launches(R, [&](int64_t first, int64_t n) {
+      const Top a{static_cast<const T*>(logits) + first * ld, n, C, ld, K, 1.0f / tau, ids + first * K, vals + first * K,
+                  rows::or_null(lse, first), 1, C};
+      const dim3 grid((unsigned)n);
+      if (C <= rows::kShortRow)
+        hipLaunchKernelGGL((top_short<T>), dim3((unsigned)((n + rows::kShortRows - 1) / rows::kShortRows)), dim3(256), 0,
+                           s, a);
+      // one wave (20000 rows of 700 float32, K 8, 40, 100: 38, 84, 338 us in blocks with the bound; 33, 39, 61 so)
+      else if (Q <= rows::kWaveVectors<T> * kWave) {
+        int size = 2;
+        while (size < K) size <<= 1;
+        hipLaunchKernelGGL((top_wave<T>), grid, dim3(kWave), size * sizeof(uint64_t), s, a);
+      }
+      // (the workspace's size is that of rows that are not aligned, which may be a vector longer)
+      else if (const int parts = top_parts(R, C, dtype, K); parts > 1 && (Q > 16 * 1024 || R <= cu_count() / 2)) {
+        constexpr int kVec = rows::Row<T>::kVec;
+        Top part = a;
+        part.parts = parts;
+        part.part_C = ((C + parts - 1) / parts + kVec - 1) / kVec * kVec;
+        top_carve(workspace, R, parts, K, &part);
+        hipLaunchKernelGGL((top_tile<T, kPartThreads, 4>), dim3((unsigned)(R * parts)), dim3(kPartThreads), 0, s, part);
+        hipLaunchKernelGGL(top_merge, grid, dim3(kMerged), 0, s, part, a);
+      } else if (Q <= 4 * 256 && nth_of<256>(K, least) <= kNthMost)
+        hipLaunchKernelGGL((top_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
+      else if (Q <= 8 * 512 && nth_of<512>(K, least) <= kNthMost && R >= cu_count())
+        hipLaunchKernelGGL((top_tile<T, 512, 8>), grid, dim3(512), 0, s, a);
+      else if (Q <= 4 * 1024 && nth_of<1024>(K, least) <= kNthMost)
+        hipLaunchKernelGGL((top_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
+      else if (Q <= 16 * 1024 && nth_of<1024>(K, least) <= kNthMost)
+        hipLaunchKernelGGL((top_tile<T, 1024, 16>), grid, dim3(1024), 0, s, a);
+      else if (Q <= 4096)
+        hipLaunchKernelGGL((top_rows<T, 256>), grid, dim3(256), 0, s, a);
+      else
+        hipLaunchKernelGGL((top_rows<T, 1024>), grid, dim3(1024), 0, s, a);
+      return launch_status();
+    });
   });
 }

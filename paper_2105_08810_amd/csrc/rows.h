@@ -749,6 +749,22 @@ inline int most_vectors(const void* p, int C, int64_t ld) {
 
 inline int type_size(int dtype) { return dtype == SNN_F32 ? 4 : dtype == SNN_BF16 || dtype == SNN_F16 ? 2 : 0; }
 
+// Rows of one launch. A dispatch counts its threads in 32 bits, and a row has up to 1024 of them; a call of more rows is
+// several launches. (A multiple of the rows of a block.)
+constexpr int64_t kRowsAtOnce = 1 << 21;
+// f(first, number) for each launch's rows, until one fails.
+template <class F>
+inline snn_status in_launches(int64_t R, F f) {
+  snn_status ok = SNN_OK;
+  for (int64_t first = 0; first < R && ok == SNN_OK; first += kRowsAtOnce)
+    ok = f(first, R - first < kRowsAtOnce ? R - first : kRowsAtOnce);
+  return ok;
+}
+template <class T>
+inline T* or_null(T* p, int64_t offset) {
+  return p ? p + offset : nullptr;
+}
+
 // Arguments of a matrix of rows.
 inline snn_status check_rows(const void* p, int dtype, int64_t R, int C, int64_t ld) {
   const int size = type_size(dtype);

@@ -273,3 +273,44 @@ def test_distill_at_the_ends_of_the_range(C, dtype):
             tol = rel * (env[r] + 4 * share[r] * (l is not None) / (R * tau)) + tiny + 2.0 ** -126
             bad = ~(np.abs(got[r] - want[r]) <= tol + out * (np.abs(want[r]) + tol))
             assert not bad.any(), (names[r], tau, np.flatnonzero(bad)[:4], got[r][bad][:4], want[r][bad][:4])
+
+
+# ---------------------------------------------------------------- more rows than one launch counts
+
+def _some_rows(R):
+    """Rows at the ends, at where one launch may end and another begin, and between."""
+    at = {0, 1, R - 1, R // 2}
+    for k in range(10, 32):
+        at |= {(1 << k) - 1, 1 << k, (1 << k) + 1}
+    return sorted(r for r in at if r < R)
+
+
+@pytest.mark.parametrize("R,C", [((1 << 28) + 5, 1), ((1 << 26) + 5, 129)])
+def test_more_rows_than_a_launch_counts(R, C):
+    """Threads of a dispatch are counted in 32 bits: 16 a row of one class, 64 a row of 129 pass that. Every row is what it
+    is in a call of its own."""
+    g = torch.Generator(device="cuda").manual_seed(C)
+    z = torch.empty((R, C), dtype=torch.bfloat16, device="cuda")
+    for part in z.split(1 << 24):
+        part.copy_(torch.randn(part.shape, generator=g, device="cuda", dtype=torch.bfloat16))
+    at = _some_rows(R)
+    K = min(C, 2)
+    ids, vals, lse = snn.readout_top(z, K, 2.0)
+    for r in at:
+        for a, b in zip((ids, vals, lse), snn.readout_top(z[r:r + 1], K, 2.0)):
+            assert torch.equal(a[r:r + 1], b), r
+    if C == 1:
+        assert bool((ids == 0).all()) and torch.equal(vals.view(-1), z.view(-1).float())
+    loss, row_loss, grad = snn.readout_distill(z, ids, vals, lse, 1.0)
+    one = torch.full((1,), 1.0 / R, device="cuda")  # the mean's weight, rounded to float32
+    assert abs(float(loss) - float(row_loss.double().sum() * one.double())) <= U * abs(float(loss)) + 1e-9
+    for r in at:
+        alone = snn.readout_distill(z[r:r + 1], ids[r:r + 1], vals[r:r + 1], lse[r:r + 1], 1.0, one)
+        assert torch.equal(row_loss[r:r + 1], alone[1]) and torch.equal(grad[r:r + 1], alone[2]), r
+    del ids, vals, lse, row_loss, grad
+    u = torch.rand(R, generator=g, device="cuda")
+    p = torch.full((R,), 0.7, device="cuda")
+    cls, logp, kept = snn.readout_sample(z, u, None, None, p)
+    for r in at:
+        for a, b in zip((cls, logp, kept), snn.readout_sample(z[r:r + 1], u[r:r + 1], None, None, p[r:r + 1])):
+            assert torch.equal(a[r:r + 1], b), r

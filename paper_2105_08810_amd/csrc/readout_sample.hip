@@ -87,7 +87,6 @@ struct RowSettings {
   __device__ __forceinline__ RowSettings(const Settings& set, int64_t r, int C) {
     u = set.u[r];
     temperature = set.temperature ? set.temperature[r] : 1.0f;
-    temperature = temperature > 1e30f ? 1e30f : temperature;  // beyond it every finite logit has the same weight
     k = set.top_k ? set.top_k[r] : 0;
     if (k <= 0 || k > C) k = C;
     if (!(temperature > 0.0f)) k = 1;

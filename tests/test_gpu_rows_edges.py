@@ -314,3 +314,35 @@ def test_more_rows_than_a_launch_counts(R, C):
     for r in at:
         for a, b in zip((cls, logp, kept), snn.readout_sample(z[r:r + 1], u[r:r + 1], None, None, p[r:r + 1])):
             assert torch.equal(a[r:r + 1], b), r
+
+
+# ---------------------------------------------------------------- the highest temperatures
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C", [5, 20, 100, 700, 2048, 3000, 12000, 40000, 140003])
+def test_draws_at_the_highest_temperatures(C, dtype):
+    """Up to the largest float32 a temperature is what it says, masks of the type's lowest value included, and beyond it all
+    finite logits are alike."""
+    temperature = np.array([1e29, 1e31, 1e36, 2e37, 1e38, 3e38, INF, INF], np.float32)
+    R = len(temperature)
+    rng = np.random.default_rng(C)
+    z = rng.standard_normal((R, C)).astype(np.float32) * 3
+    z[rng.random((R, C)) < 0.4] = torch.finfo(DTYPES[dtype]).min
+    z[rng.random((R, C)) < 0.1] = -INF
+    z[:, C // 2] = 1.0
+    view = torch.from_numpy(z).to(DTYPES[dtype]).cuda()
+    x = view.float()
+    m = x.amax(1, keepdim=True)
+    t = torch.where(x == m, torch.zeros_like(x), (x - m) * (1.0 / torch.from_numpy(temperature).cuda()[:, None]))
+    e = torch.where(x > -INF, torch.exp(t), torch.zeros_like(x)).cpu().numpy()
+    x = x.cpu().numpy()
+    u = rng.random(R).astype(np.float32)
+    top_k = rng.integers(1, C + 1, R).astype(np.int32)
+    top_p = (0.5 + 0.5 * rng.random(R)).astype(np.float32)
+    for k, p in ((None, None), (top_k, None), (None, top_p), (top_k, top_p)):
+        cls, logp, kept = (v.cpu().numpy() for v in snn.readout_sample(view, *_device(u, temperature, k, p)))
+        for r in range(R):
+            j, n, total, own = rows.sample_row(x[r], e[r], u[r], 0 if k is None else int(k[r]), 1.0 if p is None else p[r])
+            assert (cls[r], kept[r]) == (j, n), (temperature[r], k is None, p is None)
+            want = math.log(own / total)  # as a drawn weight is within 2^-32 of its e
+            assert abs(logp[r] - want) <= U * 8 * (24 + abs(want))

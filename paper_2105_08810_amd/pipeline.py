@@ -31,8 +31,8 @@ class Record:
 @dataclass
 class Distill:
     """Distillation of a network's readout from a teacher's record, a term of the training loss beside the
-    cross-entropy: sum over the rows of weight_r KL(teacher || student at step t of sample b). weight None: the mean
-    over all rows, times `scale`."""
+    cross-entropy: `scale` times the sum over the rows of weight_r KL(teacher || student at step t of sample b). weight
+    None: the mean over all rows."""
     record: Record
     weight: Optional[torch.Tensor] = None  # [T, B]; rows of weight 0 are not read
     scale: float = 1.0
@@ -59,8 +59,9 @@ class ReadoutRows:
         sum over time for either loss mode."""
         T, B, C = self.V_out.shape
         rec, weight = distill.record, distill.weight
-        if weight is None and distill.scale != 1.0:
-            weight = torch.full((T, B), distill.scale / (T * B), dtype=torch.float32, device=self.V_out.device)
+        if distill.scale != 1.0:
+            weight = weight * distill.scale if weight is not None else \
+                torch.full((T, B), distill.scale / (T * B), dtype=torch.float32, device=self.V_out.device)
         csr, eps, ce, eps_dense = self.readout(dense=dense or self.loss_mode == 0)
         grad = eps.view(T, B, C) if self.loss_mode == 1 and not dense else eps_dense
         kd, _, _ = snn.readout_distill(self.V_out, rec.ids, rec.vals, rec.lse, rec.tau, weight, grad=grad,

@@ -87,3 +87,15 @@ def test_allocate_drops_the_active_sets(monkeypatch):
         net.allocate().forward(0.5)
         assert given[-1] == snn.snn_active_bits_words(T, B, 4)
         assert net.bits_bth == 0.5
+
+
+@pytest.mark.parametrize("kind", ["dense", "conv"])
+def test_scale_is_a_factor_of_any_weight(calls, kind):
+    net = _network(kind, 3, 2, 5).allocate()
+    rec, weight = _record(3, 2), torch.rand((3, 2))
+    for w, scale in ((None, 1.0), (None, 0.5), (weight, 1.0), (weight, 0.5), (weight, 0.0)):
+        net.readout_distilled(pipeline.Distill(rec, w, scale))
+        got = torch.full((3, 2), 1 / 6) if calls[-1] is None else calls[-1]
+        want = (torch.full((3, 2), 1 / 6) if w is None else w) * scale
+        assert got.shape == (3, 2) and torch.allclose(got, want, rtol=1e-6, atol=0.0)
+    assert torch.equal(rec.vals, _record(3, 2).vals) and bool((weight > 0).any())  # neither is changed

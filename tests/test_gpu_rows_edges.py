@@ -346,3 +346,91 @@ def test_draws_at_the_highest_temperatures(C, dtype):
             assert (cls[r], kept[r]) == (j, n), (temperature[r], k is None, p is None)
             want = math.log(own / total)  # as a drawn weight is within 2^-32 of its e
             assert abs(logp[r] - want) <= U * 8 * (24 + abs(want))
+
+
+# ---------------------------------------------------------------- the longest rows, and ways that few calls take
+
+def _long_rows(rng, C, lead, dtype, kind):
+    z = (rng.standard_normal((1, C)) * 2.5).astype(np.float32)
+    if kind == "ties":
+        z = np.round(z)
+    full = torch.full((C + lead,), float("nan"), dtype=DTYPES[dtype], device="cuda")
+    view = full[lead:].view(1, C)
+    view.copy_(torch.from_numpy(z))
+    return view, view.float().cpu().numpy()
+
+
+LONGEST = [(1 << 20, 0, "f32", "normal"), ((1 << 20) - 1, 1, "bf16", "ties"), (1 << 20, 3, "f16", "normal"),
+           (300001, 1, "f32", "ties"), (600003, 3, "bf16", "normal")]
+
+
+@pytest.mark.parametrize("C,lead,dtype,kind", LONGEST)
+def test_longest_records(C, lead, dtype, kind):
+    view, z = _long_rows(np.random.default_rng(C + lead), C, lead, dtype, kind)
+    for K in (1, 60, 1024):
+        ids, vals, lse = snn.readout_top(view, K, 1.5)
+        i, v, l = rows.top(z, K, 1.5)
+        assert np.array_equal(ids.cpu().numpy(), i) and np.array_equal(vals.cpu().numpy().astype(np.float64), v)
+        # a thread's share of the additions, a tree, and the roundings around them
+        assert abs(float(lse[0]) - l[0]) <= U * (4 * np.abs(z).max() / 1.5 + 8 * (1 + math.log(C)) + C / 1024 + 86)
+
+
+@pytest.mark.parametrize("C,lead,dtype,kind", LONGEST)
+def test_longest_distillation(C, lead, dtype, kind):
+    rng = np.random.default_rng(C + lead)
+    view, z = _long_rows(rng, C, lead, dtype, kind)
+    ids, vals, lse = rows.top((0.7 * z + rng.standard_normal(z.shape)).astype(np.float32), 200, 1.5)
+    rec = ids.astype(np.int32), vals.astype(np.float32), lse.astype(np.float32)
+    for tail in (True, False):
+        r = rec[0], rec[1], rec[2] if tail else None
+        loss, row_loss, grad = snn.readout_distill(view, *_device(*r), 1.5)
+        lo, _, want, env, share = rows.distill(z, *r, 1.5)
+        A = (np.abs(z).max() + np.abs(rec[1]).max()) / 1.5 + 1
+        rel = U * (102 + C / 1024 + 200 / 64 + 6 * A)
+        assert abs(float(row_loss[0]) - lo) <= rel * (1 + 2 * A) + (rel * (2 + 2 * A) if tail else 0)
+        assert float(loss[0]) == float(row_loss[0])
+        out, tiny = ROUND[dtype]
+        tol = rel * (env + 4 * share * tail / 1.5) + tiny
+        got = grad.double().cpu().numpy()
+        assert (np.abs(got - want) <= tol + out * (np.abs(want) + tol) * 1.01 + 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("C,lead,dtype,kind", LONGEST)
+def test_longest_draws(C, lead, dtype, kind):
+    rng = np.random.default_rng(C + lead)
+    view, z = _long_rows(rng, C, lead, dtype, kind)
+    x = view.float()
+    for k, p, temperature, u in ((0, 1.0, 1.0, 0.61), (0, 0.9, 0.7, 0.3), (700, 0.95, 1.3, 0.97), (5, 1.0, 1.0, 0.5),
+                                 (1, 1.0, 1.0, 0.2)):
+        t = torch.full((1,), temperature, device="cuda")
+        m = x.amax(1, keepdim=True)
+        e = torch.exp(torch.where(x == m, torch.zeros_like(x), (x - m) * (1.0 / t[:, None]))).cpu().numpy()
+        cls, logp, kept = snn.readout_sample(view, torch.full((1,), u, device="cuda"), t,
+                                             torch.full((1,), k, dtype=torch.int32, device="cuda"),
+                                             torch.full((1,), p, device="cuda"))
+        j, n, total, own = rows.sample_row(z[0], e[0], np.float32(u), k, np.float32(p))
+        assert (int(cls[0]), int(kept[0])) == (j, n), (k, p)
+        assert abs(float(logp[0]) - math.log(own / total)) <= U * 8 * (24 + abs(math.log(own / total)))
+
+
+@pytest.mark.parametrize("R,C,K", [(3, 5000, 600), (3, 4096, 1000), (2, 9001, 1024)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_records_of_many_classes_of_middle_rows(R, C, K, dtype):
+    rng = np.random.default_rng(C + K)
+    view = torch.from_numpy((rng.standard_normal((R, C)) * 2).astype(np.float32)).to(DTYPES[dtype]).cuda()
+    i, v, _ = rows.top(view.float().cpu().numpy(), K, 1.0)
+    ids, vals, _ = snn.readout_top(view, K, 1.0)
+    assert np.array_equal(ids.cpu().numpy(), i) and np.array_equal(vals.cpu().numpy().astype(np.float64), v)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("R", [3, 700])
+@pytest.mark.parametrize("C", [20, 120, 1000, 5000, 18000, 70001])
+def test_loss_without_a_gradient_is_the_same(R, C, dtype):
+    g = torch.Generator(device="cuda").manual_seed(C)
+    z = torch.randn((R, C), generator=g, device="cuda").to(DTYPES[dtype])
+    rec = snn.readout_top(z.float() + torch.randn((R, C), generator=g, device="cuda"), 4, 2.0)
+    weight = torch.rand(R, generator=g, device="cuda")
+    weight[::5] = 0.0
+    with_grad, without = snn.readout_distill(z, *rec, 2.0, weight), snn.readout_distill(z, *rec, 2.0, weight, want_grad=False)
+    assert without[2] is None and torch.equal(with_grad[0], without[0]) and torch.equal(with_grad[1], without[1])

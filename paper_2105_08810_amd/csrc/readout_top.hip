@@ -396,12 +396,17 @@ constexpr int kPartThreads = 512;
 constexpr int kPartVectors = 4 * kPartThreads;
 constexpr int kMerged = 1024;  // listed classes of a row's parts
 
-// Parts that a row is shared among: where it is longer than two of them and the rows alone leave most compute units
-// idle (24 rows of 131072 float16, K 50: 30 us in a block each, 23 so), or it is beyond a block's registers.
+// Rows of at least so many classes are shared among blocks though one block could hold them, where they leave most
+// compute units idle. In a block each and so, K 50, kernels alone: 24 x 130000 float16 31 and 23 us, bfloat16 26 and 22;
+// 128 x 130000 bfloat16 32 and 29; but 64 x 80000 bfloat16 21 and 22, 24 x 60000 float32 18 and 21, 24 x 20000 14 and 18.
+constexpr int kSharedRow = 98304;
+// Parts that a row is shared among: 1, or beyond a block's registers as many as hold it (8192 x 131072 float32, K 50: 2.9 ms
+// in passes by a block each, 1.4 ms so). The parts' records take up to 8 KB a row: of at most 2^14 rows.
 inline int top_parts(int64_t R, int C, int dtype, int K) {
   const int per = 16 / rows::type_size(dtype);
   const int Q = (C + 2 * per - 2) / per;  // as of a row that is not aligned
-  if (Q <= 2 * kPartVectors || (R > cu_count() / 2 && (Q <= 16 * 1024 || R > (1 << 14))) || K > kPartThreads / kWave * 16) return 1;
+  if (Q <= 16 * 1024 ? C < kSharedRow || R > cu_count() / 2 : R > (1 << 14)) return 1;
+  if (K > kPartThreads / kWave * 16) return 1;
   const int parts = (Q + kPartVectors - 2) / (kPartVectors - 1);  // the cuts may add a vector to each
   return parts * K <= kMerged && parts <= kWave ? parts : 1;
 }
@@ -482,7 +487,7 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
         hipLaunchKernelGGL((top_wave<T>), grid, dim3(kWave), size * sizeof(uint64_t), s, a);
       }
       // (the workspace's size is that of rows that are not aligned, which may be a vector longer)
-      else if (const int parts = top_parts(R, C, dtype, K); parts > 1 && (Q > 16 * 1024 || R <= cu_count() / 2)) {
+      else if (const int parts = top_parts(R, C, dtype, K); parts > 1 && (Q > 16 * 1024 || (C >= kSharedRow && R <= cu_count() / 2))) {
         constexpr int kVec = rows::Row<T>::kVec;
         Top part = a;
         part.parts = parts;
@@ -492,7 +497,9 @@ extern "C" snn_status snn_readout_top(const void* logits, int dtype, int64_t R, 
         hipLaunchKernelGGL(top_merge, grid, dim3(kMerged), 0, s, part, a);
       } else if (Q <= 4 * 256 && nth_of<256>(K, least) <= kNthMost)
         hipLaunchKernelGGL((top_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
-      else if (Q <= 8 * 512 && nth_of<512>(K, least) <= kNthMost && R >= cu_count())
+      // (in 1024 threads and in 512, K 50, kernels alone: 64 x 9000 float32 15 and 10 us; bfloat16 256 x 32003 18 and 15,
+      // 64 x 16000 16 and 11, but 16 x 32003 13 and 14)
+      else if (Q <= 8 * 512 && nth_of<512>(K, least) <= kNthMost && (sizeof(T) == 4 || R >= cu_count() / 4))
         hipLaunchKernelGGL((top_tile<T, 512, 8>), grid, dim3(512), 0, s, a);
       else if (Q <= 4 * 1024 && nth_of<1024>(K, least) <= kNthMost)
         hipLaunchKernelGGL((top_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);

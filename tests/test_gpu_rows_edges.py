@@ -434,3 +434,35 @@ def test_loss_without_a_gradient_is_the_same(R, C, dtype):
     weight[::5] = 0.0
     with_grad, without = snn.readout_distill(z, *rec, 2.0, weight), snn.readout_distill(z, *rec, 2.0, weight, want_grad=False)
     assert without[2] is None and torch.equal(with_grad[0], without[0]) and torch.equal(with_grad[1], without[1])
+
+
+# ---------------------------------------------------------------- where one way ends and another begins
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("R,C,lead", [(1, 65536, 0), (2, 65536, 1), (2, 98303, 0), (2, 98304, 3), (128, 98304, 0), (129, 98304, 0),
+                                      (2, 131072, 0), (130, 131071, 1), (3, 16384, 0), (3, 16385, 1), (63, 32768, 0),
+                                      (64, 32768, 0), (64, 32761, 5)])
+def test_records_where_ways_change(R, C, lead, dtype):
+    g = torch.Generator(device="cuda").manual_seed(C)
+    full = torch.randn(R * C + lead, generator=g, device="cuda").to(DTYPES[dtype])
+    z = full[lead:].view(R, C)
+    x = z.float()
+    for K in (3, 100):
+        ids, vals, lse = snn.readout_top(z, K, 2.0)
+        v, i = torch.sort(x, dim=1, descending=True, stable=True)
+        assert torch.equal(ids, i[:, :K].to(torch.int32)) and torch.equal(vals, v[:, :K])
+        # logits below 8: two roundings of the quotient, a logarithm below 12, a thread's additions and a tree
+        assert float((lse.double() - torch.logsumexp(x.double() / 2.0, 1)).abs().max()) <= U * (16 + 8 * 13 + 128 + 86)
+
+
+def test_graph_of_rows_shared_among_blocks():
+    z, u = torch.randn((5, 140001), device="cuda"), torch.rand(5, device="cuda")
+    call = lambda: (*snn.readout_top(z, 40, 1.5), *snn.readout_sample(z, u, top_p=torch.full_like(u, 0.9)))  # noqa: E731
+    call()
+    g = pipeline.Graphed(call)
+    for _ in range(3):
+        z.copy_(torch.randn_like(z))
+        u.copy_(torch.rand_like(u))
+        got, want = [t.clone() for t in g()], call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -703,8 +703,14 @@ extern "C" snn_status snn_readout_distill(const void* logits, int dtype, int64_t
     using T = decltype(type);
     constexpr int kWide = sizeof(T) == 4 ? 16 : 8;  // 64 values of a thread in registers
     const int Q = rows::most_vectors<T>(logits, C, ld);
-    const bool many = R >= 2 * cu_count(), small = Q <= 16 * Small<T>::NV;
+    const bool small = Q <= 16 * Small<T>::NV;
+    // one block of all rows, which needs no launch for the loss (17 x 20 float32 5.6 us, 7.5 in blocks of 16 rows; 64 x 100
+    // 7.4 and 7.8, kernels alone)
     if (small) n = R <= 64 ? 1 : (R + 15) / 16;
+    // Rows of more vectors than 1024 threads hold four of, 16-bit rows and rows that fill the chip take narrow blocks with
+    // kWide vectors a thread: 1 x 20000 float32 12.5 us in 1024 threads and 8.6 so, 1 x 10000 bfloat16 8.9 and 7.1, 300 x
+    // 12000 float32 16.7 and 12.3; but 1 x 12000 float32 7.2 and 7.6, 256 x 16384 float32 11.8 and 12.8.
+    const bool narrow = sizeof(T) == 2 || Q > 4 * 1024 || R > cu_count();
     return rows::in_launches(R, [&](int64_t first, int64_t count) {
       using rows::or_null;
       const Distill a{static_cast<const T*>(logits) + first * ld, C, ld, ids + first * K, vals + first * K,
@@ -721,12 +727,12 @@ extern "C" snn_status snn_readout_distill(const void* logits, int dtype, int64_t
         hipLaunchKernelGGL((distill_tile<T, 64, 4>), grid, dim3(64), 0, s, a);
       } else if (Q <= 4 * 256) {
         hipLaunchKernelGGL((distill_tile<T, 256, 4>), grid, dim3(256), 0, s, a);
-      } else if (Q <= kWide * 256 && many) {
+      } else if (Q <= kWide * 256 && narrow) {
         hipLaunchKernelGGL((distill_tile<T, 256, kWide>), grid, dim3(256), 0, s, a);
-      } else if (Q <= kWide * 512 && many) {
+      } else if (Q <= kWide * 512 && narrow) {
         hipLaunchKernelGGL((distill_tile<T, 512, kWide>), grid, dim3(512), 0, s, a);
-      } else if (Q <= 4 * 1024) {
-        hipLaunchKernelGGL((distill_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
+      } else if (sizeof(T) == 4 && Q <= 4 * 1024) {
+        if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((distill_tile<T, 1024, 4>), grid, dim3(1024), 0, s, a);
       } else if (Q <= kWide * 1024) {
         hipLaunchKernelGGL((distill_tile<T, 1024, kWide>), grid, dim3(1024), 0, s, a);
       } else {

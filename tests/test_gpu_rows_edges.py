@@ -466,3 +466,33 @@ def test_graph_of_rows_shared_among_blocks():
         got, want = [t.clone() for t in g()], call()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("R,C", [(3, 1025), (3, 4097), (256, 4100), (257, 4100), (3, 16384), (3, 16385), (257, 16384), (3, 32768),
+                                 (3, 32769), (3, 65536), (3, 65537), (64, 128), (65, 128), (64, 129)])
+def test_distillation_where_ways_change(R, C, dtype):
+    """Against the formula in 64 bits on the device."""
+    g = torch.Generator(device="cuda").manual_seed(R + C)
+    z = (torch.randn((R, C), generator=g, device="cuda") * 2).to(DTYPES[dtype])
+    K, tau = 9, 1.5
+    ids, vals, lse = snn.readout_top(z.float() * 0.7 + torch.randn((R, C), generator=g, device="cuda"), K, tau)
+    at = ids.long()
+    logq = torch.log_softmax(z.double() / tau, 1)
+    logp = vals.double() / tau - lse.double()[:, None]
+    p = torch.exp(logp)
+    left = (1 - p.sum(1)).clamp_min(0)
+    others = torch.exp(logq).scatter(1, at, 0.0)
+    q_t = others.sum(1)
+    want = (p * (logp - logq.gather(1, at))).sum(1) + left * (torch.log(left) - torch.log(q_t))
+    target = (others * (left / q_t)[:, None]).scatter(1, at, p)
+    grad = (torch.exp(logq) - target) / (tau * R)
+    loss, row_loss, got = snn.readout_distill(z, ids, vals, lse, tau)
+    # float32 sums and exponents of numbers of size A; p_t = 1 - sum p, which goes to the others by their share
+    A = float(z.float().abs().max() + vals.abs().max()) / tau + math.log(C)
+    rel = U * (102 + C / 1024 + 6 * A)
+    assert bool(((row_loss.double() - want).abs() <= rel * (4 + 4 * A)).all())
+    assert abs(float(loss) - float(want.mean())) <= rel * (4 + 4 * A)
+    out, tiny = ROUND[dtype]
+    tol = rel * (torch.exp(logq) + target + 4 * others / q_t[:, None]) / (tau * R) + tiny
+    assert bool(((got.double() - grad).abs() <= tol + out * (grad.abs() + tol)).all())

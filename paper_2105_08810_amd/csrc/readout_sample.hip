@@ -848,9 +848,12 @@ struct Split {
   }
 };
 
-// Parts that a row is shared among: from the length on where several launches take less than one block (1 row of 32003
-// float32: 19 us in one block with top-k 50, 22 in parts; of 128011 bf16 29 and 23), where the rows alone leave most compute
-// units idle or do not fit a block's registers (10 KB of workspace a part).
+// Parts that a row is shared among: from the length on where several launches take less than one block, where the rows
+// alone leave most compute units idle or do not fit a block's registers. In a block and in parts, kernels alone: by
+// requests 64 x 40000 float32 54 and 43 us, 64 x 130000 bfloat16 133 and 61; with top-k 50 1 x 40000 float32 17 and 22,
+// 1 x 130000 bfloat16 31 and 23. Beyond the registers, in passes and in parts: 64 x 131072 float32 with top-k 50 320 and
+// 34, by requests, some with a top-k that is not collected, 345 and 383; 1000 x 131072 1390 and 286, 1314 and 688. A part
+// has 10 KB of workspace: at most 320 MB.
 inline int split_parts(int64_t R, int C, int dtype) {
   const int per = 16 / rows::type_size(dtype);
   const int Q = (C + 2 * per - 2) / per;  // as of a row that is not aligned
@@ -1164,7 +1167,12 @@ extern "C" snn_status snn_readout_sample(const void* logits, int dtype, int64_t 
                               or_null(min_p, first)},
                      cls + first, or_null(logp, first), or_null(kept, first)};
       const dim3 grid((unsigned)n);
-      if (C <= rows::kShortRow && (C <= 32 || R > cu_count()))
+      // 16 lanes a row compare each value with all others where an order is asked for: few rows of many classes go a wave
+      // each. By requests, float32, a wave each and so, kernels alone: 16 x 20 8 and 6 us, 2048 x 48 13 and 11, 2048 x 100 13
+      // and 26, 20000 x 100 47 and 40, 20000 x 128 49 and 55 (bfloat16 with top-k 50 77 and 55); without an order 256 x 128
+      // bfloat16 6 and 5, 20000 x 128 36 and 9.
+      const bool ordered = top_k || top_p;
+      if (C <= rows::kShortRow && (C <= 48 || !ordered || R >= 100 * (C - 32)))
         hipLaunchKernelGGL((sample_short<T>), dim3((unsigned)((n + rows::kShortRows - 1) / rows::kShortRows)), dim3(256),
                            0, s, a);
       // up to 32 values a lane: one wave, without barriers (in a block of 256 that lists and orders what is kept 23265 rows

@@ -496,3 +496,26 @@ def test_distillation_where_ways_change(R, C, dtype):
     out, tiny = ROUND[dtype]
     tol = rel * (torch.exp(logq) + target + 4 * others / q_t[:, None]) / (tau * R) + tiny
     assert bool(((got.double() - grad).abs() <= tol + out * (grad.abs() + tol)).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [33, 48, 49, 64, 100, 128])
+def test_draws_where_ways_change(C, dtype):
+    """Rows drawn in calls of many and of few rows, with and without an order, have the same answers."""
+    R = 100 * (C - 32) + 3
+    g = torch.Generator(device="cuda").manual_seed(C)
+    z = (torch.randn((R, C), generator=g, device="cuda") * 2).round(decimals=1).to(DTYPES[dtype])
+    u = torch.rand(R, generator=g, device="cuda")
+    k = torch.randint(0, C + 1, (R,), generator=g, device="cuda", dtype=torch.int32)
+    p, m = torch.rand(R, generator=g, device="cuda"), torch.rand(R, generator=g, device="cuda") * 0.1
+    t = torch.rand(R, generator=g, device="cuda") * 2
+    for settings in ((t, k, p, m), (t, None, p, None), (None, k, None, None), (t, None, None, m)):
+        whole = snn.readout_sample(z, u, *settings)
+        for part in (slice(0, 40), slice(R - 41, R)):
+            few = snn.readout_sample(z[part], u[part], *(None if s is None else s[part] for s in settings))
+            assert all(torch.equal(a[part], b) for a, b in zip(whole, few))
+    e = torch.exp((z.float() - z.float().amax(1, keepdim=True)) * (1.0 / torch.ones((R, 1), device="cuda"))).cpu().numpy()
+    x = z.float().cpu().numpy()
+    cls, _, kept = snn.readout_sample(z, u, None, k, None)
+    for r in range(0, R, 97):
+        assert (int(cls[r]), int(kept[r])) == rows.sample_row(x[r], e[r], u[r].cpu().numpy(), int(k[r]))[:2]

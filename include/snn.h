@@ -494,9 +494,9 @@ snn_status snn_conv_dense_dw(const float* trace_in, const float* V, const float*
  * a network; the membrane V_out [T,B,C] of the readout is R = T*B rows r = t*B + b of C classes.
  *   logits   R rows of C values of type `dtype`; row r begins at element r*ld, ld >= C (rows may lie in wider ones).
  *            The address needs the alignment of its type only; 16-byte aligned rows are read fastest.
- * R up to 2^31 - 1, C up to 2^20, K up to 1024 classes in a record; larger: SNN_ERR_UNSUPPORTED. SNN_ERR_INVALID_ARG
- * also for an unknown dtype, ld < C, an address that is no multiple of the type's size, K > C, and a tau that is not
- * positive and finite. Offsets are formed in 64 bits. All results are deterministic.
+ * R up to 2^31 - 1 (beyond 2^21 a call is several launches), C up to 2^20, K up to 1024 classes in a record; larger:
+ * SNN_ERR_UNSUPPORTED. SNN_ERR_INVALID_ARG also for an unknown dtype, ld < C, an address that is no multiple of the type's
+ * size, K > C, and a tau that is not positive and finite. Offsets are formed in 64 bits. All results are deterministic.
  */
 typedef enum { SNN_F32 = 0, SNN_BF16 = 1, SNN_F16 = 2 } snn_dtype;
 
@@ -506,7 +506,8 @@ typedef enum { SNN_F32 = 0, SNN_BF16 = 1, SNN_F16 = 2 } snn_dtype;
  *   vals     float32 [R,K] (written): their logits, not divided by tau
  *   lse      float32 [R] (written unless NULL): log sum_j exp(z_j / tau) over all C classes, so that a listed class has
  *            the probability exp(val / tau - lse); -inf for a row of -inf, +inf for one that holds +inf
- * NaN counts as -inf, and -inf is not listed: a row with fewer than K others ends in ids -1, vals -inf.
+ * NaN counts as -inf, and -inf is not listed: a row with fewer than K others ends in ids -1, vals -inf. lse is a float32:
+ * of a row whose logits are all far from 0 (masks of the type's lowest value) it keeps nothing of log C.
  * Workspace: needed for few long rows alone; the query gives 0 for others, and workspace may then be NULL.
  */
 size_t snn_readout_top_workspace(int64_t R, int C, int dtype, int K);
@@ -544,8 +545,10 @@ snn_status snn_readout_distill(const void* logits, int dtype, int64_t R, int C, 
 
 /*
  * Draws one class per row. The settings are device arrays, one value a row; a NULL one leaves its filter out.
- *   u           float32 [R] uniform numbers in [0,1) (values outside are taken as the nearest end)
- *   temperature float32 [R]; NULL: 1. Not above 0 (or NaN): the first of the largest logits.
+ *   u           float32 [R] uniform numbers in [0,1) (values outside are taken as the nearest end). Their steps of 2^-24
+ *               are what a draw can tell apart: finer differences in probability are in the weights but not in u.
+ *   temperature float32 [R]; NULL: 1. Not above 0 (or NaN): the first of the largest logits. At infinity all finite
+ *               logits are alike.
  *   top_k       int32 [R]; <= 0: all classes
  *   top_p       float32 [R]; >= 1: all, <= 0 or NaN: one class
  *   min_p       float32 [R]; <= 0 or NaN: all, above 1 as 1

@@ -8,15 +8,15 @@
 // A row is held in registers. What top-k keeps is collected by the waves' n-th largest lanes, as a teacher's record is;
 // what top-p keeps is either among those or found by a histogram of t and an order within one of its bins; without
 // either filter the weights are summed in runs along the row and the drawn class is sought in one run.
-//   sample_short   16 lanes a row of up to 128 classes
+//   sample_short   16 lanes a row of up to 128 classes; few of more than 48 with an order take a wave each
 //   sample_tile    a block a row, in registers; one wave up to 2048 classes, whose cuts cut_in_wave finds
 //   split_*        a row's parts in blocks of their own: few long rows, rows beyond the registers
 //   sample_rows    a block a row, read several times: the rest
 //
-// Measured: 1024 x 65536 float32 with a temperature: 136 us (2.0 TB/s), bound by the vector instructions of the
-// exponentials and 64-bit sums; 64 x 128011 bfloat16, mixed settings, in parts: 64 us, and 1 x 32003 float32 with
-// top-k 50: 18 us, both bound by latency; 23265 x 590 bfloat16, mixed settings: 124 us, bound by the vector instructions of
-// some 15 to 30 comparisons a value; 25600 x 20 float32, mixed settings: 14.6 us.
+// Measured: 1024 x 65536 float32 with a temperature: 135 us (2.0 TB/s), vector instructions (exponentials, the filters'
+// comparisons, 64-bit sums) issued 62% of the time with one block a compute unit; 64 x 128011 bfloat16, mixed settings, in
+// parts: 63 us, and 1 x 32003 float32 with top-k 50: 19 us, waves waiting about 60% of the time; 23265 x 590 bfloat16,
+// mixed settings: 117 us, some 15 to 30 comparisons a value; 25600 x 20 float32, mixed settings: 14.3 us.
 #include <cfloat>
 
 #include "rows.h"

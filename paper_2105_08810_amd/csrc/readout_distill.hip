@@ -27,7 +27,6 @@ namespace {
 using namespace rows;
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLn2 = 0.69314718055994530942f;
 
 // A sum of exp(x / tau) over some logits x: the largest of them, and the sum relative to it. Logits are subtracted before
 // they are scaled by c = log2(e) / tau: the product of one could overflow (masks of the type's lowest value), and its

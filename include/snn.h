@@ -105,6 +105,18 @@ snn_status snn_lif_forward_traces(const uint8_t* s_in, const float* W, int T, in
                                   void* stream);
 
 /*
+ * The recurrence alone, for a layer whose weighted inputs are known (the rows that a network's tokens pick, see
+ * snn_embed): as snn_lif_forward_traces with
+ *   V            [T,B,N] float32: the weighted input of step t in the rows of step t+1, t = 0..T-2 (read), which the
+ *                membrane potential replaces; V[0] = 0 (written). The weighted input of step T-1 has no place: it
+ *                enters no V.
+ *   b_th         ignored where active_bits is NULL; trace_out, active_bits NULL where not wanted
+ */
+snn_status snn_lif_forward_currents(float* V, int T, int B, int N, float alpha, float theta, float b_th,
+                                    uint8_t* s_out, float* trace_out, float alpha_next, uint64_t* active_bits,
+                                    void* stream);
+
+/*
  * Active-set compaction (Definition 1) with the truncated spike derivative (Definition 2).
  *   V        [T,B,N] float32 (read)
  *   active   |V - theta| < b_th in float32, strictly (b_th = +INFINITY: every finite V)
@@ -569,6 +581,96 @@ snn_status snn_readout_sample(const void* logits, int dtype, int64_t R, int C, i
                               const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                               int32_t* cls, float* logp, int32_t* kept, void* workspace, size_t workspace_bytes,
                               void* stream);
+
+/*
+ * Operators of a network on sequences of tokens: a row is one token, (t, b) at r = t*B + b. Rows of x, y, E, W and their
+ * gradients begin at element r*ld, ld >= their width, and need the alignment of their type only (16-byte aligned rows are
+ * the fastest); elements between the width and ld are neither read nor written. Types are snn_dtype's. Outputs may not
+ * overlap inputs. Sums are float32 or wider, results rounded once and deterministic.
+ */
+
+/*
+ * Rows of an embedding: out[r] = scale * E[ids[r]], a row of zeros for an id outside [0,V).
+ *   E        V rows of N values of type dtype
+ *   ids      int32 [R]
+ *   out      R rows of N values of dtype (written)
+ * R, V up to 2^31 - 1, N up to 2^20; larger: SNN_ERR_UNSUPPORTED. SNN_ERR_INVALID_ARG also for a NaN scale.
+ */
+snn_status snn_embed(const void* E, int dtype, int64_t V, int N, int64_t ld_e, const int32_t* ids, int64_t R,
+                     float scale, void* out, int64_t ld_out, void* stream);
+
+/*
+ * Its gradient: dE[v] = scale * sum over the rows r with ids[r] = v of dout[r].
+ *   dout     R rows of N values of dtype; rows whose id is outside [0,V) are not used
+ *   dE       V rows of N values of dtype (written; rows of tokens that do not occur are 0)
+ *   accumulate  nonzero: dE += instead (rows of tokens that do not occur are not touched)
+ * R below 2^30; larger: SNN_ERR_UNSUPPORTED, and the query gives 0.
+ */
+size_t snn_embed_grad_workspace(int dtype, int64_t V, int N, int64_t R);
+snn_status snn_embed_grad(const int32_t* ids, int64_t R, const void* dout, int dtype, int64_t ld_out, int64_t V, int N,
+                          float scale, void* dE, int64_t ld_e, int accumulate, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * Layer norm of rows: y = (x - mean) rstd gamma + beta, mean and 1 / rstd^2 = variance + eps over the row's N values.
+ *   x        R rows of N values of x_dtype
+ *   gamma, beta  float32 [N], or NULL for 1 and 0
+ *   eps      >= 0, finite
+ *   y        R rows of N values of y_dtype (written)
+ *   mean, rstd  float32 [R] (written unless NULL), what the backward pass takes
+ * R up to 2^31 - 1, N up to 2^20. A row of one value has y = beta; a row whose variance and eps are both 0 has rstd = inf
+ * and y NaN.
+ */
+snn_status snn_layer_norm(const void* x, int x_dtype, int64_t R, int N, int64_t ld_x, const float* gamma,
+                          const float* beta, float eps, void* y, int y_dtype, int64_t ld_y, float* mean, float* rstd,
+                          void* stream);
+
+/*
+ * Its backward pass: with h = (x - mean) rstd and a = dy gamma,
+ *   dx = rstd (a - mean(a) - h mean(a h)),  dgamma = sum_r dy h,  dbeta = sum_r dy
+ *   dy       R rows of N values of y_dtype
+ *   x, gamma, mean, rstd  as the forward had and wrote them
+ *   dx       R rows of N values of x_dtype (written unless NULL)
+ *   dgamma, dbeta  float32 [N] (written unless NULL)
+ * Workspace: needed for dgamma and dbeta only, NULL otherwise.
+ */
+size_t snn_layer_norm_grad_workspace(int x_dtype, int y_dtype, int64_t R, int N);
+snn_status snn_layer_norm_grad(const void* dy, int y_dtype, int64_t ld_dy, const void* x, int x_dtype, int64_t ld_x,
+                               int64_t R, int N, const float* gamma, const float* mean, const float* rstd, void* dx,
+                               int64_t ld_dx, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/*
+ * Softmax cross entropy of linear logits z = x W against one target a row, with both gradients; the R x C logits are
+ * never in memory together. A readout without threshold is such a product: V_out = trace W_out.
+ *   x        R rows of H values of dtype
+ *   W        H rows of C values of dtype
+ *   targets  int32 [R]; a row whose target is outside [0,C) takes no part: it is not read, its loss and gradient are 0
+ *   weight   float32 [R], or NULL for one over the number of rows that have a target. A row of weight 0 takes no part.
+ *   loss     float32 [1] (written): sum_r weight_r L_r, L_r = log sum_c exp(z_rc) - z_r,target; 0 if no row takes part
+ *   row_loss float32 [R] (written unless NULL): L_r
+ *   dx       R rows of H values of dtype (written unless NULL): weight_r (softmax(z_r) - onehot) W^T
+ *   dW       H rows of C values of dtype (written unless NULL): x^T (weight_r (softmax(z_r) - onehot))
+ * R up to 2^24, H up to 2^16, C up to 2^20, ld_w up to 2^31 - 1; larger: SNN_ERR_UNSUPPORTED. The workspace query takes
+ * whether a gradient is wanted. The workspace grows with R H, and with R times a piece of the classes (bounded).
+ */
+size_t snn_linear_ce_workspace(int dtype, int64_t R, int H, int C, int grad);
+snn_status snn_linear_ce(const void* x, const void* W, int dtype, int64_t R, int H, int C, int64_t ld_x, int64_t ld_w,
+                         const int32_t* targets, const float* weight, float* loss, float* row_loss, void* dx,
+                         int64_t ld_dx, void* dW, int64_t ld_dw, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The adjoint of a leaky integration u[t+1] = alpha u[t] + i[t], u[0] = 0 (a trace, or a membrane between its spikes):
+ * from x, a loss's gradient by u, its gradient by i,
+ *   y[T-1] = 0,  y[t] = alpha y[t+1] + x[t+1]
+ *   x        float32 [T,B,N] with in_row_ptr NULL; else the entries [in_cap] of a CSR over the T*B rows (row_ptr
+ *            [T*B+1], columns ascending and at most once in a row), times in_g [in_cap] unless NULL; 0 elsewhere
+ *   y        float32 [T,B,N] with out_row_ptr NULL; else its values at the entries [out_cap] of such a CSR (written)
+ * Row pointers past a capacity count as the capacity.
+ */
+snn_status snn_leak_grad(const float* x, const int32_t* in_row_ptr, const int32_t* in_col_idx, const float* in_g,
+                         int64_t in_cap, int T, int B, int N, float alpha, float* y, const int32_t* out_row_ptr,
+                         const int32_t* out_col_idx, int64_t out_cap, void* stream);
 
 #ifdef __cplusplus
 }

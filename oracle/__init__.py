@@ -28,6 +28,8 @@ What it computes, and where the paper defines it:
 * adam.py     -- the Adam update (App. E's optimiser; Kingma and Ba, Algorithm 1).
 * rows.py     -- operators on rows of logits (the K largest, distillation with its
   gradient, drawing a class), in 64 bits.
+* tokens.py   -- operators of a network on sequences of tokens (embedding, layer
+  norm, cross entropy of linear logits, the leak's adjoint), in 64 bits.
 * train.py    -- a whole training step (loss with penalties, gradient, Adam) and
   the sparse vs full-surrogate gradient difference of App. H.
 * conv.py     -- the convolutional spiking layer (3x3, padding 1) with 2x2 max

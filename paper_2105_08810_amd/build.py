@@ -32,6 +32,10 @@ SOURCES = [
     "readout_distill.hip",
     "readout_sample.hip",
     "train_step.hip",
+    "embed.hip",
+    "layer_norm.hip",
+    "linear_ce.hip",
+    "leak_grad.hip",
     "conv_layer.hip",
 ]
 # The forward and the compaction decide spikes and active sets, which must be bit-exact:

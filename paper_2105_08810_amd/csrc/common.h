@@ -95,7 +95,8 @@ ColsParts cols_enqueue(const float* trace_in, int T, int B, int N_in, int N_out,
 
 // Dense float32 products (gemm.hip). K slice z of `splits` goes to C + z * c_split.
 //   gemm_split_km  C = sum_k A[k, m] B[k, n], operands in three bf16 parts, float32 sums
-//   gemm_split_kc  C = sum_k A[m, k] B[n, k], the same
+//   gemm_split_kc  C = sum_k A[m, k] B[n, k], the same; C += with accumulate
+//   gemm_split_kr  C = sum_k A[m, k] B[k, n], the same
 //   gemm_f64_km    C = sum_k A[k, m] B[k, n], products and sums in float64
 // plan_splits: the K slices of a km product whose whole rounds of blocks run at mac_rate multiply-adds a second,
 // and the time this should take with the partials' sum.
@@ -107,6 +108,8 @@ SplitPlan plan_splits(int M, int N, int K, double mac_rate);
 void gemm_split_km(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc, int splits,
                    size_t c_split, hipStream_t s);
 void gemm_split_kc(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
+                   hipStream_t s, bool accumulate = false);
+void gemm_split_kr(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
                    hipStream_t s);
 // The elements (r, col_idx[e]) of C, as gemm_split_kc forms it, at the entries e < cap of a CSR over C's
 // rows: out[e] (0 for a column outside [0, N)). What is not an entry is not written.

@@ -170,12 +170,13 @@ __device__ __forceinline__ BlockTile row_tile(int tiles_m, int tiles_n) {
 // below (a sum over all rows of positive traces) adds up coherently. A's sign turns from one fold and one tile of
 // rows to the next, so that it cancels (dW of the first of three 1024 x 1024 layers, 27% active: 1.89e-7 -> 1.51e-7
 // of the result from 64 bits; 1.80e-7 entry by entry).
-template <bool KM, bool VEC, bool GATHER>
+// KA, KB: k down the rows of A, of B (load_stage's KM). accumulate: C += instead (one K slice alone).
+template <bool KA, bool KB, bool VEC, bool GATHER>
 __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, const float* __restrict__ A, int lda,
                                                            const float* __restrict__ B, int ldb,
                                                            float* __restrict__ C, int ldc, int k_per_split,
                                                            size_t c_split, int tiles_m, int tiles_n, int splits,
-                                                           GatherOut to, Gate gate) {
+                                                           int accumulate, GatherOut to, Gate gate) {
   if (!gate_open(gate)) return;
   constexpr int TN = GATHER ? 2 : 4;  // 16-wide column tiles of a wavefront
   constexpr int BN = 32 * TN;
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, 
   Stage<BN>& Bs = *reinterpret_cast<Stage<BN>*>(lds + sizeof(Stage<kBM>));
   const int w = threadIdx.x / kWave;
   const int l = threadIdx.x % kWave;
-  const BlockTile bt = KM ? slice_tile(tiles_m, tiles_n, splits) : row_tile(tiles_m, tiles_n);
+  const BlockTile bt = KA && KB ? slice_tile(tiles_m, tiles_n, splits) : row_tile(tiles_m, tiles_n);
   if (!bt.ok) return;
   const int m0 = bt.tm * kBM, n0 = bt.tn * BN;
   const int wm = (w / 2) * 64, wn = (w % 2) * (BN / 2);
@@ -255,17 +256,17 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, 
 
   float xa[2][8], xb[BN / 64][8];
   if (k_lo < k_hi) {
-    load_stage<KM, VEC, kBM>(A, lda, m0, M, k_lo, k_hi, xa);
-    load_stage<KM, VEC, BN>(B, ldb, n0, N, k_lo, k_hi, xb);
+    load_stage<KA, VEC, kBM>(A, lda, m0, M, k_lo, k_hi, xa);
+    load_stage<KB, VEC, BN>(B, ldb, n0, N, k_lo, k_hi, xb);
   }
   int stage = 0;
   for (int k0 = k_lo; k0 < k_hi; k0 += kBK) {
-    store_stage<KM, kBM>(As, xa, up);
-    store_stage<KM, BN>(Bs, xb, kUp);
+    store_stage<KA, kBM>(As, xa, up);
+    store_stage<KB, BN>(Bs, xb, kUp);
     __syncthreads();
     if (k0 + kBK < k_hi) {
-      load_stage<KM, VEC, kBM>(A, lda, m0, M, k0 + kBK, k_hi, xa);
-      load_stage<KM, VEC, BN>(B, ldb, n0, N, k0 + kBK, k_hi, xb);
+      load_stage<KA, VEC, kBM>(A, lda, m0, M, k0 + kBK, k_hi, xa);
+      load_stage<KB, VEC, BN>(B, ldb, n0, N, k0 + kBK, k_hi, xb);
     }
     bf16x8 fa[3][4];
 #pragma unroll
@@ -311,10 +312,10 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, 
     clear_total();
     down = 1.0f;
     for (int k0 = k_lo; k0 < k_hi; k0 += kBK) {
-      load_stage<KM, VEC, kBM>(A, lda, m0, M, k0, k_hi, xa);
-      load_stage<KM, VEC, BN>(B, ldb, n0, N, k0, k_hi, xb);
-      store_wide<KM, kBM>(Aw, xa);
-      store_wide<KM, BN>(Bw, xb);
+      load_stage<KA, VEC, kBM>(A, lda, m0, M, k0, k_hi, xa);
+      load_stage<KB, VEC, BN>(B, ldb, n0, N, k0, k_hi, xb);
+      store_wide<KA, kBM>(Aw, xa);
+      store_wide<KB, BN>(Bw, xb);
       __syncthreads();
       for (int k = 0; k < kBK; k += 4)
 #pragma unroll
@@ -339,7 +340,11 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, 
         for (int v = 0; v < 4; ++v) {
           const int m = m0 + wm + 16 * a + 4 * lk + v;
           const int n = n0 + wn + 16 * b + lr;
-          if (m < M && n < N) Cz[(size_t)m * ldc + n] = (lead[a][b][v] + rest[a][b][v]) * down;
+          if (m < M && n < N) {
+            float* c = Cz + (size_t)m * ldc + n;
+            const float sum = (lead[a][b][v] + rest[a][b][v]) * down;
+            *c = accumulate ? *c + sum : sum;
+          }
         }
   } else {
     float(*tile)[BN + 4] = reinterpret_cast<float(*)[BN + 4]>(lds);
@@ -499,39 +504,45 @@ void gemm_split_km(int M, int N, int K, const float* A, int lda, const float* B,
   const int tm = (M + kBM - 1) / kBM, tn = (N + kBN - 1) / kBN;
   int kps = (K + splits - 1) / splits;
   kps = (kps + kBK - 1) / kBK * kBK;
-  hipLaunchKernelGGL((gemm_split3<true, false, false>), dim3((unsigned)(splits * tm * tn)), dim3(kThreads), 0, s, M, N,
-                     K, A, lda, B, ldb, C, ldc, kps, c_split, tm, tn, splits, GatherOut{}, Gate{});
+  hipLaunchKernelGGL((gemm_split3<true, true, false, false>), dim3((unsigned)(splits * tm * tn)), dim3(kThreads), 0, s,
+                     M, N, K, A, lda, B, ldb, C, ldc, kps, c_split, tm, tn, splits, 0, GatherOut{}, Gate{});
 }
 
 namespace {
 
-template <bool GATHER>
-void launch_kc(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
+// A with k along its rows; B with k down its rows (KB) or along them.
+template <bool KB, bool GATHER>
+void launch_kc(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc, int accumulate,
                const GatherOut& to, const Gate& gate, hipStream_t s) {
   const int bn = GATHER ? kBN / 2 : kBN;
   const int tm = (M + kBM - 1) / kBM, tn = (N + bn - 1) / bn;
-  const bool vec = lda % 4 == 0 && ldb % 4 == 0 && reinterpret_cast<uintptr_t>(A) % 16 == 0 &&
-                   reinterpret_cast<uintptr_t>(B) % 16 == 0;
+  const bool vec = lda % 4 == 0 && reinterpret_cast<uintptr_t>(A) % 16 == 0 &&
+                   (KB || (ldb % 4 == 0 && reinterpret_cast<uintptr_t>(B) % 16 == 0));
   const int kps = (K + kBK - 1) / kBK * kBK;
   const dim3 g((unsigned)((tm >= 32 ? (tm + 7) / 8 * 8 : tm) * tn));
   if (vec)
-    hipLaunchKernelGGL((gemm_split3<false, true, GATHER>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
-                       kps, 0, tm, tn, 1, to, gate);
+    hipLaunchKernelGGL((gemm_split3<false, KB, true, GATHER>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
+                       kps, 0, tm, tn, 1, accumulate, to, gate);
   else
-    hipLaunchKernelGGL((gemm_split3<false, false, GATHER>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
-                       kps, 0, tm, tn, 1, to, gate);
+    hipLaunchKernelGGL((gemm_split3<false, KB, false, GATHER>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
+                       kps, 0, tm, tn, 1, accumulate, to, gate);
 }
 
 }  // namespace
 
 void gemm_split_kc(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
+                   hipStream_t s, bool accumulate) {
+  launch_kc<false, false>(M, N, K, A, lda, B, ldb, C, ldc, accumulate, GatherOut{}, Gate{}, s);
+}
+
+void gemm_split_kr(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
                    hipStream_t s) {
-  launch_kc<false>(M, N, K, A, lda, B, ldb, C, ldc, GatherOut{}, Gate{}, s);
+  launch_kc<true, false>(M, N, K, A, lda, B, ldb, C, ldc, 0, GatherOut{}, Gate{}, s);
 }
 
 void gemm_split_kc_gather(int M, int N, int K, const float* A, int lda, const float* B, int ldb, const GatherOut& to,
                           const Gate& gate, hipStream_t s) {
-  launch_kc<true>(M, N, K, A, lda, B, ldb, nullptr, 0, to, gate, s);
+  launch_kc<false, true>(M, N, K, A, lda, B, ldb, nullptr, 0, 0, to, gate, s);
 }
 
 void gemm_f64_km(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc, int splits,

@@ -1,0 +1,463 @@
+// Layer norm of rows and its backward pass.
+//
+//   y = h gamma + beta,  h = (x - mean) rstd,  mean = sum x / N,  rstd = 1 / sqrt(sum (x - mean)^2 / N + eps)
+//   a = dy gamma,  dx = rstd (a - mean(a) - h mean(a h)),  dgamma = sum over rows of dy h,  dbeta = sum over rows of dy
+//
+// Bound: memory. A row is read once into the registers of its lanes (16 lanes, a wavefront, or a block of 256 or 1024
+// threads by its width), the squares are summed about the mean that is already known, and the results are written from
+// the registers. The backward pass reads x and dy once; each group of lanes walks many rows and keeps its columns' shares
+// of dgamma and dbeta in registers, a block adds its groups' shares and writes one partial row, and norm_columns adds the
+// partial rows in a fixed order in float64. Rows beyond a block's registers are read once more for every sum.
+#include <algorithm>
+
+#include "vectors.h"
+
+namespace snn {
+namespace {
+
+using namespace vectors;
+
+constexpr int kMaxWidth = 1 << 20;
+
+// Sum over a group of L lanes (16 or 64) or a block of L threads, the same in every lane; red holds a value a wavefront.
+template <int L>
+__device__ __forceinline__ float group_sum(float v, float* red) {
+#pragma unroll
+  for (int off = (L < kWave ? L : kWave) / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
+  if constexpr (L > kWave) {
+    const int w = threadIdx.x / kWave;
+    __syncthreads();  // the sums before these have been read
+    if (lane_id() == 0) red[w] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < L / kWave; ++k) v += red[k];
+  }
+  return v;
+}
+
+// What the launches share. E elements a vector, Q vectors a lane, L lanes a row, B threads a block.
+template <int L>
+constexpr int kBlock = L > 256 ? L : 256;
+
+template <class TX, class TY>
+constexpr int kE = sizeof(TX) == 4 || sizeof(TY) == 4 ? 4 : 8;
+
+template <class TX, class TY, int L, int Q>
+__global__ __launch_bounds__(kBlock<L>) void norm_forward(const TX* __restrict__ x, int64_t ld_x, int64_t R, int N,
+                                                          const float* __restrict__ gamma,
+                                                          const float* __restrict__ beta, float eps, TY* __restrict__ y,
+                                                          int64_t ld_y, float* __restrict__ mean,
+                                                          float* __restrict__ rstd) {
+  constexpr int E = kE<TX, TY>;
+  constexpr int G = kBlock<L> / L;  // rows of a block
+  __shared__ float red[kBlock<L> / kWave];
+  const int64_t r = (int64_t)blockIdx.x * G + threadIdx.x / L;
+  const int l = threadIdx.x % L;
+  if (L <= kWave && r >= R) return;  // whole groups; with L > kWave a block is one row
+  const TX* row = x + r * ld_x;
+  float v[Q][E];
+  float s = 0.0f;
+#pragma unroll
+  for (int q = 0; q < Q; ++q) load_in<TX, E>(row, (q * L + l) * E, N, v[q]);
+#pragma unroll
+  for (int q = 0; q < Q; ++q)
+#pragma unroll
+    for (int u = 0; u < E; ++u) s += v[q][u];
+  const float m = group_sum<L>(s, red) / (float)N;
+  float d2 = 0.0f;
+#pragma unroll
+  for (int q = 0; q < Q; ++q)
+#pragma unroll
+    for (int u = 0; u < E; ++u) {
+      const float d = v[q][u] - m;
+      v[q][u] = d;
+      if ((q * L + l) * E + u < N) d2 = fmaf(d, d, d2);
+    }
+  const float k = 1.0f / sqrtf(group_sum<L>(d2, red) / (float)N + eps);
+  TY* out = y + r * ld_y;
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const int i = (q * L + l) * E;
+    if (i >= N) continue;
+    float g[E], b[E];
+    if (gamma) load_in<float, E>(gamma, i, N, g);
+    if (beta) load_in<float, E>(beta, i, N, b);
+#pragma unroll
+    for (int u = 0; u < E; ++u) {
+      const float h = v[q][u] * k;
+      v[q][u] = gamma ? (beta ? fmaf(h, g[u], b[u]) : h * g[u]) : (beta ? h + b[u] : h);
+    }
+    store_in<TY, E>(out, i, N, v[q]);
+  }
+  if (l == 0) {
+    if (mean) mean[r] = m;
+    if (rstd) rstd[r] = k;
+  }
+}
+
+// dx, and a block's shares of dgamma and dbeta to part[block][2][N] (part NULL: none are wanted).
+template <class TX, class TY, int L, int Q>
+__global__ __launch_bounds__(kBlock<L>) void norm_backward(const TY* __restrict__ dy, int64_t ld_dy,
+                                                           const TX* __restrict__ x, int64_t ld_x, int64_t R, int N,
+                                                           const float* __restrict__ gamma,
+                                                           const float* __restrict__ mean,
+                                                           const float* __restrict__ rstd, TX* __restrict__ dx,
+                                                           int64_t ld_dx, float* __restrict__ part) {
+  constexpr int E = kE<TX, TY>;
+  constexpr int G = kBlock<L> / L;
+  __shared__ float red[kBlock<L> / kWave];
+  extern __shared__ float share[];  // [G][L * E] of one vector of the groups' shares
+  const int g = threadIdx.x / L, l = threadIdx.x % L;
+  float dg[Q][E], db[Q][E];
+#pragma unroll
+  for (int q = 0; q < Q; ++q)
+#pragma unroll
+    for (int u = 0; u < E; ++u) dg[q][u] = db[q][u] = 0.0f;
+  for (int64_t r0 = (int64_t)blockIdx.x * G; r0 < R; r0 += (int64_t)gridDim.x * G) {
+    const int64_t r = r0 + g;
+    if (r >= R) break;  // with L > kWave a block is one row: all its threads or none
+    const float m = mean[r], k = rstd[r];
+    float h[Q][E], a[Q][E];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      load_in<TX, E>(x + r * ld_x, (q * L + l) * E, N, h[q]);
+      load_in<TY, E>(dy + r * ld_dy, (q * L + l) * E, N, a[q]);
+    }
+    float s = 0.0f, sh = 0.0f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int i = (q * L + l) * E;
+      float w[E];
+      if (gamma) load_in<float, E>(gamma, min(i, N), N, w);
+#pragma unroll
+      for (int u = 0; u < E; ++u) {
+        h[q][u] = (h[q][u] - m) * k;
+        if (part) {
+          dg[q][u] = fmaf(a[q][u], h[q][u], dg[q][u]);
+          db[q][u] += a[q][u];
+        }
+        if (gamma) a[q][u] *= w[u];
+        s += a[q][u];  // 0 past the row's end
+        sh = fmaf(a[q][u], h[q][u], sh);
+      }
+    }
+    if (dx) {
+      s = group_sum<L>(s, red) / (float)N;
+      sh = group_sum<L>(sh, red) / (float)N;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const int i = (q * L + l) * E;
+        if (i >= N) continue;
+        float o[E];
+#pragma unroll
+        for (int u = 0; u < E; ++u) o[u] = k * (a[q][u] - s - h[q][u] * sh);
+        store_in<TX, E>(dx + r * ld_dx, i, N, o);
+      }
+    }
+  }
+  if (!part) return;
+  float* mine = part + (size_t)blockIdx.x * 2 * N;
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const int i = (q * L + l) * E;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      float t[E];
+#pragma unroll
+      for (int u = 0; u < E; ++u) t[u] = which ? db[q][u] : dg[q][u];
+      if constexpr (G > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < E; ++u) share[(g * L + l) * E + u] = t[u];
+        __syncthreads();
+        if (g == 0) {
+          for (int o = 1; o < G; ++o)
+#pragma unroll
+            for (int u = 0; u < E; ++u) t[u] += share[(o * L + l) * E + u];
+        }
+      }
+      if (g == 0 && i < N) store_in<float, E>(mine + (size_t)which * N, i, N, t);
+    }
+  }
+}
+
+// dgamma and dbeta: the sums of the parts' columns, in float64. A block takes 64 columns, its wavefronts every
+// kColumnWaves-th part.
+constexpr int kColumnWaves = 16;
+__global__ __launch_bounds__(kColumnWaves * kWave) void norm_columns(const float* __restrict__ part, int n, int N,
+                                                                     float* __restrict__ dgamma,
+                                                                     float* __restrict__ dbeta) {
+  __shared__ double sum[kColumnWaves][kWave];
+  const int w = threadIdx.x / kWave, l = lane_id();
+  const int64_t j = (int64_t)blockIdx.x * kWave + l;  // of 2 N: dgamma, then dbeta
+  double s = 0.0;
+  if (j < 2 * (int64_t)N) {
+#pragma unroll 8
+    for (int p = w; p < n; p += kColumnWaves) s += (double)part[(size_t)p * 2 * N + j];
+  }
+  sum[w][l] = s;
+  __syncthreads();
+  if (w == 0 && j < 2 * (int64_t)N) {
+    for (int o = 1; o < kColumnWaves; ++o) s += sum[o][l];
+    float* out = j < N ? dgamma : dbeta;
+    if (out) out[j < N ? j : j - N] = (float)s;
+  }
+}
+
+// Rows beyond a block's registers: a block walks its row three times.
+constexpr int kLong = 1024;
+template <class TX, class TY>
+__global__ __launch_bounds__(kLong) void norm_forward_long(const TX* __restrict__ x, int64_t ld_x, int N,
+                                                           const float* __restrict__ gamma,
+                                                           const float* __restrict__ beta, float eps, TY* __restrict__ y,
+                                                           int64_t ld_y, float* __restrict__ mean,
+                                                           float* __restrict__ rstd) {
+  constexpr int E = kE<TX, TY>;
+  __shared__ float red[kLong / kWave];
+  const int64_t r = blockIdx.x;
+  const TX* row = x + r * ld_x;
+  float s = 0.0f;
+  for (int i = threadIdx.x * E; i < N; i += kLong * E) {
+    float v[E];
+    load_in<TX, E>(row, i, N, v);
+#pragma unroll
+    for (int u = 0; u < E; ++u) s += v[u];
+  }
+  const float m = group_sum<kLong>(s, red) / (float)N;
+  float d2 = 0.0f;
+  for (int i = threadIdx.x * E; i < N; i += kLong * E) {
+    float v[E];
+    load_in<TX, E>(row, i, N, v);
+#pragma unroll
+    for (int u = 0; u < E; ++u)
+      if (i + u < N) d2 = fmaf(v[u] - m, v[u] - m, d2);
+  }
+  const float k = 1.0f / sqrtf(group_sum<kLong>(d2, red) / (float)N + eps);
+  for (int i = threadIdx.x * E; i < N; i += kLong * E) {
+    float v[E], g[E], b[E];
+    load_in<TX, E>(row, i, N, v);
+    if (gamma) load_in<float, E>(gamma, i, N, g);
+    if (beta) load_in<float, E>(beta, i, N, b);
+#pragma unroll
+    for (int u = 0; u < E; ++u) {
+      const float h = (v[u] - m) * k;
+      v[u] = gamma ? (beta ? fmaf(h, g[u], b[u]) : h * g[u]) : (beta ? h + b[u] : h);
+    }
+    store_in<TY, E>(y + r * ld_y, i, N, v);
+  }
+  if (threadIdx.x == 0) {
+    if (mean) mean[r] = m;
+    if (rstd) rstd[r] = k;
+  }
+}
+
+template <class TX, class TY>
+__global__ __launch_bounds__(kLong) void norm_backward_long(const TY* __restrict__ dy, int64_t ld_dy,
+                                                            const TX* __restrict__ x, int64_t ld_x, int N,
+                                                            const float* __restrict__ gamma,
+                                                            const float* __restrict__ mean,
+                                                            const float* __restrict__ rstd, TX* __restrict__ dx,
+                                                            int64_t ld_dx) {
+  constexpr int E = kE<TX, TY>;
+  __shared__ float red[kLong / kWave];
+  const int64_t r = blockIdx.x;
+  const float m = mean[r], k = rstd[r];
+  float s = 0.0f, sh = 0.0f;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int i = threadIdx.x * E; i < N; i += kLong * E) {
+      float h[E], a[E], w[E];
+      load_in<TX, E>(x + r * ld_x, i, N, h);
+      load_in<TY, E>(dy + r * ld_dy, i, N, a);
+      if (gamma) load_in<float, E>(gamma, i, N, w);
+#pragma unroll
+      for (int u = 0; u < E; ++u) {
+        h[u] = (h[u] - m) * k;
+        if (gamma) a[u] *= w[u];
+        if (pass == 0) {
+          s += a[u];
+          sh = fmaf(a[u], h[u], sh);
+        } else {
+          a[u] = k * (a[u] - s - h[u] * sh);
+        }
+      }
+      if (pass) store_in<TX, E>(dx + r * ld_dx, i, N, a);
+    }
+    if (pass == 0) {
+      s = group_sum<kLong>(s, red) / (float)N;
+      sh = group_sum<kLong>(sh, red) / (float)N;
+    }
+  }
+}
+
+// Long rows' shares of dgamma and dbeta: a thread a column, part p the rows p, p + gridDim.y, ...
+template <class TX, class TY>
+__global__ __launch_bounds__(256) void norm_columns_long(const TY* __restrict__ dy, int64_t ld_dy,
+                                                         const TX* __restrict__ x, int64_t ld_x, int64_t R, int N,
+                                                         const float* __restrict__ mean,
+                                                         const float* __restrict__ rstd, float* __restrict__ part) {
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j >= N) return;
+  float dg = 0.0f, db = 0.0f;
+  for (int64_t r = blockIdx.y; r < R; r += gridDim.y) {
+    const float d = to_float(dy[r * ld_dy + j]);
+    dg = fmaf(d, (to_float(x[r * ld_x + j]) - mean[r]) * rstd[r], dg);
+    db += d;
+  }
+  part[(size_t)blockIdx.y * 2 * N + j] = dg;
+  part[(size_t)blockIdx.y * 2 * N + N + j] = db;
+}
+
+// How a row of N is spread: lanes and vectors a lane; L 0: beyond a block's registers.
+struct Shape {
+  int L, Q;
+};
+Shape shape_of(int N, int E) {
+  const int v = (N + E - 1) / E;
+  if (v <= 16) return {16, 1};
+  if (v <= 64) return {64, 1};
+  if (v <= 128) return {64, 2};
+  if (v <= 256) return {64, 4};
+  if (v <= 512) return {256, 2};
+  if (v <= 1024) return {256, 4};
+  if (v <= 2048) return {1024, 2};
+  if (v <= 4096) return {1024, 4};
+  return {0, 0};
+}
+
+int vector_of(int x_dtype, int y_dtype) { return x_dtype == SNN_F32 || y_dtype == SNN_F32 ? 4 : 8; }
+
+// Blocks of the backward pass, each with a partial row: enough for four a compute unit, few enough that a block has
+// several rows to add up.
+int parts_of(int64_t R, int N, int E) {
+  const Shape sh = shape_of(N, E);
+  if (!sh.L) return (int)std::min<int64_t>(R, 64);
+  const int G = sh.L >= 256 ? 1 : 256 / sh.L;
+  const int64_t blocks = (R + G - 1) / G;
+  return (int)std::min<int64_t>(blocks, 1024);
+}
+
+constexpr int64_t kLaunchRows = (int64_t)1 << 21;  // a dispatch counts threads in 32 bits
+
+template <class TX, class TY>
+void forward(const void* x, int64_t ld_x, int64_t R, int N, const float* gamma, const float* beta, float eps, void* y,
+             int64_t ld_y, float* mean, float* rstd, hipStream_t s) {
+  const Shape sh = shape_of(N, kE<TX, TY>);
+  for (int64_t r = 0; r < R; r += kLaunchRows) {
+    const int64_t n = std::min(kLaunchRows, R - r);
+    const TX* px = static_cast<const TX*>(x) + r * ld_x;
+    TY* py = static_cast<TY*>(y) + r * ld_y;
+    float *pm = mean ? mean + r : nullptr, *pr = rstd ? rstd + r : nullptr;
+#define SNN_N(L_, Q_)                                                                                            \
+  hipLaunchKernelGGL((norm_forward<TX, TY, L_, Q_>), dim3((unsigned)((n + kBlock<L_> / L_ - 1) / (kBlock<L_> / L_))), \
+                     dim3(kBlock<L_>), 0, s, px, ld_x, n, N, gamma, beta, eps, py, ld_y, pm, pr)
+    if (sh.L == 16) SNN_N(16, 1);
+    else if (sh.L == 64 && sh.Q == 1) SNN_N(64, 1);
+    else if (sh.L == 64 && sh.Q == 2) SNN_N(64, 2);
+    else if (sh.L == 64) SNN_N(64, 4);
+    else if (sh.L == 256 && sh.Q == 2) SNN_N(256, 2);
+    else if (sh.L == 256) SNN_N(256, 4);
+    else if (sh.L == 1024 && sh.Q == 2) SNN_N(1024, 2);
+    else if (sh.L == 1024) SNN_N(1024, 4);
+    else
+      hipLaunchKernelGGL((norm_forward_long<TX, TY>), dim3((unsigned)n), dim3(kLong), 0, s, px, ld_x, N, gamma, beta, eps,
+                         py, ld_y, pm, pr);
+#undef SNN_N
+  }
+}
+
+template <class TX, class TY>
+void backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int64_t R, int N, const float* gamma,
+              const float* mean, const float* rstd, void* dx, int64_t ld_dx, float* part, int parts, hipStream_t s) {
+  constexpr int E = kE<TX, TY>;
+  const Shape sh = shape_of(N, E);
+  const TY* pdy = static_cast<const TY*>(dy);
+  const TX* px = static_cast<const TX*>(x);
+  TX* pdx = static_cast<TX*>(dx);
+#define SNN_N(L_, Q_)                                                                                                \
+  hipLaunchKernelGGL((norm_backward<TX, TY, L_, Q_>), dim3((unsigned)parts), dim3(kBlock<L_>),                        \
+                     L_ < 256 ? 256 * E * sizeof(float) : 0, s, pdy, ld_dy, px, ld_x, R, N, gamma, mean, rstd, pdx,  \
+                     ld_dx, part)
+  if (sh.L == 16) SNN_N(16, 1);
+  else if (sh.L == 64 && sh.Q == 1) SNN_N(64, 1);
+  else if (sh.L == 64 && sh.Q == 2) SNN_N(64, 2);
+  else if (sh.L == 64) SNN_N(64, 4);
+  else if (sh.L == 256 && sh.Q == 2) SNN_N(256, 2);
+  else if (sh.L == 256) SNN_N(256, 4);
+  else if (sh.L == 1024 && sh.Q == 2) SNN_N(1024, 2);
+  else if (sh.L == 1024) SNN_N(1024, 4);
+  else {
+    for (int64_t r = 0; pdx && r < R; r += kLaunchRows)
+      hipLaunchKernelGGL((norm_backward_long<TX, TY>), dim3((unsigned)std::min(kLaunchRows, R - r)), dim3(kLong), 0, s,
+                         pdy + r * ld_dy, ld_dy, px + r * ld_x, ld_x, N, gamma, mean + r, rstd + r, pdx + r * ld_dx, ld_dx);
+    if (part)
+      hipLaunchKernelGGL((norm_columns_long<TX, TY>), dim3((unsigned)((N + 255) / 256), (unsigned)parts), dim3(256), 0, s,
+                         pdy, ld_dy, px, ld_x, R, N, mean, rstd, part);
+  }
+#undef SNN_N
+}
+
+snn_status check_sizes(int x_dtype, int y_dtype, int64_t R, int N) {
+  if (!dtype_size(x_dtype) || !dtype_size(y_dtype) || R <= 0 || N <= 0) return SNN_ERR_INVALID_ARG;
+  if (R > INT32_MAX || N > kMaxWidth) return SNN_ERR_UNSUPPORTED;
+  return SNN_OK;
+}
+
+// The pairs of types: F(TX, TY).
+#define SNN_PAIRS(F)                                                                          \
+  if (x_dtype == SNN_F32 && y_dtype == SNN_F32) F(float, float);                              \
+  else if (x_dtype == SNN_F32 && y_dtype == SNN_BF16) F(float, Bf16);                         \
+  else if (x_dtype == SNN_F32) F(float, F16);                                                 \
+  else if (x_dtype == SNN_BF16 && y_dtype == SNN_F32) F(Bf16, float);                         \
+  else if (x_dtype == SNN_BF16 && y_dtype == SNN_BF16) F(Bf16, Bf16);                         \
+  else if (x_dtype == SNN_BF16) F(Bf16, F16);                                                 \
+  else if (y_dtype == SNN_F32) F(F16, float);                                                 \
+  else if (y_dtype == SNN_BF16) F(F16, Bf16);                                                 \
+  else F(F16, F16)
+
+}  // namespace
+}  // namespace snn
+
+using namespace snn;
+
+extern "C" snn_status snn_layer_norm(const void* x, int x_dtype, int64_t R, int N, int64_t ld_x, const float* gamma,
+                                     const float* beta, float eps, void* y, int y_dtype, int64_t ld_y, float* mean,
+                                     float* rstd, void* stream) {
+  if (!x || !y) return SNN_ERR_INVALID_ARG;
+  if (const snn_status st = check_sizes(x_dtype, y_dtype, R, N)) return st;
+  if (ld_x < N || ld_y < N || !(eps >= 0.0f) || isinf(eps)) return SNN_ERR_INVALID_ARG;
+  if (misaligned(x, x_dtype) || misaligned(y, y_dtype)) return SNN_ERR_INVALID_ARG;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+#define SNN_F(TX, TY) forward<TX, TY>(x, ld_x, R, N, gamma, beta, eps, y, ld_y, mean, rstd, s)
+  SNN_PAIRS(SNN_F);
+#undef SNN_F
+  return launch_status();
+}
+
+extern "C" size_t snn_layer_norm_grad_workspace(int x_dtype, int y_dtype, int64_t R, int N) {
+  if (check_sizes(x_dtype, y_dtype, R, N) != SNN_OK) return 0;
+  return align256((size_t)parts_of(R, N, vector_of(x_dtype, y_dtype)) * 2 * N * sizeof(float));
+}
+
+extern "C" snn_status snn_layer_norm_grad(const void* dy, int y_dtype, int64_t ld_dy, const void* x, int x_dtype,
+                                          int64_t ld_x, int64_t R, int N, const float* gamma, const float* mean,
+                                          const float* rstd, void* dx, int64_t ld_dx, float* dgamma, float* dbeta,
+                                          void* workspace, size_t workspace_bytes, void* stream) {
+  if (!dy || !x || !mean || !rstd || (!dx && !dgamma && !dbeta)) return SNN_ERR_INVALID_ARG;
+  if (const snn_status st = check_sizes(x_dtype, y_dtype, R, N)) return st;
+  if (ld_dy < N || ld_x < N || (dx && ld_dx < N)) return SNN_ERR_INVALID_ARG;
+  if (misaligned(dy, y_dtype) || misaligned(x, x_dtype) || misaligned(dx, x_dtype)) return SNN_ERR_INVALID_ARG;
+  const bool columns = dgamma || dbeta;
+  if (columns && (!workspace || workspace_bytes < snn_layer_norm_grad_workspace(x_dtype, y_dtype, R, N)))
+    return SNN_ERR_INVALID_ARG;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  float* part = columns ? static_cast<float*>(workspace) : nullptr;
+  const int parts = parts_of(R, N, vector_of(x_dtype, y_dtype));
+#define SNN_F(TX, TY) backward<TX, TY>(dy, ld_dy, x, ld_x, R, N, gamma, mean, rstd, dx, ld_dx, part, parts, s)
+  SNN_PAIRS(SNN_F);
+#undef SNN_F
+  if (columns)
+    hipLaunchKernelGGL(norm_columns, dim3((unsigned)((2 * (int64_t)N + kWave - 1) / kWave)), dim3(kColumnWaves * kWave), 0,
+                       s, part, parts, N, dgamma, dbeta);
+  return launch_status();
+}

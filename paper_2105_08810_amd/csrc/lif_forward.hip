@@ -1086,6 +1086,18 @@ extern "C" snn_status snn_lif_forward_traces(const uint8_t* s_in, const float* W
                           active_bits, stream);
 }
 
+extern "C" snn_status snn_lif_forward_currents(float* V, int T, int B, int N, float alpha, float theta, float b_th,
+                                               uint8_t* s_out, float* trace_out, float alpha_next,
+                                               uint64_t* active_bits, void* stream) {
+  if (!V || !s_out || bad_dim(T) || bad_dim(B) || bad_dim(N) || too_big(T, B, N)) return SNN_ERR_INVALID_ARG;
+  if (bad_alpha(alpha) || isnan(theta) || (trace_out && bad_alpha(alpha_next))) return SNN_ERR_INVALID_ARG;
+  if (active_bits && (isnan(b_th) || b_th < 0.0f)) return SNN_ERR_INVALID_ARG;
+  const int nv = (int)(((size_t)B * N + kScanThreads - 1) / kScanThreads);
+  hipLaunchKernelGGL(lif_scan, dim3((unsigned)nv), dim3(kScanThreads), 0, static_cast<hipStream_t>(stream), nullptr, T, B,
+                     1, N, alpha, theta, b_th, V, s_out, nullptr, trace_out, alpha_next, active_bits, nv);
+  return launch_status();
+}
+
 namespace {
 
 // snn_conv_lif_forward, and with P the pooling and the pooled trace.

@@ -66,6 +66,16 @@ _SIGNATURES = {
     "snn_readout_distill": (_I, [_P, _I, _I64, _I, _I64, _P, _P, _P, _I, _F, _P, _P, _P, _P, _I64, _I, _P, _SZ, _P]),
     "snn_readout_sample_workspace": (_SZ, [_I64, _I, _I]),
     "snn_readout_sample": (_I, [_P, _I, _I64, _I, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "snn_lif_forward_currents": (_I, [_P, _I, _I, _I, _F, _F, _F, _P, _P, _F, _P, _P]),
+    "snn_embed": (_I, [_P, _I, _I64, _I, _I64, _P, _I64, _F, _P, _I64, _P]),
+    "snn_embed_grad_workspace": (_SZ, [_I, _I64, _I, _I64]),
+    "snn_embed_grad": (_I, [_P, _I64, _P, _I, _I64, _I64, _I, _F, _P, _I64, _I, _P, _SZ, _P]),
+    "snn_layer_norm": (_I, [_P, _I, _I64, _I, _I64, _P, _P, _F, _P, _I, _I64, _P, _P, _P]),
+    "snn_layer_norm_grad_workspace": (_SZ, [_I, _I, _I64, _I]),
+    "snn_layer_norm_grad": (_I, [_P, _I, _I64, _P, _I, _I64, _I64, _I, _P, _P, _P, _P, _I64, _P, _P, _P, _SZ, _P]),
+    "snn_linear_ce_workspace": (_SZ, [_I, _I64, _I, _I, _I]),
+    "snn_linear_ce": (_I, [_P, _P, _I, _I64, _I, _I, _I64, _I64, _P, _P, _P, _P, _P, _I64, _P, _I64, _P, _SZ, _P]),
+    "snn_leak_grad": (_I, [_P, _P, _P, _P, _I64, _I, _I, _I, _F, _P, _P, _P, _I64, _P]),
     "snn_activity_reg_workspace": (_SZ, [_I, _I, _I]),
     "snn_activity_reg": (_I, [_P, _I, _I, _I, _F, _F, _F, _F, _P, _P, _P, _P, _SZ, _P]),
     "snn_activity_reg_grad": (_I, [_P, _I, _I, _I, _P, _P, _I64, _P, _P]),
@@ -431,6 +441,110 @@ def snn_readout_sample(logits, u, temperature, top_k, top_p, min_p, cls, logp=No
         _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
 
 
+def snn_lif_forward_currents(V, T, B, N, alpha, theta, b_th, s_out, trace_out=None, alpha_next=1.0, active_bits=None,
+                             stream=None):
+    _check("snn_lif_forward_currents", lib().snn_lif_forward_currents(
+        _ptr(V, torch.float32, "V"), T, B, N, float(alpha), float(theta), float(b_th), _ptr(s_out, torch.uint8, "s_out"),
+        _ptr(trace_out, torch.float32, "trace_out"), float(alpha_next), _ptr(active_bits, torch.int64, "active_bits"),
+        _stream(stream)))
+
+
+def snn_embed(E, ids, scale, out, stream=None):
+    p, code, V, N, ld = _rows(E, "E")
+    o, code_o, R, N_o, ld_o = _rows(out, "out")
+    if (code_o, N_o) != (code, N):
+        raise ValueError("out must have the type and the width of E")
+    _check("snn_embed", lib().snn_embed(p, code, V, N, ld, _of_rows(ids, R, torch.int32, "ids"), R, float(scale), o, ld_o,
+                                        _stream(stream)))
+
+
+def snn_embed_grad_workspace(dtype, V, N, R) -> int:
+    return int(lib().snn_embed_grad_workspace(_DTYPES[dtype], V, N, R))
+
+
+def snn_embed_grad(ids, dout, scale, dE, accumulate, ws, stream=None):
+    o, code, R, N, ld_o = _rows(dout, "dout")
+    p, code_e, V, N_e, ld_e = _rows(dE, "dE")
+    if (code_e, N_e) != (code, N):
+        raise ValueError("dE must have the type and the width of dout")
+    _check("snn_embed_grad", lib().snn_embed_grad(
+        _of_rows(ids, R, torch.int32, "ids"), R, o, code, ld_o, V, N, float(scale), p, ld_e, int(accumulate),
+        _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
+
+
+def snn_layer_norm(x, gamma, beta, eps, y, mean=None, rstd=None, stream=None):
+    p, code, R, N, ld = _rows(x, "x")
+    o, code_o, R_o, N_o, ld_o = _rows(y, "y")
+    if (R_o, N_o) != (R, N):
+        raise ValueError("y must have the shape of x")
+    f32 = torch.float32
+    _check("snn_layer_norm", lib().snn_layer_norm(
+        p, code, R, N, ld, _of_rows(gamma, N, f32, "gamma"), _of_rows(beta, N, f32, "beta"), float(eps), o, code_o, ld_o,
+        _of_rows(mean, R, f32, "mean"), _of_rows(rstd, R, f32, "rstd"), _stream(stream)))
+
+
+def snn_layer_norm_grad_workspace(x_dtype, y_dtype, R, N) -> int:
+    return int(lib().snn_layer_norm_grad_workspace(_DTYPES[x_dtype], _DTYPES[y_dtype], R, N))
+
+
+def snn_layer_norm_grad(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws, stream=None):
+    d, code_y, R, N, ld_dy = _rows(dy, "dy")
+    p, code, R_x, N_x, ld = _rows(x, "x")
+    if (R_x, N_x) != (R, N):
+        raise ValueError("x must have the shape of dy")
+    g, ld_dx = None, 0
+    if dx is not None:
+        g, code_g, R_g, N_g, ld_dx = _rows(dx, "dx")
+        if (code_g, R_g, N_g) != (code, R, N):
+            raise ValueError("dx must have the type and the shape of x")
+    f32 = torch.float32
+    _check("snn_layer_norm_grad", lib().snn_layer_norm_grad(
+        d, code_y, ld_dy, p, code, ld, R, N, _of_rows(gamma, N, f32, "gamma"), _of_rows(mean, R, f32, "mean"),
+        _of_rows(rstd, R, f32, "rstd"), g, ld_dx, _of_rows(dgamma, N, f32, "dgamma"), _of_rows(dbeta, N, f32, "dbeta"),
+        _ptr(ws, None, "workspace"), _nbytes(ws), _stream(stream)))
+
+
+def snn_linear_ce_workspace(dtype, R, H, C, grad) -> int:
+    return int(lib().snn_linear_ce_workspace(_DTYPES[dtype], R, H, C, int(grad)))
+
+
+def snn_linear_ce(x, W, targets, weight, loss, row_loss, dx, dW, ws, stream=None):
+    p, code, R, H, ld = _rows(x, "x")
+    w, code_w, H_w, C, ld_w = _rows(W, "W")
+    if (code_w, H_w) != (code, H):
+        raise ValueError("W must have the type of x and a row for each of its columns")
+    grads = []
+    for t, name, shape in ((dx, "dx", (R, H)), (dW, "dW", (H, C))):
+        if t is None:
+            grads += [None, 0]
+            continue
+        g, code_g, R_g, C_g, ld_g = _rows(t, name)
+        if code_g != code or (R_g, C_g) != shape:
+            raise ValueError(f"{name} must have the type and the shape of {name[1:]}")
+        grads += [g, ld_g]
+    f32 = torch.float32
+    _check("snn_linear_ce", lib().snn_linear_ce(
+        p, w, code, R, H, C, ld, ld_w, _of_rows(targets, R, torch.int32, "targets"), _of_rows(weight, R, f32, "weight"),
+        _of_rows(loss, 1, f32, "loss"), _of_rows(row_loss, R, f32, "row_loss"), *grads, _ptr(ws, None, "workspace"),
+        _nbytes(ws), _stream(stream)))
+
+
+def snn_leak_grad(x, inp, T, B, N, alpha, y, out, stream=None):
+    """inp, out: a Csr over the T*B rows or None for a dense side (Csr.g is inp's factor)."""
+    sides = []
+    for t, csr, name in ((x, inp, "x"), (y, out, "y")):
+        f = _of_rows(t, T * B * N, torch.float32, name) if csr is None else _ptr(t, torch.float32, name)
+        n = 0 if csr is None else min(csr.capacity, t.numel(), csr.col_idx.numel())
+        rp = None if csr is None else _of_rows(csr.row_ptr, T * B + 1, torch.int32, f"{name}'s row_ptr")
+        sides.append((f, rp, None if csr is None else _ptr(csr.col_idx, torch.int32, f"{name}'s col_idx"), n))
+    (px, irp, icol, icap), (py, orp, ocol, ocap) = sides
+    g = None if inp is None or inp.g is None else _ptr(inp.g, torch.float32, "inp.g")
+    if g is not None:
+        icap = min(icap, inp.g.numel())
+    _check("snn_leak_grad", lib().snn_leak_grad(px, irp, icol, g, icap, T, B, N, float(alpha), py, orp, ocol, ocap,
+                                                _stream(stream)))
+
+
 def snn_activity_reg_workspace(T, B, N) -> int:
     return int(lib().snn_activity_reg_workspace(T, B, N))
 
@@ -731,6 +845,96 @@ def readout_sample(logits: torch.Tensor, u, temperature=None, top_k=None, top_p=
         _of_rows(top_k, R, torch.int32, "top_k"), _of_rows(top_p, R, f32, "top_p"), _of_rows(min_p, R, f32, "min_p"),
         cls.data_ptr(), logp.data_ptr(), kept.data_ptr(), _ptr(ws, None, "workspace"), _nbytes(ws), _stream()))
     return cls, logp, kept
+
+
+def embed(E: torch.Tensor, ids: torch.Tensor, scale=1.0, out=None, stream=None):
+    """Rows of an embedding E [V, N] picked by ids [...] (int32), times scale: [..., N]."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return embed(E, ids, scale, out)
+    if out is None:
+        out = torch.empty((*ids.shape, E.shape[-1]), dtype=E.dtype, device=E.device)
+    snn_embed(E, ids, scale, out if out.dim() > 1 else out.view(1, -1))
+    return out
+
+
+def embed_grad(ids: torch.Tensor, dout: torch.Tensor, V: int, scale=1.0, dE=None, accumulate=False, ws=None, stream=None):
+    """Gradient [V, N] of an embedding from that of its picked rows, dout [..., N]; one that is given is written, or
+    added to with accumulate."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return embed_grad(ids, dout, V, scale, dE, accumulate, ws)
+    if accumulate and dE is None:
+        raise ValueError("embed_grad: accumulate needs a dE to add to")
+    N = dout.shape[-1]
+    if dE is None:
+        dE = torch.empty((V, N), dtype=dout.dtype, device=dout.device)
+    elif dE.shape[0] != V:
+        raise ValueError(f"dE must have {V} rows")
+    if ws is None:
+        ws = workspace(snn_embed_grad_workspace(dout.dtype, V, N, ids.numel()), dout.device)
+    snn_embed_grad(ids, dout if dout.dim() > 1 else dout.view(1, -1), scale, dE, accumulate, ws)
+    return dE
+
+
+def layer_norm(x: torch.Tensor, gamma=None, beta=None, eps=1e-5, out_dtype=None, out=None, stream=None):
+    """Layer norm of rows x [..., N]: (y like x, of out_dtype; mean [...], rstd [...])."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return layer_norm(x, gamma, beta, eps, out_dtype, out)
+    if out is None:
+        out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
+    snn_layer_norm(x, gamma, beta, eps, out, mean, rstd)
+    return out, mean, rstd
+
+
+def layer_norm_grad(dy: torch.Tensor, x, gamma, mean, rstd, want_dx=True, want_dgamma=True, want_dbeta=True, ws=None,
+                    stream=None):
+    """Backward pass of layer_norm: (dx like x, dgamma [N], dbeta [N]), None for what is not wanted."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return layer_norm_grad(dy, x, gamma, mean, rstd, want_dx, want_dgamma, want_dbeta, ws)
+    N, dev = x.shape[-1], x.device
+    dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if want_dx else None
+    dgamma = torch.empty(N, dtype=torch.float32, device=dev) if want_dgamma else None
+    dbeta = torch.empty(N, dtype=torch.float32, device=dev) if want_dbeta else None
+    if ws is None and (want_dgamma or want_dbeta):
+        ws = workspace(snn_layer_norm_grad_workspace(x.dtype, dy.dtype, mean.numel(), N), dev)
+    snn_layer_norm_grad(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws)
+    return dx, dgamma, dbeta
+
+
+def linear_ce(x: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, weight=None, want_grad=True, ws=None, stream=None):
+    """Cross entropy of the logits x W of rows x [..., H] and W [H, C] against targets [...]: (loss [1], row_loss [...],
+    dx like x or None, dW [H, C] or None)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return linear_ce(x, W, targets, weight, want_grad, ws)
+    dev = x.device
+    (H, C), R = W.shape, targets.numel()
+    loss = torch.empty(1, dtype=torch.float32, device=dev)
+    row_loss = torch.empty(targets.shape, dtype=torch.float32, device=dev)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if want_grad else None
+    dW = torch.empty((H, C), dtype=W.dtype, device=dev) if want_grad else None
+    if ws is None:
+        ws = workspace(snn_linear_ce_workspace(x.dtype, R, H, C, want_grad), dev)
+    snn_linear_ce(x, W, targets, weight, loss, row_loss, dx, dW, ws)
+    return loss, row_loss, dx, dW
+
+
+def leak_grad(x: torch.Tensor, alpha, shape, inp: Optional[Csr] = None, out: Optional[Csr] = None, y=None, stream=None):
+    """The adjoint of a leaky integration over shape (T, B, N): x dense, or the values at inp's entries (times inp.g);
+    y dense, or the values at out's entries."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return leak_grad(x, alpha, shape, inp, out, y)
+    T, B, N = shape
+    if y is None:
+        y = torch.empty(tuple(shape) if out is None else out.capacity, dtype=torch.float32, device=x.device)
+    snn_leak_grad(x, inp, T, B, N, alpha, y, out)
+    return y
 
 
 def sparse_backward(W, trace_in, alpha, out: Csr, eps_out, inp: Optional[Csr] = None, ws=None, aux_stream=None):

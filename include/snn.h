@@ -651,7 +651,7 @@ snn_status snn_layer_norm_grad(const void* dy, int y_dtype, int64_t ld_dy, const
  *   row_loss float32 [R] (written unless NULL): L_r
  *   dx       R rows of H values of dtype (written unless NULL): weight_r (softmax(z_r) - onehot) W^T
  *   dW       H rows of C values of dtype (written unless NULL): x^T (weight_r (softmax(z_r) - onehot))
- * R up to 2^24, H up to 2^16, C up to 2^20, ld_w up to 2^31 - 1; larger: SNN_ERR_UNSUPPORTED. The workspace query takes
+ * R up to 2^24, H up to 2^16, C up to 2^20, distances of rows up to 2^31 - 1; larger: SNN_ERR_UNSUPPORTED. The workspace query takes
  * whether a gradient is wanted. The workspace grows with R H, and with R times a piece of the classes (bounded).
  */
 size_t snn_linear_ce_workspace(int dtype, int64_t R, int H, int C, int grad);

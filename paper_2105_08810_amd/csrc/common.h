@@ -94,7 +94,8 @@ ColsParts cols_enqueue(const float* trace_in, int T, int B, int N_in, int N_out,
                        void* workspace, const Gate& gate, hipStream_t s);
 
 // Dense float32 products (gemm.hip). K slice z of `splits` goes to C + z * c_split.
-//   gemm_split_km  C = sum_k A[k, m] B[k, n], operands in three bf16 parts, float32 sums
+//   gemm_split_km  C = sum_k A[k, m] B[k, n], operands in three bf16 parts, float32 sums; with live only the rows k of A
+//                  whose bit (k of word k / 32) is set are taken (the others as 0, whatever they hold)
 //   gemm_split_kc  C = sum_k A[m, k] B[n, k], the same; C += with accumulate
 //   gemm_split_kr  C = sum_k A[m, k] B[k, n], the same
 //   gemm_f64_km    C = sum_k A[k, m] B[k, n], products and sums in float64
@@ -106,7 +107,7 @@ struct SplitPlan {
 };
 SplitPlan plan_splits(int M, int N, int K, double mac_rate);
 void gemm_split_km(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc, int splits,
-                   size_t c_split, hipStream_t s);
+                   size_t c_split, hipStream_t s, const uint32_t* live = nullptr);
 void gemm_split_kc(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
                    hipStream_t s, bool accumulate = false);
 void gemm_split_kr(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,

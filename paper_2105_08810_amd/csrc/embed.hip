@@ -4,11 +4,11 @@
 //
 // Both are streams: the lookup reads and writes R rows of N, the gradient reads R rows and writes V. A token's rows are
 // summed in their order, so the rows are first sorted by token (stable):
-//   up to kRankRows rows: every row counts the rows that come before it (embed_rank, one launch, R^2 comparisons)
+//   up to 16384 rows: every row counts the rows that come before it (embed_rank, one launch, R^2 comparisons)
 //   more: by digits of 9 bits from the lowest on, a pass of counts, their prefix and places each
 // and the sorted rows are cut into chunks of `per` rows: embed_sum sums the runs of a token inside a chunk and writes the
-// gradient of tokens that lie wholly in one; what reaches over a chunk's end is kept as a partial sum, which embed_rest
-// adds up in order while it clears the rows of tokens that did not occur. Frequent tokens (a tenth of a text is one
+// gradient of tokens that lie wholly in one; what reaches over a chunk's end is kept as partial sums, which embed_rest
+// adds up in a fixed order while it clears the rows of tokens that did not occur. Frequent tokens (a tenth of a text is one
 // token) so are the work of many blocks, and the result does not depend on which of them ends first. Sums are float32
 // over at most 128 rows, then over the chunks; a result is rounded once.
 #include <algorithm>
@@ -21,12 +21,17 @@ namespace {
 using namespace vectors;
 
 constexpr int kThreads = 256;
-constexpr int kRankRows = 8192;    // rows sorted by counting
+constexpr int kRankRows = 16384;   // rows sorted by counting (64 KB of keys in LDS)
+constexpr int kRankThreads = 1024;
+constexpr int kRankShare = 32;     // threads that share a row's comparisons
 constexpr int kDigit = 9;          // bits of a digit
 constexpr int kBins = 1 << kDigit;
 constexpr int kSortThreads = 256;
-constexpr int kSortSteps = 16;     // steps of 64 rows of a wavefront
-constexpr int kSortRows = kSortThreads * kSortSteps;
+// Steps of 64 rows of a wavefront: few where that is needed to fill the card (128000 rows, two passes: counts and places
+// 13 us a pass with 4, 23 with 16), more for the longest lists, whose counts (a block's 512 each) would grow too large.
+constexpr int kFewSteps = 4, kManySteps = 16;
+constexpr int64_t kFewStepsRows = (int64_t)1 << 20;
+int sort_rows(int64_t R) { return kSortThreads * (R <= kFewStepsRows ? kFewSteps : kManySteps); }
 constexpr int kMaxPer = 128;
 constexpr int kMaxWidth = 1 << 20;
 
@@ -41,6 +46,14 @@ int lanes_log2(int N, int E) {
 template <class T>
 constexpr int kE = 16 / (int)sizeof(T);
 
+// x * scale as a float32: the compiler would form a float16 product and its rounding in one instruction, whose results differ
+// from the other types' way (product in float32, then rounded) by the second rounding.
+__device__ __forceinline__ float scaled(float x, float scale) {
+  float p = x * scale;
+  asm("" : "+v"(p));
+  return p;
+}
+
 template <class T>
 __global__ __launch_bounds__(kThreads) void embed_lookup(const T* __restrict__ E, int64_t V, int N, int64_t ld_e,
                                                          const int32_t* __restrict__ ids, int64_t R, float scale,
@@ -53,12 +66,19 @@ __global__ __launch_bounds__(kThreads) void embed_lookup(const T* __restrict__ E
   const bool ok = id >= 0 && id < V;
   const T* e = E + (ok ? id : 0) * ld_e;
   T* o = out + r * ld_out;
-  for (int i = l * kE<T>; i < N; i += lanes * kE<T>) {
-    float x[kE<T>];
-    load_in<T, kE<T>>(e, i, N, x);
+  constexpr int kAhead = 4;  // vectors under way
+  for (int i = l * kE<T>; i < N; i += kAhead * lanes * kE<T>) {
+    Raw<T, kE<T>> raw[kAhead];
 #pragma unroll
-    for (int u = 0; u < kE<T>; ++u) x[u] = ok ? x[u] * scale : 0.0f;
-    store_in<T, kE<T>>(o, i, N, x);
+    for (int q = 0; q < kAhead; ++q) raw[q] = raw_in<T, kE<T>>(e, min(i + q * lanes * kE<T>, N), N);
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) {
+      float x[kE<T>];
+      raw[q].to(x);
+#pragma unroll
+      for (int u = 0; u < kE<T>; ++u) x[u] = ok ? scaled(x[u], scale) : 0.0f;
+      store_past_in<T, kE<T>>(o, min(i + q * lanes * kE<T>, N), N, x);
+    }
   }
 }
 
@@ -74,25 +94,39 @@ __global__ void embed_clear_ends(int32_t* __restrict__ first, int64_t V) {
     first[v] = -1;
 }
 
-// The place of each row among all R <= kRankRows. A block ranks 32 rows, 8 threads a row share the comparisons.
-// first[v] = -1 for every token on the way.
-__global__ __launch_bounds__(kThreads) void embed_rank(const int32_t* __restrict__ ids, int R, int64_t V,
-                                                       uint32_t* __restrict__ keys, int32_t* __restrict__ order,
-                                                       int32_t* __restrict__ first) {
-  __shared__ uint32_t k[kRankRows];
-  for (int i = threadIdx.x; i < R; i += kThreads) k[i] = key_of(ids[i], V);
-  for (int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x; v < V; v += (int64_t)gridDim.x * kThreads) first[v] = -1;
+// The place of each row among all R <= kRankRows: how many rows have a smaller key, or the same and come before it. A block
+// ranks 32 rows, 32 threads share a row, four keys a read. first[v] = -1 for every token on the way. 8192 rows: 9 us
+// (56 with 8 threads a row, 256 a block and a key a read).
+__global__ __launch_bounds__(kRankThreads) void embed_rank(const int32_t* __restrict__ ids, int R, int64_t V,
+                                                           uint32_t* __restrict__ keys, int32_t* __restrict__ order,
+                                                           int32_t* __restrict__ first) {
+  extern __shared__ __attribute__((aligned(16))) uint32_t k[];  // R keys, up to a multiple of 4 of the largest value
+  const int Q = (R + 3) / 4;
+  for (int64_t v = (int64_t)blockIdx.x * kRankThreads + threadIdx.x; v < V; v += (int64_t)gridDim.x * kRankThreads) first[v] = -1;
+  if (blockIdx.x * (kRankThreads / kRankShare) >= (unsigned)R) return;
+  for (int i = threadIdx.x; i < 4 * Q; i += kRankThreads) k[i] = i < R ? key_of(ids[i], V) : 0xffffffffu;
   __syncthreads();
-  const int r = blockIdx.x * 32 + threadIdx.x / 8;
-  const int part = threadIdx.x % 8;
-  if (r >= R) return;
-  const uint32_t mine = k[r];
+  const int r = min(blockIdx.x * (kRankThreads / kRankShare) + threadIdx.x / kRankShare, (unsigned)R - 1);
+  const int part = threadIdx.x % kRankShare;
+  const uint32_t mine = k[r];  // at most 2^31 - 1
+  const int own = r / 4;
+  const uint4* k4 = reinterpret_cast<const uint4*>(k);
   int before = 0;
-  for (int j = part; j < r; j += 8) before += k[j] <= mine;
-  for (int j = r + 1 + part; j < R; j += 8) before += k[j] < mine;
+  const auto count = [&](int q, uint32_t than) {
+    const uint4 x = k4[q];
+    before += (x.x < than) + (x.y < than) + (x.z < than) + (x.w < than);
+  };
+#pragma unroll 4
+  for (int q = part; q < own; q += kRankShare) count(q, mine + 1);
+#pragma unroll 4
+  for (int q = own + 1 + part; q < Q; q += kRankShare) count(q, mine);
+  if (part < 4) {
+    const int j = 4 * own + part;
+    before += k[j] < mine + (j < r ? 1 : 0);
+  }
 #pragma unroll
-  for (int off = 4; off > 0; off >>= 1) before += __shfl_xor(before, off, kWave);
-  if (part == 0) {
+  for (int off = kRankShare / 2; off > 0; off >>= 1) before += __shfl_xor(before, off, kWave);
+  if (part == 0 && blockIdx.x * (kRankThreads / kRankShare) + threadIdx.x / kRankShare < (unsigned)R) {
     keys[before] = mine;
     order[before] = r;
   }
@@ -101,13 +135,14 @@ __global__ __launch_bounds__(kThreads) void embed_rank(const int32_t* __restrict
 __device__ __forceinline__ int digit_of(uint32_t k, int shift) { return (int)(k >> shift) & (kBins - 1); }
 
 // counts[d * blocks + block]: the block's rows with digit d. keys NULL: the rows' own (the first pass).
+template <int kSortSteps>
 __global__ __launch_bounds__(kSortThreads) void embed_count(const uint32_t* __restrict__ keys,
                                                             const int32_t* __restrict__ ids, int R, int64_t V, int shift,
                                                             int32_t* __restrict__ counts) {
   __shared__ int n[kBins];
   for (int d = threadIdx.x; d < kBins; d += kSortThreads) n[d] = 0;
   __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kSortRows;
+  const int64_t base = (int64_t)blockIdx.x * (kSortThreads * kSortSteps);
   for (int s = 0; s < kSortSteps; ++s) {
     const int64_t i = base + s * kSortThreads + threadIdx.x;
     if (i < R) atomicAdd(&n[digit_of(keys ? keys[i] : key_of(ids[i], V), shift)], 1);
@@ -118,6 +153,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_count(const uint32_t* __re
 
 // Each row to its place: after the rows of smaller digits, of the same digit in earlier blocks (offs, the prefix of
 // counts), in earlier wavefronts of the block and in earlier lanes. A wavefront owns kSortSteps * 64 rows in a row.
+template <int kSortSteps>
 __global__ __launch_bounds__(kSortThreads) void embed_place(const uint32_t* __restrict__ keys,
                                                             const int32_t* __restrict__ order,
                                                             const int32_t* __restrict__ ids, int R, int64_t V, int shift,
@@ -129,7 +165,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_place(const uint32_t* __re
   const int w = threadIdx.x / kWave, l = lane_id();
   for (int d = threadIdx.x; d < W * kBins; d += kSortThreads) (&at[0][0])[d] = 0;
   __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kSortRows + w * kSortSteps * kWave;
+  const int64_t base = ((int64_t)blockIdx.x * (kSortThreads / kWave) + w) * (kSortSteps * kWave);
   uint32_t k[kSortSteps];
 #pragma unroll
   for (int s = 0; s < kSortSteps; ++s) {
@@ -190,42 +226,50 @@ __global__ __launch_bounds__(kThreads) void embed_sum(const uint32_t* __restrict
   const int l = threadIdx.x & ((1 << sh) - 1);
   const int i = (slab * (1 << sh) + l) * kE<T>;  // this lane's columns
   const int lo = c * per, hi = min(R, lo + per);
-  constexpr int kAhead = 8;
+  constexpr int kAhead = 8;  // rows under way
   float acc[kE<T>];
 #pragma unroll
   for (int u = 0; u < kE<T>; ++u) acc[u] = 0.0f;
   uint32_t prev = lo > 0 ? keys[lo - 1] : 0xffffffffu;  // no key: V <= 2^31 - 1
   const uint32_t after = hi < R ? keys[hi] : 0xffffffffu;
   bool began = keys[lo] != prev;                        // the present run began in this chunk
-  for (int p = lo; p < hi; p += kAhead) {
-    float x[kAhead][kE<T>];
+  struct Batch {
+    Raw<T, kE<T>> raw[kAhead];
     uint32_t k[kAhead + 1];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) k[u] = p + u < hi ? keys[p + u] : after;
-    k[kAhead] = p + kAhead < hi ? keys[p + kAhead] : after;
+  };
+  const auto fetch = [&](Batch& f, int p) {
+    int32_t r[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int64_t r = order[min(p + u, hi - 1)];
-      load_in<T, kE<T>>(dout + r * ld, min(i, N), N, x[u]);
+      f.k[u] = p + u < hi ? keys[p + u] : after;
+      r[u] = order[min(p + u, hi - 1)];
     }
+    f.k[kAhead] = p + kAhead < hi ? keys[p + kAhead] : after;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) f.raw[u] = raw_in<T, kE<T>>(dout + r[u] * ld, min(i, N), N);
+  };
+  const auto add = [&](const Batch& f, int p) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      if (p + u < hi && k[u] < (uint32_t)V) {
+      const uint32_t k = f.k[u];
+      if (p + u < hi && k < (uint32_t)V) {
+        float x[kE<T>];
+        f.raw[u].to(x);
 #pragma unroll
-        for (int q = 0; q < kE<T>; ++q) acc[q] += x[u][q];
-        const bool begins = k[u] != prev, ends = k[u + 1] != k[u] || p + u + 1 == R;
-        if (begins && slab == 0 && l == 0) first[k[u]] = p + u;
-        if (ends && slab == 0 && l == 0) last[k[u]] = p + u + 1;
+        for (int q = 0; q < kE<T>; ++q) acc[q] += x[q];
+        const bool begins = k != prev, ends = f.k[u + 1] != k || p + u + 1 == R;
+        if (begins && slab == 0 && l == 0) first[k] = p + u;
+        if (ends && slab == 0 && l == 0) last[k] = p + u + 1;
         if (begins) began = true;
         if (ends || p + u + 1 == hi) {
           if (began && ends) {
-            T* row = dE + (int64_t)k[u] * ld_e;
+            T* row = dE + (int64_t)k * ld_e;
             if (i < N) {
               float y[kE<T>], old[kE<T>];
               if (accumulate) load_in<T, kE<T>>(row, i, N, old);
 #pragma unroll
               for (int q = 0; q < kE<T>; ++q) y[q] = accumulate ? fmaf(acc[q], scale, old[q]) : acc[q] * scale;
-              store_in<T, kE<T>>(row, i, N, y);
+              store_past_in<T, kE<T>>(row, i, N, y);
             }
           } else {
             float* part = (began ? tail : head) + (size_t)c * N;
@@ -235,51 +279,83 @@ __global__ __launch_bounds__(kThreads) void embed_sum(const uint32_t* __restrict
           for (int q = 0; q < kE<T>; ++q) acc[q] = 0.0f;
         }
       }
-      prev = k[u];
+      prev = k;
+    }
+  };
+  // the next batch's rows are requested before the present one's sums are stored: loads and stores retire in order
+  Batch f0, f1;
+  fetch(f0, lo);
+  for (int p = lo; p < hi; p += 2 * kAhead) {
+    if (p + kAhead < hi) fetch(f1, p + kAhead);
+    add(f0, p);
+    if (p + kAhead < hi) {
+      if (p + 2 * kAhead < hi) fetch(f0, p + 2 * kAhead);
+      add(f1, p + kAhead);
     }
   }
 }
 
-// Tokens that reach over several chunks, and (without accumulate) rows of zeros for those that did not occur.
+// Blocks [0, jobs): a chunk and slab each, the token whose rows begin in the chunk and go on behind it, if there is one: its
+// partial sums, the wavefronts a quarter of them each. The others: rows of zeros for the tokens that did not occur
+// (first[v] < 0), a wavefront kZeros tokens.
+constexpr int kZeros = 4;
 template <class T>
-__global__ __launch_bounds__(kThreads) void embed_rest(int64_t V, int N, const int32_t* __restrict__ first,
+__global__ __launch_bounds__(kThreads) void embed_rest(const uint32_t* __restrict__ keys, int R, int64_t V, int N,
+                                                       const int32_t* __restrict__ first,
                                                        const int32_t* __restrict__ last, const float* __restrict__ head,
-                                                       const float* __restrict__ tail, float scale, int per, int sh,
-                                                       T* __restrict__ dE, int64_t ld_e, int accumulate) {
-  const int lanes = 1 << sh;
-  const int l = threadIdx.x & (lanes - 1);
-  for (int64_t v = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> sh; v < V; v += ((int64_t)gridDim.x * kThreads) >> sh) {
-    const int f = first[v];
-    int c0 = 0, c1 = -1;
-    if (f >= 0) {
-      c0 = f / per;
-      c1 = (last[v] - 1) / per;
-      if (c0 == c1) continue;
-    } else if (accumulate) {
-      continue;
-    }
-    T* row = dE + v * ld_e;
-    for (int i = l * kE<T>; i < N; i += lanes * kE<T>) {
-      float y[kE<T>];
+                                                       const float* __restrict__ tail, float scale, int per, int slabs,
+                                                       int jobs, T* __restrict__ dE, int64_t ld_e, int accumulate) {
+  constexpr int W = kThreads / kWave;
+  const int w = threadIdx.x / kWave, l = lane_id();
+  if ((int)blockIdx.x >= jobs) {
+    float zero[kE<T>];
 #pragma unroll
-      for (int u = 0; u < kE<T>; ++u) y[u] = 0.0f;
-      if (f >= 0) {
-        load_in<float, kE<T>>(tail + (size_t)c0 * N, i, N, y);
-#pragma unroll 4
-        for (int c = c0 + 1; c <= c1; ++c) {
-          float x[kE<T>];
-          load_in<float, kE<T>>(head + (size_t)c * N, i, N, x);
-#pragma unroll
-          for (int u = 0; u < kE<T>; ++u) y[u] += x[u];
-        }
-        float old[kE<T>];
-        if (accumulate) load_in<T, kE<T>>(row, i, N, old);
-#pragma unroll
-        for (int u = 0; u < kE<T>; ++u) y[u] = accumulate ? fmaf(y[u], scale, old[u]) : y[u] * scale;
+    for (int u = 0; u < kE<T>; ++u) zero[u] = 0.0f;
+    for (int64_t v0 = ((int64_t)(blockIdx.x - jobs) * W + w) * kZeros; v0 < V;
+         v0 += (int64_t)(gridDim.x - jobs) * W * kZeros) {
+      uint64_t absent = __ballot(l < kZeros && v0 + l < V && first[min(v0 + l, V - 1)] < 0);
+      while (absent) {
+        const int64_t v = v0 + __builtin_ctzll(absent);
+        absent &= absent - 1;
+        for (int i = l * kE<T>; i < N; i += kWave * kE<T>) store_past_in<T, kE<T>>(dE + v * ld_e, i, N, zero);
       }
-      store_in<T, kE<T>>(row, i, N, y);
     }
+    return;
   }
+  const int c0 = blockIdx.x / slabs, slab = blockIdx.x % slabs;
+  const int64_t hi = (int64_t)(c0 + 1) * per;
+  if (hi >= R) return;
+  const uint32_t k = keys[hi - 1];
+  if (k >= (uint32_t)V || keys[hi] != k || first[k] / per != c0) return;
+  const int n = (last[k] - 1) / per - c0;  // chunks behind c0
+  const int share = (n + W - 1) / W;
+  const int i = (slab * kWave + l) * kE<T>;
+  float y[kE<T>];
+#pragma unroll
+  for (int u = 0; u < kE<T>; ++u) y[u] = 0.0f;
+  if (w == 0) load_in<float, kE<T>>(tail + (size_t)c0 * N, min(i, N), N, y);
+#pragma unroll 8
+  for (int c = c0 + 1 + w * share; c <= c0 + min(n, (w + 1) * share); ++c) {
+    float x[kE<T>];
+    load_in<float, kE<T>>(head + (size_t)c * N, min(i, N), N, x);
+#pragma unroll
+    for (int u = 0; u < kE<T>; ++u) y[u] += x[u];
+  }
+  __shared__ float all[W][kWave][kE<T> + 1];
+#pragma unroll
+  for (int u = 0; u < kE<T>; ++u) all[w][l][u] = y[u];
+  __syncthreads();
+  if (w > 0 || i >= N) return;
+  T* row = dE + (int64_t)k * ld_e;
+  float old[kE<T>];
+  if (accumulate) load_in<T, kE<T>>(row, i, N, old);
+#pragma unroll
+  for (int u = 0; u < kE<T>; ++u) {
+#pragma unroll
+    for (int o = 1; o < W; ++o) y[u] += all[o][l][u];
+    y[u] = accumulate ? fmaf(y[u], scale, old[u]) : y[u] * scale;
+  }
+  store_past_in<T, kE<T>>(row, i, N, y);
 }
 
 struct GradPlan {
@@ -292,7 +368,7 @@ GradPlan plan_grad(int64_t R, int64_t V) {
   p.per = 8;
   while (p.per < kMaxPer && (R + p.per - 1) / p.per > 2048) p.per *= 2;
   p.chunks = (int)((R + p.per - 1) / p.per);
-  p.sort_blocks = (int)((R + kSortRows - 1) / kSortRows);
+  p.sort_blocks = (int)((R + sort_rows(R) - 1) / sort_rows(R));
   p.passes = 0;
   for (int64_t top = V; top > 0; top >>= kDigit) ++p.passes;  // the largest key is V
   return p;
@@ -352,9 +428,11 @@ void launch_sums(int R, int64_t V, int N, const void* dout, int64_t ld, float sc
   hipLaunchKernelGGL(embed_sum<T>, dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, keys,
                      order, R, V, N, static_cast<const T*>(dout), ld, scale, p.per, p.chunks, slabs, sh,
                      static_cast<T*>(dE), ld_e, accumulate, g.first, g.last, g.head, g.tail);
-  const int64_t rest = std::min<int64_t>(((V << sh) + kThreads - 1) / kThreads, (int64_t)1 << 20);
-  hipLaunchKernelGGL(embed_rest<T>, dim3((unsigned)rest), dim3(kThreads), 0, s, V, N, g.first, g.last, g.head, g.tail,
-                     scale, p.per, sh, static_cast<T*>(dE), ld_e, accumulate);
+  const int wide = (N + kE<T> * kWave - 1) / (kE<T> * kWave);
+  const int jobs = p.chunks * wide;
+  const int64_t zeros = accumulate ? 0 : std::min<int64_t>((V + kZeros * kThreads / kWave - 1) / (kZeros * kThreads / kWave), 1 << 20);
+  hipLaunchKernelGGL(embed_rest<T>, dim3((unsigned)(jobs + zeros)), dim3(kThreads), 0, s, keys, R, V, N, g.first, g.last,
+                     g.head, g.tail, scale, p.per, wide, jobs, static_cast<T*>(dE), ld_e, accumulate);
 }
 
 // The sizes that both calls refuse.
@@ -364,10 +442,11 @@ snn_status check_sizes(int dtype, int64_t V, int N, int64_t R) {
   return SNN_OK;
 }
 
-// embed_sum's grid and partial sums: chunks of at least kMaxPer rows where R is large.
+// Whether the grids of embed_sum and embed_rest can be launched.
 bool sums_fit(int64_t R, int64_t V, int N) {
   const GradPlan p = plan_grad(R, V);
-  return (int64_t)p.chunks * ((N + 255) / 256) * kWave < ((int64_t)1 << 32) && R < ((int64_t)1 << 30);
+  // a dispatch counts threads in 32 bits
+  return R < ((int64_t)1 << 30) && (int64_t)p.chunks * ((N + 255) / 256) * kThreads < ((int64_t)1 << 31);
 }
 
 }  // namespace
@@ -407,9 +486,10 @@ extern "C" snn_status snn_embed_grad(const int32_t* ids, int64_t R, const void* 
   hipStream_t s = static_cast<hipStream_t>(stream);
   int at = 0;
   if (R <= kRankRows) {
-    const int64_t clear = std::min<int64_t>((V + 1023) / 1024, 256);  // blocks past the rows clear first[] alone
-    hipLaunchKernelGGL(embed_rank, dim3((unsigned)std::max((R + 31) / 32, clear)), dim3(kThreads), 0, s, ids, (int)R, V, g.keys[0],
-                       g.order[0], g.first);
+    const int64_t clear = std::min<int64_t>((V + 4095) / 4096, 256);  // blocks past the rows clear first[] alone
+    const int rows = kRankThreads / kRankShare;
+    hipLaunchKernelGGL(embed_rank, dim3((unsigned)std::max((R + rows - 1) / rows, clear)), dim3(kRankThreads),
+                       (size_t)(R + 3) / 4 * 16, s, ids, (int)R, V, g.keys[0], g.order[0], g.first);
   } else {
     hipLaunchKernelGGL(embed_clear_ends, dim3((unsigned)std::min<int64_t>((V + 255) / 256, 4096)), dim3(256), 0, s, g.first,
                        V);
@@ -418,10 +498,12 @@ extern "C" snn_status snn_embed_grad(const int32_t* ids, int64_t R, const void* 
       const int32_t* rows = pass ? g.order[at] : nullptr;
       const int to = pass ? at ^ 1 : 0;
       const dim3 grid((unsigned)p.sort_blocks);
-      hipLaunchKernelGGL(embed_count, grid, dim3(kSortThreads), 0, s, from, ids, (int)R, V, pass * kDigit, g.counts);
+      const bool few = R <= kFewStepsRows;
+      hipLaunchKernelGGL((few ? embed_count<kFewSteps> : embed_count<kManySteps>), grid, dim3(kSortThreads), 0, s, from, ids,
+                         (int)R, V, pass * kDigit, g.counts);
       launch_exclusive_scan(g.counts, kBins * p.sort_blocks, g.offs, g.total, g.temp, s);
-      hipLaunchKernelGGL(embed_place, grid, dim3(kSortThreads), 0, s, from, rows, ids, (int)R, V, pass * kDigit, g.offs,
-                         g.keys[to], g.order[to]);
+      hipLaunchKernelGGL((few ? embed_place<kFewSteps> : embed_place<kManySteps>), grid, dim3(kSortThreads), 0, s, from, rows,
+                         ids, (int)R, V, pass * kDigit, g.offs, g.keys[to], g.order[to]);
       at = to;
     }
   }

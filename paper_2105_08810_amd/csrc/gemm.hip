@@ -59,7 +59,8 @@ __device__ __forceinline__ void split8(const float (&x)[8], uint4& h, uint4& m, 
 //   KM: element (r, k) at p[k * ld + r] (rows contiguous): a piece is eight loads, each 256 contiguous
 //       bytes over a wavefront.
 //   else p[r * ld + k] (k contiguous): a piece is 32 contiguous bytes.
-// Rows past the end read the last row (their results are not stored); k past k_hi reads as 0.
+// Rows past the end read the last row (their results are not stored); k past k_hi reads as 0, and so does a k whose bit of
+// live (32 k a word, KM only) is 0.
 template <bool KM, int ROWS>
 __device__ __forceinline__ void piece_of(int q, int& row, int& kc) {
   const int idx = threadIdx.x + kThreads * q;
@@ -67,9 +68,9 @@ __device__ __forceinline__ void piece_of(int q, int& row, int& kc) {
   kc = KM ? idx / ROWS : idx % kKC;
 }
 
-template <bool KM, bool VEC, int ROWS>
+template <bool KM, bool VEC, int ROWS, bool MASK = false>
 __device__ __forceinline__ void load_stage(const float* __restrict__ p, int ld, int r0, int R, int k0, int k_hi,
-                                           float (&x)[ROWS / 64][8]) {
+                                           float (&x)[ROWS / 64][8], const uint32_t* __restrict__ live = nullptr) {
 #pragma unroll
   for (int q = 0; q < ROWS / 64; ++q) {
     int row, kc;
@@ -83,6 +84,11 @@ __device__ __forceinline__ void load_stage(const float* __restrict__ p, int ld, 
       } else {
 #pragma unroll
         for (int u = 0; u < 8; ++u) x[q][u] = k + u < k_hi ? p[(size_t)(k + u) * ld + r] : 0.0f;
+      }
+      if (MASK) {
+        const uint32_t bits = live[k0 / kBK] >> (8 * kc);  // stages begin at multiples of 32
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[q][u] = bits >> u & 1 ? x[q][u] : 0.0f;
       }
     } else {
       const float* s = p + (size_t)r * ld + k;
@@ -170,13 +176,15 @@ __device__ __forceinline__ BlockTile row_tile(int tiles_m, int tiles_n) {
 // below (a sum over all rows of positive traces) adds up coherently. A's sign turns from one fold and one tile of
 // rows to the next, so that it cancels (dW of the first of three 1024 x 1024 layers, 27% active: 1.89e-7 -> 1.51e-7
 // of the result from 64 bits; 1.80e-7 entry by entry).
-// KA, KB: k down the rows of A, of B (load_stage's KM). accumulate: C += instead (one K slice alone).
-template <bool KA, bool KB, bool VEC, bool GATHER>
+// KA, KB: k down the rows of A, of B (load_stage's KM). accumulate: C += instead (one K slice alone). MASK: only the k
+// whose bit of live is set take part.
+template <bool KA, bool KB, bool VEC, bool GATHER, bool MASK = false>
 __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, const float* __restrict__ A, int lda,
                                                            const float* __restrict__ B, int ldb,
                                                            float* __restrict__ C, int ldc, int k_per_split,
                                                            size_t c_split, int tiles_m, int tiles_n, int splits,
-                                                           int accumulate, GatherOut to, Gate gate) {
+                                                           int accumulate, const uint32_t* __restrict__ live,
+                                                           GatherOut to, Gate gate) {
   if (!gate_open(gate)) return;
   constexpr int TN = GATHER ? 2 : 4;  // 16-wide column tiles of a wavefront
   constexpr int BN = 32 * TN;
@@ -256,7 +264,7 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, 
 
   float xa[2][8], xb[BN / 64][8];
   if (k_lo < k_hi) {
-    load_stage<KA, VEC, kBM>(A, lda, m0, M, k_lo, k_hi, xa);
+    load_stage<KA, VEC, kBM, MASK>(A, lda, m0, M, k_lo, k_hi, xa, live);
     load_stage<KB, VEC, BN>(B, ldb, n0, N, k_lo, k_hi, xb);
   }
   int stage = 0;
@@ -265,7 +273,7 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, 
     store_stage<KB, BN>(Bs, xb, kUp);
     __syncthreads();
     if (k0 + kBK < k_hi) {
-      load_stage<KA, VEC, kBM>(A, lda, m0, M, k0 + kBK, k_hi, xa);
+      load_stage<KA, VEC, kBM, MASK>(A, lda, m0, M, k0 + kBK, k_hi, xa, live);
       load_stage<KB, VEC, BN>(B, ldb, n0, N, k0 + kBK, k_hi, xb);
     }
     bf16x8 fa[3][4];
@@ -312,7 +320,7 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, 
     clear_total();
     down = 1.0f;
     for (int k0 = k_lo; k0 < k_hi; k0 += kBK) {
-      load_stage<KA, VEC, kBM>(A, lda, m0, M, k0, k_hi, xa);
+      load_stage<KA, VEC, kBM, MASK>(A, lda, m0, M, k0, k_hi, xa, live);
       load_stage<KB, VEC, BN>(B, ldb, n0, N, k0, k_hi, xb);
       store_wide<KA, kBM>(Aw, xa);
       store_wide<KB, BN>(Bw, xb);
@@ -500,12 +508,17 @@ SplitPlan plan_splits(int M, int N, int K, double mac_rate) {
 }
 
 void gemm_split_km(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc, int splits,
-                   size_t c_split, hipStream_t s) {
+                   size_t c_split, hipStream_t s, const uint32_t* live) {
   const int tm = (M + kBM - 1) / kBM, tn = (N + kBN - 1) / kBN;
   int kps = (K + splits - 1) / splits;
   kps = (kps + kBK - 1) / kBK * kBK;
-  hipLaunchKernelGGL((gemm_split3<true, true, false, false>), dim3((unsigned)(splits * tm * tn)), dim3(kThreads), 0, s,
-                     M, N, K, A, lda, B, ldb, C, ldc, kps, c_split, tm, tn, splits, 0, GatherOut{}, Gate{});
+  const dim3 g((unsigned)(splits * tm * tn));
+  if (live)
+    hipLaunchKernelGGL((gemm_split3<true, true, false, false, true>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C,
+                       ldc, kps, c_split, tm, tn, splits, 0, live, GatherOut{}, Gate{});
+  else
+    hipLaunchKernelGGL((gemm_split3<true, true, false, false>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
+                       kps, c_split, tm, tn, splits, 0, nullptr, GatherOut{}, Gate{});
 }
 
 namespace {
@@ -522,10 +535,10 @@ void launch_kc(int M, int N, int K, const float* A, int lda, const float* B, int
   const dim3 g((unsigned)((tm >= 32 ? (tm + 7) / 8 * 8 : tm) * tn));
   if (vec)
     hipLaunchKernelGGL((gemm_split3<false, KB, true, GATHER>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
-                       kps, 0, tm, tn, 1, accumulate, to, gate);
+                       kps, 0, tm, tn, 1, accumulate, nullptr, to, gate);
   else
     hipLaunchKernelGGL((gemm_split3<false, KB, false, GATHER>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
-                       kps, 0, tm, tn, 1, accumulate, to, gate);
+                       kps, 0, tm, tn, 1, accumulate, nullptr, to, gate);
 }
 
 }  // namespace

@@ -36,12 +36,50 @@ __device__ __forceinline__ float group_sum(float v, float* red) {
   return v;
 }
 
+template <int L>
+__device__ __forceinline__ void group_sum2(float& a, float& b, float2* red) {
+#pragma unroll
+  for (int off = (L < kWave ? L : kWave) / 2; off > 0; off >>= 1) {
+    a += __shfl_xor(a, off, kWave);
+    b += __shfl_xor(b, off, kWave);
+  }
+  if constexpr (L > kWave) {
+    __syncthreads();
+    if (lane_id() == 0) red[threadIdx.x / kWave] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0.0f;
+#pragma unroll
+    for (int k = 0; k < L / kWave; ++k) {
+      a += red[k].x;
+      b += red[k].y;
+    }
+  }
+}
+
 // What the launches share. E elements a vector, Q vectors a lane, L lanes a row, B threads a block.
 template <int L>
 constexpr int kBlock = L > 256 ? L : 256;
 
 template <class TX, class TY>
 constexpr int kE = sizeof(TX) == 4 || sizeof(TY) == 4 ? 4 : 8;
+
+// A row's values stay in registers as they were read: the compiler would keep their float32 forms as well, twice the
+// registers in 16 bits, and so half the rows under way.
+template <class T, int E, int Q>
+__device__ __forceinline__ void kept(Raw<T, E> (&raw)[Q]) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int u = 0; u < E / 2; ++u) asm volatile("" : "+v"(raw[q].w[u]));
+  }
+}
+
+// Whether a wavefront holds anything of its vector q: the last vectors of most of a block's wavefronts may lie past the row.
+template <int L, int E>
+__device__ __forceinline__ bool any_of(int q, int N) {
+  return L <= kWave || (q * L + __builtin_amdgcn_readfirstlane((int)threadIdx.x & ~(kWave - 1))) * E < N;
+}
 
 template <class TX, class TY, int L, int Q>
 __global__ __launch_bounds__(kBlock<L>) void norm_forward(const TX* __restrict__ x, int64_t ld_x, int64_t R, int N,
@@ -50,49 +88,74 @@ __global__ __launch_bounds__(kBlock<L>) void norm_forward(const TX* __restrict__
                                                           int64_t ld_y, float* __restrict__ mean,
                                                           float* __restrict__ rstd) {
   constexpr int E = kE<TX, TY>;
-  constexpr int G = kBlock<L> / L;  // rows of a block
+  constexpr int G = kBlock<L> / L;  // rows of a block at a time
   __shared__ float red[kBlock<L> / kWave];
-  const int64_t r = (int64_t)blockIdx.x * G + threadIdx.x / L;
   const int l = threadIdx.x % L;
-  if (L <= kWave && r >= R) return;  // whole groups; with L > kWave a block is one row
-  const TX* row = x + r * ld_x;
-  float v[Q][E];
-  float s = 0.0f;
-#pragma unroll
-  for (int q = 0; q < Q; ++q) load_in<TX, E>(row, (q * L + l) * E, N, v[q]);
-#pragma unroll
-  for (int q = 0; q < Q; ++q)
-#pragma unroll
-    for (int u = 0; u < E; ++u) s += v[q][u];
-  const float m = group_sum<L>(s, red) / (float)N;
-  float d2 = 0.0f;
-#pragma unroll
-  for (int q = 0; q < Q; ++q)
-#pragma unroll
-    for (int u = 0; u < E; ++u) {
-      const float d = v[q][u] - m;
-      v[q][u] = d;
-      if ((q * L + l) * E + u < N) d2 = fmaf(d, d, d2);
-    }
-  const float k = 1.0f / sqrtf(group_sum<L>(d2, red) / (float)N + eps);
-  TY* out = y + r * ld_y;
+  float g[Q][E], b[Q][E];
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
-    const int i = (q * L + l) * E;
-    if (i >= N) continue;
-    float g[E], b[E];
-    if (gamma) load_in<float, E>(gamma, i, N, g);
-    if (beta) load_in<float, E>(beta, i, N, b);
+    const int i = min((q * L + l) * E, N);
+    if (gamma) load_in<float, E>(gamma, i, N, g[q]);
+    if (beta) load_in<float, E>(beta, i, N, b[q]);
 #pragma unroll
     for (int u = 0; u < E; ++u) {
-      const float h = v[q][u] * k;
-      v[q][u] = gamma ? (beta ? fmaf(h, g[u], b[u]) : h * g[u]) : (beta ? h + b[u] : h);
+      if (!gamma) g[q][u] = 1.0f;
+      if (!beta) b[q][u] = -0.0f;  // h + -0 is h
     }
-    store_in<TY, E>(out, i, N, v[q]);
   }
-  if (l == 0) {
-    if (mean) mean[r] = m;
-    if (rstd) rstd[r] = k;
+  // with L > kWave a block is one row: all its threads or none
+  const int64_t step = (int64_t)gridDim.x * G;
+  int64_t r = (int64_t)blockIdx.x * G + threadIdx.x / L;
+  if (r >= R) return;
+  Raw<TX, E> raw[Q], next[Q];
+  const auto fetch = [&](Raw<TX, E> (&to)[Q], int64_t row) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) to[q] = raw_in<TX, E>(x + row * ld_x, (q * L + l) * E, N);
+  };
+  fetch(raw, r);
+  for (; r < R; r += step) {
+    if (r + step < R) fetch(next, r + step);
+    float s = 0.0f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      if (!any_of<L, E>(q, N)) continue;
+      float v[E];
+      raw[q].to(v);
+#pragma unroll
+      for (int u = 0; u < E; ++u) s += v[u];
+    }
+    const float m = group_sum<L>(s, red) / (float)N;
+    kept(raw);
+    float d2 = 0.0f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      if (!any_of<L, E>(q, N)) continue;
+      float v[E];
+      raw[q].to(v);
+#pragma unroll
+      for (int u = 0; u < E; ++u) {
+        const float d = v[u] - m;
+        if ((q * L + l) * E + u < N) d2 = fmaf(d, d, d2);
+      }
+    }
+    const float k = 1.0f / sqrtf(group_sum<L>(d2, red) / (float)N + eps);
+    kept(raw);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int i = (q * L + l) * E;
+      if (i >= N) continue;
+      float v[E];
+      raw[q].to(v);
+#pragma unroll
+      for (int u = 0; u < E; ++u) v[u] = fmaf((v[u] - m) * k, g[q][u], b[q][u]);
+      store_past_in<TY, E>(y + r * ld_y, i, N, v);
+    }
+    if (l == 0) {
+      if (mean) mean[r] = m;
+      if (rstd) rstd[r] = k;
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q) raw[q] = next[q];
   }
 }
 
@@ -106,53 +169,79 @@ __global__ __launch_bounds__(kBlock<L>) void norm_backward(const TY* __restrict_
                                                            int64_t ld_dx, float* __restrict__ part) {
   constexpr int E = kE<TX, TY>;
   constexpr int G = kBlock<L> / L;
-  __shared__ float red[kBlock<L> / kWave];
+  __shared__ float2 red[kBlock<L> / kWave];
   extern __shared__ float share[];  // [G][L * E] of one vector of the groups' shares
   const int g = threadIdx.x / L, l = threadIdx.x % L;
-  float dg[Q][E], db[Q][E];
+  float dg[Q][E], db[Q][E], w[Q][E];
 #pragma unroll
-  for (int q = 0; q < Q; ++q)
+  for (int q = 0; q < Q; ++q) {
+    if (gamma) load_in<float, E>(gamma, min((q * L + l) * E, N), N, w[q]);
 #pragma unroll
-    for (int u = 0; u < E; ++u) dg[q][u] = db[q][u] = 0.0f;
-  for (int64_t r0 = (int64_t)blockIdx.x * G; r0 < R; r0 += (int64_t)gridDim.x * G) {
-    const int64_t r = r0 + g;
-    if (r >= R) break;  // with L > kWave a block is one row: all its threads or none
-    const float m = mean[r], k = rstd[r];
-    float h[Q][E], a[Q][E];
+    for (int u = 0; u < E; ++u) {
+      dg[q][u] = db[q][u] = 0.0f;
+      if (!gamma) w[q][u] = 1.0f;
+    }
+  }
+  // with L > kWave a block is one row: all its threads or none
+  const int64_t step = (int64_t)gridDim.x * G;
+  Raw<TX, E> rx[Q], nx[Q];
+  Raw<TY, E> ry[Q], ny[Q];
+  float m = 0.0f, k = 0.0f, nm = 0.0f, nk = 0.0f;
+  const auto fetch = [&](int64_t row) {
+    nm = mean[row];
+    nk = rstd[row];
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      load_in<TX, E>(x + r * ld_x, (q * L + l) * E, N, h[q]);
-      load_in<TY, E>(dy + r * ld_dy, (q * L + l) * E, N, a[q]);
+      nx[q] = raw_in<TX, E>(x + row * ld_x, (q * L + l) * E, N);
+      ny[q] = raw_in<TY, E>(dy + row * ld_dy, (q * L + l) * E, N);
     }
+  };
+  int64_t r = (int64_t)blockIdx.x * G + g;
+  if (r < R) fetch(r);
+  for (; r < R; r += step) {
+    m = nm;
+    k = nk;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      rx[q] = nx[q];
+      ry[q] = ny[q];
+    }
+    if (r + step < R) fetch(r + step);
     float s = 0.0f, sh = 0.0f;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      const int i = (q * L + l) * E;
-      float w[E];
-      if (gamma) load_in<float, E>(gamma, min(i, N), N, w);
+      if (!any_of<L, E>(q, N)) continue;
+      float h[E], a[E];
+      rx[q].to(h);
+      ry[q].to(a);
 #pragma unroll
       for (int u = 0; u < E; ++u) {
-        h[q][u] = (h[q][u] - m) * k;
+        h[u] = (h[u] - m) * k;
         if (part) {
-          dg[q][u] = fmaf(a[q][u], h[q][u], dg[q][u]);
-          db[q][u] += a[q][u];
+          dg[q][u] = fmaf(a[u], h[u], dg[q][u]);
+          db[q][u] += a[u];
         }
-        if (gamma) a[q][u] *= w[u];
-        s += a[q][u];  // 0 past the row's end
-        sh = fmaf(a[q][u], h[q][u], sh);
+        a[u] *= w[q][u];
+        s += a[u];  // 0 past the row's end
+        sh = fmaf(a[u], h[u], sh);
       }
     }
     if (dx) {
-      s = group_sum<L>(s, red) / (float)N;
-      sh = group_sum<L>(sh, red) / (float)N;
+      group_sum2<L>(s, sh, red);
+      s /= (float)N;
+      sh /= (float)N;
+      kept(rx);
+      kept(ry);
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         const int i = (q * L + l) * E;
         if (i >= N) continue;
-        float o[E];
+        float h[E], a[E];
+        rx[q].to(h);
+        ry[q].to(a);
 #pragma unroll
-        for (int u = 0; u < E; ++u) o[u] = k * (a[q][u] - s - h[q][u] * sh);
-        store_in<TX, E>(dx + r * ld_dx, i, N, o);
+        for (int u = 0; u < E; ++u) a[u] = k * (a[u] * w[q][u] - s - (h[u] - m) * k * sh);
+        store_past_in<TX, E>(dx + r * ld_dx, i, N, a);
       }
     }
   }
@@ -308,16 +397,18 @@ __global__ __launch_bounds__(256) void norm_columns_long(const TY* __restrict__ 
   part[(size_t)blockIdx.y * 2 * N + N + j] = db;
 }
 
-// How a row of N is spread: lanes and vectors a lane; L 0: beyond a block's registers.
+// How a row of N is spread: lanes and vectors a lane; L 0: beyond a block's registers. A wavefront alone needs no barrier
+// between its sums; with more than 20 values a lane (gamma, beta and their gradients are held beside the row's) too few
+// wavefronts fit, and a block of 256 takes the row.
 struct Shape {
   int L, Q;
 };
 Shape shape_of(int N, int E) {
   const int v = (N + E - 1) / E;
   if (v <= 16) return {16, 1};
-  if (v <= 64) return {64, 1};
-  if (v <= 128) return {64, 2};
-  if (v <= 256) return {64, 4};
+  for (int q = 1; q * E <= 20; ++q)
+    if (v <= 64 * q) return {64, q};
+  if (v <= 256) return {256, 1};
   if (v <= 512) return {256, 2};
   if (v <= 1024) return {256, 4};
   if (v <= 2048) return {1024, 2};
@@ -348,13 +439,17 @@ void forward(const void* x, int64_t ld_x, int64_t R, int N, const float* gamma, 
     const TX* px = static_cast<const TX*>(x) + r * ld_x;
     TY* py = static_cast<TY*>(y) + r * ld_y;
     float *pm = mean ? mean + r : nullptr, *pr = rstd ? rstd + r : nullptr;
+    const int64_t most = (int64_t)8 * cu_count();  // blocks; beyond, a block walks several rows with one gamma and beta
 #define SNN_N(L_, Q_)                                                                                            \
-  hipLaunchKernelGGL((norm_forward<TX, TY, L_, Q_>), dim3((unsigned)((n + kBlock<L_> / L_ - 1) / (kBlock<L_> / L_))), \
+  hipLaunchKernelGGL((norm_forward<TX, TY, L_, Q_>), dim3((unsigned)std::min(most, (n + kBlock<L_> / L_ - 1) / (kBlock<L_> / L_))), \
                      dim3(kBlock<L_>), 0, s, px, ld_x, n, N, gamma, beta, eps, py, ld_y, pm, pr)
     if (sh.L == 16) SNN_N(16, 1);
     else if (sh.L == 64 && sh.Q == 1) SNN_N(64, 1);
     else if (sh.L == 64 && sh.Q == 2) SNN_N(64, 2);
-    else if (sh.L == 64) SNN_N(64, 4);
+    else if (sh.L == 64 && sh.Q == 3) SNN_N(64, 3);
+    else if (sh.L == 64 && sh.Q == 4) SNN_N(64, 4);
+    else if (sh.L == 64) SNN_N(64, 5);
+    else if (sh.L == 256 && sh.Q == 1) SNN_N(256, 1);
     else if (sh.L == 256 && sh.Q == 2) SNN_N(256, 2);
     else if (sh.L == 256) SNN_N(256, 4);
     else if (sh.L == 1024 && sh.Q == 2) SNN_N(1024, 2);
@@ -381,7 +476,10 @@ void backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int64_
   if (sh.L == 16) SNN_N(16, 1);
   else if (sh.L == 64 && sh.Q == 1) SNN_N(64, 1);
   else if (sh.L == 64 && sh.Q == 2) SNN_N(64, 2);
-  else if (sh.L == 64) SNN_N(64, 4);
+  else if (sh.L == 64 && sh.Q == 3) SNN_N(64, 3);
+  else if (sh.L == 64 && sh.Q == 4) SNN_N(64, 4);
+  else if (sh.L == 64) SNN_N(64, 5);
+  else if (sh.L == 256 && sh.Q == 1) SNN_N(256, 1);
   else if (sh.L == 256 && sh.Q == 2) SNN_N(256, 2);
   else if (sh.L == 256) SNN_N(256, 4);
   else if (sh.L == 1024 && sh.Q == 2) SNN_N(1024, 2);

@@ -6,8 +6,7 @@
 // The logits of all classes are never in memory together: the classes are taken in pieces, each piece's logits are formed,
 // give their share of every row's sum of exponentials and are dropped; with the rows' lse known a piece's logits are formed
 // again (unless there is one piece) and turned into its columns of dz, from which its share of dx and its columns of dW
-// follow. Rows without a target (or of weight 0) are taken out first: the others lie packed, in their order, before rows of
-// zeros, so that nothing of the former is read again.
+// follow. Rows without a target (or of weight 0) take no part, whatever they hold.
 #include <algorithm>
 
 #include "gemm16.h"
@@ -19,43 +18,50 @@ using namespace vectors;
 
 constexpr int kMaxRows = 1 << 24;
 constexpr int kMaxHidden = 1 << 16;
+// ------------------------------------------------------------------ float32
+
 constexpr int64_t kPiece = (int64_t)1 << 27;  // logits of a piece
 constexpr int kWaves = 4;                     // rows of a block in the kernels with a wavefront a row
+constexpr int kCountParts = 256;
 
-__device__ __forceinline__ bool has_target(int32_t t, int C) { return t >= 0 && t < C; }
-
-// live[r]: whether row r takes part.
-__global__ void ce_live(const int32_t* __restrict__ targets, const float* __restrict__ weight, int R, int C,
-                        int32_t* __restrict__ live) {
-  const int r = blockIdx.x * blockDim.x + threadIdx.x;
-  if (r < R) live[r] = has_target(targets[r], C) && (!weight || weight[r] != 0.0f);
+__device__ __forceinline__ bool takes_part(const int32_t* targets, const float* weight, int r, int C) {
+  const int32_t t = targets[r];
+  return t >= 0 && t < C && (!weight || weight[r] != 0.0f);
 }
 
-// Rows to their packed places: pos[r] = live rows before r, pos[R] = their number. Row r of x as float32, a row of zeros
-// for one that takes no part (these lie behind the others).
-__global__ __launch_bounds__(kWaves * kWave) void ce_pack(const float* __restrict__ x, int64_t ld, int R, int H,
-                                                          const int32_t* __restrict__ targets,
-                                                          const float* __restrict__ weight,
-                                                          const int32_t* __restrict__ pos, float* __restrict__ X,
-                                                          int32_t* __restrict__ target, float* __restrict__ w) {
-  const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
-  if (r >= R) return;
-  const int n = pos[R], p0 = pos[r];
-  const bool live = pos[r + 1] > p0;
-  const int p = live ? p0 : n + (r - p0);
-  for (int i = lane_id(); i < H; i += kWave) X[(size_t)p * H + i] = live ? x[(int64_t)r * ld + i] : 0.0f;
-  if (lane_id() == 0) {
-    target[p] = live ? targets[r] : -1;
-    w[p] = !live ? 0.0f : weight ? weight[r] : 1.0f / (float)n;
+// Bit r of live: whether row r takes part (0 behind the last); parts[block]: how many of the block's rows do.
+__global__ __launch_bounds__(256) void ce_live(const int32_t* __restrict__ targets, const float* __restrict__ weight, int R,
+                                               int C, uint64_t* __restrict__ live, int32_t* __restrict__ parts) {
+  int n = 0;
+  for (int r0 = blockIdx.x * 256 + (threadIdx.x & ~(kWave - 1)); r0 < R; r0 += gridDim.x * 256) {
+    const int r = r0 + lane_id();
+    const uint64_t on = __ballot(r < R && takes_part(targets, weight, r, C));
+    if (lane_id() == 0) live[r0 / 64] = on;
+    n += __popcll(on);
   }
+  __shared__ int all[256 / kWave];
+  if (lane_id() == 0) all[threadIdx.x / kWave] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) parts[blockIdx.x] = all[0] + all[1] + all[2] + all[3];
+}
+
+__device__ __forceinline__ bool alive(const uint64_t* live, int r) { return live[r >> 6] >> (r & 63) & 1; }
+
+// A row's weight where all that take part weigh the same: one over their number, from ce_live's n parts. A wavefront calls.
+__device__ __forceinline__ float same_weight(const int32_t* __restrict__ parts, int n) {
+  int s = 0;
+  for (int k = lane_id(); k < n; k += kWave) s += parts[k];
+  s = wave_sum_int(s);
+  return s > 0 ? 1.0f / (float)s : 0.0f;
 }
 
 // A piece's share of every row's largest logit and sum of exponentials, and the target's logit.
 __global__ __launch_bounds__(kWaves * kWave) void ce_sums(const float* __restrict__ z, int R, int n, int c0,
-                                                          const int32_t* __restrict__ target, float* __restrict__ top,
+                                                          const int32_t* __restrict__ targets,
+                                                          const uint64_t* __restrict__ live, float* __restrict__ top,
                                                           float* __restrict__ sum, float* __restrict__ at_target) {
   const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
-  if (r >= R) return;
+  if (r >= R || !alive(live, r)) return;
   const float* row = z + (size_t)r * n;
   const int l = lane_id();
   float m = -INFINITY;
@@ -75,65 +81,78 @@ __global__ __launch_bounds__(kWaves * kWave) void ce_sums(const float* __restric
     }
     top[r] = m;
     sum[r] = s;
-    const int t = target[r] - c0;
-    if (target[r] >= 0 && t >= 0 && t < n) at_target[r] = row[t];
+    const int t = targets[r] - c0;
+    if (t >= 0 && t < n) at_target[r] = row[t];
   }
 }
 
-// Each row's log-sum-exp and loss; loss parts of a block in float64. Rows that take no part have loss 0.
-__global__ __launch_bounds__(256) void ce_losses(int R, const int32_t* __restrict__ pos, const float* __restrict__ top,
-                                                 const float* __restrict__ sum, const float* __restrict__ at_target,
-                                                 const float* __restrict__ w, float* __restrict__ lse,
-                                                 float* __restrict__ row_loss, double* __restrict__ parts) {
-  double s = 0.0;
-  for (int r = blockIdx.x * 256 + threadIdx.x; r < R; r += gridDim.x * 256) {
-    const int p = pos[r];
-    float loss = 0.0f;
-    if (pos[r + 1] > p) {
-      const float log_sum = logf(sum[p]);
-      lse[p] = top[p] + log_sum;
-      loss = (top[p] - at_target[p]) + log_sum;
-      s += (double)w[p] * (double)loss;
-    }
-    if (row_loss) row_loss[r] = loss;
-  }
+// Sum of a block's values in float64, in a fixed order; the first thread has it.
+__device__ __forceinline__ double block_total(double s) {
   __shared__ double all[256];
+  __syncthreads();
   all[threadIdx.x] = s;
   __syncthreads();
   for (int off = 128; off > 0; off >>= 1) {
     if ((int)threadIdx.x < off) all[threadIdx.x] += all[threadIdx.x + off];
     __syncthreads();
   }
-  if (threadIdx.x == 0) parts[blockIdx.x] = all[0];
+  return all[0];
 }
 
-__global__ void ce_total(const double* __restrict__ parts, int n, float* __restrict__ loss) {
+__device__ __forceinline__ void total_of(const double* __restrict__ parts, int n, float* __restrict__ loss) {
   double s = 0.0;
-  for (int k = 0; k < n; ++k) s += parts[k];
-  *loss = (float)s;
+  for (int k = threadIdx.x; k < n; k += 256) s += parts[k];
+  s = block_total(s);
+  if (threadIdx.x == 0) *loss = (float)s;
 }
 
-// z to dz in place; rows behind the live ones to 0.
+__global__ __launch_bounds__(256) void ce_total(const double* __restrict__ parts, int n, float* __restrict__ loss) {
+  total_of(parts, n, loss);
+}
+
+// Each row's log-sum-exp and loss; the weighted losses of a block in float64.
+__global__ __launch_bounds__(256) void ce_losses(int R, const uint64_t* __restrict__ live, const int32_t* __restrict__ counts,
+                                                 int n_counts, const float* __restrict__ weight,
+                                                 const float* __restrict__ top, const float* __restrict__ sum,
+                                                 const float* __restrict__ at_target, float* __restrict__ lse,
+                                                 float* __restrict__ row_loss, double* __restrict__ parts) {
+  const float same = weight ? 0.0f : same_weight(counts, n_counts);
+  double s = 0.0;
+  for (int r = blockIdx.x * 256 + threadIdx.x; r < R; r += gridDim.x * 256) {
+    float loss = 0.0f;
+    if (alive(live, r)) {
+      const float log_sum = logf(sum[r]);
+      lse[r] = top[r] + log_sum;
+      loss = (top[r] - at_target[r]) + log_sum;
+      s += (double)(weight ? weight[r] : same) * (double)loss;
+    }
+    if (row_loss) row_loss[r] = loss;
+  }
+  s = block_total(s);
+  if (threadIdx.x == 0) parts[blockIdx.x] = s;
+}
+
+// z to dz in place; 0 in rows that take no part.
 __global__ __launch_bounds__(kWaves * kWave) void ce_dz(float* __restrict__ z, int R, int n, int c0,
-                                                        const int32_t* __restrict__ target, const float* __restrict__ w,
-                                                        const float* __restrict__ lse) {
+                                                        const int32_t* __restrict__ targets,
+                                                        const uint64_t* __restrict__ live,
+                                                        const int32_t* __restrict__ counts, int n_counts,
+                                                        const float* __restrict__ weight, const float* __restrict__ lse) {
   const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
   if (r >= R) return;
   float* row = z + (size_t)r * n;
-  const int t = target[r];
-  const float k = w[r], ref = t >= 0 ? lse[r] : 0.0f;
-  for (int i = lane_id(); i < n; i += kWave)
-    row[i] = t >= 0 ? k * (expf(row[i] - ref) - (c0 + i == t ? 1.0f : 0.0f)) : 0.0f;
+  const bool on = alive(live, r);
+  const float k = weight ? weight[r] : same_weight(counts, n_counts), ref = on ? lse[r] : 0.0f;
+  const int t = targets[r] - c0;
+  for (int i = lane_id(); i < n; i += kWave) row[i] = on ? k * (expf(row[i] - ref) - (i == t ? 1.0f : 0.0f)) : 0.0f;
 }
 
-__global__ __launch_bounds__(kWaves * kWave) void ce_dx(const float* __restrict__ dX, int R, int H,
-                                                        const int32_t* __restrict__ pos, float* __restrict__ dx,
-                                                        int64_t ld) {
+// dx of the rows that take no part.
+__global__ __launch_bounds__(kWaves * kWave) void ce_dead_rows(const uint64_t* __restrict__ live, int R, int H,
+                                                               float* __restrict__ dx, int64_t ld) {
   const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
-  if (r >= R) return;
-  const int p = pos[r];
-  const bool live = pos[r + 1] > p;
-  for (int i = lane_id(); i < H; i += kWave) dx[(int64_t)r * ld + i] = live ? dX[(size_t)p * H + i] : 0.0f;
+  if (r >= R || alive(live, r)) return;
+  for (int i = lane_id(); i < H; i += kWave) dx[(int64_t)r * ld + i] = 0.0f;
 }
 
 // A piece's columns of dW from its K slices, summed in order.
@@ -147,14 +166,346 @@ __global__ void ce_dw(const float* __restrict__ part, int slices, int H, int n, 
   }
 }
 
+// Few classes (up to kFew): everything of a row but dW in one launch. A block of four wavefronts takes 64 RT rows, a
+// wavefront 16 RT of them and all classes, on the bf16 matrix cores with both operands in three parts (h + m + l, the six
+// products down to 2^-16 of the leading one; values below 2^-110 lose some of their last bits, one of 2^128 - 2^119 and more
+// counts as infinite). m is the class and n the row, so the accumulators hold every class of a row in four lanes:
+// log-sum-exp, loss and dz are formed there, and, as a lane has four neighbouring classes of one row, its dz are the second
+// product's operand as they stand: dx = dz W^T. So x is read and dx written once, and of the logits only dz leaves the
+// registers (for dW). W's parts are made beforehand in the order of both products (ce_few_parts). Bound: the matrix cores
+// (12 products of 128000 x 1024 x 112 in bf16 terms: 150 us at their nominal rate) beside reading x and writing dx (205 us).
+constexpr int kFew = 128;
+constexpr int kCountHere = 8192;  // rows up to which every block counts those with a target itself
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+constexpr float kDzUp = 0x1p30f;  // dz / w enters the second product raised, so that small probabilities keep their bits
+
+__device__ __forceinline__ void split8(const float (&x)[8], uint4 (&part)[3]) {
+  uint32_t w[3][4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    float a = x[2 * q], b = x[2 * q + 1];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      w[p][q] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+      a -= __uint_as_float(w[p][q] << 16);
+      b -= __uint_as_float(w[p][q] & 0xffff0000u);
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < 3; ++p) part[p] = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+}
+
+// Term t of a product of parts: the five smaller ones, smallest first, then the leading one (to an accumulator of its own).
+constexpr int kTerms = 6;
+__device__ __forceinline__ void mfma_term(int t, const uint4 (&a)[3], const uint4 (&b)[3], f32x4& lead, f32x4& rest) {
+  constexpr int kTerm[kTerms][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+  f32x4& c = t == kTerms - 1 ? lead : rest;
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[kTerm[t][0]]),
+                                              __builtin_bit_cast(bf16x8, b[kTerm[t][1]]), c, 0, 0, 0);
+}
+
+// W's parts, zeros past its ends. For the first product [stage of 32 h][part][h / 8 % 4][class], 8 h of one class each; for
+// the second [stage of 32 h][part][32-class step][g][h], of one h the 8 classes 32 step + 4 g + v and 16 more.
+template <int NT>
+__global__ __launch_bounds__(256) void ce_few_parts(const float* __restrict__ W, int64_t ld, int H, int C,
+                                                    uint4* __restrict__ first, uint4* __restrict__ second) {
+  constexpr int Cp = NT * 16, S = (NT + 1) / 2;
+  const int stage = blockIdx.x;
+  for (int q = threadIdx.x; q < 4 * Cp + 32 * 4 * S; q += 256) {
+    float x[8];
+    uint4 part[3];
+    if (q < 4 * Cp) {
+      const int kc = q / Cp, c = q % Cp;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int h = stage * 32 + 8 * kc + u;
+        x[u] = h < H && c < C ? W[(int64_t)h * ld + c] : 0.0f;
+      }
+      split8(x, part);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) first[((size_t)stage * 3 + p) * 4 * Cp + q] = part[p];
+    } else {
+      const int at = q - 4 * Cp, h = stage * 32 + at % 32, g = at / 32 % 4, step = at / 128;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int c = 32 * step + 16 * (u / 4) + 4 * g + u % 4;
+        x[u] = h < H && c < C ? W[(int64_t)h * ld + c] : 0.0f;
+      }
+      split8(x, part);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) second[((size_t)stage * 3 + p) * 128 * S + at] = part[p];
+    }
+  }
+}
+
+template <int NT, int RT, bool VEC>  // 16-class tiles, 16-row tiles of a wavefront; whether H is a multiple of 4
+__global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, int64_t ld_x, const uint4* __restrict__ first,
+                                                 const uint4* __restrict__ second, int R, int H, int C,
+                                                 const int32_t* __restrict__ targets, const float* __restrict__ weight,
+                                                 const int32_t* __restrict__ counts, int n_counts,
+                                                 float* __restrict__ row_loss, double* __restrict__ parts,
+                                                 float* __restrict__ dx, int64_t ld_dx, float* __restrict__ dz, int ld_dz,
+                                                 uint64_t* __restrict__ live) {
+  constexpr int kRows = 64 * RT, Cp = NT * 16, S = (NT + 1) / 2;
+  // pieces of a stage of W, two stages in LDS: lines [part][g] of its classes, or [part][step][g] of 32 h
+  constexpr int kW1 = 12 * Cp, kW2 = 3 * 128 * S, kW = kW1 > kW2 ? kW1 : kW2;
+  __shared__ __attribute__((aligned(1024))) uint4 Ws[2][kW];
+  __shared__ int32_t on[kRows];
+  const int w = threadIdx.x / kWave, l = lane_id(), i = l % 16, g = l / 16;
+  const int r0 = blockIdx.x * kRows;
+  float same = 0.0f;
+  if (!weight) {
+    if (counts) {
+      same = same_weight(counts, n_counts);
+    } else {
+      int n = 0;
+      for (int q = l; q < R; q += kWave) n += takes_part(targets, weight, q, C);
+      n = wave_sum_int(n);
+      same = n > 0 ? 1.0f / (float)n : 0.0f;
+    }
+  }
+  bool alive = false;
+  if (threadIdx.x < kRows) {
+    const int q = r0 + threadIdx.x;
+    alive = q < R && takes_part(targets, weight, q, C);
+    on[threadIdx.x] = alive;
+    const uint64_t bits = __ballot(alive);
+    if (live && l == 0 && q < R) live[q / 64] = bits;
+  }
+  const bool any = __syncthreads_or(alive);
+  f32x4 lead[NT][RT], rest[NT][RT];
+#pragma unroll
+  for (int a = 0; a < NT; ++a)
+#pragma unroll
+    for (int b = 0; b < RT; ++b) lead[a][b] = rest[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int wave = __builtin_amdgcn_readfirstlane(w);
+  const uint32_t lds = (uint32_t)(uintptr_t)(gemm16::LdsPtr)(char*)&Ws[0][0];
+  const auto load_w = [&](const uint4* from, int n, int buf) {  // straight into LDS, 64 pieces at a time
+    for (int q = wave; q < n / kWave; q += 4)
+      gemm16::load_to_lds(from, (uint32_t)(q * kWave + l) * 16, __builtin_amdgcn_readfirstlane(lds + (buf * kW + q * kWave) * 16));
+  };
+  // A lane's part of a stage of x: 8 h of one row of each of its tiles, the second product operand as it stands. Past H
+  // any of the row's values will do, since W is 0 there; rows that take no part have results that nothing uses.
+  const float* px[RT];
+#pragma unroll
+  for (int b = 0; b < RT; ++b) px[b] = x + (int64_t)min(r0 + 16 * (RT * w + b) + i, R - 1) * ld_x;
+  float xs[RT][8];
+  const auto load_x = [&](int h0) {
+#pragma unroll
+    for (int b = 0; b < RT; ++b) {
+      if (VEC) {
+        load<float, 4>(px[b] + min(h0 + 8 * g, H - 4), *reinterpret_cast<float(*)[4]>(&xs[b][0]));
+        load<float, 4>(px[b] + min(h0 + 8 * g + 4, H - 4), *reinterpret_cast<float(*)[4]>(&xs[b][4]));
+      } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) xs[b][u] = px[b][min(h0 + 8 * g + u, H - 1)];
+      }
+    }
+  };
+  // every block begins at another stage: rows are often a power of two apart, and blocks at the same h would meet in the
+  // same memory channels
+  const int stages = (H + 31) / 32, begin = (int)(blockIdx.x % stages);
+  if (any) {
+    load_w(first + (size_t)begin * kW1, kW1, 0);
+    load_x(32 * begin);
+    for (int n = 0, at = begin; n < stages; ++n) {
+      at = at + 1 == stages ? 0 : at + 1;  // the stage after this one
+      uint4 fb[RT][3];
+#pragma unroll
+      for (int b = 0; b < RT; ++b) split8(xs[b], fb[b]);
+      gemm16::stage_barrier();  // this stage of W is there, the one before has been read
+      if (n + 1 < stages) {
+        load_w(first + (size_t)at * kW1, kW1, (n + 1) & 1);
+        load_x(32 * at);
+      }
+      const uint4* W1 = Ws[n & 1];
+#pragma unroll
+      for (int a = 0; a < NT; a += 2) {  // neighbours in the issue order go to different accumulators
+        uint4 fa[2][3];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int p = 0; p < 3; ++p)
+            if (a + q < NT) fa[q][p] = W1[(4 * p + g) * Cp + 16 * (a + q) + i];
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int b = 0; b < RT; ++b)
+              if (a + q < NT) mfma_term(t, fa[q], fb[b], lead[a + q < NT ? a + q : 0][b], rest[a + q < NT ? a + q : 0][b]);
+      }
+    }
+  }
+  // lane (i, g) holds rows i of the wavefront's tiles, classes 16 a + 4 g + v
+  double total = 0.0;
+  uint4 fz[RT][S][3];
+  float k[RT];
+#pragma unroll
+  for (int b = 0; b < RT; ++b) {
+    const int at = 16 * (RT * w + b) + i, r = r0 + at;
+    const bool mine = on[at];
+    const int t = mine ? targets[r] : -1;
+    float m = -INFINITY, zt = 0.0f;
+#pragma unroll
+    for (int a = 0; a < NT; ++a)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int c = 16 * a + 4 * g + v;
+        lead[a][b][v] += rest[a][b][v];
+        if (c < C) m = fmaxf(m, lead[a][b][v]);
+        if (c == t) zt = lead[a][b][v];
+      }
+    m = fmaxf(m, __shfl_xor(m, 16, kWave));
+    m = fmaxf(m, __shfl_xor(m, 32, kWave));
+    zt += __shfl_xor(zt, 16, kWave);
+    zt += __shfl_xor(zt, 32, kWave);
+    const float from = m > -INFINITY ? m : 0.0f;
+    float s = 0.0f;
+#pragma unroll
+    for (int a = 0; a < NT; ++a)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) s += 16 * a + 4 * g + v < C ? expf(lead[a][b][v] - from) : 0.0f;
+    s += __shfl_xor(s, 16, kWave);
+    s += __shfl_xor(s, 32, kWave);
+    const float log_sum = logf(s), lse = m + log_sum;
+    const float loss = mine ? (m - zt) + log_sum : 0.0f;
+    k[b] = mine ? (weight ? weight[r] : same) : 0.0f;
+    if (g == 0 && r < R && row_loss) row_loss[r] = loss;
+    if (g == 0 && mine) total += (double)k[b] * (double)loss;
+    if (!dx && !dz) continue;
+#pragma unroll
+    for (int step = 0; step < S; ++step) {
+      float d[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int a = 2 * step + u / 4, c = 16 * a + 4 * g + u % 4;
+        d[u] = a < NT && mine && c < C ? expf(lead[a < NT ? a : 0][b][u % 4] - lse) - (c == t ? 1.0f : 0.0f) : 0.0f;
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int c = 16 * (2 * step + half) + 4 * g;
+        if (dz && r < R && c < ld_dz)
+          *reinterpret_cast<f32x4*>(dz + (size_t)r * ld_dz + c) =
+              f32x4{k[b] * d[4 * half], k[b] * d[4 * half + 1], k[b] * d[4 * half + 2], k[b] * d[4 * half + 3]};
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) d[u] *= kDzUp;
+      split8(d, fz[b][step]);
+    }
+  }
+  total = block_total(total);
+  if (threadIdx.x == 0) parts[blockIdx.x] = total;
+  if (!dx) return;
+  if (any) load_w(second + (size_t)begin * kW2, kW2, 0);  // (the losses' total has passed barriers since the last reads)
+  for (int n = 0, at = begin; n < stages; ++n) {
+    const int h0 = 32 * at;
+    at = at + 1 == stages ? 0 : at + 1;
+    f32x4 d[2][RT], e[2][RT];
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int b = 0; b < RT; ++b) d[half][b] = e[half][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (any) {
+      gemm16::stage_barrier();
+      if (n + 1 < stages) load_w(second + (size_t)at * kW2, kW2, (n + 1) & 1);
+      const uint4* W2 = Ws[n & 1];
+#pragma unroll
+      for (int step = 0; step < S; ++step) {
+        uint4 fa[2][3];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int p = 0; p < 3; ++p) fa[half][p] = W2[((p * S + step) * 4 + g) * 32 + 16 * half + i];
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int b = 0; b < RT; ++b) mfma_term(t, fa[half], fz[b][step], d[half][b], e[half][b]);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < RT; ++b) {
+      const int at = 16 * (RT * w + b) + i, r = r0 + at;
+      if (r >= R) continue;
+      const bool mine = on[at];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        float o[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) o[v] = mine ? (d[half][b][v] + e[half][b][v]) * (1.0f / kDzUp) * k[b] : 0.0f;
+        store_in<float, 4>(dx + (int64_t)r * ld_dx, min(h0 + 16 * half + 4 * g, H), H, o);
+      }
+    }
+  }
+}
+
+// dW of few rows and classes: a block 16 h and all classes, its 16 wavefronts every sixteenth run of 16 rows, straight from
+// memory on the float32 matrix cores; their sums are added in LDS, in order. Block 0 also adds up the loss.
+constexpr int kFewDwRows = 4096;
+template <int NT>
+__global__ __launch_bounds__(1024) void ce_few_dw(const float* __restrict__ x, int64_t ld_x, const float* __restrict__ dz,
+                                                  int ld_dz, const uint64_t* __restrict__ live, int R, int H, int C,
+                                                  float* __restrict__ dW, int64_t ld_dw, const double* __restrict__ parts,
+                                                  int n_parts, float* __restrict__ loss) {
+  __shared__ float sum[16][NT * 16][17];
+  const int w = threadIdx.x / kWave, l = lane_id(), i = l % 16, g = l / 16;
+  const int h = blockIdx.x * 16 + i;
+  f32x4 acc[NT];
+#pragma unroll
+  for (int a = 0; a < NT; ++a) acc[a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int r0 = 16 * w; r0 < R; r0 += 256) {
+    float b[4], d[4][NT];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = r0 + 4 * j + g;
+      const bool on = r < R && h < H && alive(live, r);
+      b[j] = on ? x[(int64_t)r * ld_x + h] : 0.0f;
+#pragma unroll
+      for (int a = 0; a < NT; ++a) d[j][a] = r < R && 16 * a + i < ld_dz ? dz[(size_t)r * ld_dz + 16 * a + i] : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int a = 0; a < NT; ++a) acc[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(d[j][a], b[j], acc[a], 0, 0, 0);
+  }
+#pragma unroll
+  for (int a = 0; a < NT; ++a)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) sum[w][16 * a + 4 * g + v][i] = acc[a][v];
+  __syncthreads();
+  for (int q = threadIdx.x; q < 16 * NT * 16; q += 1024) {
+    const int c = q % (NT * 16), n = q / (NT * 16);
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += sum[k][c][n];
+    if (c < C && blockIdx.x * 16 + n < H) dW[(int64_t)(blockIdx.x * 16 + n) * ld_dw + c] = s;
+  }
+  if (blockIdx.x == 0 && threadIdx.x < kWave) {
+    double s = 0.0;
+    for (int k = l; k < n_parts; k += kWave) s += parts[k];
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, kWave);
+    if (l == 0) *loss = (float)s;
+  }
+}
+
 struct Plan {
+  bool few;
   int width, pieces, slices;  // classes of a piece; K slices of dW
+  int ld;                     // of a piece's logits
 };
 
 Plan plan_of(int R, int H, int C) {
   Plan p;
-  p.width = (int)std::min<int64_t>(C, std::max<int64_t>(256, kPiece / R / 128 * 128));
+  p.few = C <= kFew;
+  p.width = p.few ? C : (int)std::min<int64_t>(C, std::max<int64_t>(256, kPiece / R / 128 * 128));
   p.pieces = (C + p.width - 1) / p.width;
+  p.ld = p.few ? (C + 3) / 4 * 4 : p.width;
   p.slices = plan_splits(H, p.width, R, 88e12).splits;
   return p;
 }
@@ -162,64 +513,107 @@ Plan plan_of(int R, int H, int C) {
 constexpr int kLossParts = 256;
 
 struct Workspace {
-  int32_t *live, *pos, *temp, *target;
-  int64_t* total;
-  float *X, *z, *dX, *dW, *w, *top, *sum, *at_target, *lse;
+  uint64_t* live;
+  int32_t* counts;
+  uint4 *first, *second;
+  float *z, *dW, *top, *sum, *at_target, *lse;
   double* parts;
   size_t bytes;
 };
 
-Workspace carve(void* ws, int R, int H, int C, bool grad, const Plan& p) {
+Workspace carve(void* ws, int R, int H, bool grad, const Plan& p) {
   Carve c(ws);
   Workspace g;
-  g.live = c.take<int32_t>(R);
-  g.pos = c.take<int32_t>((size_t)R + 1);
-  g.temp = c.take<int32_t>(scan_temp_elems(R));
-  g.total = c.take<int64_t>(1);
-  g.target = c.take<int32_t>(R);
-  g.w = c.take<float>(R);
-  g.top = c.take<float>(R);
-  g.sum = c.take<float>(R);
-  g.at_target = c.take<float>(R);
-  g.lse = c.take<float>(R);
-  g.parts = c.take<double>(kLossParts);
-  g.X = c.take<float>((size_t)R * H);
-  g.z = c.take<float>((size_t)R * p.width);
-  g.dX = c.take<float>(grad ? (size_t)R * H : 0);
-  g.dW = c.take<float>(grad ? (size_t)p.slices * H * p.width : 0);
+  g.live = c.take<uint64_t>(((size_t)R + 63) / 64);
+  g.counts = c.take<int32_t>(kCountParts);
+  const size_t stages = p.few ? (H + 31) / 32 : 0;
+  g.first = c.take<uint4>(stages * 12 * kFew);
+  g.second = c.take<uint4>(stages * 12 * kFew);
+  const size_t rows = p.few ? 0 : (size_t)R;
+  g.top = c.take<float>(rows);
+  g.sum = c.take<float>(rows);
+  g.at_target = c.take<float>(rows);
+  g.lse = c.take<float>(rows);
+  g.parts = c.take<double>(p.few ? (R + 63) / 64 : kLossParts);
+  g.z = c.take<float>(p.few && !grad ? 0 : (size_t)R * p.ld);
+  g.dW = c.take<float>(grad && p.slices > 1 ? (size_t)p.slices * H * p.width : 0);
   g.bytes = c.off;
   return g;
+}
+
+// A piece's columns of dW (n of them) from its dz, in K slices where the product alone has few tiles.
+void enqueue_dw(const float* x, int64_t ld_x, const float* dz, int ld_dz, int R, int H, int n, float* dW, int64_t ld_dw,
+                const Plan& p, const Workspace& g, hipStream_t s) {
+  const uint32_t* live = reinterpret_cast<const uint32_t*>(g.live);  // the words' halves in order
+  if (p.slices == 1) {
+    gemm_split_km(H, n, R, x, (int)ld_x, dz, ld_dz, dW, (int)ld_dw, 1, 0, s, live);
+    return;
+  }
+  gemm_split_km(H, n, R, x, (int)ld_x, dz, ld_dz, g.dW, n, p.slices, (size_t)H * n, s, live);
+  hipLaunchKernelGGL(ce_dw, dim3((unsigned)((n + 255) / 256), (unsigned)std::min(H, 1024)), dim3(256), 0, s, g.dW, p.slices,
+                     H, n, dW, ld_dw);
+}
+
+template <int NT>
+void run_few(const float* x, int64_t ld_x, const float* W, int64_t ld_w, int R, int H, int C, const int32_t* targets,
+             const float* weight, float* loss, float* row_loss, float* dx, int64_t ld_dx, float* dW, int64_t ld_dw,
+             const Plan& p, const Workspace& g, hipStream_t s) {
+  // 32 rows a wavefront read W's parts half as often; 16 where 32 would leave compute units without a block
+  const bool wide = (R + 127) / 128 >= 2 * cu_count();
+  const int blocks = wide ? (R + 127) / 128 : (R + 63) / 64;
+  const int counted = weight || R <= kCountHere ? 0 : std::min(kCountParts, (R + 1023) / 1024);
+  if (counted)
+    hipLaunchKernelGGL(ce_live, dim3((unsigned)counted), dim3(256), 0, s, targets, weight, R, C, g.live, g.counts);
+  hipLaunchKernelGGL(ce_few_parts<NT>, dim3((unsigned)((H + 31) / 32)), dim3(256), 0, s, W, ld_w, H, C, g.first, g.second);
+  const bool vec = H % 4 == 0;
+  hipLaunchKernelGGL((wide ? (vec ? ce_few<NT, 2, true> : ce_few<NT, 2, false>) : (vec ? ce_few<NT, 1, true> : ce_few<NT, 1, false>)),
+                     dim3((unsigned)blocks), dim3(256), 0, s, x, ld_x, g.first,
+                     g.second, R, H, C, targets, weight, counted ? g.counts : nullptr, counted, row_loss, g.parts, dx, ld_dx,
+                     dW ? g.z : nullptr, p.ld, counted ? nullptr : g.live);
+  if (dW && R <= kFewDwRows) {
+    hipLaunchKernelGGL(ce_few_dw<NT>, dim3((unsigned)((H + 15) / 16)), dim3(1024), 0, s, x, ld_x, g.z, p.ld, g.live, R, H, C,
+                       dW, ld_dw, g.parts, blocks, loss);
+    return;
+  }
+  hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, blocks, loss);
+  if (dW) enqueue_dw(x, ld_x, g.z, p.ld, R, H, C, dW, ld_dw, p, g, s);
 }
 
 void run(const float* x, int64_t ld_x, const float* W, int64_t ld_w, int R, int H, int C, const int32_t* targets,
          const float* weight, float* loss, float* row_loss, float* dx, int64_t ld_dx, float* dW, int64_t ld_dw,
          const Plan& p, const Workspace& g, hipStream_t s) {
+  if (p.few) {
+#define SNN_FEW(NT)                                                                                                     \
+  run_few<NT>(x, ld_x, W, ld_w, R, H, C, targets, weight, loss, row_loss, dx, ld_dx, dW, ld_dw, p, g, s)
+    if (C <= 16) SNN_FEW(1);
+    else if (C <= 32) SNN_FEW(2);
+    else if (C <= 64) SNN_FEW(4);
+    else if (C <= 112) SNN_FEW(7);
+    else SNN_FEW(8);
+#undef SNN_FEW
+    return;
+  }
   const dim3 rows((unsigned)((R + kWaves - 1) / kWaves)), waves(kWaves * kWave);
-  const int ld = (int)ld_w;
-  hipLaunchKernelGGL(ce_live, dim3((unsigned)((R + 255) / 256)), dim3(256), 0, s, targets, weight, R, C, g.live);
-  launch_exclusive_scan(g.live, R, g.pos, g.total, g.temp, s);
-  hipLaunchKernelGGL(ce_pack, rows, waves, 0, s, x, ld_x, R, H, targets, weight, g.pos, g.X, g.target, g.w);
+  const int counted = std::min(kCountParts, (R + 1023) / 1024);
+  hipLaunchKernelGGL(ce_live, dim3((unsigned)counted), dim3(256), 0, s, targets, weight, R, C, g.live, g.counts);
   for (int c0 = 0; c0 < C; c0 += p.width) {
     const int n = std::min(p.width, C - c0);
-    gemm_split_kr(R, n, H, g.X, H, W + c0, ld, g.z, n, s);
-    hipLaunchKernelGGL(ce_sums, rows, waves, 0, s, g.z, R, n, c0, g.target, g.top, g.sum, g.at_target);
+    gemm_split_kr(R, n, H, x, (int)ld_x, W + c0, (int)ld_w, g.z, n, s);
+    hipLaunchKernelGGL(ce_sums, rows, waves, 0, s, g.z, R, n, c0, targets, g.live, g.top, g.sum, g.at_target);
   }
-  hipLaunchKernelGGL(ce_losses, dim3(kLossParts), dim3(256), 0, s, R, g.pos, g.top, g.sum, g.at_target, g.w, g.lse,
-                     row_loss, g.parts);
-  hipLaunchKernelGGL(ce_total, dim3(1), dim3(1), 0, s, g.parts, kLossParts, loss);
+  const int blocks = std::min(kLossParts, (R + 255) / 256);
+  hipLaunchKernelGGL(ce_losses, dim3((unsigned)blocks), dim3(256), 0, s, R, g.live, g.counts, counted, weight, g.top, g.sum,
+                     g.at_target, g.lse, row_loss, g.parts);
+  hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, blocks, loss);
   if (!dx && !dW) return;
   for (int c0 = 0; c0 < C; c0 += p.width) {
     const int n = std::min(p.width, C - c0);
-    if (p.pieces > 1) gemm_split_kr(R, n, H, g.X, H, W + c0, ld, g.z, n, s);
-    hipLaunchKernelGGL(ce_dz, rows, waves, 0, s, g.z, R, n, c0, g.target, g.w, g.lse);
-    if (dx) gemm_split_kc(R, H, n, g.z, n, W + c0, ld, g.dX, H, s, c0 > 0);
-    if (dW) {
-      gemm_split_km(H, n, R, g.X, H, g.z, n, g.dW, n, p.slices, (size_t)H * n, s);
-      hipLaunchKernelGGL(ce_dw, dim3((unsigned)((n + 255) / 256), (unsigned)std::min(H, 1024)), dim3(256), 0, s, g.dW,
-                         p.slices, H, n, dW + c0, ld_dw);
-    }
+    if (p.pieces > 1) gemm_split_kr(R, n, H, x, (int)ld_x, W + c0, (int)ld_w, g.z, n, s);
+    hipLaunchKernelGGL(ce_dz, rows, waves, 0, s, g.z, R, n, c0, targets, g.live, g.counts, counted, weight, g.lse);
+    if (dx) gemm_split_kc(R, H, n, g.z, n, W + c0, (int)ld_w, dx, (int)ld_dx, s, c0 > 0);
+    if (dW) enqueue_dw(x, ld_x, g.z, n, R, H, n, dW + c0, ld_dw, p, g, s);
   }
-  if (dx) hipLaunchKernelGGL(ce_dx, rows, waves, 0, s, g.dX, R, H, g.pos, dx, ld_dx);
+  if (dx) hipLaunchKernelGGL(ce_dead_rows, rows, waves, 0, s, g.live, R, H, dx, ld_dx);
 }
 
 // ------------------------------------------------------------------ 16-bit operands
@@ -232,6 +626,54 @@ constexpr float kRaise = std::is_same<T, F16>::value ? 32768.0f : 1.0f;
 
 constexpr int kTile = gemm16::kTile;
 constexpr int kPart = 128;  // classes of a partial sum of exponentials: a wavefront's
+
+// pos[r]: rows before r that take part, pos[R]: their number; ref: the largest weight. Blocks of 1024 threads: one takes up
+// to kOneBlock rows, a run of them a thread; beyond, the flags' prefix is formed by the scan and ref by a launch of its own.
+constexpr int kOneBlock = 32768;
+__global__ __launch_bounds__(1024) void ce_places(const int32_t* __restrict__ targets, const float* __restrict__ weight,
+                                                  int R, int C, int32_t* __restrict__ pos, float* __restrict__ ref) {
+  __shared__ int count[1024 / kWave];
+  __shared__ float top[1024 / kWave];
+  const int per = (R + 1023) / 1024, lo = min(R, (int)threadIdx.x * per), hi = min(R, lo + per);
+  const int w = threadIdx.x / kWave;
+  int n = 0;
+  uint32_t on = 0;  // of the thread's at most 32 rows
+  float m = 0.0f;
+  for (int r = lo; r < hi; ++r)
+    if (takes_part(targets, weight, r, C)) {
+      on |= 1u << (r - lo);
+      ++n;
+      if (weight) m = fmaxf(m, fabsf(weight[r]));
+    }
+  const int upto = wave_incl_scan(n);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+  if (lane_id() == kWave - 1) {
+    count[w] = upto;
+    top[w] = m;
+  }
+  __syncthreads();
+  int p = upto - n, all = 0;
+  for (int k = 0; k < 1024 / kWave; ++k) {
+    if (k < w) p += count[k];
+    all += count[k];
+    m = fmaxf(m, top[k]);
+  }
+  for (int r = lo; r < hi; ++r) {
+    pos[r] = p;
+    p += on >> (r - lo) & 1;
+  }
+  if (threadIdx.x == 0) {
+    pos[R] = all;
+    *ref = weight ? m : (all > 0 ? 1.0f / (float)all : 0.0f);
+  }
+}
+
+__global__ __launch_bounds__(256) void ce_flags(const int32_t* __restrict__ targets, const float* __restrict__ weight, int R,
+                                                int C, int32_t* __restrict__ flags) {
+  const int r = blockIdx.x * 256 + threadIdx.x;
+  if (r < R) flags[r] = takes_part(targets, weight, r, C);
+}
 
 __global__ __launch_bounds__(1024) void ce_ref(const float* __restrict__ weight, const int32_t* __restrict__ pos, int R,
                                                float* __restrict__ ref) {
@@ -251,18 +693,21 @@ __global__ __launch_bounds__(1024) void ce_ref(const float* __restrict__ weight,
   if (threadIdx.x == 0) *ref = m;
 }
 
-// ce_pack in the type itself: rows of Hp, zeros behind H and in the rows behind the live ones up to a whole tile.
+// Rows to their packed places, row_of[place] = row: lines of Hp, zeros behind H and in the lines behind the rows that take
+// part up to a whole tile. The others' loss is 0.
 template <class T>
 __global__ __launch_bounds__(kWaves * kWave) void ce_pack16(const T* __restrict__ x, int64_t ld, int R, int Rp, int H,
                                                             int Hp, const int32_t* __restrict__ targets,
                                                             const float* __restrict__ weight,
                                                             const int32_t* __restrict__ pos, T* __restrict__ X,
-                                                            int32_t* __restrict__ target, float* __restrict__ w) {
+                                                            int32_t* __restrict__ target, float* __restrict__ w,
+                                                            int32_t* __restrict__ row_of, float* __restrict__ row_loss) {
   const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
   if (r >= Rp) return;
   const int n = pos[R], p0 = r < R ? pos[r] : n;
   const bool live = r < R && pos[r + 1] > p0;
   const int p = live ? p0 : n + (r - p0);
+  if (!live && r < R && row_loss && lane_id() == 0) row_loss[r] = 0.0f;
   if (p >= (n + kTile - 1) / kTile * kTile) return;
   for (int i = lane_id() * 8; i < Hp; i += kWave * 8) {
     T v[8];
@@ -283,6 +728,7 @@ __global__ __launch_bounds__(kWaves * kWave) void ce_pack16(const T* __restrict_
   if (lane_id() == 0) {
     target[p] = live ? targets[r] : -1;
     w[p] = !live ? 0.0f : weight ? weight[r] : 1.0f / (float)n;
+    row_of[p] = r;
   }
 }
 
@@ -381,14 +827,20 @@ __global__ __launch_bounds__(gemm16::kThreads, 2) void ce_logits16(
   }
 }
 
-// top and sum of every live row from the parts of its classes. A block takes 32 rows, 32 threads share a row's parts.
+// Every row's log-sum-exp and loss from the parts of its classes; the weighted losses of a block in float64. A block takes
+// 32 rows, 32 threads share a row's parts.
 __global__ __launch_bounds__(1024) void ce_join16(const float2* __restrict__ part, int parts, int R, int Rp,
-                                                  const int32_t* __restrict__ pos, float* __restrict__ top,
-                                                  float* __restrict__ sum) {
+                                                  const int32_t* __restrict__ pos, const int32_t* __restrict__ row_of,
+                                                  const float* __restrict__ at_target, const float* __restrict__ w,
+                                                  float* __restrict__ lse, float* __restrict__ row_loss,
+                                                  double* __restrict__ losses) {
   __shared__ float2 all[32][33];
   const int x = threadIdx.x % 32, y = threadIdx.x / 32;
   const int r = blockIdx.x * 32 + x;
-  if (blockIdx.x * 32 >= pos[R]) return;
+  if ((int)blockIdx.x * 32 >= pos[R]) {
+    if (threadIdx.x == 0) losses[blockIdx.x] = 0.0;
+    return;
+  }
   float m = -INFINITY, s = 0.0f;
   const auto add = [&](float m1, float s1) {
     const float both = fmaxf(m, m1), from = both > -INFINITY ? both : 0.0f;
@@ -404,10 +856,17 @@ __global__ __launch_bounds__(1024) void ce_join16(const float2* __restrict__ par
   __syncthreads();
   if (y == 0) {
     for (int k = 1; k < 32; ++k) add(all[k][x].x, all[k][x].y);
+    double weighted = 0.0;
     if (r < pos[R]) {
-      top[r] = m;
-      sum[r] = s;
+      const float log_sum = logf(s);
+      lse[r] = m + log_sum;
+      const float loss = (m - at_target[r]) + log_sum;
+      if (row_loss) row_loss[row_of[r]] = loss;
+      weighted = (double)w[r] * (double)loss;
     }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) weighted += __shfl_xor(weighted, off, kWave);
+    if (x == 0) losses[blockIdx.x] = weighted;
   }
 }
 
@@ -548,10 +1007,10 @@ Plan16 plan16_of(int R, int H, int C) {
 }
 
 struct Workspace16 {
-  int32_t *live, *pos, *temp, *target;
+  int32_t *flags, *pos, *temp, *target, *row_of;
   int64_t* total;
   uint16_t *X, *W, *G;
-  float *w, *top, *sum, *at_target, *lse, *ref, *dX, *dW;
+  float *w, *at_target, *lse, *ref, *dX, *dW;
   float2* part;
   double* parts;
   size_t bytes;
@@ -561,18 +1020,18 @@ struct Workspace16 {
 Workspace16 carve16(void* ws, int R, int H, int C, bool grad, const Plan16& p) {
   Carve c(ws);
   Workspace16 g;
-  g.live = c.take<int32_t>(R);
+  const size_t flags = R > kOneBlock ? (size_t)R : 0;
+  g.flags = c.take<int32_t>(flags);
   g.pos = c.take<int32_t>((size_t)R + 1);
   g.temp = c.take<int32_t>(scan_temp_elems(R));
   g.total = c.take<int64_t>(1);
   g.target = c.take<int32_t>(p.Rp);
+  g.row_of = c.take<int32_t>(p.Rp);
   g.w = c.take<float>(p.Rp);
-  g.top = c.take<float>(p.Rp);
-  g.sum = c.take<float>(p.Rp);
   g.at_target = c.take<float>(p.Rp);
   g.lse = c.take<float>(p.Rp);
   g.ref = c.take<float>(1);
-  g.parts = c.take<double>(kLossParts);
+  g.parts = c.take<double>(p.Rp / 32);
   g.part = c.take<float2>(p.parts * p.Rp);
   g.X = c.take<uint16_t>((size_t)p.Rp * p.Hp);
   g.W = c.take<uint16_t>((size_t)p.Hp * p.width);
@@ -593,10 +1052,15 @@ void run16(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int
   for (const void* f : {(const void*)ce_logits16<T, false>, (const void*)ce_logits16<T, true>, (const void*)ce_dx16<T>,
                         (const void*)ce_dw16<T>})
     ensure_dynamic_lds(f, gemm16::kLds);
-  hipLaunchKernelGGL(ce_live, dim3((unsigned)((R + 255) / 256)), dim3(256), 0, s, targets, weight, R, C, g.live);
-  launch_exclusive_scan(g.live, R, g.pos, g.total, g.temp, s);
+  if (R <= kOneBlock) {
+    hipLaunchKernelGGL(ce_places, dim3(1), dim3(1024), 0, s, targets, weight, R, C, g.pos, g.ref);
+  } else {
+    hipLaunchKernelGGL(ce_flags, dim3((unsigned)((R + 255) / 256)), dim3(256), 0, s, targets, weight, R, C, g.flags);
+    launch_exclusive_scan(g.flags, R, g.pos, g.total, g.temp, s);
+    hipLaunchKernelGGL(ce_ref, dim3(1), dim3(1024), 0, s, weight, g.pos, R, g.ref);
+  }
   hipLaunchKernelGGL(ce_pack16<T>, rows_of(p.Rp), waves, 0, s, x, ld_x, R, p.Rp, H, p.Hp, targets, weight, g.pos, X,
-                     g.target, g.w);
+                     g.target, g.w, g.row_of, row_loss);
   // W in place where its rows are whole tiles at 16-byte addresses
   const bool whole = H % kTile == 0 && C % kTile == 0 && ld_w % 8 == 0 && ld_w < (1 << 22) &&
                      reinterpret_cast<uintptr_t>(W) % 16 == 0;
@@ -621,13 +1085,10 @@ void run16(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int
                        X, p.Hp, stages_h, c0, C, R, p.Rp, tiles_m, tiles_n, g.pos, g.target, g.part, g.at_target, nullptr,
                        nullptr, nullptr, (T*)nullptr, 0);
   }
-  hipLaunchKernelGGL(ce_join16, dim3((unsigned)(p.Rp / 32)), dim3(1024), 0, s, g.part, (int)((padded(C, kTile)) / kPart), R,
-                     p.Rp, g.pos, g.top, g.sum);
-  hipLaunchKernelGGL(ce_losses, dim3(kLossParts), dim3(256), 0, s, R, g.pos, g.top, g.sum, g.at_target, g.w, g.lse,
-                     row_loss, g.parts);
-  hipLaunchKernelGGL(ce_total, dim3(1), dim3(1), 0, s, g.parts, kLossParts, loss);
+  hipLaunchKernelGGL(ce_join16, dim3((unsigned)(p.Rp / 32)), dim3(1024), 0, s, g.part, padded(C, kTile) / kPart, R, p.Rp,
+                     g.pos, g.row_of, g.at_target, g.w, g.lse, row_loss, g.parts);
+  hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, p.Rp / 32, loss);
   if (!dx && !dW) return;
-  hipLaunchKernelGGL(ce_ref, dim3(1), dim3(1024), 0, s, weight, g.pos, R, g.ref);
   for (int c0 = 0; c0 < C; c0 += p.width) {
     const int n = std::min(p.width, C - c0), tiles_m = (n + kTile - 1) / kTile;
     if (p.pieces > 1) weights(c0, n);
@@ -667,7 +1128,7 @@ using namespace snn;
 
 extern "C" size_t snn_linear_ce_workspace(int dtype, int64_t R, int H, int C, int grad) {
   if (check_sizes(dtype, R, H, C) != SNN_OK) return 0;
-  if (dtype == SNN_F32) return carve(nullptr, (int)R, H, C, grad != 0, plan_of((int)R, H, C)).bytes;
+  if (dtype == SNN_F32) return carve(nullptr, (int)R, H, grad != 0, plan_of((int)R, H, C)).bytes;
   return carve16(nullptr, (int)R, H, C, grad != 0, plan16_of((int)R, H, C)).bytes;
 }
 
@@ -680,11 +1141,11 @@ extern "C" snn_status snn_linear_ce(const void* x, const void* W, int dtype, int
   if (ld_x < H || ld_w < C || (dx && ld_dx < H) || (dW && ld_dw < C)) return SNN_ERR_INVALID_ARG;
   if (misaligned(x, dtype) || misaligned(W, dtype) || misaligned(dx, dtype) || misaligned(dW, dtype))
     return SNN_ERR_INVALID_ARG;
-  if (ld_w > INT32_MAX) return SNN_ERR_UNSUPPORTED;
+  if (ld_w > INT32_MAX || ld_x > INT32_MAX || (dx && ld_dx > INT32_MAX) || (dW && ld_dw > INT32_MAX)) return SNN_ERR_UNSUPPORTED;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (dtype == SNN_F32) {
     const Plan p = plan_of((int)R, H, C);
-    const Workspace g = carve(workspace, (int)R, H, C, dx || dW, p);
+    const Workspace g = carve(workspace, (int)R, H, dx || dW, p);
     if (workspace_bytes < g.bytes) return SNN_ERR_INVALID_ARG;
     run(static_cast<const float*>(x), ld_x, static_cast<const float*>(W), ld_w, (int)R, H, C, targets, weight, loss,
         row_loss, static_cast<float*>(dx), ld_dx, static_cast<float*>(dW), ld_dw, p, g, s);

@@ -767,8 +767,8 @@ def readout_ce(V_out: torch.Tensor, labels: torch.Tensor, mode: int, dense=False
     return Csr(row_ptr, col, None, None, nnz), eps, loss, ed
 
 
-# These three are called once a step or a token on little data, where the host's work is most of the time: they check
-# what they are given and not again what they have made themselves.
+# These, and embed and layer_norm below, are called once a step or a token on little data, where the host's work is most of
+# the time: they check what they are given and not again what they have made themselves.
 # With a stream given they work as on torch's current one: what they allocate is that stream's, since memory of another
 # stream may still be in use there, and a workspace that is dropped may be handed out there again at once.
 
@@ -852,9 +852,16 @@ def embed(E: torch.Tensor, ids: torch.Tensor, scale=1.0, out=None, stream=None):
     if stream is not None:
         with torch.cuda.stream(stream):
             return embed(E, ids, scale, out)
+    p, code, V, N, ld = _rows(E, "E")
+    R = ids.numel()
     if out is None:
-        out = torch.empty((*ids.shape, E.shape[-1]), dtype=E.dtype, device=E.device)
-    snn_embed(E, ids, scale, out if out.dim() > 1 else out.view(1, -1))
+        out = torch.empty((*ids.shape, N), dtype=E.dtype, device=E.device)
+        o, ld_o = out.data_ptr(), N
+    else:
+        o, code_o, R_o, N_o, ld_o = _rows(out if out.dim() > 1 else out.view(1, -1), "out")
+        if (code_o, R_o, N_o) != (code, R, N):
+            raise ValueError("out must have a row for each of ids, the type and the width of E")
+    _check("snn_embed", lib().snn_embed(p, code, V, N, ld, _ptr(ids, torch.int32, "ids"), R, scale, o, ld_o, _stream()))
     return out
 
 
@@ -882,11 +889,22 @@ def layer_norm(x: torch.Tensor, gamma=None, beta=None, eps=1e-5, out_dtype=None,
     if stream is not None:
         with torch.cuda.stream(stream):
             return layer_norm(x, gamma, beta, eps, out_dtype, out)
+    p, code, R, N, ld = _rows(x, "x")
+    dev, f32, shape = x.device, torch.float32, x.shape[:-1]
     if out is None:
-        out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
-    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    rstd = torch.empty_like(mean)
-    snn_layer_norm(x, gamma, beta, eps, out, mean, rstd)
+        out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=dev)
+        o, code_o, ld_o = out.data_ptr(), _DTYPES.get(out.dtype), N
+        if code_o is None:
+            raise TypeError(f"layer_norm gives float32, bfloat16 or float16, not {out.dtype}")
+    else:
+        o, code_o, R_o, N_o, ld_o = _rows(out, "out")
+        if (R_o, N_o) != (R, N):
+            raise ValueError("out must have the shape of x")
+    mean = torch.empty(shape, dtype=f32, device=dev)
+    rstd = torch.empty(shape, dtype=f32, device=dev)
+    _check("snn_layer_norm", lib().snn_layer_norm(
+        p, code, R, N, ld, _of_rows(gamma, N, f32, "gamma"), _of_rows(beta, N, f32, "beta"), eps, o, code_o, ld_o,
+        mean.data_ptr(), rstd.data_ptr(), _stream()))
     return out, mean, rstd
 
 

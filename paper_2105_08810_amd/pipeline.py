@@ -38,19 +38,31 @@ class Distill:
     scale: float = 1.0
 
 
+@dataclass
+class Norm:
+    """Layer norm of a row of N currents: (x - mean) rstd gamma + beta."""
+    gamma: torch.Tensor  # [N]
+    beta: torch.Tensor  # [N]
+    eps: float = 1e-5
+
+
 class ReadoutRows:
     """What both kinds of network do with their readout's rows: the membrane V_out [T, B, C] read as the logits of
     every step of every sample."""
 
+    def membrane(self) -> torch.Tensor:
+        """V_out of the last forward."""
+        return self.V_out
+
     def record(self, K: int, tau: float = 1.0) -> Record:
         """The forward's answers as a teacher's record."""
-        ids, vals, lse = snn.readout_top(self.V_out, K, tau)
+        ids, vals, lse = snn.readout_top(self.membrane(), K, tau)
         return Record(ids, vals, lse, tau)
 
     def draw(self, u: torch.Tensor, temperature=None, top_k=None, top_p=None, min_p=None, step: Optional[int] = None):
         """One class per sample and step drawn from uniforms u [T, B], or at one step from u [B]; settings as in
         snn.readout_sample. Returns (classes int32, log-probabilities, numbers of classes kept)."""
-        rows = self.V_out if step is None else self.V_out[step]
+        rows = self.membrane() if step is None else self.membrane()[step]
         return snn.readout_sample(rows, u, temperature, top_k, top_p, min_p)
 
     def readout_distilled(self, distill: Distill, dense=False):
@@ -88,15 +100,27 @@ class ReadoutRows:
 
 @dataclass
 class Network(ReadoutRows):
-    X: torch.Tensor  # [T, B, N_in] uint8
+    """A stack of LIF layers and a readout.
+
+    X int32 [T, B] is a sequence of tokens: the first layer's weights are an embedding [vocabulary, N], a token is one
+    input spike of its row (the same as X of one-hot spikes, which are never formed), and the layer's currents are
+    embed_scale times the picked rows, through norm_in where given. A token outside the vocabulary is no spike. The last
+    step's tokens reach no membrane, as the last step's spikes do not.
+
+    labels int32 [T, B] are a target at every step (-1: none there): the loss is the mean cross-entropy over the steps
+    that have one, on the readout's membrane of that step, which is its input trace times W_out. Neither this membrane
+    nor its gradient is kept; membrane() forms it on demand. loss_mode is then not used."""
+    X: torch.Tensor  # [T, B, N_in] uint8 spikes, or [T, B] int32 tokens
     Ws: List[torch.Tensor]
     W_out: torch.Tensor
     alphas: List[float]
     alpha_out: float
-    labels: torch.Tensor  # [B] int32
+    labels: torch.Tensor  # [B] int32, or [T, B] int32: a target at every step
     loss_mode: int  # 0 = max over t, 1 = sum over t
     theta: float = 1.0
     beta: float = 100.0
+    embed_scale: float = 1.0  # tokens only
+    norm_in: Optional[Norm] = None  # tokens only
     # forward state
     V: List[torch.Tensor] = field(default_factory=list)
     S: List[torch.Tensor] = field(default_factory=list)
@@ -113,6 +137,22 @@ class Network(ReadoutRows):
     ck: List[torch.Tensor] = field(default_factory=list)
     _aux2: Optional[torch.cuda.Stream] = None  # second dW stream of the pipelined schedule
     _every: Optional[snn.Csr] = None  # CSR of every entry of V_out (readout_distilled)
+    _embedded: Optional[torch.Tensor] = None  # the picked rows before norm_in, its means and 1 / deviations
+    _norm_stats: Optional[tuple] = None
+    norm_grads: Optional[List[torch.Tensor]] = None  # of norm_in's gamma and beta, from the last sparse_backward
+
+    def __post_init__(self):
+        if self.norm_in is not None and not self.tokens:
+            raise ValueError("norm_in is a norm of tokens' currents: X must be int32 [T, B]")
+
+    @property
+    def tokens(self) -> bool:
+        return self.X.dim() == 2
+
+    @property
+    def every_step(self) -> bool:
+        """Whether there is a target at every step."""
+        return self.labels.dim() == 2
 
     @property
     def T(self):
@@ -130,18 +170,25 @@ class Network(ReadoutRows):
         """Forward buffers, allocated once so repeated steps reuse them."""
         dev = self.X.device
         T, B = self.T, self.B
-        sizes = [self.X.shape[2]] + [W.shape[1] for W in self.Ws]
+        sizes = [self.Ws[0].shape[0]] + [W.shape[1] for W in self.Ws]
         self.V = [torch.empty((T, B, n), dtype=torch.float32, device=dev) for n in sizes[1:]]
         self.S = [torch.empty((T, B, n), dtype=torch.uint8, device=dev) for n in sizes[1:]]
         if self.recompute_k > 0:
             nck = snn.snn_trace_checkpoint_count(T, self.recompute_k)
             self.trace = [None] * self.L
-            self.ck = [torch.empty((nck, B, n), dtype=torch.float32, device=dev) for n in sizes[:-1]]
-        else:
-            self.trace = [torch.empty((T, B, n), dtype=torch.float32, device=dev) for n in sizes[:-1]]
+            self.ck = [None if self.tokens and l == 0 else torch.empty((nck, B, n), dtype=torch.float32, device=dev)
+                       for l, n in enumerate(sizes[:-1])]
+        else:  # tokens have no input trace: their layer's gradient is a sum over the tokens' rows
+            self.trace = [None if self.tokens and l == 0 else torch.empty((T, B, n), dtype=torch.float32, device=dev)
+                          for l, n in enumerate(sizes[:-1])]
         C = self.W_out.shape[1]
-        self.V_out = torch.empty((T, B, C), dtype=torch.float32, device=dev)
-        self.S_out = torch.empty((T, B, C), dtype=torch.uint8, device=dev)
+        self.V_out = self.S_out = None
+        if not self.every_step:
+            self.V_out = torch.empty((T, B, C), dtype=torch.float32, device=dev)
+            self.S_out = torch.empty((T, B, C), dtype=torch.uint8, device=dev)
+        self._embedded = self._norm_stats = None
+        if self.norm_in is not None:
+            self._embedded = torch.empty((max(T - 1, 1), B, sizes[1]), dtype=torch.float32, device=dev)
         self.trace_out = torch.empty((T, B, sizes[-1]), dtype=torch.float32, device=dev)
         self.bits, self.bits_bth = [], None  # made by a forward with b_th
         self._every = None
@@ -161,6 +208,10 @@ class Network(ReadoutRows):
         L = len(self.Ws)
         top = None
         for l, W in enumerate(self.Ws):
+            if l == 0 and self.tokens:
+                top = self._forward_tokens(b_th)
+                x = self.S[0]
+                continue
             if self.recompute_k > 0:
                 snn.trace_checkpoints(x, self.alphas[l], self.recompute_k, ck=self.ck[l])
             # A top layer whose width is whole 64-bit bitset words takes the fused forward, which
@@ -169,18 +220,57 @@ class Network(ReadoutRows):
             # readout, T = 500, B = 256: forward 1.81 -> 1.77 ms). In the two-kernel form the top layer's recurrence is the critical
             # path and the readout's own trace blocks run beside its short recurrence, so the
             # readout keeps writing it (2312 -> 200 -> 10, T = 300, B = 256: 0.446 against 0.453 ms).
-            top = self.trace_out if l == L - 1 and W.shape[1] % 64 == 0 else None
+            # With a target at every step the readout has no forward of its own, and the top layer writes it either way.
+            top = self.trace_out if l == L - 1 and (W.shape[1] % 64 == 0 or self.every_step) else None
             snn.snn_lif_forward_traces(x, W, T, B, W.shape[0], W.shape[1], self.alphas[l], self.theta,
                                        0.0 if b_th is None else b_th, self.V[l], self.S[l], self.trace[l], top,
                                        self.alpha_out, None if b_th is None else self.bits[l])
             x = self.S[l]
+        if self.every_step:
+            self.V_out = None  # of the forward before
+            return self
         snn.snn_lif_forward(x, self.W_out, T, B, self.W_out.shape[0], self.W_out.shape[1], self.alpha_out, INF,
                             self.V_out, self.S_out, None if top is not None else self.trace_out)
         return self
 
+    def _forward_tokens(self, b_th):
+        """The first layer's forward from tokens: the currents of step t straight into V's rows of step t + 1, where the
+        recurrence takes them. Returns the readout's input trace if this is the top layer, which then writes it."""
+        T, B, E, V = self.T, self.B, self.Ws[0], self.V[0]
+        if T > 1:
+            if self.norm_in is None:
+                snn.embed(E, self.X[:-1], self.embed_scale, out=V[1:])
+            else:
+                n = self.norm_in
+                snn.embed(E, self.X[:-1], self.embed_scale, out=self._embedded)
+                _, mean, rstd = snn.layer_norm(self._embedded, n.gamma, n.beta, n.eps, out=V[1:])
+                self._norm_stats = (mean, rstd)
+        top = self.trace_out if self.L == 1 else None
+        snn.snn_lif_forward_currents(V, T, B, E.shape[1], self.alphas[0], self.theta, 0.0 if b_th is None else b_th,
+                                     self.S[0], top, self.alpha_out, None if b_th is None else self.bits[0])
+        return top
+
+    def membrane(self) -> torch.Tensor:
+        """V_out of the last forward; with a target at every step it is formed now."""
+        if self.V_out is None:
+            if not self.S:
+                raise ValueError("membrane() reads a forward's spikes: call forward() first")
+            T, B, C = self.T, self.B, self.W_out.shape[1]
+            self.V_out = torch.empty((T, B, C), dtype=torch.float32, device=self.X.device)
+            S_out = torch.empty((T, B, C), dtype=torch.uint8, device=self.X.device)
+            snn.snn_lif_forward(self.S[-1], self.W_out, T, B, self.W_out.shape[0], C, self.alpha_out, INF, self.V_out, S_out)
+        return self.V_out
+
     def readout(self, dense=False):
         """Readout CSR, eps at its entries, loss (device scalar) and, if asked, dL/dV_out densely."""
+        if self.every_step:
+            raise ValueError("a target at every step: use readout_steps()")
         return snn.readout_ce(self.V_out, self.labels, self.loss_mode, dense=dense)
+
+    def readout_steps(self):
+        """With a target at every step: (gradient by the readout's input trace [T, B, N], dW_out, loss)."""
+        loss, _, dtrace, dW_out = snn.linear_ce(self.trace_out, self.W_out, self.labels)
+        return dtrace, dW_out, loss
 
     def compact(self, b_th, capacities: Optional[List[int]] = None) -> List[snn.Csr]:
         """CSR of every LIF layer's active set: from the forward's bitsets when they were marked
@@ -207,26 +297,46 @@ class Network(ReadoutRows):
         where eps[l] is the gradient w.r.t. layer l's spikes at its active entries. reg_coefs[l]
         ([B, N_l], from activity()) joins layer l's spike gradient before its backward."""
         if ro is None:
-            ro = self.readout()
-        ro_csr, ro_eps = ro[0], ro[1]
+            ro = self.readout_steps() if self.every_step else self.readout()
         ws = workspaces or [None] * (self.L + 1)
-        if aux_stream is not None and self.L >= 2 and self.recompute_k == 0 and workspaces is None:
-            return self._sparse_backward_pipelined(csrs, ro_csr, ro_eps, aux_stream, reg_coefs)
-        dW_out, eps = snn.sparse_backward(self.W_out, self.trace_out, self.alpha_out, ro_csr, ro_eps,
-                                          inp=csrs[self.L - 1], ws=ws[self.L], aux_stream=aux_stream)
+        if self.every_step:  # from the trace back to the spikes that it integrates, where they are wanted
+            dtrace, dW_out, _ = ro
+            eps = snn.leak_grad(dtrace, self.alpha_out, dtrace.shape, out=csrs[self.L - 1])
+        else:
+            ro_csr, ro_eps = ro[0], ro[1]
+            if aux_stream is not None and self.L >= 2 and self.recompute_k == 0 and workspaces is None and not self.tokens:
+                return self._sparse_backward_pipelined(csrs, ro_csr, ro_eps, aux_stream, reg_coefs)
+            dW_out, eps = snn.sparse_backward(self.W_out, self.trace_out, self.alpha_out, ro_csr, ro_eps,
+                                              inp=csrs[self.L - 1], ws=ws[self.L], aux_stream=aux_stream)
         dWs: List[Optional[torch.Tensor]] = [None] * self.L
         epss: List[Optional[torch.Tensor]] = [None] * self.L
         for l in range(self.L - 1, -1, -1):
             if reg_coefs is not None:
                 snn.activity_reg_grad(reg_coefs[l], self.T, eps, csrs[l])
             epss[l] = eps
-            if self.recompute_k > 0:
+            if l == 0 and self.tokens:
+                dWs[0] = self._backward_tokens(csrs[0], eps)
+            elif self.recompute_k > 0:
                 dWs[l], eps = self._layer_backward_recompute(l, csrs, eps, aux_stream)
             else:
                 dWs[l], eps = snn.sparse_backward(self.Ws[l], self.trace[l], self.alphas[l], csrs[l], eps,
                                                   inp=csrs[l - 1] if l > 0 else None, ws=ws[l],
                                                   aux_stream=aux_stream)
         return dWs, dW_out, epss
+
+    def _backward_tokens(self, csr: snn.Csr, eps):
+        """The embedding's gradient (and norm_in's, to norm_grads) from the first layer's spike gradient: gated and led
+        back through the leak to the currents of every step, through the norm, then summed by token."""
+        T, B, (V, N) = self.T, self.B, self.Ws[0].shape
+        dev = self.X.device
+        if T == 1:  # no current reaches a membrane
+            self.norm_grads = None if self.norm_in is None else [torch.zeros(N, device=dev) for _ in range(2)]
+            return torch.zeros((V, N), device=dev)
+        d = snn.leak_grad(eps, self.alphas[0], (T, B, N), inp=csr)[:-1]
+        if self.norm_in is not None:
+            d, dgamma, dbeta = snn.layer_norm_grad(d, self._embedded, self.norm_in.gamma, *self._norm_stats)
+            self.norm_grads = [dgamma, dbeta]
+        return snn.embed_grad(self.X[:-1], d, V, self.embed_scale)
 
     def _sparse_backward_pipelined(self, csrs, ro_csr, ro_eps, aux, reg_coefs=None):
         """The spike gradients form a chain down the layers (each needs the one above), while a
@@ -307,6 +417,8 @@ class Network(ReadoutRows):
         eps_dense list); reg_coefs as in sparse_backward."""
         if self.recompute_k > 0:
             raise ValueError("dense_backward needs the stored input traces (recompute_k = 0)")
+        if self.tokens or self.every_step:
+            raise ValueError("dense_backward takes input spikes and one label a sample")
         if ro is None or ro[3] is None:
             ro = self.readout(dense=True)
         dW_out, eps = snn.dense_backward_ref(self.W_out, self.trace_out, self.V_out, ro[3], self.alpha_out, INF,
@@ -323,7 +435,8 @@ class Network(ReadoutRows):
 
 
     def params(self) -> List[torch.Tensor]:
-        return list(self.Ws) + [self.W_out]
+        norm = [] if self.norm_in is None else [self.norm_in.gamma, self.norm_in.beta]
+        return list(self.Ws) + [self.W_out] + norm
 
     def train_step(self, opt: "Adam", b_th: float, reg: Optional["Penalty"] = None, sparse: bool = True,
                    aux_stream=None, events=None, distill: Optional[Distill] = None):
@@ -336,13 +449,20 @@ class Network(ReadoutRows):
         distill: a teacher's record that the readout learns from beside its labels.
         Returns a dict of device tensors: ce [1], penalty [1] (all layers), grads (list), nnz, and kd [1], the
         distillation loss, with distill."""
+        if not sparse and (self.tokens or self.every_step):
+            raise ValueError("the dense backward takes input spikes and one label a sample")
+        if distill is not None and self.every_step:
+            raise ValueError("distillation beside a target at every step is not offered")
         mark = (lambda k: events[k].record()) if events is not None else (lambda k: None)
         mark(0)
         self.forward(b_th if sparse and math.isfinite(b_th) else None)
         mark(1)
         acts = self.activity(reg) if reg is not None else None
         coefs = [a[0] for a in acts] if acts else None
-        ro = self.readout(dense=not sparse) if distill is None else self.readout_distilled(distill, not sparse)
+        if self.every_step:
+            ro = self.readout_steps()
+        else:
+            ro = self.readout(dense=not sparse) if distill is None else self.readout_distilled(distill, not sparse)
         mark(2)
         if sparse:
             csrs = self.compact(b_th)
@@ -354,7 +474,7 @@ class Network(ReadoutRows):
             dWs, dW_out, _ = self.dense_backward(b_th, ro, reg_coefs=coefs)
             nnz = None
         mark(4)
-        grads = list(dWs) + [dW_out]
+        grads = list(dWs) + [dW_out] + (self.norm_grads if self.norm_in is not None else [])
         opt.step(grads)
         mark(5)
         if acts:

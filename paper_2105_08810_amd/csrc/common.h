@@ -109,7 +109,7 @@ SplitPlan plan_splits(int M, int N, int K, double mac_rate);
 void gemm_split_km(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc, int splits,
                    size_t c_split, hipStream_t s, const uint32_t* live = nullptr);
 void gemm_split_kc(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
-                   hipStream_t s, bool accumulate = false);
+                   hipStream_t s, bool accumulate = false, int splits = 1, size_t c_split = 0);
 void gemm_split_kr(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
                    hipStream_t s);
 // The elements (r, col_idx[e]) of C, as gemm_split_kc forms it, at the entries e < cap of a CSR over C's

@@ -159,10 +159,12 @@ __device__ __forceinline__ BlockTile slice_tile(int tiles_m, int tiles_n, int sp
   return {t / tiles_n, t % tiles_n, z, z < splits};
 }
 
-__device__ __forceinline__ BlockTile row_tile(int tiles_m, int tiles_n) {
-  const int j = tiles_m >= 32 ? (int)blockIdx.x >> 3 : (int)blockIdx.x;
-  const int tm = tiles_m >= 32 ? (int)(blockIdx.x & 7) + 8 * (j / tiles_n) : j / tiles_n;
-  return {tm, j % tiles_n, 0, tm < tiles_m};
+__device__ __forceinline__ BlockTile row_tile(int tiles_m, int tiles_n, int splits) {
+  const int lines = tiles_m >= 32 ? (tiles_m + 7) / 8 * 8 : tiles_m;
+  const int z = (int)blockIdx.x / (lines * tiles_n), t = (int)blockIdx.x % (lines * tiles_n);
+  const int j = tiles_m >= 32 ? t >> 3 : t;
+  const int tm = tiles_m >= 32 ? (t & 7) + 8 * (j / tiles_n) : j / tiles_n;
+  return {tm, j % tiles_n, z, tm < tiles_m && z < splits};
 }
 
 // C[M x N] = sum over this block's K slice of A(m, k) B(k, n); slice z goes to C + z * c_split.
@@ -176,7 +178,7 @@ __device__ __forceinline__ BlockTile row_tile(int tiles_m, int tiles_n) {
 // below (a sum over all rows of positive traces) adds up coherently. A's sign turns from one fold and one tile of
 // rows to the next, so that it cancels (dW of the first of three 1024 x 1024 layers, 27% active: 1.89e-7 -> 1.51e-7
 // of the result from 64 bits; 1.80e-7 entry by entry).
-// KA, KB: k down the rows of A, of B (load_stage's KM). accumulate: C += instead (one K slice alone). MASK: only the k
+// KA, KB: k down the rows of A, of B (load_stage's KM). accumulate: C += instead. MASK: only the k
 // whose bit of live is set take part.
 template <bool KA, bool KB, bool VEC, bool GATHER, bool MASK = false>
 __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, const float* __restrict__ A, int lda,
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, 
   Stage<BN>& Bs = *reinterpret_cast<Stage<BN>*>(lds + sizeof(Stage<kBM>));
   const int w = threadIdx.x / kWave;
   const int l = threadIdx.x % kWave;
-  const BlockTile bt = KA && KB ? slice_tile(tiles_m, tiles_n, splits) : row_tile(tiles_m, tiles_n);
+  const BlockTile bt = KA && KB ? slice_tile(tiles_m, tiles_n, splits) : row_tile(tiles_m, tiles_n, splits);
   if (!bt.ok) return;
   const int m0 = bt.tm * kBM, n0 = bt.tn * BN;
   const int wm = (w / 2) * 64, wn = (w % 2) * (BN / 2);
@@ -526,36 +528,37 @@ namespace {
 // A with k along its rows; B with k down its rows (KB) or along them.
 template <bool KB, bool GATHER>
 void launch_kc(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc, int accumulate,
-               const GatherOut& to, const Gate& gate, hipStream_t s) {
+               int splits, size_t c_split, const GatherOut& to, const Gate& gate, hipStream_t s) {
   const int bn = GATHER ? kBN / 2 : kBN;
   const int tm = (M + kBM - 1) / kBM, tn = (N + bn - 1) / bn;
   const bool vec = lda % 4 == 0 && reinterpret_cast<uintptr_t>(A) % 16 == 0 &&
                    (KB || (ldb % 4 == 0 && reinterpret_cast<uintptr_t>(B) % 16 == 0));
-  const int kps = (K + kBK - 1) / kBK * kBK;
-  const dim3 g((unsigned)((tm >= 32 ? (tm + 7) / 8 * 8 : tm) * tn));
+  int kps = (K + splits - 1) / splits;
+  kps = (kps + kBK - 1) / kBK * kBK;
+  const dim3 g((unsigned)((tm >= 32 ? (tm + 7) / 8 * 8 : tm) * tn * splits));
   if (vec)
     hipLaunchKernelGGL((gemm_split3<false, KB, true, GATHER>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
-                       kps, 0, tm, tn, 1, accumulate, nullptr, to, gate);
+                       kps, c_split, tm, tn, splits, accumulate, nullptr, to, gate);
   else
     hipLaunchKernelGGL((gemm_split3<false, KB, false, GATHER>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
-                       kps, 0, tm, tn, 1, accumulate, nullptr, to, gate);
+                       kps, c_split, tm, tn, splits, accumulate, nullptr, to, gate);
 }
 
 }  // namespace
 
 void gemm_split_kc(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
-                   hipStream_t s, bool accumulate) {
-  launch_kc<false, false>(M, N, K, A, lda, B, ldb, C, ldc, accumulate, GatherOut{}, Gate{}, s);
+                   hipStream_t s, bool accumulate, int splits, size_t c_split) {
+  launch_kc<false, false>(M, N, K, A, lda, B, ldb, C, ldc, accumulate, splits, c_split, GatherOut{}, Gate{}, s);
 }
 
 void gemm_split_kr(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
                    hipStream_t s) {
-  launch_kc<true, false>(M, N, K, A, lda, B, ldb, C, ldc, 0, GatherOut{}, Gate{}, s);
+  launch_kc<true, false>(M, N, K, A, lda, B, ldb, C, ldc, 0, 1, 0, GatherOut{}, Gate{}, s);
 }
 
 void gemm_split_kc_gather(int M, int N, int K, const float* A, int lda, const float* B, int ldb, const GatherOut& to,
                           const Gate& gate, hipStream_t s) {
-  launch_kc<false, true>(M, N, K, A, lda, B, ldb, nullptr, 0, 0, to, gate, s);
+  launch_kc<false, true>(M, N, K, A, lda, B, ldb, nullptr, 0, 0, 1, 0, to, gate, s);
 }
 
 void gemm_f64_km(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc, int splits,

@@ -56,13 +56,13 @@ __device__ __forceinline__ float same_weight(const int32_t* __restrict__ parts, 
 }
 
 // A piece's share of every row's largest logit and sum of exponentials, and the target's logit.
-__global__ __launch_bounds__(kWaves * kWave) void ce_sums(const float* __restrict__ z, int R, int n, int c0,
+__global__ __launch_bounds__(kWaves * kWave) void ce_sums(const float* __restrict__ z, int R, int n, int ld, int c0,
                                                           const int32_t* __restrict__ targets,
                                                           const uint64_t* __restrict__ live, float* __restrict__ top,
                                                           float* __restrict__ sum, float* __restrict__ at_target) {
   const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
   if (r >= R || !alive(live, r)) return;
-  const float* row = z + (size_t)r * n;
+  const float* row = z + (size_t)r * ld;
   const int l = lane_id();
   float m = -INFINITY;
   for (int i = l; i < n; i += kWave) m = fmaxf(m, row[i]);  // a NaN is left to the sum
@@ -110,6 +110,77 @@ __global__ __launch_bounds__(256) void ce_total(const double* __restrict__ parts
   total_of(parts, n, loss);
 }
 
+// A single piece's logits to dz (with GRAD) in one launch: log-sum-exp, loss and gradient of a row a wavefront.
+template <bool GRAD>
+__global__ __launch_bounds__(kWaves * kWave) void ce_rows(float* __restrict__ z, int R, int n, int ld,
+                                                          const int32_t* __restrict__ targets,
+                                                          const uint64_t* __restrict__ live,
+                                                          const int32_t* __restrict__ counts, int n_counts,
+                                                          const float* __restrict__ weight, float* __restrict__ row_loss,
+                                                          double* __restrict__ parts) {
+  __shared__ double all[kWaves];
+  const int w = threadIdx.x / kWave, l = lane_id();
+  const int r = blockIdx.x * kWaves + w;
+  double weighted = 0.0;
+  if (r < R) {
+    float* row = z + (size_t)r * ld;
+    const bool on = alive(live, r);
+    const float k = !on ? 0.0f : weight ? weight[r] : same_weight(counts, n_counts);
+    float loss = 0.0f, lse = 0.0f;
+    const int t = on ? targets[r] : -1;
+    if (on) {
+      float m = -INFINITY;
+      for (int i = l; i < n; i += kWave) m = fmaxf(m, row[i]);  // a NaN is left to the sum
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+      const float from = m > -INFINITY ? m : 0.0f;
+      float s = 0.0f;
+      for (int i = l; i < n; i += kWave) s += expf(row[i] - from);
+      s = wave_sum(s);
+      const float log_sum = logf(s);
+      lse = m + log_sum;
+      loss = (m - row[t]) + log_sum;
+      weighted = (double)k * (double)loss;
+    }
+    if (l == 0 && row_loss) row_loss[r] = loss;
+    if (GRAD) {
+      __builtin_amdgcn_wave_barrier();  // row[t] has been read
+      for (int i = l; i < n; i += kWave) row[i] = on ? k * (expf(row[i] - lse) - (i == t ? 1.0f : 0.0f)) : 0.0f;
+    }
+  }
+  if (l == 0) all[w] = weighted;
+  __syncthreads();
+  if (threadIdx.x == 0) parts[blockIdx.x] = (all[0] + all[1]) + (all[2] + all[3]);
+}
+
+// The last launch: block 0 adds up the loss, the others clear dx in the rows that take no part (dx NULL: none).
+__global__ __launch_bounds__(kWaves * kWave) void ce_finish(const double* __restrict__ parts, int n,
+                                                            float* __restrict__ loss, const uint64_t* __restrict__ live,
+                                                            int R, int H, float* __restrict__ dx, int64_t ld) {
+  if (blockIdx.x == 0) {
+    total_of(parts, n, loss);
+    return;
+  }
+  const int r = ((int)blockIdx.x - 1) * kWaves + threadIdx.x / kWave;
+  if (r >= R || alive(live, r)) return;
+  for (int i = lane_id(); i < H; i += kWave) dx[(int64_t)r * ld + i] = 0.0f;
+}
+
+// dx from its K slices, summed in order; 0 in rows that take no part.
+__global__ __launch_bounds__(kWaves * kWave) void ce_dx(const float* __restrict__ part, int slices,
+                                                        const uint64_t* __restrict__ live, int R, int H,
+                                                        float* __restrict__ dx, int64_t ld) {
+  const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
+  if (r >= R) return;
+  const bool on = alive(live, r);
+  for (int i = lane_id(); i < H; i += kWave) {
+    float s = 0.0f;
+#pragma unroll 4
+    for (int k = 0; k < slices; ++k) s += part[((size_t)k * R + r) * H + i];
+    dx[(int64_t)r * ld + i] = on ? s : 0.0f;
+  }
+}
+
 // Each row's log-sum-exp and loss; the weighted losses of a block in float64.
 __global__ __launch_bounds__(256) void ce_losses(int R, const uint64_t* __restrict__ live, const int32_t* __restrict__ counts,
                                                  int n_counts, const float* __restrict__ weight,
@@ -133,26 +204,18 @@ __global__ __launch_bounds__(256) void ce_losses(int R, const uint64_t* __restri
 }
 
 // z to dz in place; 0 in rows that take no part.
-__global__ __launch_bounds__(kWaves * kWave) void ce_dz(float* __restrict__ z, int R, int n, int c0,
+__global__ __launch_bounds__(kWaves * kWave) void ce_dz(float* __restrict__ z, int R, int n, int ld, int c0,
                                                         const int32_t* __restrict__ targets,
                                                         const uint64_t* __restrict__ live,
                                                         const int32_t* __restrict__ counts, int n_counts,
                                                         const float* __restrict__ weight, const float* __restrict__ lse) {
   const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
   if (r >= R) return;
-  float* row = z + (size_t)r * n;
+  float* row = z + (size_t)r * ld;
   const bool on = alive(live, r);
   const float k = weight ? weight[r] : same_weight(counts, n_counts), ref = on ? lse[r] : 0.0f;
   const int t = targets[r] - c0;
   for (int i = lane_id(); i < n; i += kWave) row[i] = on ? k * (expf(row[i] - ref) - (i == t ? 1.0f : 0.0f)) : 0.0f;
-}
-
-// dx of the rows that take no part.
-__global__ __launch_bounds__(kWaves * kWave) void ce_dead_rows(const uint64_t* __restrict__ live, int R, int H,
-                                                               float* __restrict__ dx, int64_t ld) {
-  const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
-  if (r >= R || alive(live, r)) return;
-  for (int i = lane_id(); i < H; i += kWave) dx[(int64_t)r * ld + i] = 0.0f;
 }
 
 // A piece's columns of dW from its K slices, summed in order.
@@ -209,8 +272,8 @@ __device__ __forceinline__ void mfma_term(int t, const uint4 (&a)[3], const uint
 
 // W's parts, zeros past its ends. For the first product [stage of 32 h][part][h / 8 % 4][class], 8 h of one class each; for
 // the second [stage of 32 h][part][32-class step][g][h], of one h the 8 classes 32 step + 4 g + v and 16 more.
-template <int NT>
-__global__ __launch_bounds__(256) void ce_few_parts(const float* __restrict__ W, int64_t ld, int H, int C,
+template <class T, int NT>
+__global__ __launch_bounds__(256) void ce_few_parts(const T* __restrict__ W, int64_t ld, int H, int C,
                                                     uint4* __restrict__ first, uint4* __restrict__ second) {
   constexpr int Cp = NT * 16, S = (NT + 1) / 2;
   const int stage = blockIdx.x;
@@ -222,7 +285,7 @@ __global__ __launch_bounds__(256) void ce_few_parts(const float* __restrict__ W,
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int h = stage * 32 + 8 * kc + u;
-        x[u] = h < H && c < C ? W[(int64_t)h * ld + c] : 0.0f;
+        x[u] = h < H && c < C ? to_float(W[(int64_t)h * ld + c]) : 0.0f;
       }
       split8(x, part);
 #pragma unroll
@@ -232,7 +295,7 @@ __global__ __launch_bounds__(256) void ce_few_parts(const float* __restrict__ W,
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int c = 32 * step + 16 * (u / 4) + 4 * g + u % 4;
-        x[u] = h < H && c < C ? W[(int64_t)h * ld + c] : 0.0f;
+        x[u] = h < H && c < C ? to_float(W[(int64_t)h * ld + c]) : 0.0f;
       }
       split8(x, part);
 #pragma unroll
@@ -241,13 +304,13 @@ __global__ __launch_bounds__(256) void ce_few_parts(const float* __restrict__ W,
   }
 }
 
-template <int NT, int RT, bool VEC>  // 16-class tiles, 16-row tiles of a wavefront; whether H is a multiple of 4
-__global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, int64_t ld_x, const uint4* __restrict__ first,
+template <class T, int NT, int RT, bool VEC>  // 16-class tiles, 16-row tiles of a wavefront; whether H is a multiple of 8
+__global__ __launch_bounds__(256, 2) void ce_few(const T* __restrict__ x, int64_t ld_x, const uint4* __restrict__ first,
                                                  const uint4* __restrict__ second, int R, int H, int C,
                                                  const int32_t* __restrict__ targets, const float* __restrict__ weight,
                                                  const int32_t* __restrict__ counts, int n_counts,
                                                  float* __restrict__ row_loss, double* __restrict__ parts,
-                                                 float* __restrict__ dx, int64_t ld_dx, float* __restrict__ dz, int ld_dz,
+                                                 T* __restrict__ dx, int64_t ld_dx, float* __restrict__ dz, int ld_dz,
                                                  uint64_t* __restrict__ live) {
   constexpr int kRows = 64 * RT, Cp = NT * 16, S = (NT + 1) / 2;
   // pieces of a stage of W, two stages in LDS: lines [part][g] of its classes, or [part][step][g] of 32 h
@@ -289,21 +352,30 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
   };
   // A lane's part of a stage of x: 8 h of one row of each of its tiles, the second product operand as it stands. Past H
   // any of the row's values will do, since W is 0 there; rows that take no part have results that nothing uses.
-  const float* px[RT];
+  const T* px[RT];
 #pragma unroll
   for (int b = 0; b < RT; ++b) px[b] = x + (int64_t)min(r0 + 16 * (RT * w + b) + i, R - 1) * ld_x;
-  float xs[RT][8];
+  constexpr int kE = 16 / (int)sizeof(T);
+  Raw<T, kE> xs[RT][8 / kE];
+  float xe[RT][8];
   const auto load_x = [&](int h0) {
 #pragma unroll
     for (int b = 0; b < RT; ++b) {
-      if (VEC) {
-        load<float, 4>(px[b] + min(h0 + 8 * g, H - 4), *reinterpret_cast<float(*)[4]>(&xs[b][0]));
-        load<float, 4>(px[b] + min(h0 + 8 * g + 4, H - 4), *reinterpret_cast<float(*)[4]>(&xs[b][4]));
+      if constexpr (VEC) {
+#pragma unroll
+        for (int q = 0; q < 8 / kE; ++q) __builtin_memcpy(xs[b][q].w, px[b] + min(h0 + 8 * g + kE * q, H - kE), 16);
       } else {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) xs[b][u] = px[b][min(h0 + 8 * g + u, H - 1)];
+        for (int u = 0; u < 8; ++u) xe[b][u] = to_float(px[b][min(h0 + 8 * g + u, H - 1)]);
       }
     }
+  };
+  const auto split_x = [&](int b, uint4 (&part)[3]) {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int q = 0; q < 8 / kE; ++q) xs[b][q].to(*reinterpret_cast<float(*)[kE]>(&xe[b][kE * q]));
+    }
+    split8(xe[b], part);
   };
   // every block begins at another stage: rows are often a power of two apart, and blocks at the same h would meet in the
   // same memory channels
@@ -315,7 +387,7 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
       at = at + 1 == stages ? 0 : at + 1;  // the stage after this one
       uint4 fb[RT][3];
 #pragma unroll
-      for (int b = 0; b < RT; ++b) split8(xs[b], fb[b]);
+      for (int b = 0; b < RT; ++b) split_x(b, fb[b]);
       gemm16::stage_barrier();  // this stage of W is there, the one before has been read
       if (n + 1 < stages) {
         load_w(first + (size_t)at * kW1, kW1, (n + 1) & 1);
@@ -438,7 +510,7 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
         float o[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) o[v] = mine ? (d[half][b][v] + e[half][b][v]) * (1.0f / kDzUp) * k[b] : 0.0f;
-        store_in<float, 4>(dx + (int64_t)r * ld_dx, min(h0 + 16 * half + 4 * g, H), H, o);
+        store_in<T, 4>(dx + (int64_t)r * ld_dx, min(h0 + 16 * half + 4 * g, H), H, o);
       }
     }
   }
@@ -447,10 +519,10 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
 // dW of few rows and classes: a block 16 h and all classes, its 16 wavefronts every sixteenth run of 16 rows, straight from
 // memory on the float32 matrix cores; their sums are added in LDS, in order. Block 0 also adds up the loss.
 constexpr int kFewDwRows = 4096;
-template <int NT>
-__global__ __launch_bounds__(1024) void ce_few_dw(const float* __restrict__ x, int64_t ld_x, const float* __restrict__ dz,
+template <class T, int NT>
+__global__ __launch_bounds__(1024) void ce_few_dw(const T* __restrict__ x, int64_t ld_x, const float* __restrict__ dz,
                                                   int ld_dz, const uint64_t* __restrict__ live, int R, int H, int C,
-                                                  float* __restrict__ dW, int64_t ld_dw, const double* __restrict__ parts,
+                                                  T* __restrict__ dW, int64_t ld_dw, const double* __restrict__ parts,
                                                   int n_parts, float* __restrict__ loss) {
   __shared__ float sum[16][NT * 16][17];
   const int w = threadIdx.x / kWave, l = lane_id(), i = l % 16, g = l / 16;
@@ -464,7 +536,7 @@ __global__ __launch_bounds__(1024) void ce_few_dw(const float* __restrict__ x, i
     for (int j = 0; j < 4; ++j) {
       const int r = r0 + 4 * j + g;
       const bool on = r < R && h < H && alive(live, r);
-      b[j] = on ? x[(int64_t)r * ld_x + h] : 0.0f;
+      b[j] = on ? to_float(x[(int64_t)r * ld_x + h]) : 0.0f;
 #pragma unroll
       for (int a = 0; a < NT; ++a) d[j][a] = r < R && 16 * a + i < ld_dz ? dz[(size_t)r * ld_dz + 16 * a + i] : 0.0f;
     }
@@ -483,7 +555,7 @@ __global__ __launch_bounds__(1024) void ce_few_dw(const float* __restrict__ x, i
     float s = 0.0f;
 #pragma unroll
     for (int k = 0; k < 16; ++k) s += sum[k][c][n];
-    if (c < C && blockIdx.x * 16 + n < H) dW[(int64_t)(blockIdx.x * 16 + n) * ld_dw + c] = s;
+    if (c < C && blockIdx.x * 16 + n < H) dW[(int64_t)(blockIdx.x * 16 + n) * ld_dw + c] = from_float<T>(s);
   }
   if (blockIdx.x == 0 && threadIdx.x < kWave) {
     double s = 0.0;
@@ -494,19 +566,22 @@ __global__ __launch_bounds__(1024) void ce_few_dw(const float* __restrict__ x, i
   }
 }
 
+// Whether a call takes the way of few classes: in 16 bits only where its dW does, whose rows are multiplied in float32.
+bool few_of(int dtype, int R, int C) { return C <= kFew && (dtype == SNN_F32 || R <= kFewDwRows); }
+
 struct Plan {
-  bool few;
-  int width, pieces, slices;  // classes of a piece; K slices of dW
+  int width, pieces;          // classes of a piece
+  int dw_slices, dx_slices;   // K slices of the gradients' products
   int ld;                     // of a piece's logits
 };
 
 Plan plan_of(int R, int H, int C) {
   Plan p;
-  p.few = C <= kFew;
-  p.width = p.few ? C : (int)std::min<int64_t>(C, std::max<int64_t>(256, kPiece / R / 128 * 128));
+  p.width = (int)std::min<int64_t>(C, std::max<int64_t>(256, kPiece / R / 128 * 128));
   p.pieces = (C + p.width - 1) / p.width;
-  p.ld = p.few ? (C + 3) / 4 * 4 : p.width;
-  p.slices = plan_splits(H, p.width, R, 88e12).splits;
+  p.ld = (p.width + 3) / 4 * 4;
+  p.dw_slices = plan_splits(H, p.width, R, 88e12).splits;
+  p.dx_slices = plan_splits(R, H, p.width, 88e12).splits;
   return p;
 }
 
@@ -516,27 +591,28 @@ struct Workspace {
   uint64_t* live;
   int32_t* counts;
   uint4 *first, *second;
-  float *z, *dW, *top, *sum, *at_target, *lse;
+  float *z, *dX, *dW, *top, *sum, *at_target, *lse;
   double* parts;
   size_t bytes;
 };
 
-Workspace carve(void* ws, int R, int H, bool grad, const Plan& p) {
+Workspace carve(void* ws, int R, int H, bool few, bool grad, const Plan& p) {
   Carve c(ws);
   Workspace g;
   g.live = c.take<uint64_t>(((size_t)R + 63) / 64);
   g.counts = c.take<int32_t>(kCountParts);
-  const size_t stages = p.few ? (H + 31) / 32 : 0;
+  const size_t stages = few ? (H + 31) / 32 : 0;
   g.first = c.take<uint4>(stages * 12 * kFew);
   g.second = c.take<uint4>(stages * 12 * kFew);
-  const size_t rows = p.few ? 0 : (size_t)R;
+  const size_t rows = few || p.pieces == 1 ? 0 : (size_t)R;
   g.top = c.take<float>(rows);
   g.sum = c.take<float>(rows);
   g.at_target = c.take<float>(rows);
   g.lse = c.take<float>(rows);
-  g.parts = c.take<double>(p.few ? (R + 63) / 64 : kLossParts);
-  g.z = c.take<float>(p.few && !grad ? 0 : (size_t)R * p.ld);
-  g.dW = c.take<float>(grad && p.slices > 1 ? (size_t)p.slices * H * p.width : 0);
+  g.parts = c.take<double>(few ? (R + 63) / 64 : p.pieces == 1 ? (R + kWaves - 1) / kWaves : kLossParts);
+  g.z = c.take<float>(few && !grad ? 0 : (size_t)R * p.ld);
+  g.dX = c.take<float>(!few && grad && p.dx_slices > 1 ? (size_t)p.dx_slices * R * H : 0);
+  g.dW = c.take<float>(grad && p.dw_slices > 1 ? (size_t)p.dw_slices * H * p.width : 0);
   g.bytes = c.off;
   return g;
 }
@@ -545,75 +621,100 @@ Workspace carve(void* ws, int R, int H, bool grad, const Plan& p) {
 void enqueue_dw(const float* x, int64_t ld_x, const float* dz, int ld_dz, int R, int H, int n, float* dW, int64_t ld_dw,
                 const Plan& p, const Workspace& g, hipStream_t s) {
   const uint32_t* live = reinterpret_cast<const uint32_t*>(g.live);  // the words' halves in order
-  if (p.slices == 1) {
+  if (p.dw_slices == 1) {
     gemm_split_km(H, n, R, x, (int)ld_x, dz, ld_dz, dW, (int)ld_dw, 1, 0, s, live);
     return;
   }
-  gemm_split_km(H, n, R, x, (int)ld_x, dz, ld_dz, g.dW, n, p.slices, (size_t)H * n, s, live);
-  hipLaunchKernelGGL(ce_dw, dim3((unsigned)((n + 255) / 256), (unsigned)std::min(H, 1024)), dim3(256), 0, s, g.dW, p.slices,
-                     H, n, dW, ld_dw);
+  gemm_split_km(H, n, R, x, (int)ld_x, dz, ld_dz, g.dW, n, p.dw_slices, (size_t)H * n, s, live);
+  hipLaunchKernelGGL(ce_dw, dim3((unsigned)((n + 255) / 256), (unsigned)std::min(H, 1024)), dim3(256), 0, s, g.dW,
+                     p.dw_slices, H, n, dW, ld_dw);
 }
 
-template <int NT>
-void run_few(const float* x, int64_t ld_x, const float* W, int64_t ld_w, int R, int H, int C, const int32_t* targets,
-             const float* weight, float* loss, float* row_loss, float* dx, int64_t ld_dx, float* dW, int64_t ld_dw,
-             const Plan& p, const Workspace& g, hipStream_t s) {
+template <class T, int NT>
+void run_few(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int C, const int32_t* targets,
+             const float* weight, float* loss, float* row_loss, T* dx, int64_t ld_dx, T* dW, int64_t ld_dw, const Plan& p,
+             const Workspace& g, hipStream_t s) {
   // 32 rows a wavefront read W's parts half as often; 16 where 32 would leave compute units without a block
-  const bool wide = (R + 127) / 128 >= 2 * cu_count();
+  const bool wide = (R + 127) / 128 >= 2 * cu_count(), vec = H % 8 == 0;
   const int blocks = wide ? (R + 127) / 128 : (R + 63) / 64;
   const int counted = weight || R <= kCountHere ? 0 : std::min(kCountParts, (R + 1023) / 1024);
   if (counted)
     hipLaunchKernelGGL(ce_live, dim3((unsigned)counted), dim3(256), 0, s, targets, weight, R, C, g.live, g.counts);
-  hipLaunchKernelGGL(ce_few_parts<NT>, dim3((unsigned)((H + 31) / 32)), dim3(256), 0, s, W, ld_w, H, C, g.first, g.second);
-  const bool vec = H % 4 == 0;
-  hipLaunchKernelGGL((wide ? (vec ? ce_few<NT, 2, true> : ce_few<NT, 2, false>) : (vec ? ce_few<NT, 1, true> : ce_few<NT, 1, false>)),
-                     dim3((unsigned)blocks), dim3(256), 0, s, x, ld_x, g.first,
-                     g.second, R, H, C, targets, weight, counted ? g.counts : nullptr, counted, row_loss, g.parts, dx, ld_dx,
-                     dW ? g.z : nullptr, p.ld, counted ? nullptr : g.live);
+  hipLaunchKernelGGL((ce_few_parts<T, NT>), dim3((unsigned)((H + 31) / 32)), dim3(256), 0, s, W, ld_w, H, C, g.first,
+                     g.second);
+  const auto few = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, x, ld_x, g.first, g.second, R, H, C, targets, weight,
+                       counted ? g.counts : nullptr, counted, row_loss, g.parts, dx, ld_dx, dW ? g.z : nullptr, p.ld,
+                       counted ? nullptr : g.live);
+  };
+  if constexpr (sizeof(T) == 4) {
+    if (wide) few(vec ? ce_few<T, NT, 2, true> : ce_few<T, NT, 2, false>);
+    else few(vec ? ce_few<T, NT, 1, true> : ce_few<T, NT, 1, false>);
+  } else {
+    few(vec ? ce_few<T, NT, 1, true> : ce_few<T, NT, 1, false>);  // at most kFewDwRows rows
+  }
   if (dW && R <= kFewDwRows) {
-    hipLaunchKernelGGL(ce_few_dw<NT>, dim3((unsigned)((H + 15) / 16)), dim3(1024), 0, s, x, ld_x, g.z, p.ld, g.live, R, H, C,
-                       dW, ld_dw, g.parts, blocks, loss);
+    hipLaunchKernelGGL((ce_few_dw<T, NT>), dim3((unsigned)((H + 15) / 16)), dim3(1024), 0, s, x, ld_x, g.z, p.ld, g.live, R,
+                       H, C, dW, ld_dw, g.parts, blocks, loss);
     return;
   }
   hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, blocks, loss);
-  if (dW) enqueue_dw(x, ld_x, g.z, p.ld, R, H, C, dW, ld_dw, p, g, s);
+  if constexpr (sizeof(T) == 4) {
+    if (dW) enqueue_dw(x, ld_x, g.z, p.ld, R, H, C, dW, ld_dw, p, g, s);
+  }
+}
+
+template <class T>
+void run_few(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int C, const int32_t* targets,
+             const float* weight, float* loss, float* row_loss, T* dx, int64_t ld_dx, T* dW, int64_t ld_dw, const Plan& p,
+             const Workspace& g, hipStream_t s) {
+#define SNN_FEW(NT)                                                                                                       \
+  run_few<T, NT>(x, ld_x, W, ld_w, R, H, C, targets, weight, loss, row_loss, dx, ld_dx, dW, ld_dw, p, g, s)
+  if (C <= 16) SNN_FEW(1);
+  else if (C <= 32) SNN_FEW(2);
+  else if (C <= 64) SNN_FEW(4);
+  else if (C <= 112) SNN_FEW(7);
+  else SNN_FEW(8);
+#undef SNN_FEW
 }
 
 void run(const float* x, int64_t ld_x, const float* W, int64_t ld_w, int R, int H, int C, const int32_t* targets,
          const float* weight, float* loss, float* row_loss, float* dx, int64_t ld_dx, float* dW, int64_t ld_dw,
          const Plan& p, const Workspace& g, hipStream_t s) {
-  if (p.few) {
-#define SNN_FEW(NT)                                                                                                     \
-  run_few<NT>(x, ld_x, W, ld_w, R, H, C, targets, weight, loss, row_loss, dx, ld_dx, dW, ld_dw, p, g, s)
-    if (C <= 16) SNN_FEW(1);
-    else if (C <= 32) SNN_FEW(2);
-    else if (C <= 64) SNN_FEW(4);
-    else if (C <= 112) SNN_FEW(7);
-    else SNN_FEW(8);
-#undef SNN_FEW
-    return;
-  }
   const dim3 rows((unsigned)((R + kWaves - 1) / kWaves)), waves(kWaves * kWave);
   const int counted = std::min(kCountParts, (R + 1023) / 1024);
+  const bool grad = dx || dW;
   hipLaunchKernelGGL(ce_live, dim3((unsigned)counted), dim3(256), 0, s, targets, weight, R, C, g.live, g.counts);
-  for (int c0 = 0; c0 < C; c0 += p.width) {
-    const int n = std::min(p.width, C - c0);
-    gemm_split_kr(R, n, H, x, (int)ld_x, W + c0, (int)ld_w, g.z, n, s);
-    hipLaunchKernelGGL(ce_sums, rows, waves, 0, s, g.z, R, n, c0, targets, g.live, g.top, g.sum, g.at_target);
+  int n_parts = (int)rows.x;
+  if (p.pieces == 1) {
+    gemm_split_kr(R, C, H, x, (int)ld_x, W, (int)ld_w, g.z, p.ld, s);
+    hipLaunchKernelGGL((grad ? ce_rows<true> : ce_rows<false>), rows, waves, 0, s, g.z, R, C, p.ld, targets, g.live,
+                       g.counts, counted, weight, row_loss, g.parts);
+  } else {
+    for (int c0 = 0; c0 < C; c0 += p.width) {
+      const int n = std::min(p.width, C - c0);
+      gemm_split_kr(R, n, H, x, (int)ld_x, W + c0, (int)ld_w, g.z, p.ld, s);
+      hipLaunchKernelGGL(ce_sums, rows, waves, 0, s, g.z, R, n, p.ld, c0, targets, g.live, g.top, g.sum, g.at_target);
+    }
+    n_parts = std::min(kLossParts, (R + 255) / 256);
+    hipLaunchKernelGGL(ce_losses, dim3((unsigned)n_parts), dim3(256), 0, s, R, g.live, g.counts, counted, weight, g.top,
+                       g.sum, g.at_target, g.lse, row_loss, g.parts);
   }
-  const int blocks = std::min(kLossParts, (R + 255) / 256);
-  hipLaunchKernelGGL(ce_losses, dim3((unsigned)blocks), dim3(256), 0, s, R, g.live, g.counts, counted, weight, g.top, g.sum,
-                     g.at_target, g.lse, row_loss, g.parts);
-  hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, blocks, loss);
-  if (!dx && !dW) return;
-  for (int c0 = 0; c0 < C; c0 += p.width) {
+  float* to = p.dx_slices > 1 ? g.dX : dx;
+  const int ld_to = p.dx_slices > 1 ? H : (int)ld_dx;
+  for (int c0 = 0; grad && c0 < C; c0 += p.width) {
     const int n = std::min(p.width, C - c0);
-    if (p.pieces > 1) gemm_split_kr(R, n, H, x, (int)ld_x, W + c0, (int)ld_w, g.z, n, s);
-    hipLaunchKernelGGL(ce_dz, rows, waves, 0, s, g.z, R, n, c0, targets, g.live, g.counts, counted, weight, g.lse);
-    if (dx) gemm_split_kc(R, H, n, g.z, n, W + c0, (int)ld_w, dx, (int)ld_dx, s, c0 > 0);
-    if (dW) enqueue_dw(x, ld_x, g.z, n, R, H, n, dW + c0, ld_dw, p, g, s);
+    if (p.pieces > 1) {
+      gemm_split_kr(R, n, H, x, (int)ld_x, W + c0, (int)ld_w, g.z, p.ld, s);
+      hipLaunchKernelGGL(ce_dz, rows, waves, 0, s, g.z, R, n, p.ld, c0, targets, g.live, g.counts, counted, weight, g.lse);
+    }
+    if (dx) gemm_split_kc(R, H, n, g.z, p.ld, W + c0, (int)ld_w, to, ld_to, s, c0 > 0, p.dx_slices, (size_t)R * H);
+    if (dW) enqueue_dw(x, ld_x, g.z, p.ld, R, H, n, dW + c0, ld_dw, p, g, s);
   }
-  if (dx) hipLaunchKernelGGL(ce_dead_rows, rows, waves, 0, s, g.live, R, H, dx, ld_dx);
+  if (dx && p.dx_slices > 1)
+    hipLaunchKernelGGL(ce_dx, rows, waves, 0, s, g.dX, p.dx_slices, g.live, R, H, dx, ld_dx);
+  const bool clear = dx && p.dx_slices == 1;
+  hipLaunchKernelGGL(ce_finish, dim3(1 + (clear ? rows.x : 0)), waves, 0, s, g.parts, n_parts, loss, g.live, R, H, dx, ld_dx);
 }
 
 // ------------------------------------------------------------------ 16-bit operands
@@ -766,18 +867,29 @@ __global__ __launch_bounds__(gemm16::kThreads, 2) void ce_logits16(
   const gemm16::Tiles t = gemm16::tile_of(tiles_m, tiles_n, 1);
   if (!t.ok || t.n * kTile >= pos[R]) return;
   gemm16::Product<T, true, false> z;
-  z.run(W, ldw, t.m * kTile, X, Hp, t.n * kTile, 0, stages, smem);
   const int l = lane_id(), g = l / 16;
   const int m0 = t.m * kTile + z.m_of_wave();
   const int first = c0 + m0;  // class of the wavefront's first m
   const int n0 = t.n * kTile + z.n_of_wave() + l % 16;
+  // what the rows need at the end is asked for now
+  int32_t tgt[4];
+  float top[4], k[4];
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    tgt[b] = target[n0 + 16 * b];
+    if (GRAD) {
+      top[b] = tgt[b] >= 0 ? lse[n0 + 16 * b] : 0.0f;
+      k[b] = tgt[b] >= 0 ? w[n0 + 16 * b] / *ref * kRaise<T> : 0.0f;
+    }
+  }
+  z.run(W, ldw, t.m * kTile, X, Hp, t.n * kTile, 0, stages, smem);
   constexpr float kLog2e = 1.44269504088896340736f;
   const bool ragged = first + kPart > C;
 #pragma unroll
   for (int b = 0; b < 4; ++b) {
     const int n = n0 + 16 * b;
-    const int at = target[n] - first;  // the target among this wavefront's classes
-    const bool here = target[n] >= 0 && (unsigned)at < (unsigned)kPart;
+    const int at = tgt[b] - first;  // the target among this wavefront's classes
+    const bool here = tgt[b] >= 0 && (unsigned)at < (unsigned)kPart;
     if (ragged) {
 #pragma unroll
       for (int a = 0; a < 8; ++a)
@@ -810,16 +922,14 @@ __global__ __launch_bounds__(gemm16::kThreads, 2) void ce_logits16(
       s += __shfl_xor(s, 32, kWave);
       if (g == 0) part[(size_t)(first / kPart) * Rp + n] = make_float2(m, s);
     } else {
-      const bool live = target[n] >= 0;
-      const float k = live ? w[n] / *ref * kRaise<T> : 0.0f;
-      const float from = live ? lse[n] : 0.0f;
+      const bool live = tgt[b] >= 0;
 #pragma unroll
       for (int a = 0; a < 8; ++a) {
         T d[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const float p = __builtin_amdgcn_exp2f((z.acc[a][b][v] - from) * kLog2e);
-          d[v] = from_float<T>(live ? k * (p - (here && at == 16 * a + 4 * g + v ? 1.0f : 0.0f)) : 0.0f);
+          const float p = __builtin_amdgcn_exp2f((z.acc[a][b][v] - top[b]) * kLog2e);
+          d[v] = from_float<T>(live ? k[b] * (p - (here && at == 16 * a + 4 * g + v ? 1.0f : 0.0f)) : 0.0f);
         }
         *reinterpret_cast<uint2*>(G + (size_t)n * ldg + m0 + 16 * a + 4 * g) = __builtin_bit_cast(uint2, d);
       }
@@ -894,27 +1004,41 @@ __global__ __launch_bounds__(gemm16::kThreads, 2) void ce_dx16(const T* __restri
     }
 }
 
+// dx from its K slices: a block takes 256 h of a row, its wavefronts a quarter of the slices each. Block (0, 0) also adds up
+// the loss.
 template <class T>
 __global__ __launch_bounds__(kWaves * kWave) void ce_dx_out16(const float* __restrict__ dX, int slices, int R, int Rp, int H,
                                                               int Hp, const int32_t* __restrict__ pos,
                                                               const float* __restrict__ ref, T* __restrict__ dx,
-                                                              int64_t ld) {
-  const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
-  if (r >= R) return;
+                                                              int64_t ld, const double* __restrict__ parts, int n_parts,
+                                                              float* __restrict__ loss) {
+  __shared__ float4 all[kWaves][kWave];
+  if (blockIdx.x == 0 && blockIdx.y == 0) total_of(parts, n_parts, loss);
+  const int w = threadIdx.x / kWave, l = lane_id();
+  const int r = blockIdx.x, i = (blockIdx.y * kWave + l) * 4;
   const int p = pos[r];
   const bool live = pos[r + 1] > p;
-  const float k = *ref / kRaise<T>;
-  for (int i = lane_id() * 4; i < H; i += kWave * 4) {
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (live)
-      for (int q = 0; q < slices; ++q) {
-        const float4 v = *reinterpret_cast<const float4*>(dX + ((size_t)q * Rp + p) * Hp + i);
-        s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
-      }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) s[u] *= k;
-    store_in<T, 4>(dx + (int64_t)r * ld, i, H, s);
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (live && i < Hp) {
+    const int share = (slices + kWaves - 1) / kWaves;
+#pragma unroll 4
+    for (int q = w * share; q < min(slices, (w + 1) * share); ++q) {
+      const float4 v = *reinterpret_cast<const float4*>(dX + ((size_t)q * Rp + p) * Hp + i);
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
   }
+  all[w][l] = s;
+  __syncthreads();
+  if (w > 0 || i >= H) return;
+  float o[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+  for (int q = 1; q < kWaves; ++q) {
+    o[0] += all[q][l].x; o[1] += all[q][l].y; o[2] += all[q][l].z; o[3] += all[q][l].w;
+  }
+  const float k = *ref / kRaise<T>;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) o[u] *= k;
+  store_in<T, 4>(dx + (int64_t)r * ld, i, H, o);
 }
 
 // dW of a piece's n columns: the tile itself with one slice, else its share to part[slice][h][width].
@@ -1087,7 +1211,7 @@ void run16(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int
   }
   hipLaunchKernelGGL(ce_join16, dim3((unsigned)(p.Rp / 32)), dim3(1024), 0, s, g.part, padded(C, kTile) / kPart, R, p.Rp,
                      g.pos, g.row_of, g.at_target, g.w, g.lse, row_loss, g.parts);
-  hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, p.Rp / 32, loss);
+  if (!dx) hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, p.Rp / 32, loss);
   if (!dx && !dW) return;
   for (int c0 = 0; c0 < C; c0 += p.width) {
     const int n = std::min(p.width, C - c0), tiles_m = (n + kTile - 1) / kTile;
@@ -1111,8 +1235,8 @@ void run16(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int
     }
   }
   if (dx)
-    hipLaunchKernelGGL(ce_dx_out16<T>, rows_of(R), waves, 0, s, g.dX, p.dx_slices, R, p.Rp, H, p.Hp, g.pos, g.ref, dx,
-                       ld_dx);
+    hipLaunchKernelGGL(ce_dx_out16<T>, dim3((unsigned)R, (unsigned)((H + 255) / 256)), waves, 0, s, g.dX, p.dx_slices, R,
+                       p.Rp, H, p.Hp, g.pos, g.ref, dx, ld_dx, g.parts, p.Rp / 32, loss);
 }
 
 snn_status check_sizes(int dtype, int64_t R, int H, int C) {
@@ -1128,7 +1252,8 @@ using namespace snn;
 
 extern "C" size_t snn_linear_ce_workspace(int dtype, int64_t R, int H, int C, int grad) {
   if (check_sizes(dtype, R, H, C) != SNN_OK) return 0;
-  if (dtype == SNN_F32) return carve(nullptr, (int)R, H, grad != 0, plan_of((int)R, H, C)).bytes;
+  const bool few = few_of(dtype, (int)R, C);
+  if (few || dtype == SNN_F32) return carve(nullptr, (int)R, H, few, grad != 0, plan_of((int)R, H, C)).bytes;
   return carve16(nullptr, (int)R, H, C, grad != 0, plan16_of((int)R, H, C)).bytes;
 }
 
@@ -1143,22 +1268,25 @@ extern "C" snn_status snn_linear_ce(const void* x, const void* W, int dtype, int
     return SNN_ERR_INVALID_ARG;
   if (ld_w > INT32_MAX || ld_x > INT32_MAX || (dx && ld_dx > INT32_MAX) || (dW && ld_dw > INT32_MAX)) return SNN_ERR_UNSUPPORTED;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (dtype == SNN_F32) {
+  const bool few = few_of(dtype, (int)R, C);
+  if (few || dtype == SNN_F32) {
     const Plan p = plan_of((int)R, H, C);
-    const Workspace g = carve(workspace, (int)R, H, dx || dW, p);
+    const Workspace g = carve(workspace, (int)R, H, few, dx || dW, p);
     if (workspace_bytes < g.bytes) return SNN_ERR_INVALID_ARG;
-    run(static_cast<const float*>(x), ld_x, static_cast<const float*>(W), ld_w, (int)R, H, C, targets, weight, loss,
-        row_loss, static_cast<float*>(dx), ld_dx, static_cast<float*>(dW), ld_dw, p, g, s);
+#define SNN_CE(RUN, T)                                                                                                \
+  RUN(static_cast<const T*>(x), ld_x, static_cast<const T*>(W), ld_w, (int)R, H, C, targets, weight, loss, row_loss,  \
+      static_cast<T*>(dx), ld_dx, static_cast<T*>(dW), ld_dw, p, g, s)
+    if (!few) SNN_CE(run, float);
+    else if (dtype == SNN_F32) SNN_CE(run_few<float>, float);
+    else if (dtype == SNN_BF16) SNN_CE(run_few<Bf16>, Bf16);
+    else SNN_CE(run_few<F16>, F16);
     return launch_status();
   }
   const Plan16 p = plan16_of((int)R, H, C);
   const Workspace16 g = carve16(workspace, (int)R, H, C, dx || dW, p);
   if (workspace_bytes < g.bytes) return SNN_ERR_INVALID_ARG;
-#define SNN_CE(T)                                                                                                   \
-  run16<T>(static_cast<const T*>(x), ld_x, static_cast<const T*>(W), ld_w, (int)R, H, C, targets, weight, loss,     \
-           row_loss, static_cast<T*>(dx), ld_dx, static_cast<T*>(dW), ld_dw, p, g, s)
-  if (dtype == SNN_BF16) SNN_CE(Bf16);
-  else SNN_CE(F16);
+  if (dtype == SNN_BF16) SNN_CE(run16, Bf16);
+  else SNN_CE(run16, F16);
 #undef SNN_CE
   return launch_status();
 }

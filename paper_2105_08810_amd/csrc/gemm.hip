@@ -58,7 +58,7 @@ __device__ __forceinline__ void split8(const float (&x)[8], uint4& h, uint4& m, 
 // One operand's share of a stage of ROWS (128 or 64) rows: two pieces or one (8 k of one row each) per thread.
 //   KM: element (r, k) at p[k * ld + r] (rows contiguous): a piece is eight loads, each 256 contiguous
 //       bytes over a wavefront.
-//   else p[r * ld + k] (k contiguous): a piece is 32 contiguous bytes.
+//   else p[r * ld + k] (k contiguous): a piece is 32 contiguous bytes, at any alignment.
 // Rows past the end read the last row (their results are not stored); k past k_hi reads as 0, and so does a k whose bit of
 // live (32 k a word, KM only) is 0.
 template <bool KM, int ROWS>
@@ -68,7 +68,7 @@ __device__ __forceinline__ void piece_of(int q, int& row, int& kc) {
   kc = KM ? idx / ROWS : idx % kKC;
 }
 
-template <bool KM, bool VEC, int ROWS, bool MASK = false>
+template <bool KM, int ROWS, bool MASK = false>
 __device__ __forceinline__ void load_stage(const float* __restrict__ p, int ld, int r0, int R, int k0, int k_hi,
                                            float (&x)[ROWS / 64][8], const uint32_t* __restrict__ live = nullptr) {
 #pragma unroll
@@ -92,10 +92,8 @@ __device__ __forceinline__ void load_stage(const float* __restrict__ p, int ld, 
       }
     } else {
       const float* s = p + (size_t)r * ld + k;
-      if (VEC && k + 8 <= k_hi) {
-        const float4 a = *reinterpret_cast<const float4*>(s), b = *reinterpret_cast<const float4*>(s + 4);
-        x[q][0] = a.x; x[q][1] = a.y; x[q][2] = a.z; x[q][3] = a.w;
-        x[q][4] = b.x; x[q][5] = b.y; x[q][6] = b.z; x[q][7] = b.w;
+      if (k + 8 <= k_hi) {
+        __builtin_memcpy(x[q], s, 32);
       } else {
 #pragma unroll
         for (int u = 0; u < 8; ++u) x[q][u] = k + u < k_hi ? s[u] : 0.0f;
@@ -180,7 +178,7 @@ __device__ __forceinline__ BlockTile row_tile(int tiles_m, int tiles_n, int spli
 // of the result from 64 bits; 1.80e-7 entry by entry).
 // KA, KB: k down the rows of A, of B (load_stage's KM). accumulate: C += instead. MASK: only the k
 // whose bit of live is set take part.
-template <bool KA, bool KB, bool VEC, bool GATHER, bool MASK = false>
+template <bool KA, bool KB, bool GATHER, bool MASK = false>
 __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, const float* __restrict__ A, int lda,
                                                            const float* __restrict__ B, int ldb,
                                                            float* __restrict__ C, int ldc, int k_per_split,
@@ -266,8 +264,8 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, 
 
   float xa[2][8], xb[BN / 64][8];
   if (k_lo < k_hi) {
-    load_stage<KA, VEC, kBM, MASK>(A, lda, m0, M, k_lo, k_hi, xa, live);
-    load_stage<KB, VEC, BN>(B, ldb, n0, N, k_lo, k_hi, xb);
+    load_stage<KA, kBM, MASK>(A, lda, m0, M, k_lo, k_hi, xa, live);
+    load_stage<KB, BN>(B, ldb, n0, N, k_lo, k_hi, xb);
   }
   int stage = 0;
   for (int k0 = k_lo; k0 < k_hi; k0 += kBK) {
@@ -275,8 +273,8 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, 
     store_stage<KB, BN>(Bs, xb, kUp);
     __syncthreads();
     if (k0 + kBK < k_hi) {
-      load_stage<KA, VEC, kBM, MASK>(A, lda, m0, M, k0 + kBK, k_hi, xa, live);
-      load_stage<KB, VEC, BN>(B, ldb, n0, N, k0 + kBK, k_hi, xb);
+      load_stage<KA, kBM, MASK>(A, lda, m0, M, k0 + kBK, k_hi, xa, live);
+      load_stage<KB, BN>(B, ldb, n0, N, k0 + kBK, k_hi, xb);
     }
     bf16x8 fa[3][4];
 #pragma unroll
@@ -322,8 +320,8 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_split3(int M, int N, int K, 
     clear_total();
     down = 1.0f;
     for (int k0 = k_lo; k0 < k_hi; k0 += kBK) {
-      load_stage<KA, VEC, kBM, MASK>(A, lda, m0, M, k0, k_hi, xa, live);
-      load_stage<KB, VEC, BN>(B, ldb, n0, N, k0, k_hi, xb);
+      load_stage<KA, kBM, MASK>(A, lda, m0, M, k0, k_hi, xa, live);
+      load_stage<KB, BN>(B, ldb, n0, N, k0, k_hi, xb);
       store_wide<KA, kBM>(Aw, xa);
       store_wide<KB, BN>(Bw, xb);
       __syncthreads();
@@ -516,10 +514,10 @@ void gemm_split_km(int M, int N, int K, const float* A, int lda, const float* B,
   kps = (kps + kBK - 1) / kBK * kBK;
   const dim3 g((unsigned)(splits * tm * tn));
   if (live)
-    hipLaunchKernelGGL((gemm_split3<true, true, false, false, true>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C,
+    hipLaunchKernelGGL((gemm_split3<true, true, false, true>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C,
                        ldc, kps, c_split, tm, tn, splits, 0, live, GatherOut{}, Gate{});
   else
-    hipLaunchKernelGGL((gemm_split3<true, true, false, false>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
+    hipLaunchKernelGGL((gemm_split3<true, true, false>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
                        kps, c_split, tm, tn, splits, 0, nullptr, GatherOut{}, Gate{});
 }
 
@@ -531,17 +529,11 @@ void launch_kc(int M, int N, int K, const float* A, int lda, const float* B, int
                int splits, size_t c_split, const GatherOut& to, const Gate& gate, hipStream_t s) {
   const int bn = GATHER ? kBN / 2 : kBN;
   const int tm = (M + kBM - 1) / kBM, tn = (N + bn - 1) / bn;
-  const bool vec = lda % 4 == 0 && reinterpret_cast<uintptr_t>(A) % 16 == 0 &&
-                   (KB || (ldb % 4 == 0 && reinterpret_cast<uintptr_t>(B) % 16 == 0));
   int kps = (K + splits - 1) / splits;
   kps = (kps + kBK - 1) / kBK * kBK;
   const dim3 g((unsigned)((tm >= 32 ? (tm + 7) / 8 * 8 : tm) * tn * splits));
-  if (vec)
-    hipLaunchKernelGGL((gemm_split3<false, KB, true, GATHER>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
-                       kps, c_split, tm, tn, splits, accumulate, nullptr, to, gate);
-  else
-    hipLaunchKernelGGL((gemm_split3<false, KB, false, GATHER>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc,
-                       kps, c_split, tm, tn, splits, accumulate, nullptr, to, gate);
+  hipLaunchKernelGGL((gemm_split3<false, KB, GATHER>), g, dim3(kThreads), 0, s, M, N, K, A, lda, B, ldb, C, ldc, kps,
+                     c_split, tm, tn, splits, accumulate, nullptr, to, gate);
 }
 
 }  // namespace

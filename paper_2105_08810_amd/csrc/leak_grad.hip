@@ -26,6 +26,8 @@ struct Entries {
   int64_t cap;
 };
 
+constexpr int kEntries = 4;  // of a thread under way
+
 __device__ __forceinline__ int64_t clamped(int32_t e, int64_t cap) { return e < 0 ? 0 : (e > cap ? cap : e); }
 
 template <bool IN, bool OUT>
@@ -65,9 +67,19 @@ __global__ __launch_bounds__(kCols) void leak_walk(int T, int B, int N, int slab
       if (t1 - row >= 1) {
         const int64_t r = (int64_t)(t1 - row) * B + b;
         const int64_t e1 = clamped(in.row_ptr[r + 1], in.cap);
-        for (int64_t e = clamped(in.row_ptr[r], in.cap) + lane; e < e1; e += kRowLanes) {
-          const int j = in.col[e] - c0;
-          if ((unsigned)j < (unsigned)kCols) tile[row][j] = in.g ? x[e] * in.g[e] : x[e];
+        for (int64_t e = clamped(in.row_ptr[r], in.cap) + lane; e < e1; e += kEntries * kRowLanes) {
+          int j[kEntries];
+          float xe[kEntries], ge[kEntries];
+#pragma unroll
+          for (int q = 0; q < kEntries; ++q) {
+            const int64_t at = min(e + q * kRowLanes, e1 - 1);
+            j[q] = in.col[at] - c0;
+            xe[q] = x[at];
+            ge[q] = in.g ? in.g[at] : 1.0f;
+          }
+#pragma unroll
+          for (int q = 0; q < kEntries; ++q)
+            if (e + q * kRowLanes < e1 && (unsigned)j[q] < (unsigned)kCols) tile[row][j[q]] = xe[q] * ge[q];
         }
       }
       __syncthreads();
@@ -90,9 +102,13 @@ __global__ __launch_bounds__(kCols) void leak_walk(int T, int B, int N, int slab
       if (t1 - row >= 1) {
         const int64_t r = (int64_t)(t1 - row - 1) * B + b;
         const int64_t e1 = clamped(out.row_ptr[r + 1], out.cap);
-        for (int64_t e = clamped(out.row_ptr[r], out.cap) + lane; e < e1; e += kRowLanes) {
-          const int j = out.col[e] - c0;
-          if ((unsigned)j < (unsigned)kCols) y[e] = tile[row][j];
+        for (int64_t e = clamped(out.row_ptr[r], out.cap) + lane; e < e1; e += kEntries * kRowLanes) {
+          int j[kEntries];
+#pragma unroll
+          for (int q = 0; q < kEntries; ++q) j[q] = out.col[min(e + q * kRowLanes, e1 - 1)] - c0;
+#pragma unroll
+          for (int q = 0; q < kEntries; ++q)
+            if (e + q * kRowLanes < e1 && (unsigned)j[q] < (unsigned)kCols) y[e + q * kRowLanes] = tile[row][j[q]];
         }
       }
       __syncthreads();

@@ -725,8 +725,9 @@ void run(const float* x, int64_t ld_x, const float* W, int64_t ld_w, int R, int 
 template <class T>
 constexpr float kRaise = std::is_same<T, F16>::value ? 32768.0f : 1.0f;
 
-constexpr int kTile = gemm16::kTile;
-constexpr int kPart = 128;  // classes of a partial sum of exponentials: a wavefront's
+// Classes of a partial sum of exponentials: a wavefront's.
+template <int TILE>
+constexpr int kPart = gemm16::Shape<TILE>::kWaveM;
 
 // pos[r]: rows before r that take part, pos[R]: their number; ref: the largest weight. Blocks of 1024 threads: one takes up
 // to kOneBlock rows, a run of them a thread; beyond, the flags' prefix is formed by the scan and ref by a launch of its own.
@@ -795,21 +796,26 @@ __global__ __launch_bounds__(1024) void ce_ref(const float* __restrict__ weight,
 }
 
 // Rows to their packed places, row_of[place] = row: lines of Hp, zeros behind H and in the lines behind the rows that take
-// part up to a whole tile. The others' loss is 0.
+// part up to a whole tile. The others' loss is 0, and their dx where the product writes dx itself (dx NULL: it does not).
 template <class T>
 __global__ __launch_bounds__(kWaves * kWave) void ce_pack16(const T* __restrict__ x, int64_t ld, int R, int Rp, int H,
                                                             int Hp, const int32_t* __restrict__ targets,
                                                             const float* __restrict__ weight,
                                                             const int32_t* __restrict__ pos, T* __restrict__ X,
                                                             int32_t* __restrict__ target, float* __restrict__ w,
-                                                            int32_t* __restrict__ row_of, float* __restrict__ row_loss) {
+                                                            int32_t* __restrict__ row_of, float* __restrict__ row_loss,
+                                                            int tile, T* __restrict__ dx, int64_t ld_dx) {
   const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
   if (r >= Rp) return;
   const int n = pos[R], p0 = r < R ? pos[r] : n;
   const bool live = r < R && pos[r + 1] > p0;
   const int p = live ? p0 : n + (r - p0);
-  if (!live && r < R && row_loss && lane_id() == 0) row_loss[r] = 0.0f;
-  if (p >= (n + kTile - 1) / kTile * kTile) return;
+  if (!live && r < R) {
+    if (row_loss && lane_id() == 0) row_loss[r] = 0.0f;
+    if (dx)
+      for (int i = lane_id(); i < H; i += kWave) dx[(int64_t)r * ld_dx + i] = T{0};
+  }
+  if (p >= (n + tile - 1) / tile * tile) return;
   for (int i = lane_id() * 8; i < Hp; i += kWave * 8) {
     T v[8];
 #pragma unroll
@@ -856,43 +862,44 @@ __global__ __launch_bounds__(256) void ce_weights16(const T* __restrict__ W, int
 }
 
 // Logits of a tile of classes (m) and rows (n). GRAD false: every row's largest logit and sum of exponentials over the
-// 128 classes of a wavefront, to part[class / 128][row], and the target's logit. GRAD true: dz to G[row][class].
-template <class T, bool GRAD>
-__global__ __launch_bounds__(gemm16::kThreads, 2) void ce_logits16(
+// classes of a wavefront, to part[class / kPart][row], and the target's logit. GRAD true: dz to G[row][class].
+template <class T, bool GRAD, int TILE>
+__global__ __launch_bounds__(gemm16::Shape<TILE>::kThreads, 2) void ce_logits16(
     const T* __restrict__ W, int64_t ldw, const T* __restrict__ X, int Hp, int stages, int c0, int C, int R, int Rp,
     int tiles_m, int tiles_n, const int32_t* __restrict__ pos, const int32_t* __restrict__ target,
     float2* __restrict__ part, float* __restrict__ at_target, const float* __restrict__ lse, const float* __restrict__ w,
     const float* __restrict__ ref, T* __restrict__ G, int64_t ldg) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const gemm16::Tiles t = gemm16::tile_of(tiles_m, tiles_n, 1);
-  if (!t.ok || t.n * kTile >= pos[R]) return;
-  gemm16::Product<T, true, false> z;
+  if (!t.ok || t.n * TILE >= pos[R]) return;
+  using S = gemm16::Shape<TILE>;
+  gemm16::Product<T, true, false, TILE> z;
   const int l = lane_id(), g = l / 16;
-  const int m0 = t.m * kTile + z.m_of_wave();
+  const int m0 = t.m * TILE + z.m_of_wave();
   const int first = c0 + m0;  // class of the wavefront's first m
-  const int n0 = t.n * kTile + z.n_of_wave() + l % 16;
+  const int n0 = t.n * TILE + z.n_of_wave() + l % 16;
   // what the rows need at the end is asked for now
-  int32_t tgt[4];
-  float top[4], k[4];
+  int32_t tgt[S::kB];
+  float top[S::kB], k[S::kB];
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
+  for (int b = 0; b < S::kB; ++b) {
     tgt[b] = target[n0 + 16 * b];
     if (GRAD) {
       top[b] = tgt[b] >= 0 ? lse[n0 + 16 * b] : 0.0f;
       k[b] = tgt[b] >= 0 ? w[n0 + 16 * b] / *ref * kRaise<T> : 0.0f;
     }
   }
-  z.run(W, ldw, t.m * kTile, X, Hp, t.n * kTile, 0, stages, smem);
+  z.run(W, ldw, t.m * TILE, X, Hp, t.n * TILE, 0, stages, smem);
   constexpr float kLog2e = 1.44269504088896340736f;
-  const bool ragged = first + kPart > C;
+  const bool ragged = first + kPart<TILE> > C;
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
+  for (int b = 0; b < S::kB; ++b) {
     const int n = n0 + 16 * b;
     const int at = tgt[b] - first;  // the target among this wavefront's classes
-    const bool here = tgt[b] >= 0 && (unsigned)at < (unsigned)kPart;
+    const bool here = tgt[b] >= 0 && (unsigned)at < (unsigned)kPart<TILE>;
     if (ragged) {
 #pragma unroll
-      for (int a = 0; a < 8; ++a)
+      for (int a = 0; a < S::kA; ++a)
 #pragma unroll
         for (int v = 0; v < 4; ++v)
           if (first + 16 * a + 4 * g + v >= C) z.acc[a][b][v] = -INFINITY;
@@ -900,14 +907,14 @@ __global__ __launch_bounds__(gemm16::kThreads, 2) void ce_logits16(
     if constexpr (!GRAD) {
       if (here && (at / 4) % 4 == g) {
 #pragma unroll
-        for (int a = 0; a < 8; ++a)
+        for (int a = 0; a < S::kA; ++a)
 #pragma unroll
           for (int v = 0; v < 4; ++v)
             if (at == 16 * a + 4 * g + v) at_target[n] = z.acc[a][b][v];
       }
       float m = -INFINITY;
 #pragma unroll
-      for (int a = 0; a < 8; ++a)
+      for (int a = 0; a < S::kA; ++a)
 #pragma unroll
         for (int v = 0; v < 4; ++v) m = fmaxf(m, z.acc[a][b][v]);
       m = fmaxf(m, __shfl_xor(m, 16, kWave));
@@ -915,16 +922,16 @@ __global__ __launch_bounds__(gemm16::kThreads, 2) void ce_logits16(
       const float from = m > -INFINITY ? m : 0.0f;
       float s = 0.0f;
 #pragma unroll
-      for (int a = 0; a < 8; ++a)
+      for (int a = 0; a < S::kA; ++a)
 #pragma unroll
         for (int v = 0; v < 4; ++v) s += __builtin_amdgcn_exp2f((z.acc[a][b][v] - from) * kLog2e);
       s += __shfl_xor(s, 16, kWave);
       s += __shfl_xor(s, 32, kWave);
-      if (g == 0) part[(size_t)(first / kPart) * Rp + n] = make_float2(m, s);
+      if (g == 0) part[(size_t)(first / kPart<TILE>) * Rp + n] = make_float2(m, s);
     } else {
       const bool live = tgt[b] >= 0;
 #pragma unroll
-      for (int a = 0; a < 8; ++a) {
+      for (int a = 0; a < S::kA; ++a) {
         T d[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
@@ -980,25 +987,43 @@ __global__ __launch_bounds__(1024) void ce_join16(const float2* __restrict__ par
   }
 }
 
-// A K slice's dx of a piece: dX[slice][row][h] (+)= sum over its classes of G W.
-template <class T>
-__global__ __launch_bounds__(gemm16::kThreads, 2) void ce_dx16(const T* __restrict__ W, int64_t ldw, const T* __restrict__ G,
-                                                               int64_t ldg, int stages, int per, int R, int Rp, int Hp,
-                                                               int tiles_m, int tiles_n, int slices,
-                                                               const int32_t* __restrict__ pos, int accumulate,
-                                                               float* __restrict__ dX) {
+// A K slice's dx of a piece: dX[slice][row][h] (+)= sum over its classes of G W; with dx the whole of it, to the rows' places.
+template <class T, int TILE>
+__global__ __launch_bounds__(gemm16::Shape<TILE>::kThreads, 2) void ce_dx16(
+    const T* __restrict__ W, int64_t ldw, const T* __restrict__ G, int64_t ldg, int stages, int per, int R, int Rp, int H,
+    int Hp, int tiles_m, int tiles_n, int slices, const int32_t* __restrict__ pos, int accumulate, float* __restrict__ dX,
+    const int32_t* __restrict__ row_of, const float* __restrict__ ref, T* __restrict__ dx, int64_t ld) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const gemm16::Tiles t = gemm16::tile_of(tiles_m, tiles_n, slices);
-  if (!t.ok || t.n * kTile >= pos[R]) return;
-  gemm16::Product<T, false, false> d;
+  if (!t.ok || t.n * TILE >= pos[R]) return;
+  using S = gemm16::Shape<TILE>;
+  gemm16::Product<T, false, false, TILE> d;
   const int from = t.slice * per;
-  d.run(W, ldw, t.m * kTile, G, ldg, t.n * kTile, (int64_t)from * gemm16::kK, max(0, min(per, stages - from)), smem);
+  d.run(W, ldw, t.m * TILE, G, ldg, t.n * TILE, (int64_t)from * gemm16::kK, max(0, min(per, stages - from)), smem);
   const int l = lane_id();
-  float* out = dX + ((size_t)t.slice * Rp + t.n * kTile + d.n_of_wave() + l % 16) * Hp + t.m * kTile + d.m_of_wave() + l / 16 * 4;
+  const int n0 = t.n * TILE + d.n_of_wave() + l % 16, m0 = t.m * TILE + d.m_of_wave() + l / 16 * 4;
+  if (dx) {
+    const float k = *ref / kRaise<T>;
 #pragma unroll
-  for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < S::kB; ++b) {
+      const int n = n0 + 16 * b;
+      if (n >= pos[R]) continue;
+      T* row = dx + (int64_t)row_of[n] * ld;
 #pragma unroll
-    for (int a = 0; a < 8; ++a) {
+      for (int a = 0; a < S::kA; ++a) {
+        float v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = d.acc[a][b][u] * k;
+        store_in<T, 4>(row, min(m0 + 16 * a, H), H, v);
+      }
+    }
+    return;
+  }
+  float* out = dX + ((size_t)t.slice * Rp + n0) * Hp + m0;
+#pragma unroll
+  for (int b = 0; b < S::kB; ++b)
+#pragma unroll
+    for (int a = 0; a < S::kA; ++a) {
       gemm16::f32x4* o = reinterpret_cast<gemm16::f32x4*>(out + (size_t)16 * b * Hp + 16 * a);
       *o = accumulate ? *o + d.acc[a][b] : d.acc[a][b];
     }
@@ -1042,8 +1067,8 @@ __global__ __launch_bounds__(kWaves * kWave) void ce_dx_out16(const float* __res
 }
 
 // dW of a piece's n columns: the tile itself with one slice, else its share to part[slice][h][width].
-template <class T>
-__global__ __launch_bounds__(gemm16::kThreads, 2) void ce_dw16(const T* __restrict__ G, int64_t ldg, const T* __restrict__ X,
+template <class T, int TILE>
+__global__ __launch_bounds__(gemm16::Shape<TILE>::kThreads, 2) void ce_dw16(const T* __restrict__ G, int64_t ldg, const T* __restrict__ X,
                                                                int Hp, int R, int H, int n, int width, int tiles_m,
                                                                int tiles_n, int slices, const int32_t* __restrict__ pos,
                                                                const float* __restrict__ ref, T* __restrict__ dW,
@@ -1053,17 +1078,18 @@ __global__ __launch_bounds__(gemm16::kThreads, 2) void ce_dw16(const T* __restri
   if (!t.ok) return;
   const int stages = (pos[R] + gemm16::kK - 1) / gemm16::kK;
   const int per = (stages + slices - 1) / slices, from = t.slice * per;
-  gemm16::Product<T, true, true> d;
-  d.run(G, ldg, t.m * kTile, X, Hp, t.n * kTile, (int64_t)from * gemm16::kK, max(0, min(per, stages - from)), smem);
+  using S = gemm16::Shape<TILE>;
+  gemm16::Product<T, true, true, TILE> d;
+  d.run(G, ldg, t.m * TILE, X, Hp, t.n * TILE, (int64_t)from * gemm16::kK, max(0, min(per, stages - from)), smem);
   const int l = lane_id();
-  const int m0 = t.m * kTile + d.m_of_wave() + l / 16 * 4, n0 = t.n * kTile + d.n_of_wave() + l % 16;
+  const int m0 = t.m * TILE + d.m_of_wave() + l / 16 * 4, n0 = t.n * TILE + d.n_of_wave() + l % 16;
   const float k = *ref / kRaise<T>;
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
+  for (int b = 0; b < S::kB; ++b) {
     const int h = n0 + 16 * b;
     if (h >= H) continue;
 #pragma unroll
-    for (int a = 0; a < 8; ++a) {
+    for (int a = 0; a < S::kA; ++a) {
       const int c = m0 + 16 * a;
       if (slices > 1) {
         *reinterpret_cast<gemm16::f32x4*>(part + ((size_t)t.slice * H + h) * width + c) = d.acc[a][b];
@@ -1092,15 +1118,16 @@ __global__ void ce_dw_out16(const float* __restrict__ part, int slices, int H, i
 
 constexpr int64_t kPiece16 = (int64_t)1 << 28;  // dz values of a piece
 
-// K slices of a product of `tiles` tiles and `stages` stages: a block a compute unit and round, a stage about a
-// microsecond, a slice's share of a tile (written and read) a quarter of one.
-int slices_of(int64_t tiles, int stages) {
-  const int64_t cus = cu_count();
+// K slices of a product of `tiles` tiles and `stages` stages: blocks go in rounds over the compute units (two at a time of
+// the small tile, at half the speed each), a stage takes a microsecond, a slice's share of a tile (written and read) a
+// quarter of one.
+int slices_of(int64_t tiles, int stages, int tile) {
+  const int64_t at_once = cu_count() * (tile == 128 ? 2 : 1);
   int best = 1;
   double least = 0.0;
   for (int s = 1; s <= 64 && (s == 1 || s * 4 <= stages); ++s) {
-    const double rounds = (double)((tiles * s + cus - 1) / cus);
-    const double t = rounds * ((stages + s - 1) / s + 3) + (s > 1 ? 0.25 * rounds + 0.1 * s * tiles / cus : 0.0);
+    const double rounds = (double)((tiles * s + at_once - 1) / at_once);
+    const double t = rounds * ((stages + s - 1) / s + 3) + (s > 1 ? 0.25 * rounds + 0.1 * s * tiles / at_once : 0.0);
     if (s == 1 || t < least) {
       best = s;
       least = t;
@@ -1112,21 +1139,31 @@ int slices_of(int64_t tiles, int stages) {
 int padded(int n, int to) { return (n + to - 1) / to * to; }
 
 struct Plan16 {
-  int Rp, Hp, width, pieces, dx_slices, dw_slices;
+  int tile, Rp, Hp, width, pieces, dx_slices, dw_slices;
+  bool direct;   // dx from the product itself
   size_t parts;  // partial sums of exponentials a row
 };
 
+// The large tile where its blocks fill the card twice over and a product has stages enough to cover its end. Small against
+// large tile, bfloat16, us a call (rows x H x classes): 360 x 128 x 512 47, 72; 3000 x 1000 x 8000 (384 large tiles) 285, 295;
+// 2048 x 1024 x 16384 (512) 334, 303; 8192 x 1024 x 32003 2408, 2059; 4926 x 128 x 71434 1024, 1063; x 200 1417, 1254.
+int tile_of(int R, int H, int C) {
+  return H > 128 && (int64_t)((R + 255) / 256) * ((C + 255) / 256) >= 2 * cu_count() ? 256 : 128;
+}
+
 Plan16 plan16_of(int R, int H, int C) {
   Plan16 p;
-  p.Rp = padded(R, kTile);
-  p.Hp = padded(H, kTile);
-  const int most = (int)std::min<int64_t>(padded(C, kTile), std::max<int64_t>(kTile, kPiece16 / p.Rp / kTile * kTile));
+  p.tile = tile_of(R, H, C);
+  p.Rp = padded(R, p.tile);
+  p.Hp = padded(H, p.tile);
+  const int most = (int)std::min<int64_t>(padded(C, p.tile), std::max<int64_t>(p.tile, kPiece16 / p.Rp / p.tile * p.tile));
   p.pieces = (C + most - 1) / most;
-  p.width = padded((C + p.pieces - 1) / p.pieces, kTile);
+  p.width = padded((C + p.pieces - 1) / p.pieces, p.tile);
   p.pieces = (C + p.width - 1) / p.width;
-  p.dx_slices = slices_of((int64_t)(p.Hp / kTile) * (p.Rp / kTile), p.width / gemm16::kK);
-  p.dw_slices = slices_of((int64_t)(p.width / kTile) * (p.Hp / kTile), p.Rp / gemm16::kK);
-  p.parts = (size_t)p.pieces * p.width / kPart;
+  p.dx_slices = slices_of((int64_t)(p.Hp / p.tile) * (p.Rp / p.tile), p.width / gemm16::kK, p.tile);
+  p.dw_slices = slices_of((int64_t)(p.width / p.tile) * (p.Hp / p.tile), p.Rp / gemm16::kK, p.tile);
+  p.direct = p.pieces == 1 && p.dx_slices == 1;
+  p.parts = (size_t)p.pieces * p.width / (p.tile / 2);
   return p;
 }
 
@@ -1160,22 +1197,23 @@ Workspace16 carve16(void* ws, int R, int H, int C, bool grad, const Plan16& p) {
   g.X = c.take<uint16_t>((size_t)p.Rp * p.Hp);
   g.W = c.take<uint16_t>((size_t)p.Hp * p.width);
   g.G = c.take<uint16_t>(grad ? (size_t)p.Rp * p.width : 0);
-  g.dX = c.take<float>(grad ? (size_t)p.dx_slices * p.Rp * p.Hp : 0);
+  g.dX = c.take<float>(grad && !p.direct ? (size_t)p.dx_slices * p.Rp * p.Hp : 0);
   g.dW = c.take<float>(grad && p.dw_slices > 1 ? (size_t)p.dw_slices * H * p.width : 0);
   g.bytes = c.off;
   return g;
 }
 
-template <class T>
+template <class T, int TILE>
 void run16(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int C, const int32_t* targets,
            const float* weight, float* loss, float* row_loss, T* dx, int64_t ld_dx, T* dW, int64_t ld_dw,
            const Plan16& p, const Workspace16& g, hipStream_t s) {
   T *X = reinterpret_cast<T*>(g.X), *Wp = reinterpret_cast<T*>(g.W), *G = reinterpret_cast<T*>(g.G);
-  const dim3 waves(kWaves * kWave), block(gemm16::kThreads);
+  using S = gemm16::Shape<TILE>;
+  const dim3 waves(kWaves * kWave), block(S::kThreads);
   const auto rows_of = [](int n) { return dim3((unsigned)((n + kWaves - 1) / kWaves)); };
-  for (const void* f : {(const void*)ce_logits16<T, false>, (const void*)ce_logits16<T, true>, (const void*)ce_dx16<T>,
-                        (const void*)ce_dw16<T>})
-    ensure_dynamic_lds(f, gemm16::kLds);
+  for (const void* f : {(const void*)ce_logits16<T, false, TILE>, (const void*)ce_logits16<T, true, TILE>,
+                        (const void*)ce_dx16<T, TILE>, (const void*)ce_dw16<T, TILE>})
+    ensure_dynamic_lds(f, S::kLds);
   if (R <= kOneBlock) {
     hipLaunchKernelGGL(ce_places, dim3(1), dim3(1024), 0, s, targets, weight, R, C, g.pos, g.ref);
   } else {
@@ -1184,9 +1222,9 @@ void run16(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int
     hipLaunchKernelGGL(ce_ref, dim3(1), dim3(1024), 0, s, weight, g.pos, R, g.ref);
   }
   hipLaunchKernelGGL(ce_pack16<T>, rows_of(p.Rp), waves, 0, s, x, ld_x, R, p.Rp, H, p.Hp, targets, weight, g.pos, X,
-                     g.target, g.w, g.row_of, row_loss);
+                     g.target, g.w, g.row_of, row_loss, TILE, p.direct ? dx : nullptr, ld_dx);
   // W in place where its rows are whole tiles at 16-byte addresses
-  const bool whole = H % kTile == 0 && C % kTile == 0 && ld_w % 8 == 0 && ld_w < (1 << 22) &&
+  const bool whole = H % TILE == 0 && C % TILE == 0 && ld_w % 8 == 0 && ld_w < (1 << 22) &&
                      reinterpret_cast<uintptr_t>(W) % 16 == 0;
   const T* w = nullptr;
   int64_t ldw = 0;
@@ -1201,32 +1239,32 @@ void run16(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int
       ldw = p.width;
     }
   };
-  const int tiles_n = p.Rp / kTile, tiles_h = p.Hp / kTile, stages_h = padded(H, gemm16::kK) / gemm16::kK;
+  const int tiles_n = p.Rp / TILE, tiles_h = p.Hp / TILE, stages_h = padded(H, gemm16::kK) / gemm16::kK;
   for (int c0 = 0; c0 < C; c0 += p.width) {
-    const int n = std::min(p.width, C - c0), tiles_m = (n + kTile - 1) / kTile;
+    const int n = std::min(p.width, C - c0), tiles_m = (n + TILE - 1) / TILE;
     weights(c0, n);
-    hipLaunchKernelGGL((ce_logits16<T, false>), dim3(gemm16::grid_of(tiles_m, tiles_n, 1)), block, gemm16::kLds, s, w, ldw,
+    hipLaunchKernelGGL((ce_logits16<T, false, TILE>), dim3(gemm16::grid_of(tiles_m, tiles_n, 1)), block, S::kLds, s, w, ldw,
                        X, p.Hp, stages_h, c0, C, R, p.Rp, tiles_m, tiles_n, g.pos, g.target, g.part, g.at_target, nullptr,
                        nullptr, nullptr, (T*)nullptr, 0);
   }
-  hipLaunchKernelGGL(ce_join16, dim3((unsigned)(p.Rp / 32)), dim3(1024), 0, s, g.part, padded(C, kTile) / kPart, R, p.Rp,
+  hipLaunchKernelGGL(ce_join16, dim3((unsigned)(p.Rp / 32)), dim3(1024), 0, s, g.part, padded(C, TILE) / kPart<TILE>, R, p.Rp,
                      g.pos, g.row_of, g.at_target, g.w, g.lse, row_loss, g.parts);
-  if (!dx) hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, p.Rp / 32, loss);
+  if (!dx || p.direct) hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, p.Rp / 32, loss);
   if (!dx && !dW) return;
   for (int c0 = 0; c0 < C; c0 += p.width) {
-    const int n = std::min(p.width, C - c0), tiles_m = (n + kTile - 1) / kTile;
+    const int n = std::min(p.width, C - c0), tiles_m = (n + TILE - 1) / TILE;
     if (p.pieces > 1) weights(c0, n);
-    hipLaunchKernelGGL((ce_logits16<T, true>), dim3(gemm16::grid_of(tiles_m, tiles_n, 1)), block, gemm16::kLds, s, w, ldw,
+    hipLaunchKernelGGL((ce_logits16<T, true, TILE>), dim3(gemm16::grid_of(tiles_m, tiles_n, 1)), block, S::kLds, s, w, ldw,
                        X, p.Hp, stages_h, c0, C, R, p.Rp, tiles_m, tiles_n, g.pos, g.target, nullptr, nullptr, g.lse, g.w,
                        g.ref, G, (int64_t)p.width);
     if (dx) {
-      const int stages = tiles_m * (kTile / gemm16::kK), per = (stages + p.dx_slices - 1) / p.dx_slices;
-      hipLaunchKernelGGL(ce_dx16<T>, dim3(gemm16::grid_of(tiles_h, tiles_n, p.dx_slices)), block, gemm16::kLds, s, w, ldw,
-                         G, (int64_t)p.width, stages, per, R, p.Rp, p.Hp, tiles_h, tiles_n, p.dx_slices, g.pos, c0 > 0,
-                         g.dX);
+      const int stages = tiles_m * (TILE / gemm16::kK), per = (stages + p.dx_slices - 1) / p.dx_slices;
+      hipLaunchKernelGGL((ce_dx16<T, TILE>), dim3(gemm16::grid_of(tiles_h, tiles_n, p.dx_slices)), block, S::kLds, s, w, ldw,
+                         G, (int64_t)p.width, stages, per, R, p.Rp, H, p.Hp, tiles_h, tiles_n, p.dx_slices, g.pos, c0 > 0,
+                         g.dX, g.row_of, g.ref, p.direct ? dx : nullptr, ld_dx);
     }
     if (dW) {
-      hipLaunchKernelGGL(ce_dw16<T>, dim3(gemm16::grid_of(tiles_m, tiles_h, p.dw_slices)), block, gemm16::kLds, s, G,
+      hipLaunchKernelGGL((ce_dw16<T, TILE>), dim3(gemm16::grid_of(tiles_m, tiles_h, p.dw_slices)), block, S::kLds, s, G,
                          (int64_t)p.width, X, p.Hp, R, H, n, p.width, tiles_m, tiles_h, p.dw_slices, g.pos, g.ref, dW + c0,
                          ld_dw, g.dW);
       if (p.dw_slices > 1)
@@ -1234,9 +1272,19 @@ void run16(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int
                            g.dW, p.dw_slices, H, n, p.width, g.ref, dW + c0, ld_dw);
     }
   }
-  if (dx)
+  if (dx && !p.direct)
     hipLaunchKernelGGL(ce_dx_out16<T>, dim3((unsigned)R, (unsigned)((H + 255) / 256)), waves, 0, s, g.dX, p.dx_slices, R,
                        p.Rp, H, p.Hp, g.pos, g.ref, dx, ld_dx, g.parts, p.Rp / 32, loss);
+}
+
+template <class T>
+void run16(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int C, const int32_t* targets,
+           const float* weight, float* loss, float* row_loss, T* dx, int64_t ld_dx, T* dW, int64_t ld_dw,
+           const Plan16& p, const Workspace16& g, hipStream_t s) {
+  if (p.tile == 256)
+    run16<T, 256>(x, ld_x, W, ld_w, R, H, C, targets, weight, loss, row_loss, dx, ld_dx, dW, ld_dw, p, g, s);
+  else
+    run16<T, 128>(x, ld_x, W, ld_w, R, H, C, targets, weight, loss, row_loss, dx, ld_dx, dW, ld_dw, p, g, s);
 }
 
 snn_status check_sizes(int dtype, int64_t R, int H, int C) {
@@ -1285,8 +1333,8 @@ extern "C" snn_status snn_linear_ce(const void* x, const void* W, int dtype, int
   const Plan16 p = plan16_of((int)R, H, C);
   const Workspace16 g = carve16(workspace, (int)R, H, C, dx || dW, p);
   if (workspace_bytes < g.bytes) return SNN_ERR_INVALID_ARG;
-  if (dtype == SNN_BF16) SNN_CE(run16, Bf16);
-  else SNN_CE(run16, F16);
+  if (dtype == SNN_BF16) SNN_CE(run16<Bf16>, Bf16);
+  else SNN_CE(run16<F16>, F16);
 #undef SNN_CE
   return launch_status();
 }

@@ -8,8 +8,9 @@
 // entries of a CSR over the rows (t, b).
 //
 // Bound: memory, each dense side once. A block owns one sample's 256 columns, a thread a column, and walks time downwards
-// in tiles of 32 steps: a dense x is loaded a tile ahead into registers, entries are spread into an LDS tile [step][column]
-// (8 threads a row); y goes to memory, or to the same LDS tile, from which the rows' entries are picked.
+// in tiles of 32 steps; entries are spread into, or picked from, an LDS tile [step][column] by 8 threads a row, four each
+// under way. Loads and stores retire in order, so whatever a tile reads (a dense x, the rows' pointers, their first entries)
+// is asked for before the tile before it is stored, pointers a tile earlier still.
 #include "common.h"
 
 namespace snn {
@@ -30,11 +31,26 @@ constexpr int kEntries = 4;  // of a thread under way
 
 __device__ __forceinline__ int64_t clamped(int32_t e, int64_t cap) { return e < 0 ? 0 : (e > cap ? cap : e); }
 
+// A thread's share of a row's entries: every kRowLanes-th from `lane` on.
+struct Range {
+  int64_t e, end;
+};
+
+__device__ __forceinline__ Range range_of(const Entries& c, int t, int row_of_step, int B, int lane) {
+  Range r{0, 0};
+  if (t >= 0) {
+    const int64_t at = (int64_t)t * B + row_of_step;
+    r.end = clamped(c.row_ptr[at + 1], c.cap);
+    r.e = clamped(c.row_ptr[at], c.cap) + lane;
+  }
+  return r;
+}
+
 template <bool IN, bool OUT>
 __global__ __launch_bounds__(kCols) void leak_walk(int T, int B, int N, int slabs, float alpha,
                                                    const float* __restrict__ x, Entries in, float* __restrict__ y,
                                                    Entries out) {
-  __shared__ float tile[IN || OUT ? kSteps : 1][kCols];
+  __shared__ __attribute__((aligned(16))) float tile[IN || OUT ? kSteps : 1][kCols];
   const int b = blockIdx.x / slabs;
   const int c0 = (int)(blockIdx.x % slabs) * kCols;
   const int c = threadIdx.x;
@@ -42,13 +58,66 @@ __global__ __launch_bounds__(kCols) void leak_walk(int T, int B, int N, int slab
   const size_t step = (size_t)B * N;
   const size_t k = (size_t)b * N + (valid ? c0 + c : c0);
   const int row = threadIdx.x / kRowLanes, lane = threadIdx.x % kRowLanes;
-  // step u of tile t1: x[t1 - u] enters y[t1 - u - 1], for t1 - u >= 1
-  const auto load = [&](float (&v)[kSteps], int t1) {
+  // step u of a tile that begins at t1: x[t1 - u] enters y[t1 - u - 1], for t1 - u >= 1
+  float v[kSteps], ahead[IN ? 1 : kSteps];
+  const auto load = [&](int t1) {
+    if constexpr (!IN) {
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) v[u] = x[(size_t)max(t1 - u, 0) * step + k];
+      for (int u = 0; u < kSteps; ++u) ahead[u] = x[(size_t)max(t1 - u, 0) * step + k];
+    }
   };
-  float v[kSteps];
-  if (!IN && T > 1) load(v, T - 1);
+  struct Some {
+    int j[kEntries];
+    float v[kEntries];
+  };
+  // loads of places past a row's entries read its last one (or the first of all) and are left out: no branch between them
+  const auto some_in = [&](const Range& r, int64_t e) {
+    Some s;
+    if (in.cap > 0) {
+      float ge[kEntries];
+#pragma unroll
+      for (int q = 0; q < kEntries; ++q) {
+        const int64_t at = max(min(e + q * kRowLanes, r.end - 1), (int64_t)0);
+        s.j[q] = in.col[at];
+        s.v[q] = x[at];
+        ge[q] = 1.0f;
+        if (in.g) ge[q] = in.g[at];
+      }
+#pragma unroll
+      for (int q = 0; q < kEntries; ++q) {
+        s.j[q] = e + q * kRowLanes < r.end ? s.j[q] - c0 : -1;
+        s.v[q] *= ge[q];
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < kEntries; ++q) s.j[q] = -1;
+    }
+    return s;
+  };
+  const auto some_out = [&](const Range& r, int64_t e) {
+    Some s;
+#pragma unroll
+    for (int q = 0; q < kEntries; ++q) s.j[q] = -1;
+    if (out.cap > 0) {
+      int j[kEntries];
+#pragma unroll
+      for (int q = 0; q < kEntries; ++q) j[q] = out.col[max(min(e + q * kRowLanes, r.end - 1), (int64_t)0)];
+#pragma unroll
+      for (int q = 0; q < kEntries; ++q)
+        if (e + q * kRowLanes < r.end) s.j[q] = j[q] - c0;
+    }
+    return s;
+  };
+  const auto spread = [&](const Some& s) {
+#pragma unroll
+    for (int q = 0; q < kEntries; ++q)
+      if ((unsigned)s.j[q] < (unsigned)kCols) tile[row][s.j[q]] = s.v[q];
+  };
+  const auto pick = [&](const Some& s, int64_t e) {
+#pragma unroll
+    for (int q = 0; q < kEntries; ++q)
+      if ((unsigned)s.j[q] < (unsigned)kCols) y[e + q * kRowLanes] = tile[row][s.j[q]];
+  };
   // y[T-1] = 0
   if (OUT) {
     const int64_t r = (int64_t)(T - 1) * B + b;
@@ -58,34 +127,42 @@ __global__ __launch_bounds__(kCols) void leak_walk(int T, int B, int N, int slab
   } else if (valid) {
     y[(size_t)(T - 1) * step + k] = 0.0f;
   }
+  Range ri{0, 0}, ri_next{0, 0}, ro{0, 0}, ro_next{0, 0};
+  Some si, so;
+  if (T > 1) {
+    load(T - 1);
+    if (IN) {
+      ri = range_of(in, T - 1 - row >= 1 ? T - 1 - row : -1, b, B, lane);
+      ri_next = range_of(in, T - 1 - kSteps - row >= 1 ? T - 1 - kSteps - row : -1, b, B, lane);
+      si = some_in(ri, ri.e);
+    }
+    if (OUT) {
+      ro = range_of(out, T - 2 - row, b, B, lane);
+      ro_next = range_of(out, T - 2 - kSteps - row, b, B, lane);
+      so = some_out(ro, ro.e);
+    }
+  }
   float d = 0.0f;
   for (int t1 = T - 1; t1 > 0; t1 -= kSteps) {
-    if (IN) {
+    const int t2 = t1 - kSteps, t3 = t2 - kSteps;  // where the next tiles begin
+    if constexpr (IN) {
+      float4* clear = reinterpret_cast<float4*>(&tile[0][0]);
 #pragma unroll
-      for (int u = 0; u < kSteps; ++u) tile[u][c] = 0.0f;
+      for (int u = 0; u < kSteps / 4; ++u) clear[u * kCols + c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       __syncthreads();
-      if (t1 - row >= 1) {
-        const int64_t r = (int64_t)(t1 - row) * B + b;
-        const int64_t e1 = clamped(in.row_ptr[r + 1], in.cap);
-        for (int64_t e = clamped(in.row_ptr[r], in.cap) + lane; e < e1; e += kEntries * kRowLanes) {
-          int j[kEntries];
-          float xe[kEntries], ge[kEntries];
-#pragma unroll
-          for (int q = 0; q < kEntries; ++q) {
-            const int64_t at = min(e + q * kRowLanes, e1 - 1);
-            j[q] = in.col[at] - c0;
-            xe[q] = x[at];
-            ge[q] = in.g ? in.g[at] : 1.0f;
-          }
-#pragma unroll
-          for (int q = 0; q < kEntries; ++q)
-            if (e + q * kRowLanes < e1 && (unsigned)j[q] < (unsigned)kCols) tile[row][j[q]] = xe[q] * ge[q];
-        }
-      }
+      spread(si);
+      for (int64_t e = ri.e + kEntries * kRowLanes; e < ri.end; e += kEntries * kRowLanes) spread(some_in(ri, e));
       __syncthreads();
 #pragma unroll
       for (int u = 0; u < kSteps; ++u) v[u] = tile[u][c];
       if (OUT) __syncthreads();
+      ri = ri_next;
+      ri_next = range_of(in, t3 - row >= 1 ? t3 - row : -1, b, B, lane);
+      si = some_in(ri, ri.e);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kSteps; ++u) v[u] = ahead[u];
+      if (t2 > 0) load(t2);
     }
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {
@@ -93,24 +170,18 @@ __global__ __launch_bounds__(kCols) void leak_walk(int T, int B, int N, int slab
       if (t >= 0) {
         d = fmaf(alpha, d, v[u]);
         if (OUT) tile[u][c] = d;
-        else if (valid) y[(size_t)t * step + k] = d;
+        else if (valid) __builtin_nontemporal_store(d, y + (size_t)t * step + k);
       }
     }
-    if (!IN && t1 - kSteps > 0) load(v, t1 - kSteps);
-    if (OUT) {
+    if constexpr (OUT) {
       __syncthreads();
-      if (t1 - row >= 1) {
-        const int64_t r = (int64_t)(t1 - row - 1) * B + b;
-        const int64_t e1 = clamped(out.row_ptr[r + 1], out.cap);
-        for (int64_t e = clamped(out.row_ptr[r], out.cap) + lane; e < e1; e += kEntries * kRowLanes) {
-          int j[kEntries];
-#pragma unroll
-          for (int q = 0; q < kEntries; ++q) j[q] = out.col[min(e + q * kRowLanes, e1 - 1)] - c0;
-#pragma unroll
-          for (int q = 0; q < kEntries; ++q)
-            if (e + q * kRowLanes < e1 && (unsigned)j[q] < (unsigned)kCols) y[e + q * kRowLanes] = tile[row][j[q]];
-        }
-      }
+      const Range r = ro;
+      const Some s = so;
+      ro = ro_next;
+      ro_next = range_of(out, t3 - 1 - row, b, B, lane);
+      so = some_out(ro, ro.e);
+      pick(s, r.e);
+      for (int64_t e = r.e + kEntries * kRowLanes; e < r.end; e += kEntries * kRowLanes) pick(some_out(r, e), e);
       __syncthreads();
     } else if (IN) {
       __syncthreads();  // the tile is cleared next

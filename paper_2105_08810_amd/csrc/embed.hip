@@ -70,14 +70,14 @@ __global__ __launch_bounds__(kThreads) void embed_lookup(const T* __restrict__ E
   for (int i = l * kE<T>; i < N; i += kAhead * lanes * kE<T>) {
     Raw<T, kE<T>> raw[kAhead];
 #pragma unroll
-    for (int q = 0; q < kAhead; ++q) raw[q] = raw_in<T, kE<T>>(e, min(i + q * lanes * kE<T>, N), N);
+    for (int q = 0; q < kAhead; ++q) raw[q] = span_load<T, kE<T>>(e, i + q * lanes * kE<T>, N);
 #pragma unroll
     for (int q = 0; q < kAhead; ++q) {
       float x[kE<T>];
       raw[q].to(x);
 #pragma unroll
       for (int u = 0; u < kE<T>; ++u) x[u] = ok ? scaled(x[u], scale) : 0.0f;
-      store_past_in<T, kE<T>>(o, min(i + q * lanes * kE<T>, N), N, x);
+      span_store<T, kE<T>, true>(o, i + q * lanes * kE<T>, N, x);
     }
   }
 }
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kThreads) void embed_sum(const uint32_t* __restrict
     }
     f.k[kAhead] = p + kAhead < hi ? keys[p + kAhead] : after;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) f.raw[u] = raw_in<T, kE<T>>(dout + r[u] * ld, min(i, N), N);
+    for (int u = 0; u < kAhead; ++u) f.raw[u] = span_load<T, kE<T>>(dout + r[u] * ld, i, N);
   };
   const auto add = [&](const Batch& f, int p) {
 #pragma unroll
@@ -266,14 +266,14 @@ __global__ __launch_bounds__(kThreads) void embed_sum(const uint32_t* __restrict
             T* row = dE + (int64_t)k * ld_e;
             if (i < N) {
               float y[kE<T>], old[kE<T>];
-              if (accumulate) load_in<T, kE<T>>(row, i, N, old);
+              if (accumulate) span_load<T, kE<T>>(row, i, N).to(old);
 #pragma unroll
               for (int q = 0; q < kE<T>; ++q) y[q] = accumulate ? fmaf(acc[q], scale, old[q]) : acc[q] * scale;
-              store_past_in<T, kE<T>>(row, i, N, y);
+              span_store<T, kE<T>, true>(row, i, N, y);
             }
           } else {
             float* part = (began ? tail : head) + (size_t)c * N;
-            if (i < N) store_in<float, kE<T>>(part, i, N, acc);
+            if (i < N) span_store<float, kE<T>, false>(part, i, N, acc);
           }
 #pragma unroll
           for (int q = 0; q < kE<T>; ++q) acc[q] = 0.0f;
@@ -333,11 +333,11 @@ __global__ __launch_bounds__(kThreads) void embed_rest(const uint32_t* __restric
   float y[kE<T>];
 #pragma unroll
   for (int u = 0; u < kE<T>; ++u) y[u] = 0.0f;
-  if (w == 0) load_in<float, kE<T>>(tail + (size_t)c0 * N, min(i, N), N, y);
+  if (w == 0) span_load<float, kE<T>>(tail + (size_t)c0 * N, i, N).to(y);
 #pragma unroll 8
   for (int c = c0 + 1 + w * share; c <= c0 + min(n, (w + 1) * share); ++c) {
     float x[kE<T>];
-    load_in<float, kE<T>>(head + (size_t)c * N, min(i, N), N, x);
+    span_load<float, kE<T>>(head + (size_t)c * N, i, N).to(x);
 #pragma unroll
     for (int u = 0; u < kE<T>; ++u) y[u] += x[u];
   }
@@ -348,14 +348,14 @@ __global__ __launch_bounds__(kThreads) void embed_rest(const uint32_t* __restric
   if (w > 0 || i >= N) return;
   T* row = dE + (int64_t)k * ld_e;
   float old[kE<T>];
-  if (accumulate) load_in<T, kE<T>>(row, i, N, old);
+  if (accumulate) span_load<T, kE<T>>(row, i, N).to(old);
 #pragma unroll
   for (int u = 0; u < kE<T>; ++u) {
 #pragma unroll
     for (int o = 1; o < W; ++o) y[u] += all[o][l][u];
     y[u] = accumulate ? fmaf(y[u], scale, old[u]) : y[u] * scale;
   }
-  store_past_in<T, kE<T>>(row, i, N, y);
+  span_store<T, kE<T>, true>(row, i, N, y);
 }
 
 struct GradPlan {

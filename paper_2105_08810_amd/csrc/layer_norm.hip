@@ -3,7 +3,7 @@
 //   y = h gamma + beta,  h = (x - mean) rstd,  mean = sum x / N,  rstd = 1 / sqrt(sum (x - mean)^2 / N + eps)
 //   a = dy gamma,  dx = rstd (a - mean(a) - h mean(a h)),  dgamma = sum over rows of dy h,  dbeta = sum over rows of dy
 //
-// Bound: memory. A row is read once into the registers of its lanes (16 lanes, a wavefront, or a block of 256 or 1024
+// Bound: memory. A row is read once into the registers of its lanes (16 lanes, a wavefront, or a block of 256 to 1024
 // threads by its width), the squares are summed about the mean that is already known, and the results are written from
 // the registers. The backward pass reads x and dy once; each group of lanes walks many rows and keeps its columns' shares
 // of dgamma and dbeta in registers, a block adds its groups' shares and writes one partial row, and norm_columns adds the
@@ -60,6 +60,10 @@ __device__ __forceinline__ void group_sum2(float& a, float& b, float2* red) {
 template <int L>
 constexpr int kBlock = L > 256 ? L : 256;
 
+// Whether a row may be shorter than a vector: only the narrowest rows are.
+template <int L>
+constexpr bool kShort = L == 16;
+
 template <class TX, class TY>
 constexpr int kE = sizeof(TX) == 4 || sizeof(TY) == 4 ? 4 : 8;
 
@@ -73,6 +77,12 @@ __device__ __forceinline__ void kept(Raw<T, E> (&raw)[Q]) {
 #pragma unroll
       for (int u = 0; u < E / 2; ++u) asm volatile("" : "+v"(raw[q].w[u]));
   }
+}
+
+// Whether a row may end in its lanes' vector q, or before it: shape_of takes as few vectors as there can be.
+template <int L, int Q>
+__device__ __forceinline__ constexpr bool ragged(int q) {
+  return q == Q - 1 || (L == 1024 && Q == 4 && q >= 2);
 }
 
 // Whether a wavefront holds anything of its vector q: the last vectors of most of a block's wavefronts may lie past the row.
@@ -92,16 +102,18 @@ __global__ __launch_bounds__(kBlock<L>) void norm_forward(const TX* __restrict__
   __shared__ float red[kBlock<L> / kWave];
   const int l = threadIdx.x % L;
   float g[Q][E], b[Q][E];
+  bool own[Q][E];
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
-    const int i = min((q * L + l) * E, N);
-    if (gamma) load_in<float, E>(gamma, i, N, g[q]);
-    if (beta) load_in<float, E>(beta, i, N, b[q]);
+    const int i = (q * L + l) * E;
+    if (gamma) span_load<float, E, kShort<L>>(gamma, i, N).to(g[q]);
+    if (beta) span_load<float, E, kShort<L>>(beta, i, N).to(b[q]);
 #pragma unroll
     for (int u = 0; u < E; ++u) {
       if (!gamma) g[q][u] = 1.0f;
       if (!beta) b[q][u] = -0.0f;  // h + -0 is h
     }
+    span_own<E, kShort<L>>(i, N, own[q]);
   }
   // with L > kWave a block is one row: all its threads or none
   const int64_t step = (int64_t)gridDim.x * G;
@@ -110,7 +122,7 @@ __global__ __launch_bounds__(kBlock<L>) void norm_forward(const TX* __restrict__
   Raw<TX, E> raw[Q], next[Q];
   const auto fetch = [&](Raw<TX, E> (&to)[Q], int64_t row) {
 #pragma unroll
-    for (int q = 0; q < Q; ++q) to[q] = raw_in<TX, E>(x + row * ld_x, (q * L + l) * E, N);
+    for (int q = 0; q < Q; ++q) to[q] = span_load<TX, E, kShort<L>>(x + row * ld_x, (q * L + l) * E, N);
   };
   fetch(raw, r);
   for (; r < R; r += step) {
@@ -122,7 +134,7 @@ __global__ __launch_bounds__(kBlock<L>) void norm_forward(const TX* __restrict__
       float v[E];
       raw[q].to(v);
 #pragma unroll
-      for (int u = 0; u < E; ++u) s += v[u];
+      for (int u = 0; u < E; ++u) s += !ragged<L, Q>(q) || own[q][u] ? v[u] : 0.0f;
     }
     const float m = group_sum<L>(s, red) / (float)N;
     kept(raw);
@@ -134,21 +146,20 @@ __global__ __launch_bounds__(kBlock<L>) void norm_forward(const TX* __restrict__
       raw[q].to(v);
 #pragma unroll
       for (int u = 0; u < E; ++u) {
-        const float d = v[u] - m;
-        if ((q * L + l) * E + u < N) d2 = fmaf(d, d, d2);
+        const float d = !ragged<L, Q>(q) || own[q][u] ? v[u] - m : 0.0f;
+        d2 = fmaf(d, d, d2);
       }
     }
     const float k = 1.0f / sqrtf(group_sum<L>(d2, red) / (float)N + eps);
     kept(raw);
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      const int i = (q * L + l) * E;
-      if (i >= N) continue;
+      if (!any_of<L, E>(q, N)) continue;
       float v[E];
       raw[q].to(v);
 #pragma unroll
       for (int u = 0; u < E; ++u) v[u] = fmaf((v[u] - m) * k, g[q][u], b[q][u]);
-      store_past_in<TY, E>(y + r * ld_y, i, N, v);
+      span_store<TY, E, true, kShort<L>>(y + r * ld_y, (q * L + l) * E, N, v);
     }
     if (l == 0) {
       if (mean) mean[r] = m;
@@ -173,14 +184,17 @@ __global__ __launch_bounds__(kBlock<L>) void norm_backward(const TY* __restrict_
   extern __shared__ float share[];  // [G][L * E] of one vector of the groups' shares
   const int g = threadIdx.x / L, l = threadIdx.x % L;
   float dg[Q][E], db[Q][E], w[Q][E];
+  bool own[Q][E];
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
-    if (gamma) load_in<float, E>(gamma, min((q * L + l) * E, N), N, w[q]);
+    const int i = (q * L + l) * E;
+    if (gamma) span_load<float, E, kShort<L>>(gamma, i, N).to(w[q]);
 #pragma unroll
     for (int u = 0; u < E; ++u) {
       dg[q][u] = db[q][u] = 0.0f;
       if (!gamma) w[q][u] = 1.0f;
     }
+    span_own<E, kShort<L>>(i, N, own[q]);
   }
   // with L > kWave a block is one row: all its threads or none
   const int64_t step = (int64_t)gridDim.x * G;
@@ -192,8 +206,8 @@ __global__ __launch_bounds__(kBlock<L>) void norm_backward(const TY* __restrict_
     nk = rstd[row];
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      nx[q] = raw_in<TX, E>(x + row * ld_x, (q * L + l) * E, N);
-      ny[q] = raw_in<TY, E>(dy + row * ld_dy, (q * L + l) * E, N);
+      nx[q] = span_load<TX, E, kShort<L>>(x + row * ld_x, (q * L + l) * E, N);
+      ny[q] = span_load<TY, E, kShort<L>>(dy + row * ld_dy, (q * L + l) * E, N);
     }
   };
   int64_t r = (int64_t)blockIdx.x * G + g;
@@ -221,9 +235,12 @@ __global__ __launch_bounds__(kBlock<L>) void norm_backward(const TY* __restrict_
           dg[q][u] = fmaf(a[u], h[u], dg[q][u]);
           db[q][u] += a[u];
         }
+        // others' elements enter neither sum (the dgamma, dbeta and dx that the lane makes of them are not stored); as 0
+        // times one that is infinite they would
+        const bool mine = !ragged<L, Q>(q) || own[q][u];
         a[u] *= w[q][u];
-        s += a[u];  // 0 past the row's end
-        sh = fmaf(a[u], h[u], sh);
+        s += mine ? a[u] : 0.0f;
+        sh = mine ? fmaf(a[u], h[u], sh) : sh;
       }
     }
     if (dx) {
@@ -234,14 +251,13 @@ __global__ __launch_bounds__(kBlock<L>) void norm_backward(const TY* __restrict_
       kept(ry);
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
-        const int i = (q * L + l) * E;
-        if (i >= N) continue;
+        if (!any_of<L, E>(q, N)) continue;
         float h[E], a[E];
         rx[q].to(h);
         ry[q].to(a);
 #pragma unroll
         for (int u = 0; u < E; ++u) a[u] = k * (a[u] * w[q][u] - s - (h[u] - m) * k * sh);
-        store_past_in<TX, E>(dx + r * ld_dx, i, N, a);
+        span_store<TX, E, true, kShort<L>>(dx + r * ld_dx, (q * L + l) * E, N, a);
       }
     }
   }
@@ -266,29 +282,29 @@ __global__ __launch_bounds__(kBlock<L>) void norm_backward(const TY* __restrict_
             for (int u = 0; u < E; ++u) t[u] += share[(o * L + l) * E + u];
         }
       }
-      if (g == 0 && i < N) store_in<float, E>(mine + (size_t)which * N, i, N, t);
+      if (g == 0) span_store<float, E, false, kShort<L>>(mine + (size_t)which * N, i, N, t);
     }
   }
 }
 
-// dgamma and dbeta: the sums of the parts' columns, in float64. A block takes 64 columns, its wavefronts every
-// kColumnWaves-th part.
-constexpr int kColumnWaves = 16;
-__global__ __launch_bounds__(kColumnWaves * kWave) void norm_columns(const float* __restrict__ part, int n, int N,
-                                                                     float* __restrict__ dgamma,
-                                                                     float* __restrict__ dbeta) {
-  __shared__ double sum[kColumnWaves][kWave];
-  const int w = threadIdx.x / kWave, l = lane_id();
-  const int64_t j = (int64_t)blockIdx.x * kWave + l;  // of 2 N: dgamma, then dbeta
+// dgamma and dbeta: the sums of the parts' columns, in float64. A block takes 32 columns, each half of its wavefronts every
+// kStreams-th part, 16 of them under way together.
+constexpr int kColumns = 32, kStreams = 32;
+__global__ __launch_bounds__(kColumns * kStreams) void norm_columns(const float* __restrict__ part, int n, int N,
+                                                                    float* __restrict__ dgamma,
+                                                                    float* __restrict__ dbeta) {
+  __shared__ double sum[kStreams][kColumns];
+  const int w = threadIdx.x / kColumns, l = threadIdx.x % kColumns;
+  const int64_t j = (int64_t)blockIdx.x * kColumns + l;  // of 2 N: dgamma, then dbeta
   double s = 0.0;
   if (j < 2 * (int64_t)N) {
-#pragma unroll 8
-    for (int p = w; p < n; p += kColumnWaves) s += (double)part[(size_t)p * 2 * N + j];
+#pragma unroll 16
+    for (int p = w; p < n; p += kStreams) s += (double)part[(size_t)p * 2 * N + j];
   }
   sum[w][l] = s;
   __syncthreads();
   if (w == 0 && j < 2 * (int64_t)N) {
-    for (int o = 1; o < kColumnWaves; ++o) s += sum[o][l];
+    for (int o = 1; o < kStreams; ++o) s += sum[o][l];
     float* out = j < N ? dgamma : dbeta;
     if (out) out[j < N ? j : j - N] = (float)s;
   }
@@ -397,9 +413,10 @@ __global__ __launch_bounds__(256) void norm_columns_long(const TY* __restrict__ 
   part[(size_t)blockIdx.y * 2 * N + N + j] = db;
 }
 
-// How a row of N is spread: lanes and vectors a lane; L 0: beyond a block's registers. A wavefront alone needs no barrier
+// How a row of N is spread: lanes and vectors a lane. L 0: beyond a block's registers. A wavefront alone needs no barrier
 // between its sums; with more than 20 values a lane (gamma, beta and their gradients are held beside the row's) too few
-// wavefronts fit, and a block of 256 takes the row.
+// wavefronts fit, and a block takes the row: of 256 threads up to 384 vectors (8192 x 2050 bfloat16, 257 vectors, backward:
+// two each of 256 threads 33 us, one each of 384 41), of 512 and 1024 beyond.
 struct Shape {
   int L, Q;
 };
@@ -409,8 +426,9 @@ Shape shape_of(int N, int E) {
   for (int q = 1; q * E <= 20; ++q)
     if (v <= 64 * q) return {64, q};
   if (v <= 256) return {256, 1};
-  if (v <= 512) return {256, 2};
-  if (v <= 1024) return {256, 4};
+  if (v <= 384) return {256, 2};
+  if (v <= 512) return {512, 1};
+  if (v <= 1024) return {512, 2};
   if (v <= 2048) return {1024, 2};
   if (v <= 4096) return {1024, 4};
   return {0, 0};
@@ -418,14 +436,17 @@ Shape shape_of(int N, int E) {
 
 int vector_of(int x_dtype, int y_dtype) { return x_dtype == SNN_F32 || y_dtype == SNN_F32 ? 4 : 8; }
 
-// Blocks of the backward pass, each with a partial row: enough for four a compute unit, few enough that a block has
-// several rows to add up.
+// Blocks of the backward pass, each with a partial row: as many as are resident, that none is left for a second turn and
+// the partial rows are few. A wavefront's rows of several vectors, and the blocks of 512 and 1024 threads, leave room for
+// two blocks a compute unit (backward of 64000 x 2048 float32 with 1024 blocks 329 us, with 512 277; backward
+// of 8192 x 1024 bfloat16 22.8 and 18.3), the others for four (100000 x 100 float32 34 us, with 512 45; 8192 x 2050
+// bfloat16 32 and 37, 256000 x 300 130 and 164).
 int parts_of(int64_t R, int N, int E) {
   const Shape sh = shape_of(N, E);
   if (!sh.L) return (int)std::min<int64_t>(R, 64);
   const int G = sh.L >= 256 ? 1 : 256 / sh.L;
   const int64_t blocks = (R + G - 1) / G;
-  return (int)std::min<int64_t>(blocks, 1024);
+  return (int)std::min<int64_t>(blocks, sh.L >= 512 || (sh.L == 64 && sh.Q > 1) ? 512 : 1024);
 }
 
 constexpr int64_t kLaunchRows = (int64_t)1 << 21;  // a dispatch counts threads in 32 bits
@@ -450,8 +471,9 @@ void forward(const void* x, int64_t ld_x, int64_t R, int N, const float* gamma, 
     else if (sh.L == 64 && sh.Q == 4) SNN_N(64, 4);
     else if (sh.L == 64) SNN_N(64, 5);
     else if (sh.L == 256 && sh.Q == 1) SNN_N(256, 1);
-    else if (sh.L == 256 && sh.Q == 2) SNN_N(256, 2);
-    else if (sh.L == 256) SNN_N(256, 4);
+    else if (sh.L == 256) SNN_N(256, 2);
+    else if (sh.L == 512 && sh.Q == 1) SNN_N(512, 1);
+    else if (sh.L == 512) SNN_N(512, 2);
     else if (sh.L == 1024 && sh.Q == 2) SNN_N(1024, 2);
     else if (sh.L == 1024) SNN_N(1024, 4);
     else
@@ -480,8 +502,9 @@ void backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int64_
   else if (sh.L == 64 && sh.Q == 4) SNN_N(64, 4);
   else if (sh.L == 64) SNN_N(64, 5);
   else if (sh.L == 256 && sh.Q == 1) SNN_N(256, 1);
-  else if (sh.L == 256 && sh.Q == 2) SNN_N(256, 2);
-  else if (sh.L == 256) SNN_N(256, 4);
+  else if (sh.L == 256) SNN_N(256, 2);
+  else if (sh.L == 512 && sh.Q == 1) SNN_N(512, 1);
+  else if (sh.L == 512) SNN_N(512, 2);
   else if (sh.L == 1024 && sh.Q == 2) SNN_N(1024, 2);
   else if (sh.L == 1024) SNN_N(1024, 4);
   else {
@@ -555,7 +578,7 @@ extern "C" snn_status snn_layer_norm_grad(const void* dy, int y_dtype, int64_t l
   SNN_PAIRS(SNN_F);
 #undef SNN_F
   if (columns)
-    hipLaunchKernelGGL(norm_columns, dim3((unsigned)((2 * (int64_t)N + kWave - 1) / kWave)), dim3(kColumnWaves * kWave), 0,
-                       s, part, parts, N, dgamma, dbeta);
+    hipLaunchKernelGGL(norm_columns, dim3((unsigned)((2 * (int64_t)N + kColumns - 1) / kColumns)),
+                       dim3(kColumns * kStreams), 0, s, part, parts, N, dgamma, dbeta);
   return launch_status();
 }

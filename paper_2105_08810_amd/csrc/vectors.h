@@ -50,11 +50,11 @@ template <class T, int E>
 __device__ __forceinline__ Raw<T, E> raw_in(const T* row, int i, int n) {
   static_assert(E * sizeof(T) % 4 == 0, "whole words");
   Raw<T, E> r;
-  if (i + E <= n) {
-    __builtin_memcpy(r.w, row + i, sizeof(r.w));
-  } else {
+  // the zeros first and by themselves: written beside the load, in another branch, they would wait for it
 #pragma unroll
-    for (int q = 0; q < Raw<T, E>::kWords; ++q) r.w[q] = 0;
+  for (int q = 0; q < Raw<T, E>::kWords; ++q) r.w[q] = 0;
+  if (i + E <= n) __builtin_memcpy(r.w, row + i, sizeof(r.w));
+  if (i < n && i + E > n) {
 #pragma unroll
     for (int u = 0; u < E; ++u)
       if (i + u < n) {
@@ -81,6 +81,28 @@ __device__ __forceinline__ void store_in(T* row, int i, int n, const float (&x)[
   }
 }
 
+// A lane's vector of a row without a branch around its load: the vector at i where it lies inside the row, else the row's last
+// E elements, of which the first skip_of() are other lanes' (all E past the row's end). A branch for the last vector would
+// hold up every load before it. Rows shorter than E (SHORT: there may be such) are taken by raw_in, where element u is i + u.
+__device__ __forceinline__ int start_of(int i, int n, int E) { return n >= E ? min(i, n - E) : i; }
+__device__ __forceinline__ int skip_of(int i, int n, int E) { return n >= E ? min(max(i + E - n, 0), E) : 0; }
+
+template <class T, int E, bool SHORT = true>
+__device__ __forceinline__ Raw<T, E> span_load(const T* row, int i, int n) {
+  if (SHORT && n < E) return raw_in<T, E>(row, i, n);
+  Raw<T, E> r;
+  __builtin_memcpy(r.w, row + start_of(i, n, E), sizeof(r.w));
+  return r;
+}
+
+// Whether the elements of such a vector are the lane's own, not those of others or past the row.
+template <int E, bool SHORT = true>
+__device__ __forceinline__ void span_own(int i, int n, bool (&own)[E]) {
+  const int skip = skip_of(i, n, E);
+#pragma unroll
+  for (int u = 0; u < E; ++u) own[u] = SHORT && n < E ? i + u < n : u >= skip;
+}
+
 // store_in past the caches, for results much larger than they are.
 template <class T, int E>
 __device__ __forceinline__ void store_past_in(T* row, int i, int n, const float (&x)[E]) {
@@ -94,6 +116,20 @@ __device__ __forceinline__ void store_past_in(T* row, int i, int n, const float 
     __builtin_nontemporal_store(w, reinterpret_cast<Words*>(row + i));
   } else {
     store_in<T, E>(row, i, n, x);
+  }
+}
+
+// The lane's own elements of such a vector to a row, past the caches or not.
+template <class T, int E, bool PAST, bool SHORT = true>
+__device__ __forceinline__ void span_store(T* row, int i, int n, const float (&x)[E]) {
+  if (i + E <= n || (SHORT && n < E)) {
+    if constexpr (PAST) store_past_in<T, E>(row, i, n, x);
+    else store_in<T, E>(row, i, n, x);
+  } else if (i < n) {
+    const int skip = skip_of(i, n, E);
+#pragma unroll
+    for (int u = 0; u < E; ++u)
+      if (u >= skip) row[n - E + u] = from_float<T>(x[u]);
   }
 }
 

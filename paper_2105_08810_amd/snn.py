@@ -892,16 +892,15 @@ def layer_norm(x: torch.Tensor, gamma=None, beta=None, eps=1e-5, out_dtype=None,
     p, code, R, N, ld = _rows(x, "x")
     dev, f32, shape = x.device, torch.float32, x.shape[:-1]
     if out is None:
-        out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=dev)
-        o, code_o, ld_o = out.data_ptr(), _DTYPES.get(out.dtype), N
+        out = torch.empty_like(x, dtype=out_dtype, memory_format=torch.contiguous_format)
+        o, code_o, ld_o = out.data_ptr(), code if out_dtype is None else _DTYPES.get(out_dtype), N
         if code_o is None:
             raise TypeError(f"layer_norm gives float32, bfloat16 or float16, not {out.dtype}")
     else:
         o, code_o, R_o, N_o, ld_o = _rows(out, "out")
         if (R_o, N_o) != (R, N):
             raise ValueError("out must have the shape of x")
-    mean = torch.empty(shape, dtype=f32, device=dev)
-    rstd = torch.empty(shape, dtype=f32, device=dev)
+    mean, rstd = torch.empty((2, *shape), dtype=f32, device=dev).unbind(0)
     _check("snn_layer_norm", lib().snn_layer_norm(
         p, code, R, N, ld, _of_rows(gamma, N, f32, "gamma"), _of_rows(beta, N, f32, "beta"), eps, o, code_o, ld_o,
         mean.data_ptr(), rstd.data_ptr(), _stream()))

@@ -162,6 +162,25 @@ def test_layer_norm(x_dtype, y_dtype, R, N, affine, pad, lead):
     assert none is None and torch.equal(g2, dgamma) and torch.equal(b2, dbeta)
 
 
+# a row that ends inside a lane's vector, with an infinity among its last elements: only its own row's sums hold it, once
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N", [3, 9, 68, 257, 1027, 2051, 4099, 8195])
+def test_layer_norm_infinite(dtype, N):
+    gen = torch.Generator().manual_seed(N)
+    x, dy = (torch.randn(3, N, generator=gen).to(DTYPES[dtype]).cuda() for _ in range(2))
+    y0, mean0, rstd0 = snn.layer_norm(x)
+    dx0, *_ = snn.layer_norm_grad(dy, x, None, mean0, rstd0, want_dgamma=False, want_dbeta=False)
+    xi, di = x.clone(), dy.clone()
+    xi[1, N - 2] = INF
+    di[1, N - 2] = -INF
+    y, mean, rstd = snn.layer_norm(xi)
+    assert float(mean[1]) == INF and rstd[1].isnan() and y[1, N - 1].isnan()
+    assert torch.equal(y[::2], y0[::2]) and torch.equal(mean[::2], mean0[::2]) and torch.equal(rstd[::2], rstd0[::2])
+    dx, dgamma, dbeta = snn.layer_norm_grad(di, x, None, mean0, rstd0)
+    assert torch.equal(dx[::2], dx0[::2]) and not dx[1].isfinite().any()
+    assert host(~dgamma.isfinite()).nonzero()[0].tolist() == [N - 2] and float(dbeta[N - 2]) == -INF
+
+
 @pytest.mark.parametrize("R,N", [(5000, 40), (3000, 1024), (1500, 2050)])
 def test_layer_norm_many_rows(R, N):
     """More rows than groups of lanes: dgamma and dbeta gather over several rows each."""

@@ -645,14 +645,19 @@ snn_status snn_layer_norm_grad(const void* dy, int y_dtype, int64_t ld_dy, const
  * never in memory together. A readout without threshold is such a product: V_out = trace W_out.
  *   x        R rows of H values of dtype
  *   W        H rows of C values of dtype
- *   targets  int32 [R]; a row whose target is outside [0,C) takes no part: it is not read, its loss and gradient are 0
- *   weight   float32 [R], or NULL for one over the number of rows that have a target. A row of weight 0 takes no part.
+ *   targets  int32 [R]; a row whose target is outside [0,C) takes no part: whatever it holds, its loss and gradient are 0
+ *   weight   float32 [R] of finite values, or NULL for one over the number of rows that have a target. A row of weight 0
+ *            takes no part.
  *   loss     float32 [1] (written): sum_r weight_r L_r, L_r = log sum_c exp(z_rc) - z_r,target; 0 if no row takes part
  *   row_loss float32 [R] (written unless NULL): L_r
  *   dx       R rows of H values of dtype (written unless NULL): weight_r (softmax(z_r) - onehot) W^T
  *   dW       H rows of C values of dtype (written unless NULL): x^T (weight_r (softmax(z_r) - onehot))
- * R up to 2^24, H up to 2^16, C up to 2^20, distances of rows up to 2^31 - 1; larger: SNN_ERR_UNSUPPORTED. The workspace query takes
- * whether a gradient is wanted. The workspace grows with R H, and with R times a piece of the classes (bounded).
+ * In 16 bits weight_r (softmax(z_r) - onehot) is rounded to dtype as a share of the largest weight, and shares below
+ * 2^-126 (bfloat16) or 2^-40 (float16) of it count as 0. In float32 with at most 128 classes values of W from 2^97 on
+ * overflow in dx. What is not finite in x may make its row's loss and gradients NaN, in W every row's.
+ * R up to 2^24, H up to 2^16, C up to 2^20, distances of rows up to 2^31 - 1; larger: SNN_ERR_UNSUPPORTED. The workspace
+ * query takes whether a gradient is wanted. The workspace grows with R H, with R times a piece of the classes (bounded)
+ * and in 16 bits with R C / 8 bytes.
  */
 size_t snn_linear_ce_workspace(int dtype, int64_t R, int H, int C, int grad);
 snn_status snn_linear_ce(const void* x, const void* W, int dtype, int64_t R, int H, int C, int64_t ld_x, int64_t ld_w,

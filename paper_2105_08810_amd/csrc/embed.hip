@@ -28,7 +28,7 @@ constexpr int kDigit = 9;          // bits of a digit
 constexpr int kBins = 1 << kDigit;
 constexpr int kSortThreads = 256;
 // Steps of 64 rows of a wavefront: few where that is needed to fill the card (128000 rows, two passes: counts and places
-// 13 us a pass with 4, 23 with 16), more for the longest lists, whose counts (a block's 512 each) would grow too large.
+// 11 us a pass with 4, 23 with 16), more for the longest lists, whose counts (a block's 512 each) would grow too large.
 constexpr int kFewSteps = 4, kManySteps = 16;
 constexpr int64_t kFewStepsRows = (int64_t)1 << 20;
 int sort_rows(int64_t R) { return kSortThreads * (R <= kFewStepsRows ? kFewSteps : kManySteps); }
@@ -95,7 +95,7 @@ __global__ void embed_clear_ends(int32_t* __restrict__ first, int64_t V) {
 }
 
 // The place of each row among all R <= kRankRows: how many rows have a smaller key, or the same and come before it. A block
-// ranks 32 rows, 32 threads share a row, four keys a read. first[v] = -1 for every token on the way. 8192 rows: 9 us
+// ranks 32 rows, 32 threads share a row, four keys a read. first[v] = -1 for every token on the way. 8192 rows: 10 us
 // (56 with 8 threads a row, 256 a block and a key a read).
 __global__ __launch_bounds__(kRankThreads) void embed_rank(const int32_t* __restrict__ ids, int R, int64_t V,
                                                            uint32_t* __restrict__ keys, int32_t* __restrict__ order,

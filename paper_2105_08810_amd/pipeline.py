@@ -251,7 +251,8 @@ class Network(ReadoutRows):
         return top
 
     def membrane(self) -> torch.Tensor:
-        """V_out of the last forward; with a target at every step it is formed now."""
+        """V_out of the last forward; with a target at every step it is formed now, from that forward's spikes and W_out
+        as it is now."""
         if self.V_out is None:
             if not self.S:
                 raise ValueError("membrane() reads a forward's spikes: call forward() first")

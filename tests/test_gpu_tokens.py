@@ -85,7 +85,8 @@ def _ids(rng, R, V, kind):
 @pytest.mark.parametrize("R,V,N,kind", [(1, 1, 1, "one"), (1, 300, 9, "any"), (40, 7, 33, "any"), (64, 64, 8, "none"),
                                         (500, 90, 264, "zipf"), (1000, 3, 16, "sorted"), (777, 5, 1030, "one"),
                                         (8192, 600, 12, "zipf"), (8193, 600, 12, "zipf"), (20000, 1, 5, "one"),
-                                        (12345, 513, 24, "any"), (9000, 300000, 3, "zipf"), (40000, 70, 40, "sorted")])
+                                        (12345, 513, 24, "any"), (9000, 300000, 3, "zipf"), (40000, 70, 40, "sorted"),
+                                        (16384, 2000, 8, "zipf"), (16385, 2000, 8, "zipf")])
 def test_embed_grad(dtype, accumulate, R, V, N, kind):
     rng = np.random.default_rng(R + N)
     ids = _ids(rng, R, V, kind)
@@ -268,6 +269,69 @@ def test_linear_ce(dtype, R, H, C, pad, lead):
     loss, row_loss, dx, dW = snn.linear_ce(x, W, ints(t), torch.from_numpy(w).cuda(), want_grad=False)
     assert dx is None and dW is None
     assert torch.equal(row_loss, out[1]) and torch.equal(loss, out[0])
+
+
+# the widest rows: 128 and more classes, and few
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("C", [5, 130])
+def test_linear_ce_widest(dtype, C):
+    _, x, W, t = ce_case(3, 1 << 16, C, dtype, C, dead=0.0)
+    check_ce(x, W, t, None, snn.linear_ce(x, W, ints(t)), dtype)
+
+
+# more rows than one block counts, with and without weights
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("C", [6, 150])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_linear_ce_many_rows(dtype, C, weighted):
+    R = 33000
+    rng, x, W, t = ce_case(R, 8, C, dtype, C, dead=0.3)
+    x[torch.from_numpy(t < 0).cuda()] = NAN
+    w = np.where(rng.random(R) < 0.3, 0.0, rng.random(R)).astype(np.float32) if weighted else None
+    check_ce(x, W, t, w, snn.linear_ce(x, W, ints(t), None if w is None else torch.from_numpy(w).cuda()), dtype)
+
+
+def poisoned(nbytes):
+    """A workspace of NaN, and what lies behind it."""
+    ws = torch.full((nbytes + 4096,), 255, dtype=torch.uint8, device="cuda")
+    return ws[:nbytes], ws[nbytes:]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("R,H,C", [(1, 1, 1), (65, 24, 10), (300, 37, 101), (5000, 37, 101), (77, 70, 300), (500, 130, 1027),
+                                   (2900, 9, 47001)])
+def test_linear_ce_workspace(dtype, R, H, C):
+    """What the workspace held before does not matter, and nothing behind it is written."""
+    _, x, W, t = ce_case(R, H, C, dtype, 4, dead=0.2 if R > 1 else 0.0)
+    want = snn.linear_ce(x, W, ints(t))
+    ws, behind = poisoned(snn.snn_linear_ce_workspace(x.dtype, R, H, C, True))
+    got = snn.linear_ce(x, W, ints(t), ws=ws)
+    assert all(torch.equal(p, q) for p, q in zip(got, want)) and bool((behind == 255).all())
+    ws, behind = poisoned(snn.snn_linear_ce_workspace(x.dtype, R, H, C, False))
+    got = snn.linear_ce(x, W, ints(t), ws=ws, want_grad=False)
+    assert all(torch.equal(p, q) for p, q in zip(got[:2], want)) and bool((behind == 255).all())
+    with pytest.raises(snn.SnnError):
+        snn.linear_ce(x, W, ints(t), ws=ws[:-1], want_grad=False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_gradient_workspaces(dtype):
+    gen = torch.Generator().manual_seed(1)
+    for R, V, N in [(1, 1, 1), (700, 90, 33), (17000, 600, 5)]:
+        ids = torch.randint(-1, V, (R,), generator=gen, dtype=torch.int32).cuda()
+        dout = torch.randn(R, N, generator=gen).to(DTYPES[dtype]).cuda()
+        ws, behind = poisoned(snn.snn_embed_grad_workspace(dout.dtype, V, N, R))
+        assert torch.equal(snn.embed_grad(ids, dout, V, ws=ws), snn.embed_grad(ids, dout, V)) and bool((behind == 255).all())
+        with pytest.raises(snn.SnnError):
+            snn.embed_grad(ids, dout, V, ws=ws[:-1])
+    for R, N in [(1, 1), (700, 33), (300, 1030), (100, 4100), (20, 40000)]:
+        x, dy = (torch.randn(R, N, generator=gen).to(DTYPES[dtype]).cuda() for _ in range(2))
+        _, mean, rstd = snn.layer_norm(x)
+        ws, behind = poisoned(snn.snn_layer_norm_grad_workspace(x.dtype, x.dtype, R, N))
+        got, want = snn.layer_norm_grad(dy, x, None, mean, rstd, ws=ws), snn.layer_norm_grad(dy, x, None, mean, rstd)
+        assert all(torch.equal(p, q) for p, q in zip(got, want)) and bool((behind == 255).all())
+        with pytest.raises(snn.SnnError):
+            snn.layer_norm_grad(dy, x, None, mean, rstd, ws=ws[:-1])
 
 
 @pytest.mark.parametrize("dtype", DTYPES)

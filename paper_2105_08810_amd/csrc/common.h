@@ -111,7 +111,7 @@ void gemm_split_km(int M, int N, int K, const float* A, int lda, const float* B,
 void gemm_split_kc(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
                    hipStream_t s, bool accumulate = false, int splits = 1, size_t c_split = 0);
 void gemm_split_kr(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
-                   hipStream_t s);
+                   hipStream_t s, int splits = 1, size_t c_split = 0);
 // The elements (r, col_idx[e]) of C, as gemm_split_kc forms it, at the entries e < cap of a CSR over C's
 // rows: out[e] (0 for a column outside [0, N)). What is not an entry is not written.
 struct GatherOut {

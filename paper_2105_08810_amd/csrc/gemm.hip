@@ -544,8 +544,8 @@ void gemm_split_kc(int M, int N, int K, const float* A, int lda, const float* B,
 }
 
 void gemm_split_kr(int M, int N, int K, const float* A, int lda, const float* B, int ldb, float* C, int ldc,
-                   hipStream_t s) {
-  launch_kc<true, false>(M, N, K, A, lda, B, ldb, C, ldc, 0, 1, 0, GatherOut{}, Gate{}, s);
+                   hipStream_t s, int splits, size_t c_split) {
+  launch_kc<true, false>(M, N, K, A, lda, B, ldb, C, ldc, 0, splits, c_split, GatherOut{}, Gate{}, s);
 }
 
 void gemm_split_kc_gather(int M, int N, int K, const float* A, int lda, const float* B, int ldb, const GatherOut& to,

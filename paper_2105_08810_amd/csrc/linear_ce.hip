@@ -110,8 +110,7 @@ __global__ __launch_bounds__(256) void ce_total(const double* __restrict__ parts
   total_of(parts, n, loss);
 }
 
-// A single piece's logits to dz (with GRAD) in one launch: log-sum-exp, loss and gradient of a row by L threads, a wavefront
-// or a block of 1024 (7 rows of 9000: 8 us against 95 by wavefronts). ld is a multiple of 4, and rows are read past n.
+// Reduction over a wavefront or a block of L threads, the same in every one.
 template <int L>
 __device__ __forceinline__ float row_reduce(float v, bool sum, float* red) {
 #pragma unroll
@@ -130,10 +129,15 @@ __device__ __forceinline__ float row_reduce(float v, bool sum, float* red) {
   return v;
 }
 
-constexpr int kRowByBlock = 1024;  // classes from which a block takes a row
-template <bool GRAD, int L>
-__global__ __launch_bounds__(L > 256 ? L : 256) void ce_rows(float* __restrict__ z, int R, int n, int ld,
-                                                             const int32_t* __restrict__ targets,
+// A single piece's logits to dz (with GRAD) in one launch: log-sum-exp, loss and gradient of a row by L threads, a wavefront
+// or a block of 1024 (7 rows of 9000: 8 us against 95 by wavefronts), its values in Q float4 of each (Q 0: rows beyond that
+// are read for every pass). The logits are the sums of `slices` K slices, z_split apart; dz goes to the first. ld is a
+// multiple of 4, and rows are read past n.
+constexpr int kRowByBlock = 1024;    // classes from which a block takes a row
+constexpr int kRowInRegs = 32768;    // classes up to which it keeps it
+template <bool GRAD, int L, int Q>
+__global__ __launch_bounds__(L > 256 ? L : 256) void ce_rows(float* __restrict__ z, int slices, size_t z_split, int R, int n,
+                                                             int ld, const int32_t* __restrict__ targets,
                                                              const uint64_t* __restrict__ live,
                                                              const int32_t* __restrict__ counts, int n_counts,
                                                              const float* __restrict__ weight,
@@ -142,22 +146,43 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ce_rows(float* __restrict__
   __shared__ double all[G];
   __shared__ float red[L / kWave];
   const int w = threadIdx.x / L, l = threadIdx.x % L;
-  const int r = blockIdx.x * G + w;
+  const float same = weight ? 0.0f : same_weight(counts, n_counts);
   double weighted = 0.0;
-  if (r < R) {  // with L > 64 a block is one row
+  for (int r = blockIdx.x * G + w; r < R; r += gridDim.x * G) {  // with L > 64 a block is one row
     float* row = z + (size_t)r * ld;
     const bool on = alive(live, r);
-    const float k = !on ? 0.0f : weight ? weight[r] : same_weight(counts, n_counts);
+    const float k = !on ? 0.0f : weight ? weight[r] : same;
     float loss = 0.0f, lse = 0.0f;
     const int t = on ? targets[r] : -1;
+    float4 held[Q > 0 ? Q : 1];
     const auto each = [&](auto f) {
+      if constexpr (Q > 0) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+          if (4 * (q * L + l) < n) f(4 * (q * L + l), held[q]);
+      } else {
 #pragma unroll 4
-      for (int i = 4 * l; i < n; i += 4 * L) {
-        const float4 q = *reinterpret_cast<const float4*>(row + i);
-        f(i, q);
+        for (int i = 4 * l; i < n; i += 4 * L) {
+          const float4 v = *reinterpret_cast<const float4*>(row + i);
+          f(i, v);
+        }
       }
     };
     if (on) {
+      float zt = row[t];
+      for (int p = 1; p < slices; ++p) zt += row[p * z_split + t];
+      if constexpr (Q > 0) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+          if (4 * (q * L + l) < n) held[q] = *reinterpret_cast<const float4*>(row + 4 * (q * L + l));
+        for (int p = 1; p < slices; ++p)
+#pragma unroll
+          for (int q = 0; q < Q; ++q)
+            if (4 * (q * L + l) < n) {
+              const float4 v = *reinterpret_cast<const float4*>(row + p * z_split + 4 * (q * L + l));
+              held[q].x += v.x; held[q].y += v.y; held[q].z += v.z; held[q].w += v.w;
+            }
+      }
       float m = -INFINITY;
       each([&](int i, const float4& q) {  // a NaN is left to the sum
         m = fmaxf(m, q.x);
@@ -174,23 +199,25 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ce_rows(float* __restrict__
         if (i + 2 < n) s += expf(q.z - from);
         if (i + 3 < n) s += expf(q.w - from);
       });
-      s = row_reduce<L>(s, true, red);
+      s = row_reduce<L>(s, true, red);  // every thread has read row[t]
       const float log_sum = logf(s);
       lse = m + log_sum;
-      loss = (m - row[t]) + log_sum;
-      weighted = (double)k * (double)loss;
+      loss = (m - zt) + log_sum;
+      weighted += (double)k * (double)loss;
     }
     if (l == 0 && row_loss) row_loss[r] = loss;
     if (GRAD) {
-      if constexpr (L > kWave) __syncthreads();  // row[t] has been read
-      else __builtin_amdgcn_wave_barrier();
-      each([&](int i, const float4& q) {
+      if constexpr (L == kWave) __builtin_amdgcn_wave_barrier();
+      const auto store = [&](int i, const float4& q) {
         const float p[4] = {q.x, q.y, q.z, q.w};
         float d[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) d[u] = on ? k * (expf(p[u] - lse) - (i + u == t ? 1.0f : 0.0f)) : 0.0f;
         *reinterpret_cast<float4*>(row + i) = make_float4(d[0], d[1], d[2], d[3]);  // the row's own padding past n
-      });
+      };
+      if (on) each(store);
+      else
+        for (int i = 4 * l; i < n; i += 4 * L) *reinterpret_cast<float4*>(row + i) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
   }
   if (l == 0) all[w] = weighted;
@@ -201,7 +228,9 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ce_rows(float* __restrict__
   }
 }
 
-// The last launch: block 0 adds up the loss, the others clear dx in the rows that take no part (dx NULL: none).
+// The last launch: block 0 adds up the loss, the others clear dx in the rows that take no part (dx NULL: none), a wavefront
+// in those of 16 rows.
+constexpr int kClearRows = 16;
 __global__ __launch_bounds__(kWaves * kWave) void ce_finish(const double* __restrict__ parts, int n,
                                                             float* __restrict__ loss, const uint64_t* __restrict__ live,
                                                             int R, int H, float* __restrict__ dx, int64_t ld) {
@@ -209,9 +238,15 @@ __global__ __launch_bounds__(kWaves * kWave) void ce_finish(const double* __rest
     total_of(parts, n, loss);
     return;
   }
-  const int r = ((int)blockIdx.x - 1) * kWaves + threadIdx.x / kWave;
-  if (r >= R || alive(live, r)) return;
-  for (int i = lane_id(); i < H; i += kWave) dx[(int64_t)r * ld + i] = 0.0f;
+  const int r0 = (((int)blockIdx.x - 1) * kWaves + threadIdx.x / kWave) * kClearRows;
+  if (r0 >= R) return;
+  uint32_t dead = ~(uint32_t)(live[r0 >> 6] >> (r0 & 63)) & ((1u << min(R - r0, kClearRows)) - 1);
+  const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  while (dead) {
+    float* row = dx + (int64_t)(r0 + __builtin_ctz(dead)) * ld;
+    dead &= dead - 1;
+    for (int i = 4 * lane_id(); i < H; i += 4 * kWave) store_in<float, 4>(row, i, H, zero);
+  }
 }
 
 // dx from its K slices, 0 in rows that take no part: a block takes 64 h of a row, its wavefronts a quarter of the slices each.
@@ -626,7 +661,7 @@ bool few_of(int dtype, int R, int C) { return C <= kFew && (dtype == SNN_F32 || 
 
 struct Plan {
   int width, pieces;          // classes of a piece
-  int dw_slices, dx_slices;   // K slices of the gradients' products
+  int z_slices, dw_slices, dx_slices;   // K slices of the products
   int ld;                     // of a piece's logits
 };
 
@@ -635,6 +670,7 @@ Plan plan_of(int R, int H, int C) {
   p.width = (int)std::min<int64_t>(C, std::max<int64_t>(256, kPiece / R / 128 * 128));
   p.pieces = (C + p.width - 1) / p.width;
   p.ld = (p.width + 3) / 4 * 4;
+  p.z_slices = p.pieces == 1 && p.width <= kRowInRegs ? plan_splits(R, p.width, H, 88e12).splits : 1;
   p.dw_slices = plan_splits(H, p.width, R, 88e12).splits;
   p.dx_slices = plan_splits(R, H, p.width, 88e12).splits;
   return p;
@@ -665,7 +701,7 @@ Workspace carve(void* ws, int R, int H, bool few, bool grad, const Plan& p) {
   g.at_target = c.take<float>(rows);
   g.lse = c.take<float>(rows);
   g.parts = c.take<double>(few ? (R + 63) / 64 : p.pieces == 1 ? R : kLossParts);
-  g.z = c.take<float>(few && !grad ? 0 : (size_t)R * p.ld);
+  g.z = c.take<float>(few && !grad ? 0 : (size_t)R * p.ld * (few ? 1 : p.z_slices));
   g.dX = c.take<float>(!few && grad && p.dx_slices > 1 ? (size_t)p.dx_slices * R * H : 0);
   g.dW = c.take<float>(grad && p.dw_slices > 1 ? (size_t)p.dw_slices * H * p.width : 0);
   g.bytes = c.off;
@@ -747,15 +783,24 @@ void run(const float* x, int64_t ld_x, const float* W, int64_t ld_w, int R, int 
   hipLaunchKernelGGL(ce_live, dim3((unsigned)counted), dim3(256), 0, s, targets, weight, R, C, g.live, g.counts);
   int n_parts = 0;
   if (p.pieces == 1) {
-    gemm_split_kr(R, C, H, x, (int)ld_x, W, (int)ld_w, g.z, p.ld, s);
+    const size_t z_split = (size_t)R * p.ld;
+    gemm_split_kr(R, C, H, x, (int)ld_x, W, (int)ld_w, g.z, p.ld, s, p.z_slices, z_split);
     const bool by_block = C >= kRowByBlock;
-    n_parts = by_block ? R : (int)rows.x;
+    n_parts = by_block ? std::min(R, 2 * cu_count()) : std::min((int)rows.x, 8 * cu_count());
     const auto of_rows = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)n_parts), dim3(by_block ? 1024 : 256), 0, s, g.z, R, C, p.ld, targets, g.live,
-                         g.counts, counted, weight, row_loss, g.parts);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)n_parts), dim3(by_block ? 1024 : 256), 0, s, g.z, p.z_slices, z_split, R, C,
+                         p.ld, targets, g.live, g.counts, counted, weight, row_loss, g.parts);
     };
-    if (by_block) of_rows(grad ? ce_rows<true, 1024> : ce_rows<false, 1024>);
-    else of_rows(grad ? ce_rows<true, kWave> : ce_rows<false, kWave>);
+#define SNN_ROWS(L, Q) of_rows(grad ? ce_rows<true, L, Q> : ce_rows<false, L, Q>)
+    if (C <= 256) SNN_ROWS(kWave, 1);
+    else if (C <= 512) SNN_ROWS(kWave, 2);
+    else if (!by_block) SNN_ROWS(kWave, 4);
+    else if (C <= 4096) SNN_ROWS(1024, 1);
+    else if (C <= 8192) SNN_ROWS(1024, 2);
+    else if (C <= 16384) SNN_ROWS(1024, 4);
+    else if (C <= kRowInRegs) SNN_ROWS(1024, 8);
+    else SNN_ROWS(1024, 0);
+#undef SNN_ROWS
   } else {
     for (int c0 = 0; c0 < C; c0 += p.width) {
       const int n = std::min(p.width, C - c0);
@@ -781,7 +826,8 @@ void run(const float* x, int64_t ld_x, const float* W, int64_t ld_w, int R, int 
     hipLaunchKernelGGL(ce_dx, dim3((unsigned)R, (unsigned)((H + kWave - 1) / kWave)), waves, 0, s, g.dX, p.dx_slices, g.live,
                        R, H, dx, ld_dx);
   const bool clear = dx && p.dx_slices == 1;
-  hipLaunchKernelGGL(ce_finish, dim3(1 + (clear ? rows.x : 0)), waves, 0, s, g.parts, n_parts, loss, g.live, R, H, dx, ld_dx);
+  hipLaunchKernelGGL(ce_finish, dim3(1 + (clear ? (R + kWaves * kClearRows - 1) / (kWaves * kClearRows) : 0)), waves, 0, s, g.parts,
+                     n_parts, loss, g.live, R, H, dx, ld_dx);
 }
 
 // ------------------------------------------------------------------ 16-bit operands

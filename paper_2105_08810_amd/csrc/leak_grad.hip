@@ -11,7 +11,12 @@
 // in tiles of 32 steps; entries are spread into, or picked from, an LDS tile [step][column] by 8 threads a row, four each
 // under way. Loads and stores retire in order, so whatever a tile reads (a dense x, the rows' pointers, their first entries)
 // is asked for before the tile before it is stored, pointers a tile earlier still (500 x 256 x 1024, 2% of it entries, to a
-// dense y: 154 us otherwise, 124 so, 4.5 TB/s; 100 x 256 x 200 dense to entries: 11).
+// dense y: 154 us otherwise, 124 so, 4.5 TB/s).
+//
+// Where no compute unit would have a second block, a block is four groups of 256 threads and takes four tiles at a time: each
+// group walks its own from 0, and what the tiles above it leave, alpha^32 a tile, is then added as alpha^(u+1) of it to
+// step u. us without and with: 100 x 256 x 200 to entries 11.5, 8.6; 500 x 2 x 1000 77, 31; 500 x 1 x 64 33, 17; 239 x 46 x
+// 114 19, 10. With two blocks a compute unit it no longer pays (100 x 512 x 200 to a dense y 13.7, 16.7).
 #include "common.h"
 
 namespace snn {
@@ -20,6 +25,7 @@ namespace {
 constexpr int kCols = 256;
 constexpr int kSteps = 32;
 constexpr int kRowLanes = kCols / kSteps;  // threads that share a row's entries
+constexpr int kGroups = 4;
 
 struct Entries {
   const int32_t* row_ptr;
@@ -47,18 +53,20 @@ __device__ __forceinline__ Range range_of(const Entries& c, int t, int row_of_st
   return r;
 }
 
-template <bool IN, bool OUT>
-__global__ __launch_bounds__(kCols) void leak_walk(int T, int B, int N, int slabs, float alpha,
+template <bool IN, bool OUT, int G>  // G groups
+__global__ __launch_bounds__(kCols * G) void leak_walk(int T, int B, int N, int slabs, float alpha,
                                                    const float* __restrict__ x, Entries in, float* __restrict__ y,
                                                    Entries out) {
-  __shared__ __attribute__((aligned(16))) float tile[IN || OUT ? kSteps : 1][kCols];
+  __shared__ __attribute__((aligned(16))) float tiles[G][IN || OUT ? kSteps : 1][kCols];
+  __shared__ float ends[G > 1 ? 2 : 1][G][kCols];  // of two rounds in turn
   const int b = blockIdx.x / slabs;
   const int c0 = (int)(blockIdx.x % slabs) * kCols;
-  const int c = threadIdx.x;
+  const int c = threadIdx.x % kCols, group = threadIdx.x / kCols;
+  auto& tile = tiles[group];
   const bool valid = c0 + c < N;
   const size_t step = (size_t)B * N;
   const size_t k = (size_t)b * N + (valid ? c0 + c : c0);
-  const int row = threadIdx.x / kRowLanes, lane = threadIdx.x % kRowLanes;
+  const int row = c / kRowLanes, lane = c % kRowLanes;
   // step u of a tile that begins at t1: x[t1 - u] enters y[t1 - u - 1], for t1 - u >= 1
   float v[kSteps], ahead[IN ? 1 : kSteps];
   const auto load = [&](int t1) {
@@ -120,7 +128,8 @@ __global__ __launch_bounds__(kCols) void leak_walk(int T, int B, int N, int slab
       if ((unsigned)s.j[q] < (unsigned)kCols) y[e + q * kRowLanes] = tile[row][s.j[q]];
   };
   // y[T-1] = 0
-  if (OUT) {
+  if (group > 0) {
+  } else if (OUT) {
     const int64_t r = (int64_t)(T - 1) * B + b;
     const int64_t e1 = clamped(out.row_ptr[r + 1], out.cap);
     for (int64_t e = clamped(out.row_ptr[r], out.cap) + c; e < e1; e += kCols)
@@ -130,22 +139,27 @@ __global__ __launch_bounds__(kCols) void leak_walk(int T, int B, int N, int slab
   }
   Range ri{0, 0}, ri_next{0, 0}, ro{0, 0}, ro_next{0, 0};
   Some si, so;
+  constexpr int kRound = kSteps * G;
   if (T > 1) {
-    load(T - 1);
+    const int t1 = T - 1 - kSteps * group, t2 = t1 - kRound;
+    load(t1);
     if (IN) {
-      ri = range_of(in, T - 1 - row >= 1 ? T - 1 - row : -1, b, B, lane);
-      ri_next = range_of(in, T - 1 - kSteps - row >= 1 ? T - 1 - kSteps - row : -1, b, B, lane);
+      ri = range_of(in, t1 - row >= 1 ? t1 - row : -1, b, B, lane);
+      ri_next = range_of(in, t2 - row >= 1 ? t2 - row : -1, b, B, lane);
       si = some_in(ri, ri.e);
     }
     if (OUT) {
-      ro = range_of(out, T - 2 - row, b, B, lane);
-      ro_next = range_of(out, T - 2 - kSteps - row, b, B, lane);
+      ro = range_of(out, t1 - 1 - row, b, B, lane);
+      ro_next = range_of(out, t2 - 1 - row, b, B, lane);
       so = some_out(ro, ro.e);
     }
   }
-  float d = 0.0f;
-  for (int t1 = T - 1; t1 > 0; t1 -= kSteps) {
-    const int t2 = t1 - kSteps, t3 = t2 - kSteps;  // where the next tiles begin
+  float d = 0.0f, far = alpha;  // alpha^kSteps
+#pragma unroll
+  for (int k = 1; k < kSteps; k *= 2) far *= far;
+  int round = 0;
+  for (int t0 = T - 1; t0 > 0; t0 -= kRound, round ^= 1) {
+    const int t1 = t0 - kSteps * group, t2 = t1 - kRound, t3 = t2 - kRound;  // where this tile and the next ones begin
     if constexpr (IN) {
       float4* clear = reinterpret_cast<float4*>(&tile[0][0]);
 #pragma unroll
@@ -165,13 +179,33 @@ __global__ __launch_bounds__(kCols) void leak_walk(int T, int B, int N, int slab
       for (int u = 0; u < kSteps; ++u) v[u] = ahead[u];
       if (t2 > 0) load(t2);
     }
+    if constexpr (G > 1) {
+      float end = 0.0f;
+#pragma unroll
+      for (int u = 0; u < kSteps; ++u) v[u] = end = fmaf(alpha, end, v[u]);
+      ends[round][group][c] = end;
+      __syncthreads();
+      float from = d;  // where this tile begins, and the next round
+#pragma unroll
+      for (int q = 0; q < G; ++q) {
+        if (q == group) from = d;
+        d = fmaf(far, d, ends[round][q][c]);
+      }
+#pragma unroll
+      for (int u = 0; u < kSteps; ++u) {
+        from *= alpha;
+        v[u] += from;
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kSteps; ++u) v[u] = d = fmaf(alpha, d, v[u]);
+    }
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {
       const int t = t1 - u - 1;
       if (t >= 0) {
-        d = fmaf(alpha, d, v[u]);
-        if (OUT) tile[u][c] = d;
-        else if (valid) __builtin_nontemporal_store(d, y + (size_t)t * step + k);
+        if (OUT) tile[u][c] = v[u];
+        else if (valid) __builtin_nontemporal_store(v[u], y + (size_t)t * step + k);
       }
     }
     if constexpr (OUT) {
@@ -208,12 +242,21 @@ extern "C" snn_status snn_leak_grad(const float* x, const int32_t* in_row_ptr, c
   hipStream_t s = static_cast<hipStream_t>(stream);
   const Entries in{in_row_ptr, in_col_idx, in_g, in_cap}, out{out_row_ptr, out_col_idx, nullptr, out_cap};
   const dim3 grid((unsigned)(B * slabs));
-#define SNN_L(I, O) \
-  hipLaunchKernelGGL((leak_walk<I, O>), grid, dim3(kCols), 0, s, T, B, N, slabs, alpha, x, in, y, out)
-  if (in_row_ptr && out_row_ptr) SNN_L(true, true);
-  else if (in_row_ptr) SNN_L(true, false);
-  else if (out_row_ptr) SNN_L(false, true);
-  else SNN_L(false, false);
+  const bool groups = T > kSteps + 1 && B * slabs <= cu_count();
+#define SNN_L(I, O)                                                                                                    \
+  if (groups)                                                                                                          \
+    hipLaunchKernelGGL((leak_walk<I, O, kGroups>), grid, dim3(kCols * kGroups), 0, s, T, B, N, slabs, alpha, x, in, y, out); \
+  else                                                                                                                 \
+    hipLaunchKernelGGL((leak_walk<I, O, 1>), grid, dim3(kCols), 0, s, T, B, N, slabs, alpha, x, in, y, out)
+  if (in_row_ptr && out_row_ptr) {
+    SNN_L(true, true);
+  } else if (in_row_ptr) {
+    SNN_L(true, false);
+  } else if (out_row_ptr) {
+    SNN_L(false, true);
+  } else {
+    SNN_L(false, false);
+  }
 #undef SNN_L
   return launch_status();
 }

@@ -406,7 +406,7 @@ def csr_of(on, with_g=None):
 
 
 @pytest.mark.parametrize("T,B,N", [(1, 1, 1), (2, 3, 5), (20, 4, 32), (33, 2, 300), (32, 1, 256), (65, 3, 257), (100, 2, 64),
-                                   (500, 1, 40)])
+                                   (500, 1, 40), (34, 2, 70), (129, 1, 300), (130, 1, 5), (70, 600, 3)])
 @pytest.mark.parametrize("density", [0.0, 0.03, 1.0])
 def test_leak_grad(T, B, N, density):
     rng = np.random.default_rng(T + B + N)

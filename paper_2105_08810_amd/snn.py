@@ -855,7 +855,7 @@ def embed(E: torch.Tensor, ids: torch.Tensor, scale=1.0, out=None, stream=None):
     p, code, V, N, ld = _rows(E, "E")
     R = ids.numel()
     if out is None:
-        out = torch.empty((*ids.shape, N), dtype=E.dtype, device=E.device)
+        out = E.new_empty((*ids.shape, N))
         o, ld_o = out.data_ptr(), N
     else:
         o, code_o, R_o, N_o, ld_o = _rows(out if out.dim() > 1 else out.view(1, -1), "out")
@@ -875,7 +875,7 @@ def embed_grad(ids: torch.Tensor, dout: torch.Tensor, V: int, scale=1.0, dE=None
         raise ValueError("embed_grad: accumulate needs a dE to add to")
     N = dout.shape[-1]
     if dE is None:
-        dE = torch.empty((V, N), dtype=dout.dtype, device=dout.device)
+        dE = dout.new_empty((V, N))
     elif dE.shape[0] != V:
         raise ValueError(f"dE must have {V} rows")
     if ws is None:
@@ -890,7 +890,7 @@ def layer_norm(x: torch.Tensor, gamma=None, beta=None, eps=1e-5, out_dtype=None,
         with torch.cuda.stream(stream):
             return layer_norm(x, gamma, beta, eps, out_dtype, out)
     p, code, R, N, ld = _rows(x, "x")
-    dev, f32, shape = x.device, torch.float32, x.shape[:-1]
+    f32, shape = torch.float32, x.shape[:-1]
     if out is None:
         out = torch.empty_like(x, dtype=out_dtype, memory_format=torch.contiguous_format)
         o, code_o, ld_o = out.data_ptr(), code if out_dtype is None else _DTYPES.get(out_dtype), N
@@ -900,7 +900,8 @@ def layer_norm(x: torch.Tensor, gamma=None, beta=None, eps=1e-5, out_dtype=None,
         o, code_o, R_o, N_o, ld_o = _rows(out, "out")
         if (R_o, N_o) != (R, N):
             raise ValueError("out must have the shape of x")
-    mean, rstd = torch.empty((2, *shape), dtype=f32, device=dev).unbind(0)
+    mean = x.new_empty(shape, dtype=f32)
+    rstd = torch.empty_like(mean)
     _check("snn_layer_norm", lib().snn_layer_norm(
         p, code, R, N, ld, _of_rows(gamma, N, f32, "gamma"), _of_rows(beta, N, f32, "beta"), eps, o, code_o, ld_o,
         mean.data_ptr(), rstd.data_ptr(), _stream()))
@@ -913,12 +914,12 @@ def layer_norm_grad(dy: torch.Tensor, x, gamma, mean, rstd, want_dx=True, want_d
     if stream is not None:
         with torch.cuda.stream(stream):
             return layer_norm_grad(dy, x, gamma, mean, rstd, want_dx, want_dgamma, want_dbeta, ws)
-    N, dev = x.shape[-1], x.device
-    dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if want_dx else None
-    dgamma = torch.empty(N, dtype=torch.float32, device=dev) if want_dgamma else None
-    dbeta = torch.empty(N, dtype=torch.float32, device=dev) if want_dbeta else None
+    N = x.shape[-1]
+    dx = x.new_empty(x.shape) if want_dx else None
+    dgamma = x.new_empty(N, dtype=torch.float32) if want_dgamma else None
+    dbeta = x.new_empty(N, dtype=torch.float32) if want_dbeta else None
     if ws is None and (want_dgamma or want_dbeta):
-        ws = workspace(snn_layer_norm_grad_workspace(x.dtype, dy.dtype, mean.numel(), N), dev)
+        ws = workspace(snn_layer_norm_grad_workspace(x.dtype, dy.dtype, mean.numel(), N), x.device)
     snn_layer_norm_grad(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws)
     return dx, dgamma, dbeta
 
@@ -929,14 +930,13 @@ def linear_ce(x: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, weight=No
     if stream is not None:
         with torch.cuda.stream(stream):
             return linear_ce(x, W, targets, weight, want_grad, ws)
-    dev = x.device
     (H, C), R = W.shape, targets.numel()
-    loss = torch.empty(1, dtype=torch.float32, device=dev)
-    row_loss = torch.empty(targets.shape, dtype=torch.float32, device=dev)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if want_grad else None
-    dW = torch.empty((H, C), dtype=W.dtype, device=dev) if want_grad else None
+    loss = x.new_empty(1, dtype=torch.float32)
+    row_loss = x.new_empty(targets.shape, dtype=torch.float32)
+    dx = x.new_empty(x.shape) if want_grad else None
+    dW = W.new_empty((H, C)) if want_grad else None
     if ws is None:
-        ws = workspace(snn_linear_ce_workspace(x.dtype, R, H, C, want_grad), dev)
+        ws = workspace(snn_linear_ce_workspace(x.dtype, R, H, C, want_grad), x.device)
     snn_linear_ce(x, W, targets, weight, loss, row_loss, dx, dW, ws)
     return loss, row_loss, dx, dW
 
@@ -949,7 +949,7 @@ def leak_grad(x: torch.Tensor, alpha, shape, inp: Optional[Csr] = None, out: Opt
             return leak_grad(x, alpha, shape, inp, out, y)
     T, B, N = shape
     if y is None:
-        y = torch.empty(tuple(shape) if out is None else out.capacity, dtype=torch.float32, device=x.device)
+        y = x.new_empty(tuple(shape) if out is None else (out.capacity,), dtype=torch.float32)
     snn_leak_grad(x, inp, T, B, N, alpha, y, out)
     return y
 

@@ -363,8 +363,8 @@ __device__ __forceinline__ void mfma_term(int t, const uint4 (&a)[3], const uint
 
 // W's parts, zeros past its ends. For the first product [stage of 32 h][part][h / 8 % 4][class], 8 h of one class each; for
 // the second [stage of 32 h][part][32-class step][g][h], of one h the 8 classes 32 step + 4 g + v and 16 more.
-template <class T, int NT>
-__global__ __launch_bounds__(256) void ce_few_parts(const T* __restrict__ W, int64_t ld, int H, int C,
+template <int NT>
+__global__ __launch_bounds__(256) void ce_few_parts(const float* __restrict__ W, int64_t ld, int H, int C,
                                                     uint4* __restrict__ first, uint4* __restrict__ second) {
   constexpr int Cp = NT * 16, S = (NT + 1) / 2;
   const int stage = blockIdx.x;
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(256) void ce_few_parts(const T* __restrict__ W, int
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int h = stage * 32 + 8 * kc + u;
-        x[u] = h < H && c < C ? to_float(W[(int64_t)h * ld + c]) : 0.0f;
+        x[u] = h < H && c < C ? W[(int64_t)h * ld + c] : 0.0f;
       }
       split8(x, part);
 #pragma unroll
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(256) void ce_few_parts(const T* __restrict__ W, int
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int c = 32 * step + 16 * (u / 4) + 4 * g + u % 4;
-        x[u] = h < H && c < C ? to_float(W[(int64_t)h * ld + c]) : 0.0f;
+        x[u] = h < H && c < C ? W[(int64_t)h * ld + c] : 0.0f;
       }
       split8(x, part);
 #pragma unroll
@@ -395,13 +395,13 @@ __global__ __launch_bounds__(256) void ce_few_parts(const T* __restrict__ W, int
   }
 }
 
-template <class T, int NT, int RT, bool VEC>  // 16-class tiles, 16-row tiles of a wavefront; whether H is a multiple of 8
-__global__ __launch_bounds__(256, 2) void ce_few(const T* __restrict__ x, int64_t ld_x, const uint4* __restrict__ first,
+template <int NT, int RT, bool VEC>  // 16-class tiles, 16-row tiles of a wavefront; whether H is a multiple of 8
+__global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, int64_t ld_x, const uint4* __restrict__ first,
                                                  const uint4* __restrict__ second, int R, int H, int C,
                                                  const int32_t* __restrict__ targets, const float* __restrict__ weight,
                                                  const int32_t* __restrict__ counts, int n_counts,
                                                  float* __restrict__ row_loss, double* __restrict__ parts,
-                                                 T* __restrict__ dx, int64_t ld_dx, float* __restrict__ dz, int ld_dz,
+                                                 float* __restrict__ dx, int64_t ld_dx, float* __restrict__ dz, int ld_dz,
                                                  uint64_t* __restrict__ live) {
   constexpr int kRows = 64 * RT, Cp = NT * 16, S = (NT + 1) / 2;
   // pieces of a stage of W, two stages in LDS: lines [part][g] of its classes, or [part][step][g] of 32 h
@@ -443,30 +443,21 @@ __global__ __launch_bounds__(256, 2) void ce_few(const T* __restrict__ x, int64_
   };
   // A lane's part of a stage of x: 8 h of one row of each of its tiles, the second product operand as it stands. Past H
   // any of the row's values will do, since W is 0 there; rows that take no part have results that nothing uses.
-  const T* px[RT];
+  const float* px[RT];
 #pragma unroll
   for (int b = 0; b < RT; ++b) px[b] = x + (int64_t)min(r0 + 16 * (RT * w + b) + i, R - 1) * ld_x;
-  constexpr int kE = 16 / (int)sizeof(T);
-  Raw<T, kE> xs[RT][8 / kE];
   float xe[RT][8];
   const auto load_x = [&](int h0) {
 #pragma unroll
     for (int b = 0; b < RT; ++b) {
       if constexpr (VEC) {
 #pragma unroll
-        for (int q = 0; q < 8 / kE; ++q) __builtin_memcpy(xs[b][q].w, px[b] + min(h0 + 8 * g + kE * q, H - kE), 16);
+        for (int q = 0; q < 2; ++q) __builtin_memcpy(xe[b] + 4 * q, px[b] + min(h0 + 8 * g + 4 * q, H - 4), 16);
       } else {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) xe[b][u] = to_float(px[b][min(h0 + 8 * g + u, H - 1)]);
+        for (int u = 0; u < 8; ++u) xe[b][u] = px[b][min(h0 + 8 * g + u, H - 1)];
       }
     }
-  };
-  const auto split_x = [&](int b, uint4 (&part)[3]) {
-    if constexpr (VEC) {
-#pragma unroll
-      for (int q = 0; q < 8 / kE; ++q) xs[b][q].to(*reinterpret_cast<float(*)[kE]>(&xe[b][kE * q]));
-    }
-    split8(xe[b], part);
   };
   // every block begins at another stage: rows are often a power of two apart, and blocks at the same h would meet in the
   // same memory channels
@@ -478,7 +469,7 @@ __global__ __launch_bounds__(256, 2) void ce_few(const T* __restrict__ x, int64_
       at = at + 1 == stages ? 0 : at + 1;  // the stage after this one
       uint4 fb[RT][3];
 #pragma unroll
-      for (int b = 0; b < RT; ++b) split_x(b, fb[b]);
+      for (int b = 0; b < RT; ++b) split8(xe[b], fb[b]);
       gemm16::stage_barrier();  // this stage of W is there, the one before has been read
       if (n + 1 < stages) {
         load_w(first + (size_t)at * kW1, kW1, (n + 1) & 1);
@@ -601,15 +592,148 @@ __global__ __launch_bounds__(256, 2) void ce_few(const T* __restrict__ x, int64_
         float o[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) o[v] = mine ? (d[half][b][v] + e[half][b][v]) * (1.0f / kDzUp) * k[b] : 0.0f;
-        store_in<T, 4>(dx + (int64_t)r * ld_dx, min(h0 + 16 * half + 4 * g, H), H, o);
+        store_in<float, 4>(dx + (int64_t)r * ld_dx, min(h0 + 16 * half + 4 * g, H), H, o);
       }
     }
   }
 }
 
+// Few rows too (up to kFewDwRows): the float32 matrix cores, straight from memory, both products and all between in one
+// launch. A block takes 16 rows; its 16 wavefronts every sixteenth run of 16 h of the first product (their sums are added in
+// LDS, in order), a row each of what follows, and every sixteenth run of 16 h of dx. Bound: latency, and W read twice a block.
+constexpr int kFewDwRows = 4096;
+template <class T, int NT>
+__global__ __launch_bounds__(1024) void ce_small(const T* __restrict__ x, int64_t ld_x, const T* __restrict__ W, int64_t ld_w,
+                                                 int R, int H, int C, const int32_t* __restrict__ targets,
+                                                 const float* __restrict__ weight, float* __restrict__ row_loss,
+                                                 double* __restrict__ parts, T* __restrict__ dx, int64_t ld_dx,
+                                                 float* __restrict__ dz, int ld_dz, uint64_t* __restrict__ live) {
+  constexpr int Cp = NT * 16;
+  __shared__ float sum[16][Cp][17];  // of a wavefront: class, row
+  __shared__ float d[16][Cp + 4];    // row, class
+  __shared__ int count[16];
+  __shared__ double losses[16];
+  __shared__ bool on[16];
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), l = lane_id(), i = l % 16, g = l / 16;
+  const int r0 = blockIdx.x * 16;
+  int n = 0;
+  if (!weight)
+    for (int q = threadIdx.x; q < R; q += 1024) n += takes_part(targets, weight, q, C);
+  n = wave_sum_int(n);
+  if (l == 0) count[w] = n;
+  // lane (i, g) multiplies h0 + 4 g + s in step s: of row i of x, of class 16 a + i of W. W is 0 past its ends, so that past H
+  // any of the row's values will do
+  const T* px = x + (int64_t)min(r0 + i, R - 1) * ld_x;
+  f32x4 acc[NT];
+#pragma unroll
+  for (int a = 0; a < NT; ++a) acc[a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int h0 = 16 * w; h0 < H; h0 += 256) {
+    float xv[4], wv[4][NT];
+    if (h0 + 16 <= H) {
+      load<T, 4>(px + h0 + 4 * g, xv);
+    } else {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) xv[s] = to_float(px[min(h0 + 4 * g + s, H - 1)]);
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int a = 0; a < NT; ++a)
+        wv[s][a] = to_float(W[(int64_t)min(h0 + 4 * g + s, H - 1) * ld_w + min(16 * a + i, C - 1)]);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int a = 0; a < NT; ++a)
+        acc[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(h0 + 4 * g + s < H && 16 * a + i < C ? wv[s][a] : 0.0f, xv[s], acc[a],
+                                                      0, 0, 0);
+  }
+#pragma unroll
+  for (int a = 0; a < NT; ++a)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) sum[w][16 * a + 4 * g + v][i] = acc[a][v];
+  __syncthreads();
+  {  // row r0 + w, classes l and l + 64
+    const int r = r0 + w;
+    const bool mine = r < R && takes_part(targets, weight, r, C);
+    const int t = mine ? targets[r] : -1;
+    int takes = 0;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) takes += count[q];
+    const float k = !mine ? 0.0f : weight ? weight[r] : 1.0f / (float)takes;
+    constexpr int Q = (Cp + kWave - 1) / kWave;
+    float z[Q], m = -INFINITY, zt = 0.0f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int c = q * kWave + l;
+      z[q] = 0.0f;
+      if (c < Cp) {
+#pragma unroll
+        for (int p = 0; p < 16; ++p) z[q] += sum[p][c][w];
+      }
+      if (c < C) m = fmaxf(m, z[q]);  // a NaN is left to the sum
+      if (c == t) zt = z[q];
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+    zt = wave_sum(zt);
+    const float from = m > -INFINITY ? m : 0.0f;
+    float e = 0.0f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) e += q * kWave + l < C ? expf(z[q] - from) : 0.0f;
+    e = wave_sum(e);
+    const float log_sum = logf(e), lse = m + log_sum;
+    const float loss = mine ? (m - zt) + log_sum : 0.0f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int c = q * kWave + l;
+      const float v = mine && c < C ? k * (expf(z[q] - lse) - (c == t ? 1.0f : 0.0f)) : 0.0f;
+      if (c < Cp) d[w][c] = v;
+      if (dz && r < R && c < ld_dz) dz[(size_t)r * ld_dz + c] = v;
+    }
+    if (l == 0) {
+      on[w] = mine;
+      losses[w] = mine ? (double)k * (double)loss : 0.0;
+      if (r < R && row_loss) row_loss[r] = loss;
+    }
+  }
+  __syncthreads();
+  if (w == 0) {
+    const uint64_t bits = __ballot(l < 16 && on[i]);
+    if (l == 0) {
+      reinterpret_cast<uint16_t*>(live)[blockIdx.x] = (uint16_t)bits;
+      double s = 0.0;
+      for (int q = 0; q < 16; ++q) s += losses[q];
+      parts[blockIdx.x] = s;
+    }
+  }
+  if (!dx) return;
+  for (int h0 = 16 * w; h0 < H; h0 += 256) {  // lane (i, g): W's row h0 + i, dz of row i; then h0 + 4 g + v of row i
+    const T* pw = W + (int64_t)min(h0 + i, H - 1) * ld_w;
+    float wv[NT][4];
+#pragma unroll
+    for (int a = 0; a < NT; ++a) {
+      if (16 * a + 16 <= C) {
+        load<T, 4>(pw + 16 * a + 4 * g, wv[a]);
+      } else {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) wv[a][s] = to_float(pw[min(16 * a + 4 * g + s, C - 1)]);
+      }
+    }
+    f32x4 o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int a = 0; a < NT; ++a)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        o = __builtin_amdgcn_mfma_f32_16x16x4f32(wv[a][s], d[i][16 * a + 4 * g + s], o, 0, 0, 0);
+    float v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = on[i] ? o[u] : 0.0f;
+    if (r0 + i < R) store_in<T, 4>(dx + (int64_t)(r0 + i) * ld_dx, min(h0 + 4 * g, H), H, v);
+  }
+}
+
 // dW of few rows and classes: a block 16 h and all classes, its 16 wavefronts every sixteenth run of 16 rows, straight from
 // memory on the float32 matrix cores; their sums are added in LDS, in order. Block 0 also adds up the loss.
-constexpr int kFewDwRows = 4096;
 template <class T, int NT>
 __global__ __launch_bounds__(1024) void ce_few_dw(const T* __restrict__ x, int64_t ld_x, const float* __restrict__ dz,
                                                   int ld_dz, const uint64_t* __restrict__ live, int R, int H, int C,
@@ -693,7 +817,7 @@ Workspace carve(void* ws, int R, int H, bool few, bool grad, const Plan& p) {
   Workspace g;
   g.live = c.take<uint64_t>(((size_t)R + 63) / 64);
   g.counts = c.take<int32_t>(kCountParts);
-  const size_t stages = few ? (H + 31) / 32 : 0;
+  const size_t stages = few && R > kFewDwRows ? (H + 31) / 32 : 0;
   g.first = c.take<uint4>(stages * 12 * kFew);
   g.second = c.take<uint4>(stages * 12 * kFew);
   const size_t rows = few || p.pieces == 1 ? 0 : (size_t)R;
@@ -701,7 +825,7 @@ Workspace carve(void* ws, int R, int H, bool few, bool grad, const Plan& p) {
   g.sum = c.take<float>(rows);
   g.at_target = c.take<float>(rows);
   g.lse = c.take<float>(rows);
-  g.parts = c.take<double>(few ? (R + 63) / 64 : p.pieces == 1 ? R : kLossParts);
+  g.parts = c.take<double>(few ? (R + 15) / 16 : p.pieces == 1 ? R : kLossParts);
   g.z = c.take<float>(few && !grad ? 0 : (size_t)R * p.ld * (few ? 1 : p.z_slices));
   g.dX = c.take<float>(!few && grad && p.dx_slices > 1 ? (size_t)p.dx_slices * R * H : 0);
   g.dW = c.take<float>(grad && p.dw_slices > 1 ? (size_t)p.dw_slices * H * p.width : 0);
@@ -728,37 +852,36 @@ template <class T, int NT>
 void run_few(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int C, const int32_t* targets,
              const float* weight, float* loss, float* row_loss, T* dx, int64_t ld_dx, T* dW, int64_t ld_dw, const Plan& p,
              const Workspace& g, hipStream_t s) {
-  // 32 rows a wavefront read W's parts half as often; 16 where 32 would leave compute units without a block
-  const bool wide = (R + 127) / 128 >= 2 * cu_count(), vec = H % 8 == 0;
-  const int blocks = wide ? (R + 127) / 128 : (R + 63) / 64;
-  const int counted = weight || R <= kCountHere ? 0 : std::min(kCountParts, (R + 1023) / 1024);
-  if (counted)
-    hipLaunchKernelGGL(ce_live, dim3((unsigned)counted), dim3(256), 0, s, targets, weight, R, C, g.live, g.counts);
-  hipLaunchKernelGGL((ce_few_parts<T, NT>), dim3((unsigned)((H + 31) / 32)), dim3(256), 0, s, W, ld_w, H, C, g.first,
-                     g.second);
-  const auto few = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, x, ld_x, g.first, g.second, R, H, C, targets, weight,
-                       counted ? g.counts : nullptr, counted, row_loss, g.parts, dx, ld_dx, dW ? g.z : nullptr, p.ld,
-                       counted ? nullptr : g.live);
-  };
-  if constexpr (sizeof(T) == 4) {
-    if (wide) few(vec ? ce_few<T, NT, 2, true> : ce_few<T, NT, 2, false>);
-    else few(vec ? ce_few<T, NT, 1, true> : ce_few<T, NT, 1, false>);
-  } else {
-    few(vec ? ce_few<T, NT, 1, true> : ce_few<T, NT, 1, false>);  // at most kFewDwRows rows
-  }
-  if (dW && R <= kFewDwRows) {
-    hipLaunchKernelGGL((ce_few_dw<T, NT>), dim3((unsigned)((H + 15) / 16)), dim3(1024), 0, s, x, ld_x, g.z, p.ld, g.live, R,
-                       H, C, dW, ld_dw, g.parts, blocks, loss);
+  if (R <= kFewDwRows) {
+    const int blocks = (R + 15) / 16;
+    hipLaunchKernelGGL((ce_small<T, NT>), dim3((unsigned)blocks), dim3(1024), 0, s, x, ld_x, W, ld_w, R, H, C, targets, weight,
+                       row_loss, g.parts, dx, ld_dx, dW ? g.z : nullptr, p.ld, g.live);
+    if (dW)
+      hipLaunchKernelGGL((ce_few_dw<T, NT>), dim3((unsigned)((H + 15) / 16)), dim3(1024), 0, s, x, ld_x, g.z, p.ld, g.live, R,
+                         H, C, dW, ld_dw, g.parts, blocks, loss);
+    else
+      hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, blocks, loss);
     return;
   }
   if constexpr (sizeof(T) == 4) {
-    if (dW) {
-      enqueue_dw(x, ld_x, g.z, p.ld, R, H, C, dW, ld_dw, p, g, s, blocks, loss);
-      return;
-    }
+    // 32 rows a wavefront read W's parts half as often; 16 where 32 would leave compute units without a block
+    const bool wide = (R + 127) / 128 >= 2 * cu_count(), vec = H % 8 == 0;
+    const int blocks = wide ? (R + 127) / 128 : (R + 63) / 64;
+    const int counted = weight || R <= kCountHere ? 0 : std::min(kCountParts, (R + 1023) / 1024);
+    if (counted)
+      hipLaunchKernelGGL(ce_live, dim3((unsigned)counted), dim3(256), 0, s, targets, weight, R, C, g.live, g.counts);
+    hipLaunchKernelGGL((ce_few_parts<NT>), dim3((unsigned)((H + 31) / 32)), dim3(256), 0, s, W, ld_w, H, C, g.first,
+                       g.second);
+    const auto few = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, x, ld_x, g.first, g.second, R, H, C, targets,
+                         weight, counted ? g.counts : nullptr, counted, row_loss, g.parts, dx, ld_dx, dW ? g.z : nullptr,
+                         p.ld, counted ? nullptr : g.live);
+    };
+    if (wide) few(vec ? ce_few<NT, 2, true> : ce_few<NT, 2, false>);
+    else few(vec ? ce_few<NT, 1, true> : ce_few<NT, 1, false>);
+    if (dW) enqueue_dw(x, ld_x, g.z, p.ld, R, H, C, dW, ld_dw, p, g, s, blocks, loss);
+    else hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, blocks, loss);
   }
-  hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, blocks, loss);
 }
 
 template <class T>

@@ -601,7 +601,14 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
 // Few rows too (up to kFewDwRows): the float32 matrix cores, straight from memory, both products and all between in one
 // launch. A block takes 16 rows; its 16 wavefronts every sixteenth run of 16 h of the first product (their sums are added in
 // LDS, in order), a row each of what follows, and every sixteenth run of 16 h of dx. Bound: latency, and W read twice a block.
+// A lane reads V = 1, 2 or 4 neighbouring classes at once, which are one element each of V tiles: class m of tile a is
+// class_of(m) + a. The last lanes' begin early where the classes end, so that some classes are formed twice, alike.
 constexpr int kFewDwRows = 4096;
+template <int NT>
+constexpr int kV = NT < 4 ? NT : 4;
+template <int V>
+__device__ __forceinline__ int class_of(int group, int m, int C) { return min(16 * V * group + V * m, max(C - V, 0)); }
+
 template <class T, int NT>
 __global__ __launch_bounds__(1024) void ce_small(const T* __restrict__ x, int64_t ld_x, const T* __restrict__ W, int64_t ld_w,
                                                  int R, int H, int C, const int32_t* __restrict__ targets,
@@ -621,36 +628,37 @@ __global__ __launch_bounds__(1024) void ce_small(const T* __restrict__ x, int64_
     for (int q = threadIdx.x; q < R; q += 1024) n += takes_part(targets, weight, q, C);
   n = wave_sum_int(n);
   if (l == 0) count[w] = n;
-  // lane (i, g) multiplies h0 + 4 g + s in step s: of row i of x, of class 16 a + i of W. W is 0 past its ends, so that past H
-  // any of the row's values will do
+  // lane (i, g) multiplies h0 + 4 g + s in step s: of row i of x, of its classes of W
+  constexpr int V = kV<NT>;
+  int at[NT / V];
+#pragma unroll
+  for (int q = 0; q < NT / V; ++q) at[q] = class_of<V>(q, i, C);
   const T* px = x + (int64_t)min(r0 + i, R - 1) * ld_x;
   f32x4 acc[NT];
 #pragma unroll
   for (int a = 0; a < NT; ++a) acc[a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   for (int h0 = 16 * w; h0 < H; h0 += 256) {
-    float xv[4], wv[4][NT];
+    float xv[4], wv[4][NT / V][V];
     if (h0 + 16 <= H) {
       load<T, 4>(px + h0 + 4 * g, xv);
     } else {
 #pragma unroll
-      for (int s = 0; s < 4; ++s) xv[s] = to_float(px[min(h0 + 4 * g + s, H - 1)]);
+      for (int s = 0; s < 4; ++s) xv[s] = h0 + 4 * g + s < H ? to_float(px[h0 + 4 * g + s]) : 0.0f;
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
-      for (int a = 0; a < NT; ++a)
-        wv[s][a] = to_float(W[(int64_t)min(h0 + 4 * g + s, H - 1) * ld_w + min(16 * a + i, C - 1)]);
+      for (int q = 0; q < NT / V; ++q) load<T, V>(W + (int64_t)min(h0 + 4 * g + s, H - 1) * ld_w + at[q], wv[s][q]);
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int a = 0; a < NT; ++a)
-        acc[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(h0 + 4 * g + s < H && 16 * a + i < C ? wv[s][a] : 0.0f, xv[s], acc[a],
-                                                      0, 0, 0);
+        acc[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(wv[s][a / V][a % V], xv[s], acc[a], 0, 0, 0);
   }
 #pragma unroll
   for (int a = 0; a < NT; ++a)
 #pragma unroll
-    for (int v = 0; v < 4; ++v) sum[w][16 * a + 4 * g + v][i] = acc[a][v];
+    for (int v = 0; v < 4; ++v) sum[w][class_of<V>(a / V, 4 * g + v, C) + a % V][i] = acc[a][v];
   __syncthreads();
   {  // row r0 + w, classes l and l + 64
     const int r = r0 + w;
@@ -666,11 +674,11 @@ __global__ __launch_bounds__(1024) void ce_small(const T* __restrict__ x, int64_
     for (int q = 0; q < Q; ++q) {
       const int c = q * kWave + l;
       z[q] = 0.0f;
-      if (c < Cp) {
+      if (c < C) {
 #pragma unroll
         for (int p = 0; p < 16; ++p) z[q] += sum[p][c][w];
+        m = fmaxf(m, z[q]);  // a NaN is left to the sum
       }
-      if (c < C) m = fmaxf(m, z[q]);  // a NaN is left to the sum
       if (c == t) zt = z[q];
     }
 #pragma unroll
@@ -712,6 +720,7 @@ __global__ __launch_bounds__(1024) void ce_small(const T* __restrict__ x, int64_
     float wv[NT][4];
 #pragma unroll
     for (int a = 0; a < NT; ++a) {
+      if (16 * a >= C) break;
       if (16 * a + 16 <= C) {
         load<T, 4>(pw + 16 * a + 4 * g, wv[a]);
       } else {
@@ -721,10 +730,12 @@ __global__ __launch_bounds__(1024) void ce_small(const T* __restrict__ x, int64_
     }
     f32x4 o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int a = 0; a < NT; ++a)
+    for (int a = 0; a < NT; ++a) {
+      if (16 * a >= C) break;
 #pragma unroll
       for (int s = 0; s < 4; ++s)
         o = __builtin_amdgcn_mfma_f32_16x16x4f32(wv[a][s], d[i][16 * a + 4 * g + s], o, 0, 0, 0);
+    }
     float v[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) v[u] = on[i] ? o[u] : 0.0f;
@@ -732,47 +743,51 @@ __global__ __launch_bounds__(1024) void ce_small(const T* __restrict__ x, int64_
   }
 }
 
-// dW of few rows and classes: a block 16 h and all classes, its 16 wavefronts every sixteenth run of 16 rows, straight from
-// memory on the float32 matrix cores; their sums are added in LDS, in order. Block 0 also adds up the loss.
-template <class T, int NT>
+// dW of few rows and classes: a block 16 h and V tiles of classes, its 16 wavefronts every sixteenth run of 16 rows, straight
+// from memory on the float32 matrix cores; their sums are added in LDS, in order. The first block also adds up the loss. dz's
+// rows end in zeros at a multiple of 4.
+template <class T, int V>
 __global__ __launch_bounds__(1024) void ce_few_dw(const T* __restrict__ x, int64_t ld_x, const float* __restrict__ dz,
                                                   int ld_dz, const uint64_t* __restrict__ live, int R, int H, int C,
                                                   T* __restrict__ dW, int64_t ld_dw, const double* __restrict__ parts,
                                                   int n_parts, float* __restrict__ loss) {
-  __shared__ float sum[16][NT * 16][17];
+  __shared__ float sum[16][V * 16][17];  // of a wavefront: class, h
   const int w = threadIdx.x / kWave, l = lane_id(), i = l % 16, g = l / 16;
   const int h = blockIdx.x * 16 + i;
-  f32x4 acc[NT];
+  const int base = blockIdx.y * V * 16;
+  const int at = class_of<V>(blockIdx.y, i, ld_dz);
+  f32x4 acc[V];
 #pragma unroll
-  for (int a = 0; a < NT; ++a) acc[a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int a = 0; a < V; ++a) acc[a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   for (int r0 = 16 * w; r0 < R; r0 += 256) {
-    float b[4], d[4][NT];
+    float b[4], d[4][V];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = r0 + 4 * j + g;
-      const bool on = r < R && h < H && alive(live, r);
-      b[j] = on ? to_float(x[(int64_t)r * ld_x + h]) : 0.0f;
-#pragma unroll
-      for (int a = 0; a < NT; ++a) d[j][a] = r < R && 16 * a + i < ld_dz ? dz[(size_t)r * ld_dz + 16 * a + i] : 0.0f;
+      const int r = min(r0 + 4 * j + g, R - 1);
+      const bool on = r0 + 4 * j + g < R && alive(live, r);
+      b[j] = to_float(x[(int64_t)r * ld_x + min(h, H - 1)]);
+      if (!on) b[j] = 0.0f;
+      load<float, V>(dz + (size_t)r * ld_dz + at, d[j]);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int a = 0; a < NT; ++a) acc[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(d[j][a], b[j], acc[a], 0, 0, 0);
+      for (int a = 0; a < V; ++a) acc[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(d[j][a], b[j], acc[a], 0, 0, 0);
   }
 #pragma unroll
-  for (int a = 0; a < NT; ++a)
+  for (int a = 0; a < V; ++a)
 #pragma unroll
-    for (int v = 0; v < 4; ++v) sum[w][16 * a + 4 * g + v][i] = acc[a][v];
+    for (int v = 0; v < 4; ++v) sum[w][class_of<V>(blockIdx.y, 4 * g + v, ld_dz) + a - base][i] = acc[a][v];
   __syncthreads();
-  for (int q = threadIdx.x; q < 16 * NT * 16; q += 1024) {
-    const int c = q % (NT * 16), n = q / (NT * 16);
+  for (int q = threadIdx.x; q < 16 * V * 16; q += 1024) {
+    const int c = q % (V * 16), n = q / (V * 16);
+    if (base + c >= C || blockIdx.x * 16 + n >= H) continue;
     float s = 0.0f;
 #pragma unroll
     for (int k = 0; k < 16; ++k) s += sum[k][c][n];
-    if (c < C && blockIdx.x * 16 + n < H) dW[(int64_t)(blockIdx.x * 16 + n) * ld_dw + c] = from_float<T>(s);
+    dW[(int64_t)(blockIdx.x * 16 + n) * ld_dw + base + c] = from_float<T>(s);
   }
-  if (blockIdx.x == 0 && threadIdx.x < kWave) {
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < kWave) {
     double s = 0.0;
     for (int k = l; k < n_parts; k += kWave) s += parts[k];
 #pragma unroll
@@ -854,11 +869,12 @@ void run_few(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, i
              const Workspace& g, hipStream_t s) {
   if (R <= kFewDwRows) {
     const int blocks = (R + 15) / 16;
-    hipLaunchKernelGGL((ce_small<T, NT>), dim3((unsigned)blocks), dim3(1024), 0, s, x, ld_x, W, ld_w, R, H, C, targets, weight,
+    constexpr int N = NT == 7 ? 8 : NT, V = kV<N>;
+    hipLaunchKernelGGL((ce_small<T, N>), dim3((unsigned)blocks), dim3(1024), 0, s, x, ld_x, W, ld_w, R, H, C, targets, weight,
                        row_loss, g.parts, dx, ld_dx, dW ? g.z : nullptr, p.ld, g.live);
     if (dW)
-      hipLaunchKernelGGL((ce_few_dw<T, NT>), dim3((unsigned)((H + 15) / 16)), dim3(1024), 0, s, x, ld_x, g.z, p.ld, g.live, R,
-                         H, C, dW, ld_dw, g.parts, blocks, loss);
+      hipLaunchKernelGGL((ce_few_dw<T, V>), dim3((unsigned)((H + 15) / 16), N / V), dim3(1024), 0, s, x, ld_x, g.z, p.ld,
+                         g.live, R, H, C, dW, ld_dw, g.parts, blocks, loss);
     else
       hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, blocks, loss);
     return;

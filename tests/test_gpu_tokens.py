@@ -271,6 +271,16 @@ def test_linear_ce(dtype, R, H, C, pad, lead):
     assert torch.equal(row_loss, out[1]) and torch.equal(loss, out[0])
 
 
+# around every number of classes at which lanes take more of them at once, rows and columns that end inside a run of 16
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("C", [4, 15, 16, 17, 19, 31, 32, 33, 35, 61, 63, 65, 66, 95, 97, 111, 113, 127, 128, 129])
+def test_linear_ce_classes(dtype, C):
+    rng, x, W, t = ce_case(37, 41, C, dtype, C, 3, 1)
+    x[torch.from_numpy(t < 0).cuda()] = NAN
+    w = rng.random(37).astype(np.float32)
+    check_ce(x, W, t, w, snn.linear_ce(x, W, ints(t), torch.from_numpy(w).cuda()), dtype)
+
+
 # the widest rows: 128 and more classes, and few
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("C", [5, 130])

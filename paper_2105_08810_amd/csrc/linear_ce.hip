@@ -744,13 +744,13 @@ __global__ __launch_bounds__(1024) void ce_small(const T* __restrict__ x, int64_
 }
 
 // dW of few rows and classes: a block 16 h and V tiles of classes, its 16 wavefronts every sixteenth run of 16 rows, straight
-// from memory on the float32 matrix cores; their sums are added in LDS, in order. The first block also adds up the loss. dz's
-// rows end in zeros at a multiple of 4.
+// from memory on the float32 matrix cores; their sums are added in LDS, in order. Of more rows a block takes a slice, to
+// slices[slice][H][C]; else the first block also adds up the loss. dz's rows end in zeros at a multiple of 4.
 template <class T, int V>
 __global__ __launch_bounds__(1024) void ce_few_dw(const T* __restrict__ x, int64_t ld_x, const float* __restrict__ dz,
                                                   int ld_dz, const uint64_t* __restrict__ live, int R, int H, int C,
-                                                  T* __restrict__ dW, int64_t ld_dw, const double* __restrict__ parts,
-                                                  int n_parts, float* __restrict__ loss) {
+                                                  T* __restrict__ dW, int64_t ld_dw, float* __restrict__ slices,
+                                                  const double* __restrict__ parts, int n_parts, float* __restrict__ loss) {
   __shared__ float sum[16][V * 16][17];  // of a wavefront: class, h
   const int w = threadIdx.x / kWave, l = lane_id(), i = l % 16, g = l / 16;
   const int h = blockIdx.x * 16 + i;
@@ -759,11 +759,12 @@ __global__ __launch_bounds__(1024) void ce_few_dw(const T* __restrict__ x, int64
   f32x4 acc[V];
 #pragma unroll
   for (int a = 0; a < V; ++a) acc[a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int r0 = 16 * w; r0 < R; r0 += 256) {
+  const int per = ((R + 15) / 16 + gridDim.z - 1) / gridDim.z * 16, hi = min(R, ((int)blockIdx.z + 1) * per);
+  for (int r0 = blockIdx.z * per + 16 * w; r0 < hi; r0 += 256) {
     float b[4], d[4][V];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int r = min(r0 + 4 * j + g, R - 1);
+      const int r = min(r0 + 4 * j + g, R - 1);  // slices end at multiples of 16, or with the rows
       const bool on = r0 + 4 * j + g < R && alive(live, r);
       b[j] = to_float(x[(int64_t)r * ld_x + min(h, H - 1)]);
       if (!on) b[j] = 0.0f;
@@ -785,9 +786,11 @@ __global__ __launch_bounds__(1024) void ce_few_dw(const T* __restrict__ x, int64
     float s = 0.0f;
 #pragma unroll
     for (int k = 0; k < 16; ++k) s += sum[k][c][n];
-    dW[(int64_t)(blockIdx.x * 16 + n) * ld_dw + base + c] = from_float<T>(s);
+    const int at_h = blockIdx.x * 16 + n;
+    if (slices) slices[((size_t)blockIdx.z * H + at_h) * C + base + c] = s;
+    else dW[(int64_t)at_h * ld_dw + base + c] = from_float<T>(s);
   }
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < kWave) {
+  if (!slices && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < kWave) {
     double s = 0.0;
     for (int k = l; k < n_parts; k += kWave) s += parts[k];
 #pragma unroll
@@ -798,6 +801,15 @@ __global__ __launch_bounds__(1024) void ce_few_dw(const T* __restrict__ x, int64
 
 // Whether a call takes the way of few classes: in 16 bits only where its dW does, whose rows are multiplied in float32.
 bool few_of(int dtype, int R, int C) { return C <= kFew && (dtype == SNN_F32 || R <= kFewDwRows); }
+
+// Whether it also has few rows.
+bool few_rows(int R, int C) { return C <= kFew && R <= kFewDwRows; }
+
+// Whether dW of more rows is formed like that of few, a block a slice of them, and not as a product in tiles of 128 x 128, most
+// of which would lie past the classes. us a call, in tiles and so (rows x H x classes): 52460 x 681 x 9 187, 160; 13635 x
+// 261 x 39 64, 52; 130000 x 16 x 30 185, 49; 128000 x 1024 x 10 480, 469; but x 32 475, 499; 14649 x 2027 x 34 191, 207.
+constexpr int kSkinny = 64;
+bool skinny_of(int H, int C) { return C <= kSkinny && (int64_t)C * H < 32768; }
 
 struct Plan {
   int width, pieces;          // classes of a piece
@@ -811,7 +823,9 @@ Plan plan_of(int R, int H, int C) {
   p.pieces = (C + p.width - 1) / p.width;
   p.ld = (p.width + 3) / 4 * 4;
   p.z_slices = p.pieces == 1 && p.width <= kRowInRegs ? plan_splits(R, p.width, H, 88e12).splits : 1;
-  p.dw_slices = plan_splits(H, p.width, R, 88e12).splits;
+  p.dw_slices = few_rows(R, C)    ? 1
+                : skinny_of(H, C) ? std::max(2, std::min(64, 4 * cu_count() / ((H + 15) / 16)))
+                                  : plan_splits(H, p.width, R, 88e12).splits;
   p.dx_slices = plan_splits(R, H, p.width, 88e12).splits;
   return p;
 }
@@ -848,6 +862,13 @@ Workspace carve(void* ws, int R, int H, bool few, bool grad, const Plan& p) {
   return g;
 }
 
+// n columns of dW from their K slices. With loss also that, from n_parts parts.
+void enqueue_dw_sum(int n, int H, float* dW, int64_t ld_dw, const Plan& p, const Workspace& g, hipStream_t s, int n_parts,
+                    float* loss) {
+  hipLaunchKernelGGL(ce_dw, dim3((unsigned)std::min<int64_t>(((int64_t)H * n + 255) / 256, 8 * cu_count())), dim3(256), 0, s,
+                     g.dW, p.dw_slices, H, n, dW, ld_dw, g.parts, n_parts, loss);
+}
+
 // A piece's columns of dW (n of them) from its dz, in K slices where the product alone has few tiles. With loss also that,
 // from n_parts parts.
 void enqueue_dw(const float* x, int64_t ld_x, const float* dz, int ld_dz, int R, int H, int n, float* dW, int64_t ld_dw,
@@ -859,22 +880,21 @@ void enqueue_dw(const float* x, int64_t ld_x, const float* dz, int ld_dz, int R,
     return;
   }
   gemm_split_km(H, n, R, x, (int)ld_x, dz, ld_dz, g.dW, n, p.dw_slices, (size_t)H * n, s, live);
-  hipLaunchKernelGGL(ce_dw, dim3((unsigned)std::min<int64_t>(((int64_t)H * n + 255) / 256, 8 * cu_count())), dim3(256), 0, s,
-                     g.dW, p.dw_slices, H, n, dW, ld_dw, g.parts, n_parts, loss);
+  enqueue_dw_sum(n, H, dW, ld_dw, p, g, s, n_parts, loss);
 }
 
 template <class T, int NT>
 void run_few(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int C, const int32_t* targets,
              const float* weight, float* loss, float* row_loss, T* dx, int64_t ld_dx, T* dW, int64_t ld_dw, const Plan& p,
              const Workspace& g, hipStream_t s) {
-  if (R <= kFewDwRows) {
+  if (few_rows(R, C)) {
     const int blocks = (R + 15) / 16;
     constexpr int N = NT == 7 ? 8 : NT, V = kV<N>;
     hipLaunchKernelGGL((ce_small<T, N>), dim3((unsigned)blocks), dim3(1024), 0, s, x, ld_x, W, ld_w, R, H, C, targets, weight,
                        row_loss, g.parts, dx, ld_dx, dW ? g.z : nullptr, p.ld, g.live);
     if (dW)
       hipLaunchKernelGGL((ce_few_dw<T, V>), dim3((unsigned)((H + 15) / 16), N / V), dim3(1024), 0, s, x, ld_x, g.z, p.ld,
-                         g.live, R, H, C, dW, ld_dw, g.parts, blocks, loss);
+                         g.live, R, H, C, dW, ld_dw, nullptr, g.parts, blocks, loss);
     else
       hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, blocks, loss);
     return;
@@ -895,6 +915,14 @@ void run_few(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, i
     };
     if (wide) few(vec ? ce_few<NT, 2, true> : ce_few<NT, 2, false>);
     else few(vec ? ce_few<NT, 1, true> : ce_few<NT, 1, false>);
+    if constexpr (NT <= kSkinny / 16) {
+      if (dW && skinny_of(H, C)) {
+        hipLaunchKernelGGL((ce_few_dw<T, NT>), dim3((unsigned)((H + 15) / 16), 1, (unsigned)p.dw_slices), dim3(1024), 0, s, x,
+                           ld_x, g.z, p.ld, g.live, R, H, C, dW, ld_dw, g.dW, g.parts, blocks, loss);
+        enqueue_dw_sum(C, H, dW, ld_dw, p, g, s, blocks, loss);
+        return;
+      }
+    }
     if (dW) enqueue_dw(x, ld_x, g.z, p.ld, R, H, C, dW, ld_dw, p, g, s, blocks, loss);
     else hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, blocks, loss);
   }

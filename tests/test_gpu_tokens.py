@@ -271,6 +271,19 @@ def test_linear_ce(dtype, R, H, C, pad, lead):
     assert torch.equal(row_loss, out[1]) and torch.equal(loss, out[0])
 
 
+# few classes of more rows: dW in slices of the rows, of a number that divides them and not
+@pytest.mark.parametrize("R,H,C", [(4097, 7, 3), (5000, 33, 17), (9001, 20, 40), (4500, 300, 64), (4111, 600, 60)])
+def test_linear_ce_slices(R, H, C):
+    rng, x, W, t = ce_case(R, H, C, "f32", R, 3, 1)
+    x[torch.from_numpy(t < 0).cuda()] = NAN
+    out = snn.linear_ce(x, W, ints(t))
+    check_ce(x, W, t, None, out, "f32")
+    ws, behind = poisoned(snn.snn_linear_ce_workspace(x.dtype, R, H, C, True))
+    assert all(torch.equal(p, q) for p, q in zip(snn.linear_ce(x, W, ints(t), ws=ws), out)) and bool((behind == 255).all())
+    loss, *_ = snn.linear_ce(x, W, ints(t), want_grad=False)
+    assert torch.equal(loss, out[0])
+
+
 # around every number of classes at which lanes take more of them at once, rows and columns that end inside a run of 16
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("C", [4, 15, 16, 17, 19, 31, 32, 33, 35, 61, 63, 65, 66, 95, 97, 111, 113, 127, 128, 129])

@@ -652,9 +652,10 @@ snn_status snn_layer_norm_grad(const void* dy, int y_dtype, int64_t ld_dy, const
  *   row_loss float32 [R] (written unless NULL): L_r
  *   dx       R rows of H values of dtype (written unless NULL): weight_r (softmax(z_r) - onehot) W^T
  *   dW       H rows of C values of dtype (written unless NULL): x^T (weight_r (softmax(z_r) - onehot))
- * In 16 bits weight_r (softmax(z_r) - onehot) is rounded to dtype as a share of the largest weight, and shares below
- * 2^-126 (bfloat16) or 2^-40 (float16) of it count as 0. In float32 with at most 128 classes values of W from 2^97 on
- * overflow in dx. What is not finite in x may make its row's loss and gradients NaN, in W every row's.
+ * In 16 bits (but for at most 128 classes and 4096 rows) weight_r (softmax(z_r) - onehot) is rounded to dtype as a share
+ * of the largest weight, and shares below 2^-126 (bfloat16) or 2^-40 (float16) of it count as 0. In float32 with at most
+ * 128 classes and more than 4096 rows values of W from 2^97 on overflow in dx. What is not finite in x may make its row's
+ * loss and gradients NaN, in W every row's.
  * R up to 2^24, H up to 2^16, C up to 2^20, distances of rows up to 2^31 - 1; larger: SNN_ERR_UNSUPPORTED. The workspace
  * query takes whether a gradient is wanted. The workspace grows with R H, with R times a piece of the classes (bounded)
  * and in 16 bits with R C / 8 bytes.

@@ -319,8 +319,8 @@ __global__ __launch_bounds__(256) void ce_dw(const float* __restrict__ part, int
   }
 }
 
-// Few classes (up to kFew): everything of a row but dW in one launch. A block of four wavefronts takes 64 RT rows, a
-// wavefront 16 RT of them and all classes, on the bf16 matrix cores with both operands in three parts (h + m + l, the six
+// Few classes (up to kFew) of many float32 rows: everything of a row but dW in one launch. A block of four wavefronts takes
+// 64 RT rows, a wavefront 16 RT of them and all classes, on the bf16 matrix cores with both operands in three parts (h + m + l, the six
 // products down to 2^-16 of the leading one; values below 2^-110 lose some of their last bits, one of 2^128 - 2^119 and more
 // counts as infinite). m is the class and n the row, so the accumulators hold every class of a row in four lanes:
 // log-sum-exp, loss and dz are formed there, and, as a lane has four neighbouring classes of one row, its dz are the second
@@ -799,7 +799,7 @@ __global__ __launch_bounds__(1024) void ce_few_dw(const T* __restrict__ x, int64
   }
 }
 
-// Whether a call takes the way of few classes: in 16 bits only where its dW does, whose rows are multiplied in float32.
+// Whether a call takes a way of few classes: in 16 bits only that of few rows, which multiplies in float32.
 bool few_of(int dtype, int R, int C) { return C <= kFew && (dtype == SNN_F32 || R <= kFewDwRows); }
 
 // Whether it also has few rows.

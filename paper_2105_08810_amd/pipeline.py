@@ -251,11 +251,12 @@ class Network(ReadoutRows):
         return top
 
     def membrane(self) -> torch.Tensor:
-        """V_out of the last forward; with a target at every step it is formed now, from that forward's spikes and W_out
-        as it is now."""
-        if self.V_out is None:
-            if not self.S:
-                raise ValueError("membrane() reads a forward's spikes: call forward() first")
+        """V_out of the last forward; with a target at every step it is formed at each call, from the spikes and W_out as
+        they are now: a graph's replay renews the spikes without any of this class's code, so no earlier V_out is
+        handed out again."""
+        if not self.S:
+            raise ValueError("membrane() reads a forward's spikes: call forward() first")
+        if self.every_step:
             T, B, C = self.T, self.B, self.W_out.shape[1]
             self.V_out = torch.empty((T, B, C), dtype=torch.float32, device=self.X.device)
             S_out = torch.empty((T, B, C), dtype=torch.uint8, device=self.X.device)

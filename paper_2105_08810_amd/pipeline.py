@@ -139,7 +139,7 @@ class Network(ReadoutRows):
     _every: Optional[snn.Csr] = None  # CSR of every entry of V_out (readout_distilled)
     _embedded: Optional[torch.Tensor] = None  # the picked rows before norm_in, its means and 1 / deviations
     _norm_stats: Optional[tuple] = None
-    norm_grads: Optional[List[torch.Tensor]] = None  # of norm_in's gamma and beta, from the last sparse_backward
+    norm_grads: Optional[List[torch.Tensor]] = None  # of norm_in's gamma and beta: buffers that each backward rewrites
 
     def __post_init__(self):
         if self.norm_in is not None and not self.tokens:
@@ -186,9 +186,14 @@ class Network(ReadoutRows):
         if not self.every_step:
             self.V_out = torch.empty((T, B, C), dtype=torch.float32, device=dev)
             self.S_out = torch.empty((T, B, C), dtype=torch.uint8, device=dev)
-        self._embedded = self._norm_stats = None
+        # norm_in's state and gradients lie in buffers as V does: a graph's replay rewrites them, and what reads them next
+        # need not have been captured
+        self._embedded = self._norm_stats = self.norm_grads = None
         if self.norm_in is not None:
-            self._embedded = torch.empty((max(T - 1, 1), B, sizes[1]), dtype=torch.float32, device=dev)
+            rows = (max(T - 1, 1), B)
+            self._embedded = torch.empty((*rows, sizes[1]), dtype=torch.float32, device=dev)
+            self._norm_stats = tuple(torch.empty(rows, dtype=torch.float32, device=dev) for _ in range(2))
+            self.norm_grads = list(torch.zeros((2, sizes[1]), dtype=torch.float32, device=dev))
         self.trace_out = torch.empty((T, B, sizes[-1]), dtype=torch.float32, device=dev)
         self.bits, self.bits_bth = [], None  # made by a forward with b_th
         self._every = None
@@ -243,8 +248,7 @@ class Network(ReadoutRows):
             else:
                 n = self.norm_in
                 snn.embed(E, self.X[:-1], self.embed_scale, out=self._embedded)
-                _, mean, rstd = snn.layer_norm(self._embedded, n.gamma, n.beta, n.eps, out=V[1:])
-                self._norm_stats = (mean, rstd)
+                snn.snn_layer_norm(self._embedded, n.gamma, n.beta, n.eps, V[1:], *self._norm_stats)
         top = self.trace_out if self.L == 1 else None
         snn.snn_lif_forward_currents(V, T, B, E.shape[1], self.alphas[0], self.theta, 0.0 if b_th is None else b_th,
                                      self.S[0], top, self.alpha_out, None if b_th is None else self.bits[0])
@@ -332,12 +336,15 @@ class Network(ReadoutRows):
         T, B, (V, N) = self.T, self.B, self.Ws[0].shape
         dev = self.X.device
         if T == 1:  # no current reaches a membrane
-            self.norm_grads = None if self.norm_in is None else [torch.zeros(N, device=dev) for _ in range(2)]
+            for g in self.norm_grads or []:
+                g.zero_()
             return torch.zeros((V, N), device=dev)
         d = snn.leak_grad(eps, self.alphas[0], (T, B, N), inp=csr)[:-1]
         if self.norm_in is not None:
-            d, dgamma, dbeta = snn.layer_norm_grad(d, self._embedded, self.norm_in.gamma, *self._norm_stats)
-            self.norm_grads = [dgamma, dbeta]
+            dy, x = d, self._embedded
+            d = torch.empty_like(x)
+            ws = snn.workspace(snn.snn_layer_norm_grad_workspace(x.dtype, dy.dtype, (T - 1) * B, N), dev)
+            snn.snn_layer_norm_grad(dy, x, self.norm_in.gamma, *self._norm_stats, d, *self.norm_grads, ws)
         return snn.embed_grad(self.X[:-1], d, V, self.embed_scale)
 
     def _sparse_backward_pipelined(self, csrs, ro_csr, ro_eps, aux, reg_coefs=None):
@@ -476,7 +483,9 @@ class Network(ReadoutRows):
             dWs, dW_out, _ = self.dense_backward(b_th, ro, reg_coefs=coefs)
             nnz = None
         mark(4)
-        grads = list(dWs) + [dW_out] + (self.norm_grads if self.norm_in is not None else [])
+        grads = list(dWs) + [dW_out]
+        if self.norm_in is not None:  # this step's own, as the others are
+            grads += list(torch.stack(self.norm_grads))
         opt.step(grads)
         mark(5)
         if acts:

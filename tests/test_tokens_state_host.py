@@ -31,3 +31,35 @@ def test_membrane_is_formed_at_each_call(monkeypatch):
     net.W_out[0, 0] = 1.0  # as an optimizer's step does
     assert bool((net.membrane() == 103).all())
     assert not first.any() and len(calls) == 3
+
+
+def test_norm_state_is_in_buffers(monkeypatch):
+    """The norm's means and deviations, and its gradients, are where a replay of an earlier capture writes them: the same
+    tensors in every forward and backward."""
+    seen = {"forward": [], "backward": []}
+    monkeypatch.setattr(snn, "embed", lambda *a, out=None, **k: out)
+    monkeypatch.setattr(snn, "layer_norm", lambda x, *a, out=None, **k: seen["forward"].append(
+        (torch.empty(x.shape[:-1]), torch.empty(x.shape[:-1]))) or (out, *seen["forward"][-1]))
+    monkeypatch.setattr(snn, "snn_layer_norm", lambda x, g, b, e, y, mean, rstd, **k: seen["forward"].append((mean, rstd)))
+    monkeypatch.setattr(snn, "snn_lif_forward_currents", lambda *a, **k: None)
+    net = network(norm=True)
+    net.forward()
+    net.forward()
+    for mean, rstd in seen["forward"]:
+        assert mean.data_ptr() == seen["forward"][0][0].data_ptr() and rstd.data_ptr() == seen["forward"][0][1].data_ptr()
+
+    def grad(dy, x, gamma, mean, rstd, *a, **k):
+        seen["backward"].append((mean.data_ptr(), rstd.data_ptr()))
+        return torch.empty_like(x), torch.empty(5), torch.empty(5)
+
+    monkeypatch.setattr(snn, "leak_grad", lambda eps, alpha, shape, **k: torch.zeros(shape))
+    monkeypatch.setattr(snn, "layer_norm_grad", grad)
+    monkeypatch.setattr(snn, "snn_layer_norm_grad", grad)
+    monkeypatch.setattr(snn, "snn_layer_norm_grad_workspace", lambda *a: 1)
+    monkeypatch.setattr(snn, "embed_grad", lambda ids, d, V, scale: torch.zeros((V, d.shape[-1])))
+    net._backward_tokens(None, None)
+    first = [g.data_ptr() for g in net.norm_grads]
+    keep = net.norm_grads  # its memory is not handed out again
+    net._backward_tokens(None, None)
+    assert [g.data_ptr() for g in net.norm_grads] == first and keep is not None
+    assert all(p == tuple(t.data_ptr() for t in seen["forward"][0]) for p in seen["backward"])

@@ -3,6 +3,11 @@
 //   z = x W  [R,C],  lse_r = log sum_c exp z_rc,  L_r = lse_r - z_r,target,  loss = sum_r w_r L_r
 //   dz_rc = w_r (exp(z_rc - lse_r) - [c = target_r]),  dx = dz W^T,  dW = x^T dz
 //
+// With m_r the largest logit and o_r = sum over c != target of exp(z_rc - m_r), e_r = exp(z_r,target - m_r), s_r = o_r + e_r:
+// dz_rc = w_r exp(z_rc - m_r) / s_r, dz_r,target = -w_r o_r / s_r, and L_r = log(1 + o_r) where the target is the largest. So
+// nothing is rounded at the size of the logits, and no 1 is taken from a probability near 1: exp(z - lse) - 1 with lse in
+// float32 was 0.07% off for rows of 99.96% at logits near 0, 76% at logits near 300.
+//
 // The logits of all classes are never in memory together: the classes are taken in pieces, each piece's logits are formed,
 // give their share of every row's sum of exponentials and are dropped; with the rows' lse known a piece's logits are formed
 // again (unless there is one piece) and turned into its columns of dz, from which its share of dx and its columns of dW
@@ -55,7 +60,17 @@ __device__ __forceinline__ float same_weight(const int32_t* __restrict__ parts, 
   return s > 0 ? 1.0f / (float)s : 0.0f;
 }
 
-// A piece's share of every row's largest logit and sum of exponentials, and the target's logit.
+// A row's loss and 1 / s from its largest logit m, the sum o over the other classes and the target's logit.
+__device__ __forceinline__ float finish_row(float m, float o, float zt, float& inv) {
+  const float from = m > -INFINITY ? m : 0.0f;
+  const float s = o + expf(zt - from);
+  inv = 1.0f / s;
+  // a row of infinities is NaN, as s is
+  return zt == m && fabsf(m) < INFINITY ? log1pf(o) : (m - zt) + logf(s);
+}
+
+// A piece's share of every row's largest logit and sum of exponentials of classes that are not the target, and the target's
+// logit.
 __global__ __launch_bounds__(kWaves * kWave) void ce_sums(const float* __restrict__ z, int R, int n, int ld, int c0,
                                                           const int32_t* __restrict__ targets,
                                                           const uint64_t* __restrict__ live, float* __restrict__ top,
@@ -69,8 +84,9 @@ __global__ __launch_bounds__(kWaves * kWave) void ce_sums(const float* __restric
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
   const float ref = m > -INFINITY ? m : 0.0f;
+  const int t = targets[r] - c0;
   float s = 0.0f;
-  for (int i = l; i < n; i += kWave) s += expf(row[i] - ref);
+  for (int i = l; i < n; i += kWave) s += i == t ? 0.0f : expf(row[i] - ref);
   s = wave_sum(s);
   if (l == 0) {
     if (c0 > 0) {
@@ -81,7 +97,6 @@ __global__ __launch_bounds__(kWaves * kWave) void ce_sums(const float* __restric
     }
     top[r] = m;
     sum[r] = s;
-    const int t = targets[r] - c0;
     if (t >= 0 && t < n) at_target[r] = row[t];
   }
 }
@@ -152,7 +167,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ce_rows(float* __restrict__
     float* row = z + (size_t)r * ld;
     const bool on = alive(live, r);
     const float k = !on ? 0.0f : weight ? weight[r] : same;
-    float loss = 0.0f, lse = 0.0f;
+    float loss = 0.0f, from = 0.0f, inv = 0.0f, rest = 0.0f;  // rest: the others' sum over all
     const int t = on ? targets[r] : -1;
     float4 held[Q > 0 ? Q : 1];
     const auto each = [&](auto f) {
@@ -191,18 +206,17 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ce_rows(float* __restrict__
         if (i + 3 < n) m = fmaxf(m, q.w);
       });
       m = row_reduce<L>(m, false, red);
-      const float from = m > -INFINITY ? m : 0.0f;
-      float s = 0.0f;
+      from = m > -INFINITY ? m : 0.0f;
+      float o = 0.0f;
       each([&](int i, const float4& q) {
-        s += expf(q.x - from);
-        if (i + 1 < n) s += expf(q.y - from);
-        if (i + 2 < n) s += expf(q.z - from);
-        if (i + 3 < n) s += expf(q.w - from);
+        const float p[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (i + u < n && i + u != t) o += expf(p[u] - from);
       });
-      s = row_reduce<L>(s, true, red);  // every thread has read row[t]
-      const float log_sum = logf(s);
-      lse = m + log_sum;
-      loss = (m - zt) + log_sum;
+      o = row_reduce<L>(o, true, red);  // every thread has read row[t]
+      loss = finish_row(m, o, zt, inv);
+      rest = o * inv;
       weighted += (double)k * (double)loss;
     }
     if (l == 0 && row_loss) row_loss[r] = loss;
@@ -212,7 +226,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ce_rows(float* __restrict__
         const float p[4] = {q.x, q.y, q.z, q.w};
         float d[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) d[u] = on ? k * (expf(p[u] - lse) - (i + u == t ? 1.0f : 0.0f)) : 0.0f;
+        for (int u = 0; u < 4; ++u) d[u] = on ? k * (i + u == t ? -rest : expf(p[u] - from) * inv) : 0.0f;
         *reinterpret_cast<float4*>(row + i) = make_float4(d[0], d[1], d[2], d[3]);  // the row's own padding past n
       };
       if (on) each(store);
@@ -267,20 +281,18 @@ __global__ __launch_bounds__(kWaves * kWave) void ce_dx(const float* __restrict_
   if (w == 0 && i < H) dx[(int64_t)r * ld + i] = (s + all[1][l]) + (all[2][l] + all[3][l]);
 }
 
-// Each row's log-sum-exp and loss; the weighted losses of a block in float64.
+// Each row's 1 / s and loss; the weighted losses of a block in float64.
 __global__ __launch_bounds__(256) void ce_losses(int R, const uint64_t* __restrict__ live, const int32_t* __restrict__ counts,
                                                  int n_counts, const float* __restrict__ weight,
                                                  const float* __restrict__ top, const float* __restrict__ sum,
-                                                 const float* __restrict__ at_target, float* __restrict__ lse,
+                                                 const float* __restrict__ at_target, float* __restrict__ inv,
                                                  float* __restrict__ row_loss, double* __restrict__ parts) {
   const float same = weight ? 0.0f : same_weight(counts, n_counts);
   double s = 0.0;
   for (int r = blockIdx.x * 256 + threadIdx.x; r < R; r += gridDim.x * 256) {
     float loss = 0.0f;
     if (alive(live, r)) {
-      const float log_sum = logf(sum[r]);
-      lse[r] = top[r] + log_sum;
-      loss = (top[r] - at_target[r]) + log_sum;
+      loss = finish_row(top[r], sum[r], at_target[r], inv[r]);
       s += (double)(weight ? weight[r] : same) * (double)loss;
     }
     if (row_loss) row_loss[r] = loss;
@@ -294,14 +306,17 @@ __global__ __launch_bounds__(kWaves * kWave) void ce_dz(float* __restrict__ z, i
                                                         const int32_t* __restrict__ targets,
                                                         const uint64_t* __restrict__ live,
                                                         const int32_t* __restrict__ counts, int n_counts,
-                                                        const float* __restrict__ weight, const float* __restrict__ lse) {
+                                                        const float* __restrict__ weight, const float* __restrict__ top,
+                                                        const float* __restrict__ sum, const float* __restrict__ inv) {
   const int r = blockIdx.x * kWaves + threadIdx.x / kWave;
   if (r >= R) return;
   float* row = z + (size_t)r * ld;
   const bool on = alive(live, r);
-  const float k = weight ? weight[r] : same_weight(counts, n_counts), ref = on ? lse[r] : 0.0f;
+  const float k = weight ? weight[r] : same_weight(counts, n_counts);
+  const float m = on ? top[r] : 0.0f, from = m > -INFINITY ? m : 0.0f, over = on ? inv[r] : 0.0f;
+  const float rest = on ? sum[r] * over : 0.0f;
   const int t = targets[r] - c0;
-  for (int i = lane_id(); i < n; i += kWave) row[i] = on ? k * (expf(row[i] - ref) - (i == t ? 1.0f : 0.0f)) : 0.0f;
+  for (int i = lane_id(); i < n; i += kWave) row[i] = on ? k * (i == t ? -rest : expf(row[i] - from) * over) : 0.0f;
 }
 
 // A piece's columns of dW from its K slices, summed in order, 16 under way (64 slices of 1024 x 100: 21 us -> 7). With loss
@@ -518,15 +533,19 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
     zt += __shfl_xor(zt, 16, kWave);
     zt += __shfl_xor(zt, 32, kWave);
     const float from = m > -INFINITY ? m : 0.0f;
-    float s = 0.0f;
+    float o = 0.0f;
 #pragma unroll
     for (int a = 0; a < NT; ++a)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) s += 16 * a + 4 * g + v < C ? expf(lead[a][b][v] - from) : 0.0f;
-    s += __shfl_xor(s, 16, kWave);
-    s += __shfl_xor(s, 32, kWave);
-    const float log_sum = logf(s), lse = m + log_sum;
-    const float loss = mine ? (m - zt) + log_sum : 0.0f;
+      for (int v = 0; v < 4; ++v) {
+        const int c = 16 * a + 4 * g + v;
+        o += c < C && c != t ? expf(lead[a][b][v] - from) : 0.0f;
+      }
+    o += __shfl_xor(o, 16, kWave);
+    o += __shfl_xor(o, 32, kWave);
+    float inv;
+    const float of_row = finish_row(m, o, zt, inv), rest_of = o * inv;
+    const float loss = mine ? of_row : 0.0f;
     k[b] = mine ? (weight ? weight[r] : same) : 0.0f;
     if (g == 0 && r < R && row_loss) row_loss[r] = loss;
     if (g == 0 && mine) total += (double)k[b] * (double)loss;
@@ -537,7 +556,8 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int a = 2 * step + u / 4, c = 16 * a + 4 * g + u % 4;
-        d[u] = a < NT && mine && c < C ? expf(lead[a < NT ? a : 0][b][u % 4] - lse) - (c == t ? 1.0f : 0.0f) : 0.0f;
+        const float share = c == t ? -rest_of : expf(lead[a < NT ? a : 0][b][u % 4] - from) * inv;
+        d[u] = a < NT && mine && c < C ? share : 0.0f;
       }
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
@@ -685,16 +705,17 @@ __global__ __launch_bounds__(1024) void ce_small(const T* __restrict__ x, int64_
     for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
     zt = wave_sum(zt);
     const float from = m > -INFINITY ? m : 0.0f;
-    float e = 0.0f;
+    float o = 0.0f;
 #pragma unroll
-    for (int q = 0; q < Q; ++q) e += q * kWave + l < C ? expf(z[q] - from) : 0.0f;
-    e = wave_sum(e);
-    const float log_sum = logf(e), lse = m + log_sum;
-    const float loss = mine ? (m - zt) + log_sum : 0.0f;
+    for (int q = 0; q < Q; ++q) o += q * kWave + l < C && q * kWave + l != t ? expf(z[q] - from) : 0.0f;
+    o = wave_sum(o);
+    float inv;
+    const float of_row = finish_row(m, o, zt, inv), rest = o * inv;
+    const float loss = mine ? of_row : 0.0f;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       const int c = q * kWave + l;
-      const float v = mine && c < C ? k * (expf(z[q] - lse) - (c == t ? 1.0f : 0.0f)) : 0.0f;
+      const float v = mine && c < C ? k * (c == t ? -rest : expf(z[q] - from) * inv) : 0.0f;
       if (c < Cp) d[w][c] = v;
       if (dz && r < R && c < ld_dz) dz[(size_t)r * ld_dz + c] = v;
     }
@@ -836,7 +857,7 @@ struct Workspace {
   uint64_t* live;
   int32_t* counts;
   uint4 *first, *second;
-  float *z, *dX, *dW, *top, *sum, *at_target, *lse;
+  float *z, *dX, *dW, *top, *sum, *at_target, *inv;
   double* parts;
   size_t bytes;
 };
@@ -853,7 +874,7 @@ Workspace carve(void* ws, int R, int H, bool few, bool grad, const Plan& p) {
   g.top = c.take<float>(rows);
   g.sum = c.take<float>(rows);
   g.at_target = c.take<float>(rows);
-  g.lse = c.take<float>(rows);
+  g.inv = c.take<float>(rows);
   g.parts = c.take<double>(few ? (R + 15) / 16 : p.pieces == 1 ? R : kLossParts);
   g.z = c.take<float>(few && !grad ? 0 : (size_t)R * p.ld * (few ? 1 : p.z_slices));
   g.dX = c.take<float>(!few && grad && p.dx_slices > 1 ? (size_t)p.dx_slices * R * H : 0);
@@ -977,7 +998,7 @@ void run(const float* x, int64_t ld_x, const float* W, int64_t ld_w, int R, int 
     }
     n_parts = std::min(kLossParts, (R + 255) / 256);
     hipLaunchKernelGGL(ce_losses, dim3((unsigned)n_parts), dim3(256), 0, s, R, g.live, g.counts, counted, weight, g.top,
-                       g.sum, g.at_target, g.lse, row_loss, g.parts);
+                       g.sum, g.at_target, g.inv, row_loss, g.parts);
   }
   float* to = p.dx_slices > 1 ? g.dX : dx;
   const int ld_to = p.dx_slices > 1 ? H : (int)ld_dx;
@@ -985,7 +1006,8 @@ void run(const float* x, int64_t ld_x, const float* W, int64_t ld_w, int R, int 
     const int n = std::min(p.width, C - c0);
     if (p.pieces > 1) {
       gemm_split_kr(R, n, H, x, (int)ld_x, W + c0, (int)ld_w, g.z, p.ld, s);
-      hipLaunchKernelGGL(ce_dz, rows, waves, 0, s, g.z, R, n, p.ld, c0, targets, g.live, g.counts, counted, weight, g.lse);
+      hipLaunchKernelGGL(ce_dz, rows, waves, 0, s, g.z, R, n, p.ld, c0, targets, g.live, g.counts, counted, weight, g.top,
+                         g.sum, g.inv);
     }
     if (dx) gemm_split_kc(R, H, n, g.z, p.ld, W + c0, (int)ld_w, to, ld_to, s, c0 > 0, p.dx_slices, (size_t)R * H);
     if (dW) enqueue_dw(x, ld_x, g.z, p.ld, R, H, n, dW + c0, ld_dw, p, g, s);
@@ -1145,12 +1167,14 @@ __global__ __launch_bounds__(256) void ce_weights16(const T* __restrict__ W, int
 }
 
 // Logits of a tile of classes (m) and rows (n). GRAD false: every row's largest logit and sum of exponentials over the
-// classes of a wavefront, to part[class / kPart][row], and the target's logit. GRAD true: dz to G[row][class].
+// classes of a wavefront but the target, to part[class / kPart][row], and the target's logit. GRAD true: dz to
+// G[row][class], from every row's largest logit, 1 / s and o / s.
 template <class T, bool GRAD, int TILE>
 __global__ __launch_bounds__(gemm16::Shape<TILE>::kThreads, 2) void ce_logits16(
     const T* __restrict__ W, int64_t ldw, const T* __restrict__ X, int Hp, int stages, int c0, int C, int R, int Rp,
     int tiles_m, int tiles_n, const int32_t* __restrict__ pos, const int32_t* __restrict__ target,
-    float2* __restrict__ part, float* __restrict__ at_target, const float* __restrict__ lse, const float* __restrict__ w,
+    float2* __restrict__ part, float* __restrict__ at_target, const float* __restrict__ tops,
+    const float* __restrict__ inv, const float* __restrict__ rest, const float* __restrict__ w,
     const float* __restrict__ ref, T* __restrict__ G, int64_t ldg) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const gemm16::Tiles t = gemm16::tile_of(tiles_m, tiles_n, 1);
@@ -1163,13 +1187,18 @@ __global__ __launch_bounds__(gemm16::Shape<TILE>::kThreads, 2) void ce_logits16(
   const int n0 = t.n * TILE + z.n_of_wave() + l % 16;
   // what the rows need at the end is asked for now
   int32_t tgt[S::kB];
-  float top[S::kB], k[S::kB];
+  float top[S::kB], k[S::kB], kt[S::kB];  // factors of the exponentials, the target's dz
 #pragma unroll
   for (int b = 0; b < S::kB; ++b) {
     tgt[b] = target[n0 + 16 * b];
     if (GRAD) {
-      top[b] = tgt[b] >= 0 ? lse[n0 + 16 * b] : 0.0f;
-      k[b] = tgt[b] >= 0 ? w[n0 + 16 * b] / *ref * kRaise<T> : 0.0f;
+      top[b] = k[b] = kt[b] = 0.0f;
+      if (tgt[b] >= 0) {
+        const float all = w[n0 + 16 * b] / *ref * kRaise<T>;
+        top[b] = tops[n0 + 16 * b];
+        k[b] = all * inv[n0 + 16 * b];
+        kt[b] = -all * rest[n0 + 16 * b];
+      }
     }
   }
   z.run(W, ldw, t.m * TILE, X, Hp, t.n * TILE, 0, stages, smem);
@@ -1193,7 +1222,10 @@ __global__ __launch_bounds__(gemm16::Shape<TILE>::kThreads, 2) void ce_logits16(
         for (int a = 0; a < S::kA; ++a)
 #pragma unroll
           for (int v = 0; v < 4; ++v)
-            if (at == 16 * a + 4 * g + v) at_target[n] = z.acc[a][b][v];
+            if (at == 16 * a + 4 * g + v) {
+              at_target[n] = z.acc[a][b][v];
+              z.acc[a][b][v] = -INFINITY;
+            }
       }
       float m = -INFINITY;
 #pragma unroll
@@ -1218,8 +1250,8 @@ __global__ __launch_bounds__(gemm16::Shape<TILE>::kThreads, 2) void ce_logits16(
         T d[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const float p = __builtin_amdgcn_exp2f((z.acc[a][b][v] - top[b]) * kLog2e);
-          d[v] = from_float<T>(live ? k[b] * (p - (here && at == 16 * a + 4 * g + v ? 1.0f : 0.0f)) : 0.0f);
+          const float p = __builtin_amdgcn_exp2f((z.acc[a][b][v] - top[b]) * kLog2e) * k[b];
+          d[v] = from_float<T>(!live ? 0.0f : here && at == 16 * a + 4 * g + v ? kt[b] : p);
         }
         *reinterpret_cast<uint2*>(G + (size_t)n * ldg + m0 + 16 * a + 4 * g) = __builtin_bit_cast(uint2, d);
       }
@@ -1227,12 +1259,13 @@ __global__ __launch_bounds__(gemm16::Shape<TILE>::kThreads, 2) void ce_logits16(
   }
 }
 
-// Every row's log-sum-exp and loss from the parts of its classes; the weighted losses of a block in float64. A block takes
-// 32 rows, 32 threads share a row's parts.
+// Every row's largest logit, 1 / s, o / s and loss from the parts of its classes; the weighted losses of a block in
+// float64. A block takes 32 rows, 32 threads share a row's parts.
 __global__ __launch_bounds__(1024) void ce_join16(const float2* __restrict__ part, int parts, int R, int Rp,
                                                   const int32_t* __restrict__ pos, const int32_t* __restrict__ row_of,
                                                   const float* __restrict__ at_target, const float* __restrict__ w,
-                                                  float* __restrict__ lse, float* __restrict__ row_loss,
+                                                  float* __restrict__ top, float* __restrict__ inv,
+                                                  float* __restrict__ rest, float* __restrict__ row_loss,
                                                   double* __restrict__ losses) {
   __shared__ float2 all[32][33];
   const int x = threadIdx.x % 32, y = threadIdx.x / 32;
@@ -1258,9 +1291,16 @@ __global__ __launch_bounds__(1024) void ce_join16(const float2* __restrict__ par
     for (int k = 1; k < 32; ++k) add(all[k][x].x, all[k][x].y);
     double weighted = 0.0;
     if (r < pos[R]) {
-      const float log_sum = logf(s);
-      lse[r] = m + log_sum;
-      const float loss = (m - at_target[r]) + log_sum;
+      const float zt = at_target[r];
+      float over;
+      const float others = m;
+      m = fmaxf(m, zt);
+      const float from = m > -INFINITY ? m : 0.0f;
+      s *= expf(others - from);
+      const float loss = finish_row(m, s, zt, over);
+      top[r] = from;
+      inv[r] = over;
+      rest[r] = s * over;
       if (row_loss) row_loss[row_of[r]] = loss;
       weighted = (double)w[r] * (double)loss;
     }
@@ -1454,7 +1494,7 @@ struct Workspace16 {
   int32_t *flags, *pos, *temp, *target, *row_of;
   int64_t* total;
   uint16_t *X, *W, *G;
-  float *w, *at_target, *lse, *ref, *dX, *dW;
+  float *w, *at_target, *top, *inv, *rest, *ref, *dX, *dW;
   float2* part;
   double* parts;
   size_t bytes;
@@ -1473,7 +1513,9 @@ Workspace16 carve16(void* ws, int R, int H, int C, bool grad, const Plan16& p) {
   g.row_of = c.take<int32_t>(p.Rp);
   g.w = c.take<float>(p.Rp);
   g.at_target = c.take<float>(p.Rp);
-  g.lse = c.take<float>(p.Rp);
+  g.top = c.take<float>(p.Rp);
+  g.inv = c.take<float>(p.Rp);
+  g.rest = c.take<float>(p.Rp);
   g.ref = c.take<float>(1);
   g.parts = c.take<double>(p.Rp / 32);
   g.part = c.take<float2>(p.parts * p.Rp);
@@ -1528,18 +1570,19 @@ void run16(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, int
     weights(c0, n);
     hipLaunchKernelGGL((ce_logits16<T, false, TILE>), dim3(gemm16::grid_of(tiles_m, tiles_n, 1)), block, S::kLds, s, w, ldw,
                        X, p.Hp, stages_h, c0, C, R, p.Rp, tiles_m, tiles_n, g.pos, g.target, g.part, g.at_target, nullptr,
-                       nullptr, nullptr, (T*)nullptr, 0);
+                       nullptr, nullptr, nullptr, nullptr, (T*)nullptr, 0);
   }
   hipLaunchKernelGGL(ce_join16, dim3((unsigned)(p.Rp / 32)), dim3(1024), 0, s, g.part, padded(C, TILE) / kPart<TILE>, R, p.Rp,
-                     g.pos, g.row_of, g.at_target, g.w, g.lse, row_loss, g.parts);
+                     g.pos, g.row_of, g.at_target, g.w, g.top, g.inv, g.rest, row_loss,
+                     g.parts);
   if (!dx || p.direct) hipLaunchKernelGGL(ce_total, dim3(1), dim3(256), 0, s, g.parts, p.Rp / 32, loss);
   if (!dx && !dW) return;
   for (int c0 = 0; c0 < C; c0 += p.width) {
     const int n = std::min(p.width, C - c0), tiles_m = (n + TILE - 1) / TILE;
     if (p.pieces > 1) weights(c0, n);
     hipLaunchKernelGGL((ce_logits16<T, true, TILE>), dim3(gemm16::grid_of(tiles_m, tiles_n, 1)), block, S::kLds, s, w, ldw,
-                       X, p.Hp, stages_h, c0, C, R, p.Rp, tiles_m, tiles_n, g.pos, g.target, nullptr, nullptr, g.lse, g.w,
-                       g.ref, G, (int64_t)p.width);
+                       X, p.Hp, stages_h, c0, C, R, p.Rp, tiles_m, tiles_n, g.pos, g.target, nullptr, nullptr, g.top, g.inv,
+                       g.rest, g.w, g.ref, G, (int64_t)p.width);
     if (dx) {
       const int stages = tiles_m * (TILE / gemm16::kK), per = (stages + p.dx_slices - 1) / p.dx_slices;
       hipLaunchKernelGGL((ce_dx16<T, TILE>), dim3(gemm16::grid_of(tiles_h, tiles_n, p.dx_slices)), block, S::kLds, s, w, ldw,

@@ -10,7 +10,7 @@
 // gradient of tokens that lie wholly in one; what reaches over a chunk's end is kept as partial sums, which embed_rest
 // adds up in a fixed order while it clears the rows of tokens that did not occur. Frequent tokens (a tenth of a text is one
 // token) so are the work of many blocks, and the result does not depend on which of them ends first. Sums are float32
-// over at most 128 rows, then over the chunks; a result is rounded once. 128000 rows of 131072 x 1024 float32: the lookup 139
+// over at most 128 rows, float64 over the chunks; a result is rounded once. 128000 rows of 131072 x 1024 float32: the lookup 139
 // us, the gradient 278, of which the sort 45; 8192 of 32003 x 1024 bfloat16: 6 and 30, the sort 10.
 #include <algorithm>
 
@@ -297,7 +297,8 @@ __global__ __launch_bounds__(kThreads) void embed_sum(const uint32_t* __restrict
 }
 
 // Blocks [0, jobs): a chunk and slab each, the token whose rows begin in the chunk and go on behind it, if there is one: its
-// partial sums, the wavefronts a quarter of them each. The others: rows of zeros for the tokens that did not occur
+// partial sums in float64 (a chunk has at most 128 rows, so their number grows with the token's), the wavefronts a quarter
+// of them each. The others: rows of zeros for the tokens that did not occur
 // (first[v] < 0), a wavefront kZeros tokens.
 constexpr int kZeros = 4;
 template <class T>
@@ -331,32 +332,37 @@ __global__ __launch_bounds__(kThreads) void embed_rest(const uint32_t* __restric
   const int n = (last[k] - 1) / per - c0;  // chunks behind c0
   const int share = (n + W - 1) / W;
   const int i = (slab * kWave + l) * kE<T>;
-  float y[kE<T>];
+  double y[kE<T>];
 #pragma unroll
-  for (int u = 0; u < kE<T>; ++u) y[u] = 0.0f;
-  if (w == 0) span_load<float, kE<T>>(tail + (size_t)c0 * N, i, N).to(y);
+  for (int u = 0; u < kE<T>; ++u) y[u] = 0.0;
+  if (w == 0) {
+    float x[kE<T>];
+    span_load<float, kE<T>>(tail + (size_t)c0 * N, i, N).to(x);
+#pragma unroll
+    for (int u = 0; u < kE<T>; ++u) y[u] = (double)x[u];
+  }
 #pragma unroll 8
   for (int c = c0 + 1 + w * share; c <= c0 + min(n, (w + 1) * share); ++c) {
     float x[kE<T>];
     span_load<float, kE<T>>(head + (size_t)c * N, i, N).to(x);
 #pragma unroll
-    for (int u = 0; u < kE<T>; ++u) y[u] += x[u];
+    for (int u = 0; u < kE<T>; ++u) y[u] += (double)x[u];
   }
-  __shared__ float all[W][kWave][kE<T> + 1];
+  __shared__ double all[W][kWave][kE<T> + 1];
 #pragma unroll
   for (int u = 0; u < kE<T>; ++u) all[w][l][u] = y[u];
   __syncthreads();
   if (w > 0 || i >= N) return;
   T* row = dE + (int64_t)k * ld_e;
-  float old[kE<T>];
+  float old[kE<T>], out[kE<T>];
   if (accumulate) span_load<T, kE<T>>(row, i, N).to(old);
 #pragma unroll
   for (int u = 0; u < kE<T>; ++u) {
 #pragma unroll
     for (int o = 1; o < W; ++o) y[u] += all[o][l][u];
-    y[u] = accumulate ? fmaf(y[u], scale, old[u]) : y[u] * scale;
+    out[u] = (float)(accumulate ? fma(y[u], (double)scale, (double)old[u]) : y[u] * (double)scale);
   }
-  span_store<T, kE<T>, true>(row, i, N, y);
+  span_store<T, kE<T>, true>(row, i, N, out);
 }
 
 struct GradPlan {

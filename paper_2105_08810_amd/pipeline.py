@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import math
 from dataclasses import dataclass, field
-from typing import List, Optional
+from typing import ClassVar, List, Optional
 
 import torch
 
@@ -50,9 +50,9 @@ class ReadoutRows:
     """What both kinds of network do with their readout's rows: the membrane V_out [T, B, C] read as the logits of
     every step of every sample."""
 
-    def membrane(self) -> torch.Tensor:
-        """V_out of the last forward."""
-        return self.V_out
+    def membrane(self, step: Optional[int] = None) -> torch.Tensor:
+        """V_out of the last forward, or its rows [B, C] of one step."""
+        return self.V_out if step is None else self.V_out[step]
 
     def record(self, K: int, tau: float = 1.0) -> Record:
         """The forward's answers as a teacher's record."""
@@ -62,8 +62,7 @@ class ReadoutRows:
     def draw(self, u: torch.Tensor, temperature=None, top_k=None, top_p=None, min_p=None, step: Optional[int] = None):
         """One class per sample and step drawn from uniforms u [T, B], or at one step from u [B]; settings as in
         snn.readout_sample. Returns (classes int32, log-probabilities, numbers of classes kept)."""
-        rows = self.membrane() if step is None else self.membrane()[step]
-        return snn.readout_sample(rows, u, temperature, top_k, top_p, min_p)
+        return snn.readout_sample(self.membrane(step), u, temperature, top_k, top_p, min_p)
 
     def readout_distilled(self, distill: Distill, dense=False):
         """readout() with the distillation's gradient added: (CSR of every entry of V_out, eps at them, cross-entropy,
@@ -119,6 +118,8 @@ class Network(ReadoutRows):
     loss_mode: int  # 0 = max over t, 1 = sum over t
     theta: float = 1.0
     beta: float = 100.0
+    kClasses: ClassVar[int] = 4096  # that snn_lif_forward takes
+    kSliceValues: ClassVar[int] = 1 << 28
     embed_scale: float = 1.0  # tokens only
     norm_in: Optional[Norm] = None  # tokens only
     # forward state
@@ -254,18 +255,42 @@ class Network(ReadoutRows):
                                      self.S[0], top, self.alpha_out, None if b_th is None else self.bits[0])
         return top
 
-    def membrane(self) -> torch.Tensor:
-        """V_out of the last forward; with a target at every step it is formed at each call, from the spikes and W_out as
-        they are now: a graph's replay renews the spikes without any of this class's code, so no earlier V_out is
-        handed out again."""
+    def membrane(self, step: Optional[int] = None) -> torch.Tensor:
+        """V_out of the last forward, or its rows [B, C] of one step. With a target at every step they are formed at each
+        call, from the spikes and W_out as they are now: a graph's replay renews the spikes without any of this class's
+        code, so no earlier V_out is handed out again. The library's forward takes kClasses classes at a time; for one
+        step's rows also samples whose values up to that step are at most kSliceValues (or one sample), so that they need
+        no memory for T B C values. All steps together are T B C values, below 2^31."""
         if not self.S:
             raise ValueError("membrane() reads a forward's spikes: call forward() first")
-        if self.every_step:
-            T, B, C = self.T, self.B, self.W_out.shape[1]
-            self.V_out = torch.empty((T, B, C), dtype=torch.float32, device=self.X.device)
-            S_out = torch.empty((T, B, C), dtype=torch.uint8, device=self.X.device)
-            snn.snn_lif_forward(self.S[-1], self.W_out, T, B, self.W_out.shape[0], C, self.alpha_out, INF, self.V_out, S_out)
-        return self.V_out
+        if not self.every_step:
+            return self.V_out if step is None else self.V_out[step]
+        T, B, C = self.T, self.B, self.W_out.shape[1]
+        dev, n = self.X.device, min(C, self.kClasses)
+        if step is None:
+            if T * B * C >= 1 << 31:
+                raise ValueError(f"V_out of {T} x {B} x {C} is too large to be formed at once: name a step")
+            out = self.V_out = torch.empty((T, B, C), dtype=torch.float32, device=dev)
+            steps, rows = T, B
+        else:
+            if not -T <= step < T:
+                raise IndexError(f"step {step} of {T}")
+            out = torch.empty((B, C), dtype=torch.float32, device=dev)
+            steps = step % T + 1
+            rows = min(B, max(1, self.kSliceValues // (steps * n)))
+        for c in range(0, C, n):
+            W = self.W_out if n == C else self.W_out[:, c:c + n].contiguous()
+            k = W.shape[1]
+            for b in range(0, B, rows):
+                S = self.S[-1][:steps] if rows == B else self.S[-1][:steps, b:b + rows].contiguous()
+                m = S.shape[1]
+                direct = step is None and n == C
+                V = out if direct else torch.empty((steps, m, k), dtype=torch.float32, device=dev)
+                S_out = torch.empty((steps, m, k), dtype=torch.uint8, device=dev)
+                snn.snn_lif_forward(S, W, steps, m, W.shape[0], k, self.alpha_out, INF, V, S_out)
+                if not direct:
+                    out[..., b:b + m, c:c + k] = V if step is None else V[-1]
+        return out
 
     def readout(self, dense=False):
         """Readout CSR, eps at its entries, loss (device scalar) and, if asked, dL/dV_out densely."""

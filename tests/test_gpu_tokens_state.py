@@ -5,7 +5,7 @@ import copy
 import pytest
 import torch
 
-from paper_2105_08810_amd import pipeline
+from paper_2105_08810_amd import pipeline, snn
 from test_gpu_tokens_pipeline import B_TH, network
 
 pytestmark = pytest.mark.gpu
@@ -86,3 +86,47 @@ def test_norm_gradients_of_a_replay():
     kept = [t.clone() for t in one]
     two = net.train_step(opt, B_TH)["grads"]
     assert all(torch.equal(p, q) for p, q in zip(one, kept)) and not torch.equal(one[-1], two[-1])
+
+
+@pytest.mark.parametrize("per", [1, 3, 1 << 28])
+def test_one_step_by_slices(per, monkeypatch):
+    """One step's rows are those of the whole membrane, to the bit, however many samples are formed together."""
+    net = network(T=30, B=7, every=True, seed=11, sizes=(64, 48), C=130)
+    net.forward()
+    want = net.membrane()
+    u = torch.linspace(0.05, 0.95, 7, device="cuda")
+    for step in (0, 1, 17, 29, -1):
+        monkeypatch.setattr(pipeline.Network, "kSliceValues", per * 130 * (step % 30 + 1))
+        assert torch.equal(net.membrane(step), want[step])
+        assert all(torch.equal(p, q) for p, q in zip(net.draw(u, step=step), snn.readout_sample(want[step], u)))
+
+
+def test_more_classes_than_one_forward_takes():
+    """5000 classes: the membrane is that of either half of them, and records and draws read it."""
+    net = network(T=15, B=4, every=True, seed=13, C=5000)
+    net.forward()
+    V = net.membrane()
+    half = copy.copy(net)
+    for c in (slice(0, 2500), slice(2500, 5000)):
+        half.W_out = net.W_out[:, c].contiguous()
+        assert torch.equal(half.membrane(), V[..., c])
+    assert torch.equal(net.membrane(9), V[9])
+    rec = net.record(3)
+    assert torch.equal(rec.vals[..., 0], V.amax(2))
+    cls, _, _ = net.draw(torch.full((15, 4), 0.5, device="cuda"), torch.zeros((15, 4), device="cuda"))
+    assert torch.equal(V.gather(2, cls.long()[..., None])[..., 0], V.amax(2))
+
+
+def test_draw_over_a_large_vocabulary():
+    """A step of 500 x 256 samples over 32003 classes, whose membrane would have 4.1e9 values."""
+    net = network(T=500, B=256, V=50, sizes=(64,), C=32003, every=True, seed=12)
+    net.forward()
+    cls, logp, _ = net.draw(torch.full((256,), 0.5, device="cuda"), torch.zeros(256, device="cuda"), step=250)
+    z = net.trace_out[250].double() @ net.W_out.double()
+    best = z.max(1)
+    # the membrane is a sum of 250 steps of at most 64 spikes' rows, each rounded: 2^-24 of its absolute sum a step
+    tol = 500 * 2.0 ** -24 * float((net.trace_out[250].double() @ net.W_out.double().abs()).max())
+    assert bool((z.gather(1, cls.long()[:, None])[:, 0] >= best.values - 2 * tol).all())
+    assert bool(torch.isfinite(logp).all())
+    with pytest.raises(ValueError, match="name a step"):
+        net.draw(torch.zeros((500, 256), device="cuda"))

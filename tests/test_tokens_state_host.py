@@ -63,3 +63,45 @@ def test_norm_state_is_in_buffers(monkeypatch):
     net._backward_tokens(None, None)
     assert [g.data_ptr() for g in net.norm_grads] == first and keep is not None
     assert all(p == tuple(t.data_ptr() for t in seen["forward"][0]) for p in seen["backward"])
+
+
+def test_one_step_of_a_large_vocabulary(monkeypatch):
+    """One step's rows are formed for slices of the samples; all steps together are refused where they cannot be."""
+    formed = []
+
+    def forward(s_in, W, T, B, N_in, N_out, alpha, theta, V, S, trace=None):
+        formed.append((T, B, N_out))
+        assert s_in.is_contiguous() and s_in.shape == (T, B, N_in) and V.shape == S.shape == (T, B, N_out)
+        V[-1] = s_in[-1, :, :1].float()
+
+    monkeypatch.setattr(snn, "snn_lif_forward", forward)
+    net = network(T=6, B=5)
+    net.allocate()
+    net.S[-1].copy_(torch.arange(6 * 5).view(6, 5, 1).expand(6, 5, 5))
+    assert torch.equal(net.membrane(3), torch.arange(15.0, 20.0)[:, None].expand(5, 2)) and formed == [(4, 5, 2)]
+    formed.clear()
+    monkeypatch.setattr(pipeline.Network, "kSliceValues", 17)  # two samples of 4 x 2 values
+    assert torch.equal(net.membrane(3), torch.arange(15.0, 20.0)[:, None].expand(5, 2))
+    assert formed == [(4, 2, 2), (4, 2, 2), (4, 1, 2)]
+    formed.clear()
+    monkeypatch.setattr(pipeline.Network, "kSliceValues", 1)  # never less than a sample
+    assert torch.equal(net.membrane(-1), torch.arange(25.0, 30.0)[:, None].expand(5, 2)) and formed == [(6, 1, 2)] * 5
+    formed.clear()
+    monkeypatch.setattr(pipeline.Network, "kClasses", 3)  # classes by slices too
+    net.W_out = torch.zeros((5, 8))
+    monkeypatch.setattr(pipeline.Network, "kSliceValues", 48)  # four samples of 4 x 3 values
+    assert torch.equal(net.membrane(3), torch.arange(15.0, 20.0)[:, None].expand(5, 8))
+    assert formed == [(4, 4, 3), (4, 1, 3), (4, 4, 3), (4, 1, 3), (4, 4, 2), (4, 1, 2)]
+    formed.clear()
+    assert torch.equal(net.membrane()[-1], torch.arange(25.0, 30.0)[:, None].expand(5, 8))
+    assert formed == [(6, 5, 3), (6, 5, 3), (6, 5, 2)]
+    for step in (6, -7):
+        with pytest.raises(IndexError):
+            net.membrane(step)
+    net.W_out = torch.empty((5, 1), device="meta").expand(5, 1 << 27)
+    formed.clear()
+    with pytest.raises(ValueError, match="name a step"):
+        net.membrane()
+    with pytest.raises(ValueError, match="name a step"):
+        net.record(3)
+    assert not formed

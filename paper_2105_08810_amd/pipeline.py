@@ -103,8 +103,10 @@ class Network(ReadoutRows):
 
     X int32 [T, B] is a sequence of tokens: the first layer's weights are an embedding [vocabulary, N], a token is one
     input spike of its row (the same as X of one-hot spikes, which are never formed), and the layer's currents are
-    embed_scale times the picked rows, through norm_in where given. A token outside the vocabulary is no spike. The last
-    step's tokens reach no membrane, as the last step's spikes do not.
+    embed_scale times the picked rows, through norm_in where given. A token outside the vocabulary is no spike: its row is
+    zeros and trains nothing of the embedding. Behind norm_in a row of zeros is beta, as the norm of any row of equal values
+    is: such steps drive the layer with beta and count in beta's gradient. The last step's tokens reach no membrane, as the
+    last step's spikes do not.
 
     labels int32 [T, B] are a target at every step (-1: none there): the loss is the mean cross-entropy over the steps
     that have one, on the readout's membrane of that step, which is its input trace times W_out. Neither this membrane
@@ -145,6 +147,9 @@ class Network(ReadoutRows):
     def __post_init__(self):
         if self.norm_in is not None and not self.tokens:
             raise ValueError("norm_in is a norm of tokens' currents: X must be int32 [T, B]")
+        if self.norm_in is not None and not 0.0 < self.norm_in.eps < INF:
+            raise ValueError("norm_in.eps must be positive: a row of equal values (a token outside the vocabulary) has no "
+                             "deviation to divide by")
 
     @property
     def tokens(self) -> bool:

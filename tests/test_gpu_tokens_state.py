@@ -130,3 +130,21 @@ def test_draw_over_a_large_vocabulary():
     assert bool(torch.isfinite(logp).all())
     with pytest.raises(ValueError, match="name a step"):
         net.draw(torch.zeros((500, 256), device="cuda"))
+
+
+def test_tokens_outside_the_vocabulary():
+    """Without a norm they are no spike; behind it their current is beta."""
+    for norm in (False, True):
+        net = network(T=10, every=True, norm=norm, seed=14)
+        net.X.fill_(-1)
+        net.X[4, 2] = 10 ** 6
+        out = net.train_step(pipeline.Adam(net.params(), lr=1e-3), B_TH)
+        assert not bool(out["grads"][0].any())
+        net = network(T=10, every=True, norm=norm, seed=14)
+        net.X.fill_(-1)
+        net.forward()
+        V, S = net.V[0], net.S[0].float()
+        for t in range(9):
+            current = net.norm_in.beta.double() if norm else 0.0
+            want = 0.9 * V[t].double() + current - S[t].double()
+            assert float((V[t + 1].double() - want).abs().max()) < 4 * 2.0 ** -24 * (1 + float(V.abs().max()))

@@ -105,3 +105,12 @@ def test_one_step_of_a_large_vocabulary(monkeypatch):
     with pytest.raises(ValueError, match="name a step"):
         net.record(3)
     assert not formed
+
+
+@pytest.mark.parametrize("eps", [0.0, -1e-5, float("inf"), float("nan")])
+def test_norm_needs_eps(eps):
+    """With eps 0 a padded step's currents would be NaN."""
+    with pytest.raises(ValueError, match="eps"):
+        pipeline.Network(X=torch.zeros((4, 3), dtype=torch.int32), Ws=[torch.zeros((7, 5))], W_out=torch.zeros((5, 2)),
+                         alphas=[0.9], alpha_out=0.9, labels=torch.zeros((4, 3), dtype=torch.int32), loss_mode=1,
+                         norm_in=pipeline.Norm(torch.ones(5), torch.zeros(5), eps))

@@ -303,8 +303,15 @@ class Network(ReadoutRows):
             raise ValueError("a target at every step: use readout_steps()")
         return snn.readout_ce(self.V_out, self.labels, self.loss_mode, dense=dense)
 
+    def readout_distilled(self, distill: Distill, dense=False):
+        if self.every_step:
+            raise ValueError("distillation beside a target at every step is not offered")
+        return super().readout_distilled(distill, dense)
+
     def readout_steps(self):
         """With a target at every step: (gradient by the readout's input trace [T, B, N], dW_out, loss)."""
+        if not self.every_step:
+            raise ValueError("one label a sample: use readout()")
         loss, _, dtrace, dW_out = snn.linear_ce(self.trace_out, self.W_out, self.labels)
         return dtrace, dW_out, loss
 

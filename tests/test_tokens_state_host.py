@@ -114,3 +114,14 @@ def test_norm_needs_eps(eps):
         pipeline.Network(X=torch.zeros((4, 3), dtype=torch.int32), Ws=[torch.zeros((7, 5))], W_out=torch.zeros((5, 2)),
                          alphas=[0.9], alpha_out=0.9, labels=torch.zeros((4, 3), dtype=torch.int32), loss_mode=1,
                          norm_in=pipeline.Norm(torch.ones(5), torch.zeros(5), eps))
+
+
+def test_each_kind_has_its_readout():
+    """A readout of the other kind of target is refused before any device call."""
+    net = network()
+    net.allocate()
+    with pytest.raises(ValueError, match="every step"):
+        net.readout_distilled(pipeline.Distill(pipeline.Record(None, None, None)))
+    net.labels = torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="readout\\(\\)"):
+        net.readout_steps()

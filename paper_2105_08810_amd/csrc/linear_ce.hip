@@ -344,7 +344,6 @@ __global__ __launch_bounds__(256) void ce_dw(const float* __restrict__ part, int
 // (12 products of 128000 x 1024 x 112 in bf16 terms: 150 us at their nominal rate) beside reading x and writing dx (205 us);
 // measured 320 to 365.
 constexpr int kFew = 128;
-constexpr int kCountHere = 8192;  // rows up to which every block counts those with a target itself
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -425,17 +424,7 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
   __shared__ int32_t on[kRows];
   const int w = threadIdx.x / kWave, l = lane_id(), i = l % 16, g = l / 16;
   const int r0 = blockIdx.x * kRows;
-  float same = 0.0f;
-  if (!weight) {
-    if (counts) {
-      same = same_weight(counts, n_counts);
-    } else {
-      int n = 0;
-      for (int q = l; q < R; q += kWave) n += takes_part(targets, weight, q, C);
-      n = wave_sum_int(n);
-      same = n > 0 ? 1.0f / (float)n : 0.0f;
-    }
-  }
+  const float same = weight ? 0.0f : same_weight(counts, n_counts);
   bool alive = false;
   if (threadIdx.x < kRows) {
     const int q = r0 + threadIdx.x;
@@ -924,14 +913,16 @@ void run_few(const T* x, int64_t ld_x, const T* W, int64_t ld_w, int R, int H, i
     // 32 rows a wavefront read W's parts half as often; 16 where 32 would leave compute units without a block
     const bool wide = (R + 127) / 128 >= 2 * cu_count(), vec = H % 8 == 0;
     const int blocks = wide ? (R + 127) / 128 : (R + 63) / 64;
-    const int counted = weight || R <= kCountHere ? 0 : std::min(kCountParts, (R + 1023) / 1024);
+    // without weights a launch of its own counts the rows that take part (6000 x 512 x 100: 80 us, with a count in every
+    // block 100; 6000 x 200 x 10: 33, 38)
+    const int counted = weight ? 0 : std::min(kCountParts, (R + 1023) / 1024);
     if (counted)
       hipLaunchKernelGGL(ce_live, dim3((unsigned)counted), dim3(256), 0, s, targets, weight, R, C, g.live, g.counts);
     hipLaunchKernelGGL((ce_few_parts<NT>), dim3((unsigned)((H + 31) / 32)), dim3(256), 0, s, W, ld_w, H, C, g.first,
                        g.second);
     const auto few = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, x, ld_x, g.first, g.second, R, H, C, targets,
-                         weight, counted ? g.counts : nullptr, counted, row_loss, g.parts, dx, ld_dx, dW ? g.z : nullptr,
+                         weight, g.counts, counted, row_loss, g.parts, dx, ld_dx, dW ? g.z : nullptr,
                          p.ld, counted ? nullptr : g.live);
     };
     if (wide) few(vec ? ce_few<NT, 2, true> : ce_few<NT, 2, false>);

@@ -612,6 +612,9 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
 // LDS, in order), a row each of what follows, and every sixteenth run of 16 h of dx. Bound: latency, and W read twice a block.
 // A lane reads V = 1, 2 or 4 neighbouring classes at once, which are one element each of V tiles: class m of tile a is
 // class_of(m) + a. The last lanes' begin early where the classes end, so that some classes are formed twice, alike.
+// Few rows are 4096: us a call so and by the ways of more rows (rows x H x classes): float32 4096 x 200 x 10 40, 34; x 1024 x
+// 10 51, 76; x 200 x 100 63, 62; x 1024 x 100 94, 117; 8192 x 200 x 10 75, 34; x 1024 x 10 92, 99; x 1024 x 100 182, 136;
+// bfloat16 4096 x 200 x 10 40, 55; x 200 x 100 60, 56; x 1024 x 100 80, 78; 8192 x 1024 x 10 88, 92; x 200 x 100 117, 67.
 constexpr int kFewDwRows = 4096;
 template <int NT>
 constexpr int kV = NT < 4 ? NT : 4;
@@ -1026,8 +1029,10 @@ template <int TILE>
 constexpr int kPart = gemm16::Shape<TILE>::kWaveM;
 
 // pos[r]: rows before r that take part, pos[R]: their number; ref: the largest weight. Blocks of 1024 threads: one takes up
-// to kOneBlock rows, a run of them a thread; beyond, the flags' prefix is formed by the scan and ref by a launch of its own.
-constexpr int kOneBlock = 32768;
+// to kOneBlock rows, a run of them a thread; beyond, the flags' prefix is formed by the scan and ref by a launch of its own
+// (rows x 128 x 300 bfloat16, us a call by one block and by the scan: 4096 58, 65; 8192 69, 71; 16384 92, 87; 32768 129, 106).
+constexpr int kOneBlock = 8192;
+static_assert(kOneBlock <= 32 * 1024, "a thread's rows have a bit each");
 __global__ __launch_bounds__(1024) void ce_places(const int32_t* __restrict__ targets, const float* __restrict__ weight,
                                                   int R, int C, int32_t* __restrict__ pos, float* __restrict__ ref) {
   __shared__ int count[1024 / kWave];

@@ -142,3 +142,11 @@ def test_pieces_in_16_bits(dtype, R, H, C):
 def test_widths_of_norm(dtype, N):
     base.test_layer_norm(dtype, dtype, 3, N, "both", 0, 0)
     base.test_layer_norm(dtype, dtype, 2, N, "gamma", 3, 1)
+
+
+# rows on both sides of the line between one block's places and the scan's
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("R", [8192, 8193, 20000, 32769])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_places(dtype, R, weighted):
+    check(R, 8, 300, dtype, dead=0.3, weighted=weighted)

@@ -619,7 +619,7 @@ snn_status snn_embed_grad(const int32_t* ids, int64_t R, const void* dout, int d
  *   y        R rows of N values of y_dtype (written)
  *   mean, rstd  float32 [R] (written unless NULL), what the backward pass takes
  * R up to 2^31 - 1, N up to 2^20. A row of one value has y = beta; a row whose variance and eps are both 0 has rstd = inf
- * and y NaN.
+ * and y NaN. Sums and squares are float32: a row whose squared deviations add up to 2^128 or more has rstd = 0 and y = beta.
  */
 snn_status snn_layer_norm(const void* x, int x_dtype, int64_t R, int N, int64_t ld_x, const float* gamma,
                           const float* beta, float eps, void* y, int y_dtype, int64_t ld_y, float* mean, float* rstd,
@@ -641,8 +641,10 @@ snn_status snn_layer_norm_grad(const void* dy, int y_dtype, int64_t ld_dy, const
                                void* stream);
 
 /*
- * Softmax cross entropy of linear logits z = x W against one target a row, with both gradients; the R x C logits are
- * never in memory together. A readout without threshold is such a product: V_out = trace W_out.
+ * Softmax cross entropy of linear logits z = x W against one target a row, with both gradients. The logits, or their
+ * gradient in their place, are formed for a piece of the classes at a time, of at most max(2^27, 256 R) values in float32
+ * and max(2^28, 256 R) in 16 bits; what is smaller is one piece. A readout without threshold is such a product: V_out =
+ * trace W_out.
  *   x        R rows of H values of dtype
  *   W        H rows of C values of dtype
  *   targets  int32 [R]; a row whose target is outside [0,C) takes no part: whatever it holds, its loss and gradient are 0
@@ -653,12 +655,14 @@ snn_status snn_layer_norm_grad(const void* dy, int y_dtype, int64_t ld_dy, const
  *   dx       R rows of H values of dtype (written unless NULL): weight_r (softmax(z_r) - onehot) W^T
  *   dW       H rows of C values of dtype (written unless NULL): x^T (weight_r (softmax(z_r) - onehot))
  * In 16 bits (but for at most 128 classes and 4096 rows) weight_r (softmax(z_r) - onehot) is rounded to dtype as a share
- * of the largest weight, and shares below 2^-126 (bfloat16) or 2^-40 (float16) of it count as 0. In float32 with at most
- * 128 classes and more than 4096 rows values of W from 2^97 on overflow in dx. What is not finite in x may make its row's
- * loss and gradients NaN, in W every row's.
+ * of the largest weight, and shares below 2^-126 (bfloat16) or 2^-40 (float16) of it count as 0; a row's rounded terms need
+ * not add up to 0, which shows in dx where W's columns have a large part in common. In float32 with at most 128 classes and
+ * more than 4096 rows values of W from 2^97 on overflow in dx. What is not finite in x may make its row's loss and gradients
+ * NaN, in W every row's.
  * R up to 2^24, H up to 2^16, C up to 2^20, distances of rows up to 2^31 - 1; larger: SNN_ERR_UNSUPPORTED. The workspace
- * query takes whether a gradient is wanted. The workspace grows with R H, with R times a piece of the classes (bounded)
- * and in 16 bits with R C / 8 bytes.
+ * query takes whether a gradient is wanted. The workspace holds a piece; in 16 bits copies of x and of a piece's columns of
+ * W, padded to whole tiles of 128 or 256, and R C / 8 bytes of row sums; and, where a product has fewer tiles than the card
+ * takes at once, float32 partial results of it, up to 64 of the logits, of dx or of a piece's columns of dW.
  */
 size_t snn_linear_ce_workspace(int dtype, int64_t R, int H, int C, int grad);
 snn_status snn_linear_ce(const void* x, const void* W, int dtype, int64_t R, int H, int C, int64_t ld_x, int64_t ld_w,

@@ -656,9 +656,8 @@ snn_status snn_layer_norm_grad(const void* dy, int y_dtype, int64_t ld_dy, const
  *   dW       H rows of C values of dtype (written unless NULL): x^T (weight_r (softmax(z_r) - onehot))
  * In 16 bits (but for at most 128 classes and 4096 rows) weight_r (softmax(z_r) - onehot) is rounded to dtype as a share
  * of the largest weight, and shares below 2^-126 (bfloat16) or 2^-40 (float16) of it count as 0; a row's rounded terms need
- * not add up to 0, which shows in dx where W's columns have a large part in common. In float32 with at most 128 classes and
- * more than 4096 rows values of W from 2^97 on overflow in dx. What is not finite in x may make its row's loss and gradients
- * NaN, in W every row's.
+ * not add up to 0, which shows in dx where W's columns have a large part in common. What is not finite in x may make its
+ * row's loss and gradients NaN, in W every row's.
  * R up to 2^24, H up to 2^16, C up to 2^20, distances of rows up to 2^31 - 1; larger: SNN_ERR_UNSUPPORTED. The workspace
  * query takes whether a gradient is wanted. The workspace holds a piece; in 16 bits copies of x and of a piece's columns of
  * W, padded to whole tiles of 128 or 256, and R C / 8 bytes of row sums; and, where a product has fewer tiles than the card

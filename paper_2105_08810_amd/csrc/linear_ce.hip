@@ -347,7 +347,6 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-constexpr float kDzUp = 0x1p30f;  // dz / w enters the second product raised, so that small probabilities keep their bits
 
 __device__ __forceinline__ void split8(const float (&x)[8], uint4 (&part)[3]) {
   uint32_t w[3][4];
@@ -499,8 +498,10 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
   }
   // lane (i, g) holds rows i of the wavefront's tiles, classes 16 a + 4 g + v
   double total = 0.0;
+  // dz / w enters the second product raised by the power of two that brings the row's largest, the others' share, to [1, 2)
+  // (of a share below 2^-126: to below 2): its parts keep their bits, and products overflow where dx would
   uint4 fz[RT][S][3];
-  float k[RT];
+  float k[RT], down[RT];
 #pragma unroll
   for (int b = 0; b < RT; ++b) {
     const int at = 16 * (RT * w + b) + i, r = r0 + at;
@@ -538,6 +539,9 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
     if (g == 0 && r < R && row_loss) row_loss[r] = loss;
     if (g == 0 && mine) total += (double)k[b] * (double)loss;
     if (!dx && !dz) continue;
+    const uint32_t exponent = min(max(__float_as_uint(rest_of) >> 23 & 255u, 1u), 253u);
+    const float up = __uint_as_float((254u - exponent) << 23);
+    down[b] = __uint_as_float(exponent << 23);
 #pragma unroll
     for (int step = 0; step < S; ++step) {
       float d[8];
@@ -555,7 +559,7 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
               f32x4{k[b] * d[4 * half], k[b] * d[4 * half + 1], k[b] * d[4 * half + 2], k[b] * d[4 * half + 3]};
       }
 #pragma unroll
-      for (int u = 0; u < 8; ++u) d[u] *= kDzUp;
+      for (int u = 0; u < 8; ++u) d[u] *= up;
       split8(d, fz[b][step]);
     }
   }
@@ -599,7 +603,7 @@ __global__ __launch_bounds__(256, 2) void ce_few(const float* __restrict__ x, in
       for (int half = 0; half < 2; ++half) {
         float o[4];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) o[v] = mine ? (d[half][b][v] + e[half][b][v]) * (1.0f / kDzUp) * k[b] : 0.0f;
+        for (int v = 0; v < 4; ++v) o[v] = mine ? (d[half][b][v] + e[half][b][v]) * down[b] * k[b] : 0.0f;
         store_in<float, 4>(dx + (int64_t)r * ld_dx, min(h0 + 16 * half + 4 * g, H), H, o);
       }
     }

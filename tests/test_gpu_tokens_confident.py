@@ -76,3 +76,45 @@ def test_confident_rows(dtype, R, K, H, C, offset, weighted):
     tol = tol + u * (want.abs() + tol) + least
     bad = (dW[1:1 + K].double() - want).abs() > tol
     assert not bool(bad.any()), (int(bad.sum()), float(((dW[1:1 + K].double() - want).abs() / tol).max()))
+
+
+@pytest.mark.parametrize("R,C", [(300, 10), (5000, 10), (5000, 100), (66000, 120), (300, 300)])
+@pytest.mark.parametrize("up", [0, 60, 100, 124])
+def test_range_in_float32(R, C, up):
+    """x down and W up by the same power of two give the same logits and loss; dx goes up with W and dW down with x, in every
+    way alike, as long as they are in float32's range."""
+    g = torch.Generator(device="cuda").manual_seed(C)
+    H = 24
+    x = torch.randn((R, H), generator=g, device="cuda")
+    W = torch.randn((H, C), generator=g, device="cuda").clamp_(-4, 4) * 0.4
+    t = torch.randint(-1, C, (R,), generator=g, device="cuda").to(torch.int32)
+    loss, row_loss, dx, dW = snn.linear_ce(x, W, t)
+    # parts of three bfloat16 keep all bits of numbers down to 2^-110: x is taken down by that much less
+    down = min(up, 80)
+    x2, W2 = x * 2.0 ** -down, W * 2.0 ** up
+    if up > down:  # and W's hidden rows in turn: half of them carry the power, the others none
+        W2 = torch.cat([W * 2.0 ** down, torch.full((1, C), 2.0 ** up, device="cuda")])
+        x2 = torch.cat([x2, torch.zeros((R, 1), device="cuda")], 1)
+    got = snn.linear_ce(x2, W2, t)
+    assert float((got[1] - row_loss).abs().max()) < 4 * (H + 40) * U * float(row_loss.max())
+    scale = 2.0 ** down
+    for p, q in ((got[2][:, :H] / scale, dx), (got[3][:H] * scale, dW)):
+        assert bool(torch.isfinite(p).all())
+        assert float((p.double() - q.double()).norm()) < 2e-6 * float(q.double().norm())
+    if up > down:  # a row's dz add up to 0 but for their roundings, times 2^up
+        assert bool(torch.isfinite(got[2]).all())
+        assert float(got[2][:, H].abs().max()) <= 2.0 ** up * (C + 40) * 4 * U / int((t >= 0).sum())
+
+
+@pytest.mark.parametrize("R,C", [(300, 10), (5000, 10), (5000, 100), (66000, 120), (300, 300)])
+@pytest.mark.parametrize("margin", [20.0, 60.0, 80.0])
+def test_rows_next_to_certain(R, C, margin):
+    """Rows whose others' share is far below a float32's last bit of 1: their gradients keep its relative precision."""
+    x, W, t, kind, share, row = case(R, 8, 9, C, "f32", 4.0, margin, C)
+    loss, row_loss, dx, dW = snn.linear_ce(x, W, t, torch.ones(R, device="cuda"))
+    n = torch.bincount(kind, minlength=8).double()[:, None]
+    rel = (2 + 2 * (margin + 4) * 2 + C / 64 + 10 + 2 * (int(n.max()) + 8)) * U
+    assert bool(((dW[1:].double() - n * share).abs() <= rel * n * share.abs() + 1e-43).all())
+    want = share @ W.double().T
+    tol = (rel + 2 * (C + 8) * U) * (share.abs() @ W.double().abs().T)
+    assert bool(((dx.double() - want[kind]).abs() <= tol[kind] + 1e-43).all())
